@@ -520,6 +520,101 @@ BT_API bt_status bt_op_attention_bwd(const float* qkv, const float* qkv_split, c
                                      int32_t H, float* dqkv, float* dqkv_split, void* scratch, size_t scratch_bytes,
                                      uint32_t flags, void* stream);
 
+/* ----------------------------------------------------------------------------------
+ * The attention sublayer beyond plain causal attention: rotary positions, modified scores, dropout.
+ * The paper's model uses none of them (learned positions, causal softmax, no dropout); they stand
+ * beside its attention and residual kernels for models that do, in the same layouts.  All calls are
+ * asynchronous, allocate nothing, keep nothing between calls and can be captured into a graph.  All
+ * arrays of a call lie on the current device, `stream` with them.
+ * -------------------------------------------------------------------------------- */
+
+/* Rotary positions on fused qkv rows x [N, 3C] (columns q | k | v, head h at columns h*d .. of each
+ * part, d = C / H a multiple of 4): in every query and key head, pair i of the first rot_dim columns
+ * turns by the angle a = pos * theta_i,
+ *     (u, w) -> mscale * (u cos a - w sin a, u sin a + w cos a),   theta_i = base^(-2 i / rot_dim),
+ * where pair i is columns (i, i + rot_dim / 2), or (2 i, 2 i + 1) when `interleaved`.  The columns from
+ * rot_dim on and the values are left as they are.  Long contexts: BT_ROPE_LINEAR divides every theta
+ * by `factor`; BT_ROPE_BY_PARTS divides only the slow pairs, theta *= g + (1 - g) / factor with g =
+ * clamp((original_len * theta / 2 pi - low) / (high - low), 0, 1): pairs that turn more than `high`
+ * times over the original length keep their speed, those below `low` are stretched (another `base`
+ * needs no scaling kind).  mscale multiplies the rotated columns (1 = a pure rotation).
+ * 2 <= rot_dim <= min(d, 128), even.  Angles are reduced in 64 bits, so positions anywhere in int32
+ * keep the accuracy of small ones.
+ *   pos      int32 [N] (nullable: row n has position n mod T; packed documents restart theirs)
+ *   y        [N, 3C], may be x itself (then only the rotated columns are touched; not with y_split)
+ *   y_split  [2][N][3C] hi/lo planes, as the attention kernels read them; y or y_split may be NULL
+ * bt_op_rope_bwd maps the gradient dy at y to the gradient dx at x (the turn by -a, times mscale). */
+enum { BT_ROPE_PLAIN = 0, BT_ROPE_LINEAR = 1, BT_ROPE_BY_PARTS = 2 };
+typedef struct {
+    int32_t rot_dim, interleaved, scaling, original_len;
+    double base, factor, low, high;
+    float mscale;
+} bt_rope_config;
+BT_API bt_status bt_op_rope_fwd(const float* x, const int32_t* pos, int64_t N, int32_t T, int32_t C, int32_t H,
+                                const bt_rope_config* rope, float* y, float* y_split, void* stream);
+BT_API bt_status bt_op_rope_bwd(const float* dy, const int32_t* pos, int64_t N, int32_t T, int32_t C, int32_t H,
+                                const bt_rope_config* rope, float* dx, float* dx_split, void* stream);
+
+/* Key spans of a packed batch: for every position the range of keys its query may read, and the range
+ * of queries that read its key.  A document is a maximal run of equal ids in `doc` (int32 [B, T];
+ * nullable: every sequence is one document); an id below zero is padding, which reads nothing and is
+ * read by nobody.  Inside its document query i reads key j when (j <= i, or j lies in the document's
+ * prefix) and i - j < window (window 0: no limit).  The prefix is the run of positions with a
+ * non-zero `prefix` mark (int32 [B, T], nullable: none) that the document begins with; its positions see
+ * one another in both directions.  `spans` (16-byte aligned, bt_op_attention_spans_bytes(B, T) bytes; 0
+ * for more than 2^21 positions or 2^30 rows) is built once per batch and serves all layers, forward and
+ * backward, until the ids change. */
+BT_API size_t bt_op_attention_spans_bytes(int32_t B, int32_t T);
+BT_API bt_status bt_op_attention_spans(const int32_t* doc, const int32_t* prefix, int32_t window, int32_t B, int32_t T,
+                                       void* spans, size_t spans_bytes, void* stream);
+
+/* How bt_op_attention_mod_* changes the scores s_ij = q_i k_j / sqrt(d):
+ *     z_ij = softcap tanh(s_ij / softcap) - slopes[h] |i - j|      (softcap 0: z_ij = s_ij - slopes[h] |i - j|)
+ * for the pairs (i, j) that `spans` allows (device, from bt_op_attention_spans for the same B and T;
+ * NULL: j <= i).  slopes: device float [H], finite (NULL: no bias); |i - j| counts positions of the
+ * sequence.  Slopes and softcap are constants: no gradient is formed for them. */
+typedef struct {
+    float softcap;
+    const float* slopes;
+    const void* spans;
+} bt_attn_mod;
+
+/* Attention with modified scores: o_i = sum_j softmax_j(z_ij) v_j, lse [B, H, T] = log sum_j exp z_ij.  A
+ * query that may read no key gets o = 0, lse = -inf and takes no part in the backward.  Layouts as in
+ * bt_op_attention_fwd / _bwd (d in {16, 32, 64, 128}); q, k, v and d_o may be given raw and / or as hi/lo planes,
+ * the outputs asked for raw and / or as planes.  d = 64 or 128 with planes (in the backward: of both qkv and
+ * d_o) runs on tcgen05, d <= 64 otherwise on warp-level MMA, raw d = 128 and BT_FLAG_ATTN_SIMT in plain FP32.
+ * Every row of the inputs must be finite, those behind the mask too (they enter the tensor-core products
+ * with weight zero).  At most 2^21 positions, 2^30 rows, 2^24 sequence-heads, 2^33 row-heads.
+ * The backward takes the forward's inputs, o (raw) and lse and overwrites all of dqkv:
+ *     dv_j = sum_i p_ij do_i,  ds_ij = p_ij (do_i v_j - do_i o_i) (1 - tanh^2),
+ *     dq_i = sum_j ds_ij k_j / sqrt(d),  dk_j = sum_i ds_ij q_i / sqrt(d),
+ * in a fixed order (no atomics: two runs give the same bits).
+ * scratch: device, 256-byte aligned, bt_op_attention_mod_scratch_bytes bytes, contents irrelevant on entry;
+ * calls that may overlap on the GPU need one each.  bt_op_attention_mod_check synchronises the stream and
+ * returns BT_ERR_DEVICE_TIMEOUT if a bounded wait of the last call on that scratch ran out. */
+BT_API size_t bt_op_attention_mod_scratch_bytes(int32_t B, int32_t T, int32_t C, int32_t H);
+BT_API bt_status bt_op_attention_mod_fwd(const float* qkv, const float* qkv_split, int32_t B, int32_t T, int32_t C,
+                                         int32_t H, const bt_attn_mod* mod, float* o, float* o_split, float* lse,
+                                         void* scratch, size_t scratch_bytes, uint32_t flags, void* stream);
+BT_API bt_status bt_op_attention_mod_bwd(const float* qkv, const float* qkv_split, const float* o, const float* lse,
+                                         const float* d_o, const float* d_o_split, int32_t B, int32_t T, int32_t C,
+                                         int32_t H, const bt_attn_mod* mod, float* dqkv, float* dqkv_split,
+                                         void* scratch, size_t scratch_bytes, uint32_t flags, void* stream);
+BT_API bt_status bt_op_attention_mod_check(const void* scratch, void* stream);
+
+/* Dropout with a mask that is never stored: y_i = keep_i x_i / (1 - p) (+ residual_i), 0 <= p < 1.  Element i
+ * is kept when word i mod 4 of Philox-4x32-10 (Salmon et al. 2011) at counter (i / 4 mod 2^32, i / 4 >> 32,
+ * off mod 2^32, off >> 32) under the key (seed mod 2^32, seed >> 32) is at least p 2^32 (rounded to a whole
+ * number); off = offset + *d_step (d_step: device, 8-byte aligned, nullable: lets a captured step draw a new
+ * mask at every replay).  Give every call site and step its own offset.  A dropped element is zero
+ * whatever x holds there.  bt_op_dropout_bwd forms dx_i = keep_i dy_i / (1 - p) with the same seed and offset; the
+ * residual's gradient is dy itself.  Any n >= 0; planes (y_split [2][n]) need n % 4 == 0; y may be x or residual. */
+BT_API bt_status bt_op_dropout_fwd(const float* x, const float* residual, int64_t n, double p, uint64_t seed,
+                                   uint64_t offset, float* y, float* y_split, const uint64_t* d_step, void* stream);
+BT_API bt_status bt_op_dropout_bwd(const float* dy, int64_t n, double p, uint64_t seed, uint64_t offset, float* dx,
+                                   float* dx_split, const uint64_t* d_step, void* stream);
+
 /* GELU forward (Appendix "Performance Benchmarks", GELU Forward; Kernel Design and Optimization:
  * 128-bit accesses, one pass, no lossy approximation): y = GELU(x) in the exact erf form (or the
  * tanh form), n % 4 == 0. */

@@ -20,6 +20,7 @@ BT_FLAG_RECOMPUTE_LN = 64
 BT_FLAG_LOGITS_IN_PLACE = 128
 BT_FLAG_RECOMPUTE_GELU = 256
 BT_GEMM_NT, BT_GEMM_NN, BT_GEMM_TN = 0, 1, 2
+BT_ROPE_PLAIN, BT_ROPE_LINEAR, BT_ROPE_BY_PARTS = 0, 1, 2
 STATUS = {0: "BT_OK", 1: "BT_ERR_INVALID_ARG", 2: "BT_ERR_UNSUPPORTED", 3: "BT_ERR_OOM", 4: "BT_ERR_CUDA",
           5: "BT_ERR_DEVICE_TIMEOUT", 6: "BT_ERR_NOT_FOUND"}
 
@@ -42,6 +43,15 @@ class bt_adamw_config(ctypes.Structure):
 class bt_lr_schedule(ctypes.Structure):
     _fields_ = [("max_lr", ctypes.c_float), ("min_lr", ctypes.c_float), ("warmup_steps", ctypes.c_int32),
                 ("max_steps", ctypes.c_int32)]
+
+
+class bt_rope_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rot_dim", "interleaved", "scaling", "original_len")] + \
+               [(n, ctypes.c_double) for n in ("base", "factor", "low", "high")] + [("mscale", ctypes.c_float)]
+
+
+class bt_attn_mod(ctypes.Structure):
+    _fields_ = [("softcap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("spans", ctypes.c_void_p)]
 
 
 _vp, _i32, _i64, _u32, _sz, _f = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_size_t,
@@ -114,6 +124,16 @@ _SIGNATURES = {
     "bt_op_gemm": (_i32, [_i32, _i64, _i64, _i64] + [_vp] * 6 + [_sz, _u32, _vp]),
     "bt_op_attention_fwd": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _u32, _vp]),
     "bt_op_attention_bwd": (_i32, [_vp] * 6 + [_i32] * 4 + [_vp] * 3 + [_sz, _u32, _vp]),
+    "bt_op_rope_fwd": (_i32, [_vp, _vp, _i64, _i32, _i32, _i32, ctypes.POINTER(bt_rope_config), _vp, _vp, _vp]),
+    "bt_op_rope_bwd": (_i32, [_vp, _vp, _i64, _i32, _i32, _i32, ctypes.POINTER(bt_rope_config), _vp, _vp, _vp]),
+    "bt_op_attention_spans_bytes": (_sz, [_i32, _i32]),
+    "bt_op_attention_spans": (_i32, [_vp, _vp, _i32, _i32, _i32, _vp, _sz, _vp]),
+    "bt_op_attention_mod_scratch_bytes": (_sz, [_i32, _i32, _i32, _i32]),
+    "bt_op_attention_mod_fwd": (_i32, [_vp, _vp] + [_i32] * 4 + [ctypes.POINTER(bt_attn_mod)] + [_vp] * 4 + [_sz, _u32, _vp]),
+    "bt_op_attention_mod_bwd": (_i32, [_vp] * 6 + [_i32] * 4 + [ctypes.POINTER(bt_attn_mod)] + [_vp] * 3 + [_sz, _u32, _vp]),
+    "bt_op_attention_mod_check": (_i32, [_vp, _vp]),
+    "bt_op_dropout_fwd": (_i32, [_vp, _vp, _i64, ctypes.c_double, ctypes.c_uint64, ctypes.c_uint64, _vp, _vp, _vp, _vp]),
+    "bt_op_dropout_bwd": (_i32, [_vp, _i64, ctypes.c_double, ctypes.c_uint64, ctypes.c_uint64, _vp, _vp, _vp, _vp]),
     "bt_op_gelu_fwd": (_i32, [_vp, _i64, _i32, _vp, _vp, _vp]),
     "bt_op_gelu_bwd": (_i32, [_vp, _vp, _i64, _i32, _vp, _vp, _vp]),
     "bt_op_gelu_bwd_colsum": (_i32, [_vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
@@ -560,6 +580,87 @@ def bt_op_attention_bwd(qkv, o, lse, d_o, B, T, C, H, dqkv, dqkv_split, scratch,
     _check(lib().bt_op_attention_bwd(_ptr(qkv), _ptr(qkv_split), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(d_o_split), B, T,
                                      C, H, _ptr(dqkv), _ptr(dqkv_split), _ptr(scratch), scratch_bytes, flags,
                                      _stream(stream)))
+
+
+def _arr(t, dtype=torch.float32):
+    """Address of a device array; a tensor must be contiguous, of `dtype` and on the current device."""
+    if isinstance(t, torch.Tensor):
+        if t.dtype != dtype:
+            raise ValueError(f"expected a {dtype} tensor, got {t.dtype}")
+        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise ValueError(f"expected a tensor on the current device, got one on {t.device}")
+    return _ptr(t)
+
+
+def make_rope(rot_dim, interleaved=False, base=10000.0, scaling=BT_ROPE_PLAIN, factor=1.0, low=1.0, high=32.0,
+              original_len=0, mscale=1.0):
+    return bt_rope_config(rot_dim, int(interleaved), scaling, original_len, base, factor, low, high, mscale)
+
+
+def make_attn_mod(softcap=0.0, slopes=None, spans=None):
+    """The score modification of bt_op_attention_mod_*; it keeps the tensors it is given alive."""
+    mod = bt_attn_mod(softcap, _arr(slopes), _arr(spans, torch.uint8))
+    mod.tensors = (slopes, spans)
+    return mod
+
+
+def _check_mod(mod, B, T, H):
+    slopes, spans = getattr(mod, "tensors", (None, None))
+    if isinstance(slopes, torch.Tensor) and slopes.numel() < H:
+        raise ValueError(f"{slopes.numel()} slopes for {H} heads")
+    if isinstance(spans, torch.Tensor) and spans.numel() < bt_op_attention_spans_bytes(B, T):
+        raise ValueError("the spans were built for a smaller batch")
+
+
+def bt_op_rope_fwd(x, pos, N, T, C, H, rope, y, y_split=None, stream=None):
+    _check(lib().bt_op_rope_fwd(_arr(x), _arr(pos, torch.int32), N, T, C, H, ctypes.byref(rope), _arr(y), _arr(y_split),
+                                _stream(stream)))
+
+
+def bt_op_rope_bwd(dy, pos, N, T, C, H, rope, dx, dx_split=None, stream=None):
+    _check(lib().bt_op_rope_bwd(_arr(dy), _arr(pos, torch.int32), N, T, C, H, ctypes.byref(rope), _arr(dx), _arr(dx_split),
+                                _stream(stream)))
+
+
+def bt_op_attention_spans_bytes(B, T):
+    return int(lib().bt_op_attention_spans_bytes(B, T))
+
+
+def bt_op_attention_spans(doc, prefix, window, B, T, spans, spans_bytes, stream=None):
+    _check(lib().bt_op_attention_spans(_arr(doc, torch.int32), _arr(prefix, torch.int32), window, B, T,
+                                       _arr(spans, torch.uint8), spans_bytes, _stream(stream)))
+
+
+def bt_op_attention_mod_scratch_bytes(B, T, C, H):
+    return int(lib().bt_op_attention_mod_scratch_bytes(B, T, C, H))
+
+
+def bt_op_attention_mod_fwd(qkv, qkv_split, B, T, C, H, mod, o, o_split, lse, scratch, scratch_bytes, flags=0, stream=None):
+    _check_mod(mod, B, T, H)
+    _check(lib().bt_op_attention_mod_fwd(_arr(qkv), _arr(qkv_split), B, T, C, H, ctypes.byref(mod), _arr(o), _arr(o_split),
+                                         _arr(lse), _arr(scratch, torch.uint8), scratch_bytes, flags, _stream(stream)))
+
+
+def bt_op_attention_mod_bwd(qkv, qkv_split, o, lse, d_o, d_o_split, B, T, C, H, mod, dqkv, dqkv_split, scratch,
+                            scratch_bytes, flags=0, stream=None):
+    _check_mod(mod, B, T, H)
+    _check(lib().bt_op_attention_mod_bwd(_arr(qkv), _arr(qkv_split), _arr(o), _arr(lse), _arr(d_o), _arr(d_o_split), B, T,
+                                         C, H, ctypes.byref(mod), _arr(dqkv), _arr(dqkv_split), _arr(scratch, torch.uint8),
+                                         scratch_bytes, flags, _stream(stream)))
+
+
+def bt_op_attention_mod_check(scratch, stream=None):
+    _check(lib().bt_op_attention_mod_check(_arr(scratch, torch.uint8), _stream(stream)))
+
+
+def bt_op_dropout_fwd(x, residual, n, p, seed, offset, y, y_split=None, d_step=None, stream=None):
+    _check(lib().bt_op_dropout_fwd(_arr(x), _arr(residual), n, p, seed, offset, _arr(y), _arr(y_split),
+                                   _arr(d_step, torch.int64), _stream(stream)))
+
+
+def bt_op_dropout_bwd(dy, n, p, seed, offset, dx, dx_split=None, d_step=None, stream=None):
+    _check(lib().bt_op_dropout_bwd(_arr(dy), n, p, seed, offset, _arr(dx), _arr(dx_split), _arr(d_step, torch.int64),
+                                   _stream(stream)))
 
 
 def bt_op_gelu_fwd(x, n, tanh_form, y, y_split, stream=None):

@@ -1453,6 +1453,193 @@ extern "C" bt_status bt_op_attention_bwd(const float* qkv, const float* qkv_spli
     return BT_OK;
 }
 
+// ---------------------------------------------------------------- rotary positions, dropout, modified attention
+
+namespace {
+
+// Turns per position of every rotated pair: theta_i / 2 pi, theta_i = base^(-2 i / rot_dim), stretched for
+// long contexts.  Successive pairs differ by one factor, so one power serves them all.
+bt_status rope_turns(const bt_rope_config* r, int32_t d, double* turns) {
+    if (!r) return fail(BT_ERR_INVALID_ARG, "rope: config is NULL");
+    if (r->rot_dim < 2 || r->rot_dim > d || r->rot_dim % 2) return fail(BT_ERR_INVALID_ARG, "rope: rot_dim %d not an even number in [2, %d]", r->rot_dim, d);
+    if (!(r->base > 0.0) || !std::isfinite(r->base)) return fail(BT_ERR_INVALID_ARG, "rope: base must be positive");
+    if (r->scaling < BT_ROPE_PLAIN || r->scaling > BT_ROPE_BY_PARTS) return fail(BT_ERR_INVALID_ARG, "rope: scaling %d", r->scaling);
+    if (!std::isfinite(r->mscale)) return fail(BT_ERR_INVALID_ARG, "rope: mscale is not finite");
+    if (r->scaling != BT_ROPE_PLAIN && !(r->factor >= 1.0 && std::isfinite(r->factor))) return fail(BT_ERR_INVALID_ARG, "rope: factor must be at least 1");
+    if (r->scaling == BT_ROPE_BY_PARTS && (r->original_len < 1 || !(r->high > r->low) || !std::isfinite(r->high) || !std::isfinite(r->low)))
+        return fail(BT_ERR_INVALID_ARG, "rope: scaling by parts needs original_len >= 1 and low < high");
+    const double kTwoPi = 6.283185307179586476925286766559;
+    const long double step = std::pow((long double)r->base, -2.0L / r->rot_dim);
+    long double theta = 1.0L;
+    for (int i = 0; i < r->rot_dim / 2; ++i, theta *= step) {
+        double f = (double)theta;
+        if (r->scaling == BT_ROPE_LINEAR) f /= r->factor;
+        if (r->scaling == BT_ROPE_BY_PARTS) {
+            double keep = (r->original_len * f / kTwoPi - r->low) / (r->high - r->low);
+            keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+            f *= keep + (1.0 - keep) / r->factor;
+        }
+        turns[i] = f / kTwoPi;
+    }
+    return BT_OK;
+}
+
+bt_status rope_impl(const float* x, const int32_t* pos, int64_t N, int32_t T, int32_t C, int32_t H, const bt_rope_config* rope,
+                    float* y, float* y_split, float sign, void* stream) {
+    BT_PTR(x); BT_OPT_PTR(pos); BT_OPT_PTR(y); BT_OPT_PTR(y_split);
+    if (!y && !y_split) return fail(BT_ERR_INVALID_ARG, "rope: no output requested");
+    if (N < 0 || T < 1 || C < 1 || H < 1 || C % H || C > (1 << 26)) return fail(BT_ERR_INVALID_ARG, "rope: bad sizes");
+    if ((C / H) % 4) return fail(BT_ERR_INVALID_ARG, "rope: head_dim %d is not a multiple of 4", C / H);
+    RopeArgs g{};
+    if (bt_status st = rope_turns(rope, C / H < 128 ? C / H : 128, g.turns)) return st;
+    if (y_split && (y_split == x || y_split + N * 3 * (int64_t)C == x)) return fail(BT_ERR_INVALID_ARG, "rope: planes cannot be written over the input");
+    if (y == x && y_split) return fail(BT_ERR_INVALID_ARG, "rope: in place only without planes");
+    if (N == 0) return BT_OK;
+    g.x = x; g.pos = pos; g.N = N; g.T = T; g.C = C; g.H = H;
+    g.rot = rope->rot_dim; g.interleaved = rope->interleaved != 0;
+    g.sin_sign = sign; g.mscale = rope->mscale;
+    g.y = y; g.y_hi = y_split; g.y_lo = y_split ? y_split + N * 3 * (int64_t)C : nullptr;
+    BT_CUDA(launch_rope(g, (cudaStream_t)stream));
+    return BT_OK;
+}
+
+bt_status dropout_impl(const float* x, const float* residual, int64_t n, double p, uint64_t seed, uint64_t offset, float* y,
+                       float* y_split, const uint64_t* d_step, void* stream) {
+    BT_PTR(x); BT_OPT_PTR(residual); BT_OPT_PTR(y); BT_OPT_PTR(y_split);
+    if (reinterpret_cast<uintptr_t>(d_step) & 7u) return fail(BT_ERR_INVALID_ARG, "dropout: d_step is not 8-byte aligned");
+    if (!y && !y_split) return fail(BT_ERR_INVALID_ARG, "dropout: no output requested");
+    if (n < 0 || n > ((int64_t)1 << 42)) return fail(BT_ERR_INVALID_ARG, "dropout: bad size");
+    if (y_split && n % 4) return fail(BT_ERR_INVALID_ARG, "dropout: planes need n %% 4 == 0");
+    if (!(p >= 0.0 && p < 1.0)) return fail(BT_ERR_INVALID_ARG, "dropout: p must lie in [0, 1)");
+    if (n == 0) return BT_OK;
+    DropoutArgs g{x, residual, n, seed, offset, d_step, (uint64_t)std::llrint(p * 4294967296.0), (float)(1.0 / (1.0 - p)), y,
+                  y_split, y_split ? y_split + n : nullptr};
+    BT_CUDA(launch_dropout(g, (cudaStream_t)stream));
+    return BT_OK;
+}
+
+// Scratch of the modified attention: the device error word in the first 256 bytes, then [B, H, T] row sums.
+constexpr size_t kAttnModHeader = 256;
+
+bt_status attn_mod_args(AttnModArgs& g, const char* who, int32_t B, int32_t T, int32_t C, int32_t H, const bt_attn_mod* mod,
+                        const float* qkv, const float* qkv_split, void* scratch, size_t scratch_bytes) {
+    if (B < 1 || T < 1 || C < 1 || H < 1 || C % H) return fail(BT_ERR_INVALID_ARG, "%s: bad sizes", who);
+    const int d = C / H;
+    if (d != 16 && d != 32 && d != 64 && d != 128) return fail(BT_ERR_UNSUPPORTED, "%s: head_dim %d not in {16,32,64,128}", who, d);
+    if (T > (1 << 21) || (int64_t)B * T > (1 << 30) || (int64_t)B * H > (1 << 24) || (int64_t)B * H * T > ((int64_t)1 << 33))
+        return fail(BT_ERR_UNSUPPORTED, "%s: more than 2^21 positions, 2^30 rows or 2^33 row-heads", who);
+    if (!mod) return fail(BT_ERR_INVALID_ARG, "%s: mod is NULL", who);
+    if (!(mod->softcap >= 0.f) || !std::isfinite(mod->softcap)) return fail(BT_ERR_INVALID_ARG, "%s: softcap must be finite and not negative", who);
+    if (!aligned16(mod->slopes) || !aligned16(mod->spans)) return fail(BT_ERR_INVALID_ARG, "%s: slopes or spans not 16-byte aligned", who);
+    if (!qkv && !qkv_split) return fail(BT_ERR_INVALID_ARG, "%s: qkv and qkv_split both NULL", who);
+    if (reinterpret_cast<uintptr_t>(scratch) & 255u) return fail(BT_ERR_INVALID_ARG, "%s: scratch not 256-byte aligned", who);
+    if (scratch_bytes < bt_op_attention_mod_scratch_bytes(B, T, C, H)) return fail(BT_ERR_OOM, "%s: scratch too small", who);
+    const int64_t n = (int64_t)B * T;
+    g.B = B; g.T = T; g.C = C; g.H = H;
+    g.cap = mod->softcap;
+    g.slopes = mod->slopes;
+    g.spans = attention_span_view(mod->spans, B, T);
+    // both forms hold the same values: the planes serve the tensor-core kernels, the raw array the others
+    const bool planes = qkv_split && (!qkv || d >= 64);
+    g.qkv = planes ? qkv_split : qkv;
+    g.qkv_lo = planes ? qkv_split + n * 3 * C : nullptr;
+    g.err = (int*)scratch;
+    g.dvec = (float*)((uint8_t*)scratch + kAttnModHeader);
+    char msg[256];
+    if (planes && d >= 64 && !gemm_tc_init(msg, sizeof(msg))) return fail(BT_ERR_CUDA, "tensor-core attention unavailable: %s", msg);
+    return BT_OK;
+}
+
+}  // namespace
+
+extern "C" bt_status bt_op_rope_fwd(const float* x, const int32_t* pos, int64_t N, int32_t T, int32_t C, int32_t H,
+                                    const bt_rope_config* rope, float* y, float* y_split, void* stream) {
+    return rope_impl(x, pos, N, T, C, H, rope, y, y_split, 1.0f, stream);
+}
+
+extern "C" bt_status bt_op_rope_bwd(const float* dy, const int32_t* pos, int64_t N, int32_t T, int32_t C, int32_t H,
+                                    const bt_rope_config* rope, float* dx, float* dx_split, void* stream) {
+    return rope_impl(dy, pos, N, T, C, H, rope, dx, dx_split, -1.0f, stream);
+}
+
+extern "C" bt_status bt_op_dropout_fwd(const float* x, const float* residual, int64_t n, double p, uint64_t seed,
+                                       uint64_t offset, float* y, float* y_split, const uint64_t* d_step, void* stream) {
+    return dropout_impl(x, residual, n, p, seed, offset, y, y_split, d_step, stream);
+}
+
+extern "C" bt_status bt_op_dropout_bwd(const float* dy, int64_t n, double p, uint64_t seed, uint64_t offset, float* dx,
+                                       float* dx_split, const uint64_t* d_step, void* stream) {
+    return dropout_impl(dy, nullptr, n, p, seed, offset, dx, dx_split, d_step, stream);
+}
+
+extern "C" size_t bt_op_attention_spans_bytes(int32_t B, int32_t T) {
+    if (B < 1 || T < 1 || T > (1 << 21) || (int64_t)B * T > (1 << 30)) return 0;
+    return attention_spans_bytes(B, T);
+}
+
+extern "C" bt_status bt_op_attention_spans(const int32_t* doc, const int32_t* prefix, int32_t window, int32_t B, int32_t T,
+                                           void* spans, size_t spans_bytes, void* stream) {
+    BT_OPT_PTR(doc); BT_OPT_PTR(prefix); BT_PTR(spans);
+    if (B < 1 || T < 1 || window < 0) return fail(BT_ERR_INVALID_ARG, "attention_spans: bad sizes");
+    const size_t need = bt_op_attention_spans_bytes(B, T);
+    if (need == 0) return fail(BT_ERR_UNSUPPORTED, "attention_spans: more than 2^21 positions or 2^30 rows");
+    if (spans_bytes < need) return fail(BT_ERR_OOM, "attention_spans: buffer too small");
+    BT_CUDA(launch_attention_spans(doc, prefix, window, B, T, spans, (cudaStream_t)stream));
+    return BT_OK;
+}
+
+extern "C" size_t bt_op_attention_mod_scratch_bytes(int32_t B, int32_t T, int32_t C, int32_t H) {
+    if (B < 1 || T < 1 || C < 1 || H < 1) return 0;
+    return kAttnModHeader + (((size_t)B * H * T * sizeof(float) + 255) & ~(size_t)255);
+}
+
+extern "C" bt_status bt_op_attention_mod_fwd(const float* qkv, const float* qkv_split, int32_t B, int32_t T, int32_t C,
+                                             int32_t H, const bt_attn_mod* mod, float* o, float* o_split, float* lse,
+                                             void* scratch, size_t scratch_bytes, uint32_t flags, void* stream) {
+    BT_OPT_PTR(qkv); BT_OPT_PTR(qkv_split); BT_OPT_PTR(o); BT_OPT_PTR(o_split); BT_PTR(lse); BT_PTR(scratch);
+    if (!o && !o_split) return fail(BT_ERR_INVALID_ARG, "attention_mod_fwd: no output requested");
+    AttnModArgs g{};
+    if (bt_status st = attn_mod_args(g, "attention_mod_fwd", B, T, C, H, mod, qkv, qkv_split, scratch, scratch_bytes)) return st;
+    g.o = o; g.o_hi = o_split; g.o_lo = o_split ? o_split + (int64_t)B * T * C : nullptr;
+    g.lse = lse;
+    cudaStream_t s = (cudaStream_t)stream;
+    BT_CUDA(cudaMemsetAsync(g.err, 0, sizeof(int), s));
+    BT_CUDA(launch_attention_mod_fwd(g, (flags & BT_FLAG_ATTN_SIMT) != 0, s));
+    return BT_OK;
+}
+
+extern "C" bt_status bt_op_attention_mod_bwd(const float* qkv, const float* qkv_split, const float* o, const float* lse,
+                                             const float* d_o, const float* d_o_split, int32_t B, int32_t T, int32_t C,
+                                             int32_t H, const bt_attn_mod* mod, float* dqkv, float* dqkv_split,
+                                             void* scratch, size_t scratch_bytes, uint32_t flags, void* stream) {
+    BT_OPT_PTR(qkv); BT_OPT_PTR(qkv_split); BT_PTR(o); BT_PTR(lse); BT_OPT_PTR(d_o); BT_OPT_PTR(d_o_split);
+    BT_OPT_PTR(dqkv); BT_OPT_PTR(dqkv_split); BT_PTR(scratch);
+    if (!dqkv && !dqkv_split) return fail(BT_ERR_INVALID_ARG, "attention_mod_bwd: no output requested");
+    if (!d_o && !d_o_split) return fail(BT_ERR_INVALID_ARG, "attention_mod_bwd: d_o and d_o_split both NULL");
+    AttnModArgs g{};
+    if (bt_status st = attn_mod_args(g, "attention_mod_bwd", B, T, C, H, mod, qkv, qkv_split, scratch, scratch_bytes)) return st;
+    const int64_t n = (int64_t)B * T;
+    const bool planes = d_o_split && (!d_o || C / H >= 64);
+    g.d_o = planes ? d_o_split : d_o;
+    g.d_o_lo = planes ? d_o_split + n * C : nullptr;
+    g.o = const_cast<float*>(o);
+    g.lse = const_cast<float*>(lse);
+    g.dqkv = dqkv; g.dqkv_hi = dqkv_split; g.dqkv_lo = dqkv_split ? dqkv_split + n * 3 * C : nullptr;
+    cudaStream_t s = (cudaStream_t)stream;
+    BT_CUDA(cudaMemsetAsync(g.err, 0, sizeof(int), s));
+    BT_CUDA(launch_attention_mod_bwd(g, (flags & BT_FLAG_ATTN_SIMT) != 0, s));
+    return BT_OK;
+}
+
+extern "C" bt_status bt_op_attention_mod_check(const void* scratch, void* stream) {
+    BT_PTR(scratch);
+    int herr = 0;
+    BT_CUDA(cudaMemcpyAsync(&herr, scratch, sizeof(int), cudaMemcpyDeviceToHost, (cudaStream_t)stream));
+    BT_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
+    if (herr) return fail(BT_ERR_DEVICE_TIMEOUT, "attention_mod: a bounded device-side wait ran out (code %d)", herr);
+    return BT_OK;
+}
+
 extern "C" bt_status bt_op_gelu_fwd(const float* x, int64_t n, int32_t tanh_form, float* y, float* y_split,
                                     void* stream) {
     BT_PTR(x); BT_OPT_PTR(y); BT_OPT_PTR(y_split);

@@ -295,4 +295,58 @@ cudaError_t launch_attention_bwd(const float* qkv, const float* qkv_hi, int64_t 
 // gradient is the column sum of this small array.
 int64_t attention_bwd_rowgroups(int B, int T);
 
+// Key spans of a packed batch (attention_spans.cu): query i of sequence b reads keys k[b T + i].x <= j <
+// k[b T + i].y, key j is read by queries q[b T + j].x <= i < q[b T + j].y; kblock / qblock: the same ranges
+// over blocks of 64 rows, [B][ceil(T / 64)].  All null: causal.
+struct SpanView {
+    const int2 *k, *q, *kblock, *qblock;
+};
+SpanView attention_span_view(const void* spans, int B, int T);
+size_t attention_spans_bytes(int B, int T);
+cudaError_t launch_attention_spans(const int32_t* doc, const int32_t* mark, int window, int B, int T, void* spans,
+                                   cudaStream_t s);
+
+// Attention with modified scores.  An array given raw has its *_lo null; given as planes, the first
+// pointer is the hi plane.  Outputs may be asked for raw, as planes, or both.
+struct AttnModArgs {
+    int B, T, C, H;
+    float cap;                  // 0: none
+    const float* slopes;        // [H], null: none
+    SpanView spans;
+    const float *qkv, *qkv_lo;
+    float *o, *o_hi, *o_lo;     // forward: outputs; backward: o is the raw forward output
+    float* lse;                 // [B, H, T]: written by the forward, read by the backward
+    const float *d_o, *d_o_lo;
+    float* dvec;                // [B, H, T] rowsum(dO o O), scratch
+    float *dqkv, *dqkv_hi, *dqkv_lo;
+    int* err;                   // device error word of the bounded waits
+};
+cudaError_t launch_attention_mod_fwd(const AttnModArgs& g, bool simt, cudaStream_t s);
+cudaError_t launch_attention_mod_bwd(const AttnModArgs& g, bool simt, cudaStream_t s);
+
+// Rotary positions.
+struct RopeArgs {
+    const float* x;
+    const int32_t* pos;         // [N], null: n mod T
+    int64_t N;
+    int T, C, H, rot, interleaved;
+    float sin_sign, mscale;
+    float *y, *y_hi, *y_lo;
+    int rows;                   // rows per CTA (set by the launcher)
+    double turns[64];           // turns per position of each pair
+};
+cudaError_t launch_rope(RopeArgs g, cudaStream_t s);
+
+// Dropout.
+struct DropoutArgs {
+    const float *x, *residual;
+    int64_t n;
+    uint64_t seed, offset;
+    const uint64_t* d_step;     // nullable: added to offset on the device
+    uint64_t threshold;         // keep a word that is at least this
+    float scale;
+    float *y, *y_hi, *y_lo;
+};
+cudaError_t launch_dropout(const DropoutArgs& g, cudaStream_t s);
+
 }  // namespace bt
