@@ -1603,7 +1603,6 @@ extern "C" bt_status bt_op_attention_mod_fwd(const float* qkv, const float* qkv_
     g.o = o; g.o_hi = o_split; g.o_lo = o_split ? o_split + (int64_t)B * T * C : nullptr;
     g.lse = lse;
     cudaStream_t s = (cudaStream_t)stream;
-    BT_CUDA(cudaMemsetAsync(g.err, 0, sizeof(int), s));
     BT_CUDA(launch_attention_mod_fwd(g, (flags & BT_FLAG_ATTN_SIMT) != 0, s));
     return BT_OK;
 }
@@ -1626,7 +1625,6 @@ extern "C" bt_status bt_op_attention_mod_bwd(const float* qkv, const float* qkv_
     g.lse = const_cast<float*>(lse);
     g.dqkv = dqkv; g.dqkv_hi = dqkv_split; g.dqkv_lo = dqkv_split ? dqkv_split + n * 3 * C : nullptr;
     cudaStream_t s = (cudaStream_t)stream;
-    BT_CUDA(cudaMemsetAsync(g.err, 0, sizeof(int), s));
     BT_CUDA(launch_attention_mod_bwd(g, (flags & BT_FLAG_ATTN_SIMT) != 0, s));
     return BT_OK;
 }
