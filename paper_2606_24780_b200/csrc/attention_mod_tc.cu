@@ -364,7 +364,7 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
         mbar_init(bar(P_READY), 8);
         mbar_init(bar(DS_READY), 8);
         mbar_init(bar(K_READY), 4);
-        mbar_init(bar(STAT_READY), 4);
+        mbar_init(bar(STAT_READY), 8);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) alloc_tmem(tmem_slot);
@@ -491,7 +491,8 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
         const int2 span = row_range(g.spans.q, b, g.T, key, true);
         bool ok = true;
         const uint32_t c0 = 32u * (uint32_t)wg;
-        // Statistics of a tile's 64 queries (lse in base-2 units, D) through shared memory, one tile ahead.
+        // Statistics of a tile's 64 queries (lse in base-2 units, D) through shared memory, one tile ahead.  All
+        // eight warps arrive, those without a value too: no warp can be two phases behind.
         float* stat = reinterpret_cast<float*>(smem_ptr(bars + 256u + 4u * kRowTileBytes));
         const int sidx = (warp - 2) * 32 + lane;
         auto fetch_stat = [&](int t) -> float {
@@ -502,9 +503,9 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
             if (sidx < 128) {
                 stat[(t & 1) * 128 + sidx] = v;
                 __threadfence_block();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(STAT_READY));
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(STAT_READY));
         };
         float acc_v[32], acc_k[32];
 #pragma unroll
