@@ -11,6 +11,9 @@ cudaError_t launch_attention_mod_bwd_simt(const AttnModArgs& g, cudaStream_t s);
 bool attention_mod_tc_supports(const AttnModArgs& g);
 cudaError_t launch_attention_mod_fwd_tc(const AttnModArgs& g, cudaStream_t s);
 cudaError_t launch_attention_mod_bwd_tc(const AttnModArgs& g, cudaStream_t s);
+bool attention_mod_mma_supports(const AttnModArgs& g);
+cudaError_t launch_attention_mod_fwd_mma(const AttnModArgs& g, cudaStream_t s);
+cudaError_t launch_attention_mod_bwd_mma(const AttnModArgs& g, cudaStream_t s);
 bool attention_mod_tc128_supports(const AttnModArgs& g);
 cudaError_t launch_attention_mod_fwd_tc128(const AttnModArgs& g, cudaStream_t s);
 cudaError_t launch_attention_mod_bwd_tc128(const AttnModArgs& g, cudaStream_t s);
@@ -18,7 +21,8 @@ cudaError_t launch_attention_mod_bwd_tc128(const AttnModArgs& g, cudaStream_t s)
 cudaError_t launch_attention_mod_fwd(const AttnModArgs& g, bool simt, cudaStream_t s) {
     if (!simt && attention_mod_tc_supports(g)) return launch_attention_mod_fwd_tc(g, s);
     if (!simt && attention_mod_tc128_supports(g)) return launch_attention_mod_fwd_tc128(g, s);
-    const cudaError_t e = cudaMemsetAsync(g.err, 0, sizeof(int), s);   // the tensor-core kernels clear it themselves
+    if (!simt && attention_mod_mma_supports(g)) return launch_attention_mod_fwd_mma(g, s);
+    const cudaError_t e = cudaMemsetAsync(g.err, 0, sizeof(int), s);   // the other kernels clear it themselves
     if (e != cudaSuccess) return e;
     return launch_attention_mod_fwd_simt(g, s);
 }
@@ -26,6 +30,7 @@ cudaError_t launch_attention_mod_fwd(const AttnModArgs& g, bool simt, cudaStream
 cudaError_t launch_attention_mod_bwd(const AttnModArgs& g, bool simt, cudaStream_t s) {
     if (!simt && attention_mod_tc_supports(g) && g.d_o_lo) return launch_attention_mod_bwd_tc(g, s);
     if (!simt && attention_mod_tc128_supports(g) && g.d_o_lo) return launch_attention_mod_bwd_tc128(g, s);
+    if (!simt && attention_mod_mma_supports(g)) return launch_attention_mod_bwd_mma(g, s);
     cudaError_t e = cudaMemsetAsync(g.err, 0, sizeof(int), s);
     if (e == cudaSuccess) e = launch_attention_dvec(g.o, nullptr, g.d_o, g.d_o_lo, g.B, g.T, g.C, g.H, g.dvec, s);
     if (e != cudaSuccess) return e;
