@@ -15,34 +15,20 @@ constexpr float kLn2 = 0.6931471805599453f;
 // reweighted to the smallest largest relative error, 2.8e-9, one FP32 rounding in all); above,
 // 1 - 2 / (1 + e^2|u|), which is good to 2^-22 there.
 constexpr float kTanhSmall = 0.6f;
+constexpr float kTanh0 = -0.33333298563957214f, kTanh1 = 0.13331924378871918f, kTanh2 = -0.053783830255270004f,
+                kTanh3 = 0.020795971155166626f, kTanh4 = -0.005895158275961876f;
 __device__ __forceinline__ float tanh_small(float u) {
     const float w = u * u;
-    float q = fmaf(w, -0.005895158275961876f, 0.020795971155166626f);
-    q = fmaf(w, q, -0.053783830255270004f);
-    q = fmaf(w, q, 0.13331924378871918f);
-    q = fmaf(w, q, -0.33333298563957214f);
+    float q = fmaf(w, kTanh4, kTanh3);
+    q = fmaf(w, q, kTanh2);
+    q = fmaf(w, q, kTanh1);
+    q = fmaf(w, q, kTanh0);
     return fmaf(u * w, q, u);
 }
 __device__ __forceinline__ float tanh_any(float u) {
     const float t = fmaf(-2.0f, rcp_fast(1.0f + ex2_fast(2.8853900817779268f * fabsf(u))), 1.0f);
     return fabsf(u) < kTanhSmall ? tanh_small(u) : copysignf(t, u);
 }
-// u <- tanh(u).  The exponential and the reciprocal run at an eighth of the rate of a multiplication and are
-// needed only where some score of the row's tile is beyond 0.6 caps.
-template <int N>
-__device__ __forceinline__ void tanh_tile(float (&u)[N]) {
-    float top = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(u[i]));
-    if (top < kTanhSmall) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) u[i] = tanh_small(u[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) u[i] = tanh_any(u[i]);
-    }
-}
-
 // Score modification in base-2 units.  `unit` turns a dot product q k into cap units (u = unit * dot) or,
 // without a cap, straight into base-2 units; `to_log2` turns tanh into base-2 units.  The backward kernels
 // multiply their own rows by `unit` before the product instead of the scores after it.
@@ -57,38 +43,53 @@ __device__ __forceinline__ Score make_score(float scale, float cap, const float*
     s.slope2 = SLOPE ? slopes[h] * kLog2e : 0.f;
     return s;
 }
-// x: N neighbouring dot products of one row -> modified scores in base-2 units.  |first - i| is the distance of
-// position i.  Without a modification x stays as it is (the exponent's multiplication takes `unit`).
-template <bool CAP, bool SLOPE, int N>
-__device__ __forceinline__ void score_tile(float (&x)[N], const Score& s, int first) {
-    if (CAP || SLOPE) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] *= s.unit;
-    }
+// x: N neighbouring scores of one row -> modified scores in base-2 units, less ref.  UNIT: x holds plain dot products;
+// otherwise they carry s.unit already.  |first - i| is the distance of position i; `grad` (GRAD and CAP) receives
+// 1 - tanh^2.  The exponential and the reciprocal of tanh run at an eighth of the rate of a multiplication and are
+// needed only where some score of the N is beyond 0.6 caps.  A distance is linear in i unless the row lies inside the N
+// positions (no integer conversion per element: it runs at an eighth of the rate too).
+template <bool CAP, bool SLOPE, bool GRAD, bool UNIT, int N>
+__device__ __forceinline__ void score_tile(float (&x)[N], float (&grad)[N], const Score& s, int first, float ref) {
     if (CAP) {
-        tanh_tile<N>(x);
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] *= s.to_log2;
-    }
-    if (SLOPE) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = fmaf(-s.slope2, fabsf((float)(first - i)), x[i]);
-    }
-}
-// The same for dot products already multiplied by s.unit, keeping 1 - tanh^2 (`grad` untouched without a cap).
-template <bool CAP, bool SLOPE, int N>
-__device__ __forceinline__ void score_tile_grad(float (&x)[N], float (&grad)[N], const Score& s, int first) {
-    if (CAP) {
-        tanh_tile<N>(x);
+        float top = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            grad[i] = fmaf(-x[i], x[i], 1.0f);
-            x[i] *= s.to_log2;
+            if (UNIT) x[i] *= s.unit;
+            top = fmaxf(top, fabsf(x[i]));
+        }
+        if (top < kTanhSmall) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = tanh_small(x[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = tanh_any(x[i]);
+        }
+        if (GRAD) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) grad[i] = fmaf(-x[i], x[i], 1.0f);
         }
     }
+    constexpr bool kScale = CAP || UNIT;
+    const float scale = CAP ? s.to_log2 : s.unit;
     if (SLOPE) {
+        const float d = (float)first;
+        if (first >= N - 1 || first <= 0) {
+            const float step = first <= 0 ? -s.slope2 : s.slope2, start = fmaf(-step, d, -ref);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = fmaf(-s.slope2, fabsf((float)(first - i)), x[i]);
+            for (int i = 0; i < N; ++i) {
+                const float bias = fmaf(step, (float)i, start);
+                x[i] = kScale ? fmaf(x[i], scale, bias) : x[i] + bias;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float bias = fmaf(-s.slope2, fabsf(d - (float)i), -ref);
+                x[i] = kScale ? fmaf(x[i], scale, bias) : x[i] + bias;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = kScale ? fmaf(x[i], scale, -ref) : x[i] - ref;
     }
 }
 
@@ -108,6 +109,115 @@ __device__ __forceinline__ int2 row_range(const int2* spans, int b, int T, int r
     if (row >= T) return make_int2(0, 0);
     if (!spans) return keys ? make_int2(row, T) : make_int2(0, row + 1);
     return spans[(int64_t)b * T + row];
+}
+
+// ---------------------------------------------------------------- pieces of the persistent kernels
+// Register split of a kernel of several warpgroups: each gives up or takes registers of the block's launch total.
+template <int N>
+__device__ __forceinline__ void set_regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void set_regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+
+__device__ __forceinline__ void tmem_st2(uint32_t taddr, float a, float b) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};" ::"r"(taddr), "r"(__float_as_uint(a)), "r"(__float_as_uint(b)) : "memory");
+}
+__device__ __forceinline__ void tmem_ld2(uint32_t taddr, uint32_t& a, uint32_t& b) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];" : "=r"(a), "=r"(b) : "r"(taddr));
+}
+
+__device__ __forceinline__ void tmem_ldn(uint32_t taddr, uint32_t (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_stn(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void tmem_ldn(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_stn(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_ldn(uint32_t taddr, uint32_t (&r)[32]) { tc::tmem_ld32(taddr, r); }
+__device__ __forceinline__ void tmem_stn(uint32_t taddr, const uint32_t (&r)[32]) { tc::tmem_st32(taddr, r); }
+
+// A thread that owns a row reads and writes it in whole 32-byte sectors: no staging through shared memory, which the
+// next work item's tiles already occupy.
+__device__ __forceinline__ void ld_sector(const float* p, float (&v)[8]) {
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(p));
+}
+__device__ __forceinline__ void st_sector(float* p, const float (&v)[8]) {
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+                 "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+}
+
+// Eight values of a row to the raw array and / or the planes.  Rows start on 16 bytes only (C is a multiple of 16
+// floats, and so is every head's first column, but the caller's pointer need not be 32-byte aligned).
+__device__ __forceinline__ void store_sector(const float (&v)[8], int64_t at, float* raw, float* hi, float* lo) {
+    auto put = [](float* p, const float (&x)[8]) {
+        if ((reinterpret_cast<uintptr_t>(p) & 31u) == 0) {
+            st_sector(p, x);
+        } else {
+            *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+        }
+    };
+    if (raw) put(raw + at, v);
+    if (hi) {
+        float a[8], b[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) split_tf32(v[e], a[e], b[e]);
+        put(hi + at, a);
+        put(lo + at, b);
+    }
+}
+
+// Work items of a persistent kernel are the CTAs of its grid: a running CTA takes over one that has not started
+// (cluster launch control), so that a free SM always gets the next item and an item's prologue and epilogue
+// overlap its neighbours.  One thread asks; the answer is 16 bytes in shared memory.
+__device__ __forceinline__ void ask_next(uint32_t answer, uint32_t bar) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the previous answer has been read
+    tc::mbar_expect_tx(bar, 16u);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(bar) : "memory");
+}
+// Whether there is a next item; x, y its block index.  Not to be asked again after a "no".
+__device__ __forceinline__ bool next_item(uint32_t answer, int& x, int& y) {
+    uint32_t ok, cx = 0, cy = 0;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b128 h;\n\t.reg .b32 z;\n\t"
+        "ld.shared.b128 h, [%3];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n\t"
+        "selp.u32 %2, 1, 0, p;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%0, %1, z, _}, h;\n\t}"
+        : "+r"(cx), "+r"(cy), "=r"(ok) : "r"(answer) : "memory");
+    x = (int)cx;
+    y = (int)cy;
+    return ok != 0;
+}
+// grouped_block for a given linear block index.
+__device__ __forceinline__ void grouped_item(int head_group, int id, int& bh, int& y) {
+    const int nh = (int)gridDim.x, ny = (int)gridDim.y;
+    const int G = (head_group > 0 && head_group < nh) ? head_group : nh;
+    const int per = G * ny, grp = id / per, rem = id - grp * per;
+    const int first = grp * G, heads = min(G, nh - first);
+    y = rem / heads;
+    bh = first + (rem - y * heads);
+}
+// What an item is, for all roles: written by the scheduling thread, two deep.
+struct Item {
+    int bh, blk, t0, n;      // n tiles from tile t0 on; n < 0: no more items
+};
+
+// Bit k set: column k0 + k lies in the range (N <= 32 columns; the tests of single bits are an instruction each).
+template <int N>
+__device__ __forceinline__ uint32_t column_bits(int2 span, int k0) {
+    const int lo = min(max(span.x - k0, 0), N), hi = min(max(span.y - k0, 0), N);
+    const uint32_t below_hi = hi >= 32 ? 0xffffffffu : (1u << hi) - 1u, below_lo = lo >= 32 ? 0xffffffffu : (1u << lo) - 1u;
+    return below_hi & ~below_lo;
 }
 
 // Tensor map over a row-major [rows][cols] array of hi/lo planes: boxes of 32 columns x box_rows rows x both

@@ -141,7 +141,7 @@ __device__ __forceinline__ int column(int i, int t4) { return 8 * (i >> 2) + 2 *
 // Score products (own rows already times the score unit) -> modified scores in base-2 units, and 1 - tanh^2.
 template <bool CAP, bool SLOPE>
 __device__ __forceinline__ void modify(float (&x)[32], float (&grad)[32], const Score& sc, int r0, int tile0, int t4) {
-    score_tile_grad<CAP, false, 32>(x, grad, sc, 0);
+    score_tile<CAP, false, true, false, 32>(x, grad, sc, 0, 0.f);
     if (SLOPE) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)

@@ -50,16 +50,32 @@ __device__ __forceinline__ void settle() {
 
 // ------------------------------------------------------------------------------------------ forward
 //
-//   warps 0-3, 4-7   softmax warpgroups on alternate key tiles, each with its own running maximum, sum and output
-//                    in registers, merged at the end
-//   warp 8           TMA producer (Q once; K and V tiles through one ring of five slots in the order
-//                    K0 K1 V0 K2 V1 ...);  warp 9 issues S = Q K^T, warp 10 O_tile = P V (P from tensor memory)
-//   tensor memory    per buffer b: S at 256b, P_hi at 256b + 64, P_lo at 256b + 128, O_tile at 256b + 192
-constexpr int kFwdThreads = 352, kWarpLoad = 8, kWarpS = 9, kWarpO = 10, kSlots = 5;
-constexpr uint32_t kFwdSmem = 1024u + kResBytes + kSlots * kTile + 256u;
+// Persistent: the roles run over the work items (128 queries of one head) one after the other, each at its own pace, so
+// an item's loads, first products, last sums and stores overlap its neighbours'.
+//   warp 0      TMA producer and scheduler: the next item and its range of tiles; Q once per item, K and V tiles through one
+//               ring of four slots, K one tile ahead of V
+//   warp 1      S = Q K^T: [K_hi | K_lo] as one operand of 128 rows, the small terms into the second 64 columns
+//   warps 2, 3  O_tile = P V on alternate tiles, P from tensor memory, from zero in every tile (one thread issues an MMA
+//               about every 60 clocks; 24 of them would be 1,550 of a tile's 1,660 clocks of tensor pipe)
+//   warps 4-15  three softmax warpgroups on tiles in turn, thread = row.  Every tile is normalised by its own row
+//               maximum, so they carry nothing from tile to tile; the maximum is taken over the large half of the
+//               scores (any reference near it will do), then P = exp2(z - r)
+//   warps 16-19 add up: O = O 2^(m - m') + O_tile 2^(r - m'), l likewise; the row's output and lse
+//   tensor memory  buffer i at 128 i: S -> P_hi, small half of S -> P_lo; O_tile at 384 and 448
+// Two tiles in the softmax at a time are not enough to hide its latency; short rolled passes over the columns keep
+// the code in the instruction cache (32 columns unrolled cost a third more time than 16).
+#ifndef CHV
+#define CHV 16
+#endif
+constexpr int kFwdThreads = 640, kSlots = 4, kSoft = 3, CH = CHV;
+constexpr int kRegsIssue = 56, kRegsSoft = 88, kRegsAdd = 160;
+static_assert(kRegsIssue + kSoft * kRegsSoft + kRegsAdd <= 480, "registers: 640 threads get 96 each at launch");
+constexpr uint32_t kStatBytes = 8u * 2u * BR * 4u;            // (r, sum) of the last eight tiles
+constexpr uint32_t kFwdSmem = 1024u + kResBytes + kSlots * kTile + 512u + kStatBytes;
 static_assert(kFwdSmem <= 232448u, "shared memory");
+// Place of K(t) and V(t) among an item's 2n tile loads: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1).
 __device__ __forceinline__ int pos_k(int t) { return t == 0 ? 0 : 2 * t - 1; }
-__device__ __forceinline__ int pos_v(int t) { return 2 * t + 2; }
+__device__ __forceinline__ int pos_v(int t, int n) { return min(2 * t + 2, 2 * n - 1); }
 
 template <bool CAP, bool SLOPE>
 __global__ void __launch_bounds__(kFwdThreads, 1)
@@ -69,257 +85,295 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t q_s = base, ring_s = q_s + kResBytes, bars = ring_s + kSlots * kTile;
-    const uint32_t q_full = bars;
-    auto slot_full = [&](int i) { return bars + 8u * (1 + i); };
-    auto slot_empty = [&](int i) { return bars + 8u * (6 + i); };
-    auto s_full = [&](int b) { return bars + 8u * (11 + b); };
-    auto p_full = [&](int b) { return bars + 8u * (13 + b); };
-    auto o_full = [&](int b) { return bars + 8u * (15 + b); };
-    const uint32_t merge_full = bars + 8u * 17, all_done = bars + 8u * 18, tmem_slot = bars + 8u * 19;
+    enum { Q_FULL = 0, Q_EMPTY, SLOT_FULL, SLOT_EMPTY = SLOT_FULL + kSlots, S_FULL = SLOT_EMPTY + kSlots, P_DONE = S_FULL + kSoft,
+           P_FULL = P_DONE + kSoft, O_FULL = P_FULL + kSoft, O_FREE = O_FULL + 2, INFO_FULL = O_FREE + 2, INFO_EMPTY = INFO_FULL + 2,
+           NEXT = INFO_EMPTY + 2, N_BARS };
+    auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
+    constexpr uint32_t kInfo = (8u * N_BARS + 15u) & ~15u;            // two Items, the scheduler's answer, the TMEM address
+    static_assert(kInfo + 2 * sizeof(Item) + 32 <= 512, "barrier region");
     auto smem_ptr = [&](uint32_t addr) { return smem_raw + (addr - smem_u32(smem_raw)); };
+    volatile Item* info = reinterpret_cast<volatile Item*>(smem_ptr(bars + kInfo));
+    const uint32_t answer = bars + kInfo + 2u * (uint32_t)sizeof(Item), tmem_slot = answer + 16u;
+    float* tile_stat = reinterpret_cast<float*>(smem_ptr(bars + 512u));
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int bh, yb;
-    grouped_block(args.head_group, bh, yb);
-    const int qt = (int)gridDim.y - 1 - yb;
-    const int b = bh / g.H, h = bh % g.H, q0 = qt * BR;
-    const int row_base = b * g.T;
-
     if (threadIdx.x == 0) {
-        mbar_init(q_full, 1);
-        for (int i = 0; i < kSlots; ++i) {
-            mbar_init(slot_full(i), 1);
-            mbar_init(slot_empty(i), 1);
-        }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(s_full(i), 1);
-            mbar_init(p_full(i), 4);
-            mbar_init(o_full(i), 1);
-        }
-        mbar_init(merge_full, 4);
-        mbar_init(all_done, 1);
+        for (int i = 0; i < N_BARS; ++i)
+            mbar_init(bar(i), (i >= O_FULL && i < O_FREE) ? 2 : (i >= O_FREE && i < INFO_FULL) || (i >= P_FULL && i < O_FULL) ? 4
+                              : i >= INFO_EMPTY && i < NEXT ? 3 + 4 * kSoft + 4 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kWarpS) alloc_tmem(tmem_slot);
+    if (warp == 1) alloc_tmem(tmem_slot);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem_ptr(tmem_slot));
     pdl_wait();      // set-up done; global memory is touched from here on
-    pdl_trigger();
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.err = 0;
-    const int2 range = block_range(g.spans.kblock, b, g.T, q0, BR, false);
-    const int kt0 = range.x / BT64, n_kt = range.x < range.y ? (range.y - 1) / BT64 + 1 - kt0 : 0;
 
-    if (warp == kWarpLoad) {
-        if (lane == 0 && n_kt > 0) {
-            mbar_expect_tx(q_full, kResBytes);
-            for (int kb = 0; kb < 2; ++kb)
-                tma_load_3d(q_s + kb * (kResBytes / 2), &tmQ, q_full, h * HD + kb * 32, row_base + q0, 0);
+    // Every role walks the same items, each with a wait of its own; false when it ran out.
+    auto get_item = [&](int i, Item& it, bool whole_warp) -> bool {
+        const uint32_t full = bar(INFO_FULL + (i & 1)), parity = (uint32_t)(i >> 1) & 1u;
+        if (!(whole_warp ? mbar_wait_warp(full, parity, g.err, 110) : mbar_wait(full, parity, g.err, 110))) return false;
+        it.bh = info[i & 1].bh; it.blk = info[i & 1].blk; it.t0 = info[i & 1].t0; it.n = info[i & 1].n;
+        if (whole_warp) __syncwarp();
+        if (!whole_warp || lane == 0) mbar_arrive(bar(INFO_EMPTY + (i & 1)));
+        return true;
+    };
+
+    if (warp < 4) {
+        set_regs_down<kRegsIssue>();
+        if (warp == 0 && lane == 0) {
+            uint32_t c = 0, qi = 0;                     // loads and non-empty items so far
+            auto make_item = [&](int x, int y) -> Item {
+                Item it;
+                int yb;
+                grouped_item(args.head_group, y * (int)gridDim.x + x, it.bh, yb);
+                it.blk = (int)gridDim.y - 1 - yb;       // causal walks: the longest first
+                const int2 range = block_range(g.spans.kblock, it.bh / g.H, g.T, it.blk * BR, BR, false);
+                it.t0 = range.x / BT64;
+                it.n = range.x < range.y ? (range.y - 1) / BT64 + 1 - it.t0 : 0;
+                return it;
+            };
+            Item it = make_item((int)blockIdx.x, (int)blockIdx.y);
             bool ok = true;
-            const int n_pos = pos_v(n_kt - 1) + 1;
-            int slot = 0;
-            uint32_t round = 0;
-            for (int p = 0; p < n_pos && ok; ++p) {
-                const bool is_k = p == 0 || (p & 1);
-                const int t = p == 0 ? 0 : (is_k ? (p + 1) >> 1 : (p - 2) >> 1);
-                if (t < n_kt) {                          // only K(n_kt) near the end falls outside
-                    if (!mbar_wait(slot_empty(slot), (round & 1u) ^ 1u, g.err, 111)) { ok = false; break; }
-                    mbar_expect_tx(slot_full(slot), kTile);
+            for (int i = 0; ok; ++i) {
+                ok = mbar_wait(bar(INFO_EMPTY + (i & 1)), ((uint32_t)(i >> 1) & 1u) ^ 1u, g.err, 119);
+                if (!ok) break;
+                info[i & 1].bh = it.bh; info[i & 1].blk = it.blk; info[i & 1].t0 = it.t0; info[i & 1].n = it.n;
+                mbar_arrive(bar(INFO_FULL + (i & 1)));
+                if (it.n < 0) break;
+                // The next item is asked for five loads before this one's last and looked up before the last, so that its
+                // loads follow at once (a boundary cost 6,000 clocks when it was asked for only then; asked for at the
+                // start, the last items of long walks are spread worse: 10 % at 8,192 positions).
+                const int last = 2 * it.n - 1;
+                if (it.n == 0) ask_next(answer, bar(NEXT));
+                Item next{0, 0, 0, -1};
+                auto look_up = [&]() -> bool {
+                    if (!mbar_wait(bar(NEXT), (uint32_t)i & 1u, g.err, 120)) return false;
+                    int x, y;
+                    if (next_item(answer, x, y)) next = make_item(x, y);
+                    return true;
+                };
+                if (it.n == 0) ok = look_up();
+                const int h = it.bh % g.H, row0 = (it.bh / g.H) * g.T;
+                for (int p = 0; p < 2 * it.n && ok; ++p, ++c) {
+                    const bool is_k = p == 0 || ((p & 1) && p < 2 * it.n - 1);
+                    const int t = p == 0 ? 0 : p == 2 * it.n - 1 ? it.n - 1 : is_k ? (p + 1) >> 1 : (p - 2) >> 1;
+                    if (p == max(0, last - 5)) ask_next(answer, bar(NEXT));
+                    if (p == last) ok = look_up();
+                    if (!ok) break;
+                    const uint32_t slot = c % kSlots;
+                    ok = mbar_wait(bar(SLOT_EMPTY + slot), ((c / kSlots) & 1u) ^ 1u, g.err, 111);
+                    if (!ok) break;
+                    mbar_expect_tx(bar(SLOT_FULL + slot), kTile);
                     for (int kb = 0; kb < 2; ++kb)
-                        tma_load_3d(ring_s + (uint32_t)slot * kTile + kb * (kTile / 2), is_k ? &tmK : &tmV, slot_full(slot),
-                                    (is_k ? g.C : 2 * g.C) + h * HD + kb * 32, row_base + (kt0 + t) * BT64, 0);
+                        tma_load_3d(ring_s + slot * kTile + kb * (kTile / 2), is_k ? &tmK : &tmV, bar(SLOT_FULL + slot),
+                                    (is_k ? g.C : 2 * g.C) + h * HD + kb * 32, row0 + (it.t0 + t) * BT64, 0);
+                    if (p == 0) {                       // behind the first K: the previous item's last S has to be done with Q
+                        ok = mbar_wait(bar(Q_EMPTY), (qi & 1u) ^ 1u, g.err, 112);
+                        if (!ok) break;
+                        mbar_expect_tx(bar(Q_FULL), kResBytes);
+                        for (int kb = 0; kb < 2; ++kb)
+                            tma_load_3d(q_s + kb * (kResBytes / 2), &tmQ, bar(Q_FULL), h * HD + kb * 32, row0 + it.blk * BR, 0);
+                    }
                 }
-                if (++slot == kSlots) { slot = 0; ++round; }
+                if (it.n > 0) ++qi;
+                it = next;
             }
             if (!ok) settle();
-        }
-    } else if (warp == kWarpS) {
-        if (lane == 0 && n_kt > 0) {
-            constexpr uint32_t idesc = make_idesc_tf32(BR, BT64, false, false);
-            bool ok = mbar_wait(q_full, 0, g.err, 113);
+        } else if (warp == 1 && lane == 0) {
+            constexpr uint32_t idesc = make_idesc_tf32(BR, BT64, false, false), idesc2 = make_idesc_tf32(BR, 2 * BT64, false, false);
             const DescBase qd = kmaj_base(q_s);
-            for (int t = 0; t < n_kt && ok; ++t) {
-                const int buf = t & 1, pk = pos_k(t), slot = pk % kSlots;
-                if (!mbar_wait(slot_full(slot), (uint32_t)(pk / kSlots) & 1u, g.err, 114)) { ok = false; break; }
-                // S[buf] is free once the softmax of tile t - 2 has read it (it then publishes P)
-                if (t >= 2 && !mbar_wait(p_full(buf), ((t - 2) >> 1) & 1u, g.err, 120)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t d = tmem + (uint32_t)buf * 256u;
-                const DescBase kd = kmaj_base(ring_s + (uint32_t)slot * kTile);
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks) {
-                    umma_tf32(d, qd.at(kmaj_off(BR, ks, true)), kd.at(kmaj_off(BT64, ks, false)), idesc, ks > 0 ? 1u : 0u);
-                    umma_tf32(d, qd.at(kmaj_off(BR, ks, false)), kd.at(kmaj_off(BT64, ks, true)), idesc, 1u);
-                }
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                    umma_tf32(d, qd.at(kmaj_off(BR, ks, false)), kd.at(kmaj_off(BT64, ks, false)), idesc, 1u);
-                umma_commit(slot_empty(slot));
-                umma_commit(s_full(buf));
-            }
-        }
-    } else if (warp == kWarpO) {
-        if (lane == 0 && n_kt > 0) {
-            constexpr uint32_t idesc = make_idesc_tf32(BR, HD, false, true);
+            uint32_t c = 0, qi = 0, gt = 0;             // loads, non-empty items, tiles before this item
+            Item it;
             bool ok = true;
-            for (int t = 0; t < n_kt && ok; ++t) {
-                const int buf = t & 1, pv = pos_v(t), slot = pv % kSlots;
-                // P(t) published; the softmax warps read O[buf] of tile t - 2 before publishing it
-                if (!mbar_wait(p_full(buf), (t >> 1) & 1u, g.err, 115)) { ok = false; break; }
-                if (!mbar_wait(slot_full(slot), (uint32_t)(pv / kSlots) & 1u, g.err, 116)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t t0 = tmem + (uint32_t)buf * 256u, d = t0 + 192u;
-                const DescBase vd = mn_base(ring_s + (uint32_t)slot * kTile);
+            for (int i = 0; ok && (ok = get_item(i, it, false)) && it.n >= 0; ++i) {
+                if (it.n == 0) continue;
+                ok = mbar_wait(bar(Q_FULL), qi & 1u, g.err, 113);
+                for (int t = 0; t < it.n && ok; ++t, ++gt) {
+                    const uint32_t ck = c + (uint32_t)pos_k(t), slot = ck % kSlots, buf = gt % kSoft;
+                    // In this order: K and V share the slots, and a wait on a slot's phase is only sound once the load before it
+                    // in the slot has landed.  That was K(t - 2), waited for here, or, next to an item's edge, the V of a
+                    // tile at least three back (P_DONE) or of one whose slot K(0) took over (Q_FULL).
+                    if (gt >= kSoft && !mbar_wait(bar(P_DONE + buf), (gt / kSoft - 1u) & 1u, g.err, 115)) { ok = false; break; }
+                    if (!mbar_wait(bar(SLOT_FULL + slot), (ck / kSlots) & 1u, g.err, 114)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t d = tmem + buf * 128u;
+                    const DescBase kd = kmaj_base(ring_s + slot * kTile);
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) {
-                    umma_tf32_ts(d, t0 + 128u + ks * 8u, vd.at(mn_off(ks, false)), idesc, ks > 0 ? 1u : 0u);  // P_lo V_hi
-                    umma_tf32_ts(d, t0 + 64u + ks * 8u, vd.at(mn_off(ks, true)), idesc, 1u);                  // P_hi V_lo
+                    for (int ks = 0; ks < 8; ++ks) {
+                        const uint64_t k_hl = kd.at(kmaj_off(BT64, ks, false));
+                        umma_tf32(d, qd.at(kmaj_off(BR, ks, false)), k_hl, idesc2, ks > 0 ? 1u : 0u);   // Q_hi K_hi | Q_hi K_lo
+                        umma_tf32(d + 64u, qd.at(kmaj_off(BR, ks, true)), k_hl, idesc, 1u);             // + Q_lo K_hi
+                    }
+                    umma_commit(bar(SLOT_EMPTY + slot));
+                    umma_commit(bar(S_FULL + buf));
                 }
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(d, t0 + 64u + ks * 8u, vd.at(mn_off(ks, false)), idesc, 1u);
-                umma_commit(slot_empty(slot));
-                umma_commit(o_full(buf));
+                if (ok) umma_commit(bar(Q_EMPTY));
+                c += 2u * (uint32_t)it.n;
+                ++qi;
             }
-            if (ok) umma_commit(all_done);
-        }
-    } else if (warp < 8) {
-        const int wg = warp >> 2, lane_group = warp & 3;
-        const int rloc = lane_group * 32 + lane, row = q0 + rloc;
-        const uint32_t t_lane = tmem + ((uint32_t)(lane_group * 32) << 16) + (uint32_t)wg * 256u;
-        const Score sc = make_score<CAP, SLOPE>(1.0f / sqrtf((float)HD), g.cap, g.slopes, h);
-        const float c = (CAP || SLOPE) ? 1.0f : sc.unit;       // from score_tile's result to base-2 units
-        const int2 span = row_range(g.spans.k, b, g.T, row, false);
-        float m = -INFINITY, l = 0.f, corr_prev = 0.f;
-        float o_reg[HD];
+        } else if (lane == 0 && warp >= 2) {
+            // two issuing threads, tiles of their own parity; each O_tile buffer belongs to one of them
+            constexpr uint32_t idesc = make_idesc_tf32(BR, HD, false, true);
+            const uint32_t ob = (uint32_t)warp - 2u, tO = tmem + 384u + 64u * ob;
+            uint32_t c = 0, gt = 0;
+            Item it;
+            bool ok = true;
+            for (int i = 0; ok && (ok = get_item(i, it, false)) && it.n >= 0; ++i) {
+                for (int t = (int)((gt ^ ob) & 1u); t < it.n && ok; t += 2) {
+                    const uint32_t ga = gt + (uint32_t)t, cv = c + (uint32_t)pos_v(t, it.n), slot = cv % kSlots, buf = ga % kSoft;
+                    // In this order: O_FREE says that the tile two back has been added, so that the buffer's P of three tiles
+                    // back, which the other thread waited for, is past; P_FULL that every K up to this tile's has landed; the load
+                    // before V(t) in its slot was one of those or a V of this thread's.
+                    if (ga >= 2 && !mbar_wait(bar(O_FREE + ob), ((ga >> 1) - 1u) & 1u, g.err, 118)) { ok = false; break; }
+                    if (!mbar_wait(bar(P_FULL + buf), (ga / kSoft) & 1u, g.err, 116)) { ok = false; break; }
+                    if (!mbar_wait(bar(SLOT_FULL + slot), (cv / kSlots) & 1u, g.err, 117)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t p_hi = tmem + buf * 128u, p_lo = p_hi + 64u;
+                    const DescBase vd = mn_base(ring_s + slot * kTile);
 #pragma unroll
-        for (int i = 0; i < HD; ++i) o_reg[i] = 0.f;
+                    for (int ks = 0; ks < 8; ++ks) {
+                        umma_tf32_ts(tO, p_lo + ks * 8u, vd.at(mn_off(ks, false)), idesc, ks > 0 ? 1u : 0u);
+                        umma_tf32_ts(tO, p_hi + ks * 8u, vd.at(mn_off(ks, true)), idesc, 1u);
+                    }
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(tO, p_hi + ks * 8u, vd.at(mn_off(ks, false)), idesc, 1u);
+                    umma_commit(bar(SLOT_EMPTY + slot));
+                    umma_commit(bar(P_DONE + buf));
+                    mbar_arrive(bar(O_FULL + ob));      // hands on what P_FULL published: the tile's (r, sum)
+                    umma_commit(bar(O_FULL + ob));
+                }
+                c += 2u * (uint32_t)it.n;
+                gt += (uint32_t)it.n;
+            }
+        }
+    } else if (warp < 4 + 4 * kSoft) {
+        set_regs_down<kRegsSoft>();
+        const int wg = (warp - 4) >> 2, lane_group = warp & 3, rloc = lane_group * 32 + lane;
+        const uint32_t t_s = tmem + ((uint32_t)(lane_group * 32) << 16) + (uint32_t)wg * 128u;
+        uint32_t gt = 0, use = 0;
+        Item it;
         bool ok = true;
-
-        auto add_output = [&](int t, float corr) -> bool {
-            if (!mbar_wait_warp(o_full(wg), (t >> 1) & 1u, g.err, 117)) return false;
-            tc_fence_after();
-            uint32_t r0[32], r1[32];
-            tmem_ld32(t_lane + 192u, r0);
-            tmem_ld32(t_lane + 224u, r1);
-            tmem_ld_wait();
+        for (int i = 0; ok && (ok = get_item(i, it, true)) && it.n >= 0; ++i) {
+            const int b = it.bh / g.H, h = it.bh % g.H, row = it.blk * BR + rloc;
+            const Score sc = make_score<CAP, SLOPE>(1.0f / sqrtf((float)HD), g.cap, g.slopes, h);
+            const int2 span = row_range(g.spans.k, b, g.T, row, false);
+            for (int t = (wg + kSoft - (int)(gt % kSoft)) % kSoft; t < it.n; t += kSoft, ++use) {
+                if (!mbar_wait_warp(bar(S_FULL + wg), use & 1u, g.err, 121)) { ok = false; break; }
+                tc_fence_after();
+                const int key0 = (it.t0 + t) * BT64;
+                const bool whole = key0 >= span.x && key0 + BT64 <= span.y;
+                auto mask = [&](float (&z)[CH], int k0) {
+                    if (!whole) {
+                        const uint32_t bits = column_bits<CH>(span, k0);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                o_reg[i] = fmaf(o_reg[i], corr, __uint_as_float(r0[i]));
-                o_reg[32 + i] = fmaf(o_reg[32 + i], corr, __uint_as_float(r1[i]));
-            }
-            return true;
-        };
-
-        int last = -1;
-        for (int t = wg; t < n_kt && ok; t += 2) {
-            // this warpgroup's previous tile first: the P V product of this tile overwrites O[wg]
-            if (last >= 0 && !add_output(last, corr_prev)) { ok = false; break; }
-            if (!mbar_wait_warp(s_full(wg), (t >> 1) & 1u, g.err, 118)) { ok = false; break; }
-            tc_fence_after();
-            float s0[32], s1[32];
-            {
-                uint32_t r0[32], r1[32];
-                tmem_ld32(t_lane, r0);
-                tmem_ld32(t_lane + 32u, r1);
-                tmem_ld_wait();
+                        for (int k = 0; k < CH; ++k)
+                            if (!(bits >> k & 1u)) z[k] = -INFINITY;
+                    }
+                };
+                float top = -INFINITY;
+#pragma unroll 1
+                for (int c0 = 0; c0 < BT64; c0 += CH) {
+                    float z[CH], none[CH];
+                    uint32_t r[CH];
+                    tmem_ldn(t_s + c0, r);
+                    tmem_ld_wait();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    s0[i] = __uint_as_float(r0[i]);
-                    s1[i] = __uint_as_float(r1[i]);
+                    for (int k = 0; k < CH; ++k) z[k] = __uint_as_float(r[k]);
+                    if (SLOPE) score_tile<CAP, SLOPE, false, true, CH>(z, none, sc, row - key0 - c0, 0.f);   // else the maximum is at that of the product
+                    mask(z, key0 + c0);
+#pragma unroll
+                    for (int k = 0; k < CH; ++k) top = fmaxf(top, z[k]);
                 }
-            }
-            const int key0 = (kt0 + t) * BT64;
-            score_tile<CAP, SLOPE, 32>(s0, sc, row - key0);
-            score_tile<CAP, SLOPE, 32>(s1, sc, row - key0 - 32);
-            if (key0 < span.x || key0 + BT64 > span.y) {      // this row does not read the whole tile
+                const bool none_read = top == -INFINITY;                // every P of this tile is zero
+                float ref = 0.f, sum = 0.f;
+                if (!none_read) ref = SLOPE ? top : CAP ? sc.to_log2 * tanh_any(top * sc.unit) : top * sc.unit;
+#pragma unroll 1
+                for (int c0 = 0; c0 < BT64; c0 += CH) {
+                    float z[CH], none[CH];
+                    uint32_t hi[CH], lo[CH];
+                    tmem_ldn(t_s + c0, hi);
+                    tmem_ldn(t_s + 64u + c0, lo);
+                    tmem_ld_wait();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    if (key0 + i < span.x || key0 + i >= span.y) s0[i] = -INFINITY;
-                    if (key0 + 32 + i < span.x || key0 + 32 + i >= span.y) s1[i] = -INFINITY;
+                    for (int k = 0; k < CH; ++k) z[k] = __uint_as_float(hi[k]) + __uint_as_float(lo[k]);
+                    score_tile<CAP, SLOPE, false, true, CH>(z, none, sc, row - key0 - c0, ref);
+                    mask(z, key0 + c0);
+#pragma unroll
+                    for (int k = 0; k < CH; ++k) {
+                        const float p = ex2_approx(z[k]);
+                        sum += p;
+                        split_tf32_int(p, hi[k], lo[k]);
+                    }
+                    tmem_stn(t_s + c0, hi);                             // P_hi over S, P_lo over its small half
+                    tmem_stn(t_s + 64u + c0, lo);
                 }
+                float* stat = tile_stat + ((gt + (uint32_t)t) & 7u) * (2 * BR) + rloc;
+                stat[0] = none_read ? -INFINITY : ref;
+                stat[BR] = sum;
+                __threadfence_block();
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(P_FULL + wg));
             }
-            float mx = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) mx = fmaxf(mx, fmaxf(s0[i], s1[i]));
-            // a row that has read nothing yet keeps its maximum at -inf; the arithmetic stays finite
-            const float m_new = fmaxf(m, mx);
-            const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
-            const float corr = ex2_approx((m - m_use) * c);
-            const float mc = m_use * c;
-            float sum = 0.f;
-            uint32_t hi[32], lo[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const float p = ex2_approx(fmaf(s0[i], c, -mc));
-                sum += p;
-                split_tf32_int(p, hi[i], lo[i]);
-            }
-            tmem_st32(t_lane + 64u, hi);
-            tmem_st32(t_lane + 128u, lo);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const float p = ex2_approx(fmaf(s1[i], c, -mc));
-                sum += p;
-                split_tf32_int(p, hi[i], lo[i]);
-            }
-            tmem_st32(t_lane + 96u, hi);
-            tmem_st32(t_lane + 160u, lo);
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full(wg));
-            l = fmaf(l, corr, sum);
-            m = m_new;
-            corr_prev = corr;
-            last = t;
+            gt += (uint32_t)it.n;
         }
-        if (ok && last >= 0) ok = add_output(last, corr_prev);
-
-        // merge: warpgroup 1 hands (m, l, O) of its rows to warpgroup 0 through the first ring slots, idle once
-        // every product has completed
-        float* xch = reinterpret_cast<float*>(smem_ptr(ring_s));   // [128][66]
-        if (wg == 1) {
-            if (ok && n_kt > 0) ok = mbar_wait_warp(all_done, 0, g.err, 121);
-            float* dst = xch + rloc * 66;
-            dst[64] = m;
-            dst[65] = l;
+    } else {
+        set_regs_up<kRegsAdd>();
+        const int lane_group = warp & 3, rloc = lane_group * 32 + lane;
+        const uint32_t t_o = tmem + 384u + ((uint32_t)(lane_group * 32) << 16);
+        uint32_t gt = 0;
+        Item it;
+        bool ok = true;
+        for (int i = 0; ok && (ok = get_item(i, it, true)) && it.n >= 0; ++i) {
+            float acc[HD], m = -INFINITY, l = 0.f;
 #pragma unroll
-            for (int i = 0; i < HD; ++i) dst[i] = o_reg[i];
-            __threadfence_block();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(merge_full);
-        } else {
-            if (ok) ok = mbar_wait_warp(merge_full, 0, g.err, 119);
-            if (ok) {
-                const float* src = xch + rloc * 66;
-                const float m1 = src[64], l1 = src[65];
-                const float mm = fmaxf(m, m1), m_use = mm == -INFINITY ? 0.f : mm;
-                const float f0 = ex2_approx((m - m_use) * c), f1 = ex2_approx((m1 - m_use) * c);
-                l = l * f0 + l1 * f1;
-                const float inv = l > 0.f ? 1.0f / l : 0.f;             // a row that reads nothing is zero
+            for (int k = 0; k < HD; ++k) acc[k] = 0.f;
+            for (int t = 0; t < it.n; ++t, ++gt) {
+                const uint32_t ob = gt & 1u;
+                if (!mbar_wait_warp(bar(O_FULL + ob), (gt >> 1) & 1u, g.err, 122)) { ok = false; break; }
+                tc_fence_after();
+                uint32_t r0[32], r1[32];
+                tmem_ld32(t_o + 64u * ob, r0);
+                tmem_ld32(t_o + 64u * ob + 32u, r1);
+                const float* stat = tile_stat + (gt & 7u) * (2 * BR) + rloc;
+                const float ref = stat[0], sum = stat[BR];
+                tmem_ld_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(O_FREE + ob));           // before the arithmetic: a product waits for this
+                const float top = fmaxf(m, ref), use = top == -INFINITY ? 0.f : top;
+                const float keep = ex2_approx(m - use), join = ex2_approx(ref - use);
+                l = l * keep + sum * join;
+                m = top;
 #pragma unroll
-                for (int i = 0; i < HD; ++i) o_reg[i] = (o_reg[i] * f0 + src[i] * f1) * inv;
-                const int wrow0 = q0 + lane_group * 32, nvalid = max(0, min(32, g.T - wrow0));
-                const int64_t off0 = ((int64_t)(row_base + wrow0)) * g.C + h * HD;
-                float* tile = reinterpret_cast<float*>(smem_ptr(ring_s + 2u * kTile) + (uint32_t)lane_group * kRowTileBytes);
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    float v[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = o_reg[half * 32 + i];
-                    warp_rows_store(v, tile, lane, nvalid, g.o ? g.o + off0 + half * 32 : nullptr,
-                                    g.o_hi ? g.o_hi + off0 + half * 32 : nullptr, g.o_hi ? g.o_lo + off0 + half * 32 : nullptr,
-                                    g.C, nullptr);
+                for (int k = 0; k < 32; ++k) {
+                    acc[k] = fmaf(acc[k], keep, __uint_as_float(r0[k]) * join);
+                    acc[32 + k] = fmaf(acc[32 + k], keep, __uint_as_float(r1[k]) * join);
                 }
-                if (row < g.T) g.lse[((int64_t)b * g.H + h) * g.T + row] = l > 0.f ? (mm * c + log2f(l)) * kLn2 : -INFINITY;
+            }
+            const int b = it.bh / g.H, h = it.bh % g.H, row = it.blk * BR + rloc;
+            if (ok && row < g.T) {
+                const float inv = l > 0.f ? 1.0f / l : 0.f;             // a row that reads nothing is zero
+                const int64_t at = ((int64_t)b * g.T + row) * g.C + (int64_t)h * HD;
+#pragma unroll
+                for (int q = 0; q < HD; q += 8) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = acc[q + e] * inv;
+                    store_sector(v, at + q, g.o, g.o_hi, g.o_lo);
+                }
+                g.lse[((int64_t)b * g.H + h) * g.T + row] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
             }
         }
     }
 
     tc_fence_before();
     __syncthreads();
-    if (warp == kWarpS) free_tmem(tmem);
+    if (warp == 1) free_tmem(tmem);
 }
 
 // -------------------------------------------------------------------------------------- backward, dK and dV
@@ -534,7 +588,7 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
             tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 32; ++i) p[i] = __uint_as_float(s[i]) + __uint_as_float(lo[i]);
-            score_tile_grad<CAP, SLOPE, 32>(p, f, sc, key - q0);
+            score_tile<CAP, SLOPE, true, false, 32>(p, f, sc, key - q0, 0.f);
             const bool whole = q0 >= span.x && q0 + 32 <= span.y;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -870,9 +924,9 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
                 tmem_ld_wait();
 #pragma unroll
                 for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(s[i]);
-                score_tile_grad<CAP, SLOPE, 32>(x, f, sc, row - kh);
+                score_tile<CAP, SLOPE, true, false, 32>(x, f, sc, row - kh, L);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] = ex2_approx(x[i] - L);
+                for (int i = 0; i < 32; ++i) x[i] = ex2_approx(x[i]);
                 if (kh < span.x || kh + 32 > span.y) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i)

@@ -60,28 +60,6 @@ struct Mod128Args {
 //  MN-major 32-row tile: 4 column groups of [hi | lo][32 rows][128 B]; a k-step is 8 rows
 __device__ __forceinline__ constexpr uint32_t mn_off(int ks, bool lo) { return (lo ? BT_ * 128u : 0u) + (uint32_t)ks * 1024u; }
 
-template <int N>
-__device__ __forceinline__ void set_regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void set_regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
-}
-
 template <int PASS, bool CAP, bool SLOPE>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_constant__ CUtensorMap tmB1,
@@ -285,14 +263,14 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     uint32_t r[16], q[16];
-                    tmem_ld16(tb + 16u * half, r);
-                    tmem_ld16(tb + 32u + 16u * half, q);
+                    tmem_ldn(tb + 16u * half, r);
+                    tmem_ldn(tb + 32u + 16u * half, q);
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[16 * half + i] = __uint_as_float(r[i]) + __uint_as_float(q[i]);
                 }
                 float none[32];
-                score_tile_grad<CAP, SLOPE, 32>(x, none, sc, own - s0);
+                score_tile<CAP, SLOPE, false, false, 32>(x, none, sc, own - s0, 0.f);
                 if (!whole) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
@@ -311,8 +289,8 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
                         sum += p;
                         split_tf32_int(p, hi[i], lo[i]);
                     }
-                    tmem_st16(tb + 16u * half, hi);
-                    tmem_st16(tb + 32u + 16u * half, lo);
+                    tmem_stn(tb + 16u * half, hi);
+                    tmem_stn(tb + 32u + 16u * half, lo);
                 }
                 tile_stat[(t & 3) * 256 + rloc] = mx;
                 tile_stat[(t & 3) * 256 + 128 + rloc] = sum;
@@ -323,14 +301,14 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
                     const int sh = s0 + 16 * half;
                     float x[16], f[16];
                     uint32_t r[16], y[16];
-                    tmem_ld16(tb + 16u * half, r);
-                    tmem_ld16(tb + 32u + 16u * half, y);
+                    tmem_ldn(tb + 16u * half, r);
+                    tmem_ldn(tb + 32u + 16u * half, y);
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[i] = kHasY ? __uint_as_float(r[i]) : __uint_as_float(r[i]) + __uint_as_float(y[i]);
-                    score_tile_grad<CAP, SLOPE, 16>(x, f, sc, own - sh);
+                    score_tile<CAP, SLOPE, true, false, 16>(x, f, sc, own - sh, kKeys ? 0.f : L);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = ex2_approx(x[i] - (kKeys ? __shfl_sync(0xffffffffu, Lq, 16 * half + i) : L));
+                    for (int i = 0; i < 16; ++i) x[i] = ex2_approx(kKeys ? x[i] - __shfl_sync(0xffffffffu, Lq, 16 * half + i) : x[i]);
                     if (!whole) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
@@ -345,8 +323,8 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
                         }
                         split_tf32_int(z, r[i], y[i]);
                     }
-                    tmem_st16(tb + 16u * half, r);           // Z hi over X
-                    tmem_st16(tb + 32u + 16u * half, y);     // Z lo over Y
+                    tmem_stn(tb + 16u * half, r);           // Z hi over X
+                    tmem_stn(tb + 32u + 16u * half, y);     // Z lo over Y
                 }
             }
             tmem_st_wait();
