@@ -188,6 +188,20 @@ def _stream(stream):
     return stream
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_this_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
+def _call(fn, stream, *args):
+    """One C call on `stream`, by default the current one (its handle without a Stream object: the small operators
+    take a few microseconds on the GPU, and half of that here)."""
+    if stream is None:
+        stream = _raw_stream(_this_device()) if _raw_stream and torch.cuda.is_initialized() else _stream(None)
+    st = fn(*args, stream)
+    if st:
+        _check(st)
+
+
 def _check(st):
     if st != 0:
         raise BtError(st, (lib().bt_last_error() or b"").decode())
@@ -584,12 +598,17 @@ def bt_op_attention_bwd(qkv, o, lse, d_o, B, T, C, H, dqkv, dqkv_split, scratch,
 
 def _arr(t, dtype=torch.float32):
     """Address of a device array; a tensor must be contiguous, of `dtype` and on the current device."""
-    if isinstance(t, torch.Tensor):
-        if t.dtype != dtype:
-            raise ValueError(f"expected a {dtype} tensor, got {t.dtype}")
-        if not t.is_cuda or t.device.index != torch.cuda.current_device():
-            raise ValueError(f"expected a tensor on the current device, got one on {t.device}")
-    return _ptr(t)
+    if t is None or type(t) is int:
+        return t
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(type(t))
+    if t.dtype is not dtype:
+        raise ValueError(f"expected a {dtype} tensor, got {t.dtype}")
+    if not t.is_cuda or t.get_device() != _this_device():
+        raise ValueError(f"expected a tensor on the current device, got one on {t.device}")
+    if not t.is_contiguous():
+        raise ValueError("tensor arguments must be contiguous")
+    return t.data_ptr()
 
 
 def make_rope(rot_dim, interleaved=False, base=10000.0, scaling=BT_ROPE_PLAIN, factor=1.0, low=1.0, high=32.0,
@@ -613,13 +632,11 @@ def _check_mod(mod, B, T, H):
 
 
 def bt_op_rope_fwd(x, pos, N, T, C, H, rope, y, y_split=None, stream=None):
-    _check(lib().bt_op_rope_fwd(_arr(x), _arr(pos, torch.int32), N, T, C, H, ctypes.byref(rope), _arr(y), _arr(y_split),
-                                _stream(stream)))
+    _call(lib().bt_op_rope_fwd, stream, _arr(x), _arr(pos, torch.int32), N, T, C, H, rope, _arr(y), _arr(y_split))
 
 
 def bt_op_rope_bwd(dy, pos, N, T, C, H, rope, dx, dx_split=None, stream=None):
-    _check(lib().bt_op_rope_bwd(_arr(dy), _arr(pos, torch.int32), N, T, C, H, ctypes.byref(rope), _arr(dx), _arr(dx_split),
-                                _stream(stream)))
+    _call(lib().bt_op_rope_bwd, stream, _arr(dy), _arr(pos, torch.int32), N, T, C, H, rope, _arr(dx), _arr(dx_split))
 
 
 def bt_op_attention_spans_bytes(B, T):
@@ -627,8 +644,8 @@ def bt_op_attention_spans_bytes(B, T):
 
 
 def bt_op_attention_spans(doc, prefix, window, B, T, spans, spans_bytes, stream=None):
-    _check(lib().bt_op_attention_spans(_arr(doc, torch.int32), _arr(prefix, torch.int32), window, B, T,
-                                       _arr(spans, torch.uint8), spans_bytes, _stream(stream)))
+    _call(lib().bt_op_attention_spans, stream, _arr(doc, torch.int32), _arr(prefix, torch.int32), window, B, T,
+          _arr(spans, torch.uint8), spans_bytes)
 
 
 def bt_op_attention_mod_scratch_bytes(B, T, C, H):
@@ -637,30 +654,28 @@ def bt_op_attention_mod_scratch_bytes(B, T, C, H):
 
 def bt_op_attention_mod_fwd(qkv, qkv_split, B, T, C, H, mod, o, o_split, lse, scratch, scratch_bytes, flags=0, stream=None):
     _check_mod(mod, B, T, H)
-    _check(lib().bt_op_attention_mod_fwd(_arr(qkv), _arr(qkv_split), B, T, C, H, ctypes.byref(mod), _arr(o), _arr(o_split),
-                                         _arr(lse), _arr(scratch, torch.uint8), scratch_bytes, flags, _stream(stream)))
+    _call(lib().bt_op_attention_mod_fwd, stream, _arr(qkv), _arr(qkv_split), B, T, C, H, mod, _arr(o), _arr(o_split),
+          _arr(lse), _arr(scratch, torch.uint8), scratch_bytes, flags)
 
 
 def bt_op_attention_mod_bwd(qkv, qkv_split, o, lse, d_o, d_o_split, B, T, C, H, mod, dqkv, dqkv_split, scratch,
                             scratch_bytes, flags=0, stream=None):
     _check_mod(mod, B, T, H)
-    _check(lib().bt_op_attention_mod_bwd(_arr(qkv), _arr(qkv_split), _arr(o), _arr(lse), _arr(d_o), _arr(d_o_split), B, T,
-                                         C, H, ctypes.byref(mod), _arr(dqkv), _arr(dqkv_split), _arr(scratch, torch.uint8),
-                                         scratch_bytes, flags, _stream(stream)))
+    _call(lib().bt_op_attention_mod_bwd, stream, _arr(qkv), _arr(qkv_split), _arr(o), _arr(lse), _arr(d_o), _arr(d_o_split),
+          B, T, C, H, mod, _arr(dqkv), _arr(dqkv_split), _arr(scratch, torch.uint8), scratch_bytes, flags)
 
 
 def bt_op_attention_mod_check(scratch, stream=None):
-    _check(lib().bt_op_attention_mod_check(_arr(scratch, torch.uint8), _stream(stream)))
+    _call(lib().bt_op_attention_mod_check, stream, _arr(scratch, torch.uint8))
 
 
 def bt_op_dropout_fwd(x, residual, n, p, seed, offset, y, y_split=None, d_step=None, stream=None):
-    _check(lib().bt_op_dropout_fwd(_arr(x), _arr(residual), n, p, seed, offset, _arr(y), _arr(y_split),
-                                   _arr(d_step, torch.int64), _stream(stream)))
+    _call(lib().bt_op_dropout_fwd, stream, _arr(x), _arr(residual), n, p, seed, offset, _arr(y), _arr(y_split),
+          _arr(d_step, torch.int64))
 
 
 def bt_op_dropout_bwd(dy, n, p, seed, offset, dx, dx_split=None, d_step=None, stream=None):
-    _check(lib().bt_op_dropout_bwd(_arr(dy), n, p, seed, offset, _arr(dx), _arr(dx_split), _arr(d_step, torch.int64),
-                                   _stream(stream)))
+    _call(lib().bt_op_dropout_bwd, stream, _arr(dy), n, p, seed, offset, _arr(dx), _arr(dx_split), _arr(d_step, torch.int64))
 
 
 def bt_op_gelu_fwd(x, n, tanh_form, y, y_split, stream=None):

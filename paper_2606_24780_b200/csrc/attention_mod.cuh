@@ -112,6 +112,16 @@ __device__ __forceinline__ int2 row_range(const int2* spans, int b, int T, int r
 }
 
 // ---------------------------------------------------------------- pieces of the persistent kernels
+// One lane of a converged warp.  The issuing roles run on whole warps and put only the products behind this: the
+// compiler then keeps their descriptors in uniform registers, and an MMA is issued every 16 clocks at N = 32 and every 32 at N = 64,
+// which is the pipe's own rate.  (Behind a test of the lane number each descriptor is moved there by
+// itself: 45 to 60 clocks an MMA, whatever its shape.)
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 // Register split of a kernel of several warpgroups: each gives up or takes registers of the block's launch total.
 template <int N>
 __device__ __forceinline__ void set_regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -155,6 +165,15 @@ __device__ __forceinline__ void st_sector(float* p, const float (&v)[8]) {
                  "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
 }
 
+__device__ __forceinline__ void load_sector(const float* p, float (&v)[8]) {
+    if ((reinterpret_cast<uintptr_t>(p) & 31u) == 0) {
+        ld_sector(p, v);
+    } else {
+        const float4 a = ld4(p, 0), b = ld4(p, 1);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+}
 // Eight values of a row to the raw array and / or the planes.  Rows start on 16 bytes only (C is a multiple of 16
 // floats, and so is every head's first column, but the caller's pointer need not be 32-byte aligned).
 __device__ __forceinline__ void store_sector(const float (&v)[8], int64_t at, float* raw, float* hi, float* lo) {
@@ -211,6 +230,34 @@ __device__ __forceinline__ void grouped_item(int head_group, int id, int& bh, in
 struct Item {
     int bh, blk, t0, n;      // n tiles from tile t0 on; n < 0: no more items
 };
+// Item i for one role (a thread, or a whole warp); false when the wait ran out.
+__device__ __forceinline__ bool get_item(const volatile Item* info, uint32_t full, uint32_t empty, int i, Item& it, int* err, bool whole_warp) {
+    const uint32_t parity = (uint32_t)(i >> 1) & 1u, at = 8u * (uint32_t)(i & 1);
+    if (!(whole_warp ? tc::mbar_wait_warp(full + at, parity, err, 110) : tc::mbar_wait(full + at, parity, err, 110))) return false;
+    it.bh = info[i & 1].bh; it.blk = info[i & 1].blk; it.t0 = info[i & 1].t0; it.n = info[i & 1].n;
+    if (whole_warp) __syncwarp();
+    if (!whole_warp || (threadIdx.x & 31) == 0) tc::mbar_arrive(empty + at);
+    return true;
+}
+// Hands item i to the other roles.
+__device__ __forceinline__ bool put_item(volatile Item* info, uint32_t full, uint32_t empty, int i, const Item& it, int* err) {
+    const uint32_t at = 8u * (uint32_t)(i & 1);
+    if (!tc::mbar_wait(empty + at, ((uint32_t)(i >> 1) & 1u) ^ 1u, err, 119)) return false;
+    info[i & 1].bh = it.bh; info[i & 1].blk = it.blk; info[i & 1].t0 = it.t0; info[i & 1].n = it.n;
+    tc::mbar_arrive(full + at);
+    return true;
+}
+// The item of block (x, y): its rows' range as tiles of `tile` rows.
+__device__ __forceinline__ Item make_item(const AttnModArgs& g, int head_group, int x, int y, bool keys, int rows, int tile) {
+    Item it;
+    int yb;
+    grouped_item(head_group, y * (int)gridDim.x + x, it.bh, yb);
+    it.blk = keys ? yb : (int)gridDim.y - 1 - yb;        // causal walks: the longest first
+    const int2 r = block_range(keys ? g.spans.qblock : g.spans.kblock, it.bh / g.H, g.T, it.blk * rows, rows, keys);
+    it.t0 = r.x / tile;
+    it.n = r.x < r.y ? (r.y - 1) / tile + 1 - it.t0 : 0;
+    return it;
+}
 
 // Bit k set: column k0 + k lies in the range (N <= 32 columns; the tests of single bits are an instruction each).
 template <int N>

@@ -55,8 +55,7 @@ __device__ __forceinline__ void settle() {
 //   warp 0      TMA producer and scheduler: the next item and its range of tiles; Q once per item, K and V tiles through one
 //               ring of four slots, K one tile ahead of V
 //   warp 1      S = Q K^T: [K_hi | K_lo] as one operand of 128 rows, the small terms into the second 64 columns
-//   warps 2, 3  O_tile = P V on alternate tiles, P from tensor memory, from zero in every tile (one thread issues an MMA
-//               about every 60 clocks; 24 of them would be 1,550 of a tile's 1,660 clocks of tensor pipe)
+//   warps 2, 3  O_tile = P V on alternate tiles, P from tensor memory, from zero in every tile
 //   warps 4-15  three softmax warpgroups on tiles in turn, thread = row.  Every tile is normalised by its own row
 //               maximum, so they carry nothing from tile to tile; the maximum is taken over the large half of the
 //               scores (any reference near it will do), then P = exp2(z - r)
@@ -111,48 +110,29 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     pdl_wait();      // set-up done; global memory is touched from here on
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.err = 0;
 
-    // Every role walks the same items, each with a wait of its own; false when it ran out.
-    auto get_item = [&](int i, Item& it, bool whole_warp) -> bool {
-        const uint32_t full = bar(INFO_FULL + (i & 1)), parity = (uint32_t)(i >> 1) & 1u;
-        if (!(whole_warp ? mbar_wait_warp(full, parity, g.err, 110) : mbar_wait(full, parity, g.err, 110))) return false;
-        it.bh = info[i & 1].bh; it.blk = info[i & 1].blk; it.t0 = info[i & 1].t0; it.n = info[i & 1].n;
-        if (whole_warp) __syncwarp();
-        if (!whole_warp || lane == 0) mbar_arrive(bar(INFO_EMPTY + (i & 1)));
-        return true;
+    auto next = [&](int i, Item& it, bool whole_warp) -> bool {     // every role walks the same items
+        return get_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i, it, g.err, whole_warp);
     };
 
     if (warp < 4) {
         set_regs_down<kRegsIssue>();
         if (warp == 0 && lane == 0) {
             uint32_t c = 0, qi = 0;                     // loads and non-empty items so far
-            auto make_item = [&](int x, int y) -> Item {
-                Item it;
-                int yb;
-                grouped_item(args.head_group, y * (int)gridDim.x + x, it.bh, yb);
-                it.blk = (int)gridDim.y - 1 - yb;       // causal walks: the longest first
-                const int2 range = block_range(g.spans.kblock, it.bh / g.H, g.T, it.blk * BR, BR, false);
-                it.t0 = range.x / BT64;
-                it.n = range.x < range.y ? (range.y - 1) / BT64 + 1 - it.t0 : 0;
-                return it;
-            };
-            Item it = make_item((int)blockIdx.x, (int)blockIdx.y);
+            Item it = make_item(g, args.head_group, (int)blockIdx.x, (int)blockIdx.y, false, BR, BT64);
             bool ok = true;
             for (int i = 0; ok; ++i) {
-                ok = mbar_wait(bar(INFO_EMPTY + (i & 1)), ((uint32_t)(i >> 1) & 1u) ^ 1u, g.err, 119);
-                if (!ok) break;
-                info[i & 1].bh = it.bh; info[i & 1].blk = it.blk; info[i & 1].t0 = it.t0; info[i & 1].n = it.n;
-                mbar_arrive(bar(INFO_FULL + (i & 1)));
-                if (it.n < 0) break;
+                ok = put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i, it, g.err);
+                if (!ok || it.n < 0) break;
                 // The next item is asked for five loads before this one's last and looked up before the last, so that its
                 // loads follow at once (a boundary cost 6,000 clocks when it was asked for only then; asked for at the
                 // start, the last items of long walks are spread worse: 10 % at 8,192 positions).
                 const int last = 2 * it.n - 1;
                 if (it.n == 0) ask_next(answer, bar(NEXT));
-                Item next{0, 0, 0, -1};
+                Item follows{0, 0, 0, -1};
                 auto look_up = [&]() -> bool {
                     if (!mbar_wait(bar(NEXT), (uint32_t)i & 1u, g.err, 120)) return false;
                     int x, y;
-                    if (next_item(answer, x, y)) next = make_item(x, y);
+                    if (next_item(answer, x, y)) follows = make_item(g, args.head_group, x, y, false, BR, BT64);
                     return true;
                 };
                 if (it.n == 0) ok = look_up();
@@ -179,28 +159,29 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     }
                 }
                 if (it.n > 0) ++qi;
-                it = next;
+                it = follows;
             }
             if (!ok) settle();
-        } else if (warp == 1 && lane == 0) {
+        } else if (warp == 1) {
             constexpr uint32_t idesc = make_idesc_tf32(BR, BT64, false, false), idesc2 = make_idesc_tf32(BR, 2 * BT64, false, false);
             const DescBase qd = kmaj_base(q_s);
             uint32_t c = 0, qi = 0, gt = 0;             // loads, non-empty items, tiles before this item
             Item it;
             bool ok = true;
-            for (int i = 0; ok && (ok = get_item(i, it, false)) && it.n >= 0; ++i) {
+            for (int i = 0; ok && (ok = next(i, it, true)) && it.n >= 0; ++i) {
                 if (it.n == 0) continue;
-                ok = mbar_wait(bar(Q_FULL), qi & 1u, g.err, 113);
+                ok = mbar_wait_warp(bar(Q_FULL), qi & 1u, g.err, 113);
                 for (int t = 0; t < it.n && ok; ++t, ++gt) {
                     const uint32_t ck = c + (uint32_t)pos_k(t), slot = ck % kSlots, buf = gt % kSoft;
                     // In this order: K and V share the slots, and a wait on a slot's phase is only sound once the load before it
                     // in the slot has landed.  That was K(t - 2), waited for here, or, next to an item's edge, the V of a
                     // tile at least three back (P_DONE) or of one whose slot K(0) took over (Q_FULL).
-                    if (gt >= kSoft && !mbar_wait(bar(P_DONE + buf), (gt / kSoft - 1u) & 1u, g.err, 115)) { ok = false; break; }
-                    if (!mbar_wait(bar(SLOT_FULL + slot), (ck / kSlots) & 1u, g.err, 114)) { ok = false; break; }
+                    if (gt >= kSoft && !mbar_wait_warp(bar(P_DONE + buf), (gt / kSoft - 1u) & 1u, g.err, 115)) { ok = false; break; }
+                    if (!mbar_wait_warp(bar(SLOT_FULL + slot), (ck / kSlots) & 1u, g.err, 114)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t d = tmem + buf * 128u;
                     const DescBase kd = kmaj_base(ring_s + slot * kTile);
+                    if (elect_one()) {
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks) {
                         const uint64_t k_hl = kd.at(kmaj_off(BT64, ks, false));
@@ -209,30 +190,33 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     }
                     umma_commit(bar(SLOT_EMPTY + slot));
                     umma_commit(bar(S_FULL + buf));
+                    if (t == it.n - 1) umma_commit(bar(Q_EMPTY));
+                    }
+                    __syncwarp();
                 }
-                if (ok) umma_commit(bar(Q_EMPTY));
                 c += 2u * (uint32_t)it.n;
                 ++qi;
             }
-        } else if (lane == 0 && warp >= 2) {
-            // two issuing threads, tiles of their own parity; each O_tile buffer belongs to one of them
+        } else if (warp >= 2) {
+            // two issuing warps, tiles of their own parity; each O_tile buffer belongs to one of them
             constexpr uint32_t idesc = make_idesc_tf32(BR, HD, false, true);
             const uint32_t ob = (uint32_t)warp - 2u, tO = tmem + 384u + 64u * ob;
             uint32_t c = 0, gt = 0;
             Item it;
             bool ok = true;
-            for (int i = 0; ok && (ok = get_item(i, it, false)) && it.n >= 0; ++i) {
+            for (int i = 0; ok && (ok = next(i, it, true)) && it.n >= 0; ++i) {
                 for (int t = (int)((gt ^ ob) & 1u); t < it.n && ok; t += 2) {
                     const uint32_t ga = gt + (uint32_t)t, cv = c + (uint32_t)pos_v(t, it.n), slot = cv % kSlots, buf = ga % kSoft;
                     // In this order: O_FREE says that the tile two back has been added, so that the buffer's P of three tiles
                     // back, which the other thread waited for, is past; P_FULL that every K up to this tile's has landed; the load
                     // before V(t) in its slot was one of those or a V of this thread's.
-                    if (ga >= 2 && !mbar_wait(bar(O_FREE + ob), ((ga >> 1) - 1u) & 1u, g.err, 118)) { ok = false; break; }
-                    if (!mbar_wait(bar(P_FULL + buf), (ga / kSoft) & 1u, g.err, 116)) { ok = false; break; }
-                    if (!mbar_wait(bar(SLOT_FULL + slot), (cv / kSlots) & 1u, g.err, 117)) { ok = false; break; }
+                    if (ga >= 2 && !mbar_wait_warp(bar(O_FREE + ob), ((ga >> 1) - 1u) & 1u, g.err, 118)) { ok = false; break; }
+                    if (!mbar_wait_warp(bar(P_FULL + buf), (ga / kSoft) & 1u, g.err, 116)) { ok = false; break; }
+                    if (!mbar_wait_warp(bar(SLOT_FULL + slot), (cv / kSlots) & 1u, g.err, 117)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t p_hi = tmem + buf * 128u, p_lo = p_hi + 64u;
                     const DescBase vd = mn_base(ring_s + slot * kTile);
+                    if (elect_one()) {
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks) {
                         umma_tf32_ts(tO, p_lo + ks * 8u, vd.at(mn_off(ks, false)), idesc, ks > 0 ? 1u : 0u);
@@ -244,6 +228,8 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     umma_commit(bar(P_DONE + buf));
                     mbar_arrive(bar(O_FULL + ob));      // hands on what P_FULL published: the tile's (r, sum)
                     umma_commit(bar(O_FULL + ob));
+                    }
+                    __syncwarp();
                 }
                 c += 2u * (uint32_t)it.n;
                 gt += (uint32_t)it.n;
@@ -256,7 +242,7 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         uint32_t gt = 0, use = 0;
         Item it;
         bool ok = true;
-        for (int i = 0; ok && (ok = get_item(i, it, true)) && it.n >= 0; ++i) {
+        for (int i = 0; ok && (ok = next(i, it, true)) && it.n >= 0; ++i) {
             const int b = it.bh / g.H, h = it.bh % g.H, row = it.blk * BR + rloc;
             const Score sc = make_score<CAP, SLOPE>(1.0f / sqrtf((float)HD), g.cap, g.slopes, h);
             const int2 span = row_range(g.spans.k, b, g.T, row, false);
@@ -328,7 +314,7 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         uint32_t gt = 0;
         Item it;
         bool ok = true;
-        for (int i = 0; ok && (ok = get_item(i, it, true)) && it.n >= 0; ++i) {
+        for (int i = 0; ok && (ok = next(i, it, true)) && it.n >= 0; ++i) {
             float acc[HD], m = -INFINITY, l = 0.f;
 #pragma unroll
             for (int k = 0; k < HD; ++k) acc[k] = 0.f;
@@ -378,17 +364,19 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 
 // -------------------------------------------------------------------------------------- backward, dK and dV
 //
-// One CTA owns 128 keys and walks the 64-row query tiles that read them.
+// Persistent as the forward; an item is 128 keys of one head and the 64-row query tiles that read them.
 //     S^T = K' Q^T | dP^T = V dO^T | dV_tile = P^T dO | dK_tile = dS^T Q,  P^T = exp2(z - lse), dS^T = P^T o (dP^T - D) (1 - tanh^2)
-// Warp 1 issues dV(t), S^T(t+1), ..., warp 10 dK(t), dP^T(t+1), ...: within a chain the product that overwrites a
-// region follows the one that last read it.  dV(t) is complete when S^T(t+1) is (one thread's products
-// complete in order), so the element-wise threads add it to their registers between those two
-// waits, before they publish P^T(t+1), which lets dV(t+1) overwrite it; dK likewise with dP^T and dS^T.
-//   tensor memory: K' hi|lo 0-127, dK 128-191, dV 192-255, S^T -> P^T_hi 256-319, P^T_lo 320-383,
-//                  dP^T -> dS^T_hi 384-447, dS^T_lo 448-511
-//   warps 2-9: both warpgroups on every tile, 32 of its queries each; of the accumulators 32 columns each
-constexpr int kDkvThreads = 352, kWarpMma2 = 10;
-constexpr uint32_t kDkvSmem = 1024u + kResBytes + 4u * kTile + 256u + 4u * kRowTileBytes + 1024u;
+//   warp 0      TMA producer and scheduler
+//   warp 1      dV(t), S^T(t+1), dV(t+1), ...;   warp 2  dK(t), dP^T(t+1), ...: within a chain the product that overwrites a
+//               region follows the one that last read it
+//   warps 4-19  four element-wise warpgroups on every tile, thread = key, 16 of the tile's queries each, and 16 columns of
+//               dK and of dV each.  dV(t) is complete when S^T(t+1) is (one thread's products complete in order): they
+//               read it between that wait and publishing P^T(t+1), which lets dV(t+1) overwrite it; dK likewise
+//   tensor memory  K' hi|lo 0-127, dK 128-191, dV 192-255, S^T -> P^T_hi 256-319, small half -> P^T_lo 320-383,
+//               dP^T -> dS^T_hi 384-447, small half -> dS^T_lo 448-511
+constexpr int kDkvThreads = 640, kRegsIssueDkv = 64, kRegsElemDkv = 104;
+static_assert(kRegsIssueDkv + 4 * kRegsElemDkv <= 480, "registers: 640 threads get 96 each at launch");
+constexpr uint32_t kDkvSmem = 1024u + kResBytes + 4u * kTile + 512u + 1024u;
 static_assert(kDkvSmem <= 232448u, "shared memory");
 
 template <bool CAP, bool SLOPE>
@@ -401,24 +389,18 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t v_s = base, qk_s = base + kResBytes, dok_s = qk_s + kTile, dom_s = dok_s + kTile, qm_s = dom_s + kTile;
     const uint32_t bars = qm_s + kTile;
-    enum { V_FULL = 0, QK_FULL, QK_EMPTY, DOK_FULL, DOK_EMPTY, DOM_FULL, DOM_EMPTY, QM_FULL, QM_EMPTY, S_FULL,
-           DP_FULL, ACC_FULL, P_READY, DS_READY, K_READY, STAT_READY, N_BARS };
+    enum { V_FULL = 0, V_EMPTY, QK_FULL, QK_EMPTY, DOK_FULL, DOK_EMPTY, DOM_FULL, DOM_EMPTY, QM_FULL, QM_EMPTY, S_FULL, DP_FULL, ACC_V, ACC_K,
+           NEXT, INFO_FULL, INFO_EMPTY = INFO_FULL + 2, P_READY = INFO_EMPTY + 2, DS_READY, K_READY, STAT_READY, N_BARS };
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
-    const uint32_t tmem_slot = bars + 8u * N_BARS;
+    constexpr uint32_t kInfo = (8u * N_BARS + 15u) & ~15u;
+    static_assert(kInfo + 2 * sizeof(Item) + 32 <= 512, "barrier region");
     auto smem_ptr = [&](uint32_t addr) { return smem_raw + (addr - smem_u32(smem_raw)); };
+    volatile Item* info = reinterpret_cast<volatile Item*>(smem_ptr(bars + kInfo));
+    const uint32_t answer = bars + kInfo + 2u * (uint32_t)sizeof(Item), tmem_slot = answer + 16u;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int bh, yb;
-    grouped_block(args.head_group, bh, yb);
-    const int b = bh / g.H, h = bh % g.H, j0 = yb * BR;
-    const int row_base = b * g.T;
-
     if (threadIdx.x == 0) {
-        for (int i = 0; i < P_READY; ++i) mbar_init(bar(i), i == ACC_FULL ? 2 : 1);   // both issuing threads commit at the end
-        mbar_init(bar(P_READY), 8);
-        mbar_init(bar(DS_READY), 8);
-        mbar_init(bar(K_READY), 4);
-        mbar_init(bar(STAT_READY), 8);
+        for (int i = 0; i < N_BARS; ++i) mbar_init(bar(i), i >= P_READY ? 16 : i >= INFO_EMPTY ? 2 + 16 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) alloc_tmem(tmem_slot);
@@ -427,239 +409,304 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem_ptr(tmem_slot));
     pdl_wait();      // set-up done; global memory is touched from here on
-    pdl_trigger();
     const uint32_t tK_hi = tmem, tK_lo = tmem + 64, tdK = tmem + 128, tdV = tmem + 192;
     const uint32_t tS = tmem + 256, tPlo = tmem + 320, tdP = tmem + 384, tdSlo = tmem + 448;
-    const int2 range = block_range(g.spans.qblock, b, g.T, j0, BR, true);
-    const int qt0 = range.x / BT64, n_t = range.x < range.y ? (range.y - 1) / BT64 + 1 - qt0 : 0;
-    auto q_row0 = [&](int t) { return (qt0 + t) * BT64; };
+    auto next = [&](int i, Item& it, bool whole_warp) -> bool {     // every role walks the same items
+        return get_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i, it, g.err, whole_warp);
+    };
 
-    if (warp == 0) {
-        if (lane == 0 && n_t > 0) {
-            mbar_expect_tx(bar(V_FULL), kResBytes);
-            for (int kb = 0; kb < 2; ++kb)
-                tma_load_3d(v_s + kb * (kResBytes / 2), &tmVres, bar(V_FULL), 2 * g.C + h * HD + kb * 32, row_base + j0, 0);
+    if (warp < 4) {
+        set_regs_down<kRegsIssueDkv>();
+        if (warp == 0 && lane == 0) {
+            uint32_t gt = 0, vi = 0;                    // tiles and non-empty items before this item
+            Item it = make_item(g, args.head_group, (int)blockIdx.x, (int)blockIdx.y, true, BR, BT64);
             bool ok = true;
-            // in the order the products consume them: S^T(0), dP^T(0), then per tile dV(t), S^T(t+1), dK(t), dP^T(t+1)
-            for (int i = 0; i < 4 * n_t + 2 && ok; ++i) {
-                // j: 0 dO MN-major (t), 1 Q K-major (t+1), 2 Q MN-major (t), 3 dO K-major (t+1); first Q(0), dO(0) K-major
-                const int j = i == 0 ? 1 : i == 1 ? 3 : (i - 2) & 3;
-                const int t = i < 2 ? 0 : ((i - 2) >> 2) + (j & 1);
-                if (t >= n_t) continue;
-                const uint32_t dst = j == 0 ? dom_s : j == 1 ? qk_s : j == 2 ? qm_s : dok_s;
-                const CUtensorMap* tm = j == 0 ? &tmDOm : j == 1 ? &tmQk : j == 2 ? &tmQm : &tmDOk;
-                const int full = j == 0 ? DOM_FULL : j == 1 ? QK_FULL : j == 2 ? QM_FULL : DOK_FULL;
-                ok = mbar_wait_ool(bar(full + 1), (uint32_t)(t & 1) ^ 1u, g.err, 131);   // every EMPTY barrier follows its FULL barrier
-                if (!ok) break;
-                mbar_expect_tx(bar(full), kTile);
-                for (int part = 0; part < 2; ++part)
-                    tma_load_3d(dst + part * (kTile / 2), tm, bar(full), h * HD + part * 32, row_base + q_row0(t), 0);
+            for (int i = 0; ok; ++i) {
+                ok = put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i, it, g.err);
+                if (!ok || it.n < 0) break;
+                const int last = 4 * it.n + 1;          // asked for and looked up as in the forward
+                if (it.n == 0) ask_next(answer, bar(NEXT));
+                Item follows{0, 0, 0, -1};
+                auto look_up = [&]() -> bool {
+                    if (!mbar_wait(bar(NEXT), (uint32_t)i & 1u, g.err, 120)) return false;
+                    int x, y;
+                    if (next_item(answer, x, y)) follows = make_item(g, args.head_group, x, y, true, BR, BT64);
+                    return true;
+                };
+                if (it.n == 0) ok = look_up();
+                const int h = it.bh % g.H, row0 = (it.bh / g.H) * g.T;
+                // in the order the products consume them: S^T(0), dP^T(0), then per tile dV(t), S^T(t+1), dK(t), dP^T(t+1)
+                for (int p = 0; it.n > 0 && p <= last && ok; ++p) {
+                    if (p == max(0, last - 6)) ask_next(answer, bar(NEXT));
+                    if (p == last) ok = look_up();
+                    if (!ok) break;
+                    // j: 0 dO MN-major (t), 1 Q K-major (t+1), 2 Q MN-major (t), 3 dO K-major (t+1); first Q(0), dO(0) K-major
+                    const int j = p == 0 ? 1 : p == 1 ? 3 : (p - 2) & 3;
+                    const int t = p < 2 ? 0 : ((p - 2) >> 2) + (j & 1);
+                    if (t < it.n) {
+                        const uint32_t dst = j == 0 ? dom_s : j == 1 ? qk_s : j == 2 ? qm_s : dok_s;
+                        const CUtensorMap* tm = j == 0 ? &tmDOm : j == 1 ? &tmQk : j == 2 ? &tmQm : &tmDOk;
+                        const int full = j == 0 ? DOM_FULL : j == 1 ? QK_FULL : j == 2 ? QM_FULL : DOK_FULL;
+                        ok = mbar_wait(bar(full + 1), ((gt + (uint32_t)t) & 1u) ^ 1u, g.err, 131);   // every EMPTY barrier follows its FULL barrier
+                        if (!ok) break;
+                        mbar_expect_tx(bar(full), kTile);
+                        for (int part = 0; part < 2; ++part)
+                            tma_load_3d(dst + part * (kTile / 2), tm, bar(full), h * HD + part * 32, row0 + (it.t0 + t) * BT64, 0);
+                    }
+                    if (p == 0) {                       // V, once the previous item's last dP^T is done with it
+                        ok = mbar_wait(bar(V_EMPTY), (vi & 1u) ^ 1u, g.err, 132);
+                        if (!ok) break;
+                        mbar_expect_tx(bar(V_FULL), kResBytes);
+                        for (int kb = 0; kb < 2; ++kb)
+                            tma_load_3d(v_s + kb * (kResBytes / 2), &tmVres, bar(V_FULL), 2 * g.C + h * HD + kb * 32, row0 + it.blk * BR, 0);
+                    }
+                }
+                gt += (uint32_t)it.n;
+                if (it.n > 0) ++vi;
+                it = follows;
             }
             if (!ok) settle();
-        }
-    } else if (warp == 1 || warp == kWarpMma2) {
-        if (lane == 0 && n_t > 0) {
+        } else if (warp == 1 || warp == 2) {
             constexpr uint32_t idesc_a = make_idesc_tf32(BR, BT64, false, false);
             constexpr uint32_t idesc_a2 = make_idesc_tf32(BR, 2 * BT64, false, false);   // B = [hi rows | lo rows]
             constexpr uint32_t idesc_b = make_idesc_tf32(BR, HD, false, true);
             const bool score_chain = warp == 1;
-            bool ok = score_chain ? mbar_wait_ool(bar(K_READY), 0, g.err, 134) : mbar_wait_ool(bar(V_FULL), 0, g.err, 133);
-            const DescBase vd = kmaj_base(v_s), qd = kmaj_base(qk_s), od = kmaj_base(dok_s);
-            const DescBase omd = mn_base(dom_s), qmd = mn_base(qm_s);
-            // Score products: a tile's lo rows follow its hi rows, so [hi | lo] is one operand of 128 rows whose
-            // second half lands in the neighbouring 64 columns; A_lo hi joins it there, the small terms
-            // apart from the large one, and the reader adds the halves.
-            auto issue_s = [&](int t) -> bool {
-                if (!mbar_wait_ool(bar(QK_FULL), (uint32_t)(t & 1), g.err, 135)) return false;
-                tc_fence_after();
+            const DescBase vd = kmaj_base(v_s), qd = kmaj_base(score_chain ? qk_s : dok_s), bd = mn_base(score_chain ? dom_s : qm_s);
+            const uint32_t t_x = score_chain ? tS : tdP, t_xlo = score_chain ? tPlo : tdSlo, t_acc = score_chain ? tdV : tdK;
+            const int x_full = score_chain ? QK_FULL : DOK_FULL, x_done = score_chain ? S_FULL : DP_FULL;
+            const int acc_in = score_chain ? P_READY : DS_READY, acc_b = score_chain ? DOM_FULL : QM_FULL;
+            uint32_t gt = 0, ni = 0;
+            Item it;
+            bool ok = true;
+            for (int i = 0; ok && (ok = next(i, it, true)) && it.n >= 0; ++i) {
+                if (it.n == 0) continue;
+                ok = mbar_wait_warp(bar(score_chain ? K_READY : V_FULL), ni & 1u, g.err, 133);
+                for (int t = 0; t <= it.n && ok; ++t) {
+                    if (t > 0) {
+                        // dV += P^T dO or dK += dS^T Q of tile t - 1: from zero, the small terms first; it frees the
+                        // region that the next score product overwrites
+                        const uint32_t ph = (gt + (uint32_t)t - 1u) & 1u;
+                        if (!mbar_wait_warp(bar(acc_in), ph, g.err, 137) || !mbar_wait_warp(bar(acc_b), ph, g.err, 138)) { ok = false; break; }
+                        tc_fence_after();
+                        if (elect_one()) {
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) {
-                    const uint64_t q_hl = qd.at(kmaj_off(BT64, ks, false));
-                    umma_tf32_ts(tS, tK_hi + ks * 8, q_hl, idesc_a2, ks > 0 ? 1u : 0u);   // K'_hi Q_hi | K'_hi Q_lo
-                    umma_tf32_ts(tPlo, tK_lo + ks * 8, q_hl, idesc_a, 1u);                // + K'_lo Q_hi
-                }
-                umma_commit(bar(QK_EMPTY));
-                umma_commit(bar(S_FULL));
-                return true;
-            };
-            auto issue_dp = [&](int t) -> bool {
-                if (!mbar_wait_ool(bar(DOK_FULL), (uint32_t)(t & 1), g.err, 136)) return false;
-                tc_fence_after();
+                        for (int ks = 0; ks < 8; ++ks) {
+                            umma_tf32_ts(t_acc, t_xlo + ks * 8, bd.at(mn_off(ks, false)), idesc_b, ks > 0 ? 1u : 0u);
+                            umma_tf32_ts(t_acc, t_x + ks * 8, bd.at(mn_off(ks, true)), idesc_b, 1u);
+                        }
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) {
-                    const uint64_t v_hi = vd.at(kmaj_off(BR, ks, false)), v_lo = vd.at(kmaj_off(BR, ks, true));
-                    const uint64_t o_hl = od.at(kmaj_off(BT64, ks, false));
-                    umma_tf32(tdP, v_hi, o_hl, idesc_a2, ks > 0 ? 1u : 0u);    // V_hi dO_hi | V_hi dO_lo
-                    umma_tf32(tdSlo, v_lo, o_hl, idesc_a, 1u);                 // + V_lo dO_hi
-                }
-                umma_commit(bar(DOK_EMPTY));
-                umma_commit(bar(DP_FULL));
-                return true;
-            };
-            // Accumulating products, from zero in every tile, the small terms first.
-            auto issue_acc = [&](int t, uint32_t acc, uint32_t a_hi, uint32_t a_lo, const DescBase& bd, int ready, int full) -> bool {
-                if (!mbar_wait_ool(bar(ready), (uint32_t)(t & 1), g.err, 137)) return false;
-                if (!mbar_wait_ool(bar(full), (uint32_t)(t & 1), g.err, 138)) return false;
-                tc_fence_after();
+                        for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(t_acc, t_x + ks * 8, bd.at(mn_off(ks, false)), idesc_b, 1u);
+                        umma_commit(bar(acc_b + 1));
+                        if (t == it.n) umma_commit(bar(score_chain ? ACC_V : ACC_K));
+                        }
+                        __syncwarp();
+                    }
+                    if (t < it.n) {
+                        // A tile's lo rows follow its hi rows, so [hi | lo] is one operand of 128 rows whose second half lands in
+                        // the neighbouring 64 columns; A_lo hi joins it there, the small terms apart from the
+                        // large one, and the reader adds the halves.
+                        if (!mbar_wait_warp(bar(x_full), (gt + (uint32_t)t) & 1u, g.err, 135)) { ok = false; break; }
+                        tc_fence_after();
+                        if (elect_one()) {
+                        if (score_chain) {
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) {
-                    umma_tf32_ts(acc, a_lo + ks * 8, bd.at(mn_off(ks, false)), idesc_b, ks > 0 ? 1u : 0u);
-                    umma_tf32_ts(acc, a_hi + ks * 8, bd.at(mn_off(ks, true)), idesc_b, 1u);
-                }
+                            for (int ks = 0; ks < 8; ++ks) {
+                                const uint64_t b_hl = qd.at(kmaj_off(BT64, ks, false));
+                                umma_tf32_ts(t_x, tK_hi + ks * 8, b_hl, idesc_a2, ks > 0 ? 1u : 0u);      // K'_hi Q_hi | K'_hi Q_lo
+                                umma_tf32_ts(t_xlo, tK_lo + ks * 8, b_hl, idesc_a, 1u);                   // + K'_lo Q_hi
+                            }
+                        } else {
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(acc, a_hi + ks * 8, bd.at(mn_off(ks, false)), idesc_b, 1u);
-                umma_commit(bar(full + 1));
-                return true;
-            };
-            if (score_chain) {
-                for (int t = 0; t <= n_t && ok; ++t) {
-                    if (t > 0) ok = issue_acc(t - 1, tdV, tS, tPlo, omd, P_READY, DOM_FULL);   // dV += P^T dO
-                    if (ok && t < n_t) ok = issue_s(t);
+                            for (int ks = 0; ks < 8; ++ks) {
+                                const uint64_t b_hl = qd.at(kmaj_off(BT64, ks, false));
+                                umma_tf32(t_x, vd.at(kmaj_off(BR, ks, false)), b_hl, idesc_a2, ks > 0 ? 1u : 0u);   // V_hi dO_hi | V_hi dO_lo
+                                umma_tf32(t_xlo, vd.at(kmaj_off(BR, ks, true)), b_hl, idesc_a, 1u);                 // + V_lo dO_hi
+                            }
+                        }
+                        umma_commit(bar(x_full + 1));
+                        umma_commit(bar(x_done));
+                        if (!score_chain && t == it.n - 1) umma_commit(bar(V_EMPTY));
+                        }
+                        __syncwarp();
+                    }
                 }
-            } else {
-                for (int t = 0; t <= n_t && ok; ++t) {
-                    if (t > 0) ok = issue_acc(t - 1, tdK, tdP, tdSlo, qmd, DS_READY, QM_FULL); // dK += dS^T Q
-                    if (ok && t < n_t) ok = issue_dp(t);
-                }
+                gt += (uint32_t)it.n;
+                ++ni;
             }
-            if (ok) umma_commit(bar(ACC_FULL));
         }
-    } else if (warp < kWarpMma2) {
-        const int wg = (warp - 2) >> 2, lane_group = warp & 3;
-        const int etid = lane_group * 32 + lane, key = j0 + etid;
-        const uint32_t t_lane = ((uint32_t)(lane_group * 32) << 16);
+    } else {
+        set_regs_up<kRegsElemDkv>();
+        const int wg = (warp - 4) >> 2, lane_group = warp & 3, rloc = lane_group * 32 + lane;
+        const uint32_t t_lane = ((uint32_t)(lane_group * 32) << 16), c0 = 16u * (uint32_t)wg;
         const float scale = 1.0f / sqrtf((float)HD);
-        const Score sc = make_score<CAP, SLOPE>(scale, g.cap, g.slopes, h);
         const int64_t gs = 3 * (int64_t)g.C;
-        const int64_t lb = ((int64_t)b * g.H + h) * g.T;
-        if (wg == 0 && n_t > 0) {   // K' = K * unit into tensor memory
-            const int wrow0 = min(j0 + lane_group * 32, g.T - 1);
-            const int64_t off = (int64_t)(row_base + wrow0) * gs + g.C + h * HD;
-            float* tile = reinterpret_cast<float*>(smem_ptr(bars + 256u) + (uint32_t)lane_group * kRowTileBytes);
-            rows_to_tmem(g.qkv + off, g.qkv_lo + off, gs, max(1, min(32, g.T - wrow0)), sc.unit, tK_hi + t_lane, tK_lo + t_lane,
-                         tile, lane);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(K_READY));
-        }
-        const int2 span = row_range(g.spans.q, b, g.T, key, true);
-        bool ok = true;
-        const uint32_t c0 = 32u * (uint32_t)wg;
-        // Statistics of a tile's 64 queries (lse in base-2 units, D) through shared memory, one tile ahead.  All
-        // eight warps arrive, those without a value too: no warp can be two phases behind.
-        float* stat = reinterpret_cast<float*>(smem_ptr(bars + 256u + 4u * kRowTileBytes));
-        const int sidx = (warp - 2) * 32 + lane;
-        auto fetch_stat = [&](int t) -> float {
-            const int r = min(q_row0(t) + (sidx & 63), g.T - 1);   // rows past the end are masked below
-            return sidx < 64 ? __ldg(g.lse + lb + r) * kLog2e : __ldg(g.dvec + lb + r);
+        // Statistics of a tile's 64 queries (lse in base-2 units, D) through shared memory, one tile ahead, from the
+        // first warpgroup's threads.  All sixteen warps arrive: no warp can be two phases behind.
+        float* stat = reinterpret_cast<float*>(smem_ptr(bars + 512u));
+        const int sidx = (int)threadIdx.x - 128;
+        auto fetch_stat = [&](const Item& it, int t) -> float {
+            const int64_t lb = (int64_t)it.bh * g.T;
+            const int r = min((it.t0 + t) * BT64 + (sidx & 63), g.T - 1);   // rows past the end are masked below
+            return sidx >= 128 ? 0.f : sidx < 64 ? __ldg(g.lse + lb + r) * kLog2e : __ldg(g.dvec + lb + r);
         };
-        auto publish_stat = [&](int t, float v) {
+        auto publish_stat = [&](uint32_t ga, float v) {
             if (sidx < 128) {
-                stat[(t & 1) * 128 + sidx] = v;
+                stat[(ga & 1u) * 128u + sidx] = v;
                 __threadfence_block();
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(STAT_READY));
         };
-        float acc_v[32], acc_k[32];
+        // K' = K * unit of an item into tensor memory (16 columns here), and its first tile's statistics
+        auto begin_item = [&](const Item& it, const Score& sc, uint32_t ga) {
+            const float st0 = fetch_stat(it, 0);
+            const int row = min(it.blk * BR + rloc, g.T - 1);
+            const int64_t off = ((int64_t)(it.bh / g.H) * g.T + row) * gs + g.C + (int64_t)(it.bh % g.H) * HD + c0;
+            float a[2][8], e[2][8];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) acc_v[i] = acc_k[i] = 0.f;
-        auto add_tile = [&](uint32_t t_acc, float (&acc)[32]) {
-            uint32_t r[32];
-            tmem_ld32(t_acc + t_lane + c0, r);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) acc[i] += __uint_as_float(r[i]);
-        };
-        if (n_t > 0) publish_stat(0, sidx < 128 ? fetch_stat(0) : 0.f);
-        for (int t = 0; t < n_t && ok; ++t) {
-            const int q0 = q_row0(t) + 32 * wg;
-            float next_stat = 0.f;
-            if (sidx < 128 && t + 1 < n_t) next_stat = fetch_stat(t + 1);   // in flight during this tile
-            if (!mbar_wait_warp_ool(bar(STAT_READY), (uint32_t)(t & 1), g.err, 142)) { ok = false; break; }
-            const float4* Ls = reinterpret_cast<const float4*>(stat + (t & 1) * 128 + 32 * wg);
-            const float4* Ds = Ls + 16;
-            if (!mbar_wait_warp_ool(bar(S_FULL), (uint32_t)(t & 1), g.err, 141)) { ok = false; break; }
-            tc_fence_after();
-            float p[32], f[32];
-            uint32_t s[32], lo[32];
-            tmem_ld32(tS + t_lane + c0, s);
-            tmem_ld32(tPlo + t_lane + c0, lo);        // the small half of the score product
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) p[i] = __uint_as_float(s[i]) + __uint_as_float(lo[i]);
-            score_tile<CAP, SLOPE, true, false, 32>(p, f, sc, key - q0, 0.f);
-            const bool whole = q0 >= span.x && q0 + 32 <= span.y;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float4 l4 = Ls[i];
-                p[4 * i] = ex2_approx(p[4 * i] - l4.x);
-                p[4 * i + 1] = ex2_approx(p[4 * i + 1] - l4.y);
-                p[4 * i + 2] = ex2_approx(p[4 * i + 2] - l4.z);
-                p[4 * i + 3] = ex2_approx(p[4 * i + 3] - l4.w);
+            for (int q = 0; q < 2; ++q) {
+                load_sector(g.qkv + off + 8 * q, a[q]);
+                load_sector(g.qkv_lo + off + 8 * q, e[q]);
             }
-            if (!whole) {
+            uint32_t hi[16], lo[16];
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (q0 + i < span.x || q0 + i >= span.y) p[i] = 0.f;
-            }
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                split_tf32_int(p[i], s[i], lo[i]);
-                if (CAP) p[i] *= f[i];
-            }
-            if (t > 0) add_tile(tdV, acc_v);         // dV(t - 1): complete, as S^T(t) is
-            tmem_st32(tS + t_lane + c0, s);          // P^T hi over S^T
-            tmem_st32(tPlo + t_lane + c0, lo);
+            for (int k = 0; k < 16; ++k) split_tf32_int((a[k >> 3][k & 7] + e[k >> 3][k & 7]) * sc.unit, hi[k], lo[k]);
+            tmem_stn(tK_hi + t_lane + c0, hi);       // the last S^T of the item before has been read
+            tmem_stn(tK_lo + t_lane + c0, lo);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(P_READY));
-            if (!mbar_wait_warp_ool(bar(DP_FULL), (uint32_t)(t & 1), g.err, 143)) { ok = false; break; }
-            tc_fence_after();
-            tmem_ld32(tdP + t_lane + c0, s);
-            tmem_ld32(tdSlo + t_lane + c0, lo);
-            tmem_ld_wait();
+            if (lane == 0) mbar_arrive(bar(K_READY));
+            publish_stat(ga, st0);
+        };
+        auto score_of = [&](const Item& it) { return make_score<CAP, SLOPE>(scale, g.cap, g.slopes, it.bh % g.H); };
+        uint32_t gt = 0, ni = 0;
+        Item it;
+        bool ok = next(0, it, true);
+        Score sc = score_of(it);
+        if (ok && it.n > 0) begin_item(it, sc, 0);
+        for (int i = 0; ok && it.n >= 0; ++i) {
+            const int b = it.bh / g.H, h = it.bh % g.H, key = it.blk * BR + rloc;
+            const int2 span = row_range(g.spans.q, b, g.T, key, true);
+            float acc_v[16], acc_k[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float4 d4 = Ds[i];
-                const float dd[4] = {d4.x, d4.y, d4.z, d4.w};
+            for (int k = 0; k < 16; ++k) acc_v[k] = acc_k[k] = 0.f;
+            for (int t = 0; t < it.n; ++t) {
+                const uint32_t ga = gt + (uint32_t)t, ph = ga & 1u;
+                const int q0 = (it.t0 + t) * BT64 + (int)c0;
+                float next_stat = 0.f;
+                if (t + 1 < it.n) next_stat = fetch_stat(it, t + 1);        // in flight during this tile
+                if (!mbar_wait_warp(bar(STAT_READY), ph, g.err, 142)) { ok = false; break; }
+                const float4* Ls = reinterpret_cast<const float4*>(stat + ph * 128u + c0);
+                const float4* Ds = Ls + 16;
+                if (!mbar_wait_warp(bar(S_FULL), ph, g.err, 141)) { ok = false; break; }
+                tc_fence_after();
+                float p[16], f[16];
+                uint32_t s[16], lo[16];
+                tmem_ldn(tS + t_lane + c0, s);
+                tmem_ldn(tPlo + t_lane + c0, lo);
+                tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int k = 4 * i + e;
-                    const float ds = p[k] * ((__uint_as_float(s[k]) + __uint_as_float(lo[k])) - dd[e]);
-                    split_tf32_int(ds, s[k], lo[k]);
+                for (int k = 0; k < 16; ++k) p[k] = __uint_as_float(s[k]) + __uint_as_float(lo[k]);
+                score_tile<CAP, SLOPE, true, false, 16>(p, f, sc, key - q0, 0.f);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float4 l4 = Ls[q];
+                    p[4 * q] = ex2_approx(p[4 * q] - l4.x);
+                    p[4 * q + 1] = ex2_approx(p[4 * q + 1] - l4.y);
+                    p[4 * q + 2] = ex2_approx(p[4 * q + 2] - l4.z);
+                    p[4 * q + 3] = ex2_approx(p[4 * q + 3] - l4.w);
+                }
+                if (q0 < span.x || q0 + 16 > span.y) {
+                    const uint32_t bits = column_bits<16>(span, q0);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (!(bits >> k & 1u)) p[k] = 0.f;
+                }
+#pragma unroll
+                for (int k = 0; k < 16; ++k) split_tf32_int(p[k], s[k], lo[k]);
+                tmem_stn(tS + t_lane + c0, s);           // P^T over S^T
+                tmem_stn(tPlo + t_lane + c0, lo);
+                tmem_ldn(tdV + t_lane + c0, s);          // dV(t - 1): complete, as S^T(t) is (not used at t = 0)
+                tmem_ld_wait();
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(P_READY));
+                if (CAP) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) p[k] *= f[k];
+                }
+                if (t > 0) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) acc_v[k] += __uint_as_float(s[k]);
+                }
+                if (!mbar_wait_warp(bar(DP_FULL), ph, g.err, 143)) { ok = false; break; }
+                tc_fence_after();
+                tmem_ldn(tdP + t_lane + c0, s);
+                tmem_ldn(tdSlo + t_lane + c0, lo);
+                tmem_ld_wait();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float4 d4 = Ds[q];
+                    const float dd[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int k = 4 * q + e;
+                        split_tf32_int(p[k] * ((__uint_as_float(s[k]) + __uint_as_float(lo[k])) - dd[e]), s[k], lo[k]);
+                    }
+                }
+                tmem_stn(tdP + t_lane + c0, s);          // dS^T over dP^T
+                tmem_stn(tdSlo + t_lane + c0, lo);
+                tmem_ldn(tdK + t_lane + c0, s);          // dK(t - 1): complete, as dP^T(t) is
+                tmem_ld_wait();
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(DS_READY));
+                if (t > 0) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) acc_k[k] += __uint_as_float(s[k]);
+                }
+                if (t + 1 < it.n) publish_stat(ga + 1u, next_stat);
+            }
+            if (!ok) break;
+            // the next item's operand first, then what is left of this one
+            gt += (uint32_t)it.n;
+            Item follows;
+            if (!next(i + 1, follows, true)) { ok = false; break; }
+            const Score sc_next = score_of(follows);
+            if (follows.n > 0) begin_item(follows, sc_next, gt);
+            if (it.n > 0) {
+                if (!mbar_wait_warp(bar(ACC_V), ni & 1u, g.err, 144) || !mbar_wait_warp(bar(ACC_K), ni & 1u, g.err, 145)) { ok = false; break; }
+                ++ni;
+                tc_fence_after();
+                uint32_t r[16], r2[16];
+                tmem_ldn(tdV + t_lane + c0, r);
+                tmem_ldn(tdK + t_lane + c0, r2);
+                tmem_ld_wait();
+                tc_fence_before();
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    acc_v[k] += __uint_as_float(r[k]);
+                    acc_k[k] = (acc_k[k] + __uint_as_float(r2[k])) * scale;
                 }
             }
-            if (t > 0) add_tile(tdK, acc_k);         // dK(t - 1): complete, as dP^T(t) is
-            tmem_st32(tdP + t_lane + c0, s);         // dS^T hi over dP^T
-            tmem_st32(tdSlo + t_lane + c0, lo);
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(DS_READY));
-            if (t + 1 < n_t) publish_stat(t + 1, next_stat);
-        }
-        if (ok && n_t > 0) {
-            ok = mbar_wait_warp_ool(bar(ACC_FULL), 0, g.err, 144);
-            if (ok) {   // warp-uniform: the tensor-memory loads need the whole warp
-                tc_fence_after();
-                add_tile(tdV, acc_v);
-                add_tile(tdK, acc_k);
-            }
-        }
-        if (ok) {
-            const int wrow0 = j0 + lane_group * 32, nvalid = max(0, min(32, g.T - wrow0));
-            // the streamed-tile buffers are idle by now: each warp stages its rows in a slice of them
-            float* tile = reinterpret_cast<float*>(smem_ptr(qk_s) + (uint32_t)(warp - 2) * kRowTileBytes);
+            if (key < g.T) {
+                const int64_t at = ((int64_t)b * g.T + key) * gs + g.C + (int64_t)h * HD + c0;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) acc_k[i] *= scale;
+                for (int q = 0; q < 2; ++q) {
+                    float v[8];
 #pragma unroll
-            for (int part = 1; part < 3; ++part) {
-                const int64_t off = (int64_t)(row_base + wrow0) * gs + (int64_t)part * g.C + h * HD + c0;
-                warp_rows_store(part == 1 ? acc_k : acc_v, tile, lane, nvalid, g.dqkv ? g.dqkv + off : nullptr,
-                                g.dqkv_hi ? g.dqkv_hi + off : nullptr, g.dqkv_hi ? g.dqkv_lo + off : nullptr, gs, nullptr);
+                    for (int e = 0; e < 8; ++e) v[e] = acc_k[8 * q + e];
+                    store_sector(v, at + 8 * q, g.dqkv, g.dqkv_hi, g.dqkv_lo);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = acc_v[8 * q + e];
+                    store_sector(v, at + g.C + 8 * q, g.dqkv, g.dqkv_hi, g.dqkv_lo);
+                }
             }
+            it = follows;
+            sc = sc_next;
         }
     }
     tc_fence_before();
@@ -678,7 +725,7 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
 // The dQ tile is 128 wide: the column groups [K_hi g0 | K_lo g0 | K_hi g1 | K_lo g1] (g = 32 head columns) as
 // one operand of dS_hi, and dS_lo K_hi 32 columns further, on the second and third group; head columns
 // 0-31 are the sum of groups 0 and 1, 32-63 that of 2 and 3.
-constexpr int kDqThreads = 512, kWarpMma3 = 11, kWarpAdd = 12;
+constexpr int kDqThreads = 512, kWarpMma2 = 10, kWarpMma3 = 11, kWarpAdd = 12;
 constexpr uint32_t kDqSmem = 1024u + kResBytes + 5u * kTile + 256u + 512u;
 static_assert(kDqSmem <= 232448u, "shared memory");
 
