@@ -604,7 +604,7 @@ def _arr(t, dtype=torch.float32):
         raise TypeError(type(t))
     if t.dtype is not dtype:
         raise ValueError(f"expected a {dtype} tensor, got {t.dtype}")
-    if not t.is_cuda or t.get_device() != _this_device():
+    if t.get_device() != (_this_device() if t.is_cuda else None):
         raise ValueError(f"expected a tensor on the current device, got one on {t.device}")
     if not t.is_contiguous():
         raise ValueError("tensor arguments must be contiguous")

@@ -332,7 +332,8 @@ struct RopeArgs {
     int T, C, H, rot, interleaved;
     float sin_sign, mscale;
     float *y, *y_hi, *y_lo;
-    int rows;                   // rows per CTA (set by the launcher)
+    int rows;                   // set by the launcher: rows per CTA, reciprocals of the units per head
+    uint32_t m_head, m_pass;
     double turns[64];           // turns per position of each pair
 };
 cudaError_t launch_rope(RopeArgs g, cudaStream_t s);

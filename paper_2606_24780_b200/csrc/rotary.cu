@@ -19,94 +19,102 @@ constexpr int kThreads = 256;
 constexpr int kMaxRows = 8;      // rows of one CTA
 constexpr int kMaxPairs = 64;    // rot_dim / 2
 
+// q = n / d by multiplication: exact while n * d < 2^32 (m = ceil(2^32 / d), d >= 2; d = 1 has m = 0).
+__device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t m) { return m ? __umulhi(n, m) : n; }
+
+// A thread group of the CTA owns a row.  First the columns that only move (the values, the tails of partly rotated
+// heads), while the angles are formed; then the rotated ones.  Pieces are float4 (VEC) or single columns, kUnroll of them
+// requested before the first is used.  In place the first part falls away.
 template <bool VEC>
 __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs g) {
+    constexpr int W = VEC ? 4 : 1, kUnroll = VEC ? 4 : 8;
     __shared__ float2 cs[kMaxRows * kMaxPairs];
     pdl_wait();
     pdl_trigger();
     const int64_t n0 = (int64_t)blockIdx.x * g.rows;
-    const int rows = (int)min((int64_t)g.rows, g.N - n0);
-    const int half = g.rot >> 1;
-    for (int i = threadIdx.x; i < rows * half; i += kThreads) {
-        const int r = i / half, k = i - r * half;
-        const int64_t n = n0 + r;
+    const int group = kThreads / g.rows, r = (int)threadIdx.x / group, t0 = (int)threadIdx.x - r * group;
+    const int half = g.rot >> 1, d = g.C / g.H;
+    for (int i = threadIdx.x; i < g.rows * half; i += kThreads) {
+        const int row = i / half, k = i - row * half;
+        const int64_t n = min(n0 + row, g.N - 1);
         const int pos = g.pos ? g.pos[n] : (int)(n % g.T);
         const double turns = (double)pos * g.turns[k];
         float s, c;
         sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-        cs[r * half + k] = make_float2(c * g.mscale, s * g.sin_sign * g.mscale);
+        cs[i] = make_float2(c * g.mscale, s * g.sin_sign * g.mscale);
+    }
+    const bool live = n0 + r < g.N;
+    const int64_t row = (n0 + r) * 3 * (int64_t)g.C;
+    auto get = [&](int64_t at) -> float4 { return VEC ? __ldcs(reinterpret_cast<const float4*>(g.x + at)) : make_float4(g.x[at], 0.f, 0.f, 0.f); };
+    auto put = [&](int64_t at, const float4& v) {
+        if (VEC) {
+            store_raw_split(v, g.y, g.y_hi, g.y_lo, at >> 2);
+        } else {
+            if (g.y) g.y[at] = v.x;
+            if (g.y_hi) split_tf32(v.x, g.y_hi[at], g.y_lo[at]);
+        }
+    };
+    if (live && g.y != g.x) {
+        const int pass = (d - g.rot) / W, heads = 2 * g.H * pass, total = heads + g.C / W;
+        for (int t = t0; t < total; t += group * kUnroll) {
+            float4 v[kUnroll];
+            int64_t at[kUnroll];
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k) {
+                const int u = t + k * group;
+                if (u < heads) {
+                    const uint32_t hd = quotient(u, g.m_pass);
+                    at[k] = row + (int64_t)hd * d + g.rot + (u - (int)hd * pass) * W;
+                } else {
+                    at[k] = row + 2 * (int64_t)g.C + (int64_t)(u - heads) * W;
+                }
+                if (u < total) v[k] = get(at[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k)
+                if (t + k * group < total) put(at[k], v[k]);
+        }
     }
     __syncthreads();
-
-    const int d = g.C / g.H;
-    const int64_t ld = 3 * (int64_t)g.C;
-    const bool raw_in_place = g.y == g.x;
-    // One unit of the vector form is four pairs of a head (half layout: two float4 a half apart;
-    // interleaved: two neighbouring float4) or one float4 that passes through; of the scalar form one
-    // pair or one element.  The units of a head come first the rotated, then the others; heads of q and
-    // k before the values.  In place only the rotated ones exist.
-    constexpr int W = VEC ? 4 : 1;
-    const int rot_units = half / W, pass_units = raw_in_place ? 0 : (d - g.rot) / W;
-    const int per_head = rot_units + pass_units, v_units = raw_in_place ? 0 : g.C / W;
-    const int per_row = 2 * g.H * per_head + v_units;
-#pragma unroll 4
-    for (int u = threadIdx.x; u < rows * per_row; u += kThreads) {
-        const int r = u / per_row, w = u - r * per_row;
-        const int64_t row = (n0 + r) * ld;
-        int64_t at;        // first (or only) piece
-        int k = -1;        // first pair of the unit, -1: passes through
-        if (w < 2 * g.H * per_head) {
-            const int hd = w / per_head, j = w - hd * per_head;
-            at = row + (int64_t)hd * d;     // heads of k follow those of q
-            if (j < rot_units) {
-                k = j * W;
-                at += g.interleaved ? 2 * k : k;
-            } else {
-                at += g.rot + (j - rot_units) * W;
+    if (!live) return;
+    // a unit: W pairs of a head -- two pieces half a rotation apart, or (interleaved) next to one another
+    const int per_head = half / W, total = 2 * g.H * per_head;
+    const float2* angle = cs + r * half;
+    for (int t = t0; t < total; t += group * kUnroll) {
+        float4 a[kUnroll], b[kUnroll];
+        int64_t at[kUnroll];
+        int pair[kUnroll];
+        const int64_t apart = g.interleaved ? W : half;
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+            const int u = t + k * group;
+            const uint32_t hd = quotient(u, g.m_head);
+            pair[k] = (u - (int)hd * per_head) * W;
+            at[k] = row + (int64_t)hd * d + (g.interleaved ? 2 * pair[k] : pair[k]);
+            if (u < total) {
+                a[k] = get(at[k]);
+                b[k] = get(at[k] + apart);
             }
-        } else {
-            at = row + 2 * (int64_t)g.C + (int64_t)(w - 2 * g.H * per_head) * W;
         }
-        if (VEC) {
-            float4 a = *reinterpret_cast<const float4*>(g.x + at);
-            if (k < 0) {
-                store_raw_split(a, g.y, g.y_hi, g.y_lo, at >> 2);
-                continue;
-            }
-            const int64_t at2 = at + (g.interleaved ? 4 : half);
-            float4 b = *reinterpret_cast<const float4*>(g.x + at2);
-            const float2* t = cs + r * half + k;
-            const float2 t0 = t[0], t1 = t[1], t2 = t[2], t3 = t[3];
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+            if (t + k * group >= total) break;
+            const float2* c = angle + pair[k];
             float4 oa, ob;
-            if (g.interleaved) {
-                oa = make_float4(a.x * t0.x - a.y * t0.y, a.x * t0.y + a.y * t0.x, a.z * t1.x - a.w * t1.y, a.z * t1.y + a.w * t1.x);
-                ob = make_float4(b.x * t2.x - b.y * t2.y, b.x * t2.y + b.y * t2.x, b.z * t3.x - b.w * t3.y, b.z * t3.y + b.w * t3.x);
+            if (!VEC) {
+                oa.x = a[k].x * c[0].x - b[k].x * c[0].y;
+                ob.x = a[k].x * c[0].y + b[k].x * c[0].x;
+            } else if (g.interleaved) {
+                const float2 c0 = c[0], c1 = c[1], c2 = c[2], c3 = c[3];
+                oa = make_float4(a[k].x * c0.x - a[k].y * c0.y, a[k].x * c0.y + a[k].y * c0.x, a[k].z * c1.x - a[k].w * c1.y, a[k].z * c1.y + a[k].w * c1.x);
+                ob = make_float4(b[k].x * c2.x - b[k].y * c2.y, b[k].x * c2.y + b[k].y * c2.x, b[k].z * c3.x - b[k].w * c3.y, b[k].z * c3.y + b[k].w * c3.x);
             } else {
-                oa = make_float4(a.x * t0.x - b.x * t0.y, a.y * t1.x - b.y * t1.y, a.z * t2.x - b.z * t2.y, a.w * t3.x - b.w * t3.y);
-                ob = make_float4(a.x * t0.y + b.x * t0.x, a.y * t1.y + b.y * t1.x, a.z * t2.y + b.z * t2.x, a.w * t3.y + b.w * t3.x);
+                const float2 c0 = c[0], c1 = c[1], c2 = c[2], c3 = c[3];
+                oa = make_float4(a[k].x * c0.x - b[k].x * c0.y, a[k].y * c1.x - b[k].y * c1.y, a[k].z * c2.x - b[k].z * c2.y, a[k].w * c3.x - b[k].w * c3.y);
+                ob = make_float4(a[k].x * c0.y + b[k].x * c0.x, a[k].y * c1.y + b[k].y * c1.x, a[k].z * c2.y + b[k].z * c2.x, a[k].w * c3.y + b[k].w * c3.x);
             }
-            store_raw_split(oa, g.y, g.y_hi, g.y_lo, at >> 2);
-            store_raw_split(ob, g.y, g.y_hi, g.y_lo, at2 >> 2);
-        } else {
-            auto put = [&](int64_t i, float v) {
-                if (g.y) g.y[i] = v;
-                if (g.y_hi) {
-                    float h, l;
-                    split_tf32(v, h, l);
-                    g.y_hi[i] = h;
-                    g.y_lo[i] = l;
-                }
-            };
-            const float a = g.x[at];
-            if (k < 0) {
-                put(at, a);
-                continue;
-            }
-            const int64_t at2 = at + (g.interleaved ? 1 : half);
-            const float b = g.x[at2];
-            const float2 t = cs[r * half + k];
-            put(at, a * t.x - b * t.y);
-            put(at2, a * t.y + b * t.x);
+            put(at[k], oa);
+            put(at[k] + apart, ob);
         }
     }
 }
@@ -114,14 +122,18 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs g) {
 }  // namespace
 
 cudaError_t launch_rope(RopeArgs g, cudaStream_t s) {
-    // Rows per CTA: at least 2,304 float4 of work (9 per thread), while a short array still spreads over
+    // Rows per CTA (a power of two): 2,304 float4 of work (9 per thread) or more, while a short array still spreads over
     // the SMs.
     const int64_t row4 = 3 * (int64_t)g.C / 4;
-    int rows = (int)max((int64_t)1, min((int64_t)kMaxRows, (2304 + row4 - 1) / row4));
-    while (rows > 1 && (g.N + rows - 1) / rows < 148) rows >>= 1;
+    int rows = 1;
+    while (rows < kMaxRows && rows * row4 < 2304 && (g.N + 2 * rows - 1) / (2 * rows) >= 148) rows *= 2;
     g.rows = rows;
     const int64_t grid = (g.N + rows - 1) / rows;
     if (grid > 0x7fffffff) return cudaErrorInvalidValue;
+    const int w = g.rot % 8 == 0 ? 4 : 1;
+    auto magic = [](int d) -> uint32_t { return d < 2 ? 0u : (uint32_t)((0x100000000ull + (uint64_t)d - 1) / (uint64_t)d); };
+    g.m_head = magic(g.rot / 2 / w);
+    g.m_pass = magic((g.C / g.H - g.rot) / w);
     if (g.rot % 8 == 0) BT_KERNEL_LAUNCH((rope_kernel<true>), (unsigned)grid, kThreads, 0, s, g);
     else BT_KERNEL_LAUNCH((rope_kernel<false>), (unsigned)grid, kThreads, 0, s, g);
     BT_COUNT_LAUNCH();
