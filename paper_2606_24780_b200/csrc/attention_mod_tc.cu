@@ -716,46 +716,22 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
 
 // --------------------------------------------------------------------------------------------- backward, dQ
 //
-// One CTA owns 128 queries and walks the 64-key tiles they read; it also forms D = rowsum(dO o O), which the dkv
-// kernel reads.
+// Persistent as the others; an item is 128 queries of one head and the 64-key tiles they read.  It also forms D = rowsum(dO o O),
+// which the dkv kernel reads.
 //     S = Q' K^T | dP = dO V^T | dS = P o (dP - D) (1 - tanh^2) | dQ_tile = dS K
-//   warp 0 TMA; warps 1, 10, 11 issue S, dP, dQ; warps 2-5 / 6-9 the element-wise pass on alternate tiles;
-//   warps 12-15 add every dQ tile to registers (64 columns of a row per thread) and write the result.
-//   tensor memory: Q' hi|lo 0-127, dQ tile 128-255, buffer b at 256 + 128b: S -> dS_hi, dP -> dS_lo
+//   warp 0      TMA producer and scheduler;   warps 1, 2, 3 issue S, dP, dQ
+//   warps 4-11, 12-19  two pairs of element-wise warpgroups on alternate tiles, thread = row, 32 of the tile's keys each.  The
+//               pair whose tile an item begins with loads the item's Q' and forms its D while the other is at the
+//               last tile of the item before
+//   warps 20-23 add every dQ tile to registers (64 columns of a row per thread) and write the result
+//   tensor memory  Q' hi|lo 0-127, dQ tile 128-255, buffer b at 256 + 128b: S -> dS_hi, dP -> dS_lo
 // The dQ tile is 128 wide: the column groups [K_hi g0 | K_lo g0 | K_hi g1 | K_lo g1] (g = 32 head columns) as
 // one operand of dS_hi, and dS_lo K_hi 32 columns further, on the second and third group; head columns
 // 0-31 are the sum of groups 0 and 1, 32-63 that of 2 and 3.
-constexpr int kDqThreads = 512, kWarpMma2 = 10, kWarpMma3 = 11, kWarpAdd = 12;
-constexpr uint32_t kDqSmem = 1024u + kResBytes + 5u * kTile + 256u + 512u;
+constexpr int kDqThreads = 768, kRegsIssueDq = 56, kRegsElemDq = 72, kRegsAddDq = 128;
+static_assert(kRegsIssueDq + 4 * kRegsElemDq + kRegsAddDq <= 480, "registers: 768 threads get 80 each at launch");
+constexpr uint32_t kDqSmem = 1024u + kResBytes + 5u * kTile + 512u + 1024u;
 static_assert(kDqSmem <= 232448u, "shared memory");
-
-// rowsum(dO o O) over one head for the warp's 32 rows; lane r returns row r's.
-__device__ __forceinline__ float rows_dot(const float* o, const float* do_hi, const float* do_lo, long long stride, int nvalid, int lane) {
-    const int sub = lane >> 3, cq = lane & 7;
-    float acc[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        acc[i] = 0.f;
-        const long long row = (long long)max(0, min(sub + 4 * i, nvalid - 1)) * stride + 4 * cq;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const float4 x = ld4(o + row + half * 32, 0);
-            const float4 y = add4(ld4(do_hi + row + half * 32, 0), ld4(do_lo + row + half * 32, 0));
-            acc[i] += (x.x * y.x + x.y * y.y) + (x.z * y.z + x.w * y.w);
-        }
-    }
-    float d = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float v = acc[i];
-        v += __shfl_xor_sync(0xffffffffu, v, 1);
-        v += __shfl_xor_sync(0xffffffffu, v, 2);
-        v += __shfl_xor_sync(0xffffffffu, v, 4);
-        v = __shfl_sync(0xffffffffu, v, 8 * (lane & 3));     // row sub + 4 i lives in the lanes of slice `sub`
-        if ((lane >> 2) == i) d = v;                          // lane r wants row r = (r & 3) + 4 (r >> 2)
-    }
-    return d;
-}
 
 template <bool CAP, bool SLOPE>
 __global__ void __launch_bounds__(kDqThreads, 1)
@@ -764,27 +740,21 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
     const AttnModArgs& g = args.a;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t do_s = base;
-    auto kk_s = [&](int st) { return base + kResBytes + (uint32_t)st * 2u * kTile; };
-    auto vk_s = [&](int st) { return kk_s(st) + kTile; };
-    const uint32_t km_s = base + kResBytes + 4u * kTile;
-    const uint32_t bars = base + kResBytes + 5u * kTile;
-    // the S and the dP issuing threads both commit to KEMPTY and SDP
-    enum { DO_FULL = 0, KFULL0, KFULL1, KEMPTY0, KEMPTY1, MFULL, MEMPTY, SDP0, SDP1, DONE0, DONE1, DQ_FULL, DS0, DS1, Q_READY, DQ_FREE, N_BARS };
+    const uint32_t do_s = base, kv_s = base + kResBytes, km_s = kv_s + 4u * kTile, bars = km_s + kTile;   // kv_s: stage st: K at 2 st, V at 2 st + 1
+    // the S and the dP issuing warps both commit to KEMPTY and SDP
+    enum { DO_FULL = 0, DO_EMPTY, KFULL, MFULL = KFULL + 2, MEMPTY, DONE, DQ_FULL = DONE + 2, Q_FREE, NEXT, INFO_FULL, INFO_EMPTY = INFO_FULL + 2,
+           KEMPTY = INFO_EMPTY + 2, SDP = KEMPTY + 2, DQ_FREE = SDP + 2, DS, Q_READY = DS + 2, D_FREE, N_BARS };
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
-    const uint32_t tmem_slot = bars + 8u * N_BARS;
+    constexpr uint32_t kInfo = (8u * N_BARS + 15u) & ~15u;
+    static_assert(kInfo + 2 * sizeof(Item) + 32 <= 512, "barrier region");
     auto smem_ptr = [&](uint32_t addr) { return smem_raw + (addr - smem_u32(smem_raw)); };
+    volatile Item* info = reinterpret_cast<volatile Item*>(smem_ptr(bars + kInfo));
+    const uint32_t answer = bars + kInfo + 2u * (uint32_t)sizeof(Item), tmem_slot = answer + 16u;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int bh, yb;
-    grouped_block(args.head_group, bh, yb);
-    const int qt = (int)gridDim.y - 1 - yb;
-    const int b = bh / g.H, h = bh % g.H, q0 = qt * BR;
-    const int row_base = b * g.T;
-
     if (threadIdx.x == 0) {
         for (int i = 0; i < N_BARS; ++i)
-            mbar_init(bar(i), (i == KEMPTY0 || i == KEMPTY1 || i == SDP0 || i == SDP1) ? 2 : i >= DS0 ? 4 : 1);
+            mbar_init(bar(i), i == D_FREE ? 16 : i >= DS ? 8 : i == DQ_FREE ? 4 : i >= KEMPTY ? 2 : i >= INFO_EMPTY ? 3 + 16 + 4 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) alloc_tmem(tmem_slot);
@@ -793,205 +763,286 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem_ptr(tmem_slot));
     pdl_wait();      // set-up done; global memory is touched from here on
-    pdl_trigger();
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.err = 0;
     const uint32_t tQ_hi = tmem, tQ_lo = tmem + 64, tdQ = tmem + 128;
-    auto tbuf = [&](int bb) { return tmem + 256u + 128u * (uint32_t)bb; };
-    const int2 range = block_range(g.spans.kblock, b, g.T, q0, BR, false);
-    const int kt0 = range.x / BT64, n_t = range.x < range.y ? (range.y - 1) / BT64 + 1 - kt0 : 0;
+    auto tbuf = [&](uint32_t bb) { return tmem + 256u + 128u * bb; };
+    auto next = [&](int i, Item& it, bool whole_warp) -> bool {     // every role walks the same items
+        return get_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i, it, g.err, whole_warp);
+    };
 
-    if (warp == 0) {
-        if (lane == 0 && n_t > 0) {
-            mbar_expect_tx(bar(DO_FULL), kResBytes);
-            for (int kb = 0; kb < 2; ++kb)
-                tma_load_3d(do_s + kb * (kResBytes / 2), &tmDOres, bar(DO_FULL), h * HD + kb * 32, row_base + q0, 0);
-            auto load_kmajor = [&](int t) -> bool {
-                const int st = t & 1, k0 = row_base + (kt0 + t) * BT64;
-                if (!mbar_wait_ool(bar(KEMPTY0 + st), ((t >> 1) & 1u) ^ 1u, g.err, 151)) return false;
-                mbar_expect_tx(bar(KFULL0 + st), 2u * kTile);
-                for (int kb = 0; kb < 2; ++kb) {
-                    tma_load_3d(kk_s(st) + kb * (kTile / 2), &tmKk, bar(KFULL0 + st), g.C + h * HD + kb * 32, k0, 0);
-                    tma_load_3d(vk_s(st) + kb * (kTile / 2), &tmVk, bar(KFULL0 + st), 2 * g.C + h * HD + kb * 32, k0, 0);
+    if (warp < 4) {
+        set_regs_down<kRegsIssueDq>();
+        if (warp == 0) {
+            if (lane == 0) {
+                uint32_t gt = 0, di = 0;                // tiles and non-empty items before this item
+                Item it = make_item(g, args.head_group, (int)blockIdx.x, (int)blockIdx.y, false, BR, BT64);
+                bool ok = true;
+                for (int i = 0; ok; ++i) {
+                    ok = put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i, it, g.err);
+                    if (!ok || it.n < 0) break;
+                    if (it.n == 0) ask_next(answer, bar(NEXT));
+                    Item follows{0, 0, 0, -1};
+                    auto look_up = [&]() -> bool {      // asked for and looked up as in the forward
+                        if (!mbar_wait(bar(NEXT), (uint32_t)i & 1u, g.err, 120)) return false;
+                        int x, y;
+                        if (next_item(answer, x, y)) follows = make_item(g, args.head_group, x, y, false, BR, BT64);
+                        return true;
+                    };
+                    if (it.n == 0) ok = look_up();
+                    const int h = it.bh % g.H, row0 = (it.bh / g.H) * g.T;
+                    // K and V (K-major) of tile t + 1 go out before the single MN-major K buffer is waited for
+                    for (int t = -1; t < it.n && it.n > 0 && ok; ++t) {
+                        if (t == max(-1, it.n - 4)) ask_next(answer, bar(NEXT));
+                        if (t == it.n - 1) ok = look_up();
+                        if (!ok) break;
+                        if (t + 1 < it.n) {
+                            const uint32_t ga = gt + (uint32_t)(t + 1), st = ga & 1u;
+                            ok = mbar_wait(bar(KEMPTY + st), ((ga >> 1) & 1u) ^ 1u, g.err, 151);
+                            if (!ok) break;
+                            mbar_expect_tx(bar(KFULL + st), 2u * kTile);
+                            for (int kb = 0; kb < 2; ++kb) {
+                                tma_load_3d(kv_s + 2u * st * kTile + kb * (kTile / 2), &tmKk, bar(KFULL + st), g.C + h * HD + kb * 32, row0 + (it.t0 + t + 1) * BT64, 0);
+                                tma_load_3d(kv_s + (2u * st + 1u) * kTile + kb * (kTile / 2), &tmVk, bar(KFULL + st), 2 * g.C + h * HD + kb * 32, row0 + (it.t0 + t + 1) * BT64, 0);
+                            }
+                        }
+                        if (t < 0) {                    // dO, once the previous item's last dP is done with it
+                            ok = mbar_wait(bar(DO_EMPTY), (di & 1u) ^ 1u, g.err, 152);
+                            if (!ok) break;
+                            mbar_expect_tx(bar(DO_FULL), kResBytes);
+                            for (int kb = 0; kb < 2; ++kb)
+                                tma_load_3d(do_s + kb * (kResBytes / 2), &tmDOres, bar(DO_FULL), h * HD + kb * 32, row0 + it.blk * BR, 0);
+                        } else {
+                            ok = mbar_wait(bar(MEMPTY), ((gt + (uint32_t)t) & 1u) ^ 1u, g.err, 153);
+                            if (!ok) break;
+                            mbar_expect_tx(bar(MFULL), kTile);
+                            for (int grp = 0; grp < 2; ++grp)
+                                tma_load_3d(km_s + grp * (kTile / 2), &tmKm, bar(MFULL), g.C + h * HD + grp * 32, row0 + (it.t0 + t) * BT64, 0);
+                        }
+                    }
+                    gt += (uint32_t)it.n;
+                    if (it.n > 0) ++di;
+                    it = follows;
                 }
-                return true;
-            };
-            // the K-major tiles of t + 1 go out before the wait for the single MN-major buffer
-            bool ok = load_kmajor(0);
-            for (int t = 0; t < n_t && ok; ++t) {
-                if (t + 1 < n_t) ok = load_kmajor(t + 1);
-                // the MN-major buffer first stages the query rows
-                if (ok && t == 0) ok = mbar_wait_ool(bar(Q_READY), 0, g.err, 152);
-                if (ok) ok = mbar_wait_ool(bar(MEMPTY), (t & 1u) ^ 1u, g.err, 153);
-                if (!ok) break;
-                mbar_expect_tx(bar(MFULL), kTile);
-                for (int grp = 0; grp < 2; ++grp)
-                    tma_load_3d(km_s + grp * (kTile / 2), &tmKm, bar(MFULL), g.C + h * HD + grp * 32, row_base + (kt0 + t) * BT64, 0);
+                if (!ok) settle();
             }
-            if (!ok) settle();
-        }
-    } else if (warp == 1 || warp == kWarpMma2) {
-        if (lane == 0 && n_t > 0) {
+        } else if (warp < 3) {
             constexpr uint32_t idesc = make_idesc_tf32(BR, BT64, false, false);
             const bool s_product = warp == 1;
-            bool ok = s_product ? mbar_wait_ool(bar(Q_READY), 0, g.err, 154) : mbar_wait_ool(bar(DO_FULL), 0, g.err, 155);
             const DescBase dod = kmaj_base(do_s);
-            for (int t = 0; t < n_t && ok; ++t) {
-                const int st = t & 1;
-                if (!mbar_wait_ool(bar(KFULL0 + st), (t >> 1) & 1u, g.err, 156)) { ok = false; break; }
-                // buffer t & 1: the dQ product of tile t - 2 has read it
-                if (t >= 2 && !mbar_wait_ool(bar(DONE0 + st), ((t - 2) >> 1) & 1u, g.err, 157)) { ok = false; break; }
-                tc_fence_after();
-                if (s_product) {
-                    const uint32_t d = tbuf(st);
-                    const DescBase kd = kmaj_base(kk_s(st));
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) {
-                        umma_tf32_ts(d, tQ_lo + ks * 8, kd.at(kmaj_off(BT64, ks, false)), idesc, ks > 0 ? 1u : 0u);
-                        umma_tf32_ts(d, tQ_hi + ks * 8, kd.at(kmaj_off(BT64, ks, true)), idesc, 1u);
-                    }
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(d, tQ_hi + ks * 8, kd.at(kmaj_off(BT64, ks, false)), idesc, 1u);
-                } else {
-                    const uint32_t d = tbuf(st) + 64u;
-                    const DescBase vd = kmaj_base(vk_s(st));
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) {
-                        umma_tf32(d, dod.at(kmaj_off(BR, ks, true)), vd.at(kmaj_off(BT64, ks, false)), idesc, ks > 0 ? 1u : 0u);
-                        umma_tf32(d, dod.at(kmaj_off(BR, ks, false)), vd.at(kmaj_off(BT64, ks, true)), idesc, 1u);
-                    }
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)
-                        umma_tf32(d, dod.at(kmaj_off(BR, ks, false)), vd.at(kmaj_off(BT64, ks, false)), idesc, 1u);
-                }
-                umma_commit(bar(KEMPTY0 + st));
-                umma_commit(bar(SDP0 + st));
-            }
-        }
-    } else if (warp == kWarpMma3) {
-        if (lane == 0 && n_t > 0) {
-            constexpr uint32_t idesc = make_idesc_tf32(BR, HD, false, true), idesc2 = make_idesc_tf32(BR, 2 * HD, false, true);
+            uint32_t gt = 0, ni = 0;
+            Item it;
             bool ok = true;
+            for (int i = 0; ok && (ok = next(i, it, true)) && it.n >= 0; ++i) {
+                if (it.n == 0) continue;
+                ok = mbar_wait_warp(bar(s_product ? Q_READY : DO_FULL), ni & 1u, g.err, 154);
+                for (int t = 0; t < it.n && ok; ++t, ++gt) {
+                    const uint32_t st = gt & 1u;
+                    if (!mbar_wait_warp(bar(KFULL + st), (gt >> 1) & 1u, g.err, 156)) { ok = false; break; }
+                    // buffer st: the dQ product of two tiles before has read it
+                    if (gt >= 2 && !mbar_wait_warp(bar(DONE + st), ((gt >> 1) - 1u) & 1u, g.err, 157)) { ok = false; break; }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        if (s_product) {
+                            const uint32_t dst = tbuf(st);
+                            const DescBase kd = kmaj_base(kv_s + 2u * st * kTile);
+#pragma unroll
+                            for (int ks = 0; ks < 8; ++ks) {
+                                umma_tf32_ts(dst, tQ_lo + ks * 8, kd.at(kmaj_off(BT64, ks, false)), idesc, ks > 0 ? 1u : 0u);
+                                umma_tf32_ts(dst, tQ_hi + ks * 8, kd.at(kmaj_off(BT64, ks, true)), idesc, 1u);
+                            }
+#pragma unroll
+                            for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(dst, tQ_hi + ks * 8, kd.at(kmaj_off(BT64, ks, false)), idesc, 1u);
+                        } else {
+                            const uint32_t dst = tbuf(st) + 64u;
+                            const DescBase vd = kmaj_base(kv_s + (2u * st + 1u) * kTile);
+#pragma unroll
+                            for (int ks = 0; ks < 8; ++ks) {
+                                umma_tf32(dst, dod.at(kmaj_off(BR, ks, true)), vd.at(kmaj_off(BT64, ks, false)), idesc, ks > 0 ? 1u : 0u);
+                                umma_tf32(dst, dod.at(kmaj_off(BR, ks, false)), vd.at(kmaj_off(BT64, ks, true)), idesc, 1u);
+                            }
+#pragma unroll
+                            for (int ks = 0; ks < 8; ++ks)
+                                umma_tf32(dst, dod.at(kmaj_off(BR, ks, false)), vd.at(kmaj_off(BT64, ks, false)), idesc, 1u);
+                        }
+                        umma_commit(bar(KEMPTY + st));
+                        umma_commit(bar(SDP + st));
+                        if (t == it.n - 1) umma_commit(bar(s_product ? Q_FREE : DO_EMPTY));
+                    }
+                    __syncwarp();
+                }
+                ++ni;
+            }
+        } else {
+            constexpr uint32_t idesc = make_idesc_tf32(BR, HD, false, true), idesc2 = make_idesc_tf32(BR, 2 * HD, false, true);
             const DescBase kmd = mn_base(km_s), kmd4 = make_desc_base(km_s, BT64 * 128u, 512u, 1u);
-            for (int t = 0; t < n_t && ok; ++t) {
-                const int bb = t & 1;
-                if (!mbar_wait_ool(bar(DS0 + bb), (t >> 1) & 1u, g.err, 158)) { ok = false; break; }
-                if (!mbar_wait_ool(bar(MFULL), t & 1u, g.err, 159)) { ok = false; break; }
-                if (t > 0 && !mbar_wait_ool(bar(DQ_FREE), (t - 1) & 1u, g.err, 160)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t s_hi = tbuf(bb), s_lo = tbuf(bb) + 64u;
-                // one large term, to set all columns, then the small ones, then the other large ones
-                umma_tf32_ts(tdQ, s_hi, kmd4.at(mn_off(0, false)), idesc2, 0u);
+            uint32_t gt = 0;
+            Item it;
+            bool ok = true;
+            for (int i = 0; ok && (ok = next(i, it, true)) && it.n >= 0; ++i) {
+                for (int t = 0; t < it.n && ok; ++t, ++gt) {
+                    const uint32_t bb = gt & 1u;
+                    if (!mbar_wait_warp(bar(MFULL), gt & 1u, g.err, 159)) { ok = false; break; }
+                    if (gt > 0 && !mbar_wait_warp(bar(DQ_FREE), (gt - 1u) & 1u, g.err, 160)) { ok = false; break; }
+                    if (!mbar_wait_warp(bar(DS + bb), (gt >> 1) & 1u, g.err, 158)) { ok = false; break; }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t s_hi = tbuf(bb), s_lo = s_hi + 64u;
+                        // one large term, to set all columns, then the small ones, then the other large ones
+                        umma_tf32_ts(tdQ, s_hi, kmd4.at(mn_off(0, false)), idesc2, 0u);
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(tdQ + 32u, s_lo + ks * 8, kmd.at(mn_off(ks, false)), idesc, 1u);
+                        for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(tdQ + 32u, s_lo + ks * 8, kmd.at(mn_off(ks, false)), idesc, 1u);
 #pragma unroll
-                for (int ks = 1; ks < 8; ++ks) umma_tf32_ts(tdQ, s_hi + ks * 8, kmd4.at(mn_off(ks, false)), idesc2, 1u);
-                umma_commit(bar(MEMPTY));
-                umma_commit(bar(DONE0 + bb));
-                umma_commit(bar(DQ_FULL));
+                        for (int ks = 1; ks < 8; ++ks) umma_tf32_ts(tdQ, s_hi + ks * 8, kmd4.at(mn_off(ks, false)), idesc2, 1u);
+                        umma_commit(bar(MEMPTY));
+                        umma_commit(bar(DONE + bb));
+                        umma_commit(bar(DQ_FULL));
+                    }
+                    __syncwarp();
+                }
             }
         }
-    } else if (warp >= kWarpAdd) {
-        const int lane_group = warp & 3;
-        const uint32_t t_row = tdQ + ((uint32_t)(lane_group * 32) << 16);
-        float acc[2][32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) acc[0][i] = acc[1][i] = 0.f;
+    } else if (warp < 20) {
+        set_regs_down<kRegsElemDq>();
+        const uint32_t pair = (uint32_t)(warp - 4) >> 3, part = ((uint32_t)(warp - 4) >> 2) & 1u;   // 32 part .. of a tile's keys
+        const int lane_group = warp & 3, rloc = lane_group * 32 + lane;
+        const uint32_t t_lane = (uint32_t)(lane_group * 32) << 16, c0 = 32u * part;
+        const uint32_t tb = tbuf(pair) + t_lane + c0;
+        float* dsm = reinterpret_cast<float*>(smem_ptr(bars + 512u));        // [2][128]: D over each half of the head's columns
+        uint32_t gt = 0, ni = 0;
+        Item it;
         bool ok = true;
-        for (int t = 0; t < n_t && ok; ++t) {
-            if (!mbar_wait_warp_ool(bar(DQ_FULL), t & 1u, g.err, 161)) { ok = false; break; }
-            tc_fence_after();
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t r[32], r2[32];
-                tmem_ld32(t_row + half * 64, r);
-                tmem_ld32(t_row + half * 64 + 32, r2);
-                tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 32; ++i) acc[half][i] += __uint_as_float(r[i]) + __uint_as_float(r2[i]);
+        for (int i = 0; ok && (ok = next(i, it, true)) && it.n >= 0; ++i) {
+            const int b = it.bh / g.H, h = it.bh % g.H, row = it.blk * BR + rloc, rc = min(row, g.T - 1);
+            const Score sc = make_score<CAP, SLOPE>(1.0f / sqrtf((float)HD), g.cap, g.slopes, h);
+            const int64_t lb = (int64_t)it.bh * g.T;
+            if (it.n == 0) {                            // rows that read nothing: D only has to be finite
+                if (pair == 0 && part == 0 && row < g.T) g.dvec[lb + row] = 0.f;
+                continue;
             }
-            tc_fence_before();
+            if (pair == (gt & 1u)) {
+                // this pair has the item's first tile: D of 32 columns here, and Q' = Q * unit into tensor memory
+                const int64_t at = ((int64_t)b * g.T + rc) * g.C + (int64_t)h * HD + c0;
+                const int64_t qat = ((int64_t)b * g.T + rc) * 3 * (int64_t)g.C + (int64_t)h * HD + c0;
+                float d = 0.f;
+#pragma unroll 1
+                for (int q = 0; q < 32; q += 8) {
+                    float x[8], y[8], z[8];
+                    load_sector(g.o + at + q, x);
+                    load_sector(g.d_o + at + q, y);
+                    load_sector(g.d_o_lo + at + q, z);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) d = fmaf(x[e], y[e] + z[e], d);
+                }
+                // everyone has read the D, and the last S is done with the Q', of the item before
+                if (ni > 0 && (!mbar_wait_warp(bar(D_FREE), (ni - 1u) & 1u, g.err, 163) ||
+                               !mbar_wait_warp(bar(Q_FREE), (ni - 1u) & 1u, g.err, 164))) { ok = false; break; }
+                tc_fence_after();
+                dsm[part * 128u + (uint32_t)rloc] = d;
+                __threadfence_block();
+#pragma unroll 1
+                for (int q = 0; q < 32; q += 8) {
+                    float x[8], y[8];
+                    uint32_t hi[8], lo[8];
+                    load_sector(g.qkv + qat + q, x);
+                    load_sector(g.qkv_lo + qat + q, y);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) split_tf32_int((x[e] + y[e]) * sc.unit, hi[e], lo[e]);
+                    tmem_stn(tQ_hi + t_lane + c0 + q, hi);
+                    tmem_stn(tQ_lo + t_lane + c0 + q, lo);
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(Q_READY));
+            }
+            const float L = __ldg(g.lse + lb + rc) * kLog2e;
+            const int2 span = row_range(g.spans.k, b, g.T, row, false);
+            if (!mbar_wait_warp(bar(Q_READY), ni & 1u, g.err, 165)) { ok = false; break; }   // both pairs: no phase is missed
+            ++ni;
+            const float D = dsm[rloc] + dsm[128 + rloc];
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(DQ_FREE));
-        }
-        if (ok) {
-            const float scale = 1.0f / sqrtf((float)HD);
-            const int wrow0 = q0 + lane_group * 32, nvalid = max(0, min(32, g.T - wrow0));
-            const int64_t gs = 3 * (int64_t)g.C, off = (int64_t)(row_base + wrow0) * gs + h * HD;
-            // every product has completed: the K-major tiles are idle
-            float* tile = reinterpret_cast<float*>(smem_ptr(kk_s(0)) + (uint32_t)lane_group * kRowTileBytes);
+            if (lane == 0) mbar_arrive(bar(D_FREE));
+            if (pair == (gt & 1u) && part == 0 && row < g.T) g.dvec[lb + row] = D;
+            for (int t = (int)(pair ^ (gt & 1u)); t < it.n; t += 2) {
+                const uint32_t ga = gt + (uint32_t)t;
+                const int k0 = (it.t0 + t) * BT64 + (int)c0;
+                if (!mbar_wait_warp(bar(SDP + pair), (ga >> 1) & 1u, g.err, 162)) { ok = false; break; }
+                tc_fence_after();
+                const bool whole = k0 >= span.x && k0 + 32 <= span.y;
+#pragma unroll 1
+                for (int q = 0; q < 32; q += 16) {
+                    float x[16], f[16];
+                    uint32_t s[16], dp[16];
+                    tmem_ldn(tb + q, s);
+                    tmem_ldn(tb + 64u + q, dp);
+                    tmem_ld_wait();
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
+                    for (int k = 0; k < 16; ++k) x[k] = __uint_as_float(s[k]);
+                    score_tile<CAP, SLOPE, true, false, 16>(x, f, sc, row - k0 - q, L);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) acc[half][i] *= scale;
-                warp_rows_store(acc[half], tile, lane, nvalid, g.dqkv ? g.dqkv + off + half * 32 : nullptr,
-                                g.dqkv_hi ? g.dqkv_hi + off + half * 32 : nullptr, g.dqkv_hi ? g.dqkv_lo + off + half * 32 : nullptr,
-                                gs, nullptr);
+                    for (int k = 0; k < 16; ++k) x[k] = ex2_approx(x[k]);
+                    if (!whole) {
+                        const uint32_t bits = column_bits<16>(span, k0 + q);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)
+                            if (!(bits >> k & 1u)) x[k] = 0.f;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        float ds = x[k] * (__uint_as_float(dp[k]) - D);
+                        if (CAP) ds *= f[k];
+                        split_tf32_int(ds, s[k], dp[k]);
+                    }
+                    tmem_stn(tb + q, s);                                // dS hi over S
+                    tmem_stn(tb + 64u + q, dp);                         // dS lo over dP
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(DS + pair));
             }
+            gt += (uint32_t)it.n;
         }
     } else {
-        const int wg = (warp - 2) >> 2, lane_group = warp & 3;
-        const int row = q0 + lane_group * 32 + lane;
-        const uint32_t t_lane = ((uint32_t)(lane_group * 32) << 16);
-        const Score sc = make_score<CAP, SLOPE>(1.0f / sqrtf((float)HD), g.cap, g.slopes, h);
+        set_regs_up<kRegsAddDq>();
+        const int lane_group = warp & 3, rloc = lane_group * 32 + lane;
+        const uint32_t t_row = tdQ + ((uint32_t)(lane_group * 32) << 16);
+        const float scale = 1.0f / sqrtf((float)HD);
         const int64_t gs = 3 * (int64_t)g.C;
-        const int64_t lb = ((int64_t)b * g.H + h) * g.T;
-        const int wrow0 = min(q0 + lane_group * 32, g.T - 1), wvalid = max(1, min(32, g.T - wrow0));
-        if (wg == 0 && n_t > 0) {
-            const int64_t off = (int64_t)(row_base + wrow0) * gs + h * HD;
-            float* tile = reinterpret_cast<float*>(smem_ptr(km_s) + (uint32_t)lane_group * kRowTileBytes);
-            rows_to_tmem(g.qkv + off, g.qkv_lo + off, gs, wvalid, sc.unit, tQ_hi + t_lane, tQ_lo + t_lane, tile, lane);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tile is next written by TMA
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(Q_READY));
-        }
-        float* dsm = reinterpret_cast<float*>(smem_ptr(bars + 256u));
-        if (wg == 1) {
-            const long long off = (long long)(row_base + wrow0) * g.C + h * HD;
-            const float d = rows_dot(g.o + off, g.d_o + off, g.d_o_lo + off, g.C, wvalid, lane);
-            dsm[lane_group * 32 + lane] = d;
-            if (row < g.T) g.dvec[lb + row] = d;
-        }
-        asm volatile("bar.sync 2, 256;" ::: "memory");    // the eight element-wise warps, exactly once
-        const float L = g.lse[lb + min(row, g.T - 1)] * kLog2e, D = dsm[lane_group * 32 + lane];
-        const int2 span = row_range(g.spans.k, b, g.T, row, false);
+        uint32_t gt = 0;
+        Item it;
         bool ok = true;
-        const uint32_t tb = tbuf(wg) + t_lane;
-        for (int t = wg; t < n_t && ok; t += 2) {
-            const int k0 = (kt0 + t) * BT64;
-            if (!mbar_wait_warp_ool(bar(SDP0 + wg), (t >> 1) & 1u, g.err, 162)) { ok = false; break; }
-            tc_fence_after();
+        for (int i = 0; ok && (ok = next(i, it, true)) && it.n >= 0; ++i) {
+            float acc[64];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int kh = k0 + half * 32;
-                float x[32], f[32];
-                uint32_t s[32], dp[32];
-                tmem_ld32(tb + half * 32u, s);
-                tmem_ld32(tb + 64u + half * 32u, dp);
-                tmem_ld_wait();
+            for (int k = 0; k < 64; ++k) acc[k] = 0.f;
+            for (int t = 0; t < it.n; ++t, ++gt) {
+                if (!mbar_wait_warp(bar(DQ_FULL), gt & 1u, g.err, 161)) { ok = false; break; }
+                tc_fence_after();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(s[i]);
-                score_tile<CAP, SLOPE, true, false, 32>(x, f, sc, row - kh, L);
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t r[16], r2[16];
+                    tmem_ldn(t_row + (uint32_t)(64 * (q >> 1) + 16 * (q & 1)), r);
+                    tmem_ldn(t_row + (uint32_t)(64 * (q >> 1) + 16 * (q & 1) + 32), r2);
+                    tmem_ld_wait();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] = ex2_approx(x[i]);
-                if (kh < span.x || kh + 32 > span.y) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (kh + i < span.x || kh + i >= span.y) x[i] = 0.f;
+                    for (int k = 0; k < 16; ++k) acc[16 * q + k] += __uint_as_float(r[k]) + __uint_as_float(r2[k]);
                 }
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    float ds = x[i] * (__uint_as_float(dp[i]) - D);
-                    if (CAP) ds *= f[i];
-                    split_tf32_int(ds, s[i], dp[i]);
-                }
-                tmem_st32(tb + half * 32u, s);                      // dS hi over S
-                tmem_st32(tb + 64u + half * 32u, dp);               // dS lo over dP
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(DQ_FREE));
             }
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(DS0 + wg));
+            const int b = it.bh / g.H, h = it.bh % g.H, row = it.blk * BR + rloc;
+            if (ok && row < g.T) {
+                const int64_t at = ((int64_t)b * g.T + row) * gs + (int64_t)h * HD;
+#pragma unroll
+                for (int q = 0; q < 64; q += 8) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = acc[q + e] * scale;
+                    store_sector(v, at + q, g.dqkv, g.dqkv_hi, g.dqkv_lo);
+                }
+            }
         }
     }
     tc_fence_before();
