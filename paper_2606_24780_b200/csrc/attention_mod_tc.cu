@@ -119,10 +119,8 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         if (warp == 0 && lane == 0) {
             uint32_t c = 0, qi = 0;                     // loads and non-empty items so far
             Item it = make_item(g, args.head_group, (int)blockIdx.x, (int)blockIdx.y, false, BR, BT64);
-            bool ok = true;
-            for (int i = 0; ok; ++i) {
-                ok = put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i, it, g.err);
-                if (!ok || it.n < 0) break;
+            bool ok = put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), 0, it, g.err);
+            for (int i = 0; ok && it.n >= 0; ++i) {
                 // The next item is asked for five loads before this one's last and looked up before the last, so that its
                 // loads follow at once (a boundary cost 6,000 clocks when it was asked for only then; asked for at the
                 // start, the last items of long walks are spread worse: 10 % at 8,192 positions).
@@ -133,7 +131,7 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     if (!mbar_wait(bar(NEXT), (uint32_t)i & 1u, g.err, 120)) return false;
                     int x, y;
                     if (next_item(answer, x, y)) follows = make_item(g, args.head_group, x, y, false, BR, BT64);
-                    return true;
+                    return put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i + 1, follows, g.err);
                 };
                 if (it.n == 0) ok = look_up();
                 const int h = it.bh % g.H, row0 = (it.bh / g.H) * g.T;
@@ -420,10 +418,8 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
         if (warp == 0 && lane == 0) {
             uint32_t gt = 0, vi = 0;                    // tiles and non-empty items before this item
             Item it = make_item(g, args.head_group, (int)blockIdx.x, (int)blockIdx.y, true, BR, BT64);
-            bool ok = true;
-            for (int i = 0; ok; ++i) {
-                ok = put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i, it, g.err);
-                if (!ok || it.n < 0) break;
+            bool ok = put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), 0, it, g.err);
+            for (int i = 0; ok && it.n >= 0; ++i) {
                 const int last = 4 * it.n + 1;          // asked for and looked up as in the forward
                 if (it.n == 0) ask_next(answer, bar(NEXT));
                 Item follows{0, 0, 0, -1};
@@ -431,14 +427,14 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
                     if (!mbar_wait(bar(NEXT), (uint32_t)i & 1u, g.err, 120)) return false;
                     int x, y;
                     if (next_item(answer, x, y)) follows = make_item(g, args.head_group, x, y, true, BR, BT64);
-                    return true;
+                    return put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i + 1, follows, g.err);
                 };
                 if (it.n == 0) ok = look_up();
                 const int h = it.bh % g.H, row0 = (it.bh / g.H) * g.T;
                 // in the order the products consume them: S^T(0), dP^T(0), then per tile dV(t), S^T(t+1), dK(t), dP^T(t+1)
                 for (int p = 0; it.n > 0 && p <= last && ok; ++p) {
-                    if (p == max(0, last - 6)) ask_next(answer, bar(NEXT));
-                    if (p == last) ok = look_up();
+                    if (p == max(0, last - 8)) ask_next(answer, bar(NEXT));
+                    if (p == max(1, last - 3)) ok = look_up();
                     if (!ok) break;
                     // j: 0 dO MN-major (t), 1 Q K-major (t+1), 2 Q MN-major (t), 3 dO K-major (t+1); first Q(0), dO(0) K-major
                     const int j = p == 0 ? 1 : p == 1 ? 3 : (p - 2) & 3;
@@ -754,7 +750,7 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < N_BARS; ++i)
-            mbar_init(bar(i), i == D_FREE ? 16 : i >= DS ? 8 : i == DQ_FREE ? 4 : i >= KEMPTY ? 2 : i >= INFO_EMPTY ? 3 + 16 + 4 : 1);
+            mbar_init(bar(i), i == DO_EMPTY ? 9 : i == D_FREE ? 16 : i >= DS ? 8 : i == DQ_FREE ? 4 : i >= KEMPTY ? 2 : i >= INFO_EMPTY ? 3 + 16 + 4 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) alloc_tmem(tmem_slot);
@@ -776,17 +772,15 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
             if (lane == 0) {
                 uint32_t gt = 0, di = 0;                // tiles and non-empty items before this item
                 Item it = make_item(g, args.head_group, (int)blockIdx.x, (int)blockIdx.y, false, BR, BT64);
-                bool ok = true;
-                for (int i = 0; ok; ++i) {
-                    ok = put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i, it, g.err);
-                    if (!ok || it.n < 0) break;
+                bool ok = put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), 0, it, g.err);
+                for (int i = 0; ok && it.n >= 0; ++i) {
                     if (it.n == 0) ask_next(answer, bar(NEXT));
                     Item follows{0, 0, 0, -1};
                     auto look_up = [&]() -> bool {      // asked for and looked up as in the forward
                         if (!mbar_wait(bar(NEXT), (uint32_t)i & 1u, g.err, 120)) return false;
                         int x, y;
                         if (next_item(answer, x, y)) follows = make_item(g, args.head_group, x, y, false, BR, BT64);
-                        return true;
+                        return put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i + 1, follows, g.err);
                     };
                     if (it.n == 0) ok = look_up();
                     const int h = it.bh % g.H, row0 = (it.bh / g.H) * g.T;
@@ -920,40 +914,52 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
                 continue;
             }
             if (pair == (gt & 1u)) {
-                // this pair has the item's first tile: D of 32 columns here, and Q' = Q * unit into tensor memory
+                // this pair has the item's first tile: D over 32 columns here (dO lies in shared memory), and Q' = Q * unit
+                // into tensor memory; all loads of a half are on their way together
                 const int64_t at = ((int64_t)b * g.T + rc) * g.C + (int64_t)h * HD + c0;
                 const int64_t qat = ((int64_t)b * g.T + rc) * 3 * (int64_t)g.C + (int64_t)h * HD + c0;
+                const uint8_t* do_row = smem_ptr(do_s + part * (kResBytes / 2)) + rloc * 128;
                 float d = 0.f;
 #pragma unroll 1
-                for (int q = 0; q < 32; q += 8) {
-                    float x[8], y[8], z[8];
-                    load_sector(g.o + at + q, x);
-                    load_sector(g.d_o + at + q, y);
-                    load_sector(g.d_o_lo + at + q, z);
+                for (int q = 0; q < 32; q += 16) {
+                    float o[2][8], x[2][8], y[2][8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) d = fmaf(x[e], y[e] + z[e], d);
-                }
-                // everyone has read the D, and the last S is done with the Q', of the item before
-                if (ni > 0 && (!mbar_wait_warp(bar(D_FREE), (ni - 1u) & 1u, g.err, 163) ||
-                               !mbar_wait_warp(bar(Q_FREE), (ni - 1u) & 1u, g.err, 164))) { ok = false; break; }
-                tc_fence_after();
-                dsm[part * 128u + (uint32_t)rloc] = d;
-                __threadfence_block();
-#pragma unroll 1
-                for (int q = 0; q < 32; q += 8) {
-                    float x[8], y[8];
-                    uint32_t hi[8], lo[8];
-                    load_sector(g.qkv + qat + q, x);
-                    load_sector(g.qkv_lo + qat + q, y);
+                    for (int k = 0; k < 2; ++k) {
+                        load_sector(g.o + at + q + 8 * k, o[k]);
+                        load_sector(g.qkv + qat + q + 8 * k, x[k]);
+                        load_sector(g.qkv_lo + qat + q + 8 * k, y[k]);
+                    }
+                    if (q == 0) {
+                        // dO has landed; everyone has read the D, and the last S is done with the Q', of the item before
+                        if (!mbar_wait_warp(bar(DO_FULL), ni & 1u, g.err, 155) ||
+                            (ni > 0 && (!mbar_wait_warp(bar(D_FREE), (ni - 1u) & 1u, g.err, 163) ||
+                                        !mbar_wait_warp(bar(Q_FREE), (ni - 1u) & 1u, g.err, 164)))) { ok = false; break; }
+                        tc_fence_after();
+                    }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) split_tf32_int((x[e] + y[e]) * sc.unit, hi[e], lo[e]);
+                    for (int k = 0; k < 4; ++k) {       // 16-byte pieces of the row, swizzled by its number
+                        const uint32_t piece = (((uint32_t)q >> 2) + (uint32_t)k) ^ ((uint32_t)rloc & 7u);
+                        const float4 v = add4(*reinterpret_cast<const float4*>(do_row + piece * 16u),
+                                              *reinterpret_cast<const float4*>(do_row + BR * 128u + piece * 16u));
+                        const float* ok4 = &o[k >> 1][4 * (k & 1)];
+                        d = fmaf(v.x, ok4[0], fmaf(v.y, ok4[1], fmaf(v.z, ok4[2], fmaf(v.w, ok4[3], d))));
+                    }
+                    uint32_t hi[16], lo[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) split_tf32_int((x[k >> 3][k & 7] + y[k >> 3][k & 7]) * sc.unit, hi[k], lo[k]);
                     tmem_stn(tQ_hi + t_lane + c0 + q, hi);
                     tmem_stn(tQ_lo + t_lane + c0 + q, lo);
                 }
+                if (!ok) break;
+                dsm[part * 128u + (uint32_t)rloc] = d;
+                __threadfence_block();
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(Q_READY));
+                if (lane == 0) {
+                    mbar_arrive(bar(DO_EMPTY));
+                    mbar_arrive(bar(Q_READY));
+                }
             }
             const float L = __ldg(g.lse + lb + rc) * kLog2e;
             const int2 span = row_range(g.spans.k, b, g.T, row, false);
