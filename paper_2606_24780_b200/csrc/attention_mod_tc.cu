@@ -131,6 +131,14 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     if (!mbar_wait(bar(NEXT), (uint32_t)i & 1u, g.err, 120)) return false;
                     int x, y;
                     if (next_item(answer, x, y)) follows = make_item(g, args.head_group, x, y, false, BR, BT64);
+                    if (follows.n > 0) {
+                        const int h = follows.bh % g.H, row0 = (follows.bh / g.H) * g.T;
+                        for (int kb = 0; kb < 2; ++kb) {
+                            prefetch_box(&tmQ, h * HD + kb * 32, row0 + follows.blk * BR);
+                            prefetch_box(&tmK, g.C + h * HD + kb * 32, row0 + follows.t0 * BT64);
+                            prefetch_box(&tmV, 2 * g.C + h * HD + kb * 32, row0 + follows.t0 * BT64);
+                        }
+                    }
                     return put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i + 1, follows, g.err);
                 };
                 if (it.n == 0) ok = look_up();
@@ -138,8 +146,8 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 for (int p = 0; p < 2 * it.n && ok; ++p, ++c) {
                     const bool is_k = p == 0 || ((p & 1) && p < 2 * it.n - 1);
                     const int t = p == 0 ? 0 : p == 2 * it.n - 1 ? it.n - 1 : is_k ? (p + 1) >> 1 : (p - 2) >> 1;
-                    if (p == max(0, last - 5)) ask_next(answer, bar(NEXT));
-                    if (p == last) ok = look_up();
+                    if (p == max(0, last - 8)) ask_next(answer, bar(NEXT));
+                    if (p == max(1, last - 4)) ok = look_up();
                     if (!ok) break;
                     const uint32_t slot = c % kSlots;
                     ok = mbar_wait(bar(SLOT_EMPTY + slot), ((c / kSlots) & 1u) ^ 1u, g.err, 111);
@@ -427,14 +435,24 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
                     if (!mbar_wait(bar(NEXT), (uint32_t)i & 1u, g.err, 120)) return false;
                     int x, y;
                     if (next_item(answer, x, y)) follows = make_item(g, args.head_group, x, y, true, BR, BT64);
+                    if (follows.n > 0) {
+                        const int h = follows.bh % g.H, row0 = (follows.bh / g.H) * g.T, k0 = row0 + follows.blk * BR;
+                        for (int kb = 0; kb < 2; ++kb) {
+                            prefetch_box(&tmQk, g.C + h * HD + kb * 32, k0);             // K, 64 rows at a time
+                            prefetch_box(&tmQk, g.C + h * HD + kb * 32, k0 + BT64);
+                            prefetch_box(&tmVres, 2 * g.C + h * HD + kb * 32, k0);
+                            prefetch_box(&tmQk, h * HD + kb * 32, row0 + follows.t0 * BT64);
+                            prefetch_box(&tmDOk, h * HD + kb * 32, row0 + follows.t0 * BT64);
+                        }
+                    }
                     return put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i + 1, follows, g.err);
                 };
                 if (it.n == 0) ok = look_up();
                 const int h = it.bh % g.H, row0 = (it.bh / g.H) * g.T;
                 // in the order the products consume them: S^T(0), dP^T(0), then per tile dV(t), S^T(t+1), dK(t), dP^T(t+1)
                 for (int p = 0; it.n > 0 && p <= last && ok; ++p) {
-                    if (p == max(0, last - 8)) ask_next(answer, bar(NEXT));
-                    if (p == max(1, last - 3)) ok = look_up();
+                    if (p == max(0, last - 16)) ask_next(answer, bar(NEXT));
+                    if (p == max(1, last - 11)) ok = look_up();
                     if (!ok) break;
                     // j: 0 dO MN-major (t), 1 Q K-major (t+1), 2 Q MN-major (t), 3 dO K-major (t+1); first Q(0), dO(0) K-major
                     const int j = p == 0 ? 1 : p == 1 ? 3 : (p - 2) & 3;
@@ -780,14 +798,24 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
                         if (!mbar_wait(bar(NEXT), (uint32_t)i & 1u, g.err, 120)) return false;
                         int x, y;
                         if (next_item(answer, x, y)) follows = make_item(g, args.head_group, x, y, false, BR, BT64);
+                        if (follows.n > 0) {
+                            const int h = follows.bh % g.H, row0 = (follows.bh / g.H) * g.T, q0 = row0 + follows.blk * BR;
+                            for (int kb = 0; kb < 2; ++kb) {
+                                prefetch_box(&tmDOres, h * HD + kb * 32, q0);
+                                prefetch_box(&tmKk, h * HD + kb * 32, q0);               // Q, 64 rows at a time
+                                prefetch_box(&tmKk, h * HD + kb * 32, q0 + BT64);
+                                prefetch_box(&tmKk, g.C + h * HD + kb * 32, row0 + follows.t0 * BT64);
+                                prefetch_box(&tmVk, 2 * g.C + h * HD + kb * 32, row0 + follows.t0 * BT64);
+                            }
+                        }
                         return put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i + 1, follows, g.err);
                     };
                     if (it.n == 0) ok = look_up();
                     const int h = it.bh % g.H, row0 = (it.bh / g.H) * g.T;
                     // K and V (K-major) of tile t + 1 go out before the single MN-major K buffer is waited for
                     for (int t = -1; t < it.n && it.n > 0 && ok; ++t) {
-                        if (t == max(-1, it.n - 4)) ask_next(answer, bar(NEXT));
-                        if (t == it.n - 1) ok = look_up();
+                        if (t == max(-1, it.n - 5)) ask_next(answer, bar(NEXT));
+                        if (t == max(0, it.n - 4)) ok = look_up();
                         if (!ok) break;
                         if (t + 1 < it.n) {
                             const uint32_t ga = gt + (uint32_t)(t + 1), st = ga & 1u;
