@@ -17,8 +17,7 @@
 // the threads that add the tiles up rescale by the running maximum.  Tiles, masks, score function and the
 // reason why no accumulator outlives a tile are those of attention_mod_tc.cu.
 //
-//   warp 0 TMA; warps 1, 2, 3 issue X, Y, Out (one thread issues an MMA about every 57 clocks, X and Y are
-//   32 columns wide and would wait for a single issuer); warps 4-7, 8-11 the element-wise pass on alternate
+//   warp 0 TMA; warps 1, 2, 3 issue X, Y, Out; warps 4-7, 8-11 the element-wise pass on alternate
 //   tiles; warps 12-15 add the Out tiles: 128 columns of a row per thread, for which the other
 //   warpgroups give up registers (64 + 2 * 112 + 208 = 496 of the 512 a lane of four warpgroups holds at launch).
 //   tensor memory: A1 hi 0-127, lo 128-255, Out tile 256-383, buffer b at 384 + 64 b: X -> Z_hi, Y -> Z_lo
@@ -142,19 +141,20 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
             }
             if (!ok)
                 for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // let loads in flight land
-        } else if (warp == 1 && lane == 0 && n_t > 0) {
+        } else if (warp == 1 && n_t > 0) {
             // ---- X.  Without Y the 64 columns of a buffer are free: [B1_hi | B1_lo] is one operand of 64 rows, A1_lo B1_hi
             // joins the small half, and the reader adds the halves.  With Y: the small terms first.
             constexpr uint32_t idesc = make_idesc_tf32(BR, BT_, false, false), idesc2 = make_idesc_tf32(BR, 2 * BT_, false, false);
-            bool ok = mbar_wait(bar(A1_READY), 0, g.err, 173);
+            bool ok = mbar_wait_warp(bar(A1_READY), 0, g.err, 173);
             for (int t = 0; t < n_t && ok; ++t) {
                 const int st = t % S1;
                 const uint32_t tX = tbuf(t & 1);
-                if (!mbar_wait(bar(B1_FULL + st), (uint32_t)(t / S1) & 1u, g.err, 175)) { ok = false; break; }
+                if (!mbar_wait_warp(bar(B1_FULL + st), (uint32_t)(t / S1) & 1u, g.err, 175)) { ok = false; break; }
                 // the Out product of tile t - 2 has read this buffer
-                if (t >= 2 && !mbar_wait(bar(Z_DONE0 + (t & 1)), (uint32_t)((t - 2) >> 1) & 1u, g.err, 176)) { ok = false; break; }
+                if (t >= 2 && !mbar_wait_warp(bar(Z_DONE0 + (t & 1)), (uint32_t)((t - 2) >> 1) & 1u, g.err, 176)) { ok = false; break; }
                 tc_fence_after();
                 const DescBase bd = kmaj_base(b1_stage(st));
+                if (elect_one()) {
                 if (kHasY) {
 #pragma unroll
                     for (int ks = 0; ks < 16; ++ks) {
@@ -172,16 +172,19 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
                 }
                 umma_commit(bar(B1_EMPTY + st));
                 umma_commit(bar(XY_FULL0 + (t & 1)));
+                }
+                __syncwarp();
             }
-        } else if (kHasY && warp == 2 && lane == 0 && n_t > 0) {
+        } else if (kHasY && warp == 2 && n_t > 0) {
             constexpr uint32_t idesc = make_idesc_tf32(BR, BT_, false, false);
-            bool ok = mbar_wait(bar(A2_FULL), 0, g.err, 174);
+            bool ok = mbar_wait_warp(bar(A2_FULL), 0, g.err, 174);
             const DescBase ad = kmaj_base(a2_s), bd = kmaj_base(b2_s);
             for (int t = 0; t < n_t && ok; ++t) {
                 const uint32_t tY = tbuf(t & 1) + 32u;
-                if (!mbar_wait(bar(B2_FULL), (uint32_t)t & 1u, g.err, 177)) { ok = false; break; }
-                if (t >= 2 && !mbar_wait(bar(Z_DONE0 + (t & 1)), (uint32_t)((t - 2) >> 1) & 1u, g.err, 178)) { ok = false; break; }
+                if (!mbar_wait_warp(bar(B2_FULL), (uint32_t)t & 1u, g.err, 177)) { ok = false; break; }
+                if (t >= 2 && !mbar_wait_warp(bar(Z_DONE0 + (t & 1)), (uint32_t)((t - 2) >> 1) & 1u, g.err, 178)) { ok = false; break; }
                 tc_fence_after();
+                if (elect_one()) {
 #pragma unroll
                 for (int ks = 0; ks < 16; ++ks) {
                     umma_tf32(tY, ad.at(kmaj_off(BR, ks, true)), bd.at(kmaj_off(BT_, ks, false)), idesc, ks > 0 ? 1u : 0u);
@@ -192,19 +195,22 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
                     umma_tf32(tY, ad.at(kmaj_off(BR, ks, false)), bd.at(kmaj_off(BT_, ks, false)), idesc, 1u);
                 umma_commit(bar(B2_EMPTY));
                 umma_commit(bar(XY_FULL0 + (t & 1)));
+                }
+                __syncwarp();
             }
-        } else if (warp == 3 && lane == 0 && n_t > 0) {
+        } else if (warp == 3 && n_t > 0) {
             // ---- Out_tile = Z B3, from zero, the small terms first
             constexpr uint32_t idesc = make_idesc_tf32(BR, HD, false, true);
             bool ok = true;
             for (int t = 0; t < n_t && ok; ++t) {
                 const int st = t % S3;
                 const uint32_t z_hi = tbuf(t & 1), z_lo = z_hi + 32u;
-                if (!mbar_wait(bar(Z_READY0 + (t & 1)), (uint32_t)(t >> 1) & 1u, g.err, 179)) { ok = false; break; }
-                if (!mbar_wait(bar(B3_FULL + st), (uint32_t)(t / S3) & 1u, g.err, 180)) { ok = false; break; }
-                if (!mbar_wait(bar(OUT_FREE), (uint32_t)t & 1u, g.err, 181)) { ok = false; break; }
+                if (!mbar_wait_warp(bar(Z_READY0 + (t & 1)), (uint32_t)(t >> 1) & 1u, g.err, 179)) { ok = false; break; }
+                if (!mbar_wait_warp(bar(B3_FULL + st), (uint32_t)(t / S3) & 1u, g.err, 180)) { ok = false; break; }
+                if (!mbar_wait_warp(bar(OUT_FREE), (uint32_t)t & 1u, g.err, 181)) { ok = false; break; }
                 tc_fence_after();
                 const DescBase bd = make_desc_base(b3_stage(st), 2u * BT_ * 128u, 512u, 1u);
+                if (elect_one()) {
 #pragma unroll
                 for (int ks = 0; ks < 4; ++ks) {
                     umma_tf32_ts(tOut, z_lo + ks * 8, bd.at(mn_off(ks, false)), idesc, ks > 0 ? 1u : 0u);
@@ -215,6 +221,8 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
                 umma_commit(bar(B3_EMPTY + st));
                 umma_commit(bar(Z_DONE0 + (t & 1)));
                 umma_commit(bar(OUT_FULL));
+                }
+                __syncwarp();
             }
         }
     } else if (warp < 12) {
@@ -259,44 +267,49 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
             tc_fence_after();
             const bool whole = s0 >= span.x && s0 + BT_ <= span.y;
             if (PASS == P_FWD) {
-                float x[32];
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint32_t r[16], q[16];
-                    tmem_ldn(tb + 16u * half, r);
-                    tmem_ldn(tb + 32u + 16u * half, q);
+                // the reference from the large half of the scores: any value near the maximum will do
+                float top = -INFINITY, sum = 0.f;
+#pragma unroll 1
+                for (int q = 0; q < 32; q += 16) {
+                    float z[16], none[16];
+                    uint32_t r[16];
+                    tmem_ldn(tb + q, r);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[16 * half + i] = __uint_as_float(r[i]) + __uint_as_float(q[i]);
+                    for (int i = 0; i < 16; ++i) z[i] = __uint_as_float(r[i]);
+                    if (SLOPE) score_tile<CAP, SLOPE, false, false, 16>(z, none, sc, own - s0 - q, 0.f);   // else the maximum is at that of the product
+                    const uint32_t bits = whole ? 0xffffu : column_bits<16>(span, s0 + q);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (bits >> i & 1u) top = fmaxf(top, z[i]);
                 }
-                float none[32];
-                score_tile<CAP, SLOPE, false, false, 32>(x, none, sc, own - s0, 0.f);
-                if (!whole) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (s0 + i < span.x || s0 + i >= span.y) x[i] = -INFINITY;
-                }
-                float mx = -INFINITY, sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) mx = fmaxf(mx, x[i]);
-                const float ref = mx == -INFINITY ? 0.f : mx;    // nothing read in this tile: every P is zero
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
+                const bool none_read = top == -INFINITY;                // every P of this tile is zero
+                const float ref = none_read ? 0.f : (CAP && !SLOPE) ? sc.to_log2 * tanh_any(top) : top;
+#pragma unroll 1
+                for (int q = 0; q < 32; q += 16) {
+                    float z[16], none[16];
                     uint32_t hi[16], lo[16];
+                    tmem_ldn(tb + q, hi);
+                    tmem_ldn(tb + 32u + q, lo);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] = __uint_as_float(hi[i]) + __uint_as_float(lo[i]);
+                    score_tile<CAP, SLOPE, false, false, 16>(z, none, sc, own - s0 - q, ref);
+                    const uint32_t bits = whole ? 0xffffu : column_bits<16>(span, s0 + q);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const float p = ex2_approx(x[16 * half + i] - ref);
+                        const float p = (bits >> i & 1u) ? ex2_approx(z[i]) : 0.f;
                         sum += p;
                         split_tf32_int(p, hi[i], lo[i]);
                     }
-                    tmem_stn(tb + 16u * half, hi);
-                    tmem_stn(tb + 32u + 16u * half, lo);
+                    tmem_stn(tb + q, hi);
+                    tmem_stn(tb + 32u + q, lo);
                 }
-                tile_stat[(t & 3) * 256 + rloc] = mx;
+                tile_stat[(t & 3) * 256 + rloc] = none_read ? -INFINITY : ref;
                 tile_stat[(t & 3) * 256 + 128 + rloc] = sum;
                 __threadfence_block();
             } else {
-#pragma unroll
+#pragma unroll 1
                 for (int half = 0; half < 2; ++half) {
                     const int sh = s0 + 16 * half;
                     float x[16], f[16];
@@ -307,24 +320,19 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[i] = kHasY ? __uint_as_float(r[i]) : __uint_as_float(r[i]) + __uint_as_float(y[i]);
                     score_tile<CAP, SLOPE, true, false, 16>(x, f, sc, own - sh, kKeys ? 0.f : L);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = ex2_approx(kKeys ? x[i] - __shfl_sync(0xffffffffu, Lq, 16 * half + i) : x[i]);
-                    if (!whole) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (sh + i < span.x || sh + i >= span.y) x[i] = 0.f;
-                    }
+                    const uint32_t bits = whole ? 0xffffu : column_bits<16>(span, sh);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        float z = x[i];
+                        const float a = kKeys ? x[i] - __shfl_sync(0xffffffffu, Lq, 16 * half + i) : x[i];
+                        float z = (bits >> i & 1u) ? ex2_approx(a) : 0.f;
                         if (kHasY) {
                             z *= __uint_as_float(y[i]) - (PASS == P_DK ? __shfl_sync(0xffffffffu, Dq, 16 * half + i) : D);
                             if (CAP) z *= f[i];
                         }
                         split_tf32_int(z, r[i], y[i]);
                     }
-                    tmem_stn(tb + 16u * half, r);           // Z hi over X
-                    tmem_stn(tb + 32u + 16u * half, y);     // Z lo over Y
+                    tmem_stn(tb + 16u * half, r);            // Z hi over X
+                    tmem_stn(tb + 32u + 16u * half, y);      // Z lo over Y
                 }
             }
             tmem_st_wait();

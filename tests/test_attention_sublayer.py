@@ -352,8 +352,16 @@ def test_spans_of_long_sequences():
     mark = np.zeros((2, T), np.int32)
     mark[0, :4096] = 1
     mark[1, 10000:13000] = 1
+    lone = np.zeros((2, T), np.int32)        # one document per sequence, all of the first and 9,000 of the second in the prefix
+    lone[0], lone[1, :9000] = 1, 1
+    for ids, marks in ((doc, mark), (None, lone), (np.zeros((2, T), np.int32), None)):
+        check_long_spans(ids, marks, T, rng)
+
+
+def check_long_spans(ids, marks, T, rng):
+    doc, mark = np.zeros((2, T), np.int32) if ids is None else ids, np.zeros((2, T), np.int32) if marks is None else marks
     for window in (0, 300):
-        raw = spans_of(doc, mark, window, 2, T).view(torch.int32).cpu().numpy().reshape(-1, 2)
+        raw = spans_of(ids, marks, window, 2, T).view(torch.int32).cpu().numpy().reshape(-1, 2)
         for s in range(2):
             cuts = [0] + list(np.flatnonzero(np.diff(doc[s])) + 1) + [T]
             for a, e in zip(cuts[:-1], cuts[1:]):
