@@ -288,12 +288,12 @@ inline bool plane_map(CUtensorMap* tm, const float* base, int64_t cols, int64_t 
 }
 
 // Runs `stmt` with kCap and kSlope the constants of the call's modification.
-#define BT_FOR_MOD(g, stmt)                                                             \
+#define BT_FOR_MOD(g, ...)                                                             \
     do {                                                                                \
-        if ((g).cap > 0.f && (g).slopes) { constexpr bool kCap = true, kSlope = true; stmt; }   \
-        else if ((g).cap > 0.f) { constexpr bool kCap = true, kSlope = false; stmt; }   \
-        else if ((g).slopes) { constexpr bool kCap = false, kSlope = true; stmt; }      \
-        else { constexpr bool kCap = false, kSlope = false; stmt; }                     \
+        if ((g).cap > 0.f && (g).slopes) { constexpr bool kCap = true, kSlope = true; __VA_ARGS__; }   \
+        else if ((g).cap > 0.f) { constexpr bool kCap = true, kSlope = false; __VA_ARGS__; }   \
+        else if ((g).slopes) { constexpr bool kCap = false, kSlope = true; __VA_ARGS__; }      \
+        else { constexpr bool kCap = false, kSlope = false; __VA_ARGS__; }                     \
     } while (0)
 
 }  // namespace mod

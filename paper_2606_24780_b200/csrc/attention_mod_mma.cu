@@ -430,25 +430,25 @@ __global__ void __launch_bounds__(kThreads, HD == 64 ? 1 : 2) dkv_kernel(const A
 template <int HD>
 constexpr int smem_bytes() { return (4 * kRows * (HD + 4) + 256) * (int)sizeof(float); }
 
-template <typename K>
-cudaError_t go(K kernel, int smem, const AttnModArgs& g, cudaStream_t s) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+template <auto KERNEL>
+cudaError_t go(int smem, const AttnModArgs& g, cudaStream_t s) {
+    const cudaError_t e = allow_smem<KERNEL>(smem);
     if (e != cudaSuccess) return e;
-    BT_KERNEL_LAUNCH(kernel, dim3((g.T + kRows - 1) / kRows, g.B * g.H), kThreads, smem, s, g);
+    BT_KERNEL_LAUNCH(KERNEL, dim3((g.T + kRows - 1) / kRows, g.B * g.H), kThreads, smem, s, g);
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }
 
 template <int HD>
 cudaError_t fwd(const AttnModArgs& g, cudaStream_t s) {
-    BT_FOR_MOD(g, return go(fwd_kernel<HD, kCap, kSlope>, smem_bytes<HD>(), g, s));
+    BT_FOR_MOD(g, return (go<fwd_kernel<HD, kCap, kSlope>>(smem_bytes<HD>(), g, s)));
 }
 template <int HD>
 cudaError_t bwd(const AttnModArgs& g, cudaStream_t s) {
     cudaError_t e;
     BT_FOR_MOD(g, {
-        if ((e = go(dq_kernel<HD, kCap, kSlope>, smem_bytes<HD>(), g, s)) != cudaSuccess) return e;   // first: it forms D
-        return go(dkv_kernel<HD, kCap, kSlope>, smem_bytes<HD>(), g, s);
+        if ((e = go<dq_kernel<HD, kCap, kSlope>>(smem_bytes<HD>(), g, s)) != cudaSuccess) return e;   // first: it forms D
+        return go<dkv_kernel<HD, kCap, kSlope>>(smem_bytes<HD>(), g, s);
     });
 }
 

@@ -1097,7 +1097,7 @@ cudaError_t launch_attention_mod_fwd_tc(const AttnModArgs& g, cudaStream_t s) {
     const dim3 grid(g.B * g.H, (g.T + BR - 1) / BR);
     const ModTcArgs a{g, attn_head_group((int)grid.x, (int)grid.y)};
     BT_FOR_MOD(g, {
-        cudaError_t e = cudaFuncSetAttribute(attn_mod_fwd_kernel<kCap, kSlope>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFwdSmem);
+        cudaError_t e = allow_smem<attn_mod_fwd_kernel<kCap, kSlope>>(kFwdSmem);
         if (e != cudaSuccess) return e;
         BT_KERNEL_LAUNCH((attn_mod_fwd_kernel<kCap, kSlope>), grid, kFwdThreads, kFwdSmem, s, q, k, v, a);
     });
@@ -1115,9 +1115,9 @@ cudaError_t launch_attention_mod_bwd_tc(const AttnModArgs& g, cudaStream_t s) {
     const dim3 grid(g.B * g.H, (g.T + BR - 1) / BR);
     const ModTcArgs a{g, attn_head_group((int)grid.x, (int)grid.y)};
     BT_FOR_MOD(g, {
-        cudaError_t e = cudaFuncSetAttribute(attn_mod_dq_kernel<kCap, kSlope>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDqSmem);
+        cudaError_t e = allow_smem<attn_mod_dq_kernel<kCap, kSlope>>(kDqSmem);
         if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(attn_mod_dkv_kernel<kCap, kSlope>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDkvSmem);
+            e = allow_smem<attn_mod_dkv_kernel<kCap, kSlope>>(kDkvSmem);
         if (e != cudaSuccess) return e;
         // the dq kernel goes first: it also forms D
         BT_KERNEL_LAUNCH((attn_mod_dq_kernel<kCap, kSlope>), grid, kDqThreads, kDqSmem, s, qkv_k, qkv_m, qkv_k, do_res, a);

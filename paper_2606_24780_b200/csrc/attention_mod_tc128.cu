@@ -19,7 +19,7 @@
 //
 //   warp 0 TMA; warps 1, 2, 3 issue X, Y, Out; warps 4-7, 8-11 the element-wise pass on alternate
 //   tiles; warps 12-15 add the Out tiles: 128 columns of a row per thread, for which the other
-//   warpgroups give up registers (64 + 2 * 112 + 208 = 496 of the 512 a lane of four warpgroups holds at launch).
+//   warpgroups give up registers.
 //   tensor memory: A1 hi 0-127, lo 128-255, Out tile 256-383, buffer b at 384 + 64 b: X -> Z_hi, Y -> Z_lo
 //   shared memory: with A2 one buffer per stream; without, its 128 KB are two more stages of B1 and two of B3
 // Waits are inlined: a call would hold a warpgroup to the registers of the callee.
@@ -40,8 +40,12 @@ constexpr uint32_t kRes = 4u * 2u * BR * 128u;     // 128 own rows: 4 k-blocks x
 constexpr uint32_t kTile = 4u * 2u * BT_ * 128u;   // streamed tile: 4 blocks x (hi, lo) x 32 rows x 128 B
 constexpr uint32_t kSmem = 1024u + kRes + 3u * kTile + 256u;
 static_assert(kSmem <= 232448u, "shared memory");
-constexpr int kRegsIssue = 64, kRegsElement = 112, kRegsAdd = 208;
-static_assert(kRegsIssue + 2 * kRegsElement + kRegsAdd <= 65536 / 128, "registers");
+// registers of a lane by warpgroup: issuing, element-wise (two), adding; the passes with Y issue more products
+__host__ __device__ constexpr int regs_issue(bool y) { return y ? 80 : 64; }
+__host__ __device__ constexpr int regs_element(bool y) { return y ? 104 : 112; }
+constexpr int kRegsAdd = 208;
+static_assert(regs_issue(true) + 2 * regs_element(true) + kRegsAdd <= 512 && regs_issue(false) + 2 * regs_element(false) + kRegsAdd <= 512,
+              "registers: 512 threads get 128 each at launch");
 
 enum Pass { P_FWD = 0, P_DQ = 1, P_DK = 2, P_DV = 3 };
 
@@ -111,7 +115,7 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
     const int t0 = range.x / BT_, n_t = range.x < range.y ? (range.y - 1) / BT_ + 1 - t0 : 0;
 
     if (warp < 4) {
-        set_regs_down<kRegsIssue>();
+        set_regs_down<regs_issue(kHasY)>();
         if (warp == 0 && lane == 0 && n_t > 0) {
             if (kHasY) {
                 mbar_expect_tx(bar(A2_FULL), kRes);
@@ -227,7 +231,7 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
         }
     } else if (warp < 12) {
         // ---------------------------------------------------------------- element-wise warpgroups
-        set_regs_down<kRegsElement>();
+        set_regs_down<regs_element(kHasY)>();
         const int wg = (warp - 4) >> 2, lane_group = warp & 3;
         const int rloc = lane_group * 32 + lane, own = r0 + rloc;
         const uint32_t t_lane = ((uint32_t)(lane_group * 32) << 16);
@@ -414,7 +418,7 @@ cudaError_t launch_pass(const CUtensorMap& a2, const CUtensorMap& b1, const CUte
     const AttnModArgs& g = args.a;
     const dim3 grid(g.B * g.H, (g.T + BR - 1) / BR);
     BT_FOR_MOD(g, {
-        const cudaError_t e = cudaFuncSetAttribute(attn_mod128_kernel<PASS, kCap, kSlope>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+        const cudaError_t e = allow_smem<attn_mod128_kernel<PASS, kCap, kSlope>>(kSmem);
         if (e != cudaSuccess) return e;
         BT_KERNEL_LAUNCH((attn_mod128_kernel<PASS, kCap, kSlope>), grid, kThreads, kSmem, s, a2, b1, b2, b3, args);
     });

@@ -158,6 +158,20 @@ cudaError_t launch_k(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t sme
 #define BT_KERNEL_LAUNCH(kernel, grid, block, smem, stream, ...) \
     (void)bt::launch_k(kernel, dim3(grid), dim3(block), (size_t)(smem), stream, __VA_ARGS__)
 
+// Lets KERNEL use `bytes` of dynamic shared memory: once per device and kernel (asking costs a small launch a microsecond).
+template <auto KERNEL>
+cudaError_t allow_smem(size_t bytes) {
+    static std::atomic<unsigned long long> done{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
 enum GemmLayout { kNT = 0, kNN = 1, kTN = 2 };
 
 // One weight matrix of the parameter arena ([rows, cols] row-major at float offset `off`) and the
