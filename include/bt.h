@@ -583,7 +583,8 @@ typedef struct {
  * query that may read no key gets o = 0, lse = -inf and takes no part in the backward.  Layouts as in
  * bt_op_attention_fwd / _bwd (d in {16, 32, 64, 128}); q, k, v and d_o may be given raw and / or as hi/lo planes,
  * the outputs asked for raw and / or as planes.  d = 64 or 128 with planes (in the backward: of both qkv and
- * d_o) runs on tcgen05, d <= 64 otherwise on warp-level MMA, raw d = 128 and BT_FLAG_ATTN_SIMT in plain FP32.
+ * d_o) runs on tcgen05, and so does d = 16 or 32 when T d > 4096 (planes not given are made in scratch); d <= 64
+ * otherwise on warp-level MMA, raw d = 128 and BT_FLAG_ATTN_SIMT in plain FP32.
  * Every row of the inputs must be finite, those behind the mask too (they enter the tensor-core products
  * with weight zero).  At most 2^21 positions, 2^30 rows, 2^24 sequence-heads, 2^33 row-heads.
  * The backward takes the forward's inputs, o (raw) and lse and overwrites all of dqkv:

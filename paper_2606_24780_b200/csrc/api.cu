@@ -1518,8 +1518,10 @@ bt_status dropout_impl(const float* x, const float* residual, int64_t n, double 
     return BT_OK;
 }
 
-// Scratch of the modified attention: the device error word in the first 256 bytes, then [B, H, T] row sums.
+// Scratch of the modified attention: the device error word in the first 256 bytes, then [B, H, T] row sums, then for
+// heads of 16 and 32 columns the planes that their tensor-core kernels read (callers have those as raw arrays).
 constexpr size_t kAttnModHeader = 256;
+size_t attn_mod_sums(int32_t B, int32_t T, int32_t H) { return ((size_t)B * H * T * sizeof(float) + 255) & ~(size_t)255; }
 
 bt_status attn_mod_args(AttnModArgs& g, const char* who, int32_t B, int32_t T, int32_t C, int32_t H, const bt_attn_mod* mod,
                         const float* qkv, const float* qkv_split, void* scratch, size_t scratch_bytes) {
@@ -1539,14 +1541,15 @@ bt_status attn_mod_args(AttnModArgs& g, const char* who, int32_t B, int32_t T, i
     g.cap = mod->softcap;
     g.slopes = mod->slopes;
     g.spans = attention_span_view(mod->spans, B, T);
-    // both forms hold the same values: the planes serve the tensor-core kernels, the raw array the others
-    const bool planes = qkv_split && (!qkv || d >= 64);
+    // both forms hold the same values: the planes serve the tcgen05 kernels, the raw array the others
+    const bool planes = qkv_split && (!qkv || attn_mod_wants_planes(T, d));
     g.qkv = planes ? qkv_split : qkv;
     g.qkv_lo = planes ? qkv_split + n * 3 * C : nullptr;
     g.err = (int*)scratch;
     g.dvec = (float*)((uint8_t*)scratch + kAttnModHeader);
+    g.planes = d < 64 ? (float*)((uint8_t*)scratch + kAttnModHeader + attn_mod_sums(B, T, H)) : nullptr;
     char msg[256];
-    if (planes && d >= 64 && !gemm_tc_init(msg, sizeof(msg))) return fail(BT_ERR_CUDA, "tensor-core attention unavailable: %s", msg);
+    if ((planes || d < 64) && !gemm_tc_init(msg, sizeof(msg))) return fail(BT_ERR_CUDA, "tensor-core attention unavailable: %s", msg);
     return BT_OK;
 }
 
@@ -1590,7 +1593,8 @@ extern "C" bt_status bt_op_attention_spans(const int32_t* doc, const int32_t* pr
 
 extern "C" size_t bt_op_attention_mod_scratch_bytes(int32_t B, int32_t T, int32_t C, int32_t H) {
     if (B < 1 || T < 1 || C < 1 || H < 1) return 0;
-    return kAttnModHeader + (((size_t)B * H * T * sizeof(float) + 255) & ~(size_t)255);
+    const size_t planes = C / H < 64 ? 8 * (size_t)B * T * C * sizeof(float) : 0;
+    return kAttnModHeader + attn_mod_sums(B, T, H) + planes;
 }
 
 extern "C" bt_status bt_op_attention_mod_fwd(const float* qkv, const float* qkv_split, int32_t B, int32_t T, int32_t C,
@@ -1618,7 +1622,7 @@ extern "C" bt_status bt_op_attention_mod_bwd(const float* qkv, const float* qkv_
     AttnModArgs g{};
     if (bt_status st = attn_mod_args(g, "attention_mod_bwd", B, T, C, H, mod, qkv, qkv_split, scratch, scratch_bytes)) return st;
     const int64_t n = (int64_t)B * T;
-    const bool planes = d_o_split && (!d_o || C / H >= 64);
+    const bool planes = d_o_split && (!d_o || attn_mod_wants_planes(T, C / H));
     g.d_o = planes ? d_o_split : d_o;
     g.d_o_lo = planes ? d_o_split + n * C : nullptr;
     g.o = const_cast<float*>(o);

@@ -1,4 +1,4 @@
-// Attention with modified scores on warp-level MMA (head_dim 16, 32, and 64 without planes), 3xTF32.
+// Attention with modified scores on warp-level MMA, 3xTF32: short sequences of heads of 16 and 32 columns, and heads of 64 without planes.
 //
 // One CTA owns 64 rows of one head, 16 per warp, and walks the 64-row tiles of the other side between the ends
 // of its rows' ranges; a warp skips the tiles none of its rows reads.  Streamed tiles go through
@@ -9,8 +9,8 @@
 //   forward  rows = queries, online softmax in base 2
 //   dq       rows = queries; also D = rowsum(dO o O), which dkv reads
 //   dkv      rows = keys
-// Bound by the legacy tensor pipe (512 multiply-adds a clock and SM) and the splits in front of it; these are
-// the small head sizes, where tcgen05's 128-row tiles would be mostly operand traffic.
+// Bound by issue: the splits in front of the products and the score function, on top of the legacy tensor pipe
+// (gradients at 2,000 positions: pipe 47 % busy, 2.0 instructions a clock).  They serve calls that are over before that counts.
 #include "attention_mod.cuh"
 
 namespace bt {

@@ -1,10 +1,10 @@
-// Attention with modified scores on the 5th-generation tensor cores, head_dim 64, 3xTF32.
+// Attention with modified scores on the 5th-generation tensor cores, head_dim 64, 32 and 16, 3xTF32.
 //
-// The division of the work is that of the plain causal kernels (one CTA = 128 rows of one head, one
-// row per tensor-memory lane, 64-row tiles of the other side, products spread over several issuing
-// threads, bounded mbarrier waits): see attention_tc.cu and attention_tc_bwd.cu.  What differs:
+// As in the plain causal kernels an item of work is 128 rows of one head, one row per tensor-memory lane, against 64-row
+// tiles of the other side, with bounded mbarrier waits.  Unlike there the kernels are persistent: every role walks the
+// items at its own pace, and what each does is written at each kernel.
 //
-//   Tiles      A CTA walks the tiles between the ends of its rows' ranges (SpanView): with packed documents
+//   Tiles      An item walks the tiles between the ends of its rows' ranges (SpanView): with packed documents
 //              the work is that of the documents.  A thread owns a row, so the mask is two comparisons
 //              with the row's own range, made only in tiles that the range does not cover.
 //   Scores     z = cap tanh(u) - slope |i - j| in base-2 units (attention_mod.cuh), at compile time with or
@@ -24,15 +24,17 @@ using namespace mod;
 
 namespace {
 
-constexpr int HD = 64, BR = 128, BT64 = 64;
-constexpr uint32_t kResBytes = 2u * 2u * BR * 128u;    // 128 own rows: 2 k-blocks x (hi, lo) x 128 rows x 128 B
-constexpr uint32_t kTile = 2u * 2u * BT64 * 128u;      // one streamed 64-row tile (hi, lo) in one layout
-//  MN-major 64-row tile: 2 column groups of [hi | lo][64 rows][128 B]; a k-step is 8 rows
+// HD: columns of a head as the tiles hold them, 64 or 32; a head of 16 is a tile of 32 whose other half the copies fill with zeros
+constexpr int BR = 128, BT64 = 64;
+template <int HD> constexpr uint32_t kRes = HD / 32 * 2u * BR * 128u;         // 128 own rows: k-blocks of 32 columns x (hi, lo) x 128 rows x 128 B
+template <int HD> constexpr uint32_t kTileBytes = HD / 32 * 2u * BT64 * 128u; // one streamed 64-row tile (hi, lo) in one layout
+//  MN-major 64-row tile: column groups of [hi | lo][64 rows][128 B]; a k-step is 8 rows
 __device__ __forceinline__ constexpr uint32_t mn_off(int ks, bool lo) { return (lo ? BT64 * 128u : 0u) + (uint32_t)ks * 1024u; }
 __device__ __forceinline__ DescBase mn_base(uint32_t tile) { return make_desc_base(tile, 2u * BT64 * 128u, 512u, 1u); }
 
 struct ModTcArgs {
     AttnModArgs a;
+    int d;                   // the heads' own columns
     int head_group;          // heads per group of the CTA order (grouped_block)
 };
 
@@ -42,6 +44,16 @@ __device__ __forceinline__ void alloc_tmem(uint32_t slot) {
 }
 __device__ __forceinline__ void free_tmem(uint32_t tmem) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+// Box of head_map: columns from c0 on of one head (of q, k and v heads counted through), rows from row on, both planes.
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int head, int row) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"((unsigned long long)tm), "r"(c0), "r"(head), "r"(row), "r"(0), "r"(bar) : "memory");
+}
+// Brings a box into L2: the operands that an item begins with are 200 to 300 KB, and all SMs start theirs at about the same time.
+__device__ __forceinline__ void prefetch_box(const CUtensorMap* tm, int c0, int head, int row) {
+    asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];"
+                 ::"l"((unsigned long long)tm), "r"(c0), "r"(head), "r"(row), "r"(0) : "memory");
 }
 // A role whose wait ran out lets copies in flight land before the CTA exits.
 __device__ __forceinline__ void settle() {
@@ -63,24 +75,24 @@ __device__ __forceinline__ void settle() {
 //   tensor memory  buffer i at 128 i: S -> P_hi, small half of S -> P_lo; O_tile at 384 and 448
 // Two tiles in the softmax at a time are not enough to hide its latency; short rolled passes over the columns keep
 // the code in the instruction cache (32 columns unrolled cost a third more time than 16).
-#ifndef CHV
-#define CHV 16
-#endif
-constexpr int kFwdThreads = 640, kSlots = 4, kSoft = 3, CH = CHV;
+constexpr int kFwdThreads = 640, kSlots = 4, kSoft = 3, CH = 16;
 constexpr int kRegsIssue = 56, kRegsSoft = 88, kRegsAdd = 160;
 static_assert(kRegsIssue + kSoft * kRegsSoft + kRegsAdd <= 480, "registers: 640 threads get 96 each at launch");
 constexpr uint32_t kStatBytes = 8u * 2u * BR * 4u;            // (r, sum) of the last eight tiles
-constexpr uint32_t kFwdSmem = 1024u + kResBytes + kSlots * kTile + 512u + kStatBytes;
-static_assert(kFwdSmem <= 232448u, "shared memory");
+template <int HD> constexpr uint32_t kFwdSmem = 1024u + kRes<HD> + kSlots * kTileBytes<HD> + 512u + kStatBytes;
+static_assert(kFwdSmem<64> <= 232448u, "shared memory");
 // Place of K(t) and V(t) among an item's 2n tile loads: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1).
 __device__ __forceinline__ int pos_k(int t) { return t == 0 ? 0 : 2 * t - 1; }
 __device__ __forceinline__ int pos_v(int t, int n) { return min(2 * t + 2, 2 * n - 1); }
 
-template <bool CAP, bool SLOPE>
+template <int HD, bool CAP, bool SLOPE>
 __global__ void __launch_bounds__(kFwdThreads, 1)
 attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const ModTcArgs args) {
     const AttnModArgs& g = args.a;
+    constexpr uint32_t kResBytes = kRes<HD>, kTile = kTileBytes<HD>;
+    constexpr int KB = HD / 32, KS = HD / 8;             // k-blocks, and k-steps of a product over the head's columns
+    const int d = HD == 64 ? HD : args.d;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t q_s = base, ring_s = q_s + kResBytes, bars = ring_s + kSlots * kTile;
@@ -133,10 +145,10 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     if (next_item(answer, x, y)) follows = make_item(g, args.head_group, x, y, false, BR, BT64);
                     if (follows.n > 0) {
                         const int h = follows.bh % g.H, row0 = (follows.bh / g.H) * g.T;
-                        for (int kb = 0; kb < 2; ++kb) {
-                            prefetch_box(&tmQ, h * HD + kb * 32, row0 + follows.blk * BR);
-                            prefetch_box(&tmK, g.C + h * HD + kb * 32, row0 + follows.t0 * BT64);
-                            prefetch_box(&tmV, 2 * g.C + h * HD + kb * 32, row0 + follows.t0 * BT64);
+                        for (int kb = 0; kb < KB; ++kb) {
+                            prefetch_box(&tmQ, kb * 32, h, row0 + follows.blk * BR);
+                            prefetch_box(&tmK, kb * 32, g.H + h, row0 + follows.t0 * BT64);
+                            prefetch_box(&tmV, kb * 32, 2 * g.H + h, row0 + follows.t0 * BT64);
                         }
                     }
                     return put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i + 1, follows, g.err);
@@ -153,15 +165,15 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     ok = mbar_wait(bar(SLOT_EMPTY + slot), ((c / kSlots) & 1u) ^ 1u, g.err, 111);
                     if (!ok) break;
                     mbar_expect_tx(bar(SLOT_FULL + slot), kTile);
-                    for (int kb = 0; kb < 2; ++kb)
-                        tma_load_3d(ring_s + slot * kTile + kb * (kTile / 2), is_k ? &tmK : &tmV, bar(SLOT_FULL + slot),
-                                    (is_k ? g.C : 2 * g.C) + h * HD + kb * 32, row0 + (it.t0 + t) * BT64, 0);
+                    for (int kb = 0; kb < KB; ++kb)
+                        load_box(ring_s + slot * kTile + kb * (kTile / KB), is_k ? &tmK : &tmV, bar(SLOT_FULL + slot),
+                                    kb * 32, (is_k ? g.H : 2 * g.H) + h, row0 + (it.t0 + t) * BT64);
                     if (p == 0) {                       // behind the first K: the previous item's last S has to be done with Q
                         ok = mbar_wait(bar(Q_EMPTY), (qi & 1u) ^ 1u, g.err, 112);
                         if (!ok) break;
                         mbar_expect_tx(bar(Q_FULL), kResBytes);
-                        for (int kb = 0; kb < 2; ++kb)
-                            tma_load_3d(q_s + kb * (kResBytes / 2), &tmQ, bar(Q_FULL), h * HD + kb * 32, row0 + it.blk * BR, 0);
+                        for (int kb = 0; kb < KB; ++kb)
+                            load_box(q_s + kb * (kResBytes / KB), &tmQ, bar(Q_FULL), kb * 32, h, row0 + it.blk * BR);
                     }
                 }
                 if (it.n > 0) ++qi;
@@ -185,18 +197,18 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     if (gt >= kSoft && !mbar_wait_warp(bar(P_DONE + buf), (gt / kSoft - 1u) & 1u, g.err, 115)) { ok = false; break; }
                     if (!mbar_wait_warp(bar(SLOT_FULL + slot), (ck / kSlots) & 1u, g.err, 114)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t d = tmem + buf * 128u;
+                    const uint32_t tS = tmem + buf * 128u;
                     const DescBase kd = kmaj_base(ring_s + slot * kTile);
                     if (elect_one()) {
 #pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) {
-                        const uint64_t k_hl = kd.at(kmaj_off(BT64, ks, false));
-                        umma_tf32(d, qd.at(kmaj_off(BR, ks, false)), k_hl, idesc2, ks > 0 ? 1u : 0u);   // Q_hi K_hi | Q_hi K_lo
-                        umma_tf32(d + 64u, qd.at(kmaj_off(BR, ks, true)), k_hl, idesc, 1u);             // + Q_lo K_hi
-                    }
-                    umma_commit(bar(SLOT_EMPTY + slot));
-                    umma_commit(bar(S_FULL + buf));
-                    if (t == it.n - 1) umma_commit(bar(Q_EMPTY));
+                        for (int ks = 0; ks < KS; ++ks) {
+                            const uint64_t k_hl = kd.at(kmaj_off(BT64, ks, false));
+                            umma_tf32(tS, qd.at(kmaj_off(BR, ks, false)), k_hl, idesc2, ks > 0 ? 1u : 0u);   // Q_hi K_hi | Q_hi K_lo
+                            umma_tf32(tS + 64u, qd.at(kmaj_off(BR, ks, true)), k_hl, idesc, 1u);             // + Q_lo K_hi
+                        }
+                        umma_commit(bar(SLOT_EMPTY + slot));
+                        umma_commit(bar(S_FULL + buf));
+                        if (t == it.n - 1) umma_commit(bar(Q_EMPTY));
                     }
                     __syncwarp();
                 }
@@ -224,16 +236,16 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     const DescBase vd = mn_base(ring_s + slot * kTile);
                     if (elect_one()) {
 #pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) {
-                        umma_tf32_ts(tO, p_lo + ks * 8u, vd.at(mn_off(ks, false)), idesc, ks > 0 ? 1u : 0u);
-                        umma_tf32_ts(tO, p_hi + ks * 8u, vd.at(mn_off(ks, true)), idesc, 1u);
-                    }
+                        for (int ks = 0; ks < 8; ++ks) {
+                            umma_tf32_ts(tO, p_lo + ks * 8u, vd.at(mn_off(ks, false)), idesc, ks > 0 ? 1u : 0u);
+                            umma_tf32_ts(tO, p_hi + ks * 8u, vd.at(mn_off(ks, true)), idesc, 1u);
+                        }
 #pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(tO, p_hi + ks * 8u, vd.at(mn_off(ks, false)), idesc, 1u);
-                    umma_commit(bar(SLOT_EMPTY + slot));
-                    umma_commit(bar(P_DONE + buf));
-                    mbar_arrive(bar(O_FULL + ob));      // hands on what P_FULL published: the tile's (r, sum)
-                    umma_commit(bar(O_FULL + ob));
+                        for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(tO, p_hi + ks * 8u, vd.at(mn_off(ks, false)), idesc, 1u);
+                        umma_commit(bar(SLOT_EMPTY + slot));
+                        umma_commit(bar(P_DONE + buf));
+                        mbar_arrive(bar(O_FULL + ob));      // hands on what P_FULL published: the tile's (r, sum)
+                        umma_commit(bar(O_FULL + ob));
                     }
                     __syncwarp();
                 }
@@ -250,7 +262,7 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         bool ok = true;
         for (int i = 0; ok && (ok = next(i, it, true)) && it.n >= 0; ++i) {
             const int b = it.bh / g.H, h = it.bh % g.H, row = it.blk * BR + rloc;
-            const Score sc = make_score<CAP, SLOPE>(1.0f / sqrtf((float)HD), g.cap, g.slopes, h);
+            const Score sc = make_score<CAP, SLOPE>(1.0f / sqrtf((float)d), g.cap, g.slopes, h);
             const int2 span = row_range(g.spans.k, b, g.T, row, false);
             for (int t = (wg + kSoft - (int)(gt % kSoft)) % kSoft; t < it.n; t += kSoft, ++use) {
                 if (!mbar_wait_warp(bar(S_FULL + wg), use & 1u, g.err, 121)) { ok = false; break; }
@@ -328,9 +340,9 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 const uint32_t ob = gt & 1u;
                 if (!mbar_wait_warp(bar(O_FULL + ob), (gt >> 1) & 1u, g.err, 122)) { ok = false; break; }
                 tc_fence_after();
-                uint32_t r0[32], r1[32];
-                tmem_ld32(t_o + 64u * ob, r0);
-                tmem_ld32(t_o + 64u * ob + 32u, r1);
+                uint32_t r[KB][32];
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) tmem_ld32(t_o + 64u * ob + 32u * kb, r[kb]);
                 const float* stat = tile_stat + (gt & 7u) * (2 * BR) + rloc;
                 const float ref = stat[0], sum = stat[BR];
                 tmem_ld_wait();
@@ -342,17 +354,15 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 l = l * keep + sum * join;
                 m = top;
 #pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    acc[k] = fmaf(acc[k], keep, __uint_as_float(r0[k]) * join);
-                    acc[32 + k] = fmaf(acc[32 + k], keep, __uint_as_float(r1[k]) * join);
-                }
+                for (int k = 0; k < HD; ++k) acc[k] = fmaf(acc[k], keep, __uint_as_float(r[k >> 5][k & 31]) * join);
             }
             const int b = it.bh / g.H, h = it.bh % g.H, row = it.blk * BR + rloc;
             if (ok && row < g.T) {
                 const float inv = l > 0.f ? 1.0f / l : 0.f;             // a row that reads nothing is zero
-                const int64_t at = ((int64_t)b * g.T + row) * g.C + (int64_t)h * HD;
+                const int64_t at = ((int64_t)b * g.T + row) * g.C + (int64_t)h * d;
 #pragma unroll
                 for (int q = 0; q < HD; q += 8) {
+                    if (q >= d) break;
                     float v[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = acc[q + e] * inv;
@@ -382,15 +392,18 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 //               dP^T -> dS^T_hi 384-447, small half -> dS^T_lo 448-511
 constexpr int kDkvThreads = 640, kRegsIssueDkv = 64, kRegsElemDkv = 104;
 static_assert(kRegsIssueDkv + 4 * kRegsElemDkv <= 480, "registers: 640 threads get 96 each at launch");
-constexpr uint32_t kDkvSmem = 1024u + kResBytes + 4u * kTile + 512u + 1024u;
-static_assert(kDkvSmem <= 232448u, "shared memory");
+template <int HD> constexpr uint32_t kDkvSmem = 1024u + kRes<HD> + 4u * kTileBytes<HD> + 512u + 1024u;
+static_assert(kDkvSmem<64> <= 232448u, "shared memory");
 
-template <bool CAP, bool SLOPE>
+template <int HD, bool CAP, bool SLOPE>
 __global__ void __launch_bounds__(kDkvThreads, 1)
 attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_constant__ CUtensorMap tmQm,
                     const __grid_constant__ CUtensorMap tmDOk, const __grid_constant__ CUtensorMap tmDOm,
                     const __grid_constant__ CUtensorMap tmVres, const ModTcArgs args) {
     const AttnModArgs& g = args.a;
+    constexpr uint32_t kResBytes = kRes<HD>, kTile = kTileBytes<HD>;
+    constexpr int KB = HD / 32, KS = HD / 8;             // k-blocks, and k-steps of a product over the head's columns
+    const int d = HD == 64 ? HD : args.d;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t v_s = base, qk_s = base + kResBytes, dok_s = qk_s + kTile, dom_s = dok_s + kTile, qm_s = dom_s + kTile;
@@ -437,12 +450,12 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
                     if (next_item(answer, x, y)) follows = make_item(g, args.head_group, x, y, true, BR, BT64);
                     if (follows.n > 0) {
                         const int h = follows.bh % g.H, row0 = (follows.bh / g.H) * g.T, k0 = row0 + follows.blk * BR;
-                        for (int kb = 0; kb < 2; ++kb) {
-                            prefetch_box(&tmQk, g.C + h * HD + kb * 32, k0);             // K, 64 rows at a time
-                            prefetch_box(&tmQk, g.C + h * HD + kb * 32, k0 + BT64);
-                            prefetch_box(&tmVres, 2 * g.C + h * HD + kb * 32, k0);
-                            prefetch_box(&tmQk, h * HD + kb * 32, row0 + follows.t0 * BT64);
-                            prefetch_box(&tmDOk, h * HD + kb * 32, row0 + follows.t0 * BT64);
+                        for (int kb = 0; kb < KB; ++kb) {
+                            prefetch_box(&tmQk, kb * 32, g.H + h, k0);             // K, 64 rows at a time
+                            prefetch_box(&tmQk, kb * 32, g.H + h, k0 + BT64);
+                            prefetch_box(&tmVres, kb * 32, 2 * g.H + h, k0);
+                            prefetch_box(&tmQk, kb * 32, h, row0 + follows.t0 * BT64);
+                            prefetch_box(&tmDOk, kb * 32, h, row0 + follows.t0 * BT64);
                         }
                     }
                     return put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i + 1, follows, g.err);
@@ -464,15 +477,15 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
                         ok = mbar_wait(bar(full + 1), ((gt + (uint32_t)t) & 1u) ^ 1u, g.err, 131);   // every EMPTY barrier follows its FULL barrier
                         if (!ok) break;
                         mbar_expect_tx(bar(full), kTile);
-                        for (int part = 0; part < 2; ++part)
-                            tma_load_3d(dst + part * (kTile / 2), tm, bar(full), h * HD + part * 32, row0 + (it.t0 + t) * BT64, 0);
+                        for (int kb = 0; kb < KB; ++kb)
+                            load_box(dst + kb * (kTile / KB), tm, bar(full), kb * 32, h, row0 + (it.t0 + t) * BT64);
                     }
                     if (p == 0) {                       // V, once the previous item's last dP^T is done with it
                         ok = mbar_wait(bar(V_EMPTY), (vi & 1u) ^ 1u, g.err, 132);
                         if (!ok) break;
                         mbar_expect_tx(bar(V_FULL), kResBytes);
-                        for (int kb = 0; kb < 2; ++kb)
-                            tma_load_3d(v_s + kb * (kResBytes / 2), &tmVres, bar(V_FULL), 2 * g.C + h * HD + kb * 32, row0 + it.blk * BR, 0);
+                        for (int kb = 0; kb < KB; ++kb)
+                            load_box(v_s + kb * (kResBytes / KB), &tmVres, bar(V_FULL), kb * 32, 2 * g.H + h, row0 + it.blk * BR);
                     }
                 }
                 gt += (uint32_t)it.n;
@@ -504,14 +517,14 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
                         tc_fence_after();
                         if (elect_one()) {
 #pragma unroll
-                        for (int ks = 0; ks < 8; ++ks) {
-                            umma_tf32_ts(t_acc, t_xlo + ks * 8, bd.at(mn_off(ks, false)), idesc_b, ks > 0 ? 1u : 0u);
-                            umma_tf32_ts(t_acc, t_x + ks * 8, bd.at(mn_off(ks, true)), idesc_b, 1u);
-                        }
+                            for (int ks = 0; ks < 8; ++ks) {
+                                umma_tf32_ts(t_acc, t_xlo + ks * 8, bd.at(mn_off(ks, false)), idesc_b, ks > 0 ? 1u : 0u);
+                                umma_tf32_ts(t_acc, t_x + ks * 8, bd.at(mn_off(ks, true)), idesc_b, 1u);
+                            }
 #pragma unroll
-                        for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(t_acc, t_x + ks * 8, bd.at(mn_off(ks, false)), idesc_b, 1u);
-                        umma_commit(bar(acc_b + 1));
-                        if (t == it.n) umma_commit(bar(score_chain ? ACC_V : ACC_K));
+                            for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(t_acc, t_x + ks * 8, bd.at(mn_off(ks, false)), idesc_b, 1u);
+                            umma_commit(bar(acc_b + 1));
+                            if (t == it.n) umma_commit(bar(score_chain ? ACC_V : ACC_K));
                         }
                         __syncwarp();
                     }
@@ -522,24 +535,24 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
                         if (!mbar_wait_warp(bar(x_full), (gt + (uint32_t)t) & 1u, g.err, 135)) { ok = false; break; }
                         tc_fence_after();
                         if (elect_one()) {
-                        if (score_chain) {
+                            if (score_chain) {
 #pragma unroll
-                            for (int ks = 0; ks < 8; ++ks) {
-                                const uint64_t b_hl = qd.at(kmaj_off(BT64, ks, false));
-                                umma_tf32_ts(t_x, tK_hi + ks * 8, b_hl, idesc_a2, ks > 0 ? 1u : 0u);      // K'_hi Q_hi | K'_hi Q_lo
-                                umma_tf32_ts(t_xlo, tK_lo + ks * 8, b_hl, idesc_a, 1u);                   // + K'_lo Q_hi
-                            }
-                        } else {
+                                for (int ks = 0; ks < KS; ++ks) {
+                                    const uint64_t b_hl = qd.at(kmaj_off(BT64, ks, false));
+                                    umma_tf32_ts(t_x, tK_hi + ks * 8, b_hl, idesc_a2, ks > 0 ? 1u : 0u);      // K'_hi Q_hi | K'_hi Q_lo
+                                    umma_tf32_ts(t_xlo, tK_lo + ks * 8, b_hl, idesc_a, 1u);                   // + K'_lo Q_hi
+                                }
+                            } else {
 #pragma unroll
-                            for (int ks = 0; ks < 8; ++ks) {
-                                const uint64_t b_hl = qd.at(kmaj_off(BT64, ks, false));
-                                umma_tf32(t_x, vd.at(kmaj_off(BR, ks, false)), b_hl, idesc_a2, ks > 0 ? 1u : 0u);   // V_hi dO_hi | V_hi dO_lo
-                                umma_tf32(t_xlo, vd.at(kmaj_off(BR, ks, true)), b_hl, idesc_a, 1u);                 // + V_lo dO_hi
+                                for (int ks = 0; ks < KS; ++ks) {
+                                    const uint64_t b_hl = qd.at(kmaj_off(BT64, ks, false));
+                                    umma_tf32(t_x, vd.at(kmaj_off(BR, ks, false)), b_hl, idesc_a2, ks > 0 ? 1u : 0u);   // V_hi dO_hi | V_hi dO_lo
+                                    umma_tf32(t_xlo, vd.at(kmaj_off(BR, ks, true)), b_hl, idesc_a, 1u);                 // + V_lo dO_hi
+                                }
                             }
-                        }
-                        umma_commit(bar(x_full + 1));
-                        umma_commit(bar(x_done));
-                        if (!score_chain && t == it.n - 1) umma_commit(bar(V_EMPTY));
+                            umma_commit(bar(x_full + 1));
+                            umma_commit(bar(x_done));
+                            if (!score_chain && t == it.n - 1) umma_commit(bar(V_EMPTY));
                         }
                         __syncwarp();
                     }
@@ -552,8 +565,9 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
         set_regs_up<kRegsElemDkv>();
         const int wg = (warp - 4) >> 2, lane_group = warp & 3, rloc = lane_group * 32 + lane;
         const uint32_t t_lane = ((uint32_t)(lane_group * 32) << 16), c0 = 16u * (uint32_t)wg;
-        const float scale = 1.0f / sqrtf((float)HD);
+        const float scale = 1.0f / sqrtf((float)d);
         const int64_t gs = 3 * (int64_t)g.C;
+        const bool tile_cols = HD == 64 || c0 < (uint32_t)HD, own_cols = HD == 64 || c0 < (uint32_t)d;   // narrow heads: the first warpgroups hold all columns
         // Statistics of a tile's 64 queries (lse in base-2 units, D) through shared memory, one tile ahead, from the
         // first warpgroup's threads.  All sixteen warps arrive: no warp can be two phases behind.
         float* stat = reinterpret_cast<float*>(smem_ptr(bars + 512u));
@@ -575,19 +589,22 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
         auto begin_item = [&](const Item& it, const Score& sc, uint32_t ga) {
             const float st0 = fetch_stat(it, 0);
             const int row = min(it.blk * BR + rloc, g.T - 1);
-            const int64_t off = ((int64_t)(it.bh / g.H) * g.T + row) * gs + g.C + (int64_t)(it.bh % g.H) * HD + c0;
-            float a[2][8], e[2][8];
+            const int64_t off = ((int64_t)(it.bh / g.H) * g.T + row) * gs + g.C + (int64_t)(it.bh % g.H) * d + c0;
+            float a[2][8] = {}, e[2][8] = {};
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
+                if (!own_cols) break;
                 load_sector(g.qkv + off + 8 * q, a[q]);
                 load_sector(g.qkv_lo + off + 8 * q, e[q]);
             }
-            uint32_t hi[16], lo[16];
+            if (tile_cols) {
+                uint32_t hi[16], lo[16];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) split_tf32_int((a[k >> 3][k & 7] + e[k >> 3][k & 7]) * sc.unit, hi[k], lo[k]);
-            tmem_stn(tK_hi + t_lane + c0, hi);       // the last S^T of the item before has been read
-            tmem_stn(tK_lo + t_lane + c0, lo);
-            tmem_st_wait();
+                for (int k = 0; k < 16; ++k) split_tf32_int((a[k >> 3][k & 7] + e[k >> 3][k & 7]) * sc.unit, hi[k], lo[k]);
+                tmem_stn(tK_hi + t_lane + c0, hi);   // the last S^T of the item before has been read
+                tmem_stn(tK_lo + t_lane + c0, lo);
+                tmem_st_wait();
+            }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(K_READY));
@@ -641,7 +658,7 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
                 for (int k = 0; k < 16; ++k) split_tf32_int(p[k], s[k], lo[k]);
                 tmem_stn(tS + t_lane + c0, s);           // P^T over S^T
                 tmem_stn(tPlo + t_lane + c0, lo);
-                tmem_ldn(tdV + t_lane + c0, s);          // dV(t - 1): complete, as S^T(t) is (not used at t = 0)
+                if (tile_cols) tmem_ldn(tdV + t_lane + c0, s);   // dV(t - 1): complete, as S^T(t) is (not used at t = 0)
                 tmem_ld_wait();
                 tmem_st_wait();
                 tc_fence_before();
@@ -651,7 +668,7 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
 #pragma unroll
                     for (int k = 0; k < 16; ++k) p[k] *= f[k];
                 }
-                if (t > 0) {
+                if (tile_cols && t > 0) {
 #pragma unroll
                     for (int k = 0; k < 16; ++k) acc_v[k] += __uint_as_float(s[k]);
                 }
@@ -672,13 +689,13 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
                 }
                 tmem_stn(tdP + t_lane + c0, s);          // dS^T over dP^T
                 tmem_stn(tdSlo + t_lane + c0, lo);
-                tmem_ldn(tdK + t_lane + c0, s);          // dK(t - 1): complete, as dP^T(t) is
+                if (tile_cols) tmem_ldn(tdK + t_lane + c0, s);   // dK(t - 1): complete, as dP^T(t) is
                 tmem_ld_wait();
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(DS_READY));
-                if (t > 0) {
+                if (tile_cols && t > 0) {
 #pragma unroll
                     for (int k = 0; k < 16; ++k) acc_k[k] += __uint_as_float(s[k]);
                 }
@@ -695,19 +712,21 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
                 if (!mbar_wait_warp(bar(ACC_V), ni & 1u, g.err, 144) || !mbar_wait_warp(bar(ACC_K), ni & 1u, g.err, 145)) { ok = false; break; }
                 ++ni;
                 tc_fence_after();
-                uint32_t r[16], r2[16];
-                tmem_ldn(tdV + t_lane + c0, r);
-                tmem_ldn(tdK + t_lane + c0, r2);
-                tmem_ld_wait();
-                tc_fence_before();
+                if (tile_cols) {
+                    uint32_t r[16], r2[16];
+                    tmem_ldn(tdV + t_lane + c0, r);
+                    tmem_ldn(tdK + t_lane + c0, r2);
+                    tmem_ld_wait();
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    acc_v[k] += __uint_as_float(r[k]);
-                    acc_k[k] = (acc_k[k] + __uint_as_float(r2[k])) * scale;
+                    for (int k = 0; k < 16; ++k) {
+                        acc_v[k] += __uint_as_float(r[k]);
+                        acc_k[k] = (acc_k[k] + __uint_as_float(r2[k])) * scale;
+                    }
                 }
+                tc_fence_before();
             }
-            if (key < g.T) {
-                const int64_t at = ((int64_t)b * g.T + key) * gs + g.C + (int64_t)h * HD + c0;
+            if (key < g.T && own_cols) {
+                const int64_t at = ((int64_t)b * g.T + key) * gs + g.C + (int64_t)h * d + c0;
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
                     float v[8];
@@ -739,19 +758,22 @@ attn_mod_dkv_kernel(const __grid_constant__ CUtensorMap tmQk, const __grid_const
 //               last tile of the item before
 //   warps 20-23 add every dQ tile to registers (64 columns of a row per thread) and write the result
 //   tensor memory  Q' hi|lo 0-127, dQ tile 128-255, buffer b at 256 + 128b: S -> dS_hi, dP -> dS_lo
-// The dQ tile is 128 wide: the column groups [K_hi g0 | K_lo g0 | K_hi g1 | K_lo g1] (g = 32 head columns) as
+// The dQ tile is 128 wide (heads of 32 and fewer: the first half of this): the column groups [K_hi g0 | K_lo g0 | K_hi g1 | K_lo g1] (g = 32 head columns) as
 // one operand of dS_hi, and dS_lo K_hi 32 columns further, on the second and third group; head columns
 // 0-31 are the sum of groups 0 and 1, 32-63 that of 2 and 3.
 constexpr int kDqThreads = 768, kRegsIssueDq = 56, kRegsElemDq = 72, kRegsAddDq = 128;
 static_assert(kRegsIssueDq + 4 * kRegsElemDq + kRegsAddDq <= 480, "registers: 768 threads get 80 each at launch");
-constexpr uint32_t kDqSmem = 1024u + kResBytes + 5u * kTile + 512u + 1024u;
-static_assert(kDqSmem <= 232448u, "shared memory");
+template <int HD> constexpr uint32_t kDqSmem = 1024u + kRes<HD> + 5u * kTileBytes<HD> + 512u + 1024u;
+static_assert(kDqSmem<64> <= 232448u, "shared memory");
 
-template <bool CAP, bool SLOPE>
+template <int HD, bool CAP, bool SLOPE>
 __global__ void __launch_bounds__(kDqThreads, 1)
 attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_constant__ CUtensorMap tmKm,
                    const __grid_constant__ CUtensorMap tmVk, const __grid_constant__ CUtensorMap tmDOres, const ModTcArgs args) {
     const AttnModArgs& g = args.a;
+    constexpr uint32_t kResBytes = kRes<HD>, kTile = kTileBytes<HD>;
+    constexpr int KB = HD / 32, KS = HD / 8;             // k-blocks, and k-steps of a product over the head's columns
+    const int d = HD == 64 ? HD : args.d;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t do_s = base, kv_s = base + kResBytes, km_s = kv_s + 4u * kTile, bars = km_s + kTile;   // kv_s: stage st: K at 2 st, V at 2 st + 1
@@ -800,12 +822,12 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
                         if (next_item(answer, x, y)) follows = make_item(g, args.head_group, x, y, false, BR, BT64);
                         if (follows.n > 0) {
                             const int h = follows.bh % g.H, row0 = (follows.bh / g.H) * g.T, q0 = row0 + follows.blk * BR;
-                            for (int kb = 0; kb < 2; ++kb) {
-                                prefetch_box(&tmDOres, h * HD + kb * 32, q0);
-                                prefetch_box(&tmKk, h * HD + kb * 32, q0);               // Q, 64 rows at a time
-                                prefetch_box(&tmKk, h * HD + kb * 32, q0 + BT64);
-                                prefetch_box(&tmKk, g.C + h * HD + kb * 32, row0 + follows.t0 * BT64);
-                                prefetch_box(&tmVk, 2 * g.C + h * HD + kb * 32, row0 + follows.t0 * BT64);
+                            for (int kb = 0; kb < KB; ++kb) {
+                                prefetch_box(&tmDOres, kb * 32, h, q0);
+                                prefetch_box(&tmKk, kb * 32, h, q0);               // Q, 64 rows at a time
+                                prefetch_box(&tmKk, kb * 32, h, q0 + BT64);
+                                prefetch_box(&tmKk, kb * 32, g.H + h, row0 + follows.t0 * BT64);
+                                prefetch_box(&tmVk, kb * 32, 2 * g.H + h, row0 + follows.t0 * BT64);
                             }
                         }
                         return put_item(info, bar(INFO_FULL), bar(INFO_EMPTY), i + 1, follows, g.err);
@@ -822,23 +844,23 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
                             ok = mbar_wait(bar(KEMPTY + st), ((ga >> 1) & 1u) ^ 1u, g.err, 151);
                             if (!ok) break;
                             mbar_expect_tx(bar(KFULL + st), 2u * kTile);
-                            for (int kb = 0; kb < 2; ++kb) {
-                                tma_load_3d(kv_s + 2u * st * kTile + kb * (kTile / 2), &tmKk, bar(KFULL + st), g.C + h * HD + kb * 32, row0 + (it.t0 + t + 1) * BT64, 0);
-                                tma_load_3d(kv_s + (2u * st + 1u) * kTile + kb * (kTile / 2), &tmVk, bar(KFULL + st), 2 * g.C + h * HD + kb * 32, row0 + (it.t0 + t + 1) * BT64, 0);
+                            for (int kb = 0; kb < KB; ++kb) {
+                                load_box(kv_s + 2u * st * kTile + kb * (kTile / KB), &tmKk, bar(KFULL + st), kb * 32, g.H + h, row0 + (it.t0 + t + 1) * BT64);
+                                load_box(kv_s + (2u * st + 1u) * kTile + kb * (kTile / KB), &tmVk, bar(KFULL + st), kb * 32, 2 * g.H + h, row0 + (it.t0 + t + 1) * BT64);
                             }
                         }
                         if (t < 0) {                    // dO, once the previous item's last dP is done with it
                             ok = mbar_wait(bar(DO_EMPTY), (di & 1u) ^ 1u, g.err, 152);
                             if (!ok) break;
                             mbar_expect_tx(bar(DO_FULL), kResBytes);
-                            for (int kb = 0; kb < 2; ++kb)
-                                tma_load_3d(do_s + kb * (kResBytes / 2), &tmDOres, bar(DO_FULL), h * HD + kb * 32, row0 + it.blk * BR, 0);
+                            for (int kb = 0; kb < KB; ++kb)
+                                load_box(do_s + kb * (kResBytes / KB), &tmDOres, bar(DO_FULL), kb * 32, h, row0 + it.blk * BR);
                         } else {
                             ok = mbar_wait(bar(MEMPTY), ((gt + (uint32_t)t) & 1u) ^ 1u, g.err, 153);
                             if (!ok) break;
                             mbar_expect_tx(bar(MFULL), kTile);
-                            for (int grp = 0; grp < 2; ++grp)
-                                tma_load_3d(km_s + grp * (kTile / 2), &tmKm, bar(MFULL), g.C + h * HD + grp * 32, row0 + (it.t0 + t) * BT64, 0);
+                            for (int kb = 0; kb < KB; ++kb)
+                                load_box(km_s + kb * (kTile / KB), &tmKm, bar(MFULL), kb * 32, g.H + h, row0 + (it.t0 + t) * BT64);
                         }
                     }
                     gt += (uint32_t)it.n;
@@ -868,22 +890,22 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
                             const uint32_t dst = tbuf(st);
                             const DescBase kd = kmaj_base(kv_s + 2u * st * kTile);
 #pragma unroll
-                            for (int ks = 0; ks < 8; ++ks) {
+                            for (int ks = 0; ks < KS; ++ks) {
                                 umma_tf32_ts(dst, tQ_lo + ks * 8, kd.at(kmaj_off(BT64, ks, false)), idesc, ks > 0 ? 1u : 0u);
                                 umma_tf32_ts(dst, tQ_hi + ks * 8, kd.at(kmaj_off(BT64, ks, true)), idesc, 1u);
                             }
 #pragma unroll
-                            for (int ks = 0; ks < 8; ++ks) umma_tf32_ts(dst, tQ_hi + ks * 8, kd.at(kmaj_off(BT64, ks, false)), idesc, 1u);
+                            for (int ks = 0; ks < KS; ++ks) umma_tf32_ts(dst, tQ_hi + ks * 8, kd.at(kmaj_off(BT64, ks, false)), idesc, 1u);
                         } else {
                             const uint32_t dst = tbuf(st) + 64u;
                             const DescBase vd = kmaj_base(kv_s + (2u * st + 1u) * kTile);
 #pragma unroll
-                            for (int ks = 0; ks < 8; ++ks) {
+                            for (int ks = 0; ks < KS; ++ks) {
                                 umma_tf32(dst, dod.at(kmaj_off(BR, ks, true)), vd.at(kmaj_off(BT64, ks, false)), idesc, ks > 0 ? 1u : 0u);
                                 umma_tf32(dst, dod.at(kmaj_off(BR, ks, false)), vd.at(kmaj_off(BT64, ks, true)), idesc, 1u);
                             }
 #pragma unroll
-                            for (int ks = 0; ks < 8; ++ks)
+                            for (int ks = 0; ks < KS; ++ks)
                                 umma_tf32(dst, dod.at(kmaj_off(BR, ks, false)), vd.at(kmaj_off(BT64, ks, false)), idesc, 1u);
                         }
                         umma_commit(bar(KEMPTY + st));
@@ -935,24 +957,27 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
         bool ok = true;
         for (int i = 0; ok && (ok = next(i, it, true)) && it.n >= 0; ++i) {
             const int b = it.bh / g.H, h = it.bh % g.H, row = it.blk * BR + rloc, rc = min(row, g.T - 1);
-            const Score sc = make_score<CAP, SLOPE>(1.0f / sqrtf((float)HD), g.cap, g.slopes, h);
+            const Score sc = make_score<CAP, SLOPE>(1.0f / sqrtf((float)d), g.cap, g.slopes, h);
             const int64_t lb = (int64_t)it.bh * g.T;
             if (it.n == 0) {                            // rows that read nothing: D only has to be finite
                 if (pair == 0 && part == 0 && row < g.T) g.dvec[lb + row] = 0.f;
                 continue;
             }
             if (pair == (gt & 1u)) {
-                // this pair has the item's first tile: D over 32 columns here (dO lies in shared memory), and Q' = Q * unit
+                // this pair has the item's first tile: D over half the columns here (dO lies in shared memory), and Q' = Q * unit
                 // into tensor memory; all loads of a half are on their way together
-                const int64_t at = ((int64_t)b * g.T + rc) * g.C + (int64_t)h * HD + c0;
-                const int64_t qat = ((int64_t)b * g.T + rc) * 3 * (int64_t)g.C + (int64_t)h * HD + c0;
-                const uint8_t* do_row = smem_ptr(do_s + part * (kResBytes / 2)) + rloc * 128;
-                float d = 0.f;
+                constexpr int kCols = HD / 2;
+                const int h0 = (int)part * kCols;
+                const int64_t at = ((int64_t)b * g.T + rc) * g.C + (int64_t)h * d + h0;
+                const int64_t qat = ((int64_t)b * g.T + rc) * 3 * (int64_t)g.C + (int64_t)h * d + h0;
+                const uint8_t* do_row = smem_ptr(do_s + (uint32_t)(h0 >> 5) * (kResBytes / KB)) + rloc * 128;
+                float dot = 0.f;
 #pragma unroll 1
-                for (int q = 0; q < 32; q += 16) {
-                    float o[2][8], x[2][8], y[2][8];
+                for (int q = 0; q < kCols; q += 16) {
+                    float o[2][8] = {}, x[2][8] = {}, y[2][8] = {};
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
+                        if (HD < 64 && h0 >= d) break;  // a head of 16: the second part's columns are zeros
                         load_sector(g.o + at + q + 8 * k, o[k]);
                         load_sector(g.qkv + qat + q + 8 * k, x[k]);
                         load_sector(g.qkv_lo + qat + q + 8 * k, y[k]);
@@ -966,20 +991,20 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
                     }
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {       // 16-byte pieces of the row, swizzled by its number
-                        const uint32_t piece = (((uint32_t)q >> 2) + (uint32_t)k) ^ ((uint32_t)rloc & 7u);
+                        const uint32_t piece = ((((uint32_t)(h0 + q) & 31u) >> 2) + (uint32_t)k) ^ ((uint32_t)rloc & 7u);
                         const float4 v = add4(*reinterpret_cast<const float4*>(do_row + piece * 16u),
                                               *reinterpret_cast<const float4*>(do_row + BR * 128u + piece * 16u));
                         const float* ok4 = &o[k >> 1][4 * (k & 1)];
-                        d = fmaf(v.x, ok4[0], fmaf(v.y, ok4[1], fmaf(v.z, ok4[2], fmaf(v.w, ok4[3], d))));
+                        dot = fmaf(v.x, ok4[0], fmaf(v.y, ok4[1], fmaf(v.z, ok4[2], fmaf(v.w, ok4[3], dot))));
                     }
                     uint32_t hi[16], lo[16];
 #pragma unroll
                     for (int k = 0; k < 16; ++k) split_tf32_int((x[k >> 3][k & 7] + y[k >> 3][k & 7]) * sc.unit, hi[k], lo[k]);
-                    tmem_stn(tQ_hi + t_lane + c0 + q, hi);
-                    tmem_stn(tQ_lo + t_lane + c0 + q, lo);
+                    tmem_stn(tQ_hi + t_lane + (uint32_t)(h0 + q), hi);
+                    tmem_stn(tQ_lo + t_lane + (uint32_t)(h0 + q), lo);
                 }
                 if (!ok) break;
-                dsm[part * 128u + (uint32_t)rloc] = d;
+                dsm[part * 128u + (uint32_t)rloc] = dot;
                 __threadfence_block();
                 tmem_st_wait();
                 tc_fence_before();
@@ -1041,20 +1066,20 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
         set_regs_up<kRegsAddDq>();
         const int lane_group = warp & 3, rloc = lane_group * 32 + lane;
         const uint32_t t_row = tdQ + ((uint32_t)(lane_group * 32) << 16);
-        const float scale = 1.0f / sqrtf((float)HD);
+        const float scale = 1.0f / sqrtf((float)d);
         const int64_t gs = 3 * (int64_t)g.C;
         uint32_t gt = 0;
         Item it;
         bool ok = true;
         for (int i = 0; ok && (ok = next(i, it, true)) && it.n >= 0; ++i) {
-            float acc[64];
+            float acc[HD];
 #pragma unroll
-            for (int k = 0; k < 64; ++k) acc[k] = 0.f;
+            for (int k = 0; k < HD; ++k) acc[k] = 0.f;
             for (int t = 0; t < it.n; ++t, ++gt) {
                 if (!mbar_wait_warp(bar(DQ_FULL), gt & 1u, g.err, 161)) { ok = false; break; }
                 tc_fence_after();
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < HD / 16; ++q) {
                     uint32_t r[16], r2[16];
                     tmem_ldn(t_row + (uint32_t)(64 * (q >> 1) + 16 * (q & 1)), r);
                     tmem_ldn(t_row + (uint32_t)(64 * (q >> 1) + 16 * (q & 1) + 32), r2);
@@ -1068,9 +1093,10 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
             }
             const int b = it.bh / g.H, h = it.bh % g.H, row = it.blk * BR + rloc;
             if (ok && row < g.T) {
-                const int64_t at = ((int64_t)b * g.T + row) * gs + (int64_t)h * HD;
+                const int64_t at = ((int64_t)b * g.T + row) * gs + (int64_t)h * d;
 #pragma unroll
-                for (int q = 0; q < 64; q += 8) {
+                for (int q = 0; q < HD; q += 8) {
+                    if (q >= d) break;
                     float v[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = acc[q + e] * scale;
@@ -1086,46 +1112,76 @@ attn_mod_dq_kernel(const __grid_constant__ CUtensorMap tmKk, const __grid_consta
 
 }  // namespace
 
-bool attention_mod_tc_supports(const AttnModArgs& g) { return g.C / g.H == HD && g.qkv_lo; }
+namespace {
 
-cudaError_t launch_attention_mod_fwd_tc(const AttnModArgs& g, cudaStream_t s) {
-    const int64_t rows = (int64_t)g.B * g.T, cols = 3 * (int64_t)g.C;
+// Tensor map over the hi/lo planes [2][rows][heads][d] of whole heads: boxes of 32 columns (zeros past d) x one head x box_rows rows x
+// both planes, K-major (128-byte swizzle) or MN-major (128-byte swizzle with 32-byte atoms).
+bool head_map(CUtensorMap* tm, const float* base, int d, int64_t heads, int64_t rows, uint32_t box_rows, bool mn_major) {
+    EncodeTiledFn enc = tensor_map_encoder();
+    if (!enc) return false;
+    cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)rows, 2};
+    cuuint64_t strides[3] = {(cuuint64_t)d * 4, (cuuint64_t)(heads * d) * 4, (cuuint64_t)(rows * heads * d) * 4};
+    cuuint32_t box[4] = {32, 1, box_rows, 2};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return enc(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, (void*)base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               mn_major ? CU_TENSOR_MAP_SWIZZLE_128B_ATOM_32B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int HD>
+cudaError_t launch_fwd(const AttnModArgs& g, cudaStream_t s) {
+    const int64_t rows = (int64_t)g.B * g.T;
+    const int d = g.C / g.H;
     CUtensorMap q, k, v;
-    if (!plane_map(&q, g.qkv, cols, rows, BR, false) || !plane_map(&k, g.qkv, cols, rows, BT64, false) ||
-        !plane_map(&v, g.qkv, cols, rows, BT64, true))
+    if (!head_map(&q, g.qkv, d, 3 * g.H, rows, BR, false) || !head_map(&k, g.qkv, d, 3 * g.H, rows, BT64, false) ||
+        !head_map(&v, g.qkv, d, 3 * g.H, rows, BT64, true))
         return cudaErrorInvalidValue;
     const dim3 grid(g.B * g.H, (g.T + BR - 1) / BR);
-    const ModTcArgs a{g, attn_head_group((int)grid.x, (int)grid.y)};
+    const ModTcArgs a{g, d, attn_head_group((int)grid.x, (int)grid.y)};
     BT_FOR_MOD(g, {
-        cudaError_t e = allow_smem<attn_mod_fwd_kernel<kCap, kSlope>>(kFwdSmem);
+        cudaError_t e = allow_smem<attn_mod_fwd_kernel<HD, kCap, kSlope>>(kFwdSmem<HD>);
         if (e != cudaSuccess) return e;
-        BT_KERNEL_LAUNCH((attn_mod_fwd_kernel<kCap, kSlope>), grid, kFwdThreads, kFwdSmem, s, q, k, v, a);
+        BT_KERNEL_LAUNCH((attn_mod_fwd_kernel<HD, kCap, kSlope>), grid, kFwdThreads, kFwdSmem<HD>, s, q, k, v, a);
     });
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }
 
-cudaError_t launch_attention_mod_bwd_tc(const AttnModArgs& g, cudaStream_t s) {
-    const int64_t rows = (int64_t)g.B * g.T, cols = 3 * (int64_t)g.C;
+template <int HD>
+cudaError_t launch_bwd(const AttnModArgs& g, cudaStream_t s) {
+    const int64_t rows = (int64_t)g.B * g.T;
+    const int d = g.C / g.H;
     CUtensorMap qkv_k, qkv_m, qkv_res, do_k, do_m, do_res;
-    if (!plane_map(&qkv_k, g.qkv, cols, rows, BT64, false) || !plane_map(&qkv_m, g.qkv, cols, rows, BT64, true) ||
-        !plane_map(&qkv_res, g.qkv, cols, rows, BR, false) || !plane_map(&do_k, g.d_o, g.C, rows, BT64, false) ||
-        !plane_map(&do_m, g.d_o, g.C, rows, BT64, true) || !plane_map(&do_res, g.d_o, g.C, rows, BR, false))
+    if (!head_map(&qkv_k, g.qkv, d, 3 * g.H, rows, BT64, false) || !head_map(&qkv_m, g.qkv, d, 3 * g.H, rows, BT64, true) ||
+        !head_map(&qkv_res, g.qkv, d, 3 * g.H, rows, BR, false) || !head_map(&do_k, g.d_o, d, g.H, rows, BT64, false) ||
+        !head_map(&do_m, g.d_o, d, g.H, rows, BT64, true) || !head_map(&do_res, g.d_o, d, g.H, rows, BR, false))
         return cudaErrorInvalidValue;
     const dim3 grid(g.B * g.H, (g.T + BR - 1) / BR);
-    const ModTcArgs a{g, attn_head_group((int)grid.x, (int)grid.y)};
+    const ModTcArgs a{g, d, attn_head_group((int)grid.x, (int)grid.y)};
     BT_FOR_MOD(g, {
-        cudaError_t e = allow_smem<attn_mod_dq_kernel<kCap, kSlope>>(kDqSmem);
+        cudaError_t e = allow_smem<attn_mod_dq_kernel<HD, kCap, kSlope>>(kDqSmem<HD>);
         if (e == cudaSuccess)
-            e = allow_smem<attn_mod_dkv_kernel<kCap, kSlope>>(kDkvSmem);
+            e = allow_smem<attn_mod_dkv_kernel<HD, kCap, kSlope>>(kDkvSmem<HD>);
         if (e != cudaSuccess) return e;
         // the dq kernel goes first: it also forms D
-        BT_KERNEL_LAUNCH((attn_mod_dq_kernel<kCap, kSlope>), grid, kDqThreads, kDqSmem, s, qkv_k, qkv_m, qkv_k, do_res, a);
-        BT_KERNEL_LAUNCH((attn_mod_dkv_kernel<kCap, kSlope>), grid, kDkvThreads, kDkvSmem, s, qkv_k, qkv_m, do_k, do_m, qkv_res, a);
+        BT_KERNEL_LAUNCH((attn_mod_dq_kernel<HD, kCap, kSlope>), grid, kDqThreads, kDqSmem<HD>, s, qkv_k, qkv_m, qkv_k, do_res, a);
+        BT_KERNEL_LAUNCH((attn_mod_dkv_kernel<HD, kCap, kSlope>), grid, kDkvThreads, kDkvSmem<HD>, s, qkv_k, qkv_m, do_k, do_m, qkv_res, a);
     });
     BT_COUNT_LAUNCH();
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
+}
+
+}  // namespace
+
+bool attention_mod_tc_supports(const AttnModArgs& g) { return g.C / g.H == 64 && g.qkv_lo; }   // narrower heads: narrow_tc
+
+cudaError_t launch_attention_mod_fwd_tc(const AttnModArgs& g, cudaStream_t s) {
+    return g.C / g.H == 64 ? launch_fwd<64>(g, s) : launch_fwd<32>(g, s);
+}
+
+cudaError_t launch_attention_mod_bwd_tc(const AttnModArgs& g, cudaStream_t s) {
+    return g.C / g.H == 64 ? launch_bwd<64>(g, s) : launch_bwd<32>(g, s);
 }
 
 }  // namespace bt

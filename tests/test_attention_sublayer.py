@@ -642,6 +642,99 @@ def test_attention_mod_two_streams():
 
 
 @gpu
+@pytest.mark.parametrize("d,T", [(16, 100), (16, 300), (32, 100), (32, 200), (64, 200), (128, 140)])
+def test_attention_mod_every_form_of_the_inputs(d, T):
+    """qkv and d_o raw, as planes, and both, in every combination; the scratch holds anything."""
+    case = Case(2, T, 2, d, seed=d, mean=80, pad=20, cap=30.0, slope=True)
+    B, C, H = case.B, case.C, case.H
+    o, lse = case.o.reshape(B * T, C).float().contiguous(), case.lse.float().contiguous()
+    for x in ((case.qkv, None), (None, planes_of(case.qkv)), (case.qkv, planes_of(case.qkv))):
+        out, got = torch.empty(B * T, C, device=DEV), torch.empty(B, H, T, device=DEV)
+        b.bt_op_attention_mod_fwd(*x, B, T, C, H, case.mod, out, None, got, case.scratch, case.scratch.numel())
+        assert close(out.view_as(case.o), case.o, TOL)
+        for g in ((case.d_o, None), (None, planes_of(case.d_o)), (case.d_o, planes_of(case.d_o))):
+            case.scratch.fill_(255)
+            dqkv = torch.empty(B * T, 3 * C, device=DEV)
+            b.bt_op_attention_mod_bwd(*x, o, lse, *g, B, T, C, H, case.mod, dqkv, None, case.scratch, case.scratch.numel())
+            b.bt_op_attention_mod_check(case.scratch)
+            for n in range(3):
+                assert close(dqkv.view_as(case.grad)[:, :, n], case.grad[:, :, n], TOL, case.size[n])
+
+
+def off16(*shape):
+    """An array that starts 16 bytes behind a 32-byte boundary."""
+    n = math.prod(shape)
+    t = torch.empty(n + 8, device=DEV)[4:4 + n].view(shape)
+    assert t.data_ptr() % 32 == 16
+    return t
+
+
+@gpu
+@pytest.mark.parametrize("d,T", [(16, 300), (32, 60), (32, 200), (64, 200), (128, 140)])
+def test_attention_mod_arrays_on_16_bytes(d, T):
+    """Arrays need 16-byte alignment only: the same bits as from 32-byte aligned ones."""
+    case = Case(2, T, 3, d, seed=5, cap=30.0, mean=70)
+    B, C, H = case.B, case.C, case.H
+    o, lse = case.o.reshape(B * T, C).float().contiguous(), case.lse.float().contiguous()
+    for planes in ((False, True) if d >= 64 else (False,)):
+        got = []
+        for new in (lambda *s: torch.empty(*s, device=DEV), off16):
+            put = lambda t: new(*t.shape).copy_(t)  # noqa: B023,E731
+            x = (None, put(planes_of(case.qkv))) if planes else (put(case.qkv), None)
+            g = (None, put(planes_of(case.d_o))) if planes else (put(case.d_o), None)
+            out, out2, l2 = new(B * T, C), new(2, B * T, C), new(B, H, T)
+            dx, dx2 = new(B * T, 3 * C), new(2, B * T, 3 * C)
+            b.bt_op_attention_mod_fwd(*x, B, T, C, H, case.mod, out, out2, l2, case.scratch, case.scratch.numel())
+            b.bt_op_attention_mod_bwd(*x, put(o), put(lse), *g, B, T, C, H, case.mod, dx, dx2, case.scratch, case.scratch.numel())
+            got.append((out, out2, l2, dx, dx2))
+        assert all(torch.equal(p, q) for p, q in zip(*got))
+        assert close(got[1][0].view_as(case.o), case.o, TOL)
+
+
+@gpu
+@pytest.mark.parametrize("d,planes", [(16, False), (32, True), (64, False), (64, True)])
+def test_attention_mod_more_heads_than_a_grid_axis(d, planes):
+    """65,600 sequences of three positions; they are alike, so the answer is that of one."""
+    B, T = 65600, 3
+    one = Case(1, T, 1, d, cap=20.0, seed=3)
+    arg = (lambda t: (None, planes_of(t))) if planes else (lambda t: (t, None))
+    o, lse = torch.empty(B * T, d, device=DEV), torch.empty(B, 1, T, device=DEV)
+    size = b.bt_op_attention_mod_scratch_bytes(B, T, d, 1)
+    scratch, mod, dqkv = torch.empty(size, dtype=torch.uint8, device=DEV), b.make_attn_mod(20.0), torch.empty(B * T, 3 * d, device=DEV)
+    x, g = arg(one.qkv.repeat(B, 1)), arg(one.d_o.repeat(B, 1))
+    b.bt_op_attention_mod_fwd(*x, B, T, d, 1, mod, o, None, lse, scratch, size)
+    b.bt_op_attention_mod_bwd(*x, o, lse, *g, B, T, d, 1, mod, dqkv, None, scratch, size)
+    b.bt_op_attention_mod_check(scratch)
+    for all_, first, want in ((o, o[:T], one.o), (dqkv, dqkv[:T], one.grad)):
+        assert torch.equal(all_.view(B, T, -1), first[None].expand(B, -1, -1))
+        assert close(first.view_as(want), want, TOL, sum(one.size))
+
+
+@gpu
+def test_attention_mod_narrow_heads_on_two_streams():
+    """Heads of 32 go through planes in the call's own scratch: two calls at once do not meet."""
+    cases = [Case(2, 400, 4, 32, seed=s, mean=200, cap=30.0) for s in (1, 2)]
+    want = [(*k.forward(False), k.backward(False)) for k in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(5):
+        got = []
+        for k, s in zip(cases, streams):
+            s.wait_stream(torch.cuda.current_stream())
+            B, T, C, H = k.B, k.T, k.C, k.H
+            o, lse, dqkv = torch.empty(B * T, C, device=DEV), torch.empty(B, H, T, device=DEV), torch.empty(B * T, 3 * C, device=DEV)
+            o_in, lse_in = k.o.reshape(B * T, C).float().contiguous(), k.lse.float().contiguous()
+            torch.cuda.synchronize()
+            # the stream by name, not as the current one
+            b.bt_op_attention_mod_fwd(k.qkv, None, B, T, C, H, k.mod, o, None, lse, k.scratch, k.scratch.numel(), stream=s.cuda_stream)
+            b.bt_op_attention_mod_bwd(k.qkv, None, o_in, lse_in, k.d_o, None, B, T, C, H, k.mod, dqkv, None, k.scratch,
+                                      k.scratch.numel(), stream=s.cuda_stream)
+            got.append((o, lse, dqkv, o_in, lse_in))
+        torch.cuda.synchronize()
+        for w, g in zip(want, got):
+            assert all(torch.equal(p, q) for p, q in zip(w, g))
+
+
+@gpu
 def test_attention_mod_plain_equals_causal_attention():
     """Without a modification the operator is the causal attention beside it."""
     B, T, H, d = 2, 300, 3, 64
