@@ -572,7 +572,7 @@ BT_API bt_status bt_op_attention_spans(const int32_t* doc, const int32_t* prefix
  *     z_ij = softcap tanh(s_ij / softcap) - slopes[h] |i - j|      (softcap 0: z_ij = s_ij - slopes[h] |i - j|)
  * for the pairs (i, j) that `spans` allows (device, from bt_op_attention_spans for the same B and T;
  * NULL: j <= i).  slopes: device float [H], finite (NULL: no bias); |i - j| counts positions of the
- * sequence.  Slopes and softcap are constants: no gradient is formed for them. */
+ * sequence.  softcap is 0 or from 1e-20 to 1e20.  Slopes and softcap are constants: no gradient is formed for them. */
 typedef struct {
     float softcap;
     const float* slopes;
@@ -585,6 +585,7 @@ typedef struct {
  * the outputs asked for raw and / or as planes.  d = 64 or 128 with planes (in the backward: of both qkv and
  * d_o) runs on tcgen05, and so does d = 16 or 32 when T d > 4096 (planes not given are made in scratch); d <= 64
  * otherwise on warp-level MMA, raw d = 128 and BT_FLAG_ATTN_SIMT in plain FP32.
+ * Raw d = 64 is the slow way to a long sequence: planes from bt_op_split cost one pass.  No output may overlap an input.
  * Every row of the inputs must be finite, those behind the mask too (they enter the tensor-core products
  * with weight zero).  At most 2^21 positions, 2^30 rows, 2^24 sequence-heads, 2^33 row-heads.
  * The backward takes the forward's inputs, o (raw) and lse and overwrites all of dqkv:

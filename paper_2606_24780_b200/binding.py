@@ -624,11 +624,15 @@ def make_attn_mod(softcap=0.0, slopes=None, spans=None):
 
 
 def _check_mod(mod, B, T, H):
+    if getattr(mod, "fits", None) == (B, T, H):
+        return
     slopes, spans = getattr(mod, "tensors", (None, None))
     if isinstance(slopes, torch.Tensor) and slopes.numel() < H:
         raise ValueError(f"{slopes.numel()} slopes for {H} heads")
     if isinstance(spans, torch.Tensor) and spans.numel() < bt_op_attention_spans_bytes(B, T):
         raise ValueError("the spans were built for a smaller batch")
+    if mod is not None:
+        mod.fits = (B, T, H)
 
 
 def bt_op_rope_fwd(x, pos, N, T, C, H, rope, y, y_split=None, stream=None):

@@ -1531,7 +1531,9 @@ bt_status attn_mod_args(AttnModArgs& g, const char* who, int32_t B, int32_t T, i
     if (T > (1 << 21) || (int64_t)B * T > (1 << 30) || (int64_t)B * H > (1 << 24) || (int64_t)B * H * T > ((int64_t)1 << 33))
         return fail(BT_ERR_UNSUPPORTED, "%s: more than 2^21 positions, 2^30 rows or 2^33 row-heads", who);
     if (!mod) return fail(BT_ERR_INVALID_ARG, "%s: mod is NULL", who);
-    if (!(mod->softcap >= 0.f) || !std::isfinite(mod->softcap)) return fail(BT_ERR_INVALID_ARG, "%s: softcap must be finite and not negative", who);
+    // within these bounds 1 / (softcap sqrt d) and the products with it stay clear of FP32's ends
+    if (!(mod->softcap == 0.f || (mod->softcap >= 1e-20f && mod->softcap <= 1e20f)))
+        return fail(BT_ERR_INVALID_ARG, "%s: softcap must be 0 or from 1e-20 to 1e20", who);
     if (!aligned16(mod->slopes) || !aligned16(mod->spans)) return fail(BT_ERR_INVALID_ARG, "%s: slopes or spans not 16-byte aligned", who);
     if (!qkv && !qkv_split) return fail(BT_ERR_INVALID_ARG, "%s: qkv and qkv_split both NULL", who);
     if (reinterpret_cast<uintptr_t>(scratch) & 255u) return fail(BT_ERR_INVALID_ARG, "%s: scratch not 256-byte aligned", who);
@@ -1604,6 +1606,8 @@ extern "C" bt_status bt_op_attention_mod_fwd(const float* qkv, const float* qkv_
     if (!o && !o_split) return fail(BT_ERR_INVALID_ARG, "attention_mod_fwd: no output requested");
     AttnModArgs g{};
     if (bt_status st = attn_mod_args(g, "attention_mod_fwd", B, T, C, H, mod, qkv, qkv_split, scratch, scratch_bytes)) return st;
+    if ((o && (o == qkv || o == qkv_split)) || (o_split && (o_split == qkv || o_split == qkv_split)))
+        return fail(BT_ERR_INVALID_ARG, "attention_mod_fwd: an output over an input");
     g.o = o; g.o_hi = o_split; g.o_lo = o_split ? o_split + (int64_t)B * T * C : nullptr;
     g.lse = lse;
     cudaStream_t s = (cudaStream_t)stream;
@@ -1621,6 +1625,9 @@ extern "C" bt_status bt_op_attention_mod_bwd(const float* qkv, const float* qkv_
     if (!d_o && !d_o_split) return fail(BT_ERR_INVALID_ARG, "attention_mod_bwd: d_o and d_o_split both NULL");
     AttnModArgs g{};
     if (bt_status st = attn_mod_args(g, "attention_mod_bwd", B, T, C, H, mod, qkv, qkv_split, scratch, scratch_bytes)) return st;
+    for (const float* out : {(const float*)dqkv, (const float*)dqkv_split})
+        for (const float* in : {qkv, qkv_split, o, lse, d_o, d_o_split})
+            if (out && out == in) return fail(BT_ERR_INVALID_ARG, "attention_mod_bwd: an output over an input");
     const int64_t n = (int64_t)B * T;
     const bool planes = d_o_split && (!d_o || attn_mod_wants_planes(T, C / H));
     g.d_o = planes ? d_o_split : d_o;

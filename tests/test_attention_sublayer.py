@@ -185,6 +185,8 @@ def test_attention_mod_refusals(lib):
     fwd(2, B=1 << 13, T=1 << 18, size=1 << 50)
     fwd(1, mod=b.make_attn_mod(softcap=-1.0)), fwd(1, mod=b.make_attn_mod(softcap=math.inf)), fwd(1, mod=b.make_attn_mod(softcap=math.nan))
     fwd(1, mod=b.make_attn_mod(slopes=A + 4)), fwd(1, mod=b.make_attn_mod(spans=A + 8))
+    fwd(1, mod=b.make_attn_mod(softcap=1e-21)), fwd(1, mod=b.make_attn_mod(softcap=2e20)), fwd(1, qkv=A, o=A), fwd(1, o=None, o_split=A)
+    bwd(1, dqkv=A), bwd(1, o=2 * A, dqkv=2 * A), bwd(1, d_o=3 * A, dqkv=3 * A)
     bwd(1, o=None), bwd(1, lse=None), bwd(1, d_o=None), bwd(1, dqkv=None), bwd(1, scratch=None), bwd(3, size=n - 1), bwd(1, H=3)
     refused(1, b.bt_op_attention_mod_check, None)
     # the C entries take a NULL modification
@@ -642,6 +644,17 @@ def test_attention_mod_two_streams():
 
 
 @gpu
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+def test_attention_mod_softcaps_at_the_ends_of_the_range(d):
+    """1e-20: every score is worth nothing, rows are plain means and pass no gradient on to q and k.  1e20: no cap at all."""
+    for cap in (1e-20, 1e20):
+        for T in (60, 270):
+            case = Case(1, T, 2, d, cap=cap, seed=T)
+            for planes, flags in ways(d):
+                case.check(planes, flags)
+
+
+@gpu
 @pytest.mark.parametrize("d,T", [(16, 100), (16, 300), (32, 100), (32, 200), (64, 200), (128, 140)])
 def test_attention_mod_every_form_of_the_inputs(d, T):
     """qkv and d_o raw, as planes, and both, in every combination; the scratch holds anything."""
@@ -692,7 +705,7 @@ def test_attention_mod_arrays_on_16_bytes(d, T):
 
 
 @gpu
-@pytest.mark.parametrize("d,planes", [(16, False), (32, True), (64, False), (64, True)])
+@pytest.mark.parametrize("d,planes", [(16, False), (32, True), (64, False), (64, True), (128, True)])
 def test_attention_mod_more_heads_than_a_grid_axis(d, planes):
     """65,600 sequences of three positions; they are alike, so the answer is that of one."""
     B, T = 65600, 3
@@ -732,6 +745,48 @@ def test_attention_mod_narrow_heads_on_two_streams():
         torch.cuda.synchronize()
         for w, g in zip(want, got):
             assert all(torch.equal(p, q) for p, q in zip(w, g))
+
+
+@gpu
+@pytest.mark.parametrize("d,planes", [(32, False), (64, True), (128, True)])
+def test_attention_mod_past_two_to_the_31_elements(d, planes):
+    """1,000 sequences of 1,000 positions: qkv alone has 2.3e9 elements.  All are alike, so the answer is that of one."""
+    B, T, C = 1000, 1000, 768
+    H = C // d
+    one = Case(1, T, H, d, cap=20.0, seed=3, mean=300)
+    spans = spans_of(random_layout(np.random.default_rng(3 + 7 * T), 1, T, 300, 0, 0)[0].repeat(B, 0), None, 0, B, T)
+    mod, size = b.make_attn_mod(20.0, None, spans), b.bt_op_attention_mod_scratch_bytes(B, T, C, H)
+    scratch = torch.empty(size, dtype=torch.uint8, device=DEV)
+    if planes:
+        arg = lambda t: (None, planes_of(t)[:, None].expand(2, B, *t.shape).contiguous())  # noqa: E731
+    else:
+        arg = lambda t: (t.repeat(B, 1), None)  # noqa: E731
+    x = arg(one.qkv)
+    o, lse = torch.empty(B, T, C, device=DEV), torch.empty(B, H, T, device=DEV)
+    b.bt_op_attention_mod_fwd(*x, B, T, C, H, mod, o, None, lse, scratch, size)
+    assert close(o[0].view_as(one.o), one.o, TOL)
+    assert all(torch.equal(o[n], o[0]) for n in range(B)) and torch.equal(lse, lse[:1].expand_as(lse))
+    g, dqkv = arg(one.d_o), torch.empty(B, T, 3 * C, device=DEV)
+    b.bt_op_attention_mod_bwd(*x, o, lse, *g, B, T, C, H, mod, dqkv, None, scratch, size)
+    b.bt_op_attention_mod_check(scratch)
+    assert close(dqkv[0].view_as(one.grad), one.grad, TOL, sum(one.size))
+    assert all(torch.equal(dqkv[n], dqkv[0]) for n in range(B))
+
+
+@gpu
+def test_rope_and_dropout_past_two_to_the_32_elements():
+    H, d, N = 12, 64, 1_900_000
+    C, cfg = H * d, b.make_rope(d)
+    few = rand(1, 1000, 3 * C)
+    x, want = few.repeat(N // 1000, 1), torch.empty_like(few)          # 4.4e9 elements
+    b.bt_op_rope_fwd(few, None, 1000, 1000, C, H, cfg, want)
+    b.bt_op_rope_fwd(x, None, N, 1000, C, H, cfg, x)
+    assert all(torch.equal(part, want) for part in x.split(1000))
+    n = 2 ** 32 + 1028
+    x = x.view(-1)[:n].fill_(1.0)
+    b.bt_op_dropout_fwd(x, None, n, 0.5, 7, 9, x)
+    for at in (0, 2 ** 31 - 32, 2 ** 32 - 32, n - 64):
+        assert np.array_equal(np64(x[at:at + 64]) != 0, keep_mask(64, 0.5, 7, 9, at // 4))
 
 
 @gpu
