@@ -27,21 +27,40 @@ namespace {
 // and of 16 columns, zeros in half of the tcgen05 tiles: T 256, batch 32    52, 52;   161, 166.
 bool narrow_tc(const AttnModArgs& g) { return g.planes && (attn_mod_wants_planes(g.T, g.C / g.H) || !attention_mod_mma_supports(g)); }
 
+// Up to two arrays into planes in one launch; x.n4 and y.n4 float4 values (a launch costs as much as 3 MB of copying).
+struct ToSplit {
+    const float* from;
+    float *hi, *lo;
+    int64_t n4;
+};
+__global__ void __launch_bounds__(256) split_two_kernel(const ToSplit x, const ToSplit y) {
+    pdl_wait();
+    pdl_trigger();
+    for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < x.n4 + y.n4; i += (int64_t)gridDim.x * blockDim.x) {
+        const ToSplit& a = i < x.n4 ? x : y;
+        const int64_t k = i < x.n4 ? i : i - x.n4;
+        store_raw_split(ld4(a.from, k), nullptr, a.hi, a.lo, k);
+    }
+}
+
 cudaError_t narrow_planes(AttnModArgs& g, cudaStream_t s) {
     const int64_t n = (int64_t)g.B * g.T * g.C;
-    cudaError_t e = cudaSuccess;
+    ToSplit x{}, y{};
     if (!g.qkv_lo) {
-        e = launch_split(g.qkv, g.planes, g.planes + 3 * n, 3 * n, s);
-        g.qkv = g.planes;
-        g.qkv_lo = g.planes + 3 * n;
+        x = ToSplit{g.qkv, g.planes, g.planes + 3 * n, 3 * n / 4};
+        g.qkv = x.hi;
+        g.qkv_lo = x.lo;
     }
-    if (e == cudaSuccess && g.d_o && !g.d_o_lo) {
-        float* p = g.planes + 6 * n;
-        e = launch_split(g.d_o, p, p + n, n, s);
-        g.d_o = p;
-        g.d_o_lo = p + n;
+    if (g.d_o && !g.d_o_lo) {
+        y = ToSplit{g.d_o, g.planes + 6 * n, g.planes + 7 * n, n / 4};
+        g.d_o = y.hi;
+        g.d_o_lo = y.lo;
     }
-    return e;
+    if (x.n4 + y.n4 == 0) return cudaSuccess;
+    const int64_t blocks = (x.n4 + y.n4 + 255) / 256;
+    BT_KERNEL_LAUNCH((split_two_kernel), (int)(blocks < 148 * 16 ? blocks : 148 * 16), 256, 0, s, x, y);
+    BT_COUNT_LAUNCH();
+    return cudaGetLastError();
 }
 
 }  // namespace
