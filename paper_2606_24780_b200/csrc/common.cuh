@@ -364,6 +364,7 @@ struct DropoutArgs {
     uint64_t threshold;         // keep a word that is at least this
     float scale;
     float *y, *y_hi, *y_lo;
+    uint32_t key[20];           // set by the launcher: the generator's round keys
 };
 cudaError_t launch_dropout(const DropoutArgs& g, cudaStream_t s);
 
