@@ -192,11 +192,17 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _this_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
+_cuda_up = False
+
+
 def _call(fn, stream, *args):
     """One C call on `stream`, by default the current one (its handle without a Stream object: the small operators
     take a few microseconds on the GPU, and half of that here)."""
     if stream is None:
-        stream = _raw_stream(_this_device()) if _raw_stream and torch.cuda.is_initialized() else _stream(None)
+        global _cuda_up
+        if not _cuda_up:
+            _cuda_up = _raw_stream is not None and torch.cuda.is_initialized()
+        stream = _raw_stream(_this_device()) if _cuda_up else _stream(None)
     st = fn(*args, stream)
     if st:
         _check(st)
@@ -602,13 +608,14 @@ def _arr(t, dtype=torch.float32):
         return t
     if not isinstance(t, torch.Tensor):
         raise TypeError(type(t))
+    device = t.get_device()                                 # -1: not a device array
+    if device >= 0 and t.dtype is dtype and device == _this_device() and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype is not dtype:
         raise ValueError(f"expected a {dtype} tensor, got {t.dtype}")
-    if t.get_device() != (_this_device() if t.is_cuda else None):
+    if device < 0 or device != _this_device():
         raise ValueError(f"expected a tensor on the current device, got one on {t.device}")
-    if not t.is_contiguous():
-        raise ValueError("tensor arguments must be contiguous")
-    return t.data_ptr()
+    raise ValueError("tensor arguments must be contiguous")
 
 
 def make_rope(rot_dim, interleaved=False, base=10000.0, scaling=BT_ROPE_PLAIN, factor=1.0, low=1.0, high=32.0,
