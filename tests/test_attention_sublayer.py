@@ -6,8 +6,8 @@ of the running sum per instruction, 24 instructions for 64 columns, so at most 2
 half of that on average).  A score error e moves a probability by e, so with scores of a few units an output
 or gradient is within 1e-5 of its norm; the plain FP32 kernels are well inside that.
 """
-import ctypes
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -787,6 +787,51 @@ def test_rope_and_dropout_past_two_to_the_32_elements():
     b.bt_op_dropout_fwd(x, None, n, 0.5, 7, 9, x)
     for at in (0, 2 ** 31 - 32, 2 ** 32 - 32, n - 64):
         assert np.array_equal(np64(x[at:at + 64]) != 0, keep_mask(64, 0.5, 7, 9, at // 4))
+
+
+@gpu
+@pytest.mark.parametrize("d,T", [(16, 60), (16, 300), (32, 200), (64, 200), (128, 140)])
+def test_attention_mod_planes_alone_as_the_output(d, T):
+    """Without a raw output the planes are those of the call that writes both."""
+    case = Case(2, T, 2, d, seed=8, mean=70, pad=15, cap=30.0)
+    B, C, H = case.B, case.C, case.H
+    o_in, lse_in = case.o.reshape(B * T, C).float().contiguous(), case.lse.float().contiguous()
+    for planes, flags in ways(d):
+        x = (None, planes_of(case.qkv)) if planes else (case.qkv, None)
+        g = (None, planes_of(case.d_o)) if planes else (case.d_o, None)
+        got = []
+        for raw in (True, False):
+            o, dx = (torch.empty(B * T, C, device=DEV), torch.empty(B * T, 3 * C, device=DEV)) if raw else (None, None)
+            o2, dx2, lse = torch.empty(2, B * T, C, device=DEV), torch.empty(2, B * T, 3 * C, device=DEV), torch.empty(B, H, T, device=DEV)
+            b.bt_op_attention_mod_fwd(*x, B, T, C, H, case.mod, o, o2, lse, case.scratch, case.scratch.numel(), flags)
+            b.bt_op_attention_mod_bwd(*x, o_in, lse_in, *g, B, T, C, H, case.mod, dx, dx2, case.scratch, case.scratch.numel(), flags)
+            got.append((o2, dx2, lse))
+        assert all(torch.equal(p, q) for p, q in zip(*got))
+        assert close(got[1][0].sum(0).view_as(case.o), case.o, TOL)
+
+
+@gpu
+def test_attention_mod_from_several_host_threads():
+    cases = [Case(2, 300, 3, d, seed=d, mean=100, cap=30.0) for d in (32, 64, 128, 64)]
+    want = [(*k.forward(k.d >= 64), k.backward(k.d >= 64)) for k in cases]
+    bad = []
+
+    def work(k, w):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(10):
+                    if not all(torch.equal(p, q) for p, q in zip(w, (*k.forward(k.d >= 64), k.backward(k.d >= 64)))):
+                        bad.append(k.d)
+        except Exception as e:  # noqa: BLE001
+            bad.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=a) for a in zip(cases, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad, bad
 
 
 @gpu
