@@ -582,17 +582,17 @@ typedef struct {
 /* Attention with modified scores: o_i = sum_j softmax_j(z_ij) v_j, lse [B, H, T] = log sum_j exp z_ij.  A
  * query that may read no key gets o = 0, lse = -inf and takes no part in the backward.  Layouts as in
  * bt_op_attention_fwd / _bwd (d in {16, 32, 64, 128}); q, k, v and d_o may be given raw and / or as hi/lo planes,
- * the outputs asked for raw and / or as planes.  d = 64 or 128 with planes (in the backward: of both qkv and
- * d_o) runs on tcgen05, and so does d = 16 or 32 when T d > 4096 (planes not given are made in scratch); d <= 64
- * otherwise on warp-level MMA, raw d = 128 and BT_FLAG_ATTN_SIMT in plain FP32.
- * Raw d = 64 is the slow way to a long sequence: planes from bt_op_split cost one pass.  No output may overlap an input.
+ * the outputs asked for raw and / or as planes.  The kernels run on tcgen05 and read planes (those not given are made
+ * in scratch, one pass more); d < 64 with T d <= 4096 runs on warp-level MMA and reads raw arrays if it can, and
+ * BT_FLAG_ATTN_SIMT in plain FP32.  No output may overlap an input.
  * Every row of the inputs must be finite, those behind the mask too (they enter the tensor-core products
  * with weight zero).  At most 2^21 positions, 2^30 rows, 2^24 sequence-heads, 2^33 row-heads.
  * The backward takes the forward's inputs, o (raw) and lse and overwrites all of dqkv:
  *     dv_j = sum_i p_ij do_i,  ds_ij = p_ij (do_i v_j - do_i o_i) (1 - tanh^2),
  *     dq_i = sum_j ds_ij k_j / sqrt(d),  dk_j = sum_i ds_ij q_i / sqrt(d),
  * in a fixed order (no atomics: two runs give the same bits).
- * scratch: device, 256-byte aligned, bt_op_attention_mod_scratch_bytes bytes, contents irrelevant on entry;
+ * scratch: device, 256-byte aligned, bt_op_attention_mod_scratch_bytes bytes (a call with d >= 64 that is given
+ * planes of qkv, and of d_o in the backward, needs only 256 + 4 B H T, rounded up to 256), contents irrelevant on entry;
  * calls that may overlap on the GPU need one each.  bt_op_attention_mod_check synchronises the stream and
  * returns BT_ERR_DEVICE_TIMEOUT if a bounded wait of the last call on that scratch ran out. */
 BT_API size_t bt_op_attention_mod_scratch_bytes(int32_t B, int32_t T, int32_t C, int32_t H);

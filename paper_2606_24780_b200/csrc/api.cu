@@ -1518,13 +1518,13 @@ bt_status dropout_impl(const float* x, const float* residual, int64_t n, double 
     return BT_OK;
 }
 
-// Scratch of the modified attention: the device error word in the first 256 bytes, then [B, H, T] row sums, then for
-// heads of 16 and 32 columns the planes that their tensor-core kernels read (callers have those as raw arrays).
+// Scratch of the modified attention: the device error word in the first 256 bytes, then [B, H, T] row sums, then the
+// planes that the tensor-core kernels read, where the caller has raw arrays.
 constexpr size_t kAttnModHeader = 256;
 size_t attn_mod_sums(int32_t B, int32_t T, int32_t H) { return ((size_t)B * H * T * sizeof(float) + 255) & ~(size_t)255; }
 
 bt_status attn_mod_args(AttnModArgs& g, const char* who, int32_t B, int32_t T, int32_t C, int32_t H, const bt_attn_mod* mod,
-                        const float* qkv, const float* qkv_split, void* scratch, size_t scratch_bytes) {
+                        const float* qkv, const float* qkv_split, bool all_split, void* scratch, size_t scratch_bytes) {
     if (B < 1 || T < 1 || C < 1 || H < 1 || C % H) return fail(BT_ERR_INVALID_ARG, "%s: bad sizes", who);
     const int d = C / H;
     if (d != 16 && d != 32 && d != 64 && d != 128) return fail(BT_ERR_UNSUPPORTED, "%s: head_dim %d not in {16,32,64,128}", who, d);
@@ -1537,7 +1537,9 @@ bt_status attn_mod_args(AttnModArgs& g, const char* who, int32_t B, int32_t T, i
     if (!aligned16(mod->slopes) || !aligned16(mod->spans)) return fail(BT_ERR_INVALID_ARG, "%s: slopes or spans not 16-byte aligned", who);
     if (!qkv && !qkv_split) return fail(BT_ERR_INVALID_ARG, "%s: qkv and qkv_split both NULL", who);
     if (reinterpret_cast<uintptr_t>(scratch) & 255u) return fail(BT_ERR_INVALID_ARG, "%s: scratch not 256-byte aligned", who);
-    if (scratch_bytes < bt_op_attention_mod_scratch_bytes(B, T, C, H)) return fail(BT_ERR_OOM, "%s: scratch too small", who);
+    const size_t sums = kAttnModHeader + attn_mod_sums(B, T, H);
+    const bool own_planes = !(all_split && d >= 64);
+    if (scratch_bytes < (own_planes ? bt_op_attention_mod_scratch_bytes(B, T, C, H) : sums)) return fail(BT_ERR_OOM, "%s: scratch too small", who);
     const int64_t n = (int64_t)B * T;
     g.B = B; g.T = T; g.C = C; g.H = H;
     g.cap = mod->softcap;
@@ -1549,9 +1551,9 @@ bt_status attn_mod_args(AttnModArgs& g, const char* who, int32_t B, int32_t T, i
     g.qkv_lo = planes ? qkv_split + n * 3 * C : nullptr;
     g.err = (int*)scratch;
     g.dvec = (float*)((uint8_t*)scratch + kAttnModHeader);
-    g.planes = d < 64 ? (float*)((uint8_t*)scratch + kAttnModHeader + attn_mod_sums(B, T, H)) : nullptr;
+    g.planes = own_planes ? (float*)((uint8_t*)scratch + sums) : nullptr;
     char msg[256];
-    if ((planes || d < 64) && !gemm_tc_init(msg, sizeof(msg))) return fail(BT_ERR_CUDA, "tensor-core attention unavailable: %s", msg);
+    if (!gemm_tc_init(msg, sizeof(msg))) return fail(BT_ERR_CUDA, "tensor-core attention unavailable: %s", msg);
     return BT_OK;
 }
 
@@ -1595,8 +1597,7 @@ extern "C" bt_status bt_op_attention_spans(const int32_t* doc, const int32_t* pr
 
 extern "C" size_t bt_op_attention_mod_scratch_bytes(int32_t B, int32_t T, int32_t C, int32_t H) {
     if (B < 1 || T < 1 || C < 1 || H < 1) return 0;
-    const size_t planes = C / H < 64 ? 8 * (size_t)B * T * C * sizeof(float) : 0;
-    return kAttnModHeader + attn_mod_sums(B, T, H) + planes;
+    return kAttnModHeader + attn_mod_sums(B, T, H) + 8 * (size_t)B * T * C * sizeof(float);
 }
 
 extern "C" bt_status bt_op_attention_mod_fwd(const float* qkv, const float* qkv_split, int32_t B, int32_t T, int32_t C,
@@ -1605,7 +1606,7 @@ extern "C" bt_status bt_op_attention_mod_fwd(const float* qkv, const float* qkv_
     BT_OPT_PTR(qkv); BT_OPT_PTR(qkv_split); BT_OPT_PTR(o); BT_OPT_PTR(o_split); BT_PTR(lse); BT_PTR(scratch);
     if (!o && !o_split) return fail(BT_ERR_INVALID_ARG, "attention_mod_fwd: no output requested");
     AttnModArgs g{};
-    if (bt_status st = attn_mod_args(g, "attention_mod_fwd", B, T, C, H, mod, qkv, qkv_split, scratch, scratch_bytes)) return st;
+    if (bt_status st = attn_mod_args(g, "attention_mod_fwd", B, T, C, H, mod, qkv, qkv_split, qkv_split, scratch, scratch_bytes)) return st;
     if ((o && (o == qkv || o == qkv_split)) || (o_split && (o_split == qkv || o_split == qkv_split)))
         return fail(BT_ERR_INVALID_ARG, "attention_mod_fwd: an output over an input");
     g.o = o; g.o_hi = o_split; g.o_lo = o_split ? o_split + (int64_t)B * T * C : nullptr;
@@ -1624,7 +1625,7 @@ extern "C" bt_status bt_op_attention_mod_bwd(const float* qkv, const float* qkv_
     if (!dqkv && !dqkv_split) return fail(BT_ERR_INVALID_ARG, "attention_mod_bwd: no output requested");
     if (!d_o && !d_o_split) return fail(BT_ERR_INVALID_ARG, "attention_mod_bwd: d_o and d_o_split both NULL");
     AttnModArgs g{};
-    if (bt_status st = attn_mod_args(g, "attention_mod_bwd", B, T, C, H, mod, qkv, qkv_split, scratch, scratch_bytes)) return st;
+    if (bt_status st = attn_mod_args(g, "attention_mod_bwd", B, T, C, H, mod, qkv, qkv_split, qkv_split && d_o_split, scratch, scratch_bytes)) return st;
     for (const float* out : {(const float*)dqkv, (const float*)dqkv_split})
         for (const float* in : {qkv, qkv_split, o, lse, d_o, d_o_split})
             if (out && out == in) return fail(BT_ERR_INVALID_ARG, "attention_mod_bwd: an output over an input");

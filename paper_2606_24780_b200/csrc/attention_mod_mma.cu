@@ -1,4 +1,4 @@
-// Attention with modified scores on warp-level MMA, 3xTF32: short sequences of heads of 16 and 32 columns, and heads of 64 without planes.
+// Attention with modified scores on warp-level MMA, 3xTF32: short sequences of heads of 16 and 32 columns.
 //
 // One CTA owns 64 rows of one head, 16 per warp, and walks the 64-row tiles of the other side between the ends
 // of its rows' ranges; a warp skips the tiles none of its rows reads.  Streamed tiles go through
@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 2) dq_kernel(const AttnModArgs g) {
 }
 
 template <int HD, bool CAP, bool SLOPE>
-__global__ void __launch_bounds__(kThreads, HD == 64 ? 1 : 2) dkv_kernel(const AttnModArgs g) {
+__global__ void __launch_bounds__(kThreads, 2) dkv_kernel(const AttnModArgs g) {
     constexpr int TILE = kRows * (HD + 4);
     extern __shared__ float sm[];   // Q[2], dO[2], then lse[2][64], D[2][64]
     pdl_wait();
@@ -454,16 +454,14 @@ cudaError_t bwd(const AttnModArgs& g, cudaStream_t s) {
 
 }  // namespace
 
-// grid.y is the sequence-head: at most 65,535 of them (the plain kernels take the rest).
-bool attention_mod_mma_supports(const AttnModArgs& g) { return g.C / g.H <= 64 && (int64_t)g.B * g.H <= 65535; }
+// grid.y is the sequence-head: at most 65,535 of them.
+bool attention_mod_mma_supports(const AttnModArgs& g) { return g.C / g.H <= 32 && (int64_t)g.B * g.H <= 65535; }
 
 cudaError_t launch_attention_mod_fwd_mma(const AttnModArgs& g, cudaStream_t s) {
-    const int d = g.C / g.H;
-    return d == 16 ? fwd<16>(g, s) : d == 32 ? fwd<32>(g, s) : fwd<64>(g, s);
+    return g.C / g.H == 16 ? fwd<16>(g, s) : fwd<32>(g, s);
 }
 cudaError_t launch_attention_mod_bwd_mma(const AttnModArgs& g, cudaStream_t s) {
-    const int d = g.C / g.H;
-    return d == 16 ? bwd<16>(g, s) : d == 32 ? bwd<32>(g, s) : bwd<64>(g, s);
+    return g.C / g.H == 16 ? bwd<16>(g, s) : bwd<32>(g, s);
 }
 
 }  // namespace bt

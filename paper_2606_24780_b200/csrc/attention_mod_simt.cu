@@ -1,5 +1,5 @@
-// Attention with modified scores in plain FP32: the reference for the tensor-core kernels (selected
-// with BT_FLAG_ATTN_SIMT) and the kernel for raw 128-wide heads.  One warp owns one (sequence, head,
+// Attention with modified scores in plain FP32: the reference for the tensor-core kernels, selected
+// with BT_FLAG_ATTN_SIMT.  One warp owns one (sequence, head,
 // position); lanes own head columns; every dot product is a warp-shuffle reduction.  The forward is the
 // textbook two-pass softmax, deliberately not the one-pass recurrence of the fast kernels.
 //     z_ij = c tanh(q_i k_j / (c sqrt d)) - slope |i - j|     (c = 0: z_ij = q_i k_j / sqrt d - slope |i - j|)

@@ -1182,8 +1182,6 @@ cudaError_t launch_bwd(const AttnModArgs& g, cudaStream_t s) {
 
 }  // namespace
 
-bool attention_mod_tc_supports(const AttnModArgs& g) { return g.C / g.H == 64 && g.qkv_lo; }   // narrower heads: narrow_tc
-
 cudaError_t launch_attention_mod_fwd_tc(const AttnModArgs& g, cudaStream_t s) {
     return g.C / g.H == 64 ? launch_fwd<64>(g, s) : launch_fwd<32>(g, s);
 }

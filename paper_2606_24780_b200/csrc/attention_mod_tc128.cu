@@ -430,8 +430,6 @@ cudaError_t launch_pass(const CUtensorMap& a2, const CUtensorMap& b1, const CUte
 
 }  // namespace
 
-bool attention_mod_tc128_supports(const AttnModArgs& g) { return g.C / g.H == HD && g.qkv_lo; }
-
 cudaError_t launch_attention_mod_fwd_tc128(const AttnModArgs& g, cudaStream_t s) {
     const int64_t rows = (int64_t)g.B * g.T, cols = 3 * (int64_t)g.C;
     CUtensorMap k, v;

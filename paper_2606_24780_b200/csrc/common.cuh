@@ -332,11 +332,11 @@ struct AttnModArgs {
     float* lse;                 // [B, H, T]: written by the forward, read by the backward
     const float *d_o, *d_o_lo;
     float* dvec;                // [B, H, T] rowsum(dO o O), scratch
-    float* planes;              // heads of 16 and 32: scratch for the hi/lo planes of qkv and dO (null: wider heads)
+    float* planes;              // scratch for the hi/lo planes of qkv and dO (null: all given as planes)
     float *dqkv, *dqkv_hi, *dqkv_lo;
     int* err;                   // device error word of the bounded waits
 };
-// Whether the kernels for this length and head_dim read planes (made from a raw array if need be when d < 64).
+// Whether the kernels for this length and head_dim read planes (made from raw arrays if need be): those on tcgen05.
 inline bool attn_mod_wants_planes(int T, int d) { return d >= 64 || (int64_t)T * d > 4096; }
 cudaError_t launch_attention_mod_fwd(const AttnModArgs& g, bool simt, cudaStream_t s);
 cudaError_t launch_attention_mod_bwd(const AttnModArgs& g, bool simt, cudaStream_t s);

@@ -835,6 +835,28 @@ def test_attention_mod_from_several_host_threads():
 
 
 @gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_mod_scratch_of_calls_given_planes(d):
+    """They need the error word and the row sums only; the bytes behind those stay as they were."""
+    case = Case(3, 150, 2, d, seed=4, cap=30.0, mean=60)
+    B, T, C, H = case.B, case.T, case.C, case.H
+    small = 256 + (4 * B * H * T + 255) // 256 * 256
+    buf = torch.full((small + 4096,), 77, dtype=torch.uint8, device=DEV)
+    x, g = planes_of(case.qkv), planes_of(case.d_o)
+    o, lse, dqkv = torch.empty(B * T, C, device=DEV), torch.empty(B, H, T, device=DEV), torch.empty(B * T, 3 * C, device=DEV)
+    b.bt_op_attention_mod_fwd(None, x, B, T, C, H, case.mod, o, None, lse, buf, small)
+    b.bt_op_attention_mod_bwd(None, x, o, lse, None, g, B, T, C, H, case.mod, dqkv, None, buf, small)
+    b.bt_op_attention_mod_check(buf)
+    assert (buf[small:] == 77).all()
+    for n in range(3):
+        assert close(dqkv.view_as(case.grad)[:, :, n], case.grad[:, :, n], TOL, case.size[n])
+    with pytest.raises(b.BtError):
+        b.bt_op_attention_mod_bwd(None, x, o, lse, case.d_o, None, B, T, C, H, case.mod, dqkv, None, buf, small)
+    with pytest.raises(b.BtError):
+        b.bt_op_attention_mod_fwd(None, x, B, T, C, H, case.mod, o, None, lse, buf, small - 1)
+
+
+@gpu
 def test_attention_mod_plain_equals_causal_attention():
     """Without a modification the operator is the causal attention beside it."""
     B, T, H, d = 2, 300, 3, 64
