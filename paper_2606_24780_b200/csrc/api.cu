@@ -1552,8 +1552,14 @@ bt_status attn_mod_args(AttnModArgs& g, const char* who, int32_t B, int32_t T, i
     g.err = (int*)scratch;
     g.dvec = (float*)((uint8_t*)scratch + kAttnModHeader);
     g.planes = own_planes ? (float*)((uint8_t*)scratch + sums) : nullptr;
+    return BT_OK;
+}
+
+// After the checks of arguments, which need no driver.
+bt_status attn_mod_ready(const char* who, uint32_t flags) {
     char msg[256];
-    if (!gemm_tc_init(msg, sizeof(msg))) return fail(BT_ERR_CUDA, "tensor-core attention unavailable: %s", msg);
+    if (!(flags & BT_FLAG_ATTN_SIMT) && !gemm_tc_init(msg, sizeof(msg)))
+        return fail(BT_ERR_CUDA, "%s: tensor-core attention unavailable: %s", who, msg);
     return BT_OK;
 }
 
@@ -1612,6 +1618,7 @@ extern "C" bt_status bt_op_attention_mod_fwd(const float* qkv, const float* qkv_
     g.o = o; g.o_hi = o_split; g.o_lo = o_split ? o_split + (int64_t)B * T * C : nullptr;
     g.lse = lse;
     cudaStream_t s = (cudaStream_t)stream;
+    if (bt_status st = attn_mod_ready("attention_mod_fwd", flags)) return st;
     BT_CUDA(launch_attention_mod_fwd(g, (flags & BT_FLAG_ATTN_SIMT) != 0, s));
     return BT_OK;
 }
@@ -1637,6 +1644,7 @@ extern "C" bt_status bt_op_attention_mod_bwd(const float* qkv, const float* qkv_
     g.lse = const_cast<float*>(lse);
     g.dqkv = dqkv; g.dqkv_hi = dqkv_split; g.dqkv_lo = dqkv_split ? dqkv_split + n * 3 * C : nullptr;
     cudaStream_t s = (cudaStream_t)stream;
+    if (bt_status st = attn_mod_ready("attention_mod_bwd", flags)) return st;
     BT_CUDA(launch_attention_mod_bwd(g, (flags & BT_FLAG_ATTN_SIMT) != 0, s));
     return BT_OK;
 }
