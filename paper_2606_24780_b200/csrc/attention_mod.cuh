@@ -47,7 +47,8 @@ __device__ __forceinline__ Score make_score(float scale, float cap, const float*
 // otherwise they carry s.unit already.  |first - i| is the distance of position i; `grad` (GRAD and CAP) receives
 // 1 - tanh^2.  The exponential and the reciprocal of tanh run at an eighth of the rate of a multiplication and are
 // needed only where some score of the N is beyond 0.6 caps.  A distance is linear in i unless the row lies inside the N
-// positions (no integer conversion per element: it runs at an eighth of the rate too).
+// positions (no integer conversion per element: it runs at an eighth of the rate too).  __fadd_rn: the same roundings
+// whether ref is known to be zero or not (a sum fused with the bias's product would have another).
 template <bool CAP, bool SLOPE, bool GRAD, bool UNIT, int N>
 __device__ __forceinline__ void score_tile(float (&x)[N], float (&grad)[N], const Score& s, int first, float ref) {
     if (CAP) {
@@ -78,18 +79,41 @@ __device__ __forceinline__ void score_tile(float (&x)[N], float (&grad)[N], cons
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float bias = fmaf(step, (float)i, start);
-                x[i] = kScale ? fmaf(x[i], scale, bias) : x[i] + bias;
+                x[i] = kScale ? fmaf(x[i], scale, bias) : __fadd_rn(x[i], bias);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float bias = fmaf(-s.slope2, fabsf(d - (float)i), -ref);
-                x[i] = kScale ? fmaf(x[i], scale, bias) : x[i] + bias;
+                x[i] = kScale ? fmaf(x[i], scale, bias) : __fadd_rn(x[i], bias);
             }
         }
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = kScale ? fmaf(x[i], scale, -ref) : x[i] - ref;
+    }
+}
+
+// The reference that a tile's scores are taken less of before the exponential.  Usually score_tile subtracts it inside a fused
+// operation, unrounded.  Where it or a bias reaches 2^24, a score's own rounding is a unit of the exponent or more, and the
+// fused difference would be that rounding's, up to any size; there the rounded score less the reference, which is the largest
+// of the same rounded scores: never above zero (tanh may be a rounding out of order), and zero for the largest.
+struct Reference {
+    float now, later;
+    bool far;               // some row of the warp: uniform
+};
+// slope2, distance: the bias of no column of the tile is larger than their product.
+__device__ __forceinline__ Reference make_reference(float ref, float slope2, int distance) {
+    const bool far = __any_sync(0xffffffffu, fmaxf(fabsf(ref), fabsf(slope2) * (float)distance) >= 16777216.0f);
+    return {far ? 0.f : ref, ref, far};
+}
+template <int N>
+__device__ __forceinline__ void less_reference(float (&z)[N], const Reference& r) {
+    if (!r.far) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        z[i] -= r.later;
+        z[i] = z[i] > 0.f ? 0.f : z[i];     // not fminf: NaN stays
     }
 }
 

@@ -71,8 +71,8 @@ __device__ __forceinline__ void settle() {
 //   warp 1      S = Q K^T: [K_hi | K_lo] as one operand of 128 rows, the small terms into the second 64 columns
 //   warps 2, 3  O_tile = P V on alternate tiles, P from tensor memory, from zero in every tile
 //   warps 4-15  three softmax warpgroups on tiles in turn, thread = row.  Every tile is normalised by its own row
-//               maximum, so they carry nothing from tile to tile; the maximum is taken over the large half of the
-//               scores (any reference near it will do), then P = exp2(z - r)
+//               maximum, so they carry nothing from tile to tile: a pass over the scores for the maximum (over both halves
+//               of them: the small one grows with the scores, to hundreds at 1e5), then P = exp2(z - r)
 //   warps 16-19 add up: O = O 2^(m - m') + O_tile 2^(r - m'), l likewise; the row's output and lse
 //   tensor memory  buffer i at 128 i: S -> P_hi, small half of S -> P_lo; O_tile at 384 and 448
 // Two tiles in the softmax at a time are not enough to hide its latency; short rolled passes over the columns keep
@@ -285,11 +285,12 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll 1
                 for (int c0 = 0; c0 < BT64; c0 += CH) {
                     float z[CH], none[CH];
-                    uint32_t r[CH];
-                    tmem_ldn(t_s + c0, r);
+                    uint32_t hi[CH], lo[CH];
+                    tmem_ldn(t_s + c0, hi);
+                    tmem_ldn(t_s + 64u + c0, lo);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int k = 0; k < CH; ++k) z[k] = __uint_as_float(r[k]);
+                    for (int k = 0; k < CH; ++k) z[k] = __uint_as_float(hi[k]) + __uint_as_float(lo[k]);
                     if (SLOPE) score_tile<CAP, SLOPE, false, true, CH>(z, none, sc, row - key0 - c0, 0.f);   // else the maximum is at that of the product
                     mask(z, key0 + c0);
 #pragma unroll
@@ -298,6 +299,7 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 const bool none_read = top == -INFINITY;                // every P of this tile is zero
                 float ref = 0.f, sum = 0.f;
                 if (!none_read) ref = SLOPE ? top : CAP ? sc.to_log2 * tanh_any(top * sc.unit) : top * sc.unit;
+                const Reference rf = make_reference(ref, sc.slope2, abs(row - key0) + BT64);
 #pragma unroll 1
                 for (int c0 = 0; c0 < BT64; c0 += CH) {
                     float z[CH], none[CH];
@@ -307,7 +309,8 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     tmem_ld_wait();
 #pragma unroll
                     for (int k = 0; k < CH; ++k) z[k] = __uint_as_float(hi[k]) + __uint_as_float(lo[k]);
-                    score_tile<CAP, SLOPE, false, true, CH>(z, none, sc, row - key0 - c0, ref);
+                    score_tile<CAP, SLOPE, false, true, CH>(z, none, sc, row - key0 - c0, rf.now);
+                    less_reference(z, rf);
                     mask(z, key0 + c0);
 #pragma unroll
                     for (int k = 0; k < CH; ++k) {

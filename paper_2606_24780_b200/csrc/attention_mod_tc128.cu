@@ -273,24 +273,8 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
             tc_fence_after();
             const bool whole = s0 >= span.x && s0 + BT_ <= span.y;
             if (PASS == P_FWD) {
-                // the reference from the large half of the scores: any value near the maximum will do
+                // the reference from whole scores: the small half grows with them
                 float top = -INFINITY, sum = 0.f;
-#pragma unroll 1
-                for (int q = 0; q < 32; q += 16) {
-                    float z[16], none[16];
-                    uint32_t r[16];
-                    tmem_ldn(tb + q, r);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) z[i] = __uint_as_float(r[i]);
-                    if (SLOPE) score_tile<CAP, SLOPE, false, false, 16>(z, none, sc, own - s0 - q, 0.f);   // else the maximum is at that of the product
-                    const uint32_t bits = whole ? 0xffffu : column_bits<16>(span, s0 + q);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (bits >> i & 1u) top = fmaxf(top, z[i]);
-                }
-                const bool none_read = top == -INFINITY;                // every P of this tile is zero
-                const float ref = none_read ? 0.f : (CAP && !SLOPE) ? sc.to_log2 * tanh_any(top) : top;
 #pragma unroll 1
                 for (int q = 0; q < 32; q += 16) {
                     float z[16], none[16];
@@ -300,7 +284,26 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < 16; ++i) z[i] = __uint_as_float(hi[i]) + __uint_as_float(lo[i]);
-                    score_tile<CAP, SLOPE, false, false, 16>(z, none, sc, own - s0 - q, ref);
+                    if (SLOPE) score_tile<CAP, SLOPE, false, false, 16>(z, none, sc, own - s0 - q, 0.f);   // else the maximum is at that of the product
+                    const uint32_t bits = whole ? 0xffffu : column_bits<16>(span, s0 + q);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (bits >> i & 1u) top = fmaxf(top, z[i]);
+                }
+                const bool none_read = top == -INFINITY;                // every P of this tile is zero
+                const float ref = none_read ? 0.f : (CAP && !SLOPE) ? sc.to_log2 * tanh_any(top) : top;
+                const Reference rf = make_reference(ref, sc.slope2, abs(own - s0) + BT_);
+#pragma unroll 1
+                for (int q = 0; q < 32; q += 16) {
+                    float z[16], none[16];
+                    uint32_t hi[16], lo[16];
+                    tmem_ldn(tb + q, hi);
+                    tmem_ldn(tb + 32u + q, lo);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] = __uint_as_float(hi[i]) + __uint_as_float(lo[i]);
+                    score_tile<CAP, SLOPE, false, false, 16>(z, none, sc, own - s0 - q, rf.now);
+                    less_reference(z, rf);
                     const uint32_t bits = whole ? 0xffffu : column_bits<16>(span, s0 + q);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {

@@ -1,0 +1,97 @@
+"""The attention sublayer's operators where their arithmetic could give way: scores and biases far beyond a softmax's usual
+range, saturated caps, rows that overflow, very wide heads, span tables of another shape, empty arrays; and the device error word."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_24780_b200 import binding as b
+
+from gpu_util import DEV
+from test_attention_sublayer import A, TOL, Case, attention64, close, lib, rand, refused, see_matrix, spans_of, ways  # noqa: F401
+
+gpu = pytest.mark.gpu
+
+
+def given(qkv, d_o, B, T, H, d, cap=0.0, slopes=None, doc=None):
+    """A Case of these inputs; qkv [B * T, 3 H d]."""
+    case = Case.__new__(Case)
+    case.B, case.T, case.H, case.d, case.C = B, T, H, d, H * d
+    case.qkv, case.d_o, case.slopes = qkv.contiguous(), d_o.contiguous(), slopes
+    see = torch.tensor(see_matrix(doc, None, 0, B, T), device=DEV)
+    case.spans = None if doc is None else spans_of(doc, None, 0, B, T)
+    case.mod = b.make_attn_mod(cap, slopes, case.spans)
+    case.o, case.lse, case.grad, case.size = attention64(case.qkv.double().view(B, T, 3, H, d), see, cap,
+                                                         None if slopes is None else slopes.double(), case.d_o.double().view(B, T, H, d))
+    size = b.bt_op_attention_mod_scratch_bytes(B, T, case.C, H)
+    case.scratch = torch.full((size,), 255, dtype=torch.uint8, device=DEV)
+    return case
+
+
+# ------------------------------------------------------------------------------- scores beyond the usual range
+
+@gpu
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("T", [60, 270])
+@pytest.mark.parametrize("value", [150.06, 199.94])
+def test_equal_scores_of_a_hundred_thousand(d, T, value):
+    """All of q and k the same: every score is the same number, formed by the same operations, whatever its rounding, so every
+    key that is read weighs the same.  The values lie between two TF32 numbers, all on the same side: what the rounded
+    halves alone give is off by hundreds in the exponent."""
+    H = 2
+    qkv = rand(1, T, 3 * H * d)
+    qkv[:, :2 * H * d] = value
+    for cap in (0.0, 1e20):
+        case = given(qkv, rand(2, T, H * d), 1, T, H, d, cap)
+        for planes, flags in ways(d):
+            o, lse = case.forward(planes, flags)
+            assert close(o.view_as(case.o), case.o, TOL)
+            assert ((lse.double() - case.lse).abs() <= TOL * case.lse.abs()).all()
+            assert torch.isfinite(case.backward(planes, flags)).all()
+
+
+@gpu
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("scale", [100.0, 300.0, 1e6, 1e12])
+def test_random_scores_of_a_hundred_thousand_and_more(d, scale):
+    """One key takes the row: where its score leads by more than the scores' own errors, the row is that key's value.  An error
+    is below 48 * 2^-23 of sum_c |q_c k_c| / sqrt(d) (48 tensor-core additions for 128 columns); a lead of 17 more leaves the others
+    less than 1e-7 of the weight."""
+    H = 2
+    for T in (60, 270):
+        qkv = rand(3, T, 3 * H * d)
+        qkv[:, :2 * H * d] *= scale
+        x = qkv.double().view(T, 3, H, d).permute(1, 2, 0, 3)
+        q, k, v = x[0], x[1], x[2]
+        below = torch.tril(torch.ones(T, T, dtype=torch.bool, device=DEV))
+        s = (q @ k.transpose(1, 2) / math.sqrt(d)).masked_fill(~below, -math.inf)
+        off = 48 * 2.0 ** -23 * (q.abs() @ k.abs().transpose(1, 2) / math.sqrt(d)).amax(2)
+        two, at = s.topk(2, 2)
+        clear = two[..., 0] - two[..., 1] > 2 * off + 17
+        assert clear.double().mean() > 0.5
+        want = torch.gather(v, 1, at[..., :1].expand(-1, -1, d))
+        case = given(qkv, rand(4, T, H * d), 1, T, H, d)
+        for planes, flags in ways(d):
+            o, lse = case.forward(planes, flags)
+            o = o.view(T, H, d).permute(1, 0, 2).double()
+            assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+            assert close(o[clear], want[clear], TOL)
+            assert ((lse[0].double() - two[..., 0]).abs() <= off + 1)[clear].all()
+
+
+@gpu
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("slope", [1e4, -1e4, 1e7, -1e7, 1e12, -1e30])
+def test_biases_beyond_every_score(d, slope):
+    """A slope that outweighs all scores leaves each query its own key, a negative one the first key of the sequence.  The bias of
+    neighbouring keys differs by more than one rounding of the largest, so the weights are 0 and 1 in FP32 as well."""
+    H = 2
+    slopes = torch.full((H,), slope, device=DEV)
+    for T in (60, 270):
+        for cap in (0.0, 30.0):
+            case = given(rand(5, T, 3 * H * d), rand(6, T, H * d), 1, T, H, d, cap, slopes)
+            for planes, flags in ways(d):
+                o, lse = case.forward(planes, flags)
+                assert close(o.view_as(case.o), case.o, TOL)
+                assert torch.isfinite(lse).all()
