@@ -135,6 +135,15 @@ __device__ __forceinline__ int2 row_range(const int2* spans, int b, int T, int r
     return spans[(int64_t)b * T + row];
 }
 
+// The factor of a row's output and its lse, from its maximum (base 2) and sum.  A row that reads nothing has weight zero
+// and lse -inf; one whose scores left FP32's range is not a number in both, also if every one of them is -inf.
+__device__ __forceinline__ float row_factor(float l, int2 span) {
+    return l != 0.f ? 1.0f / l : span.x < span.y ? __int_as_float(0x7fffffff) : 0.f;
+}
+__device__ __forceinline__ float row_lse(float m, float l, int2 span) {
+    return l != 0.f ? (m + log2f(l)) * kLn2 : span.x < span.y ? __int_as_float(0x7fffffff) : -INFINITY;
+}
+
 // ---------------------------------------------------------------- pieces of the persistent kernels
 // One lane of a converged warp.  The issuing roles run on whole warps and put only the products behind this: the
 // compiler then keeps their descriptors in uniform registers, and an MMA is issued every 16 clocks at N = 32 and every 32 at N = 64,

@@ -284,9 +284,9 @@ __global__ void __launch_bounds__(kThreads, 2) fwd_kernel(const AttnModArgs g) {
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         l[r] = quad_sum(l[r]);
-        inv[r] = l[r] > 0.f ? 1.0f / l[r] : 0.f;             // a row that reads nothing is zero
+        inv[r] = row_factor(l[r], w.span[r]);
         const int row = r ? w.r1 : w.r0;
-        if (w.t4 == 0 && row < g.T) g.lse[w.stat + row] = l[r] > 0.f ? (m[r] + log2f(l[r])) * kLn2 : -INFINITY;
+        if (w.t4 == 0 && row < g.T) g.lse[w.stat + row] = row_lse(m[r], l[r], w.span[r]);
     }
     store<HD>(o, inv[0], inv[1], w.r0, w.r1, g.T, w.t4, (int64_t)w.b * g.T * g.C + (int64_t)w.h * HD, g.C, g.o, g.o_hi, g.o_lo);
 }

@@ -365,7 +365,8 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             }
             const int b = it.bh / g.H, h = it.bh % g.H, row = it.blk * BR + rloc;
             if (ok && row < g.T) {
-                const float inv = l > 0.f ? 1.0f / l : 0.f;             // a row that reads nothing is zero
+                const int2 span = l != 0.f ? make_int2(0, 0) : row_range(g.spans.k, b, g.T, row, false);
+                const float inv = row_factor(l, span);
                 const int64_t at = ((int64_t)b * g.T + row) * g.C + (int64_t)h * d;
 #pragma unroll
                 for (int q = 0; q < HD; q += 8) {
@@ -375,7 +376,7 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     for (int e = 0; e < 8; ++e) v[e] = acc[q + e] * inv;
                     store_sector(v, at + q, g.o, g.o_hi, g.o_lo);
                 }
-                g.lse[((int64_t)b * g.H + h) * g.T + row] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                g.lse[((int64_t)b * g.H + h) * g.T + row] = row_lse(m, l, span);
             }
         }
     }

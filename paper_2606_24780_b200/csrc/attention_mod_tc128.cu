@@ -398,7 +398,8 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
             const int wrow0 = r0 + lane_group * 32, nvalid = max(0, min(32, g.T - wrow0));
             const long long off = (long long)(row_base + wrow0) * args.out_stride + args.out_col + h * HD;
             float* tile = reinterpret_cast<float*>(smem_ptr(b1_s) + (uint32_t)lane_group * kRowTileBytes);
-            const float mul = PASS == P_FWD ? (l > 0.f ? 1.0f / l : 0.f) : args.out_mul;
+            const int2 span = PASS == P_FWD && l == 0.f ? row_range(g.spans.k, b, g.T, r0 + rloc, false) : make_int2(0, 0);
+            const float mul = PASS == P_FWD ? row_factor(l, span) : args.out_mul;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
 #pragma unroll
@@ -408,7 +409,7 @@ attn_mod128_kernel(const __grid_constant__ CUtensorMap tmA2, const __grid_consta
                                 args.out_stride, nullptr);
             }
             if (PASS == P_FWD && r0 + rloc < g.T)
-                g.lse[((int64_t)b * g.H + h) * g.T + r0 + rloc] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                g.lse[((int64_t)b * g.H + h) * g.T + r0 + rloc] = row_lse(m, l, span);
         }
     }
     tc_fence_before();

@@ -95,3 +95,24 @@ def test_biases_beyond_every_score(d, slope):
                 o, lse = case.forward(planes, flags)
                 assert close(o.view_as(case.o), case.o, TOL)
                 assert torch.isfinite(lse).all()
+
+
+@gpu
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("signs", [(1, 1), (1, -1), (0, 0)])
+def test_rows_out_of_fp32s_range_are_not_taken_for_rows_that_read_nothing(d, signs):
+    """q and k of 5e19: every product is beyond FP32 (to +inf, to -inf, or of either sign), so no score is a number.  The rows
+    that read them have no value; rows of padding, which read nothing, are zero with lse -inf as always."""
+    H = 2
+    for T in (60, 270):
+        qkv = rand(7, T, 3, H * d)
+        for part, sign in enumerate(signs):
+            size = 5e19 * (0.5 + torch.rand(T, H * d, generator=torch.Generator(DEV).manual_seed(8 + part), device=DEV))
+            qkv[:, part] = size * (sign or torch.sign(qkv[:, part]))
+        doc = np.zeros((1, T), np.int32)
+        doc[0, T // 2:] = -1
+        case = given(qkv.view(T, -1), rand(9, T, H * d), 1, T, H, d, doc=doc)
+        for planes, flags in ways(d):
+            o, lse = case.forward(planes, flags)
+            assert torch.isnan(lse[:, :, :T // 2]).all() and torch.isnan(o[:T // 2]).all()
+            assert (lse[:, :, T // 2:] == -math.inf).all()
