@@ -47,7 +47,8 @@ __device__ __forceinline__ Score make_score(float scale, float cap, const float*
 // otherwise they carry s.unit already.  |first - i| is the distance of position i; `grad` (GRAD and CAP) receives
 // 1 - tanh^2.  The exponential and the reciprocal of tanh run at an eighth of the rate of a multiplication and are
 // needed only where some score of the N is beyond 0.6 caps.  A distance is linear in i unless the row lies inside the N
-// positions (no integer conversion per element: it runs at an eighth of the rate too).  __fadd_rn: the same roundings
+// positions (no integer conversion per element: it runs at an eighth of the rate too); counted down to a position near
+// the row, a distance would keep the rounding of the far end, so there each is formed by itself.  __fadd_rn: the same roundings
 // whether ref is known to be zero or not (a sum fused with the bias's product would have another).
 template <bool CAP, bool SLOPE, bool GRAD, bool UNIT, int N>
 __device__ __forceinline__ void score_tile(float (&x)[N], float (&grad)[N], const Score& s, int first, float ref) {
@@ -74,7 +75,7 @@ __device__ __forceinline__ void score_tile(float (&x)[N], float (&grad)[N], cons
     const float scale = CAP ? s.to_log2 : s.unit;
     if (SLOPE) {
         const float d = (float)first;
-        if (first >= N - 1 || first <= 0) {
+        if (first >= 2 * N || first <= 0) {
             const float step = first <= 0 ? -s.slope2 : s.slope2, start = fmaf(-step, d, -ref);
 #pragma unroll
             for (int i = 0; i < N; ++i) {

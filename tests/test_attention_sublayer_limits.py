@@ -99,6 +99,21 @@ def test_biases_beyond_every_score(d, slope):
 
 @gpu
 @pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("slope", [100.0, 1e4, 1e7, 1e12])
+def test_a_steep_bias_leaves_the_own_key_its_score(d, slope):
+    """The distance to the own key is zero, and so is its bias, whatever the slope; the row's lse is that one score, and the
+    gradients are those of a query that reads a single key."""
+    H = 2
+    slopes = torch.full((H,), slope, device=DEV)
+    for T in (60, 270):
+        for cap in (0.0, 30.0):
+            case = given(rand(5, T, 3 * H * d), rand(6, T, H * d), 1, T, H, d, cap, slopes)
+            for planes, flags in ways(d):
+                case.check(planes, flags)
+
+
+@gpu
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
 @pytest.mark.parametrize("signs", [(1, 1), (1, -1), (0, 0)])
 def test_rows_out_of_fp32s_range_are_not_taken_for_rows_that_read_nothing(d, signs):
     """q and k of 5e19: every product is beyond FP32 (to +inf, to -inf, or of either sign), so no score is a number.  The rows
