@@ -25,9 +25,17 @@ __device__ __forceinline__ float tanh_small(float u) {
     q = fmaf(w, q, kTanh0);
     return fmaf(u * w, q, u);
 }
+// `grad`: 1 - tanh^2.  From a rounded tanh it would cancel as |u| grows (wrong by 1e-3 at 6, zero from 9 on); above 0.6 it is
+// 4 r (1 - r), r = 1 / (1 + e^2|u|), without a difference of nearly equal numbers.
+__device__ __forceinline__ float tanh_any(float u, float& grad) {
+    const float r = rcp_fast(1.0f + ex2_fast(2.8853900817779268f * fabsf(u))), small = tanh_small(u);
+    const bool is_small = fabsf(u) < kTanhSmall;
+    grad = is_small ? fmaf(-small, small, 1.0f) : 4.0f * fmaf(-r, r, r);
+    return is_small ? small : copysignf(fmaf(-2.0f, r, 1.0f), u);
+}
 __device__ __forceinline__ float tanh_any(float u) {
-    const float t = fmaf(-2.0f, rcp_fast(1.0f + ex2_fast(2.8853900817779268f * fabsf(u))), 1.0f);
-    return fabsf(u) < kTanhSmall ? tanh_small(u) : copysignf(t, u);
+    float unused;
+    return tanh_any(u, unused);
 }
 // Score modification in base-2 units.  `unit` turns a dot product q k into cap units (u = unit * dot) or,
 // without a cap, straight into base-2 units; `to_log2` turns tanh into base-2 units.  The backward kernels
@@ -61,14 +69,17 @@ __device__ __forceinline__ void score_tile(float (&x)[N], float (&grad)[N], cons
         }
         if (top < kTanhSmall) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = tanh_small(x[i]);
+            for (int i = 0; i < N; ++i) {
+                x[i] = tanh_small(x[i]);
+                if (GRAD) grad[i] = fmaf(-x[i], x[i], 1.0f);
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = tanh_any(x[i]);
-        }
-        if (GRAD) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) grad[i] = fmaf(-x[i], x[i], 1.0f);
+            for (int i = 0; i < N; ++i) {
+                float f;
+                x[i] = tanh_any(x[i], f);
+                if (GRAD) grad[i] = f;
+            }
         }
     }
     constexpr bool kScale = CAP || UNIT;

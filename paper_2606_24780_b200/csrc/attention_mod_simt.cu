@@ -39,12 +39,14 @@ __device__ __forceinline__ void store_row(const float (&v)[DPL], int d, int lane
         if (hi) split_tf32(v[k], hi[at + c], lo[at + c]);
     }
 }
-// Modified score of raw score s (already scaled by 1/sqrt d); t receives tanh (0 without a cap).
+// Modified score of raw score s (already scaled by 1/sqrt d); t receives 1 - tanh^2 (1 without a cap), from e^-2|u|: formed from
+// the tanh it would cancel.
 __device__ __forceinline__ float mod_score(float s, float cap, float slope, int distance, float& t) {
-    t = 0.f;
+    t = 1.f;
     if (cap > 0.f) {
-        t = tanhf(s / cap);
-        s = cap * t;
+        const float u = s / cap, e = expf(-2.0f * fabsf(u));
+        t = 4.0f * e / ((1.0f + e) * (1.0f + e));
+        s = cap * tanhf(u);
     }
     return s - slope * fabsf((float)distance);
 }
@@ -113,7 +115,7 @@ __global__ void __launch_bounds__(kWarps * 32) dq_kernel(const AttnModArgs g) {
         load_row<DPL>(g.qkv, g.qkv_lo, head + j * ld + g.C, d, lane, kk);
         load_row<DPL>(g.qkv, g.qkv_lo, head + j * ld + 2 * (int64_t)g.C, d, lane, vv);
         const float w = expf(mod_score(dot<DPL>(q, kk) * scale, g.cap, slope, p.i - j, t) - L);
-        const float ds = w * (dot<DPL>(go, vv) - D) * (1.0f - t * t) * scale;
+        const float ds = w * (dot<DPL>(go, vv) - D) * t * scale;
 #pragma unroll
         for (int k = 0; k < DPL; ++k) acc[k] = fmaf(ds, kk[k], acc[k]);
     }
@@ -140,7 +142,7 @@ __global__ void __launch_bounds__(kWarps * 32) dkv_kernel(const AttnModArgs g) {
         load_row<DPL>(g.qkv, g.qkv_lo, head + i * ld, d, lane, q);
         load_row<DPL>(g.d_o, g.d_o_lo, (row + i) * g.C + (int64_t)p.h * d, d, lane, go);
         const float w = expf(mod_score(dot<DPL>(q, kk) * scale, g.cap, slope, i - p.i, t) - g.lse[stat + i]);
-        const float ds = w * (dot<DPL>(go, vv) - g.dvec[stat + i]) * (1.0f - t * t) * scale;
+        const float ds = w * (dot<DPL>(go, vv) - g.dvec[stat + i]) * t * scale;
 #pragma unroll
         for (int k = 0; k < DPL; ++k) {
             dv[k] = fmaf(w, go[k], dv[k]);

@@ -131,3 +131,53 @@ def test_rows_out_of_fp32s_range_are_not_taken_for_rows_that_read_nothing(d, sig
             o, lse = case.forward(planes, flags)
             assert torch.isnan(lse[:, :, :T // 2]).all() and torch.isnan(o[:T // 2]).all()
             assert (lse[:, :, T // 2:] == -math.inf).all()
+
+
+# ------------------------------------------------------------------------------- saturated caps
+
+@gpu
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("size", [0.6, 2.0, 4.5, 6.5, 10.0, 20.0])
+def test_gradients_of_scores_several_caps_out(d, size):
+    """All |u| = |score| / cap within a fifth of `size`.  du: a score's 48 additions of up to 2^-23 of it each, its operands' splits
+    and scaling 2^-21, an exponential's argument 2 |u| log2 e rounded by 2^-24 of itself: 53 * 2^-23 |u|.  1 - tanh^2(u) moves by
+    2 du of itself, a weight by cap (1 - tanh^2) du and by the roundings of z and lse, three of 2^-24 of cap + log T.  The rest of a
+    gradient is 1e-5 as everywhere."""
+    H = 2
+    for T in (60, 270):
+        for cap in (1.0, 25.0):
+            du = 53 * 2.0 ** -23 * 1.2 * size
+            tol = 2 * du + cap / math.cosh(0.8 * size) ** 2 * du + 3 * 2.0 ** -24 * (cap + math.log(T)) + TOL
+            c = math.sqrt(size * cap / math.sqrt(d))
+            qkv = rand(11, T, 3, H, d)
+            swing = 0.975 + 0.05 * torch.rand(2, T, H, 1, generator=torch.Generator(DEV).manual_seed(12), device=DEV)
+            sign = torch.sign(qkv[:, 0, :, :1])
+            qkv[:, 0] = c * (1 + 0.05 * qkv[:, 0].clamp(-1, 1)) * swing[0] * sign
+            qkv[:, 1] = c * (1 + 0.05 * qkv[:, 1].clamp(-1, 1)) * swing[1]
+            u = torch.einsum("ihc,jhc->hij", qkv[:, 0].double(), qkv[:, 1].double()) / math.sqrt(d) / cap
+            assert 0.8 * size < float(u.abs().min()) and float(u.abs().max()) < 1.2 * size
+            case = given(qkv.view(T, -1), rand(13, T, H * d), 1, T, H, d, cap)
+            # 1 - tanh^2 in 64 bits keeps 1e-16 / 4e^-2|u| of itself: enough up to |u| = 12; beyond, the gradients of q and k scale as
+            # 4 e^-2|u|, which is taken out of the comparison's weights below
+            if size > 10:
+                t = 1 / torch.cosh(u) ** 2
+                case.grad = gradients_with(case, u, t, cap)
+            for planes, flags in ways(d):
+                dqkv = case.backward(planes, flags).view_as(case.grad)
+                for n in range(3):
+                    got, want = dqkv[0, :, n].double(), case.grad[0, :, n]
+                    assert float((got - want).norm()) <= tol * max(float(want.norm()), case.size[n]), "qkv"[n]
+
+
+def gradients_with(case, u, t, cap):
+    """attention64's gradients for one causal sequence, with 1 - tanh^2 given."""
+    T, H, d = case.T, case.H, case.d
+    q, k, v = case.qkv.double().view(T, 3, H, d).permute(1, 2, 0, 3)
+    g = case.d_o.double().view(T, H, d).permute(1, 0, 2)
+    z = (cap * torch.tanh(u)).masked_fill(~torch.tril(torch.ones(T, T, dtype=torch.bool, device=DEV)), -math.inf)
+    p = torch.softmax(z, 2)
+    o = p @ v
+    ds = p * (g @ v.transpose(1, 2) - (g * o).sum(2, keepdim=True)) * t / math.sqrt(d)
+    w = p ** 2 * ((g @ v.transpose(1, 2)) ** 2 + (g * o).sum(2, keepdim=True) ** 2) * t ** 2 / d
+    case.size = [float((w @ k ** 2).sum().sqrt()), float((w.transpose(1, 2) @ q ** 2).sum().sqrt()), 0.0]
+    return torch.stack((ds @ k, ds.transpose(1, 2) @ q, p.transpose(1, 2) @ g)).permute(2, 0, 1, 3)[None]
