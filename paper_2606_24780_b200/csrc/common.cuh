@@ -349,8 +349,9 @@ struct RopeArgs {
     int T, C, H, rot, interleaved;
     float sin_sign, mscale;
     float *y, *y_hi, *y_lo;
-    int rows;                   // set by the launcher: rows per CTA, reciprocals of the units per head
-    uint32_t m_head, m_pass;
+    struct Divisor { uint32_t m, s; };
+    int rows;                   // set by the launcher: rows per CTA, the units per head as divisors
+    Divisor head, pass;
     double turns[64];           // turns per position of each pair
 };
 cudaError_t launch_rope(RopeArgs g, cudaStream_t s);

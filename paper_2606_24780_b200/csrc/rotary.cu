@@ -20,8 +20,9 @@ constexpr int kThreads = 256;
 constexpr int kMaxRows = 8;      // rows of one CTA
 constexpr int kMaxPairs = 64;    // rot_dim / 2
 
-// q = n / d by multiplication: exact while n * d < 2^32 (m = ceil(2^32 / d), d >= 2; d = 1 has m = 0).
-__device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t m) { return m ? __umulhi(n, m) : n; }
+// n / d for n < 2^31 by multiplication: with 2^s < d <= 2^(s + 1), m = ceil(2^(32 + s) / d) has 32 bits, and its excess, below
+// 2^-(32 + s) n of a quotient, is less than the 1 / d that a quotient may be off.  A row has at most 2 C units, C <= 2^26.
+__device__ __forceinline__ uint32_t quotient(uint32_t n, const RopeArgs::Divisor& d) { return d.m ? __umulhi(n, d.m) >> d.s : n; }
 
 // A thread group of the CTA owns a row.  First the columns that only move (the values, the tails of partly rotated
 // heads), while the angles are formed; then the rotated ones.  Pieces are float4 (VEC) or single columns, kUnroll of them
@@ -64,7 +65,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs g) {
             for (int k = 0; k < kUnroll; ++k) {
                 const int u = t + k * group;
                 if (u < heads) {
-                    const uint32_t hd = quotient(u, g.m_pass);
+                    const uint32_t hd = quotient(u, g.pass);
                     at[k] = row + (int64_t)hd * d + g.rot + (u - (int)hd * pass) * W;
                 } else {
                     at[k] = row + 2 * (int64_t)g.C + (int64_t)(u - heads) * W;
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs g) {
 #pragma unroll
         for (int k = 0; k < kUnroll; ++k) {
             const int u = t + k * group;
-            const uint32_t hd = quotient(u, g.m_head);
+            const uint32_t hd = quotient(u, g.head);
             pair[k] = (u - (int)hd * per_head) * W;
             at[k] = row + (int64_t)hd * d + (g.interleaved ? 2 * pair[k] : pair[k]);
             if (u < total) {
@@ -132,9 +133,14 @@ cudaError_t launch_rope(RopeArgs g, cudaStream_t s) {
     const int64_t grid = (g.N + rows - 1) / rows;
     if (grid > 0x7fffffff) return cudaErrorInvalidValue;
     const int w = g.rot % 8 == 0 ? 4 : 1;
-    auto magic = [](int d) -> uint32_t { return d < 2 ? 0u : (uint32_t)((0x100000000ull + (uint64_t)d - 1) / (uint64_t)d); };
-    g.m_head = magic(g.rot / 2 / w);
-    g.m_pass = magic((g.C / g.H - g.rot) / w);
+    auto divisor = [](uint32_t d) -> RopeArgs::Divisor {
+        if (d < 2) return {0u, 0u};
+        uint32_t s = 0;
+        while ((2u << s) < d) ++s;
+        return {(uint32_t)(((0x100000000ull << s) + d - 1) / d), s};
+    };
+    g.head = divisor(g.rot / 2 / w);
+    g.pass = divisor((g.C / g.H - g.rot) / w);
     if (g.rot % 8 == 0) BT_KERNEL_LAUNCH((rope_kernel<true>), (unsigned)grid, kThreads, 0, s, g);
     else BT_KERNEL_LAUNCH((rope_kernel<false>), (unsigned)grid, kThreads, 0, s, g);
     BT_COUNT_LAUNCH();

@@ -181,3 +181,28 @@ def gradients_with(case, u, t, cap):
     w = p ** 2 * ((g @ v.transpose(1, 2)) ** 2 + (g * o).sum(2, keepdim=True) ** 2) * t ** 2 / d
     case.size = [float((w @ k ** 2).sum().sqrt()), float((w.transpose(1, 2) @ q ** 2).sum().sqrt()), 0.0]
     return torch.stack((ds @ k, ds.transpose(1, 2) @ q, p.transpose(1, 2) @ g)).permute(2, 0, 1, 3)[None]
+
+
+# ------------------------------------------------------------------------------- rotary positions of wide heads
+
+@gpu
+@pytest.mark.parametrize("H,d,rot,inter", [
+    (1, 65532, 4, False), (1, 65536, 2, True), (32, 16380, 2, False), (8192, 1000, 6, False), (1, 1 << 20, 8, True), (3, 1 << 20, 8, False),
+    (1 << 15, 128, 128, False), (1, 1 << 26, 8, False)])
+def test_rope_of_heads_hardly_turned(H, d, rot, inter):
+    """Every column is written once, from its own place, however many there are: none of y's old contents stay, and what does not turn
+    is copied bit for bit."""
+    C, N = H * d, 2 if H * d < 1 << 24 else 1
+    x = rand(1, N, 3 * C)
+    pos = torch.tensor([5, 1 << 20][:N], dtype=torch.int32, device=DEV)
+    y = torch.full_like(x, math.nan)
+    b.bt_op_rope_fwd(x, pos, N, 1, C, H, b.make_rope(rot, inter), y)
+    got, was = y.view(N, 3, H, d), x.view(N, 3, H, d)
+    assert torch.equal(got[:, 2], was[:, 2]) and torch.equal(got[:, :2, :, rot:], was[:, :2, :, rot:])
+    for i in range(rot // 2):
+        u, w = (2 * i, 2 * i + 1) if inter else (i, i + rot // 2)
+        a = pos.double() * 10000.0 ** (-2.0 * i / rot)
+        c, s = torch.cos(a)[:, None, None], torch.sin(a)[:, None, None]
+        p, q = was[:, :2, :, u].double(), was[:, :2, :, w].double()
+        off = 8 * 2.0 ** -24 * (p.abs() + q.abs())      # two products and a sum, sine and cosine within 2^-22
+        assert ((got[:, :2, :, u] - (p * c - q * s)).abs() <= off).all() and ((got[:, :2, :, w] - (p * s + q * c)).abs() <= off).all()
