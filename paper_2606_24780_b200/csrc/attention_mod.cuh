@@ -129,7 +129,8 @@ __device__ __forceinline__ void less_reference(float (&z)[N], const Reference& r
     }
 }
 
-// Rows [lo, hi) that `rows` own rows from r0 on have to walk (64-row blocks; without spans: causal).
+// Rows [lo, hi) that `rows` own rows from r0 on have to walk (64-row blocks; without spans: causal).  Whatever the table
+// holds -- it may have been built for other lengths -- a walk stays inside the sequence.
 __device__ __forceinline__ int2 block_range(const int2* blocks, int b, int T, int r0, int rows, bool keys) {
     if (!blocks) return keys ? make_int2(r0, T) : make_int2(0, min(r0 + rows, T));
     const int nb = (T + 63) >> 6;
@@ -138,13 +139,14 @@ __device__ __forceinline__ int2 block_range(const int2* blocks, int b, int T, in
         const int2 v = blocks[(int64_t)b * nb + k];
         if (v.x < v.y) u = make_int2(min(u.x, v.x), max(u.y, v.y));
     }
-    return u.y ? u : make_int2(0, 0);
+    return make_int2(max(min(u.x, T), 0), max(min(u.y, T), 0));
 }
-// The range of one own row; empty past the end of the sequence.
+// The range of one own row, inside the sequence too; empty past its end.
 __device__ __forceinline__ int2 row_range(const int2* spans, int b, int T, int row, bool keys) {
     if (row >= T) return make_int2(0, 0);
     if (!spans) return keys ? make_int2(row, T) : make_int2(0, row + 1);
-    return spans[(int64_t)b * T + row];
+    const int2 s = spans[(int64_t)b * T + row];
+    return make_int2(max(s.x, 0), min(s.y, T));
 }
 
 // The factor of a row's output and its lse, from its maximum (base 2) and sum.  A row that reads nothing has weight zero

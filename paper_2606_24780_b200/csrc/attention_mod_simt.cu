@@ -4,7 +4,7 @@
 // textbook two-pass softmax, deliberately not the one-pass recurrence of the fast kernels.
 //     z_ij = c tanh(q_i k_j / (c sqrt d)) - slope |i - j|     (c = 0: z_ij = q_i k_j / sqrt d - slope |i - j|)
 //     dz_ij / d(q_i k_j) = (1 - tanh^2) / sqrt d
-#include "common.cuh"
+#include "attention_mod.cuh"
 
 namespace bt {
 
@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kWarps * 32) fwd_kernel(const AttnModArgs g) {
     const int lane = threadIdx.x & 31, d = g.C / g.H;
     const float scale = 1.0f / sqrtf((float)d), slope = g.slopes ? g.slopes[p.h] : 0.f;
     const int64_t ld = 3 * (int64_t)g.C, head = (int64_t)p.b * g.T * ld + (int64_t)p.h * d;
-    const int2 span = g.spans.k ? g.spans.k[(int64_t)p.b * g.T + p.i] : make_int2(0, p.i + 1);
+    const int2 span = mod::row_range(g.spans.k, p.b, g.T, p.i, false);
     float q[DPL], kv[DPL], acc[DPL], t;
     load_row<DPL>(g.qkv, g.qkv_lo, head + p.i * ld, d, lane, q);
     float mx = -INFINITY, l = 0.f;
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kWarps * 32) dq_kernel(const AttnModArgs g) {
     const int lane = threadIdx.x & 31, d = g.C / g.H;
     const float scale = 1.0f / sqrtf((float)d), slope = g.slopes ? g.slopes[p.h] : 0.f;
     const int64_t ld = 3 * (int64_t)g.C, row = (int64_t)p.b * g.T, head = row * ld + (int64_t)p.h * d;
-    const int2 span = g.spans.k ? g.spans.k[row + p.i] : make_int2(0, p.i + 1);
+    const int2 span = mod::row_range(g.spans.k, p.b, g.T, p.i, false);
     float q[DPL], go[DPL], kk[DPL], vv[DPL], acc[DPL], t;
     load_row<DPL>(g.qkv, g.qkv_lo, head + p.i * ld, d, lane, q);
     load_row<DPL>(g.d_o, g.d_o_lo, (row + p.i) * g.C + (int64_t)p.h * d, d, lane, go);
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(kWarps * 32) dkv_kernel(const AttnModArgs g) {
     const float scale = 1.0f / sqrtf((float)d), slope = g.slopes ? g.slopes[p.h] : 0.f;
     const int64_t ld = 3 * (int64_t)g.C, row = (int64_t)p.b * g.T, head = row * ld + (int64_t)p.h * d;
     const int64_t stat = ((int64_t)p.b * g.H + p.h) * g.T;
-    const int2 span = g.spans.q ? g.spans.q[row + p.i] : make_int2(p.i, g.T);
+    const int2 span = mod::row_range(g.spans.q, p.b, g.T, p.i, true);
     float q[DPL], go[DPL], kk[DPL], vv[DPL], dk[DPL], dv[DPL], t;
     load_row<DPL>(g.qkv, g.qkv_lo, head + p.i * ld + g.C, d, lane, kk);
     load_row<DPL>(g.qkv, g.qkv_lo, head + p.i * ld + 2 * (int64_t)g.C, d, lane, vv);

@@ -206,3 +206,30 @@ def test_rope_of_heads_hardly_turned(H, d, rot, inter):
         p, q = was[:, :2, :, u].double(), was[:, :2, :, w].double()
         off = 8 * 2.0 ** -24 * (p.abs() + q.abs())      # two products and a sum, sine and cosine within 2^-22
         assert ((got[:, :2, :, u] - (p * c - q * s)).abs() <= off).all() and ((got[:, :2, :, w] - (p * s + q * c)).abs() <= off).all()
+
+
+# ------------------------------------------------------------------------------- span tables of another shape
+
+@gpu
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+def test_spans_of_another_shape_reach_no_other_sequence(d):
+    """A table of 2 x 512 positions has the size of one of 4 x 256 or 8 x 128, and its ranges go past their ends.  What a row reads
+    that way is not specified, but it lies inside its sequence: the last sequence's outputs do not change with the others'
+    contents, and the call ends.  Tables of arbitrary numbers likewise."""
+    H = 2
+    wrong = spans_of(None, None, 0, 2, 512)
+    noise = torch.randint(-2 ** 31, 2 ** 31 - 1, (wrong.numel() // 4,), generator=torch.Generator(DEV).manual_seed(14), dtype=torch.int32, device=DEV)
+    small = torch.randint(-600, 600, noise.shape, generator=torch.Generator(DEV).manual_seed(15), dtype=torch.int32, device=DEV)
+    for B, T in ((4, 256), (8, 128), (3, 100), (2, 333)):
+        for table in (wrong, noise.view(torch.uint8), small.view(torch.uint8)):
+            case = given(rand(16, B * T, 3 * H * d), rand(17, B * T, H * d), B, T, H, d)
+            case.mod = b.make_attn_mod(20.0, None, table)
+            for planes, flags in ways(d):
+                got = [t.clone() for t in (*case.forward(planes, flags), case.backward(planes, flags))]
+                was = case.qkv.clone()
+                case.qkv[:(B - 1) * T] = rand(18, (B - 1) * T, 3 * H * d)
+                again = (*case.forward(planes, flags), case.backward(planes, flags))
+                case.qkv = was
+                for x, y in zip(got, again):
+                    x, y = x.reshape(B, -1)[-1], y.reshape(B, -1)[-1]
+                    assert torch.equal(torch.nan_to_num(x, 0.0, 1.0, -1.0), torch.nan_to_num(y, 0.0, 1.0, -1.0))
