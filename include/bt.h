@@ -586,9 +586,10 @@ typedef struct {
  * in scratch, one pass more); d < 64 with T d <= 4096 runs on warp-level MMA and reads raw arrays if it can, and
  * BT_FLAG_ATTN_SIMT in plain FP32.  No output may overlap an input.
  * Every row of the inputs must be finite, those behind the mask too (they enter the tensor-core products
- * with weight zero).  Scores and biases may be of any size that FP32 holds; the backward forms its weights from lse, in
- * FP32 too, so a weight there is off by 2^-22 of its row's largest |z|: keep |z| below 1e4 where gradients matter, and below
- * 2^28.  A row whose scores are not (products beyond FP32) is not a number in o and lse.  At most 2^21 positions, 2^30 rows, 2^24 sequence-heads, 2^33 row-heads.
+ * with weight zero).  Scores and biases may be of any size that FP32 holds; a row whose scores are beyond it is not
+ * a number in o and lse.  The backward forms its weights from lse, in FP32 too, so a weight there is off by 2^-22 of its
+ * row's largest |z|: keep |z| below 1e4 where gradients matter, and below 2^28.
+ * At most 2^21 positions, 2^30 rows, 2^24 sequence-heads, 2^33 row-heads; 128-wide heads on tcgen05 with 3 C below 2^31.
  * The backward takes the forward's inputs, o (raw) and lse and overwrites all of dqkv:
  *     dv_j = sum_i p_ij do_i,  ds_ij = p_ij (do_i v_j - do_i o_i) (1 - tanh^2),
  *     dq_i = sum_j ds_ij k_j / sqrt(d),  dk_j = sum_i ds_ij q_i / sqrt(d),

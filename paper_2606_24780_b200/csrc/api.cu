@@ -1555,8 +1555,10 @@ bt_status attn_mod_args(AttnModArgs& g, const char* who, int32_t B, int32_t T, i
     return BT_OK;
 }
 
-// After the checks of arguments, which need no driver.
-bt_status attn_mod_ready(const char* who, uint32_t flags) {
+// After the checks of arguments, which need no driver.  The 128-wide tensor-core kernels count a row's columns in 32 bits.
+bt_status attn_mod_ready(const char* who, const AttnModArgs& g, uint32_t flags) {
+    if (!(flags & BT_FLAG_ATTN_SIMT) && g.C / g.H == 128 && 3 * (int64_t)g.C > INT32_MAX)
+        return fail(BT_ERR_UNSUPPORTED, "%s: rows of more than 2^31 columns", who);
     char msg[256];
     if (!(flags & BT_FLAG_ATTN_SIMT) && !gemm_tc_init(msg, sizeof(msg)))
         return fail(BT_ERR_CUDA, "%s: tensor-core attention unavailable: %s", who, msg);
@@ -1618,7 +1620,7 @@ extern "C" bt_status bt_op_attention_mod_fwd(const float* qkv, const float* qkv_
     g.o = o; g.o_hi = o_split; g.o_lo = o_split ? o_split + (int64_t)B * T * C : nullptr;
     g.lse = lse;
     cudaStream_t s = (cudaStream_t)stream;
-    if (bt_status st = attn_mod_ready("attention_mod_fwd", flags)) return st;
+    if (bt_status st = attn_mod_ready("attention_mod_fwd", g, flags)) return st;
     BT_CUDA(launch_attention_mod_fwd(g, (flags & BT_FLAG_ATTN_SIMT) != 0, s));
     return BT_OK;
 }
@@ -1644,7 +1646,7 @@ extern "C" bt_status bt_op_attention_mod_bwd(const float* qkv, const float* qkv_
     g.lse = const_cast<float*>(lse);
     g.dqkv = dqkv; g.dqkv_hi = dqkv_split; g.dqkv_lo = dqkv_split ? dqkv_split + n * 3 * C : nullptr;
     cudaStream_t s = (cudaStream_t)stream;
-    if (bt_status st = attn_mod_ready("attention_mod_bwd", flags)) return st;
+    if (bt_status st = attn_mod_ready("attention_mod_bwd", g, flags)) return st;
     BT_CUDA(launch_attention_mod_bwd(g, (flags & BT_FLAG_ATTN_SIMT) != 0, s));
     return BT_OK;
 }

@@ -29,6 +29,17 @@ def given(qkv, d_o, B, T, H, d, cap=0.0, slopes=None, doc=None):
     return case
 
 
+# ------------------------------------------------------------------------------- CPU: refusals
+
+def test_rows_of_more_than_two_to_the_31_columns_are_refused(lib):
+    """128-wide heads, on tcgen05: the columns of a row are counted in 32 bits there."""
+    H = (1 << 31) // (3 * 128) + 1
+    for heads in (H, 1 << 23):
+        refused(2, b.bt_op_attention_mod_fwd, A, None, 1, 1, 128 * heads, heads, b.make_attn_mod(), 2 * A, None, 3 * A, 4 * A, 1 << 62)
+        refused(2, b.bt_op_attention_mod_bwd, A, None, 2 * A, 3 * A, 4 * A, None, 1, 1, 128 * heads, heads, b.make_attn_mod(), 5 * A, None,
+                6 * A, 1 << 62)
+
+
 # ------------------------------------------------------------------------------- scores beyond the usual range
 
 @gpu
