@@ -540,6 +540,7 @@ BT_API bt_status bt_op_attention_bwd(const float* qkv, const float* qkv_split, c
  * needs no scaling kind).  mscale multiplies the rotated columns (1 = a pure rotation).
  * 2 <= rot_dim <= min(d, 128), even.  Angles are reduced in 64 bits, so positions anywhere in int32
  * keep the accuracy of small ones.
+ *   x        N = 0 is nothing to do, the arrays may be NULL then
  *   pos      int32 [N] (nullable: row n has position n mod T; packed documents restart theirs)
  *   y        [N, 3C], may be x itself (then only the rotated columns are touched; not with y_split)
  *   y_split  [2][N][3C] hi/lo planes, as the attention kernels read them; y or y_split may be NULL
@@ -614,7 +615,7 @@ BT_API bt_status bt_op_attention_mod_check(const void* scratch, void* stream);
  * number); off = offset + *d_step (d_step: device, 8-byte aligned, nullable: lets a captured step draw a new
  * mask at every replay).  Give every call site and step its own offset.  A dropped element is zero
  * whatever x holds there.  bt_op_dropout_bwd forms dx_i = keep_i dy_i / (1 - p) with the same seed and offset; the
- * residual's gradient is dy itself.  Any n >= 0; planes (y_split [2][n]) need n % 4 == 0; y may be x or residual. */
+ * residual's gradient is dy itself.  Any n >= 0 (0: the arrays may be NULL); planes (y_split [2][n]) need n % 4 == 0; y may be x or residual. */
 BT_API bt_status bt_op_dropout_fwd(const float* x, const float* residual, int64_t n, double p, uint64_t seed,
                                    uint64_t offset, float* y, float* y_split, const uint64_t* d_step, void* stream);
 BT_API bt_status bt_op_dropout_bwd(const float* dy, int64_t n, double p, uint64_t seed, uint64_t offset, float* dx,

@@ -1486,15 +1486,16 @@ bt_status rope_turns(const bt_rope_config* r, int32_t d, double* turns) {
 
 bt_status rope_impl(const float* x, const int32_t* pos, int64_t N, int32_t T, int32_t C, int32_t H, const bt_rope_config* rope,
                     float* y, float* y_split, float sign, void* stream) {
-    BT_PTR(x); BT_OPT_PTR(pos); BT_OPT_PTR(y); BT_OPT_PTR(y_split);
-    if (!y && !y_split) return fail(BT_ERR_INVALID_ARG, "rope: no output requested");
+    if (N != 0) BT_PTR(x);              // an empty array may have no address
+    BT_OPT_PTR(x); BT_OPT_PTR(pos); BT_OPT_PTR(y); BT_OPT_PTR(y_split);
+    if (N != 0 && !y && !y_split) return fail(BT_ERR_INVALID_ARG, "rope: no output requested");
     if (N < 0 || T < 1 || C < 1 || H < 1 || C % H || C > (1 << 26)) return fail(BT_ERR_INVALID_ARG, "rope: bad sizes");
     if ((C / H) % 4) return fail(BT_ERR_INVALID_ARG, "rope: head_dim %d is not a multiple of 4", C / H);
     RopeArgs g{};
     if (bt_status st = rope_turns(rope, C / H < 128 ? C / H : 128, g.turns)) return st;
+    if (N == 0) return BT_OK;
     if (y_split && (y_split == x || y_split + N * 3 * (int64_t)C == x)) return fail(BT_ERR_INVALID_ARG, "rope: planes cannot be written over the input");
     if (y == x && y_split) return fail(BT_ERR_INVALID_ARG, "rope: in place only without planes");
-    if (N == 0) return BT_OK;
     g.x = x; g.pos = pos; g.N = N; g.T = T; g.C = C; g.H = H;
     g.rot = rope->rot_dim; g.interleaved = rope->interleaved != 0;
     g.sin_sign = sign; g.mscale = rope->mscale;
@@ -1505,9 +1506,10 @@ bt_status rope_impl(const float* x, const int32_t* pos, int64_t N, int32_t T, in
 
 bt_status dropout_impl(const float* x, const float* residual, int64_t n, double p, uint64_t seed, uint64_t offset, float* y,
                        float* y_split, const uint64_t* d_step, void* stream) {
-    BT_PTR(x); BT_OPT_PTR(residual); BT_OPT_PTR(y); BT_OPT_PTR(y_split);
+    if (n != 0) BT_PTR(x);              // an empty array may have no address
+    BT_OPT_PTR(x); BT_OPT_PTR(residual); BT_OPT_PTR(y); BT_OPT_PTR(y_split);
     if (reinterpret_cast<uintptr_t>(d_step) & 7u) return fail(BT_ERR_INVALID_ARG, "dropout: d_step is not 8-byte aligned");
-    if (!y && !y_split) return fail(BT_ERR_INVALID_ARG, "dropout: no output requested");
+    if (n != 0 && !y && !y_split) return fail(BT_ERR_INVALID_ARG, "dropout: no output requested");
     if (n < 0 || n > ((int64_t)1 << 42)) return fail(BT_ERR_INVALID_ARG, "dropout: bad size");
     if (y_split && n % 4) return fail(BT_ERR_INVALID_ARG, "dropout: planes need n %% 4 == 0");
     if (!(p >= 0.0 && p < 1.0)) return fail(BT_ERR_INVALID_ARG, "dropout: p must lie in [0, 1)");

@@ -40,6 +40,20 @@ def test_rows_of_more_than_two_to_the_31_columns_are_refused(lib):
                 6 * A, 1 << 62)
 
 
+def test_empty_arrays_without_an_address(lib):
+    """An empty tensor's address is NULL: with nothing to do, that is no error."""
+    none = torch.empty(0)
+    assert none.data_ptr() == 0
+    cfg = b.make_rope(64)
+    for call in (b.bt_op_rope_fwd, b.bt_op_rope_bwd):
+        call(None, None, 0, 4, 768, 12, cfg, None, stream=0)
+        refused(1, call, A + 4, None, 0, 4, 768, 12, cfg, None)
+        refused(1, call, None, None, 0, 4, 768, 7, cfg, None)
+    b.bt_op_dropout_fwd(None, None, 0, 0.1, 1, 2, None, stream=0)
+    b.bt_op_dropout_bwd(None, 0, 0.1, 1, 2, None, stream=0)
+    refused(1, b.bt_op_dropout_bwd, None, 0, 1.0, 1, 2, None)
+
+
 # ------------------------------------------------------------------------------- scores beyond the usual range
 
 @gpu
