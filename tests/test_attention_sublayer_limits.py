@@ -9,7 +9,7 @@ import torch
 from paper_2606_24780_b200 import binding as b
 
 from gpu_util import DEV
-from test_attention_sublayer import A, TOL, Case, attention64, close, lib, rand, refused, see_matrix, spans_of, ways  # noqa: F401
+from test_attention_sublayer import A, TOL, Case, attention64, close, lib, planes_of, rand, random_layout, refused, see_matrix, spans_of, ways  # noqa: F401
 
 gpu = pytest.mark.gpu
 
@@ -258,3 +258,56 @@ def test_spans_of_another_shape_reach_no_other_sequence(d):
                 for x, y in zip(got, again):
                     x, y = x.reshape(B, -1)[-1], y.reshape(B, -1)[-1]
                     assert torch.equal(torch.nan_to_num(x, 0.0, 1.0, -1.0), torch.nan_to_num(y, 0.0, 1.0, -1.0))
+
+
+# ------------------------------------------------------------------------------- the error word, gradients as differences
+
+@gpu
+@pytest.mark.parametrize("d,T", [(16, 60), (16, 300), (32, 200), (64, 200), (128, 140)])
+def test_the_error_word_is_reported_and_cleared(d, T):
+    """A word left in the scratch as a wait that ran out leaves it is an error with that code; every kernel family's forward and
+    backward begin with a clear one."""
+    case = Case(2, T, 2, d, mean=50, cap=30.0)
+    B, C, H = case.B, case.C, case.H
+    o, lse, dqkv = torch.empty(B * T, C, device=DEV), torch.empty(B, H, T, device=DEV), torch.empty(B * T, 3 * C, device=DEV)
+    o_in, lse_in = case.o.reshape(B * T, C).float().contiguous(), case.lse.float().contiguous()
+    word = case.scratch[:4].view(torch.int32)
+    for planes, flags in ways(d):
+        forms = [(None, planes_of(t)) if planes else (t, None) for t in (case.qkv, case.d_o)]
+        for call in (lambda: b.bt_op_attention_mod_fwd(*forms[0], B, T, C, H, case.mod, o, None, lse, case.scratch, case.scratch.numel(), flags),
+                     lambda: b.bt_op_attention_mod_bwd(*forms[0], o_in, lse_in, *forms[1], B, T, C, H, case.mod, dqkv, None, case.scratch,
+                                                       case.scratch.numel(), flags)):
+            word.fill_(4711)
+            with pytest.raises(b.BtError, match="4711") as e:
+                b.bt_op_attention_mod_check(case.scratch)
+            assert b.STATUS[e.value.status] == "BT_ERR_DEVICE_TIMEOUT"
+            call()
+            b.bt_op_attention_mod_check(case.scratch)
+            assert int(word) == 0
+
+
+@gpu
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("mod", [dict(), dict(mean=60, prefix=10, cap=5.0, slope=True), dict(cap=1.0, scale=1.5), dict(window=20, slope=True)])
+def test_gradients_against_differences_of_the_definition(d, mod):
+    """The gradient along u, against (f(x + h u) - f(x - h u)) / 2h of f = sum(o * g) in 64 bits: no gradient formula on that side.
+    With h = 2^-12 and scores of a few units the cubic term is below 1e-6 of the derivative's scale, and 64-bit rounding
+    below 1e-16 * |f| / h.  A gradient off by 1e-5 of its norm moves the derivative along a normal u by that times a
+    normal number: six of them at most."""
+    mod = dict(mod)
+    case = Case(1, 150, 2, d, **mod)
+    B, T, H = case.B, case.T, case.H
+    slopes = None if case.slopes is None else case.slopes.double()
+    if "mean" in mod:
+        doc, mark = random_layout(np.random.default_rng(7 * T), B, T, mod["mean"], 0, mod["prefix"])       # the Case's own
+        see = see_matrix(doc, mark, 0, B, T)
+    else:
+        see = see_matrix(None, None, mod.get("window", 0), B, T)
+    see = torch.tensor(see, device=DEV)
+    x, g, h = case.qkv.double().view(B, T, 3, H, d), case.d_o.double().view(B, T, H, d), 2.0 ** -12
+    for seed in range(3):
+        u = torch.randn(x.shape, generator=torch.Generator(DEV).manual_seed(20 + seed), device=DEV, dtype=torch.float64)
+        f = [float((attention64(x + sign * h * u, see, mod.get("cap", 0.0), slopes)[0] * g).sum()) for sign in (1.0, -1.0)]
+        for planes, flags in ways(d):
+            grad = case.backward(planes, flags).double().view(x.shape)
+            assert abs(float((grad * u).sum()) - (f[0] - f[1]) / (2 * h)) <= 6 * TOL * float(grad.norm())
