@@ -538,9 +538,10 @@ BT_API bt_status bt_op_attention_bwd(const float* qkv, const float* qkv_split, c
  * clamp((original_len * theta / 2 pi - low) / (high - low), 0, 1): pairs that turn more than `high`
  * times over the original length keep their speed, those below `low` are stretched (another `base`
  * needs no scaling kind).  mscale multiplies the rotated columns (1 = a pure rotation).
- * 2 <= rot_dim <= min(d, 128), even.  Angles are reduced in 64 bits, so positions anywhere in int32
- * keep the accuracy of small ones.
- *   x        N = 0 is nothing to do, the arrays may be NULL then
+ * 2 <= rot_dim <= min(d, 128), even.  Angles are reduced in 64 bits: positions up to 2^28
+ * keep the accuracy of small ones, and at the ends of int32 an angle is off by some 3e-7 radian.
+ * C <= 2^26.
+ *   x        [N, 3C]; N = 0 is nothing to do, the arrays may be NULL then
  *   pos      int32 [N] (nullable: row n has position n mod T; packed documents restart theirs)
  *   y        [N, 3C], may be x itself (then only the rotated columns are touched; not with y_split)
  *   y_split  [2][N][3C] hi/lo planes, as the attention kernels read them; y or y_split may be NULL

@@ -22,8 +22,10 @@ namespace {
 // launch.  The warp-level ones start at once, but take three times as long per score.  16 heads of 32, cap:
 //     T 128, batch 64    forward 59 us warp-level, 57 us tcgen05;   gradients 203, 168
 //     T 2,000, batch 4   481, 192;   1,561, 532
-// and of 16 columns, zeros in half of the tcgen05 tiles: T 256, batch 32    52, 52;   161, 166.  Hence T d > 4,096.  Wider
-// heads always: one raw sequence of 64, 12 heads of 64, took 10 us warp-level and 15 so forward, 46 and 24 backward.
+// and of 16 columns, zeros in half of the tcgen05 tiles: T 256, batch 32    52, 52;   161, 166.  Hence T d > 4,096: at 4,096
+// itself heads of 16 are 3 % better off on the warp-level kernels and heads of 32 up to a fifth worse, below it
+// (T 64, heads of 32: forward 43, 64, gradients 138, 198) the former win.  Wider heads always: one raw sequence of 64, 12 heads of
+// 64, took 10 us warp-level and 15 so forward, 46 and 24 backward.
 bool on_tcgen05(const AttnModArgs& g) { return attn_mod_wants_planes(g.T, g.C / g.H) || !attention_mod_mma_supports(g); }
 
 // Up to two arrays into planes in one launch; x.n4 and y.n4 float4 values (a launch costs as much as 3 MB of copying).

@@ -12,7 +12,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 // tanh for the cap.  A capped score is cap * tanh(u), u = score / cap: for the usual small u its error
 // has to be relative to u, so below 0.6 an odd polynomial is used (least-squares fit of (tanh(u)/u - 1) / u^2
-// reweighted to the smallest largest relative error, 2.8e-9, one FP32 rounding in all); above,
+// reweighted to the smallest largest relative error, 4.7e-9, a tenth of an FP32 rounding); above,
 // 1 - 2 / (1 + e^2|u|), which is good to 2^-22 there.
 constexpr float kTanhSmall = 0.6f;
 constexpr float kTanh0 = -0.33333298563957214f, kTanh1 = 0.13331924378871918f, kTanh2 = -0.053783830255270004f,

@@ -10,7 +10,8 @@
 //   dq       rows = queries; also D = rowsum(dO o O), which dkv reads
 //   dkv      rows = keys
 // Bound by issue: the splits in front of the products and the score function, on top of the legacy tensor pipe
-// (gradients at 2,000 positions: pipe 47 % busy, 2.0 instructions a clock).  They serve calls that are over before that counts.
+// (gradients at 2,000 positions: pipe 47 % busy, 2.0 instructions a clock; 64 sequences of 128, 16 heads of 32: 31 %, 1.5 to 1.9, forward
+// 61 us, gradients 203).  They serve calls that are over before that counts.
 #include "attention_mod.cuh"
 
 namespace bt {

@@ -77,8 +77,10 @@ __device__ __forceinline__ void settle() {
 //   tensor memory  buffer i at 128 i: S -> P_hi, small half of S -> P_lo; O_tile at 384 and 448
 // Two tiles in the softmax at a time are not enough to hide its latency; short rolled passes over the columns keep
 // the code in the instruction cache (32 columns unrolled cost a third more time than 16).
-// 8 packed sequences of 1,024, 12 heads, distance bias: 69 us, tensor pipe 40 % busy; the products of a tile are 1,664 clocks, the
-// element-wise warps, at 1.7 to 2.1 instructions a clock of all four schedulers, need 2,700 with a cap.
+// 8 packed sequences of 1,024, 12 heads, distance bias: 71 us, tensor pipe 39 % busy; the products of a tile are 1,664 clocks, the
+// element-wise warps, at 1.7 to 2.1 instructions a clock of all four schedulers, need about 2,800 with a cap.  The maximum from
+// whole scores costs 3 % (433 -> 448 us at 8,192 positions, causal); writing their sum back for the second pass takes as long
+// as adding the halves again.
 constexpr int kFwdThreads = 640, kSlots = 4, kSoft = 3, CH = 16;
 constexpr int kRegsIssue = 56, kRegsSoft = 88, kRegsAdd = 160;
 static_assert(kRegsIssue + kSoft * kRegsSoft + kRegsAdd <= 480, "registers: 640 threads get 96 each at launch");

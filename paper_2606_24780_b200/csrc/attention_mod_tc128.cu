@@ -23,7 +23,7 @@
 //   tensor memory: A1 hi 0-127, lo 128-255, Out tile 256-383, buffer b at 384 + 64 b: X -> Z_hi, Y -> Z_lo
 //   shared memory: with A2 one buffer per stream; without, its 128 KB are two more stages of B1 and two of B3
 // Waits are inlined: a call would hold a warpgroup to the registers of the callee.
-// Two sequences of 1,000, 16 heads, prefix and cap: forward 64 us (tensor pipe 30 % busy), gradients 319 us.  256 blocks
+// Two sequences of 1,000, 16 heads, prefix and cap: forward 66 us (tensor pipe 29 % busy), gradients 320 us (30 to 31 %).  256 blocks
 // for 148 SMs are two rounds, and inside a block the chain X -> f -> Out of two tiles in flight is longer than its products.
 #include "attention_mod.cuh"
 
