@@ -21,7 +21,7 @@ namespace {
 // Which kernels.  The tcgen05 ones read planes; arrays given raw become planes in scratch, a pass over qkv (and dO) and a
 // launch.  The warp-level ones start at once, but take three times as long per score.  16 heads of 32, cap:
 //     T 128, batch 64    forward 59 us warp-level, 57 us tcgen05;   gradients 203, 168
-//     T 2,000, batch 4   481, 192;   1,561, 532
+//     T 2,000, batch 4   481, 195;   1,561, 532
 // and of 16 columns, zeros in half of the tcgen05 tiles: T 256, batch 32    52, 52;   161, 166.  Hence T d > 4,096: at 4,096
 // itself heads of 16 are 3 % better off on the warp-level kernels and heads of 32 up to a fifth worse, below it
 // (T 64, heads of 32: forward 43, 64, gradients 138, 198) the former win.  Wider heads always: one raw sequence of 64, 12 heads of

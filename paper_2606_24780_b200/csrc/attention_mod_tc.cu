@@ -68,19 +68,19 @@ __device__ __forceinline__ void settle() {
 // an item's loads, first products, last sums and stores overlap its neighbours'.
 //   warp 0      TMA producer and scheduler: the next item and its range of tiles; Q once per item, K and V tiles through one
 //               ring of four slots, K one tile ahead of V
-//   warp 1      S = Q K^T: [K_hi | K_lo] as one operand of 128 rows, the small terms into the second 64 columns
+//   warp 1      S = Q K^T, the small terms first
 //   warps 2, 3  O_tile = P V on alternate tiles, P from tensor memory, from zero in every tile
 //   warps 4-15  three softmax warpgroups on tiles in turn, thread = row.  Every tile is normalised by its own row
-//               maximum, so they carry nothing from tile to tile: a pass over the scores for the maximum (over both halves
-//               of them: the small one grows with the scores, to hundreds at 1e5), then P = exp2(z - r)
+//               maximum, so they carry nothing from tile to tile: a pass over the scores for the maximum (whole ones: their
+//               small terms reach hundreds at 1e5), then P = exp2(z - r)
 //   warps 16-19 add up: O = O 2^(m - m') + O_tile 2^(r - m'), l likewise; the row's output and lse
-//   tensor memory  buffer i at 128 i: S -> P_hi, small half of S -> P_lo; O_tile at 384 and 448
+//   tensor memory  buffer i at 128 i: S -> P_hi, P_lo; O_tile at 384 and 448
 // Two tiles in the softmax at a time are not enough to hide its latency; short rolled passes over the columns keep
 // the code in the instruction cache (32 columns unrolled cost a third more time than 16).
-// 8 packed sequences of 1,024, 12 heads, distance bias: 71 us, tensor pipe 39 % busy; the products of a tile are 1,664 clocks, the
-// element-wise warps, at 1.7 to 2.1 instructions a clock of all four schedulers, need about 2,800 with a cap.  The maximum from
-// whole scores costs 3 % (433 -> 448 us at 8,192 positions, causal); writing their sum back for the second pass takes as long
-// as adding the halves again.
+// 8 packed sequences of 1,024, 12 heads, distance bias: 69 us, tensor pipe 40 % busy; the products of a tile are about 1,900
+// clocks, the element-wise warps, at 1.7 to 2.1 instructions a clock of all four schedulers, need 2,700 with a cap.  S as two halves,
+// [K_hi | K_lo] as one operand, is 250 clocks less of products, but both passes of the element-wise warps have to add them:
+// 448 us in place of 437 at 8,192 positions, causal.
 constexpr int kFwdThreads = 640, kSlots = 4, kSoft = 3, CH = 16;
 constexpr int kRegsIssue = 56, kRegsSoft = 88, kRegsAdd = 160;
 static_assert(kRegsIssue + kSoft * kRegsSoft + kRegsAdd <= 480, "registers: 640 threads get 96 each at launch");
@@ -187,7 +187,7 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             }
             if (!ok) settle();
         } else if (warp == 1) {
-            constexpr uint32_t idesc = make_idesc_tf32(BR, BT64, false, false), idesc2 = make_idesc_tf32(BR, 2 * BT64, false, false);
+            constexpr uint32_t idesc = make_idesc_tf32(BR, BT64, false, false);
             const DescBase qd = kmaj_base(q_s);
             uint32_t c = 0, qi = 0, gt = 0;             // loads, non-empty items, tiles before this item
             Item it;
@@ -208,10 +208,11 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     if (elect_one()) {
 #pragma unroll
                         for (int ks = 0; ks < KS; ++ks) {
-                            const uint64_t k_hl = kd.at(kmaj_off(BT64, ks, false));
-                            umma_tf32(tS, qd.at(kmaj_off(BR, ks, false)), k_hl, idesc2, ks > 0 ? 1u : 0u);   // Q_hi K_hi | Q_hi K_lo
-                            umma_tf32(tS + 64u, qd.at(kmaj_off(BR, ks, true)), k_hl, idesc, 1u);             // + Q_lo K_hi
+                            umma_tf32(tS, qd.at(kmaj_off(BR, ks, true)), kd.at(kmaj_off(BT64, ks, false)), idesc, ks > 0 ? 1u : 0u);
+                            umma_tf32(tS, qd.at(kmaj_off(BR, ks, false)), kd.at(kmaj_off(BT64, ks, true)), idesc, 1u);
                         }
+#pragma unroll
+                        for (int ks = 0; ks < KS; ++ks) umma_tf32(tS, qd.at(kmaj_off(BR, ks, false)), kd.at(kmaj_off(BT64, ks, false)), idesc, 1u);
                         umma_commit(bar(SLOT_EMPTY + slot));
                         umma_commit(bar(S_FULL + buf));
                         if (t == it.n - 1) umma_commit(bar(Q_EMPTY));
@@ -287,12 +288,11 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll 1
                 for (int c0 = 0; c0 < BT64; c0 += CH) {
                     float z[CH], none[CH];
-                    uint32_t hi[CH], lo[CH];
-                    tmem_ldn(t_s + c0, hi);
-                    tmem_ldn(t_s + 64u + c0, lo);
+                    uint32_t r[CH];
+                    tmem_ldn(t_s + c0, r);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int k = 0; k < CH; ++k) z[k] = __uint_as_float(hi[k]) + __uint_as_float(lo[k]);
+                    for (int k = 0; k < CH; ++k) z[k] = __uint_as_float(r[k]);
                     if (SLOPE) score_tile<CAP, SLOPE, false, true, CH>(z, none, sc, row - key0 - c0, 0.f);   // else the maximum is at that of the product
                     mask(z, key0 + c0);
 #pragma unroll
@@ -307,10 +307,9 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     float z[CH], none[CH];
                     uint32_t hi[CH], lo[CH];
                     tmem_ldn(t_s + c0, hi);
-                    tmem_ldn(t_s + 64u + c0, lo);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int k = 0; k < CH; ++k) z[k] = __uint_as_float(hi[k]) + __uint_as_float(lo[k]);
+                    for (int k = 0; k < CH; ++k) z[k] = __uint_as_float(hi[k]);
                     score_tile<CAP, SLOPE, false, true, CH>(z, none, sc, row - key0 - c0, rf.now);
                     less_reference(z, rf);
                     mask(z, key0 + c0);
@@ -320,7 +319,7 @@ attn_mod_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         sum += p;
                         split_tf32_int(p, hi[k], lo[k]);
                     }
-                    tmem_stn(t_s + c0, hi);                             // P_hi over S, P_lo over its small half
+                    tmem_stn(t_s + c0, hi);                             // P_hi over S, P_lo beside it
                     tmem_stn(t_s + 64u + c0, lo);
                 }
                 float* stat = tile_stat + ((gt + (uint32_t)t) & 7u) * (2 * BR) + rloc;
