@@ -622,6 +622,85 @@ BT_API bt_status bt_op_dropout_fwd(const float* x, const float* residual, int64_
 BT_API bt_status bt_op_dropout_bwd(const float* dy, int64_t n, double p, uint64_t seed, uint64_t offset, float* dx,
                                    float* dx_split, const uint64_t* d_step, void* stream);
 
+/* ----------------------------------------------------------------------------------
+ * Losses at the language-model head.  The training step forms the logits x W^T of all rows, keeps them and
+ * their gradient, and takes the cross-entropy with bt_op_softmax_xent below: 12 bytes per row and vocabulary
+ * entry.  The calls here take the hidden states and the weights themselves: the forward keeps one (maximum,
+ * sum) pair per row and strip of the vocabulary, the backward forms the scores of one piece of the vocabulary
+ * at a time.  All calls are asynchronous, allocate nothing, keep nothing between calls and can be captured into
+ * a graph.  All arrays of a call lie on the current device, `stream` with them.
+ * -------------------------------------------------------------------------------- */
+
+/* Cross-entropy of x [N, C] against targets (int32 [N]) under the head W [V, C]:
+ *     z_nv = x_n . W_v,   lse_n = log sum_v exp z_nv,   losses_n = lse_n - z_{n, y_n},
+ *     loss_mean = inv_count sum_n w_n losses_n        (w = row_w, float [N]; NULL: ones).
+ * A target below zero marks a row without one: its loss is 0 and it has no part in the gradients, whatever
+ * its x holds; so has a row of weight 0 no part in mean and gradients.  A target from V on counts as class 0
+ * and its row + 1 is stored in *d_bad (device int32, nullable, zeroed by the caller; first writer wins).
+ *   x, w     raw [N, C] and [V, C], or x_split, w_split hi/lo planes [2][N][C] and [2][V][C]; one of each
+ *   losses, lse  [N] (lse nullable), loss_mean (nullable) 1 float, summed in a fixed order
+ * The backward takes the forward's inputs and lse and overwrites (each nullable, but not all)
+ *     dx [N, C] and / or dx_split [2][N][C]:  dx_n = g_n (sum_v q_nv W_v - W_{y_n}),   dw [V, C]:  dw_v = sum_n g_n (q_nv - [v = y_n]) x_n
+ * with q_nv = exp(z_nv - lse_n) and g_n = inv_count w_n, in a fixed order (no atomics on floats: two runs give the
+ * same bits).  piece: columns of the vocabulary worked on at a time, 0 for the library's choice; it sets the size of the
+ * scratch and not the results' accuracy.
+ * The products run on the tensor cores on pairs of FP16 numbers (22 bits of each value, scaled by powers of two so that
+ * the largest one of x's row, and of W, lies near FP16's largest): values below 2^-18 of those lose bits at an absolute
+ * 2^-40 of the largest.  Few rows run in plain FP32.  x of rows that count, and W, must be finite; a row whose scores are
+ * beyond FP32 is not a number in losses and lse.
+ * C a multiple of 32, at most 4096; V and N at most 2^24.  N = 0 is nothing to do (loss_mean and dw become 0).
+ * scratch: device, 256-byte aligned, of the stated size (K = 0), contents irrelevant on entry; calls that may
+ * overlap on the GPU need one each.  bt_op_head_check synchronises the stream and returns BT_ERR_DEVICE_TIMEOUT if a
+ * bounded wait of the last call on that scratch ran out.  No output may overlap an input. */
+BT_API size_t bt_op_head_fwd_scratch_bytes(int64_t N, int32_t C, int32_t V, int32_t K);
+BT_API size_t bt_op_head_bwd_scratch_bytes(int64_t N, int32_t C, int32_t V, int32_t K, int32_t piece);
+BT_API bt_status bt_op_head_xent_fwd(const float* x, const float* x_split, const float* w, const float* w_split,
+                                     const int32_t* targets, const float* row_w, int64_t N, int32_t C, int32_t V,
+                                     float inv_count, float* losses, float* lse, float* loss_mean, int32_t* d_bad,
+                                     void* scratch, size_t scratch_bytes, void* stream);
+BT_API bt_status bt_op_head_xent_bwd(const float* x, const float* x_split, const float* w, const float* w_split,
+                                     const int32_t* targets, const float* row_w, const float* lse, int64_t N, int32_t C,
+                                     int32_t V, float inv_count, int32_t piece, float* dx, float* dx_split, float* dw,
+                                     void* scratch, size_t scratch_bytes, void* stream);
+BT_API bt_status bt_op_head_check(const void* scratch, void* stream);
+
+/* A teacher's top logits: K entries per row (1 to 1024), ids int32 [N, K] and logits float [N, K].  An id below zero,
+ * or a logit of -inf, marks an entry that is not there (rows may have fewer than K, or none: such a row counts as
+ * one without a target); the same id twice counts with both probabilities.  With t the logits and tau the
+ * temperature (1e-4 to 1e4),
+ *     p_nk = softmax over the row's entries of t_nk / tau            (lse NULL), or
+ *     p_nk = exp(t_nk / tau - lse_n)                                 (lse float [N]: log sum exp(t / tau) of the teacher's
+ *                                                                     whole vocabulary; the rest of it is left out),
+ *     losses_n = tau^2 sum_k p_nk (log p_nk - z_{n, i_nk} + lse_n),  z and lse_n of the student's logits / tau,
+ *     d losses_n / d logits_nv = tau (S_n q_nv - sum_{k: i_nk = v} p_nk),   S_n = sum_k p_nk.
+ * No gradient is formed for the teacher. */
+typedef struct {
+    int32_t K;
+    float temperature;
+    const int32_t* ids;
+    const float* logits;
+    const float* lse;
+} bt_distill;
+
+/* The same head with this loss in the place of the cross-entropy; lse is log sum_v exp(x_n . W_v / tau).  Scratch sizes as
+ * above with the teacher's K. */
+BT_API bt_status bt_op_head_distill_fwd(const float* x, const float* x_split, const float* w, const float* w_split,
+                                        const bt_distill* teacher, const float* row_w, int64_t N, int32_t C, int32_t V,
+                                        float inv_count, float* losses, float* lse, float* loss_mean, int32_t* d_bad,
+                                        void* scratch, size_t scratch_bytes, void* stream);
+BT_API bt_status bt_op_head_distill_bwd(const float* x, const float* x_split, const float* w, const float* w_split,
+                                        const bt_distill* teacher, const float* row_w, const float* lse, int64_t N,
+                                        int32_t C, int32_t V, float inv_count, int32_t piece, float* dx, float* dx_split,
+                                        float* dw, void* scratch, size_t scratch_bytes, void* stream);
+
+/* The same loss on the student's logits [N, ld], of which the first V columns count (ld a multiple of 4, at least V):
+ * losses, loss_mean (nullable) and the gradient inv_count w_n d losses_n / d logits_nv, raw (dlogits [N, ld]) and / or as
+ * planes (dlogits_split [2][N][ld]), both optional; columns from V on become 0.  The gradient may be written over the
+ * logits, dlogits or the hi plane of dlogits_split being the same array.  N at most 2^24, V and ld at most 2^30. */
+BT_API bt_status bt_op_softmax_distill(const float* logits, const bt_distill* teacher, const float* row_w, int64_t N,
+                                       int32_t V, int32_t ld, float inv_count, float* losses, float* loss_mean,
+                                       float* dlogits, float* dlogits_split, int32_t* d_bad, void* stream);
+
 /* GELU forward (Appendix "Performance Benchmarks", GELU Forward; Kernel Design and Optimization:
  * 128-bit accesses, one pass, no lossy approximation): y = GELU(x) in the exact erf form (or the
  * tanh form), n % 4 == 0. */

@@ -54,6 +54,11 @@ class bt_attn_mod(ctypes.Structure):
     _fields_ = [("softcap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("spans", ctypes.c_void_p)]
 
 
+class bt_distill(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_int32), ("temperature", ctypes.c_float), ("ids", ctypes.c_void_p),
+                ("logits", ctypes.c_void_p), ("lse", ctypes.c_void_p)]
+
+
 _vp, _i32, _i64, _u32, _sz, _f = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_size_t,
                                   ctypes.c_float)
 _SIGNATURES = {
@@ -134,6 +139,14 @@ _SIGNATURES = {
     "bt_op_attention_mod_check": (_i32, [_vp, _vp]),
     "bt_op_dropout_fwd": (_i32, [_vp, _vp, _i64, ctypes.c_double, ctypes.c_uint64, ctypes.c_uint64, _vp, _vp, _vp, _vp]),
     "bt_op_dropout_bwd": (_i32, [_vp, _i64, ctypes.c_double, ctypes.c_uint64, ctypes.c_uint64, _vp, _vp, _vp, _vp]),
+    "bt_op_head_fwd_scratch_bytes": (_sz, [_i64, _i32, _i32, _i32]),
+    "bt_op_head_bwd_scratch_bytes": (_sz, [_i64, _i32, _i32, _i32, _i32]),
+    "bt_op_head_xent_fwd": (_i32, [_vp] * 6 + [_i64, _i32, _i32, _f] + [_vp] * 5 + [_sz, _vp]),
+    "bt_op_head_xent_bwd": (_i32, [_vp] * 7 + [_i64, _i32, _i32, _f, _i32] + [_vp] * 4 + [_sz, _vp]),
+    "bt_op_head_distill_fwd": (_i32, [_vp] * 4 + [ctypes.POINTER(bt_distill), _vp, _i64, _i32, _i32, _f] + [_vp] * 5 + [_sz, _vp]),
+    "bt_op_head_distill_bwd": (_i32, [_vp] * 4 + [ctypes.POINTER(bt_distill), _vp, _vp, _i64, _i32, _i32, _f, _i32] + [_vp] * 4 + [_sz, _vp]),
+    "bt_op_head_check": (_i32, [_vp, _vp]),
+    "bt_op_softmax_distill": (_i32, [_vp, ctypes.POINTER(bt_distill), _vp, _i64, _i32, _i32, _f] + [_vp] * 6),
     "bt_op_gelu_fwd": (_i32, [_vp, _i64, _i32, _vp, _vp, _vp]),
     "bt_op_gelu_bwd": (_i32, [_vp, _vp, _i64, _i32, _vp, _vp, _vp]),
     "bt_op_gelu_bwd_colsum": (_i32, [_vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
@@ -687,6 +700,70 @@ def bt_op_dropout_fwd(x, residual, n, p, seed, offset, y, y_split=None, d_step=N
 
 def bt_op_dropout_bwd(dy, n, p, seed, offset, dx, dx_split=None, d_step=None, stream=None):
     _call(lib().bt_op_dropout_bwd, stream, _arr(dy), n, p, seed, offset, _arr(dx), _arr(dx_split), _arr(d_step, torch.int64))
+
+
+def make_distill(ids, logits, temperature=1.0, lse=None):
+    """A teacher's top logits for bt_op_head_distill_* and bt_op_softmax_distill: ids (int32) and logits [N, K], lse [N];
+    it keeps the tensors it is given alive."""
+    if ids.dim() != 2 or logits.shape != ids.shape or (lse is not None and lse.numel() != ids.shape[0]):
+        raise ValueError("ids and logits must be [N, K], lse [N]")
+    teacher = bt_distill(ids.shape[1], temperature, _arr(ids, torch.int32), _arr(logits), _arr(lse))
+    teacher.tensors = (ids, logits, lse)
+    return teacher
+
+
+def _check_rows(teacher, N):
+    tensors = getattr(teacher, "tensors", None)
+    if tensors is not None and tensors[0].shape[0] < N:
+        raise ValueError(f"a teacher of {tensors[0].shape[0]} rows for {N}")
+
+
+def bt_op_head_fwd_scratch_bytes(N, C, V, K=0):
+    return int(lib().bt_op_head_fwd_scratch_bytes(N, C, V, K))
+
+
+def bt_op_head_bwd_scratch_bytes(N, C, V, K=0, piece=0):
+    return int(lib().bt_op_head_bwd_scratch_bytes(N, C, V, K, piece))
+
+
+def bt_op_head_xent_fwd(x, x_split, w, w_split, targets, row_w, N, C, V, inv_count, losses, lse, loss_mean, scratch,
+                        scratch_bytes, d_bad=None, stream=None):
+    _call(lib().bt_op_head_xent_fwd, stream, _arr(x), _arr(x_split), _arr(w), _arr(w_split), _arr(targets, torch.int32),
+          _arr(row_w), N, C, V, inv_count, _arr(losses), _arr(lse), _arr(loss_mean), _arr(d_bad, torch.int32),
+          _arr(scratch, torch.uint8), scratch_bytes)
+
+
+def bt_op_head_xent_bwd(x, x_split, w, w_split, targets, row_w, lse, N, C, V, inv_count, dx, dw, scratch, scratch_bytes,
+                        piece=0, dx_split=None, stream=None):
+    _call(lib().bt_op_head_xent_bwd, stream, _arr(x), _arr(x_split), _arr(w), _arr(w_split), _arr(targets, torch.int32),
+          _arr(row_w), _arr(lse), N, C, V, inv_count, piece, _arr(dx), _arr(dx_split), _arr(dw), _arr(scratch, torch.uint8),
+          scratch_bytes)
+
+
+def bt_op_head_distill_fwd(x, x_split, w, w_split, teacher, row_w, N, C, V, inv_count, losses, lse, loss_mean, scratch,
+                           scratch_bytes, d_bad=None, stream=None):
+    _check_rows(teacher, N)
+    _call(lib().bt_op_head_distill_fwd, stream, _arr(x), _arr(x_split), _arr(w), _arr(w_split), teacher, _arr(row_w), N, C, V,
+          inv_count, _arr(losses), _arr(lse), _arr(loss_mean), _arr(d_bad, torch.int32), _arr(scratch, torch.uint8),
+          scratch_bytes)
+
+
+def bt_op_head_distill_bwd(x, x_split, w, w_split, teacher, row_w, lse, N, C, V, inv_count, dx, dw, scratch, scratch_bytes,
+                           piece=0, dx_split=None, stream=None):
+    _check_rows(teacher, N)
+    _call(lib().bt_op_head_distill_bwd, stream, _arr(x), _arr(x_split), _arr(w), _arr(w_split), teacher, _arr(row_w),
+          _arr(lse), N, C, V, inv_count, piece, _arr(dx), _arr(dx_split), _arr(dw), _arr(scratch, torch.uint8), scratch_bytes)
+
+
+def bt_op_head_check(scratch, stream=None):
+    _call(lib().bt_op_head_check, stream, _arr(scratch, torch.uint8))
+
+
+def bt_op_softmax_distill(logits, teacher, row_w, N, V, ld, inv_count, losses, loss_mean, dlogits, dlogits_split=None,
+                          d_bad=None, stream=None):
+    _check_rows(teacher, N)
+    _call(lib().bt_op_softmax_distill, stream, _arr(logits), teacher, _arr(row_w), N, V, ld, inv_count, _arr(losses),
+          _arr(loss_mean), _arr(dlogits), _arr(dlogits_split), _arr(d_bad, torch.int32))
 
 
 def bt_op_gelu_fwd(x, n, tanh_form, y, y_split, stream=None):

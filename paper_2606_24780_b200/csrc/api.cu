@@ -1662,6 +1662,188 @@ extern "C" bt_status bt_op_attention_mod_check(const void* scratch, void* stream
     return BT_OK;
 }
 
+// ---------------------------------------------------------------- losses at the language-model head
+
+namespace {
+
+constexpr int64_t kHeadMost = 1 << 24;      // rows, and entries of the vocabulary
+
+bool head_sizes_ok(int64_t N, int32_t C, int32_t V, int32_t K) {
+    return N >= 0 && N <= kHeadMost && C >= 32 && C <= 4096 && C % 32 == 0 && V >= 1 && V <= kHeadMost && K >= 0 && K <= 1024;
+}
+
+bt_status loss_aim(LossAim& a, const char* who, const int32_t* targets, const bt_distill* t, bool none, const float* row_w, float inv_count) {
+    a = LossAim{};
+    a.tau = 1.0f;
+    a.inv_count = inv_count;
+    a.row_w = row_w;
+    BT_OPT_PTR(row_w);
+    if (!t) {
+        if (!none) BT_PTR(targets);
+        a.targets = targets;
+        return BT_OK;
+    }
+    if (t->K < 1 || t->K > 1024) return fail(BT_ERR_INVALID_ARG, "%s: K %d not in [1, 1024]", who, t->K);
+    if (!(t->temperature >= 1e-4f && t->temperature <= 1e4f)) return fail(BT_ERR_INVALID_ARG, "%s: temperature not in [1e-4, 1e4]", who);
+    if (!none && (!t->ids || !t->logits)) return fail(BT_ERR_INVALID_ARG, "%s: the teacher's ids or logits are NULL", who);
+    if (!aligned16(t->ids) || !aligned16(t->logits) || !aligned16(t->lse))
+        return fail(BT_ERR_INVALID_ARG, "%s: the teacher's arrays are not 16-byte aligned", who);
+    a.K = t->K;
+    a.ids = t->ids;
+    a.logits = t->logits;
+    a.lse = t->lse;
+    a.tau = t->temperature;
+    return BT_OK;
+}
+
+bt_status head_args(HeadArgs& g, const char* who, const float* x, const float* x_split, const float* w, const float* w_split,
+                    const int32_t* targets, const bt_distill* teacher, bool distill, const float* row_w, int64_t N, int32_t C,
+                    int32_t V, float inv_count, void* scratch) {
+    if (!head_sizes_ok(N, C, V, 0)) return fail(BT_ERR_INVALID_ARG, "%s: N and V up to 2^24, C a multiple of 32 up to 4096", who);
+    BT_OPT_PTR(x); BT_OPT_PTR(x_split); BT_OPT_PTR(w); BT_OPT_PTR(w_split);
+    if (N != 0 && !x && !x_split) return fail(BT_ERR_INVALID_ARG, "%s: x and x_split both NULL", who);
+    if (N != 0 && !w && !w_split) return fail(BT_ERR_INVALID_ARG, "%s: w and w_split both NULL", who);
+    if (distill && !teacher) return fail(BT_ERR_INVALID_ARG, "%s: teacher is NULL", who);
+    if (bt_status st = loss_aim(g.aim, who, targets, teacher, N == 0, row_w, inv_count)) return st;
+    if (N != 0 && !scratch) return fail(BT_ERR_INVALID_ARG, "%s: scratch is NULL", who);
+    if (reinterpret_cast<uintptr_t>(scratch) & 255u) return fail(BT_ERR_INVALID_ARG, "%s: scratch not 256-byte aligned", who);
+    g.x = x ? x : x_split;
+    g.x_lo = x ? nullptr : x_split + N * C;
+    g.w = w ? w : w_split;
+    g.w_lo = w ? nullptr : w_split + (int64_t)V * C;
+    g.N = N; g.C = C; g.V = V;
+    g.scratch = (uint8_t*)scratch;
+    return BT_OK;
+}
+
+bt_status head_fwd(const char* who, HeadArgs& g, float* losses, float* lse, float* loss_mean, int32_t* d_bad, size_t scratch_bytes,
+                   cudaStream_t s) {
+    if (g.N != 0) BT_PTR(losses);
+    BT_OPT_PTR(losses); BT_OPT_PTR(lse); BT_OPT_PTR(loss_mean);
+    if (reinterpret_cast<uintptr_t>(d_bad) & 3u) return fail(BT_ERR_INVALID_ARG, "%s: d_bad is not 4-byte aligned", who);
+    if (g.N == 0) {
+        if (loss_mean) BT_CUDA(cudaMemsetAsync(loss_mean, 0, sizeof(float), s));
+        return BT_OK;
+    }
+    if (scratch_bytes < bt_op_head_fwd_scratch_bytes(g.N, g.C, g.V, g.aim.K)) return fail(BT_ERR_OOM, "%s: scratch too small", who);
+    for (const float* out : {losses, lse, loss_mean})
+        if (out && (out == g.x || out == g.w || out == g.aim.row_w || out == g.aim.logits || out == g.aim.lse))
+            return fail(BT_ERR_INVALID_ARG, "%s: an output over an input", who);
+    g.losses = losses; g.lse = lse; g.loss_mean = loss_mean; g.bad = d_bad;
+    BT_CUDA(launch_head_fwd(g, s));
+    return BT_OK;
+}
+
+bt_status head_bwd(const char* who, HeadArgs& g, const float* lse, int32_t piece, float* dx, float* dx_split, float* dw,
+                   size_t scratch_bytes, cudaStream_t s) {
+    if (g.N != 0) BT_PTR(lse);
+    BT_OPT_PTR(lse); BT_OPT_PTR(dx); BT_OPT_PTR(dx_split); BT_OPT_PTR(dw);
+    if (piece < 0) return fail(BT_ERR_INVALID_ARG, "%s: piece below zero", who);
+    if (g.N != 0 && !dx && !dx_split && !dw) return fail(BT_ERR_INVALID_ARG, "%s: no output requested", who);
+    if (g.N == 0) {
+        if (dw) BT_CUDA(cudaMemsetAsync(dw, 0, (size_t)g.V * g.C * sizeof(float), s));
+        return BT_OK;
+    }
+    if (scratch_bytes < bt_op_head_bwd_scratch_bytes(g.N, g.C, g.V, g.aim.K, piece)) return fail(BT_ERR_OOM, "%s: scratch too small", who);
+    for (const float* out : {(const float*)dx, (const float*)dx_split, (const float*)dw})
+        if (out && (out == g.x || out == g.w || out == g.aim.row_w || out == lse || out == g.aim.logits || out == g.aim.lse))
+            return fail(BT_ERR_INVALID_ARG, "%s: an output over an input", who);
+    g.lse_in = lse;
+    g.piece = piece;
+    g.dx = dx; g.dx_hi = dx_split; g.dx_lo = dx_split ? dx_split + g.N * g.C : nullptr;
+    g.dw = dw;
+    BT_CUDA(launch_head_bwd(g, s));
+    return BT_OK;
+}
+
+}  // namespace
+
+extern "C" size_t bt_op_head_fwd_scratch_bytes(int64_t N, int32_t C, int32_t V, int32_t K) {
+    return head_sizes_ok(N, C, V, K) ? head_fwd_scratch_bytes(N, C, V, K) : 0;
+}
+
+extern "C" size_t bt_op_head_bwd_scratch_bytes(int64_t N, int32_t C, int32_t V, int32_t K, int32_t piece) {
+    return head_sizes_ok(N, C, V, K) && piece >= 0 ? head_bwd_scratch_bytes(N, C, V, K, piece) : 0;
+}
+
+extern "C" bt_status bt_op_head_xent_fwd(const float* x, const float* x_split, const float* w, const float* w_split,
+                                         const int32_t* targets, const float* row_w, int64_t N, int32_t C, int32_t V,
+                                         float inv_count, float* losses, float* lse, float* loss_mean, int32_t* d_bad,
+                                         void* scratch, size_t scratch_bytes, void* stream) {
+    HeadArgs g{};
+    if (bt_status st = head_args(g, "head_xent_fwd", x, x_split, w, w_split, targets, nullptr, false, row_w, N, C, V, inv_count, scratch)) return st;
+    return head_fwd("head_xent_fwd", g, losses, lse, loss_mean, d_bad, scratch_bytes, (cudaStream_t)stream);
+}
+
+extern "C" bt_status bt_op_head_xent_bwd(const float* x, const float* x_split, const float* w, const float* w_split,
+                                         const int32_t* targets, const float* row_w, const float* lse, int64_t N, int32_t C,
+                                         int32_t V, float inv_count, int32_t piece, float* dx, float* dx_split, float* dw,
+                                         void* scratch, size_t scratch_bytes, void* stream) {
+    HeadArgs g{};
+    if (bt_status st = head_args(g, "head_xent_bwd", x, x_split, w, w_split, targets, nullptr, false, row_w, N, C, V, inv_count, scratch)) return st;
+    return head_bwd("head_xent_bwd", g, lse, piece, dx, dx_split, dw, scratch_bytes, (cudaStream_t)stream);
+}
+
+extern "C" bt_status bt_op_head_distill_fwd(const float* x, const float* x_split, const float* w, const float* w_split,
+                                            const bt_distill* teacher, const float* row_w, int64_t N, int32_t C, int32_t V,
+                                            float inv_count, float* losses, float* lse, float* loss_mean, int32_t* d_bad,
+                                            void* scratch, size_t scratch_bytes, void* stream) {
+    HeadArgs g{};
+    if (bt_status st = head_args(g, "head_distill_fwd", x, x_split, w, w_split, nullptr, teacher, true, row_w, N, C, V, inv_count, scratch)) return st;
+    return head_fwd("head_distill_fwd", g, losses, lse, loss_mean, d_bad, scratch_bytes, (cudaStream_t)stream);
+}
+
+extern "C" bt_status bt_op_head_distill_bwd(const float* x, const float* x_split, const float* w, const float* w_split,
+                                            const bt_distill* teacher, const float* row_w, const float* lse, int64_t N,
+                                            int32_t C, int32_t V, float inv_count, int32_t piece, float* dx, float* dx_split,
+                                            float* dw, void* scratch, size_t scratch_bytes, void* stream) {
+    HeadArgs g{};
+    if (bt_status st = head_args(g, "head_distill_bwd", x, x_split, w, w_split, nullptr, teacher, true, row_w, N, C, V, inv_count, scratch)) return st;
+    return head_bwd("head_distill_bwd", g, lse, piece, dx, dx_split, dw, scratch_bytes, (cudaStream_t)stream);
+}
+
+extern "C" bt_status bt_op_head_check(const void* scratch, void* stream) {
+    if (!scratch) return fail(BT_ERR_INVALID_ARG, "scratch is NULL");
+    if (reinterpret_cast<uintptr_t>(scratch) & 255u) return fail(BT_ERR_INVALID_ARG, "head: scratch not 256-byte aligned");
+    int herr = 0;
+    BT_CUDA(cudaMemcpyAsync(&herr, scratch, sizeof(int), cudaMemcpyDeviceToHost, (cudaStream_t)stream));
+    BT_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
+    if (herr) {
+        BT_CUDA(cudaMemsetAsync(const_cast<void*>(scratch), 0, sizeof(int), (cudaStream_t)stream));   // reported once
+        return fail(BT_ERR_DEVICE_TIMEOUT, "head: a bounded device-side wait ran out (code %d)", herr);
+    }
+    return BT_OK;
+}
+
+extern "C" bt_status bt_op_softmax_distill(const float* logits, const bt_distill* teacher, const float* row_w, int64_t N,
+                                           int32_t V, int32_t ld, float inv_count, float* losses, float* loss_mean,
+                                           float* dlogits, float* dlogits_split, int32_t* d_bad, void* stream) {
+    if (N < 0 || N > kHeadMost || V < 1 || ld < V || ld % 4 || ld > (1 << 30))
+        return fail(BT_ERR_INVALID_ARG, "softmax_distill: N up to 2^24, 1 <= V <= ld <= 2^30, ld a multiple of 4");
+    if (N != 0) { BT_PTR(logits); BT_PTR(losses); }
+    BT_OPT_PTR(logits); BT_OPT_PTR(losses); BT_OPT_PTR(loss_mean); BT_OPT_PTR(dlogits); BT_OPT_PTR(dlogits_split);
+    if (reinterpret_cast<uintptr_t>(d_bad) & 3u) return fail(BT_ERR_INVALID_ARG, "softmax_distill: d_bad is not 4-byte aligned");
+    if (!teacher) return fail(BT_ERR_INVALID_ARG, "softmax_distill: teacher is NULL");
+    DistillArgs g{};
+    if (bt_status st = loss_aim(g.aim, "softmax_distill", nullptr, teacher, N == 0, row_w, inv_count)) return st;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (N == 0) {
+        if (loss_mean) BT_CUDA(cudaMemsetAsync(loss_mean, 0, sizeof(float), s));
+        return BT_OK;
+    }
+    float* lo = dlogits_split ? dlogits_split + N * ld : nullptr;
+    if (lo && lo == logits) return fail(BT_ERR_INVALID_ARG, "softmax_distill: the lo plane over the logits");
+    for (const float* out : {(const float*)losses, (const float*)loss_mean, (const float*)dlogits, (const float*)dlogits_split})
+        if (out && (out == g.aim.row_w || out == g.aim.logits || out == g.aim.lse))
+            return fail(BT_ERR_INVALID_ARG, "softmax_distill: an output over an input");
+    g.z = logits;
+    g.N = N; g.V = V; g.ld = ld;
+    g.losses = losses; g.loss_mean = loss_mean; g.bad = d_bad;
+    g.dz = dlogits; g.dz_hi = dlogits_split; g.dz_lo = lo;
+    BT_CUDA(launch_softmax_distill(g, s));
+    return BT_OK;
+}
+
 extern "C" bt_status bt_op_gelu_fwd(const float* x, int64_t n, int32_t tanh_form, float* y, float* y_split,
                                     void* stream) {
     BT_PTR(x); BT_OPT_PTR(y); BT_OPT_PTR(y_split);

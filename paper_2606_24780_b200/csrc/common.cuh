@@ -369,4 +369,43 @@ struct DropoutArgs {
 };
 cudaError_t launch_dropout(const DropoutArgs& g, cudaStream_t s);
 
+// Losses at the language-model head.  What the rows are held to: a target each, or a teacher's K entries each.
+struct LossAim {
+    const int32_t* targets;     // [N]; null: a teacher
+    int K;
+    const int32_t* ids;         // [N, K], below zero: no entry
+    const float* logits;        // [N, K]
+    const float* lse;           // [N], null: probabilities normalised over the entries
+    float tau;                  // 1 with targets
+    const float* row_w;         // [N], null: ones
+    float inv_count;
+};
+// An array given raw has its *_lo null; given as planes, the first pointer is the hi plane.
+struct HeadArgs {
+    const float *x, *x_lo, *w, *w_lo;       // [N, C], [V, C]
+    LossAim aim;
+    int64_t N;
+    int C, V;
+    float *losses, *lse, *loss_mean;        // forward
+    int* bad;
+    const float* lse_in;                    // backward
+    int piece;
+    float *dx, *dx_hi, *dx_lo, *dw;
+    uint8_t* scratch;
+};
+size_t head_fwd_scratch_bytes(int64_t N, int C, int V, int K);
+size_t head_bwd_scratch_bytes(int64_t N, int C, int V, int K, int piece);
+cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s);
+cudaError_t launch_head_bwd(const HeadArgs& g, cudaStream_t s);
+// Distillation on logits [N, ld], of which the first V columns count.
+struct DistillArgs {
+    const float* z;
+    LossAim aim;
+    int64_t N, ld;
+    int V;
+    float *losses, *loss_mean, *dz, *dz_hi, *dz_lo;
+    int* bad;
+};
+cudaError_t launch_softmax_distill(const DistillArgs& g, cudaStream_t s);
+
 }  // namespace bt

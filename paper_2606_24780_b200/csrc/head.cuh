@@ -1,0 +1,99 @@
+// The losses at the language-model head: row arithmetic and scratch shared by their kernels.
+#pragma once
+#include <math.h>
+
+#include "common.cuh"
+
+namespace bt {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kMaxEntries = 1024;           // of a teacher, per row
+
+// Scratch starts with this header; the other regions begin on multiples of 256 bytes.
+struct HeadHeader {
+    int err;                                // device error word of the bounded waits
+    unsigned rows_done;                     // rows whose loss is written: the CTA of the last one forms the mean
+};
+constexpr size_t kHeadHeader = 256;
+inline size_t head_pad(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+
+// Logit of entry k of a row in units of the softened softmax, -inf where there is none (a weight of zero).  An id
+// behind the vocabulary counts as id 0 and is recorded.
+__device__ __forceinline__ float entry_logit(const LossAim& a, int64_t row, int k, int V, int* bad, int& id) {
+    id = a.ids[row * a.K + k];
+    if (id < 0) return -INFINITY;
+    if (id >= V) {
+        if (bad) atomicCAS(bad, 0, (int)row + 1);
+        id = 0;
+    }
+    return a.logits[row * a.K + k] * (1.0f / a.tau);
+}
+
+__device__ __forceinline__ float row_weight(const LossAim& a, int64_t row) { return a.row_w ? a.row_w[row] : 1.0f; }
+
+// Sum or maximum over the block (THREADS threads, a multiple of 32); every thread gets it.  `sm` holds THREADS / 32
+// values and may be reused as soon as the call returns.
+template <int THREADS, typename T, typename F>
+__device__ __forceinline__ T block_all(T v, T* sm, F op) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+    if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
+    __syncthreads();
+    T r = sm[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 32; ++w) r = op(r, sm[w]);
+    __syncthreads();
+    return r;
+}
+struct SumOp {
+    template <typename T>
+    __device__ __forceinline__ T operator()(T a, T b) const { return a + b; }
+};
+struct MaxOp {
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+
+// The logarithm of a teacher's normaliser for one row; `any`: the row has an entry.  All threads of the block call it.
+template <int THREADS>
+__device__ __forceinline__ float teacher_norm(const LossAim& a, int64_t row, int V, int* bad, float* sm, bool& any) {
+    float m = -INFINITY;
+    int id, have = 0;
+    for (int k = threadIdx.x; k < a.K; k += THREADS) {
+        const float t = entry_logit(a, row, k, V, bad, id);
+        have |= t != -INFINITY;             // a logit that is not a number counts: the row then has no finite loss
+        m = fmaxf(m, t);
+    }
+    any = __syncthreads_or(have) != 0;
+    if (!any) return 0.f;
+    if (a.lse) return a.lse[row];
+    m = block_all<THREADS>(m, sm, MaxOp());
+    float s = 0.f;
+    for (int k = threadIdx.x; k < a.K; k += THREADS) s += expf(entry_logit(a, row, k, V, nullptr, id) - m);
+    return m + logf(block_all<THREADS>(s, sm, SumOp()));
+}
+
+// The mean loss, by the block that finishes last: inv_count * sum_n w_n losses_n in a fixed order, in 64 bits.  Rows
+// of weight zero are left out whatever their loss is.
+template <int THREADS>
+__device__ __forceinline__ void mean_by_last(const LossAim& a, const float* losses, int64_t N, unsigned* rows_done, unsigned blocks,
+                                             float* mean, double* sm) {
+    __shared__ bool last;
+    __syncthreads();                        // the block's own loss is written
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicAdd(rows_done, 1u) == blocks - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double t = 0.0;
+#pragma unroll 8
+    for (int64_t n = threadIdx.x; n < N; n += THREADS) {
+        const float w = row_weight(a, n);
+        t += w != 0.f ? (double)__ldcg(losses + n) * (double)w : 0.0;
+    }
+    t = block_all<THREADS>(t, sm, SumOp());
+    if (threadIdx.x == 0) *mean = (float)(t * (double)a.inv_count);
+}
+
+}  // namespace bt
