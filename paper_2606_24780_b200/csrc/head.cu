@@ -8,23 +8,24 @@
 // g_n = inv_count w_n tau S_n.  The forward keeps one (maximum, sum) pair per row and strip of the vocabulary, joined
 // by head_finish_kernel, which also forms the few scores that the loss needs by themselves; the backward forms z again.
 //
-// The kernels here are for few rows: the weights are read in full width by every SM and each value is used for
-// up to eight rows from registers.
+// Up to eight rows go through the kernels here in plain FP32: the weights are read once in full width and each value is used
+// for all rows from registers.  More rows go to the tensor cores (head_tc.cu) on pairs of FP16 numbers that
+// head_pairs_kernel makes of x and W.
 #include "head.cuh"
 
 namespace bt {
 
 namespace {
 
-constexpr int kRows = 8;                    // rows of x that one launch carries
+constexpr int kRows = 8;                    // rows of x that the plain kernels carry
+constexpr int kParts = 592;                 // CTAs that look for the largest value
 constexpr int kStrips = 592;                // CTAs over the vocabulary (4 per SM)
 constexpr int kThreads = 256;
 constexpr int kFinishThreads = 256;
 
-struct RowParams {                          // backward, per row
-    float L;                                // lse in units of log 2; +inf: the row has no part in the loss
-    float g;                                // inv_count w tau S
-    int target;                             // column whose aim is 1; below zero: none
+// Powers of two of the FP16 pairs: W and y are held times 2^kw and 2^ky.
+struct Scales {
+    float dx, dw;                           // from accumulators of u W and u^T y to the results
 };
 
 struct Scratch {
@@ -33,30 +34,72 @@ struct Scratch {
     RowParams* rows;                        // backward: [N]
     int* eid;                               // [N][K] columns of the aim, each once; below zero: none
     float* ep;                              // [N][K] its weights there
+    // few rows
     float* u;                               // [V][kRows]
     float* dx_part;                         // [strips][kRows][C]
+    // tensor cores
+    Scales* scales;
+    float *wpart, *ypart;                   // [kParts] largest values
+    float* rowmax;                          // [N]
+    float* rowf;                            // [N]
+    __half *x16, *y16, *w16, *u16;          // pairs: [2][N][C], [2][N][C], [2][V][C], [2][N][ldu]
+    float* partials;
 };
 
-size_t fwd_layout(Scratch& s, uint8_t* base, int64_t N) {
-    size_t at = kHeadHeader;
-    s.head = (HeadHeader*)base;
-    s.stats = (float2*)(base + at);
-    return at + head_pad((size_t)N * kStrips * sizeof(float2));
+bool few_rows(int64_t N) { return N <= kRows; }
+
+// Columns of one piece of the vocabulary, a multiple of 256: pieces of about the same size, of at most `piece` columns or
+// 512 MB of u.
+int piece_columns(int64_t N, int V, int piece) {
+    int64_t most = piece > 0 ? piece : ((int64_t)1 << 27) / N;
+    most = most < 256 ? 256 : (most + 255) / 256 * 256;
+    const int64_t pieces = (V + most - 1) / most;
+    return (int)(((V + pieces - 1) / pieces + 255) / 256 * 256);
 }
 
-size_t bwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K) {
+template <typename T>
+T* take(uint8_t* base, size_t& at, size_t n) {
+    T* p = (T*)(base + at);
+    at += head_pad(n * sizeof(T));
+    return p;
+}
+
+void tc_layout(Scratch& s, uint8_t* base, size_t& at, int64_t N, int C, int V) {
+    s.scales = take<Scales>(base, at, 1);
+    s.wpart = take<float>(base, at, kParts);
+    s.rowf = take<float>(base, at, N);
+    s.x16 = take<__half>(base, at, 2 * (size_t)N * C);
+    s.w16 = take<__half>(base, at, 2 * (size_t)V * C);
+}
+
+size_t fwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V) {
     size_t at = kHeadHeader;
+    s = Scratch{};
     s.head = (HeadHeader*)base;
-    s.rows = (RowParams*)(base + at);
-    at += head_pad((size_t)N * sizeof(RowParams));
-    s.eid = (int*)(base + at);
-    at += head_pad((size_t)N * K * 4);
-    s.ep = (float*)(base + at);
-    at += head_pad((size_t)N * K * 4);
-    s.u = (float*)(base + at);
-    at += head_pad((size_t)V * kRows * 4);
-    s.dx_part = (float*)(base + at);
-    return at + head_pad((size_t)kStrips * kRows * C * 4);
+    s.stats = take<float2>(base, at, (size_t)N * (few_rows(N) ? kStrips : head_stats_strips(V)));
+    if (!few_rows(N)) tc_layout(s, base, at, N, C, V);
+    return at;
+}
+
+size_t bwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K, int piece) {
+    size_t at = kHeadHeader;
+    s = Scratch{};
+    s.head = (HeadHeader*)base;
+    s.rows = take<RowParams>(base, at, N);
+    s.eid = take<int>(base, at, (size_t)N * K);
+    s.ep = take<float>(base, at, (size_t)N * K);
+    if (few_rows(N)) {
+        s.u = take<float>(base, at, (size_t)V * kRows);
+        s.dx_part = take<float>(base, at, (size_t)kStrips * kRows * C);
+        return at;
+    }
+    tc_layout(s, base, at, N, C, V);
+    s.ypart = take<float>(base, at, kParts);
+    s.rowmax = take<float>(base, at, N);
+    s.y16 = take<__half>(base, at, 2 * (size_t)N * C);
+    s.u16 = take<__half>(base, at, 2 * (size_t)N * piece_columns(N, V, piece));
+    s.partials = take<float>(base, at, head_partial_bytes() / sizeof(float));
+    return at;
 }
 
 __device__ __forceinline__ float4 ld_value(const float* hi, const float* lo, int64_t i4) {
@@ -107,17 +150,17 @@ __device__ __forceinline__ float warp_dots(const float4* xs, int C4, const float
     return z;
 }
 
-__device__ __forceinline__ void rows_to_smem(float4* xs, const float* x, const float* x_lo, int64_t row0, int rows, int NR, int C4) {
+__device__ __forceinline__ void rows_to_smem(float4* xs, const float* x, const float* x_lo, int rows, int NR, int C4) {
     for (int i = threadIdx.x; i < NR * C4; i += kThreads) {
         const int n = i / C4;
-        xs[i] = n < rows ? ld_value(x, x_lo, (row0 + n) * C4 + (i - n * C4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        xs[i] = n < rows ? ld_value(x, x_lo, i) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     __syncthreads();
 }
 
 // Row statistics over a strip of the vocabulary, in units of log 2.
 template <int NR, int RV>
-__global__ void __launch_bounds__(kThreads) head_stats_rows_kernel(const HeadArgs g, int64_t row0, int rows, float2* stats,
+__global__ void __launch_bounds__(kThreads) head_stats_rows_kernel(const HeadArgs g, int rows, float2* stats,
                                                                    HeadHeader* head) {
     extern __shared__ float4 xs[];
     __shared__ float2 part[kThreads];
@@ -125,7 +168,7 @@ __global__ void __launch_bounds__(kThreads) head_stats_rows_kernel(const HeadArg
     pdl_trigger();
     if (blockIdx.x == 0 && threadIdx.x == 0) *head = HeadHeader{0, 0u};
     const int C4 = g.C / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    rows_to_smem(xs, g.x, g.x_lo, row0, rows, NR, C4);
+    rows_to_smem(xs, g.x, g.x_lo, rows, NR, C4);
     constexpr int R = RV * NR, kShare = 32 / R;
     const int idx = lane / kShare, vi = idx / NR;
     const float f = kLog2e / g.aim.tau;
@@ -146,7 +189,7 @@ __global__ void __launch_bounds__(kThreads) head_stats_rows_kernel(const HeadArg
             if ((((i & 31) / kShare) % NR) == threadIdx.x && part[i].y != 0.f) m = fmaxf(m, part[i].x);
         for (int i = 0; i < kThreads; ++i)
             if ((((i & 31) / kShare) % NR) == threadIdx.x && part[i].y != 0.f) s += part[i].y * ex2_fast(part[i].x - m);
-        stats[(row0 + threadIdx.x) * gridDim.x + blockIdx.x] = make_float2(m, s);
+        stats[threadIdx.x * gridDim.x + blockIdx.x] = make_float2(m, s);
     }
 }
 
@@ -204,9 +247,14 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_kernel(const HeadA
     if (g.loss_mean) mean_by_last<kFinishThreads>(g.aim, g.losses, g.N, &head->rows_done, gridDim.x, g.loss_mean, smd);
 }
 
+// Planes: the hi plane stands for the value, whose largest it bounds within 2^-11 of itself.
+__device__ __forceinline__ float max4(float m, float4 v) {
+    return fmaxf(fmaxf(m, fmaxf(fabsf(v.x), fabsf(v.y))), fmaxf(fabsf(v.z), fabsf(v.w)));
+}
+
 // One row per CTA: what the backward needs to know of it.  Entries with the same id are joined into the first of them.
 __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArgs g, RowParams* rows, int* eid, float* ep,
-                                                                   HeadHeader* head) {
+                                                                   float* rowmax, HeadHeader* head) {
     extern __shared__ int ids[];            // [K], then the weights [K]
     __shared__ float smf[kFinishThreads / 32];
     pdl_wait();
@@ -257,21 +305,27 @@ __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArg
         r.target = -1;
     }
     if (threadIdx.x == 0) rows[row] = r;
+    if (rowmax && live) {                   // the same for all threads
+        float m = 0.f;
+        for (int c = threadIdx.x; c < g.C / 4; c += kFinishThreads) m = max4(m, ld4(g.x, row * (g.C / 4) + c));
+        m = block_all<kFinishThreads>(m, smf, MaxOp());
+        if (threadIdx.x == 0) rowmax[row] = m;
+    }
 }
 
 // u[v][n] = g_n (q_nv - [v = target]) for the rows of one launch.
 template <int NR, int RV>
-__global__ void __launch_bounds__(kThreads) head_grad_rows_kernel(const HeadArgs g, int64_t row0, int rows,
+__global__ void __launch_bounds__(kThreads) head_grad_rows_kernel(const HeadArgs g, int rows,
                                                                   const RowParams* __restrict__ params, float* __restrict__ u) {
     extern __shared__ float4 xs[];
     pdl_wait();
     pdl_trigger();
     const int C4 = g.C / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    rows_to_smem(xs, g.x, g.x_lo, row0, rows, NR, C4);
+    rows_to_smem(xs, g.x, g.x_lo, rows, NR, C4);
     constexpr int kShare = 32 / (RV * NR);
     const int idx = lane / kShare, vi = idx / NR, n = idx % NR;
     const float f = kLog2e / g.aim.tau;
-    const RowParams r = n < rows ? params[row0 + n] : RowParams{INFINITY, 0.f, -1};
+    const RowParams r = n < rows ? params[n] : RowParams{INFINITY, 0.f, -1};
     for (int64_t v0 = ((int64_t)blockIdx.x * (kThreads / 32) + warp) * RV; v0 < g.V; v0 += (int64_t)gridDim.x * (kThreads / 32) * RV) {
         const float z = warp_dots<NR, RV>(xs, C4, g.w, g.w_lo, v0, g.V) * f;
         const int64_t v = v0 + vi;
@@ -281,20 +335,20 @@ __global__ void __launch_bounds__(kThreads) head_grad_rows_kernel(const HeadArgs
 }
 
 // The teacher's part of u.
-__global__ void __launch_bounds__(256) head_grad_entries_kernel(int64_t row0, int rows, int NR, int K, const RowParams* __restrict__ params,
+__global__ void __launch_bounds__(256) head_grad_entries_kernel(int rows, int NR, int K, const RowParams* __restrict__ params,
                                                                 const int* __restrict__ eid, const float* __restrict__ ep, float* u) {
     pdl_wait();
     pdl_trigger();
     const int i = blockIdx.x * 256 + threadIdx.x;
     if (i >= rows * K) return;
-    const int n = i / K, id = eid[row0 * K + i];
-    if (id >= 0) u[(int64_t)id * NR + n] -= params[row0 + n].g * ep[row0 * K + i];
+    const int n = i / K, id = eid[i];
+    if (id >= 0) u[(int64_t)id * NR + n] -= params[n].g * ep[i];
 }
 
 // dW_v = sum_n u_vn x_n and a strip's part of dx_n = sum_v u_vn W_v: a thread owns four columns and reads u of a row of
 // W as all threads of its threadIdx.y do.
 template <int NR>
-__global__ void __launch_bounds__(kThreads) head_products_rows_kernel(const HeadArgs g, int64_t row0, int rows, const float* __restrict__ u,
+__global__ void __launch_bounds__(kThreads) head_products_rows_kernel(const HeadArgs g, int rows, const float* __restrict__ u,
                                                                   float* dx_part) {
     pdl_wait();
     pdl_trigger();
@@ -303,7 +357,7 @@ __global__ void __launch_bounds__(kThreads) head_products_rows_kernel(const Head
     float4 xv[NR], acc[NR];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-        xv[n] = n < rows ? ld_value(g.x, g.x_lo, (row0 + n) * C4 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+        xv[n] = n < rows ? ld_value(g.x, g.x_lo, n * C4 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
         acc[n] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     const int lanes = gridDim.x * blockDim.y;
@@ -325,7 +379,7 @@ __global__ void __launch_bounds__(kThreads) head_products_rows_kernel(const Head
         }
         if (g.dw) {
             float4* out = reinterpret_cast<float4*>(g.dw) + v * C4 + c;
-            *out = row0 ? add4(*out, d) : d;
+            *out = d;
         }
     }
     if (g.dx || g.dx_hi) {
@@ -335,7 +389,7 @@ __global__ void __launch_bounds__(kThreads) head_products_rows_kernel(const Head
     }
 }
 
-__global__ void __launch_bounds__(256) head_dx_rows_kernel(const HeadArgs g, int64_t row0, int rows, int NR, int parts,
+__global__ void __launch_bounds__(256) head_dx_rows_kernel(const HeadArgs g, int rows, int NR, int parts,
                                                            const float* __restrict__ dx_part) {
     __shared__ float4 sm[8][32];
     pdl_wait();
@@ -351,36 +405,192 @@ __global__ void __launch_bounds__(256) head_dx_rows_kernel(const HeadArgs g, int
     __syncthreads();
     if (y == 0 && i < rows * C4) {
         for (int k = 1; k < 8; ++k) t = add4(t, sm[k][lane]);
-        store_raw_split(t, g.dx, g.dx_hi, g.dx_lo, row0 * C4 + i);
+        store_raw_split(t, g.dx, g.dx_hi, g.dx_lo, i);
     }
+}
+
+// ---------------------------------------------------------------- FP16 pairs
+
+// The k with 2^k m in [2^14, 2^15), where 2^k is an FP32 number.
+__device__ __forceinline__ int pair_exponent(float m) {
+    const int e = (int)((__float_as_uint(m) >> 23) & 255u) - 127;
+    return min(14 - e, 126);                // zero and denormal numbers: e = -127
+}
+__device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
+
+// Largest absolute values of W, and of y_nc = g_n x_nc (backward), per CTA.
+__global__ void __launch_bounds__(kThreads) head_max_kernel(const HeadArgs g, const RowParams* __restrict__ rows,
+                                                            const float* __restrict__ rowmax, float* wpart, float* ypart, HeadHeader* head) {
+    __shared__ float smf[kThreads / 32];
+    pdl_wait();
+    pdl_trigger();
+    if (head && blockIdx.x == 0 && threadIdx.x == 0) *head = HeadHeader{0, 0u};
+    const int64_t n4 = (int64_t)g.V * (g.C / 4), step = (int64_t)gridDim.x * kThreads;
+    float m = 0.f;
+#pragma unroll 8
+    for (int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x; i < n4; i += step) m = max4(m, ld4(g.w, i));
+    m = block_all<kThreads>(m, smf, MaxOp());
+    if (threadIdx.x == 0) wpart[blockIdx.x] = m;
+    if (!rows) return;
+    m = 0.f;
+    for (int64_t n = blockIdx.x * (int64_t)kThreads + threadIdx.x; n < g.N; n += step)
+        if (rows[n].g != 0.f) m = fmaxf(m, fabsf(rows[n].g) * rowmax[n]);
+    m = block_all<kThreads>(m, smf, MaxOp());
+    if (threadIdx.x == 0) ypart[blockIdx.x] = m;
+}
+
+// Four values times s as pairs.
+__device__ __forceinline__ void pairs4(float4 v, float s, uint2& hi, uint2& lo) {
+    const float t[4] = {v.x * s, v.y * s, v.z * s, v.w * s};
+    const __half2 a = __floats2half2_rn(t[0], t[1]), b = __floats2half2_rn(t[2], t[3]);
+    const float2 fa = __half22float2(a), fb = __half22float2(b);
+    const __half2 c = __floats2half2_rn(t[0] - fa.x, t[1] - fa.y), d = __floats2half2_rn(t[2] - fb.x, t[3] - fb.y);
+    hi = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+    lo = make_uint2(*reinterpret_cast<const uint32_t*>(&c), *reinterpret_cast<const uint32_t*>(&d));
+}
+
+// W and x, and y for the backward, as pairs: W and y at one power of two, the rows of x each at its own.
+__global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, const RowParams* __restrict__ rows, const Scratch s) {
+    __shared__ float smf[kThreads / 32];
+    pdl_wait();
+    pdl_trigger();
+    float m = 0.f, my = 0.f;
+    for (int i = threadIdx.x; i < kParts; i += kThreads) {
+        m = fmaxf(m, s.wpart[i]);
+        if (rows) my = fmaxf(my, s.ypart[i]);
+    }
+    const int kw = pair_exponent(block_all<kThreads>(m, smf, MaxOp())), ky = rows ? pair_exponent(block_all<kThreads>(my, smf, MaxOp())) : 0;
+    if (rows && blockIdx.x == 0 && threadIdx.x == 0) *s.scales = Scales{ldexpf(1.0f, -15 - kw), ldexpf(1.0f, -15 - ky)};
+    const int64_t n8 = (int64_t)g.V * g.C / 8, step = (int64_t)gridDim.x * kThreads;
+    const float sw = pow2(kw);
+#pragma unroll 4
+    for (int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x; i < n8; i += step) {
+        uint2 h0, l0, h1, l1;
+        pairs4(ld_value(g.w, g.w_lo, 2 * i), sw, h0, l0);
+        pairs4(ld_value(g.w, g.w_lo, 2 * i + 1), sw, h1, l1);
+        reinterpret_cast<uint4*>(s.w16)[i] = make_uint4(h0.x, h0.y, h1.x, h1.y);
+        reinterpret_cast<uint4*>(s.w16)[n8 + i] = make_uint4(l0.x, l0.y, l1.x, l1.y);
+    }
+    const int C4 = g.C / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t nx = g.N * C4;
+    for (int64_t row = blockIdx.x * (int64_t)(kThreads / 32) + warp; row < g.N; row += gridDim.x * (int64_t)(kThreads / 32)) {
+        float mx = 0.f;
+        for (int c = lane; c < C4; c += 32) mx = max4(mx, ld4(g.x, row * C4 + c));
+        const int kx = pair_exponent(warp_max(mx));
+        const float sx = pow2(kx), sy = pow2(ky), gr = rows ? rows[row].g : 0.f;
+        for (int c = lane; c < C4; c += 32) {
+            const float4 v = ld_value(g.x, g.x_lo, row * C4 + c);
+            uint2 h, l;
+            pairs4(v, sx, h, l);
+            reinterpret_cast<uint2*>(s.x16)[row * C4 + c] = h;
+            reinterpret_cast<uint2*>(s.x16)[nx + row * C4 + c] = l;
+            if (!rows) continue;
+            pairs4(make_float4(v.x * gr, v.y * gr, v.z * gr, v.w * gr), sy, h, l);
+            if (gr == 0.f) h = l = make_uint2(0u, 0u);          // whatever the row holds
+            reinterpret_cast<uint2*>(s.y16)[row * C4 + c] = h;
+            reinterpret_cast<uint2*>(s.y16)[nx + row * C4 + c] = l;
+        }
+        // scores whose factor leaves this range are zero to FP32, or beyond it
+        if (lane == 0) s.rowf[row] = ldexpf(kLog2e / g.aim.tau, max(-120, min(120, -kx - kw)));
+    }
+}
+
+// The teacher's part of a piece of u.
+__global__ void __launch_bounds__(256) head_pair_entries_kernel(int64_t N, int K, const int* __restrict__ eid, const float* __restrict__ ep, int v0,
+                                                                int cols, __half* u, int64_t ldu, int64_t plane) {
+    pdl_wait();
+    pdl_trigger();
+    for (int64_t i = blockIdx.x * 256LL + threadIdx.x; i < N * K; i += gridDim.x * 256LL) {
+        const int c = eid[i] - v0;
+        if (eid[i] < 0 || c < 0 || c >= cols) continue;
+        __half* p = u + i / K * ldu + c;
+        const float t = (__half2float(p[0]) + __half2float(p[plane])) - 32768.0f * ep[i];
+        p[0] = __float2half_rn(t);
+        p[plane] = __float2half_rn(t - __half2float(p[0]));
+    }
+}
+
+// Raw values at `hi` as planes.
+__global__ void __launch_bounds__(256) head_planes_kernel(const float* x, float* hi, float* lo, int64_t n4) {
+    pdl_wait();
+    pdl_trigger();
+    for (int64_t i = blockIdx.x * 256LL + threadIdx.x; i < n4; i += gridDim.x * 256LL) store_raw_split(ld4(x, i), nullptr, hi, lo, i);
+}
+
+int grid_for(int64_t threads, int most) {
+    const int64_t n = (threads + 255) / 256;
+    return (int)(n < 1 ? 1 : n < most ? n : most);
+}
+
+cudaError_t make_pairs(const HeadArgs& g, const Scratch& w, bool back, cudaStream_t s) {
+    BT_KERNEL_LAUNCH((head_max_kernel), kParts, kThreads, 0, s, g, back ? w.rows : nullptr, w.rowmax, w.wpart, w.ypart, back ? nullptr : w.head);
+    BT_COUNT_LAUNCH();
+    BT_KERNEL_LAUNCH((head_pairs_kernel), 148 * 8, kThreads, 0, s, g, back ? w.rows : nullptr, w);
+    BT_COUNT_LAUNCH();
+    return cudaGetLastError();
+}
+
+HalfMat pair_matrix(const __half* p, int64_t rows, int64_t cols) { return HalfMat{p, rows * cols, rows, cols, cols}; }
+
+cudaError_t backward_in_pieces(const HeadArgs& g, const Scratch& w, int K, cudaStream_t s) {
+    cudaError_t e = make_pairs(g, w, true, s);
+    if (e != cudaSuccess) return e;
+    const HalfMat x = pair_matrix(w.x16, g.N, g.C), y = pair_matrix(w.y16, g.N, g.C);
+    const int ldu = piece_columns(g.N, g.V, g.piece);
+    float* dx = g.dx ? g.dx : g.dx_hi;      // sums over the pieces go where the result will be
+    for (int v0 = 0; v0 < g.V; v0 += ldu) {
+        const int cols = g.V - v0 < ldu ? g.V - v0 : ldu;
+        const HalfMat wp{w.w16 + (int64_t)v0 * g.C, (int64_t)g.V * g.C, cols, g.C, g.C}, u{w.u16, g.N * ldu, g.N, cols, ldu};
+        e = launch_head_grad(x, wp, v0, w.rowf, w.rows, w.u16, ldu, u.plane, &w.head->err, s);
+        if (e == cudaSuccess && K) {
+            BT_KERNEL_LAUNCH((head_pair_entries_kernel), grid_for(g.N * K, 148 * 8), 256, 0, s, g.N, K, (const int*)w.eid, (const float*)w.ep, v0,
+                             cols, w.u16, (int64_t)ldu, u.plane);
+            BT_COUNT_LAUNCH();
+        }
+        if (e == cudaSuccess && dx) e = launch_head_dx(u, wp, w.rows, &w.scales->dx, v0 > 0, dx, w.partials, &w.head->err, s);
+        if (e == cudaSuccess && g.dw) e = launch_head_dw(u, y, &w.scales->dw, g.dw + (int64_t)v0 * g.C, w.partials, &w.head->err, s);
+        if (e != cudaSuccess) return e;
+    }
+    if (g.dx_hi) {
+        BT_KERNEL_LAUNCH((head_planes_kernel), grid_for(g.N * g.C / 4, 148 * 8), 256, 0, s, (const float*)dx, g.dx_hi, g.dx_lo, g.N * g.C / 4);
+        BT_COUNT_LAUNCH();
+    }
+    return cudaGetLastError();
 }
 
 constexpr size_t rows_smem(int NR, int C) { return (size_t)NR * C * sizeof(float); }
 
 }  // namespace
 
-size_t head_fwd_scratch_bytes(int64_t N, int C, int V, int K) {
+size_t head_fwd_scratch_bytes(int64_t N, int C, int V, int) {
     Scratch s;
-    return fwd_layout(s, nullptr, N);
+    return fwd_layout(s, nullptr, N, C, V);
 }
 
 size_t head_bwd_scratch_bytes(int64_t N, int C, int V, int K, int piece) {
+    if (N < 1) return kHeadHeader;
     Scratch s;
-    return bwd_layout(s, nullptr, N, C, V, K);
+    return bwd_layout(s, nullptr, N, C, V, K, piece);
 }
 
 cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     Scratch w;
-    fwd_layout(w, g.scratch, g.N);
-    const size_t smem = rows_smem(kRows, g.C);
-    cudaError_t e = allow_smem<head_stats_rows_kernel<8, 4>>(rows_smem(kRows, 4096));
-    if (e != cudaSuccess) return e;
-    for (int64_t row0 = 0; row0 < g.N; row0 += kRows) {
-        const int rows = (int)(g.N - row0 < kRows ? g.N - row0 : kRows);
-        BT_KERNEL_LAUNCH((head_stats_rows_kernel<8, 4>), kStrips, kThreads, smem, s, g, row0, rows, w.stats, w.head);
+    fwd_layout(w, g.scratch, g.N, g.C, g.V);
+    cudaError_t e;
+    int strips = kStrips;
+    if (few_rows(g.N)) {
+        e = allow_smem<head_stats_rows_kernel<8, 4>>(rows_smem(kRows, 4096));
+        if (e != cudaSuccess) return e;
+        BT_KERNEL_LAUNCH((head_stats_rows_kernel<8, 4>), kStrips, kThreads, rows_smem(kRows, g.C), s, g, (int)g.N, w.stats, w.head);
         BT_COUNT_LAUNCH();
+    } else {
+        strips = head_stats_strips(g.V);
+        e = make_pairs(g, w, false, s);
+        if (e == cudaSuccess)
+            e = launch_head_stats(pair_matrix(w.x16, g.N, g.C), pair_matrix(w.w16, g.V, g.C), w.rowf, w.stats, &w.head->err, s);
+        if (e != cudaSuccess) return e;
     }
-    BT_KERNEL_LAUNCH((head_finish_kernel), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, kStrips, w.head);
+    BT_KERNEL_LAUNCH((head_finish_kernel), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }
@@ -388,29 +598,25 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
 cudaError_t launch_head_bwd(const HeadArgs& g, cudaStream_t s) {
     Scratch w;
     const int K = g.aim.targets ? 0 : g.aim.K, C4 = g.C / 4;
-    bwd_layout(w, g.scratch, g.N, g.C, g.V, K);
+    bwd_layout(w, g.scratch, g.N, g.C, g.V, K, g.piece);
     cudaError_t e = allow_smem<head_grad_rows_kernel<8, 4>>(rows_smem(kRows, 4096));
     if (e != cudaSuccess) return e;
-    BT_KERNEL_LAUNCH((head_rows_kernel), (unsigned)g.N, kFinishThreads, (size_t)K * 8, s, g, w.rows, w.eid, w.ep, w.head);
+    BT_KERNEL_LAUNCH((head_rows_kernel), (unsigned)g.N, kFinishThreads, (size_t)K * 8, s, g, w.rows, w.eid, w.ep, w.rowmax, w.head);
     BT_COUNT_LAUNCH();
-    const int tx = C4 < kThreads ? C4 : kThreads, ry = kThreads / tx, strips = kStrips / ry;
-    for (int64_t row0 = 0; row0 < g.N; row0 += kRows) {
-        const int rows = (int)(g.N - row0 < kRows ? g.N - row0 : kRows);
-        BT_KERNEL_LAUNCH((head_grad_rows_kernel<8, 4>), kStrips, kThreads, rows_smem(kRows, g.C), s, g, row0, rows,
-                         (const RowParams*)w.rows, w.u);
+    if (!few_rows(g.N)) return backward_in_pieces(g, w, K, s);
+    const int rows = (int)g.N, tx = C4 < kThreads ? C4 : kThreads, ry = kThreads / tx, strips = kStrips / ry;
+    BT_KERNEL_LAUNCH((head_grad_rows_kernel<8, 4>), kStrips, kThreads, rows_smem(kRows, g.C), s, g, rows, (const RowParams*)w.rows, w.u);
+    BT_COUNT_LAUNCH();
+    if (K) {
+        BT_KERNEL_LAUNCH((head_grad_entries_kernel), (rows * K + 255) / 256, 256, 0, s, rows, kRows, K, (const RowParams*)w.rows,
+                         (const int*)w.eid, (const float*)w.ep, w.u);
         BT_COUNT_LAUNCH();
-        if (K) {
-            BT_KERNEL_LAUNCH((head_grad_entries_kernel), (rows * K + 255) / 256, 256, 0, s, row0, rows, kRows, K,
-                             (const RowParams*)w.rows, (const int*)w.eid, (const float*)w.ep, w.u);
-            BT_COUNT_LAUNCH();
-        }
-        BT_KERNEL_LAUNCH((head_products_rows_kernel<8>), dim3(strips, (C4 + tx - 1) / tx), dim3(tx, ry), 0, s, g, row0, rows, (const float*)w.u, w.dx_part);
+    }
+    BT_KERNEL_LAUNCH((head_products_rows_kernel<8>), dim3(strips, (C4 + tx - 1) / tx), dim3(tx, ry), 0, s, g, rows, (const float*)w.u, w.dx_part);
+    BT_COUNT_LAUNCH();
+    if (g.dx || g.dx_hi) {
+        BT_KERNEL_LAUNCH((head_dx_rows_kernel), (rows * C4 + 31) / 32, 256, 0, s, g, rows, kRows, strips * ry, (const float*)w.dx_part);
         BT_COUNT_LAUNCH();
-        if (g.dx || g.dx_hi) {
-            BT_KERNEL_LAUNCH((head_dx_rows_kernel), (rows * C4 + 31) / 32, 256, 0, s, g, row0, rows, kRows, strips * ry,
-                             (const float*)w.dx_part);
-            BT_COUNT_LAUNCH();
-        }
     }
     return cudaGetLastError();
 }

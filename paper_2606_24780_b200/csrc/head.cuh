@@ -1,5 +1,6 @@
 // The losses at the language-model head: row arithmetic and scratch shared by their kernels.
 #pragma once
+#include <cuda_fp16.h>
 #include <math.h>
 
 #include "common.cuh"
@@ -16,6 +17,29 @@ struct HeadHeader {
 };
 constexpr size_t kHeadHeader = 256;
 inline size_t head_pad(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+
+struct RowParams {                          // backward, per row
+    float L;                                // lse in units of log 2; +inf: the row has no part in the loss
+    float g;                                // inv_count w tau S
+    int target;                             // column whose aim is 1; below zero: none
+};
+
+// The tensor-core products (head_tc.cu).  An operand: FP16 pairs, lo plane at hi + plane, ld values between rows.
+struct HalfMat {
+    const __half* hi;
+    int64_t plane, rows, cols, ld;
+};
+int head_stats_strips(int V);
+size_t head_partial_bytes();
+// stats [N][head_stats_strips(V)] = (maximum, sum) of z in units of log 2 over strips of columns; rowf: from accumulators there.
+cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, float2* stats, int* err, cudaStream_t s);
+// u = 2^15 (q - [v = target]) as pairs for the columns v0 .. v0 + w.rows - 1, zero in rows without part in the loss.
+cudaError_t launch_head_grad(const HalfMat& x, const HalfMat& w, int v0, const float* rowf, const RowParams* rows, __half* u, int64_t ldu,
+                             int64_t u_plane, int* err, cudaStream_t s);
+// dx = (+ dx) g_n scale u W;  dw = scale u^T y.
+cudaError_t launch_head_dx(const HalfMat& u, const HalfMat& w, const RowParams* rows, const float* scale, bool onto, float* dx, float* partials,
+                           int* err, cudaStream_t s);
+cudaError_t launch_head_dw(const HalfMat& u, const HalfMat& y, const float* scale, float* dw, float* partials, int* err, cudaStream_t s);
 
 // Logit of entry k of a row in units of the softened softmax, -inf where there is none (a weight of zero).  An id
 // behind the vocabulary counts as id 0 and is recorded.
