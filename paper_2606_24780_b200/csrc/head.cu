@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kRows = 8;                    // rows of x that the plain kernels carry
 constexpr int kParts = 592;                 // CTAs that look for the largest value
-constexpr int kStrips = 592;                // CTAs over the vocabulary (4 per SM)
+constexpr int kStrips = 296;                // CTAs over the vocabulary (2 per SM)
 constexpr int kThreads = 256;
 constexpr int kFinishThreads = 256;
 
@@ -110,10 +110,17 @@ __device__ __forceinline__ float dot4(float4 a, float4 b, float acc) {
     return fmaf(a.w, b.w, fmaf(a.z, b.z, fmaf(a.y, b.y, fmaf(a.x, b.x, acc))));
 }
 
-// Dot products of RV consecutive rows of W with the NR rows of x in shared memory, by one warp.  Lane l returns the one
+// The rows of W that this warp of the grid takes, to within one as many as any other.
+__device__ __forceinline__ void warp_share(int V, int64_t& v0, int64_t& v1) {
+    const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), all = (int64_t)gridDim.x * (kThreads / 32);
+    v0 = w * V / all;
+    v1 = (w + 1) * V / all;
+}
+
+// Dot products of RV consecutive rows of W (fewer before v1) with the NR rows of x in shared memory, by one warp.  Lane l returns the one
 // of row l / (32 / (RV NR)) / NR of W and row (that) % NR of x; lanes that share a product hold it alike.
 template <int NR, int RV>
-__device__ __forceinline__ float warp_dots(const float4* xs, int C4, const float* w, const float* w_lo, int64_t v0, int V) {
+__device__ __forceinline__ float warp_dots(const float4* xs, int C4, const float* w, const float* w_lo, int64_t v0, int64_t v1) {
     const int lane = threadIdx.x & 31;
     constexpr int R = RV * NR;
     float acc[R];
@@ -121,7 +128,7 @@ __device__ __forceinline__ float warp_dots(const float4* xs, int C4, const float
     for (int i = 0; i < R; ++i) acc[i] = 0.f;
     int64_t at[RV];
 #pragma unroll
-    for (int i = 0; i < RV; ++i) at[i] = (v0 + i < V ? v0 + i : V - 1) * C4;
+    for (int i = 0; i < RV; ++i) at[i] = (v0 + i < v1 ? v0 + i : v1 - 1) * C4;
 #pragma unroll 2
     for (int c = lane; c < C4; c += 32) {
         float4 wv[RV];
@@ -160,22 +167,24 @@ __device__ __forceinline__ void rows_to_smem(float4* xs, const float* x, const f
 
 // Row statistics over a strip of the vocabulary, in units of log 2.
 template <int NR, int RV>
-__global__ void __launch_bounds__(kThreads) head_stats_rows_kernel(const HeadArgs g, int rows, float2* stats,
+__global__ void __launch_bounds__(kThreads, 2) head_stats_rows_kernel(const HeadArgs g, int rows, float2* stats,
                                                                    HeadHeader* head) {
     extern __shared__ float4 xs[];
     __shared__ float2 part[kThreads];
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0 && threadIdx.x == 0) *head = HeadHeader{0, 0u};
-    const int C4 = g.C / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int C4 = g.C / 4, lane = threadIdx.x & 31;
     rows_to_smem(xs, g.x, g.x_lo, rows, NR, C4);
     constexpr int R = RV * NR, kShare = 32 / R;
     const int idx = lane / kShare, vi = idx / NR;
     const float f = kLog2e / g.aim.tau;
     float m = -INFINITY, s = 0.f;
-    for (int64_t v0 = ((int64_t)blockIdx.x * (kThreads / 32) + warp) * RV; v0 < g.V; v0 += (int64_t)gridDim.x * (kThreads / 32) * RV) {
-        const float z = warp_dots<NR, RV>(xs, C4, g.w, g.w_lo, v0, g.V) * f;
-        if (v0 + vi < g.V) {
+    int64_t v0, v1;
+    warp_share(g.V, v0, v1);
+    for (; v0 < v1; v0 += RV) {
+        const float z = warp_dots<NR, RV>(xs, C4, g.w, g.w_lo, v0, v1) * f;
+        if (v0 + vi < v1) {
             const float m1 = fmaxf(m, z);
             s = s * ex2_fast(m - m1) + ex2_fast(z - m1);
             m = m1;
@@ -247,6 +256,49 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_kernel(const HeadA
     if (g.loss_mean) mean_by_last<kFinishThreads>(g.aim, g.losses, g.N, &head->rows_done, gridDim.x, g.loss_mean, smd);
 }
 
+// The same for targets, a row per warp: with 8,192 rows the CTA per row above takes 88 us, most of it barriers, this 9.
+__global__ void __launch_bounds__(kFinishThreads) head_finish_target_kernel(const HeadArgs g, const float2* __restrict__ stats, int strips,
+                                                                            HeadHeader* head) {
+    __shared__ double smd[kFinishThreads / 32];
+    pdl_wait();
+    pdl_trigger();
+    const int64_t row = blockIdx.x * (int64_t)(kFinishThreads / 32) + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    if (row < g.N) {
+        int t = g.aim.targets[row];
+        if (t >= g.V) {
+            if (g.bad && lane == 0) atomicCAS(g.bad, 0, (int)row + 1);
+            t = 0;
+        }
+        const float2* st = stats + row * strips;
+        float m = -INFINITY, s = 0.f, z = 0.f;
+#pragma unroll 4
+        for (int i = lane; i < strips; i += 32) {
+            const float2 p = st[i];
+            if (p.y != 0.f) {
+                const float m1 = fmaxf(m, p.x);
+                s = s * ex2_fast(m - m1) + p.y * ex2_fast(p.x - m1);
+                m = m1;
+            }
+        }
+        const float top = warp_max(m);
+        s = warp_sum(s != 0.f ? s * ex2_fast(m - top) : 0.f);       // a lane without strips has the sum zero
+        const float lse = (top + log2f(s)) * kLn2;
+        const int C4 = g.C / 4;
+        if (t >= 0) {
+#pragma unroll 4
+            for (int c = lane; c < C4; c += 32)
+                z = dot4(ld_value(g.x, g.x_lo, row * C4 + c), ld_value(g.w, g.w_lo, (int64_t)t * C4 + c), z);
+            z = warp_sum(z);
+        }
+        if (lane == 0) {
+            if (g.lse) g.lse[row] = lse;
+            g.losses[row] = t >= 0 ? lse - z : 0.f;
+        }
+    }
+    if (g.loss_mean) mean_by_last<kFinishThreads>(g.aim, g.losses, g.N, &head->rows_done, gridDim.x, g.loss_mean, smd);
+}
+
 // Planes: the hi plane stands for the value, whose largest it bounds within 2^-11 of itself.
 __device__ __forceinline__ float max4(float m, float4 v) {
     return fmaxf(fmaxf(m, fmaxf(fabsf(v.x), fabsf(v.y))), fmaxf(fabsf(v.z), fabsf(v.w)));
@@ -263,7 +315,9 @@ __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArg
     const int64_t row = blockIdx.x;
     const LossAim& a = g.aim;
     RowParams r;
-    r.L = g.lse_in[row] * kLog2e;
+    const double L = (double)g.lse_in[row] * 1.4426950408889634;
+    r.L = (float)L;
+    r.L_rest = isfinite(r.L) ? (float)(L - (double)r.L) : 0.f;
     r.g = a.inv_count * row_weight(a, row) * a.tau;
     r.target = -1;
     bool live = r.g != 0.f;
@@ -301,6 +355,7 @@ __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArg
     }
     if (!live) {
         r.L = INFINITY;
+        r.L_rest = 0.f;
         r.g = 0.f;
         r.target = -1;
     }
@@ -315,22 +370,24 @@ __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArg
 
 // u[v][n] = g_n (q_nv - [v = target]) for the rows of one launch.
 template <int NR, int RV>
-__global__ void __launch_bounds__(kThreads) head_grad_rows_kernel(const HeadArgs g, int rows,
+__global__ void __launch_bounds__(kThreads, 2) head_grad_rows_kernel(const HeadArgs g, int rows,
                                                                   const RowParams* __restrict__ params, float* __restrict__ u) {
     extern __shared__ float4 xs[];
     pdl_wait();
     pdl_trigger();
-    const int C4 = g.C / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int C4 = g.C / 4, lane = threadIdx.x & 31;
     rows_to_smem(xs, g.x, g.x_lo, rows, NR, C4);
     constexpr int kShare = 32 / (RV * NR);
     const int idx = lane / kShare, vi = idx / NR, n = idx % NR;
     const float f = kLog2e / g.aim.tau;
-    const RowParams r = n < rows ? params[n] : RowParams{INFINITY, 0.f, -1};
-    for (int64_t v0 = ((int64_t)blockIdx.x * (kThreads / 32) + warp) * RV; v0 < g.V; v0 += (int64_t)gridDim.x * (kThreads / 32) * RV) {
-        const float z = warp_dots<NR, RV>(xs, C4, g.w, g.w_lo, v0, g.V) * f;
+    const RowParams r = n < rows ? params[n] : RowParams{INFINITY, 0.f, 0.f, -1};
+    int64_t v0, v1;
+    warp_share(g.V, v0, v1);
+    for (; v0 < v1; v0 += RV) {
+        const float z = warp_dots<NR, RV>(xs, C4, g.w, g.w_lo, v0, v1);
         const int64_t v = v0 + vi;
-        if (v < g.V && (lane & (kShare - 1)) == 0)
-            u[v * NR + n] = r.L == INFINITY ? 0.f : r.g * (ex2_fast(z - r.L) - (v == r.target ? 1.f : 0.f));
+        if (v < v1 && (lane & (kShare - 1)) == 0)
+            u[v * NR + n] = r.L == INFINITY ? 0.f : r.g * (ex2_fast(fmaf(z, f, -r.L) - r.L_rest) - (v == r.target ? 1.f : 0.f));
     }
 }
 
@@ -348,7 +405,7 @@ __global__ void __launch_bounds__(256) head_grad_entries_kernel(int rows, int NR
 // dW_v = sum_n u_vn x_n and a strip's part of dx_n = sum_v u_vn W_v: a thread owns four columns and reads u of a row of
 // W as all threads of its threadIdx.y do.
 template <int NR>
-__global__ void __launch_bounds__(kThreads) head_products_rows_kernel(const HeadArgs g, int rows, const float* __restrict__ u,
+__global__ void __launch_bounds__(kThreads, 2) head_products_rows_kernel(const HeadArgs g, int rows, const float* __restrict__ u,
                                                                   float* dx_part) {
     pdl_wait();
     pdl_trigger();
@@ -360,15 +417,21 @@ __global__ void __launch_bounds__(kThreads) head_products_rows_kernel(const Head
         xv[n] = n < rows ? ld_value(g.x, g.x_lo, n * C4 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
         acc[n] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    const int lanes = gridDim.x * blockDim.y;
-    for (int64_t v = blockIdx.x * blockDim.y + threadIdx.y; v < g.V; v += lanes) {
+    const int64_t lanes = (int64_t)gridDim.x * blockDim.y, at = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, v1 = (at + 1) * g.V / lanes;
+#pragma unroll 4
+    for (int64_t v = at * g.V / lanes; v < v1; ++v) {
         const float4 wv = g.dx_hi || g.dx ? ld_value(g.w, g.w_lo, v * C4 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
         float4 d = make_float4(0.f, 0.f, 0.f, 0.f);
         float uv[NR];
+        if (NR >= 4) {
 #pragma unroll
-        for (int n = 0; n < NR; n += 4) {
-            const float4 t = ld4(u, (v * NR + n) / 4);
-            uv[n] = t.x; uv[n + 1] = t.y; uv[n + 2] = t.z; uv[n + 3] = t.w;
+            for (int n = 0; n < NR; n += 4) {
+                const float4 t = ld4(u, (v * NR + n) / 4);
+                uv[n] = t.x; uv[(n + 1) % NR] = t.y; uv[(n + 2) % NR] = t.z; uv[(n + 3) % NR] = t.w;
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < NR; ++n) uv[n] = u[v * NR + n];
         }
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
@@ -398,7 +461,7 @@ __global__ void __launch_bounds__(256) head_dx_rows_kernel(const HeadArgs g, int
     const int i = blockIdx.x * 32 + lane;
     float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
     if (i < rows * C4) {
-#pragma unroll 4
+#pragma unroll 8
         for (int k = y; k < parts; k += 8) t = add4(t, ld4(dx_part, (int64_t)k * NR * C4 + i));
     }
     sm[y][lane] = t;
@@ -464,7 +527,8 @@ __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, 
     const int64_t n8 = (int64_t)g.V * g.C / 8, step = (int64_t)gridDim.x * kThreads;
     const float sw = pow2(kw);
 #pragma unroll 4
-    for (int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x; i < n8; i += step) {
+    for (int64_t k = blockIdx.x * (int64_t)kThreads + threadIdx.x; k < n8; k += step) {
+        const int64_t i = n8 - 1 - k;       // backwards: the end of W is what head_max_kernel has left in L2
         uint2 h0, l0, h1, l1;
         pairs4(ld_value(g.w, g.w_lo, 2 * i), sw, h0, l0);
         pairs4(ld_value(g.w, g.w_lo, 2 * i + 1), sw, h1, l1);
@@ -573,52 +637,76 @@ size_t head_bwd_scratch_bytes(int64_t N, int C, int V, int K, int piece) {
     return bwd_layout(s, nullptr, N, C, V, K, piece);
 }
 
+namespace {
+
+// x of more than two rows takes four rows of W at a time, one and two take eight: 32 products or fewer per lane
+template <int NR>
+cudaError_t few_fwd(const HeadArgs& g, const Scratch& w, cudaStream_t s) {
+    constexpr int RV = NR > 2 ? 4 : 8;
+    const cudaError_t e = allow_smem<head_stats_rows_kernel<NR, RV>>(rows_smem(NR, 4096));
+    if (e != cudaSuccess) return e;
+    BT_KERNEL_LAUNCH((head_stats_rows_kernel<NR, RV>), kStrips, kThreads, rows_smem(NR, g.C), s, g, (int)g.N, w.stats, w.head);
+    BT_COUNT_LAUNCH();
+    return cudaGetLastError();
+}
+
+template <int NR>
+cudaError_t few_bwd(const HeadArgs& g, const Scratch& w, int K, cudaStream_t s) {
+    constexpr int RV = NR > 2 ? 4 : 8;
+    const cudaError_t e = allow_smem<head_grad_rows_kernel<NR, RV>>(rows_smem(NR, 4096));
+    if (e != cudaSuccess) return e;
+    const int rows = (int)g.N, C4 = g.C / 4, tx = C4 < kThreads ? C4 : kThreads, ry = kThreads / tx, strips = kStrips / ry < 1 ? 1 : kStrips / ry;
+    BT_KERNEL_LAUNCH((head_grad_rows_kernel<NR, RV>), kStrips, kThreads, rows_smem(NR, g.C), s, g, rows, (const RowParams*)w.rows, w.u);
+    BT_COUNT_LAUNCH();
+    if (K) {
+        BT_KERNEL_LAUNCH((head_grad_entries_kernel), (rows * K + 255) / 256, 256, 0, s, rows, NR, K, (const RowParams*)w.rows, (const int*)w.eid,
+                         (const float*)w.ep, w.u);
+        BT_COUNT_LAUNCH();
+    }
+    BT_KERNEL_LAUNCH((head_products_rows_kernel<NR>), dim3(strips, (C4 + tx - 1) / tx), dim3(tx, ry), 0, s, g, rows, (const float*)w.u, w.dx_part);
+    BT_COUNT_LAUNCH();
+    if (g.dx || g.dx_hi) {
+        BT_KERNEL_LAUNCH((head_dx_rows_kernel), (rows * C4 + 31) / 32, 256, 0, s, g, rows, NR, strips * ry, (const float*)w.dx_part);
+        BT_COUNT_LAUNCH();
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace
+
 cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     Scratch w;
     fwd_layout(w, g.scratch, g.N, g.C, g.V);
     cudaError_t e;
     int strips = kStrips;
     if (few_rows(g.N)) {
-        e = allow_smem<head_stats_rows_kernel<8, 4>>(rows_smem(kRows, 4096));
-        if (e != cudaSuccess) return e;
-        BT_KERNEL_LAUNCH((head_stats_rows_kernel<8, 4>), kStrips, kThreads, rows_smem(kRows, g.C), s, g, (int)g.N, w.stats, w.head);
-        BT_COUNT_LAUNCH();
+        e = g.N > 4 ? few_fwd<8>(g, w, s) : g.N > 2 ? few_fwd<4>(g, w, s) : g.N > 1 ? few_fwd<2>(g, w, s) : few_fwd<1>(g, w, s);
     } else {
         strips = head_stats_strips(g.V);
         e = make_pairs(g, w, false, s);
         if (e == cudaSuccess)
             e = launch_head_stats(pair_matrix(w.x16, g.N, g.C), pair_matrix(w.w16, g.V, g.C), w.rowf, w.stats, &w.head->err, s);
-        if (e != cudaSuccess) return e;
     }
-    BT_KERNEL_LAUNCH((head_finish_kernel), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
+    if (e != cudaSuccess) return e;
+    if (g.aim.targets && !few_rows(g.N))
+        BT_KERNEL_LAUNCH((head_finish_target_kernel), (unsigned)((g.N + kFinishThreads / 32 - 1) / (kFinishThreads / 32)), kFinishThreads, 0, s, g,
+                         (const float2*)w.stats, strips, w.head);
+    else
+        BT_KERNEL_LAUNCH((head_finish_kernel), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }
 
 cudaError_t launch_head_bwd(const HeadArgs& g, cudaStream_t s) {
     Scratch w;
-    const int K = g.aim.targets ? 0 : g.aim.K, C4 = g.C / 4;
+    const int K = g.aim.targets ? 0 : g.aim.K;
     bwd_layout(w, g.scratch, g.N, g.C, g.V, K, g.piece);
-    cudaError_t e = allow_smem<head_grad_rows_kernel<8, 4>>(rows_smem(kRows, 4096));
-    if (e != cudaSuccess) return e;
     BT_KERNEL_LAUNCH((head_rows_kernel), (unsigned)g.N, kFinishThreads, (size_t)K * 8, s, g, w.rows, w.eid, w.ep, w.rowmax, w.head);
     BT_COUNT_LAUNCH();
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
     if (!few_rows(g.N)) return backward_in_pieces(g, w, K, s);
-    const int rows = (int)g.N, tx = C4 < kThreads ? C4 : kThreads, ry = kThreads / tx, strips = kStrips / ry;
-    BT_KERNEL_LAUNCH((head_grad_rows_kernel<8, 4>), kStrips, kThreads, rows_smem(kRows, g.C), s, g, rows, (const RowParams*)w.rows, w.u);
-    BT_COUNT_LAUNCH();
-    if (K) {
-        BT_KERNEL_LAUNCH((head_grad_entries_kernel), (rows * K + 255) / 256, 256, 0, s, rows, kRows, K, (const RowParams*)w.rows,
-                         (const int*)w.eid, (const float*)w.ep, w.u);
-        BT_COUNT_LAUNCH();
-    }
-    BT_KERNEL_LAUNCH((head_products_rows_kernel<8>), dim3(strips, (C4 + tx - 1) / tx), dim3(tx, ry), 0, s, g, rows, (const float*)w.u, w.dx_part);
-    BT_COUNT_LAUNCH();
-    if (g.dx || g.dx_hi) {
-        BT_KERNEL_LAUNCH((head_dx_rows_kernel), (rows * C4 + 31) / 32, 256, 0, s, g, rows, kRows, strips * ry, (const float*)w.dx_part);
-        BT_COUNT_LAUNCH();
-    }
-    return cudaGetLastError();
+    return g.N > 4 ? few_bwd<8>(g, w, K, s) : g.N > 2 ? few_bwd<4>(g, w, K, s) : g.N > 1 ? few_bwd<2>(g, w, K, s) : few_bwd<1>(g, w, K, s);
 }
 
 }  // namespace bt

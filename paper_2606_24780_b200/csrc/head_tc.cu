@@ -31,7 +31,10 @@ enum Epi { kStats, kGrad, kOut };
 
 constexpr int BM = 128;                     // rows of a CTA
 constexpr int BK = 32;                      // contraction per stage: 64-byte rows of K-major tiles
-constexpr int kChunk = 512 / BK;            // stages between two sums in registers
+#ifndef HEAD_CHUNK
+#define HEAD_CHUNK 256
+#endif
+constexpr int kChunk = HEAD_CHUNK / BK;            // stages between two sums in registers
 constexpr int kEpiWarps = 8;
 // Three warpgroups: TMA, MMA and two idle warps, then the epilogue's.  They share the launch's registers (168 each, all that an SM
 // has for 384 threads) as 56 + 2 x 224.
@@ -320,8 +323,8 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
                     g.stats[(long long)row * (2 * g.tiles_n) + 2 * w.tn + half] = cols > 0 ? make_float2(mf, s) : make_float2(-INFINITY, 0.f);
                 }
             } else if (EPI == kGrad) {
-                const RowParams r = row < g.M ? g.rows[row] : RowParams{INFINITY, 0.f, -1};
-                const float f = row < g.M ? g.rowf[row] : 0.f, L = r.L - 15.0f;
+                const RowParams r = row < g.M ? g.rows[row] : RowParams{INFINITY, 0.f, 0.f, -1};
+                const float f = row < g.M ? g.rowf[row] : 0.f;
                 const bool live = r.L != INFINITY;
                 const int hit = r.target < 0 ? -1 : r.target - g.v0 - col0;
 #pragma unroll
@@ -329,7 +332,7 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
                     if (c * 32 >= cols) break;
                     float e[32];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) e[j] = live ? ex2_fast(fmaf(v[c * 32 + j], f, -L)) : 0.f;
+                    for (int j = 0; j < 32; ++j) e[j] = live ? 32768.0f * ex2_fast(fmaf(v[c * 32 + j], f, -r.L) - r.L_rest) : 0.f;
                     if (__any_sync(0xffffffffu, hit >= c * 32 && hit < c * 32 + 32)) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
