@@ -102,6 +102,10 @@ size_t bwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K, int
     return at;
 }
 
+template <bool PLANES>
+__device__ __forceinline__ float4 ld_w(const HeadArgs& g, int64_t i4) {
+    return PLANES ? add4(ld4(g.w, i4), ld4(g.w_lo, i4)) : ld4(g.w, i4);
+}
 __device__ __forceinline__ float4 ld_value(const float* hi, const float* lo, int64_t i4) {
     const float4 a = ld4(hi, i4);
     return lo ? add4(a, ld4(lo, i4)) : a;
@@ -119,8 +123,8 @@ __device__ __forceinline__ void warp_share(int V, int64_t& v0, int64_t& v1) {
 
 // Dot products of RV consecutive rows of W (fewer before v1) with the NR rows of x in shared memory, by one warp.  Lane l returns the one
 // of row l / (32 / (RV NR)) / NR of W and row (that) % NR of x; lanes that share a product hold it alike.
-template <int NR, int RV>
-__device__ __forceinline__ float warp_dots(const float4* xs, int C4, const float* w, const float* w_lo, int64_t v0, int64_t v1) {
+template <int NR, int RV, bool PLANES>
+__device__ __forceinline__ float warp_dots(const float4* xs, int C4, const HeadArgs& g, int64_t v0, int64_t v1) {
     const int lane = threadIdx.x & 31;
     constexpr int R = RV * NR;
     float acc[R];
@@ -133,7 +137,7 @@ __device__ __forceinline__ float warp_dots(const float4* xs, int C4, const float
     for (int c = lane; c < C4; c += 32) {
         float4 wv[RV];
 #pragma unroll
-        for (int i = 0; i < RV; ++i) wv[i] = ld_value(w, w_lo, at[i] + c);
+        for (int i = 0; i < RV; ++i) wv[i] = ld_w<PLANES>(g, at[i] + c);
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
             const float4 xv = xs[n * C4 + c];
@@ -166,7 +170,7 @@ __device__ __forceinline__ void rows_to_smem(float4* xs, const float* x, const f
 }
 
 // Row statistics over a strip of the vocabulary, in units of log 2.
-template <int NR, int RV>
+template <int NR, int RV, bool PLANES>
 __global__ void __launch_bounds__(kThreads, 2) head_stats_rows_kernel(const HeadArgs g, int rows, float2* stats,
                                                                    HeadHeader* head) {
     extern __shared__ float4 xs[];
@@ -183,7 +187,7 @@ __global__ void __launch_bounds__(kThreads, 2) head_stats_rows_kernel(const Head
     int64_t v0, v1;
     warp_share(g.V, v0, v1);
     for (; v0 < v1; v0 += RV) {
-        const float z = warp_dots<NR, RV>(xs, C4, g.w, g.w_lo, v0, v1) * f;
+        const float z = warp_dots<NR, RV, PLANES>(xs, C4, g, v0, v1) * f;
         if (v0 + vi < v1) {
             const float m1 = fmaxf(m, z);
             s = s * ex2_fast(m - m1) + ex2_fast(z - m1);
@@ -369,7 +373,7 @@ __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArg
 }
 
 // u[v][n] = g_n (q_nv - [v = target]) for the rows of one launch.
-template <int NR, int RV>
+template <int NR, int RV, bool PLANES>
 __global__ void __launch_bounds__(kThreads, 2) head_grad_rows_kernel(const HeadArgs g, int rows,
                                                                   const RowParams* __restrict__ params, float* __restrict__ u) {
     extern __shared__ float4 xs[];
@@ -384,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 2) head_grad_rows_kernel(const HeadA
     int64_t v0, v1;
     warp_share(g.V, v0, v1);
     for (; v0 < v1; v0 += RV) {
-        const float z = warp_dots<NR, RV>(xs, C4, g.w, g.w_lo, v0, v1);
+        const float z = warp_dots<NR, RV, PLANES>(xs, C4, g, v0, v1);
         const int64_t v = v0 + vi;
         if (v < v1 && (lane & (kShare - 1)) == 0)
             u[v * NR + n] = r.L == INFINITY ? 0.f : r.g * (ex2_fast(fmaf(z, f, -r.L) - r.L_rest) - (v == r.target ? 1.f : 0.f));
@@ -404,7 +408,7 @@ __global__ void __launch_bounds__(256) head_grad_entries_kernel(int rows, int NR
 
 // dW_v = sum_n u_vn x_n and a strip's part of dx_n = sum_v u_vn W_v: a thread owns four columns and reads u of a row of
 // W as all threads of its threadIdx.y do.
-template <int NR>
+template <int NR, bool PLANES>
 __global__ void __launch_bounds__(kThreads, 2) head_products_rows_kernel(const HeadArgs g, int rows, const float* __restrict__ u,
                                                                   float* dx_part) {
     pdl_wait();
@@ -420,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 2) head_products_rows_kernel(const H
     const int64_t lanes = (int64_t)gridDim.x * blockDim.y, at = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, v1 = (at + 1) * g.V / lanes;
 #pragma unroll 4
     for (int64_t v = at * g.V / lanes; v < v1; ++v) {
-        const float4 wv = g.dx_hi || g.dx ? ld_value(g.w, g.w_lo, v * C4 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float4 wv = g.dx_hi || g.dx ? ld_w<PLANES>(g, v * C4 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
         float4 d = make_float4(0.f, 0.f, 0.f, 0.f);
         float uv[NR];
         if (NR >= 4) {
@@ -640,36 +644,46 @@ size_t head_bwd_scratch_bytes(int64_t N, int C, int V, int K, int piece) {
 namespace {
 
 // x of more than two rows takes four rows of W at a time, one and two take eight: 32 products or fewer per lane
-template <int NR>
+template <int NR, bool PLANES>
 cudaError_t few_fwd(const HeadArgs& g, const Scratch& w, cudaStream_t s) {
     constexpr int RV = NR > 2 ? 4 : 8;
-    const cudaError_t e = allow_smem<head_stats_rows_kernel<NR, RV>>(rows_smem(NR, 4096));
+    const cudaError_t e = allow_smem<head_stats_rows_kernel<NR, RV, PLANES>>(rows_smem(NR, 4096));
     if (e != cudaSuccess) return e;
-    BT_KERNEL_LAUNCH((head_stats_rows_kernel<NR, RV>), kStrips, kThreads, rows_smem(NR, g.C), s, g, (int)g.N, w.stats, w.head);
+    BT_KERNEL_LAUNCH((head_stats_rows_kernel<NR, RV, PLANES>), kStrips, kThreads, rows_smem(NR, g.C), s, g, (int)g.N, w.stats, w.head);
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }
 
-template <int NR>
+template <int NR, bool PLANES>
 cudaError_t few_bwd(const HeadArgs& g, const Scratch& w, int K, cudaStream_t s) {
     constexpr int RV = NR > 2 ? 4 : 8;
-    const cudaError_t e = allow_smem<head_grad_rows_kernel<NR, RV>>(rows_smem(NR, 4096));
+    const cudaError_t e = allow_smem<head_grad_rows_kernel<NR, RV, PLANES>>(rows_smem(NR, 4096));
     if (e != cudaSuccess) return e;
     const int rows = (int)g.N, C4 = g.C / 4, tx = C4 < kThreads ? C4 : kThreads, ry = kThreads / tx, strips = kStrips / ry < 1 ? 1 : kStrips / ry;
-    BT_KERNEL_LAUNCH((head_grad_rows_kernel<NR, RV>), kStrips, kThreads, rows_smem(NR, g.C), s, g, rows, (const RowParams*)w.rows, w.u);
+    BT_KERNEL_LAUNCH((head_grad_rows_kernel<NR, RV, PLANES>), kStrips, kThreads, rows_smem(NR, g.C), s, g, rows, (const RowParams*)w.rows, w.u);
     BT_COUNT_LAUNCH();
     if (K) {
         BT_KERNEL_LAUNCH((head_grad_entries_kernel), (rows * K + 255) / 256, 256, 0, s, rows, NR, K, (const RowParams*)w.rows, (const int*)w.eid,
                          (const float*)w.ep, w.u);
         BT_COUNT_LAUNCH();
     }
-    BT_KERNEL_LAUNCH((head_products_rows_kernel<NR>), dim3(strips, (C4 + tx - 1) / tx), dim3(tx, ry), 0, s, g, rows, (const float*)w.u, w.dx_part);
+    BT_KERNEL_LAUNCH((head_products_rows_kernel<NR, PLANES>), dim3(strips, (C4 + tx - 1) / tx), dim3(tx, ry), 0, s, g, rows, (const float*)w.u, w.dx_part);
     BT_COUNT_LAUNCH();
     if (g.dx || g.dx_hi) {
         BT_KERNEL_LAUNCH((head_dx_rows_kernel), (rows * C4 + 31) / 32, 256, 0, s, g, rows, NR, strips * ry, (const float*)w.dx_part);
         BT_COUNT_LAUNCH();
     }
     return cudaGetLastError();
+}
+
+template <bool PLANES>
+cudaError_t few_fwd_any(const HeadArgs& g, const Scratch& w, cudaStream_t s) {
+    return g.N > 4 ? few_fwd<8, PLANES>(g, w, s) : g.N > 2 ? few_fwd<4, PLANES>(g, w, s) : g.N > 1 ? few_fwd<2, PLANES>(g, w, s) : few_fwd<1, PLANES>(g, w, s);
+}
+template <bool PLANES>
+cudaError_t few_bwd_any(const HeadArgs& g, const Scratch& w, int K, cudaStream_t s) {
+    return g.N > 4 ? few_bwd<8, PLANES>(g, w, K, s) : g.N > 2 ? few_bwd<4, PLANES>(g, w, K, s)
+                   : g.N > 1 ? few_bwd<2, PLANES>(g, w, K, s) : few_bwd<1, PLANES>(g, w, K, s);
 }
 
 }  // namespace
@@ -680,7 +694,7 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     cudaError_t e;
     int strips = kStrips;
     if (few_rows(g.N)) {
-        e = g.N > 4 ? few_fwd<8>(g, w, s) : g.N > 2 ? few_fwd<4>(g, w, s) : g.N > 1 ? few_fwd<2>(g, w, s) : few_fwd<1>(g, w, s);
+e = g.w_lo ? few_fwd_any<true>(g, w, s) : few_fwd_any<false>(g, w, s);
     } else {
         strips = head_stats_strips(g.V);
         e = make_pairs(g, w, false, s);
@@ -706,7 +720,7 @@ cudaError_t launch_head_bwd(const HeadArgs& g, cudaStream_t s) {
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     if (!few_rows(g.N)) return backward_in_pieces(g, w, K, s);
-    return g.N > 4 ? few_bwd<8>(g, w, K, s) : g.N > 2 ? few_bwd<4>(g, w, K, s) : g.N > 1 ? few_bwd<2>(g, w, K, s) : few_bwd<1>(g, w, K, s);
+    return g.w_lo ? few_bwd_any<true>(g, w, K, s) : few_bwd_any<false>(g, w, K, s);
 }
 
 }  // namespace bt
