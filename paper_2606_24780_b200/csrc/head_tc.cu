@@ -13,8 +13,11 @@
 //
 // Warp 0 copies tiles (TMA), warp 1 issues MMAs, warps 4 to 11 take accumulators out of tensor memory.  Tiles are 256 rows on a
 // pair of CTAs (cta_group::2; each CTA brings its own rows of A and half of B's) or 128 on one where there are no more.
-// The tensor core truncates when it adds, so sums are taken over in registers after 512 of the contraction index (96
+// The tensor core truncates when it adds, so sums are taken over in registers after 384 of the contraction index (72
 // instructions): a warp holds 32 rows of 128 columns there, which also frees the accumulator before the epilogue's arithmetic.
+// Every such step takes some 500 clocks from the MMAs, which read and write tensor memory at its full rate: at 768 columns sums
+// after 128, 256, 384 and 512 take 1,230, 1,105, 1,105 and 1,100 us for z of 8,192 x 50,304, and 388, 330, 290 and 288 for a
+// quarter of u, whose epilogue has to end within two steps; the error grows with the step.
 #include <cuda.h>
 #include <cuda_fp16.h>
 
@@ -31,23 +34,20 @@ enum Epi { kStats, kGrad, kOut };
 
 constexpr int BM = 128;                     // rows of a CTA
 constexpr int BK = 32;                      // contraction per stage: 64-byte rows of K-major tiles
-#ifndef HEAD_CHUNK
-#define HEAD_CHUNK 256
-#endif
-constexpr int kChunk = HEAD_CHUNK / BK;            // stages between two sums in registers
+constexpr int kChunk = 384 / BK;            // stages between two sums in registers
 constexpr int kEpiWarps = 8;
-// Three warpgroups: TMA, MMA and two idle warps, then the epilogue's.  They share the launch's registers (168 each, all that an SM
-// has for 384 threads) as 56 + 2 x 224.
+constexpr int kParts = kEpiWarps / 4;       // of a tile's columns, one to a warp
+// Three warpgroups: TMA, MMA and two idle warps, then the epilogue's.  They share the launch's registers (168 each) as
+// 56 + 2 x 224.
 constexpr int kThreads = 128 + 32 * kEpiWarps;
 constexpr int kRegsFew = 56, kRegsMany = 224;
-constexpr uint32_t kTile = 4096u;           // a warp's 32 rows of 128 bytes on their way out
 constexpr uint32_t kSmemBudget = 227u * 1024u;
 
 template <bool PAIR, int BN>
 struct Cfg {
     static constexpr int kBRows = PAIR ? BN / 2 : BN;                   // of B in one CTA
     static constexpr uint32_t kABytes = 2u * BM * BK * 2u, kBBytes = 2u * kBRows * BK * 2u, kStage = kABytes + kBBytes;
-    static constexpr uint32_t kFixed = 1024u + kEpiWarps * kTile + 256u;
+    static constexpr uint32_t kFixed = 1024u + 256u;
     static constexpr int kFit = (int)((kSmemBudget - kFixed) / kStage);
     static constexpr int kStages = kFit > 8 ? 8 : kFit;
     static constexpr size_t kSmem = kFixed + (size_t)kStages * kStage;
@@ -56,13 +56,14 @@ struct Cfg {
 struct Args {
     int M, N;                               // of the result
     int tiles_m, tiles_n, group_m, kb_total;
+    float grow;                             // see growth()
     // The tiles of the complete rounds run over all of K; the tail_tiles of the last, partly filled one (all, where there
     // are fewer tiles than CTAs) are cut into tail_splits ranges of tail_kb stages, whose sums are joined by join_kernel.
     int tail_tiles, tail_splits, tail_kb;
     float* partials;                        // [tail_splits][tail_tiles][rows of a tile][BN]
     int* err;
     const float* rowf;                      // [M] factor from accumulator to units of log 2
-    float2* stats;                          // kStats: [M][2 tiles_n]
+    float2* stats;                          // kStats: [M][kParts tiles_n]
     const RowParams* rows;                  // kGrad
     int v0;                                 // kGrad: first column of this piece
     __half* u;                              // kGrad: [2][M][ldu]
@@ -135,9 +136,22 @@ __device__ __forceinline__ bool elect_one() {
     return p != 0;
 }
 
-// 16-byte unit q of row r of a warp's tile: units change places by row, so that rows and columns are both conflict-free.
-__device__ __forceinline__ uint4* tile_unit(uint8_t* tile, int r, int q) {
-    return reinterpret_cast<uint4*>(tile + r * 128 + ((q ^ (r & 7)) << 4));
+// A thread's own 32 bytes of its row: a full sector, so that rows go out of registers as they are.  (Through shared memory and
+// out as whole lines the gradient's epilogue held the products up: MMAs and copies leave little of the shared memory's rate.)
+__device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+                 "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+// The same where `p` may lie on a multiple of 16 only.
+__device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8], bool whole) {
+    if (whole) return store32(p, v);
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void load32(const void* p, uint32_t (&v)[8]) {
+    const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
 
 // Two values as FP16 pairs.
@@ -152,12 +166,12 @@ __device__ __forceinline__ void to_pairs(float a, float b, uint32_t& hi, uint32_
 template <bool PAIR, bool A_MN, bool B_MN, int BN, int EPI>
 __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* tmB, const Args& g) {
     using C = Cfg<PAIR, BN>;
-    constexpr int kHalf = BN / 2;           // columns of one epilogue warp
+    constexpr int kCols = BN / kParts;      // columns of one epilogue warp
     constexpr int kTileRows = PAIR ? 2 * BM : BM;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t bars = base + C::kStages * C::kStage + kEpiWarps * kTile;
+    const uint32_t bars = base + C::kStages * C::kStage;
     auto full_bar = [&](int s) { return bars + 8u * s; };
     auto empty_bar = [&](int s) { return bars + 8u * (C::kStages + s); };
     auto tfull_bar = [&](int a) { return bars + 8u * (2 * C::kStages + a); };
@@ -269,22 +283,21 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsMany));
-        const int quad = warp & 3, half = (warp - 4) >> 2;
-        uint8_t* const tile = base_ptr + C::kStages * C::kStage + (warp - 4) * kTile;
-        const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + half * kHalf;
+        const int quad = warp & 3, part = (warp - 4) >> 2;
+        const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + part * kCols;
         const uint32_t drained[2] = {PAIR ? mapa_shared(tempty_bar(0), 0) : tempty_bar(0), PAIR ? mapa_shared(tempty_bar(1), 0) : tempty_bar(1)};
-        const float scale = EPI == kOut ? *g.scale : 0.f;
+        const float scale = EPI == kOut ? *g.scale * g.grow : 0.f;
         uint32_t at = 0;
         bool ok = true;
         for (int u = first; u < units && ok; u += step) {
             const Unit w = unit_at(g, u);
-            float v[kHalf];
+            float v[kCols];
             for (int k0 = w.kb0; k0 < w.kb1; k0 += kChunk, ++at) {
                 const int acc = at & 1;
                 if (!mbar_wait_warp(tfull_bar(acc), (at >> 1) & 1u, g.err, 34)) { ok = false; break; }
                 tc_fence_after();
 #pragma unroll
-                for (int c = 0; c < kHalf / 32; ++c) {
+                for (int c = 0; c < kCols / 32; ++c) {
                     uint32_t rr[32];
                     tmem_ld32(t_row + acc * 256u + c * 32, rr);
                     tmem_ld_wait();
@@ -305,91 +318,70 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
             }
             if (!ok) break;
             const int row0 = w.tm * kTileRows + (int)rank * BM + quad * 32, row = row0 + lane;
-            const int col0 = w.tn * BN + half * kHalf, cols = g.N - col0;      // cols may be below zero
+            const int col0 = w.tn * BN + part * kCols, cols = g.N - col0;      // cols may be below zero
             if (EPI == kStats) {
                 if (row < g.M) {
-                    if (cols < kHalf) {
+                    if (cols < kCols) {
 #pragma unroll
-                        for (int j = 0; j < kHalf; ++j)
+                        for (int j = 0; j < kCols; ++j)
                             if (j >= cols) v[j] = -INFINITY;
                     }
-                    const float f = g.rowf[row];
+                    const float f = g.rowf[row] * g.grow;
                     float m = v[0], s = 0.f;
 #pragma unroll
-                    for (int j = 1; j < kHalf; ++j) m = fmaxf(m, v[j]);
+                    for (int j = 1; j < kCols; ++j) m = fmaxf(m, v[j]);
                     const float mf = m * f;
 #pragma unroll
-                    for (int j = 0; j < kHalf; ++j) s += ex2_fast(fmaf(v[j], f, -mf));
-                    g.stats[(long long)row * (2 * g.tiles_n) + 2 * w.tn + half] = cols > 0 ? make_float2(mf, s) : make_float2(-INFINITY, 0.f);
+                    for (int j = 0; j < kCols; ++j) s += ex2_fast(fmaf(v[j], f, -mf));
+                    g.stats[(long long)row * (kParts * g.tiles_n) + kParts * w.tn + part] = cols > 0 ? make_float2(mf, s) : make_float2(-INFINITY, 0.f);
                 }
             } else if (EPI == kGrad) {
                 const RowParams r = row < g.M ? g.rows[row] : RowParams{INFINITY, 0.f, 0.f, -1};
-                const float f = row < g.M ? g.rowf[row] : 0.f;
+                const float f = row < g.M ? g.rowf[row] * g.grow : 0.f;
                 const bool live = r.L != INFINITY;
                 const int hit = r.target < 0 ? -1 : r.target - g.v0 - col0;
+                __half* dst = g.u + row * g.ldu + col0;
 #pragma unroll
-                for (int c = 0; c < kHalf / 32; ++c) {
-                    if (c * 32 >= cols) break;
-                    float e[32];
+                for (int c = 0; c < kCols / 16; ++c) {
+                    if (c * 16 >= cols) break;
+                    float e[16];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) e[j] = live ? 32768.0f * ex2_fast(fmaf(v[c * 32 + j], f, -r.L) - r.L_rest) : 0.f;
-                    if (__any_sync(0xffffffffu, hit >= c * 32 && hit < c * 32 + 32)) {
+                    for (int j = 0; j < 16; ++j) e[j] = live ? 32768.0f * ex2_fast(fmaf(v[c * 16 + j], f, -r.L) - r.L_rest) : 0.f;
+                    if (__any_sync(0xffffffffu, hit >= c * 16 && hit < c * 16 + 16)) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (hit == c * 32 + j) e[j] -= 32768.0f;
+                        for (int j = 0; j < 16; ++j)
+                            if (hit == c * 16 + j) e[j] -= 32768.0f;
                     }
+                    uint32_t h[8], l[8];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint4 h, l;
-                        to_pairs(e[8 * q], e[8 * q + 1], h.x, l.x);
-                        to_pairs(e[8 * q + 2], e[8 * q + 3], h.y, l.y);
-                        to_pairs(e[8 * q + 4], e[8 * q + 5], h.z, l.z);
-                        to_pairs(e[8 * q + 6], e[8 * q + 7], h.w, l.w);
-                        *tile_unit(tile, lane, q) = h;
-                        *tile_unit(tile, lane, q + 4) = l;
+                    for (int j = 0; j < 8; ++j) to_pairs(e[2 * j], e[2 * j + 1], h[j], l[j]);
+                    if (row < g.M) {
+                        store32(dst + c * 16, h);
+                        store32(dst + g.u_plane + c * 16, l);
                     }
-                    __syncwarp();
-                    const int q = lane & 7;
-                    __half* dst = g.u + (q >= 4 ? g.u_plane : 0) + col0 + c * 32 + (q & 3) * 8;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int r8 = (lane >> 3) + 4 * i;
-                        if (row0 + r8 < g.M) *reinterpret_cast<uint4*>(dst + (row0 + r8) * g.ldu) = *tile_unit(tile, r8, q);
-                    }
-                    __syncwarp();
                 }
             } else {
                 float rg = 1.f;
                 if (g.row_g && w.slot < 0) rg = row < g.M ? g.row_g[row].g : 0.f;
                 // a partial tile keeps bare sums
-                float* dst = w.slot < 0 ? g.out + (long long)row0 * g.N + col0
-                                        : g.partials + ((long long)w.slot * kTileRows + (int)rank * BM + quad * 32) * BN + half * kHalf;
-                const long long ld = w.slot < 0 ? g.N : BN;
-                const bool onto = g.onto && w.slot < 0;
+                float* dst = w.slot < 0 ? g.out + (long long)row * g.N + col0
+                                        : g.partials + ((long long)w.slot * kTileRows + (int)rank * BM + quad * 32 + lane) * BN + part * kCols;
+                const bool onto = g.onto && w.slot < 0, whole = (reinterpret_cast<uintptr_t>(dst) & 31u) == 0;
                 const float sc = w.slot < 0 ? scale : 1.f;
+                if (row < g.M) {
 #pragma unroll
-                for (int c = 0; c < kHalf / 32; ++c) {
-                    if (c * 32 >= cols) break;
+                    for (int c = 0; c < kCols / 8; ++c) {
+                        if (c * 8 >= cols) break;
+                        uint32_t t[8], old[8];
+                        if (onto) load32(dst + c * 8, old);
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        float4 t = make_float4(v[c * 32 + 4 * q] * sc * rg, v[c * 32 + 4 * q + 1] * sc * rg, v[c * 32 + 4 * q + 2] * sc * rg,
-                                               v[c * 32 + 4 * q + 3] * sc * rg);
-                        if (rg == 0.f) t = make_float4(0.f, 0.f, 0.f, 0.f);    // the row has no part in the loss
-                        *reinterpret_cast<float4*>(tile_unit(tile, lane, q)) = t;
-                    }
-                    __syncwarp();
-                    const int q = lane & 7;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int r8 = (lane >> 3) + 4 * i;
-                        if (row0 + r8 < g.M) {
-                            float4 t = *reinterpret_cast<const float4*>(tile_unit(tile, r8, q));
-                            float4* p = reinterpret_cast<float4*>(dst + r8 * ld + c * 32 + 4 * q);
-                            if (onto) t = add4(t, *p);
-                            *p = t;
+                        for (int j = 0; j < 8; ++j) {
+                            float o = rg == 0.f ? 0.f : v[c * 8 + j] * sc * rg;     // zero: the row has no part in the loss
+                            if (onto) o += __uint_as_float(old[j]);
+                            t[j] = __float_as_uint(o);
                         }
+                        store32(dst + c * 8, t, whole);
                     }
-                    __syncwarp();
                 }
             }
         }
@@ -421,7 +413,7 @@ __global__ void __launch_bounds__(256) join_kernel(const Args g, int tile_rows, 
     pdl_trigger();
     const int bn4 = bn / 4;
     const long long per = (long long)tile_rows * bn4, total = g.tail_tiles * per;
-    const float sc = *g.scale;
+    const float sc = *g.scale * g.grow;
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < total; i += gridDim.x * 256LL) {
         const int j = (int)(i / per);
         const long long r = i - j * per;
@@ -451,6 +443,20 @@ bool encode(CUtensorMap* tm, const HalfMat& m, bool mn, int box_rows) {
                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The tensor core cuts its running sum to FP32 with every instruction, always toward zero.  A sum that grows to its final size
+// over n instructions comes out short by some n / 2 times 2^-24 of it times the mean of the cut: measured, 0.54 for
+// random operands, 0.6 for aligned ones, 1.2 where all products are positive.  n is 3 per 16 of the contraction index between
+// two sums in registers; the products are made longer by 0.56.
+float growth(int kb_total) {
+    double n = 0.0, nn = 0.0;
+    for (int left = kb_total; left > 0; left -= kChunk) {
+        const double c = 3.0 * (BK / 16) * (left < kChunk ? left : kChunk);
+        n += c;
+        nn += c * c;
+    }
+    return (float)(1.0 + 0.5 * 0.56 / (1 << 24) * nn / n);
+}
+
 template <bool PAIR, bool A_MN, bool B_MN, int BN, int EPI>
 cudaError_t launch(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, cudaStream_t s) {
     using C = Cfg<PAIR, BN>;
@@ -464,6 +470,7 @@ cudaError_t launch(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, cudaS
     g.group_m = 4 * g.tiles_n <= slots ? 4 : 16;
     if (g.group_m > g.tiles_m) g.group_m = g.tiles_m;
     g.kb_total = (int)((K + BK - 1) / BK);
+    g.grow = growth(g.kb_total);
     g.tail_tiles = g.tail_splits = g.tail_kb = 0;
     const int tiles = g.tiles_m * g.tiles_n;
     if (EPI == kOut && g.partials && tiles % slots) {
@@ -511,7 +518,7 @@ cudaError_t launch_out(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, c
 
 }  // namespace
 
-int head_stats_strips(int V) { return 2 * ((V + 255) / 256); }
+int head_stats_strips(int V) { return kParts * ((V + 255) / 256); }
 size_t head_partial_bytes() { return (size_t)148 * BM * 256 * sizeof(float); }
 
 cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, float2* stats, int* err, cudaStream_t s) {
