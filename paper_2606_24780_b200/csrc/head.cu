@@ -8,18 +8,17 @@
 // g_n = inv_count w_n tau S_n.  The forward keeps one (maximum, sum) pair per row and strip of the vocabulary, joined
 // by head_finish_kernel, which also forms the few scores that the loss needs by themselves; the backward forms z again.
 //
-// Up to eight rows go through the kernels here in plain FP32: the weights are read once in full width and each value is used
-// for all rows from registers.  More rows go to the tensor cores (head_tc.cu) on pairs of FP16 numbers that
-// head_pairs_kernel makes of x and W.
+// Few rows go through head_rows.cu in plain FP32, where the weights are read once; more rows go to the tensor cores (head_tc.cu)
+// on pairs of FP16 numbers that head_pairs_kernel makes of x and W.
+#include <climits>
+
 #include "head.cuh"
 
 namespace bt {
 
 namespace {
 
-constexpr int kRows = 8;                    // rows of x that the plain kernels carry
 constexpr int kParts = 592;                 // CTAs that look for the largest value
-constexpr int kStrips = 296;                // CTAs over the vocabulary (2 per SM)
 constexpr int kThreads = 256;
 constexpr int kFinishThreads = 256;
 
@@ -31,12 +30,15 @@ struct Scales {
 struct Scratch {
     HeadHeader* head;
     float2* stats;                          // forward: [N][strips]
+    float* colf;                            // forward, tensor cores: [V] up to a multiple of 256
+    int2* entries;                          // [N][K]
+    float* zk;                              // [N][K]
     RowParams* rows;                        // backward: [N]
     int* eid;                               // [N][K] columns of the aim, each once; below zero: none
     float* ep;                              // [N][K] its weights there
     // few rows
-    float* u;                               // [V][kRows]
-    float* dx_part;                         // [strips][kRows][C]
+    float* aim;                             // [V][kFewRows]
+    float* dx_part;                         // [parts][kFewRows][C]
     // tensor cores
     Scales* scales;
     float *wpart, *ypart;                   // [kParts] largest values
@@ -46,7 +48,9 @@ struct Scratch {
     float* partials;
 };
 
-bool few_rows(int64_t N) { return N <= kRows; }
+// Rows up to which the plain kernels are used: two passes over the weights in the forward, one in the backward, where a second one
+// would add to dW.  C 768, V 50,257, raw: 9 to 16 rows 98 us against 133 on the tensor cores, 17 to 24 148; gradients 266 against 210.
+bool few_rows(int64_t N, bool back) { return N <= (back ? 1 : 2) * kFewRows; }
 
 // Columns of one piece of the vocabulary, a multiple of 256: pieces of about the same size, of at most `piece` columns or
 // 512 MB of u.
@@ -72,12 +76,16 @@ void tc_layout(Scratch& s, uint8_t* base, size_t& at, int64_t N, int C, int V) {
     s.w16 = take<__half>(base, at, 2 * (size_t)V * C);
 }
 
-size_t fwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V) {
+size_t fwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K) {
     size_t at = kHeadHeader;
     s = Scratch{};
     s.head = (HeadHeader*)base;
-    s.stats = take<float2>(base, at, (size_t)N * (few_rows(N) ? kStrips : head_stats_strips(V)));
-    if (!few_rows(N)) tc_layout(s, base, at, N, C, V);
+    s.stats = take<float2>(base, at, (size_t)N * (few_rows(N, false) ? head_few_strips(N, C, V) : head_stats_strips(V)));
+    if (few_rows(N, false)) return at;
+    tc_layout(s, base, at, N, C, V);
+    s.colf = take<float>(base, at, (V + 255) / 256 * 256);
+    s.entries = take<int2>(base, at, (size_t)N * K);
+    s.zk = take<float>(base, at, (size_t)N * K);
     return at;
 }
 
@@ -88,9 +96,9 @@ size_t bwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K, int
     s.rows = take<RowParams>(base, at, N);
     s.eid = take<int>(base, at, (size_t)N * K);
     s.ep = take<float>(base, at, (size_t)N * K);
-    if (few_rows(N)) {
-        s.u = take<float>(base, at, (size_t)V * kRows);
-        s.dx_part = take<float>(base, at, (size_t)kStrips * kRows * C);
+    if (few_rows(N, true)) {
+        if (K) s.aim = take<float>(base, at, (size_t)V * kFewRows);
+        s.dx_part = take<float>(base, at, head_few_parts(N, C, V) * kFewRows * C);
         return at;
     }
     tc_layout(s, base, at, N, C, V);
@@ -102,10 +110,6 @@ size_t bwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K, int
     return at;
 }
 
-template <bool PLANES>
-__device__ __forceinline__ float4 ld_w(const HeadArgs& g, int64_t i4) {
-    return PLANES ? add4(ld4(g.w, i4), ld4(g.w_lo, i4)) : ld4(g.w, i4);
-}
 __device__ __forceinline__ float4 ld_value(const float* hi, const float* lo, int64_t i4) {
     const float4 a = ld4(hi, i4);
     return lo ? add4(a, ld4(lo, i4)) : a;
@@ -114,99 +118,7 @@ __device__ __forceinline__ float dot4(float4 a, float4 b, float acc) {
     return fmaf(a.w, b.w, fmaf(a.z, b.z, fmaf(a.y, b.y, fmaf(a.x, b.x, acc))));
 }
 
-// The rows of W that this warp of the grid takes, to within one as many as any other.
-__device__ __forceinline__ void warp_share(int V, int64_t& v0, int64_t& v1) {
-    const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), all = (int64_t)gridDim.x * (kThreads / 32);
-    v0 = w * V / all;
-    v1 = (w + 1) * V / all;
-}
-
-// Dot products of RV consecutive rows of W (fewer before v1) with the NR rows of x in shared memory, by one warp.  Lane l returns the one
-// of row l / (32 / (RV NR)) / NR of W and row (that) % NR of x; lanes that share a product hold it alike.
-template <int NR, int RV, bool PLANES>
-__device__ __forceinline__ float warp_dots(const float4* xs, int C4, const HeadArgs& g, int64_t v0, int64_t v1) {
-    const int lane = threadIdx.x & 31;
-    constexpr int R = RV * NR;
-    float acc[R];
-#pragma unroll
-    for (int i = 0; i < R; ++i) acc[i] = 0.f;
-    int64_t at[RV];
-#pragma unroll
-    for (int i = 0; i < RV; ++i) at[i] = (v0 + i < v1 ? v0 + i : v1 - 1) * C4;
-#pragma unroll 2
-    for (int c = lane; c < C4; c += 32) {
-        float4 wv[RV];
-#pragma unroll
-        for (int i = 0; i < RV; ++i) wv[i] = ld_w<PLANES>(g, at[i] + c);
-#pragma unroll
-        for (int n = 0; n < NR; ++n) {
-            const float4 xv = xs[n * C4 + c];
-#pragma unroll
-            for (int i = 0; i < RV; ++i) acc[i * NR + n] = dot4(wv[i], xv, acc[i * NR + n]);
-        }
-    }
-    // every step halves the products a lane carries and doubles the lanes summed
-    int o = 16;
-#pragma unroll
-    for (int half = R / 2; half >= 1; half /= 2, o /= 2) {
-        const bool up = lane & o;
-#pragma unroll
-        for (int i = 0; i < half; ++i) {
-            const float keep = up ? acc[i + half] : acc[i], give = up ? acc[i] : acc[i + half];
-            acc[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-        }
-    }
-    float z = acc[0];
-    for (; o >= 1; o /= 2) z += __shfl_xor_sync(0xffffffffu, z, o);
-    return z;
-}
-
-__device__ __forceinline__ void rows_to_smem(float4* xs, const float* x, const float* x_lo, int rows, int NR, int C4) {
-    for (int i = threadIdx.x; i < NR * C4; i += kThreads) {
-        const int n = i / C4;
-        xs[i] = n < rows ? ld_value(x, x_lo, i) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    __syncthreads();
-}
-
-// Row statistics over a strip of the vocabulary, in units of log 2.
-template <int NR, int RV, bool PLANES>
-__global__ void __launch_bounds__(kThreads, 2) head_stats_rows_kernel(const HeadArgs g, int rows, float2* stats,
-                                                                   HeadHeader* head) {
-    extern __shared__ float4 xs[];
-    __shared__ float2 part[kThreads];
-    pdl_wait();
-    pdl_trigger();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *head = HeadHeader{0, 0u};
-    const int C4 = g.C / 4, lane = threadIdx.x & 31;
-    rows_to_smem(xs, g.x, g.x_lo, rows, NR, C4);
-    constexpr int R = RV * NR, kShare = 32 / R;
-    const int idx = lane / kShare, vi = idx / NR;
-    const float f = kLog2e / g.aim.tau;
-    float m = -INFINITY, s = 0.f;
-    int64_t v0, v1;
-    warp_share(g.V, v0, v1);
-    for (; v0 < v1; v0 += RV) {
-        const float z = warp_dots<NR, RV, PLANES>(xs, C4, g, v0, v1) * f;
-        if (v0 + vi < v1) {
-            const float m1 = fmaxf(m, z);
-            s = s * ex2_fast(m - m1) + ex2_fast(z - m1);
-            m = m1;
-        }
-    }
-    part[threadIdx.x] = make_float2(m, (lane & (kShare - 1)) ? 0.f : s);
-    __syncthreads();
-    if (threadIdx.x < rows) {
-        m = -INFINITY, s = 0.f;
-        for (int i = 0; i < kThreads; ++i)
-            if ((((i & 31) / kShare) % NR) == threadIdx.x && part[i].y != 0.f) m = fmaxf(m, part[i].x);
-        for (int i = 0; i < kThreads; ++i)
-            if ((((i & 31) / kShare) % NR) == threadIdx.x && part[i].y != 0.f) s += part[i].y * ex2_fast(part[i].x - m);
-        stats[threadIdx.x * gridDim.x + blockIdx.x] = make_float2(m, s);
-    }
-}
-
-// One row per CTA: joins the partial statistics, forms the scores of the row's aim and the loss.
+// Few rows against a teacher, one per CTA: joins the partial statistics, forms the scores of the row's entries and the loss.
 __global__ void __launch_bounds__(kFinishThreads) head_finish_kernel(const HeadArgs g, const float2* __restrict__ stats, int strips,
                                                                      HeadHeader* head) {
     __shared__ float smf[kFinishThreads / 32];
@@ -233,26 +145,15 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_kernel(const HeadA
         return warp_sum(z) * (1.0f / g.aim.tau);
     };
     float loss = 0.f;
-    if (g.aim.targets) {
-        int t = g.aim.targets[row];
-        if (t >= 0) {
-            if (t >= g.V) {
-                if (g.bad && threadIdx.x == 0) atomicCAS(g.bad, 0, (int)row + 1);
-                t = 0;
-            }
-            if (warp == 0) loss = lse - score(t);
-        }
-    } else {
-        bool any;
-        const float norm = teacher_norm<kFinishThreads>(g.aim, row, g.V, g.bad, smf, any);
-        float t = 0.f;
-        for (int k = warp; any && k < g.aim.K; k += kFinishThreads / 32) {
-            int id;
-            const float lp = entry_logit(g.aim, row, k, g.V, nullptr, id) - norm, p = expf(lp);
-            if (p != 0.f) t += p * (lp + (lse - score(id)));    // NaN is not zero: such a row has no finite loss
-        }
-        loss = block_all<kFinishThreads>(lane == 0 ? t : 0.f, smf, SumOp()) * (g.aim.tau * g.aim.tau);
+    bool any;
+    const float norm = teacher_norm<kFinishThreads>(g.aim, row, g.V, g.bad, smf, any);
+    float t = 0.f;
+    for (int k = warp; any && k < g.aim.K; k += kFinishThreads / 32) {
+        int id;
+        const float lp = entry_logit(g.aim, row, k, g.V, nullptr, id) - norm, p = expf(lp);
+        if (p != 0.f) t += p * (lp + (lse - score(id)));    // NaN is not zero: such a row has no finite loss
     }
+    loss = block_all<kFinishThreads>(lane == 0 ? t : 0.f, smf, SumOp()) * (g.aim.tau * g.aim.tau);
     if (threadIdx.x == 0) {
         if (g.lse) g.lse[row] = lse;
         g.losses[row] = loss;
@@ -260,7 +161,23 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_kernel(const HeadA
     if (g.loss_mean) mean_by_last<kFinishThreads>(g.aim, g.losses, g.N, &head->rows_done, gridDim.x, g.loss_mean, smd);
 }
 
-// The same for targets, a row per warp: with 8,192 rows the CTA per row above takes 88 us, most of it barriers, this 9.
+// log sum exp of a row from its strips, by a warp.
+__device__ __forceinline__ float row_lse(const float2* st, int strips) {
+    float m = -INFINITY, s = 0.f;
+#pragma unroll 4
+    for (int i = threadIdx.x & 31; i < strips; i += 32) {
+        const float2 p = st[i];
+        if (p.y != 0.f) {                   // a strip without columns has the sum zero
+            const float m1 = fmaxf(m, p.x);
+            s = s * ex2_fast(m - m1) + p.y * ex2_fast(p.x - m1);
+            m = m1;
+        }
+    }
+    const float top = warp_max(m);
+    return (top + log2f(warp_sum(s != 0.f ? s * ex2_fast(m - top) : 0.f))) * kLn2;
+}
+
+// The loss against targets, a row per warp (a CTA per row takes 88 us for 8,192 rows, most of it barriers).
 __global__ void __launch_bounds__(kFinishThreads) head_finish_target_kernel(const HeadArgs g, const float2* __restrict__ stats, int strips,
                                                                             HeadHeader* head) {
     __shared__ double smd[kFinishThreads / 32];
@@ -274,20 +191,8 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_target_kernel(cons
             if (g.bad && lane == 0) atomicCAS(g.bad, 0, (int)row + 1);
             t = 0;
         }
-        const float2* st = stats + row * strips;
-        float m = -INFINITY, s = 0.f, z = 0.f;
-#pragma unroll 4
-        for (int i = lane; i < strips; i += 32) {
-            const float2 p = st[i];
-            if (p.y != 0.f) {
-                const float m1 = fmaxf(m, p.x);
-                s = s * ex2_fast(m - m1) + p.y * ex2_fast(p.x - m1);
-                m = m1;
-            }
-        }
-        const float top = warp_max(m);
-        s = warp_sum(s != 0.f ? s * ex2_fast(m - top) : 0.f);       // a lane without strips has the sum zero
-        const float lse = (top + log2f(s)) * kLn2;
+        const float lse = row_lse(stats + row * strips, strips);
+        float z = 0.f;
         const int C4 = g.C / 4;
         if (t >= 0) {
 #pragma unroll 4
@@ -298,6 +203,44 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_target_kernel(cons
         if (lane == 0) {
             if (g.lse) g.lse[row] = lse;
             g.losses[row] = t >= 0 ? lse - z : 0.f;
+        }
+    }
+    if (g.loss_mean) mean_by_last<kFinishThreads>(g.aim, g.losses, g.N, &head->rows_done, gridDim.x, g.loss_mean, smd);
+}
+
+// The same for a teacher whose entries' scores are there already (in units of log 2), a row per warp.
+__global__ void __launch_bounds__(kFinishThreads) head_finish_entries_kernel(const HeadArgs g, const float2* __restrict__ stats, int strips,
+                                                                             const float* __restrict__ zk, HeadHeader* head) {
+    __shared__ double smd[kFinishThreads / 32];
+    pdl_wait();
+    pdl_trigger();
+    const int64_t row = blockIdx.x * (int64_t)(kFinishThreads / 32) + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    if (row < g.N) {
+        const LossAim& a = g.aim;
+        const float lse = row_lse(stats + row * strips, strips);
+        float top = -INFINITY, sum = 0.f, loss = 0.f;
+        int id;
+        bool any = false;
+        for (int k = lane; k < a.K; k += 32) {
+            const float t = entry_logit(a, row, k, g.V, nullptr, id);
+            any |= t != -INFINITY;          // a logit that is not a number counts: the row then has no finite loss
+            top = fmaxf(top, t);
+        }
+        any = __any_sync(0xffffffffu, any);
+        if (any) {
+            top = warp_max(top);
+            for (int k = lane; k < a.K; k += 32) sum += expf(entry_logit(a, row, k, g.V, nullptr, id) - top);
+            const float norm = a.lse ? a.lse[row] : top + logf(warp_sum(sum));
+            for (int k = lane; k < a.K; k += 32) {
+                const float lp = entry_logit(a, row, k, g.V, nullptr, id) - norm, p = expf(lp);
+                if (p != 0.f) loss += p * (lp + (lse - zk[row * a.K + k] * kLn2));
+            }
+        }
+        loss = warp_sum(loss) * (a.tau * a.tau);
+        if (lane == 0) {
+            if (g.lse) g.lse[row] = lse;
+            g.losses[row] = loss;
         }
     }
     if (g.loss_mean) mean_by_last<kFinishThreads>(g.aim, g.losses, g.N, &head->rows_done, gridDim.x, g.loss_mean, smd);
@@ -372,110 +315,6 @@ __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArg
     }
 }
 
-// u[v][n] = g_n (q_nv - [v = target]) for the rows of one launch.
-template <int NR, int RV, bool PLANES>
-__global__ void __launch_bounds__(kThreads, 2) head_grad_rows_kernel(const HeadArgs g, int rows,
-                                                                  const RowParams* __restrict__ params, float* __restrict__ u) {
-    extern __shared__ float4 xs[];
-    pdl_wait();
-    pdl_trigger();
-    const int C4 = g.C / 4, lane = threadIdx.x & 31;
-    rows_to_smem(xs, g.x, g.x_lo, rows, NR, C4);
-    constexpr int kShare = 32 / (RV * NR);
-    const int idx = lane / kShare, vi = idx / NR, n = idx % NR;
-    const float f = kLog2e / g.aim.tau;
-    const RowParams r = n < rows ? params[n] : RowParams{INFINITY, 0.f, 0.f, -1};
-    int64_t v0, v1;
-    warp_share(g.V, v0, v1);
-    for (; v0 < v1; v0 += RV) {
-        const float z = warp_dots<NR, RV, PLANES>(xs, C4, g, v0, v1);
-        const int64_t v = v0 + vi;
-        if (v < v1 && (lane & (kShare - 1)) == 0)
-            u[v * NR + n] = r.L == INFINITY ? 0.f : r.g * (ex2_fast(fmaf(z, f, -r.L) - r.L_rest) - (v == r.target ? 1.f : 0.f));
-    }
-}
-
-// The teacher's part of u.
-__global__ void __launch_bounds__(256) head_grad_entries_kernel(int rows, int NR, int K, const RowParams* __restrict__ params,
-                                                                const int* __restrict__ eid, const float* __restrict__ ep, float* u) {
-    pdl_wait();
-    pdl_trigger();
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows * K) return;
-    const int n = i / K, id = eid[i];
-    if (id >= 0) u[(int64_t)id * NR + n] -= params[n].g * ep[i];
-}
-
-// dW_v = sum_n u_vn x_n and a strip's part of dx_n = sum_v u_vn W_v: a thread owns four columns and reads u of a row of
-// W as all threads of its threadIdx.y do.
-template <int NR, bool PLANES>
-__global__ void __launch_bounds__(kThreads, 2) head_products_rows_kernel(const HeadArgs g, int rows, const float* __restrict__ u,
-                                                                  float* dx_part) {
-    pdl_wait();
-    pdl_trigger();
-    const int C4 = g.C / 4, c = blockIdx.y * blockDim.x + threadIdx.x;
-    if (c >= C4) return;
-    float4 xv[NR], acc[NR];
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        xv[n] = n < rows ? ld_value(g.x, g.x_lo, n * C4 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-        acc[n] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    const int64_t lanes = (int64_t)gridDim.x * blockDim.y, at = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, v1 = (at + 1) * g.V / lanes;
-#pragma unroll 4
-    for (int64_t v = at * g.V / lanes; v < v1; ++v) {
-        const float4 wv = g.dx_hi || g.dx ? ld_w<PLANES>(g, v * C4 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-        float4 d = make_float4(0.f, 0.f, 0.f, 0.f);
-        float uv[NR];
-        if (NR >= 4) {
-#pragma unroll
-            for (int n = 0; n < NR; n += 4) {
-                const float4 t = ld4(u, (v * NR + n) / 4);
-                uv[n] = t.x; uv[(n + 1) % NR] = t.y; uv[(n + 2) % NR] = t.z; uv[(n + 3) % NR] = t.w;
-            }
-        } else {
-#pragma unroll
-            for (int n = 0; n < NR; ++n) uv[n] = u[v * NR + n];
-        }
-#pragma unroll
-        for (int n = 0; n < NR; ++n) {
-            const float t = uv[n];
-            acc[n] = make_float4(fmaf(t, wv.x, acc[n].x), fmaf(t, wv.y, acc[n].y), fmaf(t, wv.z, acc[n].z), fmaf(t, wv.w, acc[n].w));
-            // a row without part in the loss may hold anything
-            if (t != 0.f) d = make_float4(fmaf(t, xv[n].x, d.x), fmaf(t, xv[n].y, d.y), fmaf(t, xv[n].z, d.z), fmaf(t, xv[n].w, d.w));
-        }
-        if (g.dw) {
-            float4* out = reinterpret_cast<float4*>(g.dw) + v * C4 + c;
-            *out = d;
-        }
-    }
-    if (g.dx || g.dx_hi) {
-        float4* out = reinterpret_cast<float4*>(dx_part) + (int64_t)(blockIdx.x * blockDim.y + threadIdx.y) * NR * C4 + c;
-#pragma unroll
-        for (int n = 0; n < NR; ++n) out[n * C4] = acc[n];
-    }
-}
-
-__global__ void __launch_bounds__(256) head_dx_rows_kernel(const HeadArgs g, int rows, int NR, int parts,
-                                                           const float* __restrict__ dx_part) {
-    __shared__ float4 sm[8][32];
-    pdl_wait();
-    pdl_trigger();
-    const int C4 = g.C / 4, lane = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int i = blockIdx.x * 32 + lane;
-    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (i < rows * C4) {
-#pragma unroll 8
-        for (int k = y; k < parts; k += 8) t = add4(t, ld4(dx_part, (int64_t)k * NR * C4 + i));
-    }
-    sm[y][lane] = t;
-    __syncthreads();
-    if (y == 0 && i < rows * C4) {
-        for (int k = 1; k < 8; ++k) t = add4(t, sm[k][lane]);
-        store_raw_split(t, g.dx, g.dx_hi, g.dx_lo, i);
-    }
-}
-
 // ---------------------------------------------------------------- FP16 pairs
 
 // The k with 2^k m in [2^14, 2^15), where 2^k is an FP32 number.
@@ -485,20 +324,18 @@ __device__ __forceinline__ int pair_exponent(float m) {
 }
 __device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
-// Largest absolute values of W, and of y_nc = g_n x_nc (backward), per CTA.
+// Largest absolute values of W and of y_nc = g_n x_nc, per CTA.
 __global__ void __launch_bounds__(kThreads) head_max_kernel(const HeadArgs g, const RowParams* __restrict__ rows,
-                                                            const float* __restrict__ rowmax, float* wpart, float* ypart, HeadHeader* head) {
+                                                            const float* __restrict__ rowmax, float* wpart, float* ypart) {
     __shared__ float smf[kThreads / 32];
     pdl_wait();
     pdl_trigger();
-    if (head && blockIdx.x == 0 && threadIdx.x == 0) *head = HeadHeader{0, 0u};
     const int64_t n4 = (int64_t)g.V * (g.C / 4), step = (int64_t)gridDim.x * kThreads;
     float m = 0.f;
 #pragma unroll 8
     for (int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x; i < n4; i += step) m = max4(m, ld4(g.w, i));
     m = block_all<kThreads>(m, smf, MaxOp());
     if (threadIdx.x == 0) wpart[blockIdx.x] = m;
-    if (!rows) return;
     m = 0.f;
     for (int64_t n = blockIdx.x * (int64_t)kThreads + threadIdx.x; n < g.N; n += step)
         if (rows[n].g != 0.f) m = fmaxf(m, fabsf(rows[n].g) * rowmax[n]);
@@ -516,7 +353,38 @@ __device__ __forceinline__ void pairs4(float4 v, float s, uint2& hi, uint2& lo) 
     lo = make_uint2(*reinterpret_cast<const uint32_t*>(&c), *reinterpret_cast<const uint32_t*>(&d));
 }
 
-// W and x, and y for the backward, as pairs: W and y at one power of two, the rows of x each at its own.
+// A row of C values as pairs at its own power of two, which it returns; by a warp.
+__device__ __forceinline__ int row_to_pairs(const float* v, const float* v_lo, int64_t row, int C4, __half* out, int64_t plane4) {
+    const int lane = threadIdx.x & 31;
+    float m = 0.f;
+    for (int c = lane; c < C4; c += 32) m = max4(m, ld4(v, row * C4 + c));
+    const int k = pair_exponent(warp_max(m));
+    const float s = pow2(k);
+    for (int c = lane; c < C4; c += 32) {
+        uint2 h, l;
+        pairs4(ld_value(v, v_lo, row * C4 + c), s, h, l);
+        reinterpret_cast<uint2*>(out)[row * C4 + c] = h;
+        reinterpret_cast<uint2*>(out)[plane4 + row * C4 + c] = l;
+    }
+    return k;
+}
+
+// Forward: the rows of W and x as pairs, each at its own power of two, which the epilogue takes out of its column or row.
+__global__ void __launch_bounds__(kThreads) head_row_pairs_kernel(const HeadArgs g, const Scratch s) {
+    pdl_wait();
+    pdl_trigger();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *s.head = HeadHeader{0, 0u};
+    const int C4 = g.C / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t step = gridDim.x * (int64_t)(kThreads / 32), first = blockIdx.x * (int64_t)(kThreads / 32) + warp;
+    for (int64_t row = first; row < g.V + g.N; row += step) {
+        const bool of_w = row < g.V;
+        const int k = of_w ? row_to_pairs(g.w, g.w_lo, row, C4, s.w16, (int64_t)g.V * C4) : row_to_pairs(g.x, g.x_lo, row - g.V, C4, s.x16, g.N * C4);
+        // 2^-k reaches 2^-126: the factor of a row of x is log2 e / tau 2^-k, a number of FP32 in any case
+        if (lane == 0) (of_w ? s.colf[row] : s.rowf[row - g.V]) = of_w ? ldexpf(1.0f, -k) : ldexpf(kLog2e / g.aim.tau, -k);
+    }
+}
+
+// Backward: W and y at one power of two each, since they are summed over their rows, the rows of x each at its own.
 __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, const RowParams* __restrict__ rows, const Scratch s) {
     __shared__ float smf[kThreads / 32];
     pdl_wait();
@@ -524,12 +392,12 @@ __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, 
     float m = 0.f, my = 0.f;
     for (int i = threadIdx.x; i < kParts; i += kThreads) {
         m = fmaxf(m, s.wpart[i]);
-        if (rows) my = fmaxf(my, s.ypart[i]);
+        my = fmaxf(my, s.ypart[i]);
     }
-    const int kw = pair_exponent(block_all<kThreads>(m, smf, MaxOp())), ky = rows ? pair_exponent(block_all<kThreads>(my, smf, MaxOp())) : 0;
-    if (rows && blockIdx.x == 0 && threadIdx.x == 0) *s.scales = Scales{ldexpf(1.0f, -15 - kw), ldexpf(1.0f, -15 - ky)};
+    const int kw = pair_exponent(block_all<kThreads>(m, smf, MaxOp())), ky = pair_exponent(block_all<kThreads>(my, smf, MaxOp()));
+    if (blockIdx.x == 0 && threadIdx.x == 0) *s.scales = Scales{ldexpf(1.0f, -15 - kw), ldexpf(1.0f, -15 - ky)};
     const int64_t n8 = (int64_t)g.V * g.C / 8, step = (int64_t)gridDim.x * kThreads;
-    const float sw = pow2(kw);
+    const float sw = pow2(kw), sy = pow2(ky);
 #pragma unroll 4
     for (int64_t k = blockIdx.x * (int64_t)kThreads + threadIdx.x; k < n8; k += step) {
         const int64_t i = n8 - 1 - k;       // backwards: the end of W is what head_max_kernel has left in L2
@@ -542,17 +410,11 @@ __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, 
     const int C4 = g.C / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t nx = g.N * C4;
     for (int64_t row = blockIdx.x * (int64_t)(kThreads / 32) + warp; row < g.N; row += gridDim.x * (int64_t)(kThreads / 32)) {
-        float mx = 0.f;
-        for (int c = lane; c < C4; c += 32) mx = max4(mx, ld4(g.x, row * C4 + c));
-        const int kx = pair_exponent(warp_max(mx));
-        const float sx = pow2(kx), sy = pow2(ky), gr = rows ? rows[row].g : 0.f;
+        const int kx = row_to_pairs(g.x, g.x_lo, row, C4, s.x16, nx);
+        const float gr = rows[row].g;
         for (int c = lane; c < C4; c += 32) {
             const float4 v = ld_value(g.x, g.x_lo, row * C4 + c);
             uint2 h, l;
-            pairs4(v, sx, h, l);
-            reinterpret_cast<uint2*>(s.x16)[row * C4 + c] = h;
-            reinterpret_cast<uint2*>(s.x16)[nx + row * C4 + c] = l;
-            if (!rows) continue;
             pairs4(make_float4(v.x * gr, v.y * gr, v.z * gr, v.w * gr), sy, h, l);
             if (gr == 0.f) h = l = make_uint2(0u, 0u);          // whatever the row holds
             reinterpret_cast<uint2*>(s.y16)[row * C4 + c] = h;
@@ -561,6 +423,36 @@ __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, 
         // scores whose factor leaves this range are zero to FP32, or beyond it
         if (lane == 0) s.rowf[row] = ldexpf(kLog2e / g.aim.tau, max(-120, min(120, -kx - kw)));
     }
+}
+
+// A teacher's entries of a row by ascending column, those that are not there behind all columns.
+__global__ void __launch_bounds__(kThreads) head_sort_kernel(const HeadArgs g, int2* entries) {
+    __shared__ unsigned long long key[kMaxEntries];
+    pdl_wait();
+    pdl_trigger();
+    const int64_t row = blockIdx.x;
+    const LossAim& a = g.aim;
+    int n = 1;
+    while (n < a.K) n *= 2;
+    for (int k = threadIdx.x; k < n; k += kThreads) {
+        int id = -1;
+        if (k < a.K && entry_logit(a, row, k, g.V, g.bad, id) == -INFINITY) id = -1;
+        key[k] = ((unsigned long long)(id < 0 ? INT_MAX : id) << 32) | (unsigned)k;
+    }
+    for (int size = 2; size <= n; size *= 2)
+        for (int d = size / 2; d > 0; d /= 2) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < n / 2; i += kThreads) {
+                const int lo = (i / d) * 2 * d + i % d, hi = lo + d;
+                const unsigned long long x = key[lo], y = key[hi];
+                if ((x > y) == ((lo & size) == 0)) {
+                    key[lo] = y;
+                    key[hi] = x;
+                }
+            }
+        }
+    __syncthreads();
+    for (int k = threadIdx.x; k < a.K; k += kThreads) entries[row * a.K + k] = make_int2((int)(key[k] >> 32), (int)(unsigned)key[k]);
 }
 
 // The teacher's part of a piece of u.
@@ -590,18 +482,14 @@ int grid_for(int64_t threads, int most) {
     return (int)(n < 1 ? 1 : n < most ? n : most);
 }
 
-cudaError_t make_pairs(const HeadArgs& g, const Scratch& w, bool back, cudaStream_t s) {
-    BT_KERNEL_LAUNCH((head_max_kernel), kParts, kThreads, 0, s, g, back ? w.rows : nullptr, w.rowmax, w.wpart, w.ypart, back ? nullptr : w.head);
-    BT_COUNT_LAUNCH();
-    BT_KERNEL_LAUNCH((head_pairs_kernel), 148 * 8, kThreads, 0, s, g, back ? w.rows : nullptr, w);
-    BT_COUNT_LAUNCH();
-    return cudaGetLastError();
-}
-
 HalfMat pair_matrix(const __half* p, int64_t rows, int64_t cols) { return HalfMat{p, rows * cols, rows, cols, cols}; }
 
 cudaError_t backward_in_pieces(const HeadArgs& g, const Scratch& w, int K, cudaStream_t s) {
-    cudaError_t e = make_pairs(g, w, true, s);
+    BT_KERNEL_LAUNCH((head_max_kernel), kParts, kThreads, 0, s, g, (const RowParams*)w.rows, (const float*)w.rowmax, w.wpart, w.ypart);
+    BT_COUNT_LAUNCH();
+    BT_KERNEL_LAUNCH((head_pairs_kernel), 148 * 8, kThreads, 0, s, g, (const RowParams*)w.rows, w);
+    BT_COUNT_LAUNCH();
+    cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const HalfMat x = pair_matrix(w.x16, g.N, g.C), y = pair_matrix(w.y16, g.N, g.C);
     const int ldu = piece_columns(g.N, g.V, g.piece);
@@ -626,13 +514,12 @@ cudaError_t backward_in_pieces(const HeadArgs& g, const Scratch& w, int K, cudaS
     return cudaGetLastError();
 }
 
-constexpr size_t rows_smem(int NR, int C) { return (size_t)NR * C * sizeof(float); }
-
 }  // namespace
 
-size_t head_fwd_scratch_bytes(int64_t N, int C, int V, int) {
+size_t head_fwd_scratch_bytes(int64_t N, int C, int V, int K) {
+    if (N < 1) return kHeadHeader;
     Scratch s;
-    return fwd_layout(s, nullptr, N, C, V);
+    return fwd_layout(s, nullptr, N, C, V, K);
 }
 
 size_t head_bwd_scratch_bytes(int64_t N, int C, int V, int K, int piece) {
@@ -641,72 +528,32 @@ size_t head_bwd_scratch_bytes(int64_t N, int C, int V, int K, int piece) {
     return bwd_layout(s, nullptr, N, C, V, K, piece);
 }
 
-namespace {
-
-// x of more than two rows takes four rows of W at a time, one and two take eight: 32 products or fewer per lane
-template <int NR, bool PLANES>
-cudaError_t few_fwd(const HeadArgs& g, const Scratch& w, cudaStream_t s) {
-    constexpr int RV = NR > 2 ? 4 : 8;
-    const cudaError_t e = allow_smem<head_stats_rows_kernel<NR, RV, PLANES>>(rows_smem(NR, 4096));
-    if (e != cudaSuccess) return e;
-    BT_KERNEL_LAUNCH((head_stats_rows_kernel<NR, RV, PLANES>), kStrips, kThreads, rows_smem(NR, g.C), s, g, (int)g.N, w.stats, w.head);
-    BT_COUNT_LAUNCH();
-    return cudaGetLastError();
-}
-
-template <int NR, bool PLANES>
-cudaError_t few_bwd(const HeadArgs& g, const Scratch& w, int K, cudaStream_t s) {
-    constexpr int RV = NR > 2 ? 4 : 8;
-    const cudaError_t e = allow_smem<head_grad_rows_kernel<NR, RV, PLANES>>(rows_smem(NR, 4096));
-    if (e != cudaSuccess) return e;
-    const int rows = (int)g.N, C4 = g.C / 4, tx = C4 < kThreads ? C4 : kThreads, ry = kThreads / tx, strips = kStrips / ry < 1 ? 1 : kStrips / ry;
-    BT_KERNEL_LAUNCH((head_grad_rows_kernel<NR, RV, PLANES>), kStrips, kThreads, rows_smem(NR, g.C), s, g, rows, (const RowParams*)w.rows, w.u);
-    BT_COUNT_LAUNCH();
-    if (K) {
-        BT_KERNEL_LAUNCH((head_grad_entries_kernel), (rows * K + 255) / 256, 256, 0, s, rows, NR, K, (const RowParams*)w.rows, (const int*)w.eid,
-                         (const float*)w.ep, w.u);
-        BT_COUNT_LAUNCH();
-    }
-    BT_KERNEL_LAUNCH((head_products_rows_kernel<NR, PLANES>), dim3(strips, (C4 + tx - 1) / tx), dim3(tx, ry), 0, s, g, rows, (const float*)w.u, w.dx_part);
-    BT_COUNT_LAUNCH();
-    if (g.dx || g.dx_hi) {
-        BT_KERNEL_LAUNCH((head_dx_rows_kernel), (rows * C4 + 31) / 32, 256, 0, s, g, rows, NR, strips * ry, (const float*)w.dx_part);
-        BT_COUNT_LAUNCH();
-    }
-    return cudaGetLastError();
-}
-
-template <bool PLANES>
-cudaError_t few_fwd_any(const HeadArgs& g, const Scratch& w, cudaStream_t s) {
-    return g.N > 4 ? few_fwd<8, PLANES>(g, w, s) : g.N > 2 ? few_fwd<4, PLANES>(g, w, s) : g.N > 1 ? few_fwd<2, PLANES>(g, w, s) : few_fwd<1, PLANES>(g, w, s);
-}
-template <bool PLANES>
-cudaError_t few_bwd_any(const HeadArgs& g, const Scratch& w, int K, cudaStream_t s) {
-    return g.N > 4 ? few_bwd<8, PLANES>(g, w, K, s) : g.N > 2 ? few_bwd<4, PLANES>(g, w, K, s)
-                   : g.N > 1 ? few_bwd<2, PLANES>(g, w, K, s) : few_bwd<1, PLANES>(g, w, K, s);
-}
-
-}  // namespace
-
 cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     Scratch w;
-    fwd_layout(w, g.scratch, g.N, g.C, g.V);
+    const int K = g.aim.targets ? 0 : g.aim.K;
+    fwd_layout(w, g.scratch, g.N, g.C, g.V, K);
+    const bool few = few_rows(g.N, false);
+    const int strips = few ? head_few_strips(g.N, g.C, g.V) : head_stats_strips(g.V);
     cudaError_t e;
-    int strips = kStrips;
-    if (few_rows(g.N)) {
-e = g.w_lo ? few_fwd_any<true>(g, w, s) : few_fwd_any<false>(g, w, s);
+    if (few) {
+        e = launch_head_few_stats(g, w.stats, w.head, s);
     } else {
-        strips = head_stats_strips(g.V);
-        e = make_pairs(g, w, false, s);
-        if (e == cudaSuccess)
-            e = launch_head_stats(pair_matrix(w.x16, g.N, g.C), pair_matrix(w.w16, g.V, g.C), w.rowf, w.stats, &w.head->err, s);
+        BT_KERNEL_LAUNCH((head_row_pairs_kernel), 148 * 8, kThreads, 0, s, g, w);
+        BT_COUNT_LAUNCH();
+        if (K) {
+            BT_KERNEL_LAUNCH((head_sort_kernel), (unsigned)g.N, kThreads, 0, s, g, w.entries);
+            BT_COUNT_LAUNCH();
+        }
+        e = launch_head_stats(pair_matrix(w.x16, g.N, g.C), pair_matrix(w.w16, g.V, g.C), w.rowf, w.colf, K, w.entries, w.zk, w.stats, &w.head->err, s);
     }
     if (e != cudaSuccess) return e;
-    if (g.aim.targets && !few_rows(g.N))
-        BT_KERNEL_LAUNCH((head_finish_target_kernel), (unsigned)((g.N + kFinishThreads / 32 - 1) / (kFinishThreads / 32)), kFinishThreads, 0, s, g,
-                         (const float2*)w.stats, strips, w.head);
-    else
+    const unsigned ctas = (unsigned)((g.N + kFinishThreads / 32 - 1) / (kFinishThreads / 32));
+    if (!K)
+        BT_KERNEL_LAUNCH((head_finish_target_kernel), ctas, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
+    else if (few)
         BT_KERNEL_LAUNCH((head_finish_kernel), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
+    else
+        BT_KERNEL_LAUNCH((head_finish_entries_kernel), ctas, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, (const float*)w.zk, w.head);
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }
@@ -719,8 +566,8 @@ cudaError_t launch_head_bwd(const HeadArgs& g, cudaStream_t s) {
     BT_COUNT_LAUNCH();
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    if (!few_rows(g.N)) return backward_in_pieces(g, w, K, s);
-    return g.w_lo ? few_bwd_any<true>(g, w, K, s) : few_bwd_any<false>(g, w, K, s);
+    if (!few_rows(g.N, true)) return backward_in_pieces(g, w, K, s);
+    return launch_head_few_grad(g, w.rows, K, w.eid, w.ep, w.aim, w.dx_part, s);
 }
 
 }  // namespace bt

@@ -31,8 +31,10 @@ struct HalfMat {
 };
 int head_stats_strips(int V);
 size_t head_partial_bytes();
-// stats [N][head_stats_strips(V)] = (maximum, sum) of z in units of log 2 over strips of columns; rowf: from accumulators there.
-cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, float2* stats, int* err, cudaStream_t s);
+// stats [N][head_stats_strips(V)] = (maximum, sum) of z in units of log 2 over strips of columns, by rowf [N] and colf [V] from
+// accumulators there; zk [N][K] = z of the entries, of which `entries` [N][K] holds (column, place in zk) by ascending column.
+cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, const float* colf, int K, const int2* entries, float* zk,
+                              float2* stats, int* err, cudaStream_t s);
 // u = 2^15 (q - [v = target]) as pairs for the columns v0 .. v0 + w.rows - 1, zero in rows without part in the loss.
 cudaError_t launch_head_grad(const HalfMat& x, const HalfMat& w, int v0, const float* rowf, const RowParams* rows, __half* u, int64_t ldu,
                              int64_t u_plane, int* err, cudaStream_t s);
@@ -40,6 +42,15 @@ cudaError_t launch_head_grad(const HalfMat& x, const HalfMat& w, int v0, const f
 cudaError_t launch_head_dx(const HalfMat& u, const HalfMat& w, const RowParams* rows, const float* scale, bool onto, float* dx, float* partials,
                            int* err, cudaStream_t s);
 cudaError_t launch_head_dw(const HalfMat& u, const HalfMat& y, const float* scale, float* dw, float* partials, int* err, cudaStream_t s);
+
+// Few rows in plain FP32 (head_rows.cu): statistics [N][head_few_strips(N, C, V)]; gradients with a table [V][kFewRows] and parts
+// of dx [head_few_parts(N, C, V)][kFewRows][C] in scratch.
+constexpr int kFewRows = 8;                 // of x in one pass over the weights
+int head_few_strips(int64_t N, int C, int V);
+size_t head_few_parts(int64_t N, int C, int V);
+cudaError_t launch_head_few_stats(const HeadArgs& g, float2* stats, HeadHeader* head, cudaStream_t s);
+cudaError_t launch_head_few_grad(const HeadArgs& g, const RowParams* params, int K, const int* eid, const float* ep, float* aim, float* dx_part,
+                                 cudaStream_t s);
 
 // Logit of entry k of a row in units of the softened softmax, -inf where there is none (a weight of zero).  An id
 // behind the vocabulary counts as id 0 and is recorded.

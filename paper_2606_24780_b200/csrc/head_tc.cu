@@ -21,6 +21,8 @@
 #include <cuda.h>
 #include <cuda_fp16.h>
 
+#include <climits>
+
 #include "head.cuh"
 #include "tc_common.cuh"
 
@@ -63,6 +65,10 @@ struct Args {
     float* partials;                        // [tail_splits][tail_tiles][rows of a tile][BN]
     int* err;
     const float* rowf;                      // [M] factor from accumulator to units of log 2
+    const float* colf;                      // kStats: [N] the columns' part of it
+    int K;                                  // kStats: entries per row
+    const int2* entries;
+    float* zk;
     float2* stats;                          // kStats: [M][kParts tiles_n]
     const RowParams* rows;                  // kGrad
     int v0;                                 // kGrad: first column of this piece
@@ -320,20 +326,51 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
             const int row0 = w.tm * kTileRows + (int)rank * BM + quad * 32, row = row0 + lane;
             const int col0 = w.tn * BN + part * kCols, cols = g.N - col0;      // cols may be below zero
             if (EPI == kStats) {
-                if (row < g.M) {
+                if (row < g.M && cols > 0) {
+                    const float f = g.rowf[row] * g.grow;
+                    const float4* cf = reinterpret_cast<const float4*>(g.colf + col0);     // padded to a multiple of 256 columns
+#pragma unroll
+                    for (int j = 0; j < kCols / 4; ++j) {
+                        const float4 t = cf[j];
+                        v[4 * j] *= t.x * f; v[4 * j + 1] *= t.y * f; v[4 * j + 2] *= t.z * f; v[4 * j + 3] *= t.w * f;
+                    }
+                    if (g.K) {
+                        const int2* list = g.entries + (long long)row * g.K;
+                        int lo = 0, n = g.K;                // the first entry from col0 on
+                        while (n > 0) {
+                            const int h = n / 2;
+                            if (list[lo + h].x < col0) {
+                                lo += h + 1;
+                                n -= h + 1;
+                            } else {
+                                n = h;
+                            }
+                        }
+                        int2 next = lo < g.K ? list[lo] : make_int2(INT_MAX, 0);
+#pragma unroll
+                        for (int c = 0; c < kCols / 16; ++c) {
+                            if (next.x >= col0 + c * 16 + 16) continue;
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                while (next.x == col0 + c * 16 + j) {
+                                    g.zk[(long long)row * g.K + next.y] = v[c * 16 + j];
+                                    next = ++lo < g.K ? list[lo] : make_int2(INT_MAX, 0);
+                                }
+                        }
+                    }
                     if (cols < kCols) {
 #pragma unroll
                         for (int j = 0; j < kCols; ++j)
                             if (j >= cols) v[j] = -INFINITY;
                     }
-                    const float f = g.rowf[row] * g.grow;
                     float m = v[0], s = 0.f;
 #pragma unroll
                     for (int j = 1; j < kCols; ++j) m = fmaxf(m, v[j]);
-                    const float mf = m * f;
 #pragma unroll
-                    for (int j = 0; j < kCols; ++j) s += ex2_fast(fmaf(v[j], f, -mf));
-                    g.stats[(long long)row * (kParts * g.tiles_n) + kParts * w.tn + part] = cols > 0 ? make_float2(mf, s) : make_float2(-INFINITY, 0.f);
+                    for (int j = 0; j < kCols; ++j) s += ex2_fast(v[j] - m);
+                    g.stats[(long long)row * (kParts * g.tiles_n) + kParts * w.tn + part] = make_float2(m, s);
+                } else if (row < g.M) {
+                    g.stats[(long long)row * (kParts * g.tiles_n) + kParts * w.tn + part] = make_float2(-INFINITY, 0.f);
                 }
             } else if (EPI == kGrad) {
                 const RowParams r = row < g.M ? g.rows[row] : RowParams{INFINITY, 0.f, 0.f, -1};
@@ -521,10 +558,11 @@ cudaError_t launch_out(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, c
 int head_stats_strips(int V) { return kParts * ((V + 255) / 256); }
 size_t head_partial_bytes() { return (size_t)148 * BM * 256 * sizeof(float); }
 
-cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, float2* stats, int* err, cudaStream_t s) {
+cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, const float* colf, int K, const int2* entries, float* zk,
+                              float2* stats, int* err, cudaStream_t s) {
     Args g{};
     g.M = (int)x.rows; g.N = (int)w.rows;
-    g.rowf = rowf; g.stats = stats; g.err = err;
+    g.rowf = rowf; g.colf = colf; g.K = K; g.entries = entries; g.zk = zk; g.stats = stats; g.err = err;
     return launch_wide<false, false, kStats>(g, x, w, x.cols, s);
 }
 
