@@ -32,6 +32,7 @@ struct Scratch {
     float2* stats;                          // forward: [N][strips]
     float* colf;                            // forward, tensor cores: [V] up to a multiple of 256
     int2* entries;                          // [N][K]
+    uint16_t* strip_first;                  // [N][strips + 1]
     float* zk;                              // [N][K]
     RowParams* rows;                        // backward: [N]
     int* eid;                               // [N][K] columns of the aim, each once; below zero: none
@@ -86,6 +87,7 @@ size_t fwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K) {
     s.colf = take<float>(base, at, (V + 255) / 256 * 256);
     s.entries = take<int2>(base, at, (size_t)N * K);
     s.zk = take<float>(base, at, (size_t)N * K);
+    if (K) s.strip_first = take<uint16_t>(base, at, (size_t)N * (head_stats_strips(V) + 1));
     return at;
 }
 
@@ -353,23 +355,49 @@ __device__ __forceinline__ void pairs4(float4 v, float s, uint2& hi, uint2& lo) 
     lo = make_uint2(*reinterpret_cast<const uint32_t*>(&c), *reinterpret_cast<const uint32_t*>(&d));
 }
 
-// A row of C values as pairs at its own power of two, which it returns; by a warp.
+// A row of C values as pairs at its own power of two, which it returns; by a warp.  Up to 1,024 values stay in registers between the
+// search for the largest and the conversion.
+template <bool HELD>
 __device__ __forceinline__ int row_to_pairs(const float* v, const float* v_lo, int64_t row, int C4, __half* out, int64_t plane4) {
+    constexpr int kHeld = HELD ? 8 : 1;
     const int lane = threadIdx.x & 31;
+    float4 t[kHeld];
     float m = 0.f;
-    for (int c = lane; c < C4; c += 32) m = max4(m, ld4(v, row * C4 + c));
+    if (HELD) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (lane + 32 * i < C4) t[i] = ld4(v, row * C4 + lane + 32 * i);
+        if (v_lo) {
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                if (lane + 32 * i < C4) t[i] = add4(t[i], ld4(v_lo, row * C4 + lane + 32 * i));
+        }
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (lane + 32 * i < C4) m = max4(m, t[i]);
+    } else {
+        for (int c = lane; c < C4; c += 32) m = max4(m, ld4(v, row * C4 + c));
+    }
     const int k = pair_exponent(warp_max(m));
     const float s = pow2(k);
-    for (int c = lane; c < C4; c += 32) {
+    auto put = [&](int c, float4 x) {
         uint2 h, l;
-        pairs4(ld_value(v, v_lo, row * C4 + c), s, h, l);
+        pairs4(x, s, h, l);
         reinterpret_cast<uint2*>(out)[row * C4 + c] = h;
         reinterpret_cast<uint2*>(out)[plane4 + row * C4 + c] = l;
+    };
+    if (HELD) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (lane + 32 * i < C4) put(lane + 32 * i, t[i]);
+    } else {
+        for (int c = lane; c < C4; c += 32) put(c, ld_value(v, v_lo, row * C4 + c));
     }
     return k;
 }
 
 // Forward: the rows of W and x as pairs, each at its own power of two, which the epilogue takes out of its column or row.
+template <bool HELD>
 __global__ void __launch_bounds__(kThreads) head_row_pairs_kernel(const HeadArgs g, const Scratch s) {
     pdl_wait();
     pdl_trigger();
@@ -378,7 +406,8 @@ __global__ void __launch_bounds__(kThreads) head_row_pairs_kernel(const HeadArgs
     const int64_t step = gridDim.x * (int64_t)(kThreads / 32), first = blockIdx.x * (int64_t)(kThreads / 32) + warp;
     for (int64_t row = first; row < g.V + g.N; row += step) {
         const bool of_w = row < g.V;
-        const int k = of_w ? row_to_pairs(g.w, g.w_lo, row, C4, s.w16, (int64_t)g.V * C4) : row_to_pairs(g.x, g.x_lo, row - g.V, C4, s.x16, g.N * C4);
+        const int k = of_w ? row_to_pairs<HELD>(g.w, g.w_lo, row, C4, s.w16, (int64_t)g.V * C4)
+                           : row_to_pairs<HELD>(g.x, g.x_lo, row - g.V, C4, s.x16, g.N * C4);
         // 2^-k reaches 2^-126: the factor of a row of x is log2 e / tau 2^-k, a number of FP32 in any case
         if (lane == 0) (of_w ? s.colf[row] : s.rowf[row - g.V]) = of_w ? ldexpf(1.0f, -k) : ldexpf(kLog2e / g.aim.tau, -k);
     }
@@ -410,7 +439,7 @@ __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, 
     const int C4 = g.C / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t nx = g.N * C4;
     for (int64_t row = blockIdx.x * (int64_t)(kThreads / 32) + warp; row < g.N; row += gridDim.x * (int64_t)(kThreads / 32)) {
-        const int kx = row_to_pairs(g.x, g.x_lo, row, C4, s.x16, nx);
+        const int kx = row_to_pairs<false>(g.x, g.x_lo, row, C4, s.x16, nx);
         const float gr = rows[row].g;
         for (int c = lane; c < C4; c += 32) {
             const float4 v = ld_value(g.x, g.x_lo, row * C4 + c);
@@ -425,8 +454,8 @@ __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, 
     }
 }
 
-// A teacher's entries of a row by ascending column, those that are not there behind all columns.
-__global__ void __launch_bounds__(kThreads) head_sort_kernel(const HeadArgs g, int2* entries) {
+// A teacher's entries of a row by ascending column, those that are not there behind all columns, and where each strip's begin.
+__global__ void __launch_bounds__(kThreads) head_sort_kernel(const HeadArgs g, int2* entries, uint16_t* strip_first, int strips) {
     __shared__ unsigned long long key[kMaxEntries];
     pdl_wait();
     pdl_trigger();
@@ -453,6 +482,20 @@ __global__ void __launch_bounds__(kThreads) head_sort_kernel(const HeadArgs g, i
         }
     __syncthreads();
     for (int k = threadIdx.x; k < a.K; k += kThreads) entries[row * a.K + k] = make_int2((int)(key[k] >> 32), (int)(unsigned)key[k]);
+    for (int t = threadIdx.x; t <= strips; t += kThreads) {
+        const unsigned long long from = (unsigned long long)t * kStripCols << 32;
+        int lo = 0, left = a.K;             // the first entry from there on
+        while (left > 0) {
+            const int h = left / 2;
+            if (key[lo + h] < from) {
+                lo += h + 1;
+                left -= h + 1;
+            } else {
+                left = h;
+            }
+        }
+        strip_first[row * (strips + 1) + t] = (uint16_t)lo;
+    }
 }
 
 // The teacher's part of a piece of u.
@@ -538,13 +581,15 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     if (few) {
         e = launch_head_few_stats(g, w.stats, w.head, s);
     } else {
-        BT_KERNEL_LAUNCH((head_row_pairs_kernel), 148 * 8, kThreads, 0, s, g, w);
+        if (g.C <= 1024) BT_KERNEL_LAUNCH((head_row_pairs_kernel<true>), 148 * 8, kThreads, 0, s, g, w);
+        else BT_KERNEL_LAUNCH((head_row_pairs_kernel<false>), 148 * 8, kThreads, 0, s, g, w);
         BT_COUNT_LAUNCH();
         if (K) {
-            BT_KERNEL_LAUNCH((head_sort_kernel), (unsigned)g.N, kThreads, 0, s, g, w.entries);
+            BT_KERNEL_LAUNCH((head_sort_kernel), (unsigned)g.N, kThreads, 0, s, g, w.entries, w.strip_first, strips);
             BT_COUNT_LAUNCH();
         }
-        e = launch_head_stats(pair_matrix(w.x16, g.N, g.C), pair_matrix(w.w16, g.V, g.C), w.rowf, w.colf, K, w.entries, w.zk, w.stats, &w.head->err, s);
+        e = launch_head_stats(pair_matrix(w.x16, g.N, g.C), pair_matrix(w.w16, g.V, g.C), w.rowf, w.colf, K, w.entries, w.strip_first, w.zk,
+                              w.stats, &w.head->err, s);
     }
     if (e != cudaSuccess) return e;
     const unsigned ctas = (unsigned)((g.N + kFinishThreads / 32 - 1) / (kFinishThreads / 32));

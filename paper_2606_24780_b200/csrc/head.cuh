@@ -32,9 +32,11 @@ struct HalfMat {
 int head_stats_strips(int V);
 size_t head_partial_bytes();
 // stats [N][head_stats_strips(V)] = (maximum, sum) of z in units of log 2 over strips of columns, by rowf [N] and colf [V] from
-// accumulators there; zk [N][K] = z of the entries, of which `entries` [N][K] holds (column, place in zk) by ascending column.
-cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, const float* colf, int K, const int2* entries, float* zk,
-                              float2* stats, int* err, cudaStream_t s);
+// accumulators there; zk [N][K] = z of the entries, of which `entries` [N][K] holds (column, place in zk) by ascending column
+// and strip_first [N][head_stats_strips(V) + 1] the first of each strip.
+constexpr int kStripCols = 128;
+cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, const float* colf, int K, const int2* entries,
+                              const uint16_t* strip_first, float* zk, float2* stats, int* err, cudaStream_t s);
 // u = 2^15 (q - [v = target]) as pairs for the columns v0 .. v0 + w.rows - 1, zero in rows without part in the loss.
 cudaError_t launch_head_grad(const HalfMat& x, const HalfMat& w, int v0, const float* rowf, const RowParams* rows, __half* u, int64_t ldu,
                              int64_t u_plane, int* err, cudaStream_t s);

@@ -2,8 +2,8 @@
 // it is in registers: its scores z, and in the backward its gradient dW_v = sum_n u_vn x_n and its part of dx_n = sum_v u_vn W_v.
 //
 // A group of threads owns a share of the vocabulary, a thread of it four columns (eight, from 2,048 on) of every row: x, the
-// sums for dx and the current four rows of W are in registers.  The dot products are folded over a warp, 32 of them at a
-// time, in 31 shuffles, and over the group through shared memory.  Rows come in by asynchronous copies, sixteen values of
+// sums for dx and the current four rows of W are in registers.  The dot products are folded over a warp, sixteen of
+// them in sixteen shuffles, and over the group through shared memory.  Rows come in by asynchronous copies, sixteen values of
 // four ahead, into places that no other thread reads: what bounds the kernel is the copies' rate (HBM).
 #include "head.cuh"
 
@@ -17,11 +17,38 @@ __host__ __device__ constexpr int batch_rows(int nr, int cols) { return cols > 1
 __device__ __forceinline__ void copy16(float4* dst, const float4* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
 }
-__device__ __forceinline__ float dot4(float4 a, float4 b, float acc) {
-    return fmaf(a.w, b.w, fmaf(a.z, b.z, fmaf(a.y, b.y, fmaf(a.x, b.x, acc))));
+// Four values as two pairs: the SM multiplies and adds FP32 pairs in one instruction.
+struct V4 {
+    unsigned long long a, b;
+};
+__device__ __forceinline__ unsigned long long fma2(unsigned long long x, unsigned long long y, unsigned long long z) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+    return r;
 }
-__device__ __forceinline__ float4 fma4(float t, float4 a, float4 acc) {
-    return make_float4(fmaf(t, a.x, acc.x), fmaf(t, a.y, acc.y), fmaf(t, a.z, acc.z), fmaf(t, a.w, acc.w));
+__device__ __forceinline__ unsigned long long add2(unsigned long long x, unsigned long long y) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ unsigned long long both(float v) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float sum_of(unsigned long long v) {
+    float lo, hi;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+    return lo + hi;
+}
+__device__ __forceinline__ V4 ldv(const float4* p) {
+    const ulonglong2 t = *reinterpret_cast<const ulonglong2*>(p);
+    return V4{t.x, t.y};
+}
+__device__ __forceinline__ V4 addv(V4 x, V4 y) { return V4{add2(x.a, y.a), add2(x.b, y.b)}; }
+__device__ __forceinline__ V4 fmav(unsigned long long t, V4 x, V4 acc) { return V4{fma2(t, x.a, acc.a), fma2(t, x.b, acc.b)}; }
+__device__ __forceinline__ void stv(float4* p, V4 v) {
+    asm volatile("st.global.cs.v2.b64 [%0], {%1, %2};" ::"l"(p), "l"(v.a), "l"(v.b) : "memory");
 }
 
 // CTAs per SM: of up to 256 threads three for one or two rows of x, two for more; one of more threads.
@@ -37,9 +64,11 @@ struct Few {
     HeadHeader* head;
 };
 
-template <int NR, int COLS, bool PLANES, bool BACK, int THREADS>
-__global__ void __launch_bounds__(THREADS, few_ctas(NR, THREADS)) head_few_kernel(const HeadArgs g, const Few a) {
-    constexpr int kBatch = batch_rows(NR, COLS), kForms = PLANES ? 2 : 1, kDepth = 16 / (kBatch * kForms * COLS), R = kBatch * NR, kShare = 32 / R;
+template <int ROWS, int COLS, bool PLANES, bool BACK, int THREADS>
+__global__ void __launch_bounds__(THREADS, few_ctas(ROWS, THREADS)) head_few_kernel(const HeadArgs g, const Few a) {
+    // products are counted for a power of two of rows
+    constexpr int NR = ROWS > 4 ? 8 : ROWS > 2 ? 4 : ROWS, kBatch = batch_rows(NR, COLS), kForms = PLANES ? 2 : 1, kDepth = 16 / (kBatch * kForms * COLS);
+    constexpr int R = kBatch * NR, kFold = R > 16 ? 16 : R, kFoldRows = kFold / NR, kShare = 32 / kFold;
     extern __shared__ float4 slots[];       // [kDepth][kBatch][COLS][kForms][threads]: sixteen values of four per thread
     __shared__ float part[2][16][32];       // [parity][warp][product]
     __shared__ __align__(16) float us[16][32];
@@ -71,18 +100,18 @@ __global__ void __launch_bounds__(THREADS, few_ctas(NR, THREADS)) head_few_kerne
     };
     for (int b = 0; b < kDepth; ++b) fetch(b);
 
-    float4 x[NR][COLS], dx[NR][COLS];
+    V4 x[ROWS][COLS], dx[ROWS][COLS];
 #pragma unroll
-    for (int n = 0; n < NR; ++n)
+    for (int n = 0; n < ROWS; ++n)
 #pragma unroll
         for (int k = 0; k < COLS; ++k) {
             const int c = t + a.G * k;
-            x[n][k] = dx[n][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            x[n][k] = dx[n][k] = V4{0ull, 0ull};
             if (n >= a.rows || c >= C4) continue;
             if (BACK && a.params[a.row0 + n].L == INFINITY) continue;      // the row has no part in the loss, whatever it holds
             const int64_t i = (a.row0 + n) * C4 + c;
-            x[n][k] = ld4(g.x, i);
-            if (g.x_lo) x[n][k] = add4(x[n][k], ld4(g.x_lo, i));
+            x[n][k] = ldv(reinterpret_cast<const float4*>(g.x) + i);
+            if (g.x_lo) x[n][k] = addv(x[n][k], ldv(reinterpret_cast<const float4*>(g.x_lo) + i));
         }
     const int my_n = t % NR;                // of the product that this thread sums up over the group (t < R)
     RowParams mine{INFINITY, 0.f, 0.f, -1};
@@ -92,45 +121,52 @@ __global__ void __launch_bounds__(THREADS, few_ctas(NR, THREADS)) head_few_kerne
     for (int b = 0; b < batches; ++b) {
         asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
         const int64_t v0 = v_first + (int64_t)b * kBatch;
-        float4 w[kBatch][COLS];
+        V4 w[kBatch][COLS];
 #pragma unroll
         for (int r = 0; r < kBatch; ++r)
 #pragma unroll
             for (int k = 0; k < COLS; ++k) {
-                w[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                w[r][k] = V4{0ull, 0ull};
                 if (v0 + r >= v_end || t + a.G * k >= C4) continue;
                 const float4* src = slots + (((b % kDepth) * kBatch + r) * COLS + k) * kForms * blockDim.x + threadIdx.x;
-                w[r][k] = PLANES ? add4(src[0], src[blockDim.x]) : src[0];
+                w[r][k] = PLANES ? addv(ldv(src), ldv(src + blockDim.x)) : ldv(src);
             }
         fetch(b + kDepth);                  // into the places just read
 
-        float acc[R];
+        // sixteen products at a time: every step halves those that a lane carries and doubles the lanes summed, and lane l ends
+        // with product l / kShare
 #pragma unroll
-        for (int r = 0; r < kBatch; ++r)
+        for (int r0 = 0; r0 < kBatch; r0 += kFoldRows) {
+            float acc[kFold];
 #pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                acc[r * NR + n] = 0.f;
+            for (int r = 0; r < kFoldRows; ++r)
 #pragma unroll
-                for (int k = 0; k < COLS; ++k) acc[r * NR + n] = dot4(w[r][k], x[n][k], acc[r * NR + n]);
+                for (int n = 0; n < NR; ++n) {
+                    unsigned long long p = 0ull;
+                    if (n < ROWS) {
+#pragma unroll
+                        for (int k = 0; k < COLS; ++k) p = fma2(w[r0 + r][k].b, x[n % ROWS][k].b, fma2(w[r0 + r][k].a, x[n % ROWS][k].a, p));
+                    }
+                    acc[r * NR + n] = sum_of(p);
+                }
+            int o = 16;
+#pragma unroll
+            for (int half = kFold / 2; half >= 1; half /= 2, o /= 2) {
+                const bool up = lane & o;
+#pragma unroll
+                for (int i = 0; i < half; ++i) {
+                    const float keep = up ? acc[i + half] : acc[i], give = up ? acc[i] : acc[i + half];
+                    acc[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+                }
             }
-        // every step halves the products that a lane carries and doubles the lanes summed; lane l ends with product l / kShare
-        int o = 16;
+            float z = acc[0];
 #pragma unroll
-        for (int half = R / 2; half >= 1; half /= 2, o /= 2) {
-            const bool up = lane & o;
-#pragma unroll
-            for (int i = 0; i < half; ++i) {
-                const float keep = up ? acc[i + half] : acc[i], give = up ? acc[i] : acc[i + half];
-                acc[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-            }
+            for (; o >= 1; o /= 2) z += __shfl_xor_sync(0xffffffffu, z, o);
+            if ((lane & (kShare - 1)) == 0) part[b & 1][wi][r0 * NR + lane / kShare] = z;
         }
-        float z = acc[0];
-#pragma unroll
-        for (; o >= 1; o /= 2) z += __shfl_xor_sync(0xffffffffu, z, o);
-        if ((lane & (kShare - 1)) == 0) part[b & 1][wi][lane / kShare] = z;
         __syncthreads();
         if (t < R) {
-            z = part[b & 1][w0][t];
+            float z = part[b & 1][w0][t];
             for (int k = w0 + 1; k < w1; ++k) z += part[b & 1][k][t];
             const int64_t v = v0 + t / NR;
             if (!BACK) {
@@ -152,16 +188,16 @@ __global__ void __launch_bounds__(THREADS, few_ctas(NR, THREADS)) head_few_kerne
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < kBatch; ++r) {
-            float4 d[COLS];
+            V4 d[COLS];
 #pragma unroll
-            for (int k = 0; k < COLS; ++k) d[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < COLS; ++k) d[k] = V4{0ull, 0ull};
 #pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                const float u = us[gi][r * NR + n];
+            for (int n = 0; n < ROWS; ++n) {
+                const unsigned long long u = both(us[gi][r * NR + n]);
 #pragma unroll
                 for (int k = 0; k < COLS; ++k) {
-                    dx[n][k] = fma4(u, w[r][k], dx[n][k]);
-                    d[k] = fma4(u, x[n][k], d[k]);
+                    dx[n][k] = fmav(u, w[r][k], dx[n][k]);
+                    d[k] = fmav(u, x[n][k], d[k]);
                 }
             }
             if (g.dw && v0 + r < v_end) {
@@ -170,19 +206,19 @@ __global__ void __launch_bounds__(THREADS, few_ctas(NR, THREADS)) head_few_kerne
                     const int c = t + a.G * k;
                     if (c >= C4) continue;
                     float4* out = reinterpret_cast<float4*>(g.dw) + (v0 + r) * C4 + c;
-                    if (a.row0) __stcs(out, add4(*out, d[k]));
-                    else __stcs(out, d[k]);
+                    stv(out, a.row0 ? addv(ldv(out), d[k]) : d[k]);
                 }
             }
         }
     }
     if (BACK) {
         if (!a.dx_part) return;
-        for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int n = 0; n < ROWS; ++n)
 #pragma unroll
             for (int k = 0; k < COLS; ++k) {
                 const int c = t + a.G * k;
-                if (n < a.rows && c < C4) reinterpret_cast<float4*>(a.dx_part)[(at * kFewRows + n) * C4 + c] = dx[n][k];
+                if (n < a.rows && c < C4) stv(reinterpret_cast<float4*>(a.dx_part) + (at * kFewRows + n) * C4 + c, dx[n][k]);
             }
     } else {
         if (t < R) ends[gi][t] = make_float2(m, s);
@@ -247,13 +283,13 @@ int ctas_of(const Shape& p, int V, int per_sm) {
     return want < 1 ? 1 : want < most ? want : most;
 }
 
-template <int NR, int COLS, bool PLANES, bool BACK, int THREADS>
+template <int ROWS, int COLS, bool PLANES, bool BACK, int THREADS>
 cudaError_t launch(const HeadArgs& g, const Few& a, const Shape& p, int grid, cudaStream_t s) {
     constexpr size_t smem = (size_t)16 * THREADS * sizeof(float4);
-    const cudaError_t e = allow_smem<head_few_kernel<NR, COLS, PLANES, BACK, THREADS>>(smem);
+    const cudaError_t e = allow_smem<head_few_kernel<ROWS, COLS, PLANES, BACK, THREADS>>(smem);
     if (e != cudaSuccess) return e;
     const int threads = p.G * p.groups;
-    BT_KERNEL_LAUNCH((head_few_kernel<NR, COLS, PLANES, BACK, THREADS>), grid, threads, (size_t)16 * threads * sizeof(float4), s, g, a);
+    BT_KERNEL_LAUNCH((head_few_kernel<ROWS, COLS, PLANES, BACK, THREADS>), grid, threads, (size_t)16 * threads * sizeof(float4), s, g, a);
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }
@@ -262,7 +298,7 @@ template <bool PLANES, bool BACK>
 cudaError_t launch_rows(const HeadArgs& g, const Few& a, const Shape& p, int grid, cudaStream_t s) {
     if (p.cols == 2) return a.rows > 2 ? launch<4, 2, PLANES, BACK, 512>(g, a, p, grid, s) : launch<2, 2, PLANES, BACK, 512>(g, a, p, grid, s);
     if (p.G > 256) return a.rows > 4 ? launch<8, 1, PLANES, BACK, 512>(g, a, p, grid, s) : launch<4, 1, PLANES, BACK, 512>(g, a, p, grid, s);
-    return a.rows > 4 ? launch<8, 1, PLANES, BACK, 256>(g, a, p, grid, s) : a.rows > 2 ? launch<4, 1, PLANES, BACK, 256>(g, a, p, grid, s)
+    return a.rows > 6 ? launch<8, 1, PLANES, BACK, 256>(g, a, p, grid, s) : a.rows > 4 ? launch<6, 1, PLANES, BACK, 256>(g, a, p, grid, s) : a.rows > 2 ? launch<4, 1, PLANES, BACK, 256>(g, a, p, grid, s)
          : a.rows > 1 ? launch<2, 1, PLANES, BACK, 256>(g, a, p, grid, s) : launch<1, 1, PLANES, BACK, 256>(g, a, p, grid, s);
 }
 

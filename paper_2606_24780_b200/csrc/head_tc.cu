@@ -21,8 +21,6 @@
 #include <cuda.h>
 #include <cuda_fp16.h>
 
-#include <climits>
-
 #include "head.cuh"
 #include "tc_common.cuh"
 
@@ -66,8 +64,9 @@ struct Args {
     int* err;
     const float* rowf;                      // [M] factor from accumulator to units of log 2
     const float* colf;                      // kStats: [N] the columns' part of it
-    int K;                                  // kStats: entries per row
+    int K;                                  // kStats: entries per row, with those of each strip of kStripCols columns
     const int2* entries;
+    const uint16_t* strip_first;            // [M][strips + 1]
     float* zk;
     float2* stats;                          // kStats: [M][kParts tiles_n]
     const RowParams* rows;                  // kGrad
@@ -297,6 +296,16 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
         bool ok = true;
         for (int u = first; u < units && ok; u += step) {
             const Unit w = unit_at(g, u);
+            const int row0 = w.tm * kTileRows + (int)rank * BM + quad * 32, row = row0 + lane;
+            const int col0 = w.tn * BN + part * kCols, cols = g.N - col0;      // cols may be below zero
+            int e_at = 0, e_end = 0;
+            int2 entry = make_int2(0, 0);
+            if (EPI == kStats && g.K && row < g.M) {
+                const uint16_t* f = g.strip_first + (long long)row * (kParts * g.tiles_n + 1) + kParts * w.tn + part;
+                e_at = f[0];
+                e_end = f[1];
+                if (e_at < e_end) entry = g.entries[(long long)row * g.K + e_at];
+            }
             float v[kCols];
             for (int k0 = w.kb0; k0 < w.kb1; k0 += kChunk, ++at) {
                 const int acc = at & 1;
@@ -323,9 +332,23 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
                 }
             }
             if (!ok) break;
-            const int row0 = w.tm * kTileRows + (int)rank * BM + quad * 32, row = row0 + lane;
-            const int col0 = w.tn * BN + part * kCols, cols = g.N - col0;      // cols may be below zero
             if (EPI == kStats) {
+                // scores of the row's entries in this strip, the first of which is here already
+                while (__any_sync(0xffffffffu, e_at < e_end)) {
+                    const int c = e_at < e_end ? entry.x - col0 : -1;
+                    float z = 0.f;
+#pragma unroll
+                    for (int q = 0; q < kCols / 16; ++q) {
+                        if (!__any_sync(0xffffffffu, (c >> 4) == q)) continue;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (c == q * 16 + j) z = v[q * 16 + j];
+                    }
+                    if (e_at < e_end) {
+                        g.zk[(long long)row * g.K + entry.y] = z * (g.rowf[row] * g.grow * g.colf[entry.x]);
+                        if (++e_at < e_end) entry = g.entries[(long long)row * g.K + e_at];
+                    }
+                }
                 if (row < g.M && cols > 0) {
                     const float f = g.rowf[row] * g.grow;
                     const float4* cf = reinterpret_cast<const float4*>(g.colf + col0);     // padded to a multiple of 256 columns
@@ -333,30 +356,6 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
                     for (int j = 0; j < kCols / 4; ++j) {
                         const float4 t = cf[j];
                         v[4 * j] *= t.x * f; v[4 * j + 1] *= t.y * f; v[4 * j + 2] *= t.z * f; v[4 * j + 3] *= t.w * f;
-                    }
-                    if (g.K) {
-                        const int2* list = g.entries + (long long)row * g.K;
-                        int lo = 0, n = g.K;                // the first entry from col0 on
-                        while (n > 0) {
-                            const int h = n / 2;
-                            if (list[lo + h].x < col0) {
-                                lo += h + 1;
-                                n -= h + 1;
-                            } else {
-                                n = h;
-                            }
-                        }
-                        int2 next = lo < g.K ? list[lo] : make_int2(INT_MAX, 0);
-#pragma unroll
-                        for (int c = 0; c < kCols / 16; ++c) {
-                            if (next.x >= col0 + c * 16 + 16) continue;
-#pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                while (next.x == col0 + c * 16 + j) {
-                                    g.zk[(long long)row * g.K + next.y] = v[c * 16 + j];
-                                    next = ++lo < g.K ? list[lo] : make_int2(INT_MAX, 0);
-                                }
-                        }
                     }
                     if (cols < kCols) {
 #pragma unroll
@@ -555,14 +554,15 @@ cudaError_t launch_out(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, c
 
 }  // namespace
 
+static_assert(256 / kParts == kStripCols, "a strip is what one warp holds of a tile's columns");
 int head_stats_strips(int V) { return kParts * ((V + 255) / 256); }
 size_t head_partial_bytes() { return (size_t)148 * BM * 256 * sizeof(float); }
 
-cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, const float* colf, int K, const int2* entries, float* zk,
-                              float2* stats, int* err, cudaStream_t s) {
+cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, const float* colf, int K, const int2* entries,
+                              const uint16_t* strip_first, float* zk, float2* stats, int* err, cudaStream_t s) {
     Args g{};
     g.M = (int)x.rows; g.N = (int)w.rows;
-    g.rowf = rowf; g.colf = colf; g.K = K; g.entries = entries; g.zk = zk; g.stats = stats; g.err = err;
+    g.rowf = rowf; g.colf = colf; g.K = K; g.entries = entries; g.strip_first = strip_first; g.zk = zk; g.stats = stats; g.err = err;
     return launch_wide<false, false, kStats>(g, x, w, x.cols, s);
 }
 
