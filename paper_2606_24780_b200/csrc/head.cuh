@@ -18,7 +18,7 @@ struct HeadHeader {
 constexpr size_t kHeadHeader = 256;
 inline size_t head_pad(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
-struct RowParams {                          // backward, per row
+struct __align__(16) RowParams {            // backward, per row
     float L, L_rest;                        // lse in units of log 2 and its rounding; +inf: the row has no part in the loss
     float g;                                // inv_count w tau S
     int target;                             // column whose aim is 1; below zero: none

@@ -306,6 +306,10 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
                 e_end = f[1];
                 if (e_at < e_end) entry = g.entries[(long long)row * g.K + e_at];
             }
+            RowParams rp{INFINITY, 0.f, 0.f, -1};
+            float f = 0.f;
+            if (EPI != kOut && row < g.M) f = g.rowf[row] * g.grow;
+            if (EPI == kGrad && row < g.M) rp = g.rows[row];
             float v[kCols];
             for (int k0 = w.kb0; k0 < w.kb1; k0 += kChunk, ++at) {
                 const int acc = at & 1;
@@ -345,12 +349,11 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
                             if (c == q * 16 + j) z = v[q * 16 + j];
                     }
                     if (e_at < e_end) {
-                        g.zk[(long long)row * g.K + entry.y] = z * (g.rowf[row] * g.grow * g.colf[entry.x]);
+                        g.zk[(long long)row * g.K + entry.y] = z * (f * g.colf[entry.x]);
                         if (++e_at < e_end) entry = g.entries[(long long)row * g.K + e_at];
                     }
                 }
                 if (row < g.M && cols > 0) {
-                    const float f = g.rowf[row] * g.grow;
                     const float4* cf = reinterpret_cast<const float4*>(g.colf + col0);     // padded to a multiple of 256 columns
 #pragma unroll
                     for (int j = 0; j < kCols / 4; ++j) {
@@ -372,17 +375,21 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
                     g.stats[(long long)row * (kParts * g.tiles_n) + kParts * w.tn + part] = make_float2(-INFINITY, 0.f);
                 }
             } else if (EPI == kGrad) {
-                const RowParams r = row < g.M ? g.rows[row] : RowParams{INFINITY, 0.f, 0.f, -1};
-                const float f = row < g.M ? g.rowf[row] * g.grow : 0.f;
-                const bool live = r.L != INFINITY;
-                const int hit = r.target < 0 ? -1 : r.target - g.v0 - col0;
+                // 2^15 q = 2^(z - L): what L - 15 is rounded by, and z - L at a q of one, is 2^-22
+                const float L = (rp.L - 15.0f) + rp.L_rest;
+                const bool live = rp.L != INFINITY, all_live = __all_sync(0xffffffffu, live);
+                const int hit = rp.target < 0 ? -1 : rp.target - g.v0 - col0;
                 __half* dst = g.u + row * g.ldu + col0;
 #pragma unroll
                 for (int c = 0; c < kCols / 16; ++c) {
                     if (c * 16 >= cols) break;
                     float e[16];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) e[j] = live ? 32768.0f * ex2_fast(fmaf(v[c * 16 + j], f, -r.L) - r.L_rest) : 0.f;
+                    for (int j = 0; j < 16; ++j) e[j] = ex2_fast(fmaf(v[c * 16 + j], f, -L));
+                    if (!all_live) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) e[j] = live ? e[j] : 0.f;
+                    }
                     if (__any_sync(0xffffffffu, hit >= c * 16 && hit < c * 16 + 16)) {
 #pragma unroll
                         for (int j = 0; j < 16; ++j)
