@@ -248,7 +248,9 @@ cudaError_t launch_softmax_distill(const DistillArgs& g, cudaStream_t s) {
     int cs = 1;
     while (cs < 8 && ((g.N * cs * 2 <= 2 * sms && n4 > 512 * kBatch / 2 * cs) || 3 * sms / cs * n4 * 16 > ((int64_t)100 << 20))) cs *= 2;
     cudaError_t e;
-    if (cs == 1) e = n4 > 128 * kBatch ? launch_rows<512, 1>(g, s) : launch_rows<128, 1>(g, s);
+    // short rows: more of them at a time on CTAs of 128 threads.  5,171 x 3,321 39 us against 81 on 512 threads, 8,000 x 8,000 105
+    // against 148, 8,000 x 16,000 217 on 512 threads, 196 on 256, whose wide rows are slower (762 us against 717 at 50,257)
+    if (cs == 1) e = n4 > 128 * 40 ? launch_rows<512, 1>(g, s) : n4 > 128 * 16 ? launch_rows<256, 1>(g, s) : launch_rows<128, 1>(g, s);
     else e = cs == 2 ? launch_rows<512, 2>(g, s) : cs == 4 ? launch_rows<512, 4>(g, s) : launch_rows<512, 8>(g, s);
     if (e != cudaSuccess) return e;
     BT_COUNT_LAUNCH();

@@ -18,7 +18,8 @@ namespace bt {
 
 namespace {
 
-constexpr int kParts = 592;                 // CTAs that look for the largest value
+constexpr int kParts = 592;                 // CTAs that look for the largest of W
+__host__ __device__ constexpr int row_ctas(int64_t N) { return N < 1184 ? (int)N : 1184; }     // and those that look at the rows
 constexpr int kThreads = 256;
 constexpr int kFinishThreads = 256;
 
@@ -42,16 +43,19 @@ struct Scratch {
     float* dx_part;                         // [parts][kFewRows][C]
     // tensor cores
     Scales* scales;
-    float *wpart, *ypart;                   // [kParts] largest values
-    float* rowmax;                          // [N]
+    float *wpart, *ypart;                   // [kParts], [row_ctas(N)] largest values
     float* rowf;                            // [N]
     __half *x16, *y16, *w16, *u16;          // pairs: [2][N][C], [2][N][C], [2][V][C], [2][N][ldu]
     float* partials;
 };
 
-// Rows up to which the plain kernels are used: two passes over the weights in the forward, one in the backward, where a second one
-// would add to dW.  C 768, V 50,257, raw: 9 to 16 rows 98 us against 133 on the tensor cores, 17 to 24 148; gradients 266 against 210.
-bool few_rows(int64_t N, bool back) { return N <= (back ? 1 : 2) * kFewRows; }
+// Rows up to which the plain kernels are used.  Forward: two passes of eight over the weights, 16 rows against V 50,257, C 768,
+// raw 99 us, on the tensor cores 107; 24 rows 141 and 107.  Backward: a second pass adds to dW, so only one, but two where W
+// is small (9 to 16 rows, V 5,000, C 256: 39 to 43 us, on the tensor cores 61; V 23,670, C 320: 82 to 94 and 70).
+bool few_rows(int64_t N, int C, int V, bool back) {
+    const bool two = !back || (int64_t)V * C <= (1 << 22);
+    return N <= (two ? 2 : 1) * kFewRows;
+}
 
 // Columns of one piece of the vocabulary, a multiple of 256: pieces of about the same size, of at most `piece` columns or
 // 512 MB of u.
@@ -71,7 +75,6 @@ T* take(uint8_t* base, size_t& at, size_t n) {
 
 void tc_layout(Scratch& s, uint8_t* base, size_t& at, int64_t N, int C, int V) {
     s.scales = take<Scales>(base, at, 1);
-    s.wpart = take<float>(base, at, kParts);
     s.rowf = take<float>(base, at, N);
     s.x16 = take<__half>(base, at, 2 * (size_t)N * C);
     s.w16 = take<__half>(base, at, 2 * (size_t)V * C);
@@ -81,8 +84,8 @@ size_t fwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K) {
     size_t at = kHeadHeader;
     s = Scratch{};
     s.head = (HeadHeader*)base;
-    s.stats = take<float2>(base, at, (size_t)N * (few_rows(N, false) ? head_few_strips(N, C, V) : head_stats_strips(V)));
-    if (few_rows(N, false)) return at;
+    s.stats = take<float2>(base, at, (size_t)N * (few_rows(N, C, V, false) ? head_few_strips(N, C, V) : head_stats_strips(V)));
+    if (few_rows(N, C, V, false)) return at;
     tc_layout(s, base, at, N, C, V);
     s.colf = take<float>(base, at, (V + 255) / 256 * 256);
     s.entries = take<int2>(base, at, (size_t)N * K);
@@ -98,14 +101,14 @@ size_t bwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K, int
     s.rows = take<RowParams>(base, at, N);
     s.eid = take<int>(base, at, (size_t)N * K);
     s.ep = take<float>(base, at, (size_t)N * K);
-    if (few_rows(N, true)) {
+    if (few_rows(N, C, V, true)) {
         if (K) s.aim = take<float>(base, at, (size_t)V * kFewRows);
-        s.dx_part = take<float>(base, at, head_few_parts(N, C, V) * kFewRows * C);
+        s.dx_part = take<float>(base, at, (size_t)head_few_strips(N, C, V) * kFewRows * C);
         return at;
     }
     tc_layout(s, base, at, N, C, V);
-    s.ypart = take<float>(base, at, kParts);
-    s.rowmax = take<float>(base, at, N);
+    s.wpart = take<float>(base, at, kParts);
+    s.ypart = take<float>(base, at, row_ctas(N));
     s.y16 = take<__half>(base, at, 2 * (size_t)N * C);
     s.u16 = take<__half>(base, at, 2 * (size_t)N * piece_columns(N, V, piece));
     s.partials = take<float>(base, at, head_partial_bytes() / sizeof(float));
@@ -253,68 +256,82 @@ __device__ __forceinline__ float max4(float m, float4 v) {
     return fmaxf(fmaxf(m, fmaxf(fabsf(v.x), fabsf(v.y))), fmaxf(fabsf(v.z), fabsf(v.w)));
 }
 
-// One row per CTA: what the backward needs to know of it.  Entries with the same id are joined into the first of them.
+// What the backward needs to know of the rows, one at a time per CTA, and the largest values of W and of y_nc = g_n x_nc.  Entries with the same id are joined into the first of them.
 __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArgs g, RowParams* rows, int* eid, float* ep,
-                                                                   float* rowmax, HeadHeader* head) {
+                                                                   float* wpart, float* ypart, HeadHeader* head) {
     extern __shared__ int ids[];            // [K], then the weights [K]
     __shared__ float smf[kFinishThreads / 32];
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0 && threadIdx.x == 0) *head = HeadHeader{0, 0u};
-    const int64_t row = blockIdx.x;
-    const LossAim& a = g.aim;
-    RowParams r;
-    const double L = (double)g.lse_in[row] * 1.4426950408889634;
-    r.L = (float)L;
-    r.L_rest = isfinite(r.L) ? (float)(L - (double)r.L) : 0.f;
-    r.g = a.inv_count * row_weight(a, row) * a.tau;
-    r.target = -1;
-    bool live = r.g != 0.f;
-    if (a.targets) {
-        const int t = a.targets[row];
-        live = live && t >= 0;
-        r.target = t >= g.V ? 0 : t;
-    } else {
-        float* p = (float*)(ids + a.K);
-        bool any;
-        const float norm = teacher_norm<kFinishThreads>(a, row, g.V, nullptr, smf, any);
-        float sum = 0.f;
-        for (int k = threadIdx.x; k < a.K; k += kFinishThreads) {
-            int id = -1;
-            const float t = any ? entry_logit(a, row, k, g.V, nullptr, id) : -INFINITY;
-            p[k] = any ? expf(t - norm) : 0.f;
-            ids[k] = p[k] != 0.f ? id : -1;
-            sum += p[k];
-        }
-        sum = block_all<kFinishThreads>(sum, smf, SumOp());
-        live = live && sum != 0.f;
-        r.g *= sum;
-        for (int k = threadIdx.x; k < a.K; k += kFinishThreads) {
-            const int id = ids[k];
-            float w = 0.f;
-            bool first = live && id >= 0;
-            for (int j = 0; first && j < a.K; ++j) {
-                if (ids[j] != id) continue;
-                if (j < k) first = false;
-                else w += p[j];
-            }
-            eid[row * a.K + k] = first ? id : -1;
-            ep[row * a.K + k] = w / sum;
-        }
-    }
-    if (!live) {
-        r.L = INFINITY;
-        r.L_rest = 0.f;
-        r.g = 0.f;
-        r.target = -1;
-    }
-    if (threadIdx.x == 0) rows[row] = r;
-    if (rowmax && live) {                   // the same for all threads
+    const int w_ctas = wpart ? kParts : 0;
+    if ((int)blockIdx.x < w_ctas) {         // the largest of W, a part per CTA
+        const int64_t n4 = (int64_t)g.V * (g.C / 4), step = (int64_t)w_ctas * kFinishThreads;
         float m = 0.f;
-        for (int c = threadIdx.x; c < g.C / 4; c += kFinishThreads) m = max4(m, ld4(g.x, row * (g.C / 4) + c));
+#pragma unroll 8
+        for (int64_t i = blockIdx.x * (int64_t)kFinishThreads + threadIdx.x; i < n4; i += step) m = max4(m, ld4(g.w, i));
         m = block_all<kFinishThreads>(m, smf, MaxOp());
-        if (threadIdx.x == 0) rowmax[row] = m;
+        if (threadIdx.x == 0) wpart[blockIdx.x] = m;
+        return;
     }
+    const int ctas = gridDim.x - w_ctas;
+    float ymax = 0.f;
+    for (int64_t row = blockIdx.x - w_ctas; row < g.N; row += ctas) {
+        const LossAim& a = g.aim;
+        RowParams r;
+        const double L = (double)g.lse_in[row] * 1.4426950408889634;
+        r.L = (float)L;
+        r.L_rest = isfinite(r.L) ? (float)(L - (double)r.L) : 0.f;
+        r.g = a.inv_count * row_weight(a, row) * a.tau;
+        r.target = -1;
+        bool live = r.g != 0.f;
+        if (a.targets) {
+            const int t = a.targets[row];
+            live = live && t >= 0;
+            r.target = t >= g.V ? 0 : t;
+        } else {
+            float* p = (float*)(ids + a.K);
+            bool any;
+            const float norm = teacher_norm<kFinishThreads>(a, row, g.V, nullptr, smf, any);
+            float sum = 0.f;
+            for (int k = threadIdx.x; k < a.K; k += kFinishThreads) {
+                int id = -1;
+                const float t = any ? entry_logit(a, row, k, g.V, nullptr, id) : -INFINITY;
+                p[k] = any ? expf(t - norm) : 0.f;
+                ids[k] = p[k] != 0.f ? id : -1;
+                sum += p[k];
+            }
+            sum = block_all<kFinishThreads>(sum, smf, SumOp());
+            live = live && sum != 0.f;
+            r.g *= sum;
+            for (int k = threadIdx.x; k < a.K; k += kFinishThreads) {
+                const int id = ids[k];
+                float w = 0.f;
+                bool first = live && id >= 0;
+                for (int j = 0; first && j < a.K; ++j) {
+                    if (ids[j] != id) continue;
+                    if (j < k) first = false;
+                    else w += p[j];
+                }
+                eid[row * a.K + k] = first ? id : -1;
+                ep[row * a.K + k] = w / sum;
+            }
+        }
+        if (!live) {
+            r.L = INFINITY;
+            r.L_rest = 0.f;
+            r.g = 0.f;
+            r.target = -1;
+        }
+        if (threadIdx.x == 0) rows[row] = r;
+        if (ypart && live && r.g != 0.f) {      // the same for all threads
+            float m = 0.f;
+            for (int c = threadIdx.x; c < g.C / 4; c += kFinishThreads) m = max4(m, ld4(g.x, row * (g.C / 4) + c));
+            ymax = fmaxf(ymax, fabsf(r.g) * block_all<kFinishThreads>(m, smf, MaxOp()));
+        }
+        __syncthreads();                        // the entries in shared memory have been read
+    }
+    if (ypart && threadIdx.x == 0) ypart[blockIdx.x - w_ctas] = ymax;
 }
 
 // ---------------------------------------------------------------- FP16 pairs
@@ -326,25 +343,6 @@ __device__ __forceinline__ int pair_exponent(float m) {
 }
 __device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
-// Largest absolute values of W and of y_nc = g_n x_nc, per CTA.
-__global__ void __launch_bounds__(kThreads) head_max_kernel(const HeadArgs g, const RowParams* __restrict__ rows,
-                                                            const float* __restrict__ rowmax, float* wpart, float* ypart) {
-    __shared__ float smf[kThreads / 32];
-    pdl_wait();
-    pdl_trigger();
-    const int64_t n4 = (int64_t)g.V * (g.C / 4), step = (int64_t)gridDim.x * kThreads;
-    float m = 0.f;
-#pragma unroll 8
-    for (int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x; i < n4; i += step) m = max4(m, ld4(g.w, i));
-    m = block_all<kThreads>(m, smf, MaxOp());
-    if (threadIdx.x == 0) wpart[blockIdx.x] = m;
-    m = 0.f;
-    for (int64_t n = blockIdx.x * (int64_t)kThreads + threadIdx.x; n < g.N; n += step)
-        if (rows[n].g != 0.f) m = fmaxf(m, fabsf(rows[n].g) * rowmax[n]);
-    m = block_all<kThreads>(m, smf, MaxOp());
-    if (threadIdx.x == 0) ypart[blockIdx.x] = m;
-}
-
 // Four values times s as pairs.
 __device__ __forceinline__ void pairs4(float4 v, float s, uint2& hi, uint2& lo) {
     const float t[4] = {v.x * s, v.y * s, v.z * s, v.w * s};
@@ -355,30 +353,34 @@ __device__ __forceinline__ void pairs4(float4 v, float s, uint2& hi, uint2& lo) 
     lo = make_uint2(*reinterpret_cast<const uint32_t*>(&c), *reinterpret_cast<const uint32_t*>(&d));
 }
 
-// A row of C values as pairs at its own power of two, which it returns; by a warp.  Up to 1,024 values stay in registers between the
-// search for the largest and the conversion.
-template <bool HELD>
-__device__ __forceinline__ int row_to_pairs(const float* v, const float* v_lo, int64_t row, int C4, __half* out, int64_t plane4) {
-    constexpr int kHeld = HELD ? 8 : 1;
-    const int lane = threadIdx.x & 31;
+// A row of C values as pairs at its own power of two, which it returns; by LANES neighbouring lanes.  Rows of up to 32 LANES values
+// stay in registers between the search for the largest and the conversion.
+template <int LANES>
+__device__ __forceinline__ int row_to_pairs(const float* v, const float* v_lo, int64_t row, bool there, int C4, __half* out, int64_t plane4) {
+    constexpr int kHeld = 8;
+    const int lane = threadIdx.x % LANES;
+    const bool held = C4 <= kHeld * LANES;
     float4 t[kHeld];
     float m = 0.f;
-    if (HELD) {
+    if (held) {
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i)
-            if (lane + 32 * i < C4) t[i] = ld4(v, row * C4 + lane + 32 * i);
+        for (int i = 0; i < kHeld; ++i) {
+            t[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (there && lane + LANES * i < C4) t[i] = ld4(v, row * C4 + lane + LANES * i);
+        }
         if (v_lo) {
 #pragma unroll
             for (int i = 0; i < kHeld; ++i)
-                if (lane + 32 * i < C4) t[i] = add4(t[i], ld4(v_lo, row * C4 + lane + 32 * i));
+                if (there && lane + LANES * i < C4) t[i] = add4(t[i], ld4(v_lo, row * C4 + lane + LANES * i));
         }
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i)
-            if (lane + 32 * i < C4) m = max4(m, t[i]);
-    } else {
-        for (int c = lane; c < C4; c += 32) m = max4(m, ld4(v, row * C4 + c));
+        for (int i = 0; i < kHeld; ++i) m = max4(m, t[i]);
+    } else if (there) {
+        for (int c = lane; c < C4; c += LANES) m = max4(m, ld4(v, row * C4 + c));
     }
-    const int k = pair_exponent(warp_max(m));
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const int k = pair_exponent(m);
     const float s = pow2(k);
     auto put = [&](int c, float4 x) {
         uint2 h, l;
@@ -386,30 +388,32 @@ __device__ __forceinline__ int row_to_pairs(const float* v, const float* v_lo, i
         reinterpret_cast<uint2*>(out)[row * C4 + c] = h;
         reinterpret_cast<uint2*>(out)[plane4 + row * C4 + c] = l;
     };
-    if (HELD) {
+    if (held) {
 #pragma unroll
         for (int i = 0; i < kHeld; ++i)
-            if (lane + 32 * i < C4) put(lane + 32 * i, t[i]);
-    } else {
-        for (int c = lane; c < C4; c += 32) put(c, ld_value(v, v_lo, row * C4 + c));
+            if (there && lane + LANES * i < C4) put(lane + LANES * i, t[i]);
+    } else if (there) {
+        for (int c = lane; c < C4; c += LANES) put(c, ld_value(v, v_lo, row * C4 + c));
     }
     return k;
 }
 
 // Forward: the rows of W and x as pairs, each at its own power of two, which the epilogue takes out of its column or row.
-template <bool HELD>
+template <int LANES>
 __global__ void __launch_bounds__(kThreads) head_row_pairs_kernel(const HeadArgs g, const Scratch s) {
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0 && threadIdx.x == 0) *s.head = HeadHeader{0, 0u};
-    const int C4 = g.C / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t step = gridDim.x * (int64_t)(kThreads / 32), first = blockIdx.x * (int64_t)(kThreads / 32) + warp;
-    for (int64_t row = first; row < g.V + g.N; row += step) {
-        const bool of_w = row < g.V;
-        const int k = of_w ? row_to_pairs<HELD>(g.w, g.w_lo, row, C4, s.w16, (int64_t)g.V * C4)
-                           : row_to_pairs<HELD>(g.x, g.x_lo, row - g.V, C4, s.x16, g.N * C4);
+    const int C4 = g.C / 4;
+    constexpr int kAtOnce = kThreads / LANES;
+    // whole warps stay together: they share a base, and lanes whose row does not exist go along
+    for (int64_t base = blockIdx.x * (int64_t)kAtOnce; base < g.V + g.N; base += gridDim.x * (int64_t)kAtOnce) {
+        const int64_t at = base + threadIdx.x / LANES;
+        const bool of_w = at < g.V, there = at < g.V + g.N;
+        const int64_t row = of_w ? at : at - g.V;
+        const int k = row_to_pairs<LANES>(of_w ? g.w : g.x, of_w ? g.w_lo : g.x_lo, row, there, C4, of_w ? s.w16 : s.x16, (of_w ? (int64_t)g.V : g.N) * C4);
         // 2^-k reaches 2^-126: the factor of a row of x is log2 e / tau 2^-k, a number of FP32 in any case
-        if (lane == 0) (of_w ? s.colf[row] : s.rowf[row - g.V]) = of_w ? ldexpf(1.0f, -k) : ldexpf(kLog2e / g.aim.tau, -k);
+        if (there && threadIdx.x % LANES == 0) (of_w ? s.colf[row] : s.rowf[row]) = of_w ? ldexpf(1.0f, -k) : ldexpf(kLog2e / g.aim.tau, -k);
     }
 }
 
@@ -419,17 +423,15 @@ __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, 
     pdl_wait();
     pdl_trigger();
     float m = 0.f, my = 0.f;
-    for (int i = threadIdx.x; i < kParts; i += kThreads) {
-        m = fmaxf(m, s.wpart[i]);
-        my = fmaxf(my, s.ypart[i]);
-    }
+    for (int i = threadIdx.x; i < kParts; i += kThreads) m = fmaxf(m, s.wpart[i]);
+    for (int i = threadIdx.x; i < row_ctas(g.N); i += kThreads) my = fmaxf(my, s.ypart[i]);
     const int kw = pair_exponent(block_all<kThreads>(m, smf, MaxOp())), ky = pair_exponent(block_all<kThreads>(my, smf, MaxOp()));
     if (blockIdx.x == 0 && threadIdx.x == 0) *s.scales = Scales{ldexpf(1.0f, -15 - kw), ldexpf(1.0f, -15 - ky)};
     const int64_t n8 = (int64_t)g.V * g.C / 8, step = (int64_t)gridDim.x * kThreads;
     const float sw = pow2(kw), sy = pow2(ky);
 #pragma unroll 4
     for (int64_t k = blockIdx.x * (int64_t)kThreads + threadIdx.x; k < n8; k += step) {
-        const int64_t i = n8 - 1 - k;       // backwards: the end of W is what head_max_kernel has left in L2
+        const int64_t i = n8 - 1 - k;       // backwards: the end of W is what head_rows_kernel has left in L2
         uint2 h0, l0, h1, l1;
         pairs4(ld_value(g.w, g.w_lo, 2 * i), sw, h0, l0);
         pairs4(ld_value(g.w, g.w_lo, 2 * i + 1), sw, h1, l1);
@@ -439,7 +441,7 @@ __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, 
     const int C4 = g.C / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t nx = g.N * C4;
     for (int64_t row = blockIdx.x * (int64_t)(kThreads / 32) + warp; row < g.N; row += gridDim.x * (int64_t)(kThreads / 32)) {
-        const int kx = row_to_pairs<false>(g.x, g.x_lo, row, C4, s.x16, nx);
+        const int kx = row_to_pairs<32>(g.x, g.x_lo, row, true, C4, s.x16, nx);
         const float gr = rows[row].g;
         for (int c = lane; c < C4; c += 32) {
             const float4 v = ld_value(g.x, g.x_lo, row * C4 + c);
@@ -528,8 +530,6 @@ int grid_for(int64_t threads, int most) {
 HalfMat pair_matrix(const __half* p, int64_t rows, int64_t cols) { return HalfMat{p, rows * cols, rows, cols, cols}; }
 
 cudaError_t backward_in_pieces(const HeadArgs& g, const Scratch& w, int K, cudaStream_t s) {
-    BT_KERNEL_LAUNCH((head_max_kernel), kParts, kThreads, 0, s, g, (const RowParams*)w.rows, (const float*)w.rowmax, w.wpart, w.ypart);
-    BT_COUNT_LAUNCH();
     BT_KERNEL_LAUNCH((head_pairs_kernel), 148 * 8, kThreads, 0, s, g, (const RowParams*)w.rows, w);
     BT_COUNT_LAUNCH();
     cudaError_t e = cudaGetLastError();
@@ -575,14 +575,17 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     Scratch w;
     const int K = g.aim.targets ? 0 : g.aim.K;
     fwd_layout(w, g.scratch, g.N, g.C, g.V, K);
-    const bool few = few_rows(g.N, false);
+    const bool few = few_rows(g.N, g.C, g.V, false);
     const int strips = few ? head_few_strips(g.N, g.C, g.V) : head_stats_strips(g.V);
     cudaError_t e;
     if (few) {
         e = launch_head_few_stats(g, w.stats, w.head, s);
     } else {
-        if (g.C <= 1024) BT_KERNEL_LAUNCH((head_row_pairs_kernel<true>), 148 * 8, kThreads, 0, s, g, w);
-        else BT_KERNEL_LAUNCH((head_row_pairs_kernel<false>), 148 * 8, kThreads, 0, s, g, w);
+        // as few lanes to a row as hold it: many rows in flight
+        if (g.C <= 128) BT_KERNEL_LAUNCH((head_row_pairs_kernel<4>), 148 * 8, kThreads, 0, s, g, w);
+        else if (g.C <= 256) BT_KERNEL_LAUNCH((head_row_pairs_kernel<8>), 148 * 8, kThreads, 0, s, g, w);
+        else if (g.C <= 512) BT_KERNEL_LAUNCH((head_row_pairs_kernel<16>), 148 * 8, kThreads, 0, s, g, w);
+        else BT_KERNEL_LAUNCH((head_row_pairs_kernel<32>), 148 * 8, kThreads, 0, s, g, w);
         BT_COUNT_LAUNCH();
         if (K) {
             BT_KERNEL_LAUNCH((head_sort_kernel), (unsigned)g.N, kThreads, 0, s, g, w.entries, w.strip_first, strips);
@@ -607,11 +610,13 @@ cudaError_t launch_head_bwd(const HeadArgs& g, cudaStream_t s) {
     Scratch w;
     const int K = g.aim.targets ? 0 : g.aim.K;
     bwd_layout(w, g.scratch, g.N, g.C, g.V, K, g.piece);
-    BT_KERNEL_LAUNCH((head_rows_kernel), (unsigned)g.N, kFinishThreads, (size_t)K * 8, s, g, w.rows, w.eid, w.ep, w.rowmax, w.head);
+    const bool few = few_rows(g.N, g.C, g.V, true);
+    BT_KERNEL_LAUNCH((head_rows_kernel), row_ctas(g.N) + (few ? 0 : kParts), kFinishThreads, (size_t)K * 8, s, g, w.rows, w.eid, w.ep, w.wpart, w.ypart,
+                     w.head);
     BT_COUNT_LAUNCH();
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    if (!few_rows(g.N, true)) return backward_in_pieces(g, w, K, s);
+    if (!few) return backward_in_pieces(g, w, K, s);
     return launch_head_few_grad(g, w.rows, K, w.eid, w.ep, w.aim, w.dx_part, s);
 }
 

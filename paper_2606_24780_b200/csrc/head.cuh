@@ -46,10 +46,9 @@ cudaError_t launch_head_dx(const HalfMat& u, const HalfMat& w, const RowParams* 
 cudaError_t launch_head_dw(const HalfMat& u, const HalfMat& y, const float* scale, float* dw, float* partials, int* err, cudaStream_t s);
 
 // Few rows in plain FP32 (head_rows.cu): statistics [N][head_few_strips(N, C, V)]; gradients with a table [V][kFewRows] and parts
-// of dx [head_few_parts(N, C, V)][kFewRows][C] in scratch.
+// of dx [head_few_strips(N, C, V)][kFewRows][C] in scratch.
 constexpr int kFewRows = 8;                 // of x in one pass over the weights
 int head_few_strips(int64_t N, int C, int V);
-size_t head_few_parts(int64_t N, int C, int V);
 cudaError_t launch_head_few_stats(const HeadArgs& g, float2* stats, HeadHeader* head, cudaStream_t s);
 cudaError_t launch_head_few_grad(const HeadArgs& g, const RowParams* params, int K, const int* eid, const float* ep, float* aim, float* dx_part,
                                  cudaStream_t s);

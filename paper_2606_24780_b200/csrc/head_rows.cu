@@ -60,7 +60,7 @@ struct Few {
     float2* stats;                          // forward: [N][gridDim.x]
     const RowParams* params;                // backward
     const float* aim;                       // backward: [V][kFewRows] weights of a teacher's entries (nullable)
-    float* dx_part;                         // backward: [parts][kFewRows][C]
+    float* dx_part;                         // backward: [gridDim.x][kFewRows][C]
     HeadHeader* head;
 };
 
@@ -213,12 +213,23 @@ __global__ void __launch_bounds__(THREADS, few_ctas(ROWS, THREADS)) head_few_ker
     }
     if (BACK) {
         if (!a.dx_part) return;
+        // the groups' sums meet in the copies' place: [rows][COLS][threads]
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();
 #pragma unroll
         for (int n = 0; n < ROWS; ++n)
 #pragma unroll
+            for (int k = 0; k < COLS; ++k) *reinterpret_cast<ulonglong2*>(slots + (n * COLS + k) * blockDim.x + threadIdx.x) = make_ulonglong2(dx[n][k].a, dx[n][k].b);
+        __syncthreads();
+        if (gi > 0) return;
+        for (int n = 0; n < a.rows; ++n)
+#pragma unroll
             for (int k = 0; k < COLS; ++k) {
                 const int c = t + a.G * k;
-                if (n < a.rows && c < C4) stv(reinterpret_cast<float4*>(a.dx_part) + (at * kFewRows + n) * C4 + c, dx[n][k]);
+                if (c >= C4) continue;
+                V4 d = ldv(slots + (n * COLS + k) * blockDim.x + t);
+                for (int i = 1; i < groups; ++i) d = addv(d, ldv(slots + (n * COLS + k) * blockDim.x + i * a.G + t));
+                stv(reinterpret_cast<float4*>(a.dx_part) + ((int64_t)blockIdx.x * kFewRows + n) * C4 + c, d);
             }
     } else {
         if (t < R) ends[gi][t] = make_float2(m, s);
@@ -236,7 +247,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(ROWS, THREADS)) head_few_ker
     }
 }
 
-// dx of the rows from the groups' parts, 32 columns of four per CTA.
+// dx of the rows from the CTAs' parts, 32 columns of four per CTA.
 __global__ void __launch_bounds__(256) head_few_dx_kernel(const HeadArgs g, int64_t row0, int parts, const float* __restrict__ dx_part) {
     __shared__ float4 sm[8][32];
     pdl_wait();
@@ -313,8 +324,6 @@ int grid_of(const Shape& p, int V, int64_t rows) {
 }  // namespace
 
 int head_few_strips(int64_t N, int C, int V) { return grid_of(shape_of(C), V, N); }
-size_t head_few_parts(int64_t N, int C, int V) { return (size_t)head_few_strips(N, C, V) * shape_of(C).groups; }
-
 cudaError_t launch_head_few_stats(const HeadArgs& g, float2* stats, HeadHeader* head, cudaStream_t s) {
     const Shape p = shape_of(g.C);
     const int grid = grid_of(p, g.V, g.N);
@@ -347,7 +356,7 @@ cudaError_t launch_head_few_grad(const HeadArgs& g, const RowParams* params, int
         e = g.w_lo ? launch_rows<true, true>(g, a, p, grid, s) : launch_rows<false, true>(g, a, p, grid, s);
         if (e != cudaSuccess) return e;
         if (want_dx) {
-            BT_KERNEL_LAUNCH((head_few_dx_kernel), dim3((g.C / 4 + 31) / 32, a.rows), 256, 0, s, g, row0, grid * p.groups, (const float*)dx_part);
+            BT_KERNEL_LAUNCH((head_few_dx_kernel), dim3((g.C / 4 + 31) / 32, a.rows), 256, 0, s, g, row0, grid, (const float*)dx_part);
             BT_COUNT_LAUNCH();
         }
     }

@@ -450,23 +450,37 @@ head_single_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     run<false, A_MN, B_MN, BN, EPI>(&tmA, &tmB, g);
 }
 
-// The tail's partial tiles, added in the order of their ranges, through kOut's last step.
+// The tail's partial tiles through kOut's last step: LANES threads add every LANES-th range in order, then their sums.
+template <int LANES>
 __global__ void __launch_bounds__(256) join_kernel(const Args g, int tile_rows, int bn) {
+    __shared__ float4 sm[LANES][256 / LANES];
     pdl_wait();
     pdl_trigger();
-    const int bn4 = bn / 4;
+    constexpr int kOuts = 256 / LANES;
+    const int bn4 = bn / 4, y = threadIdx.x / kOuts, at = threadIdx.x % kOuts;
     const long long per = (long long)tile_rows * bn4, total = g.tail_tiles * per;
     const float sc = *g.scale * g.grow;
-    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < total; i += gridDim.x * 256LL) {
+    for (long long base = (long long)blockIdx.x * kOuts; base < total; base += (long long)gridDim.x * kOuts) {     // total is a multiple of kOuts
+        const long long i = base + at;
         const int j = (int)(i / per);
         const long long r = i - j * per;
         const int lr = (int)(r / bn4), c = 4 * (int)(r - (long long)lr * bn4);
         int tm, tn;
         tile_at(g, g.tiles_m * g.tiles_n - g.tail_tiles + j, tm, tn);
         const int row = tm * tile_rows + lr, col = tn * bn + c;
-        if (row >= g.M || col >= g.N) continue;
-        float4 t = ld4(g.partials, i);
-        for (int sp = 1; sp < g.tail_splits; ++sp) t = add4(t, ld4(g.partials, sp * total + i));
+        const bool there = row < g.M && col < g.N;
+        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (there) {
+#pragma unroll 4
+            for (int sp = y; sp < g.tail_splits; sp += LANES) t = add4(t, ld4(g.partials, sp * total + i));
+        }
+        if (LANES > 1) {
+            sm[y][at] = t;
+            __syncthreads();
+            for (int k = 1; y == 0 && k < LANES; ++k) t = add4(t, sm[k][at]);
+            __syncthreads();
+        }
+        if (!there || y > 0) continue;
         const float rg = g.row_g ? g.row_g[row].g : 1.f;
         t = rg == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(t.x * sc * rg, t.y * sc * rg, t.z * sc * rg, t.w * sc * rg);
         float4* p = reinterpret_cast<float4*>(g.out + (long long)row * g.N + col);
@@ -517,10 +531,10 @@ cudaError_t launch(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, cudaS
     g.tail_tiles = g.tail_splits = g.tail_kb = 0;
     const int tiles = g.tiles_m * g.tiles_n;
     if (EPI == kOut && g.partials && tiles % slots) {
-        // as many ranges as the last round has CTAs for, of at least four sums in registers each
+        // as many ranges as the last round has CTAs for, of at least one sum in registers each
         const int tail = tiles % slots;
         int sp = slots / tail;
-        if (sp > g.kb_total / (2 * kChunk)) sp = g.kb_total / (2 * kChunk);
+        if (sp > g.kb_total / kChunk) sp = g.kb_total / kChunk;
         if (sp > 1) {
             g.tail_kb = (g.kb_total + sp - 1) / sp;
             g.tail_splits = (g.kb_total + g.tail_kb - 1) / g.tail_kb;
@@ -540,7 +554,8 @@ cudaError_t launch(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, cudaS
     BT_COUNT_LAUNCH();
     if (g.tail_tiles) {
         const long long want = ((long long)g.tail_tiles * rows * BN / 4 + 255) / 256;
-        BT_KERNEL_LAUNCH((join_kernel), (int)(want < 148 * 8 ? want : 148 * 8), 256, 0, s, g, rows, BN);
+        if (g.tail_splits >= 8) BT_KERNEL_LAUNCH((join_kernel<8>), (int)(8 * want < 148 * 8 ? 8 * want : 148 * 8), 256, 0, s, g, rows, BN);
+        else BT_KERNEL_LAUNCH((join_kernel<1>), (int)(want < 148 * 8 ? want : 148 * 8), 256, 0, s, g, rows, BN);
         BT_COUNT_LAUNCH();
     }
     return cudaGetLastError();
