@@ -84,13 +84,13 @@ size_t fwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K) {
     size_t at = kHeadHeader;
     s = Scratch{};
     s.head = (HeadHeader*)base;
-    s.stats = take<float2>(base, at, (size_t)N * (few_rows(N, C, V, false) ? head_few_strips(N, C, V) : head_stats_strips(V)));
+    s.stats = take<float2>(base, at, (size_t)N * (few_rows(N, C, V, false) ? head_few_strips(N, C, V) : head_stats_strips(N, C, V).count));
     if (few_rows(N, C, V, false)) return at;
     tc_layout(s, base, at, N, C, V);
     s.colf = take<float>(base, at, (V + 255) / 256 * 256);
     s.entries = take<int2>(base, at, (size_t)N * K);
     s.zk = take<float>(base, at, (size_t)N * K);
-    if (K) s.strip_first = take<uint16_t>(base, at, (size_t)N * (head_stats_strips(V) + 1));
+    if (K) s.strip_first = take<uint16_t>(base, at, (size_t)N * (head_stats_strips(N, C, V).count + 1));
     return at;
 }
 
@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, 
 }
 
 // A teacher's entries of a row by ascending column, those that are not there behind all columns, and where each strip's begin.
-__global__ void __launch_bounds__(kThreads) head_sort_kernel(const HeadArgs g, int2* entries, uint16_t* strip_first, int strips) {
+__global__ void __launch_bounds__(kThreads) head_sort_kernel(const HeadArgs g, int2* entries, uint16_t* strip_first, HeadStrips strips) {
     __shared__ unsigned long long key[kMaxEntries];
     pdl_wait();
     pdl_trigger();
@@ -484,8 +484,8 @@ __global__ void __launch_bounds__(kThreads) head_sort_kernel(const HeadArgs g, i
         }
     __syncthreads();
     for (int k = threadIdx.x; k < a.K; k += kThreads) entries[row * a.K + k] = make_int2((int)(key[k] >> 32), (int)(unsigned)key[k]);
-    for (int t = threadIdx.x; t <= strips; t += kThreads) {
-        const unsigned long long from = (unsigned long long)t * kStripCols << 32;
+    for (int t = threadIdx.x; t <= strips.count; t += kThreads) {
+        const unsigned long long from = (unsigned long long)t * strips.cols << 32;
         int lo = 0, left = a.K;             // the first entry from there on
         while (left > 0) {
             const int h = left / 2;
@@ -496,7 +496,7 @@ __global__ void __launch_bounds__(kThreads) head_sort_kernel(const HeadArgs g, i
                 left = h;
             }
         }
-        strip_first[row * (strips + 1) + t] = (uint16_t)lo;
+        strip_first[row * (strips.count + 1) + t] = (uint16_t)lo;
     }
 }
 
@@ -576,7 +576,8 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     const int K = g.aim.targets ? 0 : g.aim.K;
     fwd_layout(w, g.scratch, g.N, g.C, g.V, K);
     const bool few = few_rows(g.N, g.C, g.V, false);
-    const int strips = few ? head_few_strips(g.N, g.C, g.V) : head_stats_strips(g.V);
+    const HeadStrips wide = head_stats_strips(g.N, g.C, g.V);
+    const int strips = few ? head_few_strips(g.N, g.C, g.V) : wide.count;
     cudaError_t e;
     if (few) {
         e = launch_head_few_stats(g, w.stats, w.head, s);
@@ -588,7 +589,7 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
         else BT_KERNEL_LAUNCH((head_row_pairs_kernel<32>), 148 * 8, kThreads, 0, s, g, w);
         BT_COUNT_LAUNCH();
         if (K) {
-            BT_KERNEL_LAUNCH((head_sort_kernel), (unsigned)g.N, kThreads, 0, s, g, w.entries, w.strip_first, strips);
+            BT_KERNEL_LAUNCH((head_sort_kernel), (unsigned)g.N, kThreads, 0, s, g, w.entries, w.strip_first, wide);
             BT_COUNT_LAUNCH();
         }
         e = launch_head_stats(pair_matrix(w.x16, g.N, g.C), pair_matrix(w.w16, g.V, g.C), w.rowf, w.colf, K, w.entries, w.strip_first, w.zk,

@@ -29,12 +29,14 @@ struct HalfMat {
     const __half* hi;
     int64_t plane, rows, cols, ld;
 };
-int head_stats_strips(int V);
+struct HeadStrips {
+    int cols, count;                        // columns of a strip of the statistics, strips per row
+};
+HeadStrips head_stats_strips(int64_t N, int C, int V);
 size_t head_partial_bytes();
-// stats [N][head_stats_strips(V)] = (maximum, sum) of z in units of log 2 over strips of columns, by rowf [N] and colf [V] from
+// stats [N][strips] = (maximum, sum) of z in units of log 2 over strips of columns, by rowf [N] and colf [V] from
 // accumulators there; zk [N][K] = z of the entries, of which `entries` [N][K] holds (column, place in zk) by ascending column
-// and strip_first [N][head_stats_strips(V) + 1] the first of each strip.
-constexpr int kStripCols = 128;
+// and strip_first [N][strips + 1] the first of each strip.
 cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, const float* colf, int K, const int2* entries,
                               const uint16_t* strip_first, float* zk, float2* stats, int* err, cudaStream_t s);
 // u = 2^15 (q - [v = target]) as pairs for the columns v0 .. v0 + w.rows - 1, zero in rows without part in the loss.

@@ -7,7 +7,7 @@
 // of the library's three-product TF32 GEMM, at the same 22 bits.
 //
 // Three products share one kernel; NT z = x W^T, NN dx = u W, TN dW = u^T y, with three epilogues:
-//     kStats  (maximum, sum of exponentials) of 128 columns of a row
+//     kStats  (maximum, sum of exponentials) of a strip, half a tile's columns, of a row
 //     kGrad   u = 2^15 (q - [v = target]) as pairs, the operand of the two others
 //     kOut    FP32, scaled by a power of two and by the row's own factor, over or onto what is there
 //
@@ -64,7 +64,7 @@ struct Args {
     int* err;
     const float* rowf;                      // [M] factor from accumulator to units of log 2
     const float* colf;                      // kStats: [N] the columns' part of it
-    int K;                                  // kStats: entries per row, with those of each strip of kStripCols columns
+    int K;                                  // kStats: entries per row, with the first of each strip
     const int2* entries;
     const uint16_t* strip_first;            // [M][strips + 1]
     float* zk;
@@ -514,6 +514,12 @@ float growth(int kb_total) {
     return (float)(1.0 + 0.5 * 0.56 / (1 << 24) * nn / n);
 }
 
+// Ranges of K for each tile of the last round: as many as it has CTAs for, of at least one sum in registers each.
+int ranges_of(int tail, int slots, int kb_total) {
+    const int sp = slots / tail < kb_total / kChunk ? slots / tail : kb_total / kChunk;
+    return sp > 1 ? sp : 1;
+}
+
 template <bool PAIR, bool A_MN, bool B_MN, int BN, int EPI>
 cudaError_t launch(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, cudaStream_t s) {
     using C = Cfg<PAIR, BN>;
@@ -531,10 +537,7 @@ cudaError_t launch(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, cudaS
     g.tail_tiles = g.tail_splits = g.tail_kb = 0;
     const int tiles = g.tiles_m * g.tiles_n;
     if (EPI == kOut && g.partials && tiles % slots) {
-        // as many ranges as the last round has CTAs for, of at least one sum in registers each
-        const int tail = tiles % slots;
-        int sp = slots / tail;
-        if (sp > g.kb_total / kChunk) sp = g.kb_total / kChunk;
+        const int tail = tiles % slots, sp = ranges_of(tail, slots, g.kb_total);
         if (sp > 1) {
             g.tail_kb = (g.kb_total + sp - 1) / sp;
             g.tail_splits = (g.kb_total + g.tail_kb - 1) / g.tail_kb;
@@ -561,23 +564,54 @@ cudaError_t launch(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, cudaS
     return cudaGetLastError();
 }
 
-template <bool A_MN, bool B_MN, int EPI>
-cudaError_t launch_wide(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, cudaStream_t s) {
-    return g.M > BM ? launch<true, A_MN, B_MN, 256, EPI>(g, A, B, K, s) : launch<false, A_MN, B_MN, 256, EPI>(g, A, B, K, s);
+// Tiles of a product.  A CTA's share of 256 columns takes one unit of time per stage, of 128 half of that and some of its operands
+// again; CTAs on their own (128 rows) bring twice as much of B per row as pairs (256 rows) but are twice as many.  A tile
+// costs some ten stages more for filling and emptying.  The shape of the least time over all rounds is taken (the last one counts
+// in part where it is cut along K): pairs and 256 columns where there is work for all SMs, smaller ones where there is not.
+// Gradients of 372 rows, C 1,440, V 835 take 60 us, with 256-wide pairs alone 75; of 595 rows, C 224, V 1,607 41 and 55.
+struct Tiles {
+    bool pair;
+    int bn;
+};
+Tiles choose_tiles(int64_t M, int64_t N, int64_t K, bool cut) {
+    const double kb = (double)((K + BK - 1) / BK);
+    Tiles best{true, 256};
+    double least = 1e300;
+    for (const Tiles t : {Tiles{true, 256}, Tiles{true, 128}, Tiles{false, 256}, Tiles{false, 128}}) {
+        if (t.pair && t.bn == 128 && !cut) continue;       // not compiled
+        const int64_t rows = t.pair ? 2 * BM : BM, units = ((M + rows - 1) / rows) * ((N + t.bn - 1) / t.bn), slots = t.pair ? 74 : 148;
+        const double stage = t.bn == 256 ? (t.pair ? 1.0 : 1.2) : (t.pair ? 0.7 : 0.85);
+        double rounds = (double)((units + slots - 1) / slots);
+        if (cut && units % slots) rounds += 1.0 / ranges_of((int)(units % slots), (int)slots, (int)kb) - 1.0;
+        const double cost = rounds * (kb * stage + (t.bn == 256 ? 12 : 8));
+        if (cost < least) {
+            least = cost;
+            best = t;
+        }
+    }
+    return best;
 }
 
-// Results of N columns: 256-wide tiles unless 128-wide ones leave out a third of the padding or more.
+template <int EPI>
+cudaError_t launch_wide(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, cudaStream_t s) {
+    const Tiles t = choose_tiles(g.M, g.N, K, false);
+    if (t.pair) return launch<true, false, false, 256, EPI>(g, A, B, K, s);
+    return t.bn == 256 ? launch<false, false, false, 256, EPI>(g, A, B, K, s) : launch<false, false, false, 128, EPI>(g, A, B, K, s);
+}
+
 template <bool A_MN>
 cudaError_t launch_out(Args& g, const HalfMat& A, const HalfMat& B, int64_t K, cudaStream_t s) {
-    const int at256 = (g.N + 255) / 256 * 256, at128 = (g.N + 127) / 128 * 128;
-    if (4 * at128 > 3 * at256) return launch_wide<A_MN, true, kOut>(g, A, B, K, s);
-    return g.M > BM ? launch<true, A_MN, true, 128, kOut>(g, A, B, K, s) : launch<false, A_MN, true, 128, kOut>(g, A, B, K, s);
+    const Tiles t = choose_tiles(g.M, g.N, K, true);
+    if (t.pair) return t.bn == 256 ? launch<true, A_MN, true, 256, kOut>(g, A, B, K, s) : launch<true, A_MN, true, 128, kOut>(g, A, B, K, s);
+    return t.bn == 256 ? launch<false, A_MN, true, 256, kOut>(g, A, B, K, s) : launch<false, A_MN, true, 128, kOut>(g, A, B, K, s);
 }
 
 }  // namespace
 
-static_assert(256 / kParts == kStripCols, "a strip is what one warp holds of a tile's columns");
-int head_stats_strips(int V) { return kParts * ((V + 255) / 256); }
+HeadStrips head_stats_strips(int64_t N, int C, int V) {
+    const int bn = choose_tiles(N, V, C, false).bn;
+    return HeadStrips{bn / kParts, kParts * ((V + bn - 1) / bn)};
+}
 size_t head_partial_bytes() { return (size_t)148 * BM * 256 * sizeof(float); }
 
 cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, const float* colf, int K, const int2* entries,
@@ -585,7 +619,7 @@ cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* r
     Args g{};
     g.M = (int)x.rows; g.N = (int)w.rows;
     g.rowf = rowf; g.colf = colf; g.K = K; g.entries = entries; g.strip_first = strip_first; g.zk = zk; g.stats = stats; g.err = err;
-    return launch_wide<false, false, kStats>(g, x, w, x.cols, s);
+    return launch_wide<kStats>(g, x, w, x.cols, s);
 }
 
 cudaError_t launch_head_grad(const HalfMat& x, const HalfMat& w, int v0, const float* rowf, const RowParams* rows, __half* u, int64_t ldu,
@@ -593,7 +627,7 @@ cudaError_t launch_head_grad(const HalfMat& x, const HalfMat& w, int v0, const f
     Args g{};
     g.M = (int)x.rows; g.N = (int)w.rows;
     g.rowf = rowf; g.rows = rows; g.v0 = v0; g.u = u; g.ldu = ldu; g.u_plane = u_plane; g.err = err;
-    return launch_wide<false, false, kGrad>(g, x, w, x.cols, s);
+    return launch_wide<kGrad>(g, x, w, x.cols, s);
 }
 
 cudaError_t launch_head_dx(const HalfMat& u, const HalfMat& w, const RowParams* rows, const float* scale, bool onto, float* dx, float* partials,
