@@ -8,8 +8,9 @@
 // g_n = inv_count w_n tau S_n.  The forward keeps one (maximum, sum) pair per row and strip of the vocabulary, joined
 // by head_finish_kernel, which also forms the few scores that the loss needs by themselves; the backward forms z again.
 //
-// Few rows go through head_rows.cu in plain FP32, where the weights are read once; more rows go to the tensor cores (head_tc.cu)
-// on pairs of FP16 numbers that head_pairs_kernel makes of x and W.
+// Up to eight rows go through head_rows.cu in plain FP32, where the weights are read once; the forward of up to 128 through
+// head_direct.cu, where they are read once too and go to the tensor cores as pairs of FP16 numbers; more rows, and their
+// gradients, to head_tc.cu, after kernels here have made such pairs of all of x and W.
 #include <climits>
 
 #include "head.cuh"
@@ -49,13 +50,10 @@ struct Scratch {
     float* partials;
 };
 
-// Rows up to which the plain kernels are used.  Forward: two passes of eight over the weights, 16 rows against V 50,257, C 768,
-// raw 99 us, on the tensor cores 107; 24 rows 141 and 107.  Backward: a second pass adds to dW, so only one, but two where W
-// is small (9 to 16 rows, V 5,000, C 256: 39 to 43 us, on the tensor cores 61; V 23,670, C 320: 82 to 94 and 70).
-bool few_rows(int64_t N, int C, int V, bool back) {
-    const bool two = !back || (int64_t)V * C <= (1 << 22);
-    return N <= (two ? 2 : 1) * kFewRows;
-}
+// Rows up to which the plain kernels are used: those of one pass over the weights.  V 50,257, C 768, raw: 8 rows 53 us, 9 in two
+// passes 90, 24 on the tensor cores 58.  The backward takes two passes where W is small, the second adding to dW (9 to 16 rows,
+// V 5,000, C 256: 38 to 41 us, on the tensor cores 61; V 23,670, C 320: 82 to 94 and 69).
+bool few_rows(int64_t N, int C, int V, bool back) { return N <= (back && (int64_t)V * C <= (1 << 22) ? 2 : 1) * kFewRows; }
 
 // Columns of one piece of the vocabulary, a multiple of 256: pieces of about the same size, of at most `piece` columns or
 // 512 MB of u.
@@ -80,13 +78,23 @@ void tc_layout(Scratch& s, uint8_t* base, size_t& at, int64_t N, int C, int V) {
     s.w16 = take<__half>(base, at, 2 * (size_t)V * C);
 }
 
+// Which kernels form the forward's statistics: plain FP32, tensor cores straight from W, or from pairs of all of W.
+enum Forward { kFew, kDirect, kPairs };
+Forward forward_of(int64_t N, int C, int V) { return few_rows(N, C, V, false) ? kFew : head_direct_fits(N) ? kDirect : kPairs; }
+int strips_of(int64_t N, int C, int V) {
+    const Forward f = forward_of(N, C, V);
+    return f == kFew ? head_few_strips(N, C, V) : f == kDirect ? head_direct_strips(V) : head_stats_strips(N, C, V).count;
+}
+
 size_t fwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K) {
     size_t at = kHeadHeader;
+    const Forward f = forward_of(N, C, V);
     s = Scratch{};
     s.head = (HeadHeader*)base;
-    s.stats = take<float2>(base, at, (size_t)N * (few_rows(N, C, V, false) ? head_few_strips(N, C, V) : head_stats_strips(N, C, V).count));
-    if (few_rows(N, C, V, false)) return at;
-    tc_layout(s, base, at, N, C, V);
+    s.stats = take<float2>(base, at, (size_t)N * strips_of(N, C, V));
+    if (f == kFew) return at;
+    tc_layout(s, base, at, N, C, f == kDirect ? 0 : V);
+    if (f == kDirect) return at;
     s.colf = take<float>(base, at, (V + 255) / 256 * 256);
     s.entries = take<int2>(base, at, (size_t)N * K);
     s.zk = take<float>(base, at, (size_t)N * K);
@@ -123,7 +131,7 @@ __device__ __forceinline__ float dot4(float4 a, float4 b, float acc) {
     return fmaf(a.w, b.w, fmaf(a.z, b.z, fmaf(a.y, b.y, fmaf(a.x, b.x, acc))));
 }
 
-// Few rows against a teacher, one per CTA: joins the partial statistics, forms the scores of the row's entries and the loss.
+// Up to some dozens of rows against a teacher, one per CTA: joins the partial statistics, forms the scores of the row's entries and the loss.
 __global__ void __launch_bounds__(kFinishThreads) head_finish_kernel(const HeadArgs g, const float2* __restrict__ stats, int strips,
                                                                      HeadHeader* head) {
     __shared__ float smf[kFinishThreads / 32];
@@ -336,13 +344,6 @@ __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArg
 
 // ---------------------------------------------------------------- FP16 pairs
 
-// The k with 2^k m in [2^14, 2^15), where 2^k is an FP32 number.
-__device__ __forceinline__ int pair_exponent(float m) {
-    const int e = (int)((__float_as_uint(m) >> 23) & 255u) - 127;
-    return min(14 - e, 126);                // zero and denormal numbers: e = -127
-}
-__device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
-
 // Four values times s as pairs.
 __device__ __forceinline__ void pairs4(float4 v, float s, uint2& hi, uint2& lo) {
     const float t[4] = {v.x * s, v.y * s, v.z * s, v.w * s};
@@ -398,19 +399,20 @@ __device__ __forceinline__ int row_to_pairs(const float* v, const float* v_lo, i
     return k;
 }
 
-// Forward: the rows of W and x as pairs, each at its own power of two, which the epilogue takes out of its column or row.
+// Forward: the rows of W (the first w_rows) and x as pairs, each at its own power of two, which the epilogue takes out of its
+// column or row.
 template <int LANES>
-__global__ void __launch_bounds__(kThreads) head_row_pairs_kernel(const HeadArgs g, const Scratch s) {
+__global__ void __launch_bounds__(kThreads) head_row_pairs_kernel(const HeadArgs g, int64_t w_rows, const Scratch s) {
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0 && threadIdx.x == 0) *s.head = HeadHeader{0, 0u};
     const int C4 = g.C / 4;
     constexpr int kAtOnce = kThreads / LANES;
     // whole warps stay together: they share a base, and lanes whose row does not exist go along
-    for (int64_t base = blockIdx.x * (int64_t)kAtOnce; base < g.V + g.N; base += gridDim.x * (int64_t)kAtOnce) {
+    for (int64_t base = blockIdx.x * (int64_t)kAtOnce; base < w_rows + g.N; base += gridDim.x * (int64_t)kAtOnce) {
         const int64_t at = base + threadIdx.x / LANES;
-        const bool of_w = at < g.V, there = at < g.V + g.N;
-        const int64_t row = of_w ? at : at - g.V;
+        const bool of_w = at < w_rows, there = at < w_rows + g.N;
+        const int64_t row = of_w ? at : at - w_rows;
         const int k = row_to_pairs<LANES>(of_w ? g.w : g.x, of_w ? g.w_lo : g.x_lo, row, there, C4, of_w ? s.w16 : s.x16, (of_w ? (int64_t)g.V : g.N) * C4);
         // 2^-k reaches 2^-126: the factor of a row of x is log2 e / tau 2^-k, a number of FP32 in any case
         if (there && threadIdx.x % LANES == 0) (of_w ? s.colf[row] : s.rowf[row]) = of_w ? ldexpf(1.0f, -k) : ldexpf(kLog2e / g.aim.tau, -k);
@@ -571,38 +573,51 @@ size_t head_bwd_scratch_bytes(int64_t N, int C, int V, int K, int piece) {
     return bwd_layout(s, nullptr, N, C, V, K, piece);
 }
 
+namespace {
+
+cudaError_t launch_row_pairs(const HeadArgs& g, int64_t w_rows, const Scratch& w, cudaStream_t s) {
+    // as few lanes to a row as hold it: many rows in flight
+    const int lanes = g.C <= 128 ? 4 : g.C <= 256 ? 8 : g.C <= 512 ? 16 : 32, grid = grid_for((w_rows + g.N) * lanes, 148 * 8);
+    if (lanes == 4) BT_KERNEL_LAUNCH((head_row_pairs_kernel<4>), grid, kThreads, 0, s, g, w_rows, w);
+    else if (lanes == 8) BT_KERNEL_LAUNCH((head_row_pairs_kernel<8>), grid, kThreads, 0, s, g, w_rows, w);
+    else if (lanes == 16) BT_KERNEL_LAUNCH((head_row_pairs_kernel<16>), grid, kThreads, 0, s, g, w_rows, w);
+    else BT_KERNEL_LAUNCH((head_row_pairs_kernel<32>), grid, kThreads, 0, s, g, w_rows, w);
+    BT_COUNT_LAUNCH();
+    return cudaGetLastError();
+}
+
+}  // namespace
+
 cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     Scratch w;
     const int K = g.aim.targets ? 0 : g.aim.K;
     fwd_layout(w, g.scratch, g.N, g.C, g.V, K);
-    const bool few = few_rows(g.N, g.C, g.V, false);
-    const HeadStrips wide = head_stats_strips(g.N, g.C, g.V);
-    const int strips = few ? head_few_strips(g.N, g.C, g.V) : wide.count;
-    cudaError_t e;
-    if (few) {
+    const Forward f = forward_of(g.N, g.C, g.V);
+    const int strips = strips_of(g.N, g.C, g.V);
+    const HalfMat x = pair_matrix(w.x16, g.N, g.C);
+    cudaError_t e = cudaSuccess;
+    if (f == kFew) {
         e = launch_head_few_stats(g, w.stats, w.head, s);
+    } else if (f == kDirect) {
+        e = launch_row_pairs(g, 0, w, s);
+        if (e == cudaSuccess) e = launch_head_direct(g, x, w.rowf, w.stats, &w.head->err, s);
     } else {
-        // as few lanes to a row as hold it: many rows in flight
-        if (g.C <= 128) BT_KERNEL_LAUNCH((head_row_pairs_kernel<4>), 148 * 8, kThreads, 0, s, g, w);
-        else if (g.C <= 256) BT_KERNEL_LAUNCH((head_row_pairs_kernel<8>), 148 * 8, kThreads, 0, s, g, w);
-        else if (g.C <= 512) BT_KERNEL_LAUNCH((head_row_pairs_kernel<16>), 148 * 8, kThreads, 0, s, g, w);
-        else BT_KERNEL_LAUNCH((head_row_pairs_kernel<32>), 148 * 8, kThreads, 0, s, g, w);
-        BT_COUNT_LAUNCH();
+        e = launch_row_pairs(g, g.V, w, s);
         if (K) {
-            BT_KERNEL_LAUNCH((head_sort_kernel), (unsigned)g.N, kThreads, 0, s, g, w.entries, w.strip_first, wide);
+            BT_KERNEL_LAUNCH((head_sort_kernel), (unsigned)g.N, kThreads, 0, s, g, w.entries, w.strip_first, head_stats_strips(g.N, g.C, g.V));
             BT_COUNT_LAUNCH();
         }
-        e = launch_head_stats(pair_matrix(w.x16, g.N, g.C), pair_matrix(w.w16, g.V, g.C), w.rowf, w.colf, K, w.entries, w.strip_first, w.zk,
-                              w.stats, &w.head->err, s);
+        if (e == cudaSuccess)
+            e = launch_head_stats(x, pair_matrix(w.w16, g.V, g.C), w.rowf, w.colf, K, w.entries, w.strip_first, w.zk, w.stats, &w.head->err, s);
     }
     if (e != cudaSuccess) return e;
     const unsigned ctas = (unsigned)((g.N + kFinishThreads / 32 - 1) / (kFinishThreads / 32));
     if (!K)
         BT_KERNEL_LAUNCH((head_finish_target_kernel), ctas, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
-    else if (few)
-        BT_KERNEL_LAUNCH((head_finish_kernel), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
-    else
+    else if (f == kPairs)
         BT_KERNEL_LAUNCH((head_finish_entries_kernel), ctas, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, (const float*)w.zk, w.head);
+    else
+        BT_KERNEL_LAUNCH((head_finish_kernel), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }

@@ -55,6 +55,32 @@ cudaError_t launch_head_few_stats(const HeadArgs& g, float2* stats, HeadHeader* 
 cudaError_t launch_head_few_grad(const HeadArgs& g, const RowParams* params, int K, const int* eid, const float* ep, float* aim, float* dx_part,
                                  cudaStream_t s);
 
+// FP16 pairs: the k with 2^k m in [2^14, 2^15), where 2^k and 2^-k are FP32 numbers.
+__device__ __forceinline__ int pair_exponent(float m) {
+    const int e = (int)((__float_as_uint(m) >> 23) & 255u) - 127;
+    return min(14 - e, 126);                // zero and denormal numbers: e = -127
+}
+__device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
+// Two values as FP16 pairs.
+__device__ __forceinline__ void to_pairs(float a, float b, uint32_t& hi, uint32_t& lo) {
+    const __half2 h = __floats2half2_rn(a, b);
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(a - f.x, b - f.y);
+    hi = *reinterpret_cast<const uint32_t*>(&h);
+    lo = *reinterpret_cast<const uint32_t*>(&l);
+}
+
+// The tensor core cuts its running sum to FP32 with every instruction, always toward zero.  A sum that grows to its final size
+// over n instructions comes out short by some n / 2 times 2^-24 of it times the mean of the cut: measured, 0.54 for
+// random operands, 0.6 for aligned ones, 1.2 where all products are positive.  n is 3 per 16 of the contraction index between
+// two sums in registers; the products are made longer by 0.56.
+inline float head_growth(double n) { return (float)(1.0 + 0.5 * 0.56 / (1 << 24) * n); }
+
+// Statistics of up to 128 rows straight from W (head_direct.cu): [N][head_direct_strips(V)].
+bool head_direct_fits(int64_t N);
+int head_direct_strips(int V);
+cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float* rowf, float2* stats, int* err, cudaStream_t s);
+
 // Logit of entry k of a row in units of the softened softmax, -inf where there is none (a weight of zero).  An id
 // behind the vocabulary counts as id 0 and is recorded.
 __device__ __forceinline__ float entry_logit(const LossAim& a, int64_t row, int k, int V, int* bad, int& id) {

@@ -1,0 +1,312 @@
+// The head's forward statistics for some dozens of rows of x: W goes through the SMs once, as it is, and becomes FP16 pairs on the way.
+//
+// With so few rows the weights' bytes bound the call, and a pass that makes pairs of W (read, written and read again) costs three times
+// as much.  Here a tile of 128 rows of W is the A operand of tcgen05.mma.kind::f16, in tensor memory, lane = row: a thread
+// takes 64 values of its own row out of shared memory, scales them by a power of two of their own, and stores the pairs.  The
+// same lanes hold the products, so the scale comes out again where the thread of the row adds the block to its sums in FP32.
+//
+//     warps 0, 2 (a lane) TMA: W tiles (FP32, raw or planes); the x tile's pairs
+//     warp 1 (one lane)   MMA: z^T += W x^T per 64 of the contraction index (l h' + h l' + h h')
+//     warps 4-7, 8-11     pairs of even and odd blocks
+//     warps 12-15         sums, then (maximum, sum of exponentials) over the warp's 32 rows of W for every row of x
+//
+// Both rings have an even number of stages: a stage then always belongs to the same warps.  (Two groups that took turns on one
+// stage could take the fill that the other still waits for to be theirs: a parity tells neighbouring phases apart, not more.)
+// Every wait is bounded: one that runs out sets the error word and the CTA drains and exits, still releasing its tensor memory.
+#include <cuda.h>
+
+#include "head.cuh"
+#include "tc_common.cuh"
+
+namespace bt {
+
+using namespace tc;
+
+namespace {
+
+constexpr int kTileRows = 128, kBlock = 64, kMostX = 128;
+constexpr int kThreads = 512;
+constexpr int kRegsIssue = 40, kRegsPairs = 120, kRegsSums = 224;      // of the launch's 4 x 128
+
+struct Args {
+    int N, V, tiles, blocks, Nr;            // Nr: rows of x, up to a multiple of 16
+    const float* rowf;                      // [N]
+    float2* stats;                          // [N][4 tiles]
+    float grow;
+    int* err;
+};
+
+template <bool PLANES>
+struct Cfg {
+    static constexpr uint32_t kW = (PLANES ? 2u : 1u) * kTileRows * kBlock * 4u, kX = 2u * kMostX * kBlock * 2u;
+    static constexpr int kStages = PLANES ? 2 : 4;                      // of W; two of x
+    static constexpr uint32_t kScales = 2u * kTileRows * 4u;
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kW + 2 * kX + kScales + 256;
+};
+
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// Maxima (MAX) or sums over the warp's lanes of 32 values per lane: lane l gets that of value l.
+template <bool MAX>
+__device__ __forceinline__ float across(float (&v)[32], int lane) {
+#pragma unroll
+    for (int half = 16; half >= 1; half /= 2) {
+        const bool up = lane & half;
+#pragma unroll
+        for (int i = 0; i < half; ++i) {
+            const float keep = up ? v[i + half] : v[i], give = up ? v[i] : v[i + half], got = __shfl_xor_sync(0xffffffffu, give, half);
+            v[i] = MAX ? fmaxf(keep, got) : keep + got;
+        }
+    }
+    return v[0];
+}
+
+template <bool PLANES>
+__global__ void __launch_bounds__(kThreads, 1)
+head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const Args g) {
+    using C = Cfg<PLANES>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t x_ring = base + C::kStages * C::kW;
+    float* const scales = reinterpret_cast<float*>(base_ptr + C::kStages * C::kW + 2 * C::kX);
+    const uint32_t bars = x_ring + 2 * C::kX + C::kScales;
+    auto full_bar = [&](int s) { return bars + 8u * s; };
+    auto empty_bar = [&](int s) { return bars + 8u * (C::kStages + s); };
+    auto pairs_bar = [&](int a) { return bars + 8u * (2 * C::kStages + a); };
+    auto done_bar = [&](int a) { return bars + 8u * (2 * C::kStages + 2 + a); };
+    auto drained_bar = [&](int a) { return bars + 8u * (2 * C::kStages + 4 + a); };
+    auto x_full_bar = [&](int a) { return bars + 8u * (2 * C::kStages + 6 + a); };
+    const uint32_t tmem_slot = bars + 8u * (2 * C::kStages + 8);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        prefetch_tensormap(&tmW);
+        prefetch_tensormap(&tmX);
+        for (int s = 0; s < C::kStages; ++s) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 4);     // the warps that make pairs of it
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(pairs_bar(a), 4);
+            mbar_init(done_bar(a), 1);
+            mbar_init(drained_bar(a), 4);
+            mbar_init(x_full_bar(a), 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tmem_slot) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(base_ptr + (tmem_slot - base));
+    pdl_wait();
+    pdl_trigger();
+    // tensor memory: products 0-127 and 128-255, pairs (32 columns of h, 32 of l) from 256 and 320
+    auto t_sum = [&](int a) { return tmem + 128u * a; };
+    auto t_pair = [&](int a) { return tmem + 256u + 64u * a; };
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+        if ((warp == 0 || warp == 2) && lane == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            for (int t = blockIdx.x; t < g.tiles && ok; t += gridDim.x)
+                for (int b = 0; b < g.blocks; ++b, ++it) {
+                    if (warp == 0) {
+                        const int s = it % C::kStages;
+                        if (!mbar_wait(empty_bar(s), ((it / C::kStages) & 1u) ^ 1u, g.err, 41)) { ok = false; break; }
+                        mbar_expect_tx(full_bar(s), C::kW);
+                        tma_load_3d(base + s * C::kW, &tmW, full_bar(s), b * kBlock, t * kTileRows, 0);
+                        tma_load_3d(base + s * C::kW + C::kW / 2, &tmW, full_bar(s), b * kBlock + 32, t * kTileRows, 0);
+                    } else {
+                        // the products of the block before last are done with this stage
+                        const int a = it & 1;
+                        if (!mbar_wait(done_bar(a), ((it >> 1) & 1u) ^ 1u, g.err, 47)) { ok = false; break; }
+                        mbar_expect_tx(x_full_bar(a), 2u * g.Nr * kBlock * 2u);
+                        tma_load_3d(x_ring + a * C::kX, &tmX, x_full_bar(a), b * kBlock, 0, 0);
+                    }
+                }
+            if (!ok)                        // copies in flight land before the shared memory is given back
+                for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+        }
+        if (warp == 1) {
+            // FP16 operands, A with rows of K in lanes, B K-major
+            const uint32_t idesc = (1u << 4) | ((uint32_t)(g.Nr >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
+            uint32_t it = 0;
+            bool ok = true;
+            for (int t = blockIdx.x; t < g.tiles && ok; t += gridDim.x)
+                for (int b = 0; b < g.blocks; ++b, ++it) {
+                    const int a = it & 1;
+                    if (!mbar_wait_warp(x_full_bar(a), (it >> 1) & 1u, g.err, 48) || !mbar_wait_warp(pairs_bar(a), (it >> 1) & 1u, g.err, 42)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t x_base = x_ring + a * C::kX;
+                    if (elect_one()) {
+#pragma unroll
+                        for (int j = 0; j < kBlock / 16; ++j) {
+                            const uint64_t xh = make_desc(x_base + j * 32u, 16u, 1024u, 2u), xl = make_desc(x_base + g.Nr * 128u + j * 32u, 16u, 1024u, 2u);
+                            mma_f16_ts(t_sum(a), t_pair(a) + 32u + 8u * j, xh, idesc, j > 0 ? 1u : 0u);
+                            mma_f16_ts(t_sum(a), t_pair(a) + 8u * j, xl, idesc, 1u);
+                            mma_f16_ts(t_sum(a), t_pair(a) + 8u * j, xh, idesc, 1u);
+                        }
+                        umma_commit(done_bar(a));
+                    }
+                    __syncwarp();
+                }
+        }
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsPairs));
+        const int a = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t t_row = t_pair(a) + ((uint32_t)((warp & 3) * 32) << 16);
+        uint32_t it = 0;
+        bool ok = true;
+        for (int t = blockIdx.x; t < g.tiles && ok; t += gridDim.x)
+            for (int b = 0; b < g.blocks; ++b, ++it) {
+                if ((int)(it & 1u) != a) continue;
+                const int s = it % C::kStages;
+                if (!mbar_wait_warp(full_bar(s), (it / C::kStages) & 1u, g.err, 43)) { ok = false; break; }
+                // the 16-byte units of a row of 128 bytes lie swizzled by the row
+                float v[kBlock];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const uint8_t* p = base_ptr + s * C::kW + h * (C::kW / 2) + row * 128 + ((q ^ (row & 7)) << 4);
+                        float4 w = *reinterpret_cast<const float4*>(p);
+                        if (PLANES) w = add4(w, *reinterpret_cast<const float4*>(p + kTileRows * 128));
+                        v[h * 32 + 4 * q] = w.x; v[h * 32 + 4 * q + 1] = w.y; v[h * 32 + 4 * q + 2] = w.z; v[h * 32 + 4 * q + 3] = w.w;
+                    }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(empty_bar(s));
+                float m = 0.f;
+#pragma unroll
+                for (int i = 0; i < kBlock; ++i) m = fmaxf(m, fabsf(v[i]));
+                const int k = pair_exponent(m);
+                const float sc = pow2(k);
+                uint32_t hi[32], lo[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) to_pairs(v[2 * i] * sc, v[2 * i + 1] * sc, hi[i], lo[i]);
+                // the sums of the block before last have been taken, and with them its scales and pairs
+                if (!mbar_wait_warp(drained_bar(a), ((it >> 1) & 1u) ^ 1u, g.err, 44)) { ok = false; break; }
+                tc_fence_after();
+                tmem_st32(t_row, hi);
+                tmem_st32(t_row + 32u, lo);
+                scales[a * kTileRows + row] = ldexpf(1.0f, -k - 15);      // the sums stay near W's size whatever x's
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(pairs_bar(a));
+            }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSums));
+        const int quad = warp & 3, row = quad * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        uint32_t it = 0;
+        bool ok = true;
+        for (int tile = blockIdx.x; tile < g.tiles && ok; tile += gridDim.x) {
+            float z[4][32];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) z[q][j] = 0.f;
+            for (int b = 0; b < g.blocks; ++b, ++it) {
+                const int a = it & 1;
+                // the products are there, and the block's scales before them
+                if (!mbar_wait_warp(done_bar(a), (it >> 1) & 1u, g.err, 45) || !mbar_wait_warp(pairs_bar(a), (it >> 1) & 1u, g.err, 46)) { ok = false; break; }
+                tc_fence_after();
+                const float sc = scales[a * kTileRows + row];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (q * 32 >= g.Nr) continue;
+                    uint32_t rr[32];
+                    tmem_ld32(t_sum(a) + lanes + q * 32u, rr);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) z[q][j] = fmaf(__uint_as_float(rr[j]), sc, z[q][j]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(drained_bar(a));
+            }
+            if (!ok) break;
+            const bool there = tile * kTileRows + row < g.V;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (q * 32 >= g.N) continue;
+                const int n = q * 32 + lane;
+                const float mine = n < g.N ? g.rowf[n] * g.grow : 0.f;
+                float v[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const float t = __shfl_sync(0xffffffffu, mine, j);
+                    z[q][j] = there ? z[q][j] * t * 32768.0f : -INFINITY;
+                    v[j] = z[q][j];
+                }
+                const float m = across<true>(v, lane);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const float top = __shfl_sync(0xffffffffu, m, j);
+                    v[j] = there ? ex2_fast(z[q][j] - top) : 0.f;
+                }
+                const float s = across<false>(v, lane);
+                // a warp whose rows all lie behind the vocabulary has the sum zero
+                if (n < g.N) g.stats[(long long)n * (4 * g.tiles) + 4 * tile + quad] = make_float2(m, s);
+            }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+template <bool PLANES>
+cudaError_t launch(const HeadArgs& h, const HalfMat& x, const Args& g, cudaStream_t s) {
+    using C = Cfg<PLANES>;
+    if (!tensor_map_encoder()) return cudaErrorNotSupported;
+    CUtensorMap tmW, tmX;
+    const cuuint32_t one[3] = {1, 1, 1};
+    const cuuint64_t w_dims[3] = {(cuuint64_t)h.C, (cuuint64_t)h.V, PLANES ? 2u : 1u}, w_strides[2] = {(cuuint64_t)h.C * 4, (cuuint64_t)h.V * h.C * 4};
+    const cuuint32_t w_box[3] = {32, kTileRows, PLANES ? 2u : 1u};
+    const cuuint64_t x_dims[3] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows, 2}, x_strides[2] = {(cuuint64_t)x.ld * 2, (cuuint64_t)x.plane * 2};
+    const cuuint32_t x_box[3] = {kBlock, (cuuint32_t)g.Nr, 2};
+    if (tensor_map_encoder()(&tmW, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, (void*)h.w, w_dims, w_strides, w_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
+        tensor_map_encoder()(&tmX, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, (void*)x.hi, x_dims, x_strides, x_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return cudaErrorInvalidValue;
+    const cudaError_t e = allow_smem<head_direct_kernel<PLANES>>(C::kSmem);
+    if (e != cudaSuccess) return e;
+    BT_KERNEL_LAUNCH((head_direct_kernel<PLANES>), g.tiles < sm_count() ? g.tiles : sm_count(), kThreads, C::kSmem, s, tmW, tmX, g);
+    BT_COUNT_LAUNCH();
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+bool head_direct_fits(int64_t N) { return N <= kMostX; }
+int head_direct_strips(int V) { return 4 * ((V + kTileRows - 1) / kTileRows); }
+
+cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float* rowf, float2* stats, int* err, cudaStream_t s) {
+    Args g{};
+    g.N = (int)h.N; g.V = h.V;
+    g.tiles = (h.V + kTileRows - 1) / kTileRows;
+    g.blocks = (h.C + kBlock - 1) / kBlock;
+    g.Nr = ((int)h.N + 15) / 16 * 16;
+    g.rowf = rowf; g.stats = stats; g.err = err;
+    g.grow = head_growth(3 * kBlock / 16);
+    return h.w_lo ? launch<true>(h, x, g, s) : launch<false>(h, x, g, s);
+}
+
+}  // namespace bt

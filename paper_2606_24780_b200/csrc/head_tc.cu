@@ -56,7 +56,7 @@ struct Cfg {
 struct Args {
     int M, N;                               // of the result
     int tiles_m, tiles_n, group_m, kb_total;
-    float grow;                             // see growth()
+    float grow;                             // see head_growth()
     // The tiles of the complete rounds run over all of K; the tail_tiles of the last, partly filled one (all, where there
     // are fewer tiles than CTAs) are cut into tail_splits ranges of tail_kb stages, whose sums are joined by join_kernel.
     int tail_tiles, tail_splits, tail_kb;
@@ -157,15 +157,6 @@ __device__ __forceinline__ void load32(const void* p, uint32_t (&v)[8]) {
     const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
     v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-
-// Two values as FP16 pairs.
-__device__ __forceinline__ void to_pairs(float a, float b, uint32_t& hi, uint32_t& lo) {
-    const __half2 h = __floats2half2_rn(a, b);
-    const float2 f = __half22float2(h);
-    const __half2 l = __floats2half2_rn(a - f.x, b - f.y);
-    hi = *reinterpret_cast<const uint32_t*>(&h);
-    lo = *reinterpret_cast<const uint32_t*>(&l);
 }
 
 template <bool PAIR, bool A_MN, bool B_MN, int BN, int EPI>
@@ -500,18 +491,14 @@ bool encode(CUtensorMap* tm, const HalfMat& m, bool mn, int box_rows) {
                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The tensor core cuts its running sum to FP32 with every instruction, always toward zero.  A sum that grows to its final size
-// over n instructions comes out short by some n / 2 times 2^-24 of it times the mean of the cut: measured, 0.54 for
-// random operands, 0.6 for aligned ones, 1.2 where all products are positive.  n is 3 per 16 of the contraction index between
-// two sums in registers; the products are made longer by 0.56.
 float growth(int kb_total) {
-    double n = 0.0, nn = 0.0;
+    double n = 0.0, nn = 0.0;               // the mean over the contraction index of the instructions in its sum
     for (int left = kb_total; left > 0; left -= kChunk) {
         const double c = 3.0 * (BK / 16) * (left < kChunk ? left : kChunk);
         n += c;
         nn += c * c;
     }
-    return (float)(1.0 + 0.5 * 0.56 / (1 << 24) * nn / n);
+    return head_growth(nn / n);
 }
 
 // Ranges of K for each tile of the last round: as many as it has CTAs for, of at least one sum in registers each.

@@ -250,15 +250,36 @@ def test_teacher_arrays_of_the_wrong_shape_are_refused(lib):
 @pytest.mark.parametrize("N,C,V", [(1, 32, 1), (1, 768, 50257), (2, 64, 31), (3, 96, 257), (5, 1024, 4099), (7, 4096, 300), (8, 64, 512),
                                    (9, 64, 513), (33, 160, 1000), (100, 768, 2049), (127, 64, 255), (128, 64, 256), (129, 96, 257),
                                    (255, 1056, 511), (256, 512, 1024), (257, 64, 1025), (300, 2080, 700), (513, 128, 3), (1000, 64, 5003),
-                                   (2049, 32, 130)])
+                                   (2049, 32, 130), (16, 96, 300), (17, 32, 129), (40, 4096, 300),
+                                   (200, 4096, 500), (65, 2080, 1000), (1200, 96, 40)])
 @pytest.mark.parametrize("planes", [False, True])
 def test_cross_entropy(N, C, V, planes):
     check(Case(N, C, V, planes=planes, weights=N % 2 == 1, pad=N // 5, seed=N + V))
 
 
 @gpu
+@pytest.mark.parametrize("N,C,V", [(24, 768, 50257), (100, 1024, 50257), (128, 96, 60001), (33, 2080, 40000), (11, 64, 90000)])
+@pytest.mark.parametrize("planes", [False, True])
+def test_some_dozens_of_rows_over_many_tiles(N, C, V, planes):
+    """Several tiles of 128 rows of W to every SM, of one to 33 blocks each, several times over: every value of every run."""
+    gen = torch.Generator(DEV).manual_seed(N)
+    x, w = torch.randn(N, C, generator=gen, device=DEV), torch.randn(V, C, generator=gen, device=DEV) * 2 / math.sqrt(C)
+    t = torch.randint(0, V, (N,), generator=gen, device=DEV, dtype=torch.int32)
+    z = x.double() @ w.double().T
+    want = torch.logsumexp(z, 1)
+    loss = want - z.gather(1, t.long()[:, None])[:, 0]
+    work = torch.empty(b.bt_op_head_fwd_scratch_bytes(N, C, V), dtype=torch.uint8, device=DEV)
+    operands = (None, split(x), None, split(w)) if planes else (x, None, w, None)
+    for _ in range(8):
+        losses, lse = torch.full((N,), math.nan, device=DEV), torch.full((N,), math.nan, device=DEV)
+        b.bt_op_head_xent_fwd(*operands, t, None, N, C, V, 1.0, losses, lse, None, work, work.numel())
+        b.bt_op_head_check(work)
+        assert float((lse - want).abs().max()) < TOL * 10 and float((losses - loss).abs().max()) < TOL * 10
+
+
+@gpu
 @pytest.mark.parametrize("N,C,V,K,tau,whole", [(1, 64, 40, 1, 1.0, False), (4, 32, 5, 16, 2.0, False), (8, 768, 3001, 64, 2.0, True),
-                                               (40, 96, 999, 3, 0.5, True), (130, 64, 700, 128, 4.0, False), (260, 512, 2050, 33, 1.5, True),
+                                               (40, 96, 999, 3, 0.5, True), (128, 128, 5000, 200, 2.0, False), (130, 64, 700, 128, 4.0, False), (260, 512, 2050, 33, 1.5, True),
                                                (300, 64, 1500, 1024, 1.0, False), (1001, 32, 257, 7, 1.0, False)])
 @pytest.mark.parametrize("planes", [False, True])
 def test_distillation(N, C, V, K, tau, whole, planes):
@@ -266,7 +287,7 @@ def test_distillation(N, C, V, K, tau, whole, planes):
 
 
 @gpu
-@pytest.mark.parametrize("N", [6, 300])
+@pytest.mark.parametrize("N", [6, 12, 300])
 @pytest.mark.parametrize("K", [0, 9])
 def test_gradients_in_pieces_of_the_vocabulary(N, K):
     c = Case(N, 96, 1111, K=K, tau=2.0 if K else 1.0, pad=1)
@@ -279,7 +300,7 @@ def test_gradients_in_pieces_of_the_vocabulary(N, K):
 
 
 @gpu
-@pytest.mark.parametrize("N", [5, 200])
+@pytest.mark.parametrize("N", [5, 50, 200])
 def test_outputs_asked_for_one_by_one(N):
     c = Case(N, 64, 700, weights=True, pad=2)
     lse = c.forward()[1]
@@ -295,7 +316,7 @@ def test_outputs_asked_for_one_by_one(N):
 
 
 @gpu
-@pytest.mark.parametrize("N", [4, 150])
+@pytest.mark.parametrize("N", [4, 40, 150])
 @pytest.mark.parametrize("K", [0, 5])
 def test_two_runs_give_the_same_bits(N, K):
     c = Case(N, 160, 3000, K=K, weights=True)
@@ -305,7 +326,7 @@ def test_two_runs_give_the_same_bits(N, K):
 
 
 @gpu
-@pytest.mark.parametrize("N", [4, 150])
+@pytest.mark.parametrize("N", [4, 40, 150])
 @pytest.mark.parametrize("K", [0, 5])
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
 def test_rows_without_a_target_may_hold_anything(N, K, value):
@@ -321,7 +342,7 @@ def test_rows_without_a_target_may_hold_anything(N, K, value):
 
 
 @gpu
-@pytest.mark.parametrize("N", [4, 150])
+@pytest.mark.parametrize("N", [4, 40, 150])
 def test_a_batch_without_any_target(N):
     for K in (0, 3):
         c = Case(N, 64, 300, K=K, pad=N)
@@ -340,7 +361,7 @@ def test_no_rows(K):
 
 
 @gpu
-@pytest.mark.parametrize("N", [4, 150])
+@pytest.mark.parametrize("N", [4, 40, 150])
 def test_a_row_that_is_not_a_number_stays_alone(N):
     c = Case(N, 64, 900)
     plain = c.forward()
@@ -352,7 +373,7 @@ def test_a_row_that_is_not_a_number_stays_alone(N):
 
 
 @gpu
-@pytest.mark.parametrize("N", [5, 150])
+@pytest.mark.parametrize("N", [5, 40, 150])
 def test_ids_behind_the_vocabulary_count_as_zero_and_are_recorded(N):
     c = Case(N, 64, 300)
     c.targets[3] = 300
@@ -374,7 +395,7 @@ def test_ids_behind_the_vocabulary_count_as_zero_and_are_recorded(N):
 
 
 @gpu
-@pytest.mark.parametrize("N", [4, 200])
+@pytest.mark.parametrize("N", [4, 50, 200])
 @pytest.mark.parametrize("sx,sw", [(1e4, 1e-4), (1e-6, 1e6), (1e-20, 1e20), (1e15, 1e-15), (30.0, 1.0)])
 def test_operands_of_any_size(N, sx, sw):
     """The scales cancel in the scores; the last case has scores of some 60, and tolerances relative to them."""
@@ -391,7 +412,7 @@ def test_operands_of_any_size(N, sx, sw):
 
 
 @gpu
-@pytest.mark.parametrize("N", [4, 200])
+@pytest.mark.parametrize("N", [4, 50, 200])
 def test_rows_and_weights_of_unequal_size(N):
     """Rows of x, and their weights in the loss, that differ by 2^20, and columns of W that differ by 2^10: every row of dx is
     right to its own size."""
@@ -409,7 +430,7 @@ def test_rows_and_weights_of_unequal_size(N):
 
 
 @gpu
-@pytest.mark.parametrize("N", [3, 140])
+@pytest.mark.parametrize("N", [3, 20, 140])
 @pytest.mark.parametrize("K", [0, 6])
 def test_gradients_against_differences(N, K):
     """dx and dw against central differences of the 64-bit mean loss, along random directions."""
@@ -465,7 +486,7 @@ def test_far_rows_and_vocabulary():
 
 
 @gpu
-@pytest.mark.parametrize("N", [4, 150])
+@pytest.mark.parametrize("N", [4, 40, 150])
 def test_captured_calls_and_another_stream(N):
     c = Case(N, 64, 500, weights=True)
     plain = check(c)
@@ -500,7 +521,7 @@ def test_captured_calls_and_another_stream(N):
 
 @gpu
 def test_rows_behind_the_last_are_left_alone():
-    for N in (3, 130):
+    for N in (3, 30, 130):
         c = Case(N, 64, 200)
         big = torch.full((N + 40, 64), 7.0, device=DEV)
         lse = c.forward()[1]
@@ -517,7 +538,7 @@ def test_rows_behind_the_last_are_left_alone():
 
 @gpu
 def test_scratch_is_enough_and_not_exceeded():
-    for N, C, V, K in ((3, 64, 100, 5), (150, 96, 700, 0), (300, 64, 5000, 9)):
+    for N, C, V, K in ((3, 64, 100, 5), (12, 64, 300, 3), (60, 96, 700, 4), (150, 96, 700, 0), (300, 64, 5000, 9)):
         c = Case(N, C, V, K=K)
         lse = c.forward()[1]
         for back in (False, True):
@@ -646,7 +667,7 @@ def test_no_rows_of_logits():
 # ------------------------------------------------------------------------------- GPU: together, and beside the training step
 
 @gpu
-@pytest.mark.parametrize("N", [6, 333])
+@pytest.mark.parametrize("N", [6, 77, 333])
 def test_hard_and_soft_loss_of_a_student(N):
     """0.3 cross entropy + 0.7 distillation on the same rows, from hidden states and from logits made by the library's GEMM,
     against 64-bit automatic differentiation of the sum."""
