@@ -10,7 +10,7 @@
 //     warps 4-7, 8-11     pairs of even and odd blocks
 //     warps 12-15         sums, then (maximum, sum of exponentials) over the warp's 32 rows of W for every row of x
 //
-// Both rings have an even number of stages: a stage then always belongs to the same warps.  (Two groups that took turns on one
+// W's ring has an even number of stages: a stage then always belongs to the same warps.  (Two groups that took turns on one
 // stage could take the fill that the other still waits for to be theirs: a parity tells neighbouring phases apart, not more.)
 // Every wait is bounded: one that runs out sets the error word and the CTA drains and exits, still releasing its tensor memory.
 #include <cuda.h>
@@ -30,6 +30,7 @@ constexpr int kRegsIssue = 40, kRegsPairs = 120, kRegsSums = 224;      // of the
 
 struct Args {
     int N, V, tiles, blocks, Nr;            // Nr: rows of x, up to a multiple of 16
+    int x_stages;
     const float* rowf;                      // [N]
     float2* stats;                          // [N][4 tiles]
     float grow;
@@ -38,11 +39,14 @@ struct Args {
 
 template <bool PLANES>
 struct Cfg {
-    static constexpr uint32_t kW = (PLANES ? 2u : 1u) * kTileRows * kBlock * 4u, kX = 2u * kMostX * kBlock * 2u;
-    static constexpr int kStages = PLANES ? 2 : 4;                      // of W; two of x
-    static constexpr uint32_t kScales = 2u * kTileRows * 4u;
-    static constexpr size_t kSmem = 1024 + (size_t)kStages * kW + 2 * kX + kScales + 256;
+    static constexpr uint32_t kW = (PLANES ? 2u : 1u) * kTileRows * kBlock * 4u;
+    static constexpr int kStages = PLANES ? 2 : 4;                      // of W; those of x are as many as fit
+    static constexpr uint32_t kScales = (2u * kTileRows + kMostX + 4u * kMostX) * 4u;      // scales, rowf, references of four warps
+    static constexpr uint32_t kFixed = 1024 + kStages * kW + kScales + 256;
 };
+constexpr uint32_t kSmemMost = 227u * 1024u;
+constexpr int kMostXStages = 4;
+__host__ __device__ constexpr uint32_t x_bytes(int Nr) { return 2u * Nr * kBlock * 2u; }
 
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;
@@ -76,16 +80,19 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t x_ring = base + C::kStages * C::kW;
-    float* const scales = reinterpret_cast<float*>(base_ptr + C::kStages * C::kW + 2 * C::kX);
-    const uint32_t bars = x_ring + 2 * C::kX + C::kScales;
+    const uint32_t x_size = x_bytes(g.Nr), x_ring = base + C::kStages * C::kW;
+    float* const scales = reinterpret_cast<float*>(base_ptr + C::kStages * C::kW + g.x_stages * x_size);
+    float* const row_f = scales + 2 * kTileRows;
+    float* const refs = row_f + kMostX;
+    const uint32_t bars = x_ring + g.x_stages * x_size + C::kScales;
     auto full_bar = [&](int s) { return bars + 8u * s; };
     auto empty_bar = [&](int s) { return bars + 8u * (C::kStages + s); };
     auto pairs_bar = [&](int a) { return bars + 8u * (2 * C::kStages + a); };
     auto done_bar = [&](int a) { return bars + 8u * (2 * C::kStages + 2 + a); };
     auto drained_bar = [&](int a) { return bars + 8u * (2 * C::kStages + 4 + a); };
-    auto x_full_bar = [&](int a) { return bars + 8u * (2 * C::kStages + 6 + a); };
-    const uint32_t tmem_slot = bars + 8u * (2 * C::kStages + 8);
+    auto x_full_bar = [&](int s) { return bars + 8u * (2 * C::kStages + 6 + s); };
+    auto x_empty_bar = [&](int s) { return bars + 8u * (2 * C::kStages + 6 + kMostXStages + s); };
+    const uint32_t tmem_slot = bars + 8u * (2 * C::kStages + 6 + 2 * kMostXStages);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
@@ -99,7 +106,10 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
             mbar_init(pairs_bar(a), 4);
             mbar_init(done_bar(a), 1);
             mbar_init(drained_bar(a), 4);
-            mbar_init(x_full_bar(a), 1);
+        }
+        for (int s = 0; s < g.x_stages; ++s) {
+            mbar_init(x_full_bar(s), 1);
+            mbar_init(x_empty_bar(s), 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -113,14 +123,14 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(base_ptr + (tmem_slot - base));
     pdl_wait();
     pdl_trigger();
-    // tensor memory: products 0-127 and 128-255, pairs (32 columns of h, 32 of l) from 256 and 320
+    // tensor memory: products 0-127 and 128-255, pairs (32 columns of h, 32 of l) from 256 and 320, a tile's sums from 384
     auto t_sum = [&](int a) { return tmem + 128u * a; };
     auto t_pair = [&](int a) { return tmem + 256u + 64u * a; };
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
         if ((warp == 0 || warp == 2) && lane == 0) {
-            uint32_t it = 0;
+            uint32_t it = 0, xs = 0, xp = 0;           // stage of x and how often it has come round
             bool ok = true;
             for (int t = blockIdx.x; t < g.tiles && ok; t += gridDim.x)
                 for (int b = 0; b < g.blocks; ++b, ++it) {
@@ -131,11 +141,10 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                         tma_load_3d(base + s * C::kW, &tmW, full_bar(s), b * kBlock, t * kTileRows, 0);
                         tma_load_3d(base + s * C::kW + C::kW / 2, &tmW, full_bar(s), b * kBlock + 32, t * kTileRows, 0);
                     } else {
-                        // the products of the block before last are done with this stage
-                        const int a = it & 1;
-                        if (!mbar_wait(done_bar(a), ((it >> 1) & 1u) ^ 1u, g.err, 47)) { ok = false; break; }
-                        mbar_expect_tx(x_full_bar(a), 2u * g.Nr * kBlock * 2u);
-                        tma_load_3d(x_ring + a * C::kX, &tmX, x_full_bar(a), b * kBlock, 0, 0);
+                        if (!mbar_wait(x_empty_bar(xs), (xp & 1u) ^ 1u, g.err, 47)) { ok = false; break; }
+                        mbar_expect_tx(x_full_bar(xs), x_size);
+                        tma_load_3d(x_ring + xs * x_size, &tmX, x_full_bar(xs), b * kBlock, 0, 0);
+                        if (++xs == (uint32_t)g.x_stages) xs = 0, ++xp;
                     }
                 }
             if (!ok)                        // copies in flight land before the shared memory is given back
@@ -144,14 +153,14 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         if (warp == 1) {
             // FP16 operands, A with rows of K in lanes, B K-major
             const uint32_t idesc = (1u << 4) | ((uint32_t)(g.Nr >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
-            uint32_t it = 0;
+            uint32_t it = 0, xs = 0, xp = 0;
             bool ok = true;
             for (int t = blockIdx.x; t < g.tiles && ok; t += gridDim.x)
                 for (int b = 0; b < g.blocks; ++b, ++it) {
                     const int a = it & 1;
-                    if (!mbar_wait_warp(x_full_bar(a), (it >> 1) & 1u, g.err, 48) || !mbar_wait_warp(pairs_bar(a), (it >> 1) & 1u, g.err, 42)) { ok = false; break; }
+                    if (!mbar_wait_warp(x_full_bar(xs), xp & 1u, g.err, 48) || !mbar_wait_warp(pairs_bar(a), (it >> 1) & 1u, g.err, 42)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t x_base = x_ring + a * C::kX;
+                    const uint32_t x_base = x_ring + xs * x_size;
                     if (elect_one()) {
 #pragma unroll
                         for (int j = 0; j < kBlock / 16; ++j) {
@@ -160,9 +169,11 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                             mma_f16_ts(t_sum(a), t_pair(a) + 8u * j, xl, idesc, 1u);
                             mma_f16_ts(t_sum(a), t_pair(a) + 8u * j, xh, idesc, 1u);
                         }
+                        umma_commit(x_empty_bar(xs));
                         umma_commit(done_bar(a));
                     }
                     __syncwarp();
+                    if (++xs == (uint32_t)g.x_stages) xs = 0, ++xp;
                 }
         }
     } else if (warp < 12) {
@@ -189,9 +200,10 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                     }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(empty_bar(s));
-                float m = 0.f;
+                float top[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < kBlock; ++i) m = fmaxf(m, fabsf(v[i]));
+                for (int i = 0; i < kBlock; ++i) top[i & 3] = fmaxf(top[i & 3], fabsf(v[i]));
+                const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
                 const int k = pair_exponent(m);
                 const float sc = pow2(k);
                 uint32_t hi[32], lo[32];
@@ -212,8 +224,14 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSums));
         const int quad = warp & 3, row = quad * 32 + lane;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        float* const ref = refs + quad * kMostX;
         uint32_t it = 0;
         bool ok = true;
+        for (int n = lane; n < kMostX; n += 32) {
+            if (quad == 0) row_f[n] = n < g.N ? g.rowf[n] * g.grow : 0.f;
+            ref[n] = -INFINITY;
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");         // these four warps
         for (int tile = blockIdx.x; tile < g.tiles && ok; tile += gridDim.x) {
             float z[4][32];
 #pragma unroll
@@ -227,13 +245,19 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                 tc_fence_after();
                 const float sc = scales[a * kTileRows + row];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < 4; q += 2) {        // two loads under way at a time
                     if (q * 32 >= g.Nr) continue;
-                    uint32_t rr[32];
-                    tmem_ld32(t_sum(a) + lanes + q * 32u, rr);
+                    uint32_t r0[32], r1[32];
+                    tmem_ld32(t_sum(a) + lanes + q * 32u, r0);
+                    const bool more = q * 32 + 32 < g.Nr;
+                    if (more) tmem_ld32(t_sum(a) + lanes + q * 32u + 32u, r1);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) z[q][j] = fmaf(__uint_as_float(rr[j]), sc, z[q][j]);
+                    for (int j = 0; j < 32; ++j) z[q][j] = fmaf(__uint_as_float(r0[j]), sc, z[q][j]);
+                    if (more) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[q + 1][j] = fmaf(__uint_as_float(r1[j]), sc, z[q + 1][j]);
+                    }
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -241,27 +265,52 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
             }
             if (!ok) break;
             const bool there = tile * kTileRows + row < g.V;
+            // through tensor memory, which takes an index: what follows is one piece of code for all 32 columns at a time (four
+            // of them in line are fetched anew for every tile: 16 us of 79 at 100 rows, V 50,257, C 1,024)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                if (q * 32 >= g.N) continue;
+                uint32_t r[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(z[q][j]);
+                if (q * 32 < g.N) tmem_st32(tmem + 384u + lanes + q * 32u, r);
+            }
+            tmem_st_wait();
+#pragma unroll 1
+            for (int q = 0; q * 32 < g.N; ++q) {
+                uint32_t zr[32];
+                tmem_ld32(tmem + 384u + lanes + q * 32u, zr);
+                tmem_ld_wait();
                 const int n = q * 32 + lane;
-                const float mine = n < g.N ? g.rowf[n] * g.grow : 0.f;
-                float v[32];
+                float v[32], most = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const float t = __shfl_sync(0xffffffffu, mine, j);
-                    z[q][j] = there ? z[q][j] * t * 32768.0f : -INFINITY;
-                    v[j] = z[q][j];
-                }
-                const float m = across<true>(v, lane);
+                for (int j = 0; j < 32; j += 4) {
+                    const float4 f = *reinterpret_cast<const float4*>(row_f + q * 32 + j), r = *reinterpret_cast<const float4*>(ref + q * 32 + j);
+                    const float fs[4] = {f.x, f.y, f.z, f.w}, rs[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const float top = __shfl_sync(0xffffffffu, m, j);
-                    v[j] = there ? ex2_fast(z[q][j] - top) : 0.f;
+                    for (int i = 0; i < 4; ++i) {
+                        const float zs = __uint_as_float(zr[j + i]) * fs[i] * 32768.0f;
+                        zr[j + i] = __float_as_uint(zs);
+                        v[j + i] = zs - rs[i];
+                        most = fmaxf(most, v[j + i]);
+                    }
                 }
+                // a row's reference is its maximum over the warp's part of an earlier tile, as long as that is near enough: sums
+                // of 2^20 and more take a new one, those that vanish beside it add nothing that counts
+                if (__any_sync(0xffffffffu, there && !(most <= 20.f))) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = there ? __uint_as_float(zr[j]) : -INFINITY;
+                    const float m = fmaxf(across<true>(v, lane), ref[n]);
+                    __syncwarp();
+                    ref[n] = m;
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(zr[j]) - ref[q * 32 + j];
+                }
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = there ? ex2_fast(v[j]) : 0.f;
                 const float s = across<false>(v, lane);
                 // a warp whose rows all lie behind the vocabulary has the sum zero
-                if (n < g.N) g.stats[(long long)n * (4 * g.tiles) + 4 * tile + quad] = make_float2(m, s);
+                if (n < g.N) g.stats[(long long)n * (4 * g.tiles) + 4 * tile + quad] = make_float2(ref[n], s);
             }
         }
     }
@@ -286,9 +335,13 @@ cudaError_t launch(const HeadArgs& h, const HalfMat& x, const Args& g, cudaStrea
         tensor_map_encoder()(&tmX, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, (void*)x.hi, x_dims, x_strides, x_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
-    const cudaError_t e = allow_smem<head_direct_kernel<PLANES>>(C::kSmem);
+    const uint32_t fit = (kSmemMost - C::kFixed) / x_bytes(g.Nr);
+    Args a = g;
+    a.x_stages = fit < (uint32_t)kMostXStages ? (int)fit : kMostXStages;       // two and more: 128 rows take 32 KB
+    const cudaError_t e = allow_smem<head_direct_kernel<PLANES>>(kSmemMost);
     if (e != cudaSuccess) return e;
-    BT_KERNEL_LAUNCH((head_direct_kernel<PLANES>), g.tiles < sm_count() ? g.tiles : sm_count(), kThreads, C::kSmem, s, tmW, tmX, g);
+    BT_KERNEL_LAUNCH((head_direct_kernel<PLANES>), g.tiles < sm_count() ? g.tiles : sm_count(), kThreads, (size_t)(C::kFixed + a.x_stages * x_bytes(g.Nr)), s,
+                     tmW, tmX, a);
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }
