@@ -644,9 +644,10 @@ BT_API bt_status bt_op_dropout_bwd(const float* dy, int64_t n, double p, uint64_
  * with q_nv = exp(z_nv - lse_n) and g_n = inv_count w_n, in a fixed order (no atomics on floats: two runs give the
  * same bits).  piece: columns of the vocabulary worked on at a time, 0 for the library's choice; it sets the size of the
  * scratch and not the results' accuracy.
- * The products run on the tensor cores on pairs of FP16 numbers (22 bits of each value, scaled by powers of two so that
- * the largest one of x's row, and of W, lies near FP16's largest): values below 2^-18 of those lose bits at an absolute
- * 2^-40 of the largest.  Few rows run in plain FP32.  x of rows that count, and W, must be finite; a row whose scores are
+ * The products run on the tensor cores on pairs of FP16 numbers: 22 bits of each value, scaled by powers of two so that the
+ * largest one lies near FP16's largest.  Values below 2^-18 of the largest lose bits, at an absolute 2^-40 of it.  That is the
+ * largest of x's or W's row in the forward, and in the backward that of x's row, of g_n x_n over all rows, and of all of W.
+ * Up to eight rows (sixteen in the backward of a small W) run in plain FP32.  x of rows that count, and W, must be finite; a row whose scores are
  * beyond FP32 is not a number in losses and lse.
  * C a multiple of 32, at most 4096; V and N at most 2^24.  N = 0 is nothing to do (loss_mean and dw become 0).
  * scratch: device, 256-byte aligned, of the stated size (K = 0), contents irrelevant on entry; calls that may
@@ -666,7 +667,8 @@ BT_API bt_status bt_op_head_check(const void* scratch, void* stream);
 
 /* A teacher's top logits: K entries per row (1 to 1024), ids int32 [N, K] and logits float [N, K].  An id below zero,
  * or a logit of -inf, marks an entry that is not there (rows may have fewer than K, or none: such a row counts as
- * one without a target); the same id twice counts with both probabilities.  With t the logits and tau the
+ * one without a target); the same id twice counts with both probabilities.  An id from V on counts as id 0 and its row + 1 is
+ * stored in *d_bad, as above.  With t the logits and tau the
  * temperature (1e-4 to 1e4),
  *     p_nk = softmax over the row's entries of t_nk / tau            (lse NULL), or
  *     p_nk = exp(t_nk / tau - lse_n)                                 (lse float [N]: log sum exp(t / tau) of the teacher's

@@ -1716,6 +1716,12 @@ bt_status head_args(HeadArgs& g, const char* who, const float* x, const float* x
     return BT_OK;
 }
 
+// A call without rows leaves an error word that bt_op_head_check reads as none.
+bt_status head_nothing_waited(const HeadArgs& g, size_t scratch_bytes, cudaStream_t s) {
+    if (g.scratch && scratch_bytes >= sizeof(int)) BT_CUDA(cudaMemsetAsync(g.scratch, 0, sizeof(int), s));
+    return BT_OK;
+}
+
 bt_status head_fwd(const char* who, HeadArgs& g, float* losses, float* lse, float* loss_mean, int32_t* d_bad, size_t scratch_bytes,
                    cudaStream_t s) {
     if (g.N != 0) BT_PTR(losses);
@@ -1723,7 +1729,7 @@ bt_status head_fwd(const char* who, HeadArgs& g, float* losses, float* lse, floa
     if (reinterpret_cast<uintptr_t>(d_bad) & 3u) return fail(BT_ERR_INVALID_ARG, "%s: d_bad is not 4-byte aligned", who);
     if (g.N == 0) {
         if (loss_mean) BT_CUDA(cudaMemsetAsync(loss_mean, 0, sizeof(float), s));
-        return BT_OK;
+        return head_nothing_waited(g, scratch_bytes, s);
     }
     if (scratch_bytes < bt_op_head_fwd_scratch_bytes(g.N, g.C, g.V, g.aim.K)) return fail(BT_ERR_OOM, "%s: scratch too small", who);
     for (const float* out : {losses, lse, loss_mean})
@@ -1742,7 +1748,7 @@ bt_status head_bwd(const char* who, HeadArgs& g, const float* lse, int32_t piece
     if (g.N != 0 && !dx && !dx_split && !dw) return fail(BT_ERR_INVALID_ARG, "%s: no output requested", who);
     if (g.N == 0) {
         if (dw) BT_CUDA(cudaMemsetAsync(dw, 0, (size_t)g.V * g.C * sizeof(float), s));
-        return BT_OK;
+        return head_nothing_waited(g, scratch_bytes, s);
     }
     if (scratch_bytes < bt_op_head_bwd_scratch_bytes(g.N, g.C, g.V, g.aim.K, piece)) return fail(BT_ERR_OOM, "%s: scratch too small", who);
     for (const float* out : {(const float*)dx, (const float*)dx_split, (const float*)dw})

@@ -554,6 +554,85 @@ def test_scratch_is_enough_and_not_exceeded():
             assert (area[need:] == 90).all()
 
 
+@gpu
+@pytest.mark.parametrize("N", [6, 40, 150])
+@pytest.mark.parametrize("K,V", [(20, 7), (32, 40), (33, 9), (64, 3000), (100, 11), (300, 200), (1024, 37), (1024, 3000)])
+def test_an_id_many_times(N, K, V):
+    """Entries of one id, next to one another, far apart and in every place, and ids in even steps."""
+    c = Case(N, 32, V, K=K, tau=2.0, seed=K + V)
+    k = torch.arange(K, device=DEV)
+    c.ids[1] = 3                                                  # all of them
+    c.ids[2] = (k % V).int()
+    c.ids[3] = (64 * k % V).int()
+    c.ids[4] = (k * 8 // K % V).int()
+    c.ids[5] = -1
+    c.ids[5, 0] = c.ids[5, K - 1] = V - 1                         # the first and the last
+    check(c)
+
+
+@gpu
+@pytest.mark.parametrize("N", [4, 40, 150])
+@pytest.mark.parametrize("K", [5, 40])
+def test_captured_distillation(N, K):
+    c = Case(N, 64, 500, K=K, tau=1.5, weights=True)
+    plain = check(c)
+    out = [torch.empty(n, device=DEV) for n in (N, N, 1)]
+    dx, dw = torch.empty(N, 64, device=DEV), torch.empty(500, 64, device=DEV)
+    fs = torch.empty(b.bt_op_head_fwd_scratch_bytes(N, 64, 500, K), dtype=torch.uint8, device=DEV)
+    bs = torch.empty(b.bt_op_head_bwd_scratch_bytes(N, 64, 500, K), dtype=torch.uint8, device=DEV)
+    aim = c.aim()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.bt_op_head_distill_fwd(c.x, None, c.w, None, aim, c.rw, N, 64, 500, c.inv, *out, fs, fs.numel())
+        b.bt_op_head_distill_bwd(c.x, None, c.w, None, aim, c.rw, out[1], N, 64, 500, c.inv, dx, dw, bs, bs.numel())
+    ids = c.ids.clone()
+    c.ids.copy_((ids + 7) % 500)                                  # the table of the last run's entries must not stay
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip((*out, dx, dw), check(c)))
+    c.ids.copy_(ids)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip((*out, dx, dw), plain))
+
+
+@gpu
+@pytest.mark.parametrize("N", [4, 40, 300])
+def test_two_calls_at_once(N):
+    """Two calls with a scratch each, on two streams."""
+    cases = [Case(N, 128, 9000, weights=True, seed=1), Case(N, 128, 9000, K=12, weights=True, seed=2)]
+    plain = [check(c) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                call_f, call_b = (b.bt_op_head_distill_fwd, b.bt_op_head_distill_bwd) if c.K else (b.bt_op_head_xent_fwd, b.bt_op_head_xent_bwd)
+                out = [torch.empty(n, device=DEV) for n in (N, N, 1)] + [torch.empty(N, 128, device=DEV), torch.empty(9000, 128, device=DEV)]
+                need = max(b.bt_op_head_fwd_scratch_bytes(N, 128, 9000, c.K), b.bt_op_head_bwd_scratch_bytes(N, 128, 9000, c.K))
+                work = torch.empty(need, dtype=torch.uint8, device=DEV)
+                aim = c.aim()
+                call_f(c.x, None, c.w, None, aim, c.rw, N, 128, 9000, c.inv, *out[:3], work, need)
+                call_b(c.x, None, c.w, None, aim, c.rw, out[1], N, 128, 9000, c.inv, *out[3:], work, need)
+                got.append((out, work, aim))
+        torch.cuda.synchronize()
+        for (out, _, _), want in zip(got, plain):
+            assert all(torch.equal(p, q) for p, q in zip(out, want))
+
+
+@gpu
+def test_no_rows_leave_no_error():
+    work = torch.full((4096,), 255, dtype=torch.uint8, device=DEV)
+    none, w, dw, mean = torch.empty(0, device=DEV), torch.ones(8, 32, device=DEV), torch.ones(8, 32, device=DEV), torch.ones(1, device=DEV)
+    b.bt_op_head_xent_fwd(None, None, w, None, None, None, 0, 32, 8, 1.0, None, None, mean, work, 4096)
+    b.bt_op_head_check(work)
+    work.fill_(255)
+    b.bt_op_head_xent_bwd(None, None, w, None, None, None, none, 0, 32, 8, 1.0, None, dw, work, 4096)
+    b.bt_op_head_check(work)
+    assert float(mean) == 0.0 and not dw.any()
+
+
 # ------------------------------------------------------------------------------- GPU: distillation on logits
 
 def logits_case(N, V, K, tau, whole, pad, seed=0, ld=None):
@@ -599,6 +678,25 @@ def test_distillation_on_logits(N, V, K, tau, whole, ld):
     alone = logits_run(c, dz=False)
     assert torch.equal(alone[0], losses) and torch.equal(alone[1], mean)
     assert torch.equal(logits_run(c, dz=False, planes=True)[3], s)
+
+
+@gpu
+@pytest.mark.parametrize("N", [6, 300])
+@pytest.mark.parametrize("K,V", [(20, 7), (32, 40), (33, 9), (64, 3000), (300, 9000), (1024, 37), (1024, 24577), (512, 100001)])
+def test_an_id_many_times_on_logits(N, K, V):
+    c = logits_case(N, V, K, 2.0, False, pad=0, seed=K + V)
+    k = torch.arange(K, device=DEV)
+    c.ids[1] = 3
+    c.ids[2] = (k % V).int()
+    c.ids[3] = (64 * k % V).int()
+    c.ids[4] = (k * 8 // K % V).int()
+    c.ids[5] = -1
+    c.ids[5, 0] = c.ids[5, K - 1] = V - 1
+    losses, _, g, _ = logits_run(c)
+    want = logits_want(c)
+    top = max(1.0, float(c.z.abs().max()) / 2)                    # as above
+    assert float((losses - want[0]).abs().max()) < 2e-6 * 4 * top * 2
+    assert rel(g, want[2]) < 2e-6 * top
 
 
 @gpu
