@@ -65,6 +65,7 @@ template <int THREADS, int CS>
 __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const DistillArgs g, int slice4, int mean_here) {
     __shared__ Four sm[2][THREADS / 32], all[2][CS];
     __shared__ Entries en;
+    extern __shared__ int table[];                                  // [places]
     pdl_wait();
     pdl_trigger();
     const LossAim& a = g.aim;
@@ -78,6 +79,8 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const 
     const float4* z4 = reinterpret_cast<const float4*>(z);
     const float f = kLog2e / a.tau;
 
+    const int places = id_places(a.K);
+    for (int k = threadIdx.x; k < places; k += THREADS) table[k] = -1;      // row_all has a barrier before their use
     // the row's entries
     Four m{-INFINITY, -INFINITY, 0.f, 0.f};
 #pragma unroll 1
@@ -128,15 +131,13 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const 
         const int id = en.id[k];
         const float lp = en.t[k] - norm, p = id >= 0 ? expf(lp) : 0.f;
         if (id >= 0) en.z[k] = (en.z[k] - m.a) * f;
+        twice |= seen_before(table, places, a.K, id);
         if (p != 0.f && rank == 0) {
             t.b += p;
             t.c += p * (lp - en.z[k] * kLn2);
         }
         en.t[k] = p;                                                // only this thread has read it
     }
-#pragma unroll 1
-    for (int k = threadIdx.x >> 5; k < a.K; k += THREADS / 32)      // does an id come twice?
-        for (int j = threadIdx.x & 31; j < k; j += 32) twice |= en.id[j] == en.id[k] && en.id[k] >= 0;
     t.d = twice ? 1.f : 0.f;
     t = row_all<THREADS, CS, false>(t, sm[1], all[1]);
     const float share = a.lse ? 1.f : any ? 1.0f / t.b : 0.f, S = a.lse ? t.b : any ? 1.f : 0.f;
@@ -224,6 +225,7 @@ cudaError_t launch_rows(const DistillArgs& g, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(g.N * CS));
     cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = sizeof(int) * id_places(g.aim.K);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -174,11 +174,12 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_kernel(const HeadA
     if (g.loss_mean) mean_by_last<kFinishThreads>(g.aim, g.losses, g.N, &head->rows_done, gridDim.x, g.loss_mean, smd);
 }
 
-// log sum exp of a row from its strips, by a warp.
-__device__ __forceinline__ float row_lse(const float2* st, int strips) {
+// log sum exp of a row from its strips, by one warp or all (WARPS) of a CTA.
+template <int WARPS>
+__device__ __forceinline__ float row_lse(const float2* st, int strips, float* sm) {
     float m = -INFINITY, s = 0.f;
 #pragma unroll 4
-    for (int i = threadIdx.x & 31; i < strips; i += 32) {
+    for (int i = WARPS == 1 ? threadIdx.x & 31 : threadIdx.x; i < strips; i += 32 * WARPS) {
         const float2 p = st[i];
         if (p.y != 0.f) {                   // a strip without columns has the sum zero
             const float m1 = fmaxf(m, p.x);
@@ -186,32 +187,35 @@ __device__ __forceinline__ float row_lse(const float2* st, int strips) {
             m = m1;
         }
     }
-    const float top = warp_max(m);
-    return (top + log2f(warp_sum(s != 0.f ? s * ex2_fast(m - top) : 0.f))) * kLn2;
+    const float top = WARPS == 1 ? warp_max(m) : block_all<32 * WARPS>(m, sm, MaxOp()), t = s != 0.f ? s * ex2_fast(m - top) : 0.f;
+    return (top + log2f(WARPS == 1 ? warp_sum(t) : block_all<32 * WARPS>(t, sm, SumOp()))) * kLn2;
 }
 
-// The loss against targets, a row per warp (a CTA per row takes 88 us for 8,192 rows, most of it barriers).
+// The loss against targets, a row per warp, or per CTA where there are few rows of many strips (100 rows of 592: 5 us less; 8,192
+// rows take 88 us so, most of it barriers, and 36 with a warp each).
+template <int WARPS>
 __global__ void __launch_bounds__(kFinishThreads) head_finish_target_kernel(const HeadArgs g, const float2* __restrict__ stats, int strips,
                                                                             HeadHeader* head) {
     __shared__ double smd[kFinishThreads / 32];
+    __shared__ float smf[kFinishThreads / 32];
     pdl_wait();
     pdl_trigger();
-    const int64_t row = blockIdx.x * (int64_t)(kFinishThreads / 32) + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
+    const int64_t row = WARPS == 1 ? blockIdx.x * (int64_t)(kFinishThreads / 32) + (threadIdx.x >> 5) : blockIdx.x;
+    const int lane = WARPS == 1 ? threadIdx.x & 31 : threadIdx.x;
     if (row < g.N) {
         int t = g.aim.targets[row];
         if (t >= g.V) {
             if (g.bad && lane == 0) atomicCAS(g.bad, 0, (int)row + 1);
             t = 0;
         }
-        const float lse = row_lse(stats + row * strips, strips);
+        const float lse = row_lse<WARPS>(stats + row * strips, strips, smf);
         float z = 0.f;
         const int C4 = g.C / 4;
         if (t >= 0) {
 #pragma unroll 4
-            for (int c = lane; c < C4; c += 32)
+            for (int c = lane; c < C4; c += 32 * WARPS)
                 z = dot4(ld_value(g.x, g.x_lo, row * C4 + c), ld_value(g.w, g.w_lo, (int64_t)t * C4 + c), z);
-            z = warp_sum(z);
+            z = WARPS == 1 ? warp_sum(z) : block_all<32 * WARPS>(z, smf, SumOp());
         }
         if (lane == 0) {
             if (g.lse) g.lse[row] = lse;
@@ -231,7 +235,7 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_entries_kernel(con
     const int lane = threadIdx.x & 31;
     if (row < g.N) {
         const LossAim& a = g.aim;
-        const float lse = row_lse(stats + row * strips, strips);
+        const float lse = row_lse<1>(stats + row * strips, strips, nullptr);
         float top = -INFINITY, sum = 0.f, loss = 0.f;
         int id;
         bool any = false;
@@ -267,7 +271,7 @@ __device__ __forceinline__ float max4(float m, float4 v) {
 // What the backward needs to know of the rows, one at a time per CTA, and the largest values of W and of y_nc = g_n x_nc.  Entries with the same id are joined into the first of them.
 __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArgs g, RowParams* rows, int* eid, float* ep,
                                                                    float* wpart, float* ypart, HeadHeader* head) {
-    extern __shared__ int ids[];            // [K], then the weights [K]
+    extern __shared__ int ids[];            // [K], then the weights [K] and id_places(K)
     __shared__ float smf[kFinishThreads / 32];
     pdl_wait();
     pdl_trigger();
@@ -299,7 +303,10 @@ __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArg
             r.target = t >= g.V ? 0 : t;
         } else {
             float* p = (float*)(ids + a.K);
-            bool any;
+            int* table = ids + 2 * a.K;
+            const int places = id_places(a.K);
+            for (int k = threadIdx.x; k < places; k += kFinishThreads) table[k] = -1;
+            bool any, twice = false;
             const float norm = teacher_norm<kFinishThreads>(a, row, g.V, nullptr, smf, any);
             float sum = 0.f;
             for (int k = threadIdx.x; k < a.K; k += kFinishThreads) {
@@ -307,16 +314,18 @@ __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArg
                 const float t = any ? entry_logit(a, row, k, g.V, nullptr, id) : -INFINITY;
                 p[k] = any ? expf(t - norm) : 0.f;
                 ids[k] = p[k] != 0.f ? id : -1;
+                twice |= seen_before(table, places, a.K, ids[k]);
                 sum += p[k];
             }
+            twice = __syncthreads_or(twice);
             sum = block_all<kFinishThreads>(sum, smf, SumOp());
             live = live && sum != 0.f;
             r.g *= sum;
             for (int k = threadIdx.x; k < a.K; k += kFinishThreads) {
                 const int id = ids[k];
-                float w = 0.f;
                 bool first = live && id >= 0;
-                for (int j = 0; first && j < a.K; ++j) {
+                float w = twice ? 0.f : p[k];
+                for (int j = 0; twice && first && j < a.K; ++j) {
                     if (ids[j] != id) continue;
                     if (j < k) first = false;
                     else w += p[j];
@@ -612,8 +621,10 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     }
     if (e != cudaSuccess) return e;
     const unsigned ctas = (unsigned)((g.N + kFinishThreads / 32 - 1) / (kFinishThreads / 32));
-    if (!K)
-        BT_KERNEL_LAUNCH((head_finish_target_kernel), ctas, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
+    if (!K && g.N <= 148 * 8 && strips > 256)
+        BT_KERNEL_LAUNCH((head_finish_target_kernel<kFinishThreads / 32>), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
+    else if (!K)
+        BT_KERNEL_LAUNCH((head_finish_target_kernel<1>), ctas, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
     else if (f == kPairs)
         BT_KERNEL_LAUNCH((head_finish_entries_kernel), ctas, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, (const float*)w.zk, w.head);
     else
@@ -627,7 +638,7 @@ cudaError_t launch_head_bwd(const HeadArgs& g, cudaStream_t s) {
     const int K = g.aim.targets ? 0 : g.aim.K;
     bwd_layout(w, g.scratch, g.N, g.C, g.V, K, g.piece);
     const bool few = few_rows(g.N, g.C, g.V, true);
-    BT_KERNEL_LAUNCH((head_rows_kernel), row_ctas(g.N) + (few ? 0 : kParts), kFinishThreads, (size_t)K * 8, s, g, w.rows, w.eid, w.ep, w.wpart, w.ypart,
+    BT_KERNEL_LAUNCH((head_rows_kernel), row_ctas(g.N) + (few ? 0 : kParts), kFinishThreads, (size_t)(2 * K + id_places(K)) * 4, s, g, w.rows, w.eid, w.ep, w.wpart, w.ypart,
                      w.head);
     BT_COUNT_LAUNCH();
     const cudaError_t e = cudaGetLastError();

@@ -24,24 +24,25 @@ using namespace tc;
 
 namespace {
 
-constexpr int kTileRows = 128, kBlock = 64, kMostX = 128;
+constexpr int kTileRows = 128, kGroup = 32, kBlock = 64, kMostX = 128;
 constexpr int kThreads = 512;
 constexpr int kRegsIssue = 40, kRegsPairs = 120, kRegsSums = 224;      // of the launch's 4 x 128
 
 struct Args {
-    int N, V, tiles, blocks, Nr;            // Nr: rows of x, up to a multiple of 16
+    int N, V, groups, blocks, Nr;           // groups of 32 rows of W; Nr: rows of x, up to a multiple of 16
     int x_stages;
     const float* rowf;                      // [N]
-    float2* stats;                          // [N][4 tiles]
+    float2* stats;                          // [N][4 CTAs]
     float grow;
     int* err;
 };
 
 template <bool PLANES>
 struct Cfg {
-    static constexpr uint32_t kW = (PLANES ? 2u : 1u) * kTileRows * kBlock * 4u;
+    static constexpr uint32_t kForms = PLANES ? 2u : 1u, kBox = kGroup * 32u * 4u;       // a stage: [2 halves of the block][forms][4 groups] boxes
+    static constexpr uint32_t kW = 8u * kForms * kBox;
     static constexpr int kStages = PLANES ? 2 : 4;                      // of W; those of x are as many as fit
-    static constexpr uint32_t kScales = (2u * kTileRows + kMostX + 4u * kMostX) * 4u;      // scales, rowf, references of four warps
+    static constexpr uint32_t kScales = (2u * kTileRows + kMostX + 8u * kMostX) * 4u;      // scales, rowf, references and sums of four warps
     static constexpr uint32_t kFixed = 1024 + kStages * kW + kScales + 256;
 };
 constexpr uint32_t kSmemMost = 227u * 1024u;
@@ -75,7 +76,8 @@ __device__ __forceinline__ float across(float (&v)[32], int lane) {
 
 template <bool PLANES>
 __global__ void __launch_bounds__(kThreads, 1)
-head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const Args g) {
+head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmGroup, const __grid_constant__ CUtensorMap tmX,
+                   const Args g) {
     using C = Cfg<PLANES>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -94,9 +96,14 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     auto x_empty_bar = [&](int s) { return bars + 8u * (2 * C::kStages + 6 + kMostXStages + s); };
     const uint32_t tmem_slot = bars + 8u * (2 * C::kStages + 6 + 2 * kMostXStages);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // the CTA's share of W, taken four groups at a time; the same number for all, where that takes more than once
+    const bool once = 4 * gridDim.x >= g.groups;
+    const int g0 = once ? 4 * blockIdx.x : (int)((int64_t)blockIdx.x * g.groups / gridDim.x);
+    const int g1 = once ? min(g.groups, g0 + 4) : (int)((blockIdx.x + 1LL) * g.groups / gridDim.x);
 
     if (threadIdx.x == 0) {
         prefetch_tensormap(&tmW);
+        prefetch_tensormap(&tmGroup);
         prefetch_tensormap(&tmX);
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(full_bar(s), 1);
@@ -132,14 +139,21 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         if ((warp == 0 || warp == 2) && lane == 0) {
             uint32_t it = 0, xs = 0, xp = 0;           // stage of x and how often it has come round
             bool ok = true;
-            for (int t = blockIdx.x; t < g.tiles && ok; t += gridDim.x)
+            for (int first = g0; first < g1 && ok; first += 4)
                 for (int b = 0; b < g.blocks; ++b, ++it) {
                     if (warp == 0) {
-                        const int s = it % C::kStages;
+                        const int s = it % C::kStages, n = min(4, g1 - first);
                         if (!mbar_wait(empty_bar(s), ((it / C::kStages) & 1u) ^ 1u, g.err, 41)) { ok = false; break; }
-                        mbar_expect_tx(full_bar(s), C::kW);
-                        tma_load_3d(base + s * C::kW, &tmW, full_bar(s), b * kBlock, t * kTileRows, 0);
-                        tma_load_3d(base + s * C::kW + C::kW / 2, &tmW, full_bar(s), b * kBlock + 32, t * kTileRows, 0);
+                        mbar_expect_tx(full_bar(s), 2u * C::kForms * n * C::kBox);
+                        if (n == 4) {
+                            tma_load_3d(base + s * C::kW, &tmW, full_bar(s), b * kBlock, first * kGroup, 0);
+                            tma_load_3d(base + s * C::kW + C::kW / 2, &tmW, full_bar(s), b * kBlock + 32, first * kGroup, 0);
+                        } else {
+                            for (uint32_t i = 0; i < 2 * C::kForms; ++i)
+                                for (int k = 0; k < n; ++k)
+                                    tma_load_3d(base + s * C::kW + (4u * i + k) * C::kBox, &tmGroup, full_bar(s), b * kBlock + (int)(i / C::kForms) * 32,
+                                                (first + k) * kGroup, (int)(i % C::kForms));
+                        }
                     } else {
                         if (!mbar_wait(x_empty_bar(xs), (xp & 1u) ^ 1u, g.err, 47)) { ok = false; break; }
                         mbar_expect_tx(x_full_bar(xs), x_size);
@@ -155,7 +169,7 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
             const uint32_t idesc = (1u << 4) | ((uint32_t)(g.Nr >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
             uint32_t it = 0, xs = 0, xp = 0;
             bool ok = true;
-            for (int t = blockIdx.x; t < g.tiles && ok; t += gridDim.x)
+            for (int first = g0; first < g1 && ok; first += 4)
                 for (int b = 0; b < g.blocks; ++b, ++it) {
                     const int a = it & 1;
                     if (!mbar_wait_warp(x_full_bar(xs), xp & 1u, g.err, 48) || !mbar_wait_warp(pairs_bar(a), (it >> 1) & 1u, g.err, 42)) { ok = false; break; }
@@ -178,24 +192,32 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         }
     } else if (warp < 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsPairs));
-        const int a = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
-        const uint32_t t_row = t_pair(a) + ((uint32_t)((warp & 3) * 32) << 16);
+        const int a = (warp - 4) >> 2, quad = warp & 3, row = quad * kGroup + lane;
+        const uint32_t t_row = t_pair(a) + ((uint32_t)(quad * 32) << 16);
         uint32_t it = 0;
         bool ok = true;
-        for (int t = blockIdx.x; t < g.tiles && ok; t += gridDim.x)
+        for (int first = g0; first < g1 && ok; first += 4)
             for (int b = 0; b < g.blocks; ++b, ++it) {
                 if ((int)(it & 1u) != a) continue;
                 const int s = it % C::kStages;
                 if (!mbar_wait_warp(full_bar(s), (it / C::kStages) & 1u, g.err, 43)) { ok = false; break; }
+                if (first + quad >= g1) {   // behind the share: these lanes' products are not looked at
+                    if (!mbar_wait_warp(drained_bar(a), ((it >> 1) & 1u) ^ 1u, g.err, 44)) { ok = false; break; }
+                    if (lane == 0) {
+                        mbar_arrive(empty_bar(s));
+                        mbar_arrive(pairs_bar(a));
+                    }
+                    continue;
+                }
                 // the 16-byte units of a row of 128 bytes lie swizzled by the row
                 float v[kBlock];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {
-                        const uint8_t* p = base_ptr + s * C::kW + h * (C::kW / 2) + row * 128 + ((q ^ (row & 7)) << 4);
+                        const uint8_t* p = base_ptr + s * C::kW + (4 * C::kForms * h + quad) * C::kBox + lane * 128 + ((q ^ (lane & 7)) << 4);
                         float4 w = *reinterpret_cast<const float4*>(p);
-                        if (PLANES) w = add4(w, *reinterpret_cast<const float4*>(p + kTileRows * 128));
+                        if (PLANES) w = add4(w, *reinterpret_cast<const float4*>(p + 4 * C::kBox));
                         v[h * 32 + 4 * q] = w.x; v[h * 32 + 4 * q + 1] = w.y; v[h * 32 + 4 * q + 2] = w.z; v[h * 32 + 4 * q + 3] = w.w;
                     }
                 __syncwarp();
@@ -224,15 +246,17 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSums));
         const int quad = warp & 3, row = quad * 32 + lane;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        float* const ref = refs + quad * kMostX;
+        float *const ref = refs + quad * kMostX, *const sum = refs + (4 + quad) * kMostX;     // over the tiles, in units of the reference
         uint32_t it = 0;
         bool ok = true;
         for (int n = lane; n < kMostX; n += 32) {
             if (quad == 0) row_f[n] = n < g.N ? g.rowf[n] * g.grow : 0.f;
             ref[n] = -INFINITY;
+            sum[n] = 0.f;
         }
         asm volatile("bar.sync 1, 128;" ::: "memory");         // these four warps
-        for (int tile = blockIdx.x; tile < g.tiles && ok; tile += gridDim.x) {
+        for (int first = g0; first < g1 && ok; first += 4) {
+            const bool mine = first + quad < g1;
             float z[4][32];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
@@ -246,7 +270,7 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                 const float sc = scales[a * kTileRows + row];
 #pragma unroll
                 for (int q = 0; q < 4; q += 2) {        // two loads under way at a time
-                    if (q * 32 >= g.Nr) continue;
+                    if (q * 32 >= g.Nr || !mine) continue;
                     uint32_t r0[32], r1[32];
                     tmem_ld32(t_sum(a) + lanes + q * 32u, r0);
                     const bool more = q * 32 + 32 < g.Nr;
@@ -264,7 +288,8 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                 if (lane == 0) mbar_arrive(drained_bar(a));
             }
             if (!ok) break;
-            const bool there = tile * kTileRows + row < g.V;
+            if (!mine) continue;
+            const bool there = (first + quad) * kGroup + lane < g.V;
             // through tensor memory, which takes an index: what follows is one piece of code for all 32 columns at a time (four
             // of them in line are fetched anew for every tile: 16 us of 79 at 100 rows, V 50,257, C 1,024)
 #pragma unroll
@@ -294,25 +319,28 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                         most = fmaxf(most, v[j + i]);
                     }
                 }
-                // a row's reference is its maximum over the warp's part of an earlier tile, as long as that is near enough: sums
+                // a row's reference is its maximum over the warp's part of an earlier tile, as long as that is near enough: values
                 // of 2^20 and more take a new one, those that vanish beside it add nothing that counts
                 if (__any_sync(0xffffffffu, there && !(most <= 20.f))) {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = there ? __uint_as_float(zr[j]) : -INFINITY;
                     const float m = fmaxf(across<true>(v, lane), ref[n]);
                     __syncwarp();
-                    ref[n] = m;
+                    if (m != ref[n]) {
+                        sum[n] = sum[n] != 0.f ? sum[n] * ex2_fast(ref[n] - m) : 0.f;
+                        ref[n] = m;
+                    }
                     __syncwarp();
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(zr[j]) - ref[q * 32 + j];
                 }
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = there ? ex2_fast(v[j]) : 0.f;
-                const float s = across<false>(v, lane);
-                // a warp whose rows all lie behind the vocabulary has the sum zero
-                if (n < g.N) g.stats[(long long)n * (4 * g.tiles) + 4 * tile + quad] = make_float2(ref[n], s);
+                sum[n] += across<false>(v, lane);
             }
         }
+        // a warp without rows of W has the sum zero
+        for (int n = lane; n < g.N; n += 32) g.stats[(long long)n * (4 * gridDim.x) + 4 * blockIdx.x + quad] = make_float2(ref[n], sum[n]);
     }
 
     tc_fence_before();
@@ -324,13 +352,15 @@ template <bool PLANES>
 cudaError_t launch(const HeadArgs& h, const HalfMat& x, const Args& g, cudaStream_t s) {
     using C = Cfg<PLANES>;
     if (!tensor_map_encoder()) return cudaErrorNotSupported;
-    CUtensorMap tmW, tmX;
+    CUtensorMap tmW, tmGroup, tmX;
     const cuuint32_t one[3] = {1, 1, 1};
     const cuuint64_t w_dims[3] = {(cuuint64_t)h.C, (cuuint64_t)h.V, PLANES ? 2u : 1u}, w_strides[2] = {(cuuint64_t)h.C * 4, (cuuint64_t)h.V * h.C * 4};
-    const cuuint32_t w_box[3] = {32, kTileRows, PLANES ? 2u : 1u};
+    const cuuint32_t w_box[3] = {32, kTileRows, C::kForms}, group_box[3] = {32, kGroup, 1};
     const cuuint64_t x_dims[3] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows, 2}, x_strides[2] = {(cuuint64_t)x.ld * 2, (cuuint64_t)x.plane * 2};
     const cuuint32_t x_box[3] = {kBlock, (cuuint32_t)g.Nr, 2};
     if (tensor_map_encoder()(&tmW, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, (void*)h.w, w_dims, w_strides, w_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
+        tensor_map_encoder()(&tmGroup, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, (void*)h.w, w_dims, w_strides, group_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
         tensor_map_encoder()(&tmX, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, (void*)x.hi, x_dims, x_strides, x_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
@@ -340,8 +370,8 @@ cudaError_t launch(const HeadArgs& h, const HalfMat& x, const Args& g, cudaStrea
     a.x_stages = fit < (uint32_t)kMostXStages ? (int)fit : kMostXStages;       // two and more: 128 rows take 32 KB
     const cudaError_t e = allow_smem<head_direct_kernel<PLANES>>(kSmemMost);
     if (e != cudaSuccess) return e;
-    BT_KERNEL_LAUNCH((head_direct_kernel<PLANES>), g.tiles < sm_count() ? g.tiles : sm_count(), kThreads, (size_t)(C::kFixed + a.x_stages * x_bytes(g.Nr)), s,
-                     tmW, tmX, a);
+    BT_KERNEL_LAUNCH((head_direct_kernel<PLANES>), head_direct_strips(h.V) / 4, kThreads, (size_t)(C::kFixed + a.x_stages * x_bytes(g.Nr)), s,
+                     tmW, tmGroup, tmX, a);
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }
@@ -349,12 +379,15 @@ cudaError_t launch(const HeadArgs& h, const HalfMat& x, const Args& g, cudaStrea
 }  // namespace
 
 bool head_direct_fits(int64_t N) { return N <= kMostX; }
-int head_direct_strips(int V) { return 4 * ((V + kTileRows - 1) / kTileRows); }
+int head_direct_strips(int V) {
+    const int tiles = (V + kTileRows - 1) / kTileRows, sms = sm_count();
+    return 4 * (tiles < sms ? tiles : sms);
+}
 
 cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float* rowf, float2* stats, int* err, cudaStream_t s) {
     Args g{};
     g.N = (int)h.N; g.V = h.V;
-    g.tiles = (h.V + kTileRows - 1) / kTileRows;
+    g.groups = (h.V + kGroup - 1) / kGroup;
     g.blocks = (h.C + kBlock - 1) / kBlock;
     g.Nr = ((int)h.N + 15) / 16 * 16;
     g.rowf = rowf; g.stats = stats; g.err = err;
