@@ -75,7 +75,7 @@ void tc_layout(Scratch& s, uint8_t* base, size_t& at, int64_t N, int C, int V) {
     s.scales = take<Scales>(base, at, 1);
     s.rowf = take<float>(base, at, N);
     s.x16 = take<__half>(base, at, 2 * (size_t)N * C);
-    s.w16 = take<__half>(base, at, 2 * (size_t)V * C);
+    if (V) s.w16 = take<__half>(base, at, 2 * (size_t)V * C);
 }
 
 // Which kernels form the forward's statistics: plain FP32, tensor cores straight from W, or from pairs of all of W.
@@ -114,8 +114,9 @@ size_t bwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K, int
         s.dx_part = take<float>(base, at, (size_t)head_few_strips(N, C, V) * kFewRows * C);
         return at;
     }
-    tc_layout(s, base, at, N, C, V);
-    s.wpart = take<float>(base, at, kParts);
+    const bool direct = head_direct_fits(N);
+    tc_layout(s, base, at, N, C, direct ? 0 : V);
+    if (!direct) s.wpart = take<float>(base, at, kParts);
     s.ypart = take<float>(base, at, row_ctas(N));
     s.y16 = take<__half>(base, at, 2 * (size_t)N * C);
     s.u16 = take<__half>(base, at, 2 * (size_t)N * piece_columns(N, V, piece));
@@ -428,17 +429,18 @@ __global__ void __launch_bounds__(kThreads) head_row_pairs_kernel(const HeadArgs
     }
 }
 
-// Backward: W and y at one power of two each, since they are summed over their rows, the rows of x each at its own.
+// Backward: W (where its pairs are made here) and y at one power of two each, since they are summed over their rows, the rows of x
+// each at its own.
 __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, const RowParams* __restrict__ rows, const Scratch s) {
     __shared__ float smf[kThreads / 32];
     pdl_wait();
     pdl_trigger();
     float m = 0.f, my = 0.f;
-    for (int i = threadIdx.x; i < kParts; i += kThreads) m = fmaxf(m, s.wpart[i]);
+    for (int i = threadIdx.x; s.wpart && i < kParts; i += kThreads) m = fmaxf(m, s.wpart[i]);
     for (int i = threadIdx.x; i < row_ctas(g.N); i += kThreads) my = fmaxf(my, s.ypart[i]);
-    const int kw = pair_exponent(block_all<kThreads>(m, smf, MaxOp())), ky = pair_exponent(block_all<kThreads>(my, smf, MaxOp()));
+    const int kw = s.wpart ? pair_exponent(block_all<kThreads>(m, smf, MaxOp())) : 0, ky = pair_exponent(block_all<kThreads>(my, smf, MaxOp()));
     if (blockIdx.x == 0 && threadIdx.x == 0) *s.scales = Scales{ldexpf(1.0f, -15 - kw), ldexpf(1.0f, -15 - ky)};
-    const int64_t n8 = (int64_t)g.V * g.C / 8, step = (int64_t)gridDim.x * kThreads;
+    const int64_t n8 = s.wpart ? (int64_t)g.V * g.C / 8 : 0, step = (int64_t)gridDim.x * kThreads;
     const float sw = pow2(kw), sy = pow2(ky);
 #pragma unroll 4
     for (int64_t k = blockIdx.x * (int64_t)kThreads + threadIdx.x; k < n8; k += step) {
@@ -541,7 +543,8 @@ int grid_for(int64_t threads, int most) {
 HalfMat pair_matrix(const __half* p, int64_t rows, int64_t cols) { return HalfMat{p, rows * cols, rows, cols, cols}; }
 
 cudaError_t backward_in_pieces(const HeadArgs& g, const Scratch& w, int K, cudaStream_t s) {
-    BT_KERNEL_LAUNCH((head_pairs_kernel), 148 * 8, kThreads, 0, s, g, (const RowParams*)w.rows, w);
+    const bool direct = head_direct_fits(g.N);
+    BT_KERNEL_LAUNCH((head_pairs_kernel), direct ? ((int)g.N + 7) / 8 : 148 * 8, kThreads, 0, s, g, (const RowParams*)w.rows, w);
     BT_COUNT_LAUNCH();
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
@@ -551,17 +554,19 @@ cudaError_t backward_in_pieces(const HeadArgs& g, const Scratch& w, int K, cudaS
     for (int v0 = 0; v0 < g.V; v0 += ldu) {
         const int cols = g.V - v0 < ldu ? g.V - v0 : ldu;
         const HalfMat wp{w.w16 + (int64_t)v0 * g.C, (int64_t)g.V * g.C, cols, g.C, g.C}, u{w.u16, g.N * ldu, g.N, cols, ldu};
-        e = launch_head_grad(x, wp, v0, w.rowf, w.rows, w.u16, ldu, u.plane, &w.head->err, s);
+        e = direct ? launch_head_direct_grad(g, x, v0, cols, w.rowf, w.rows, w.u16, ldu, u.plane, &w.head->err, s)
+                   : launch_head_grad(x, wp, v0, w.rowf, w.rows, w.u16, ldu, u.plane, &w.head->err, s);
         if (e == cudaSuccess && K) {
             BT_KERNEL_LAUNCH((head_pair_entries_kernel), grid_for(g.N * K, 148 * 8), 256, 0, s, g.N, K, (const int*)w.eid, (const float*)w.ep, v0,
                              cols, w.u16, (int64_t)ldu, u.plane);
             BT_COUNT_LAUNCH();
         }
-        if (e == cudaSuccess && dx) e = launch_head_dx(u, wp, w.rows, &w.scales->dx, v0 > 0, dx, w.partials, &w.head->err, s);
+        if (e == cudaSuccess && dx && direct) e = launch_head_direct_dx(g, u, v0, w.rows, v0 > 0, v0 + cols == g.V, w.partials, &w.head->err, s);
+        else if (e == cudaSuccess && dx) e = launch_head_dx(u, wp, w.rows, &w.scales->dx, v0 > 0, dx, w.partials, &w.head->err, s);
         if (e == cudaSuccess && g.dw) e = launch_head_dw(u, y, &w.scales->dw, g.dw + (int64_t)v0 * g.C, w.partials, &w.head->err, s);
         if (e != cudaSuccess) return e;
     }
-    if (g.dx_hi) {
+    if (g.dx_hi && !direct) {
         BT_KERNEL_LAUNCH((head_planes_kernel), grid_for(g.N * g.C / 4, 148 * 8), 256, 0, s, (const float*)dx, g.dx_hi, g.dx_lo, g.N * g.C / 4);
         BT_COUNT_LAUNCH();
     }
@@ -638,7 +643,7 @@ cudaError_t launch_head_bwd(const HeadArgs& g, cudaStream_t s) {
     const int K = g.aim.targets ? 0 : g.aim.K;
     bwd_layout(w, g.scratch, g.N, g.C, g.V, K, g.piece);
     const bool few = few_rows(g.N, g.C, g.V, true);
-    BT_KERNEL_LAUNCH((head_rows_kernel), row_ctas(g.N) + (few ? 0 : kParts), kFinishThreads, (size_t)(2 * K + id_places(K)) * 4, s, g, w.rows, w.eid, w.ep, w.wpart, w.ypart,
+    BT_KERNEL_LAUNCH((head_rows_kernel), row_ctas(g.N) + (w.wpart ? kParts : 0), kFinishThreads, (size_t)(2 * K + id_places(K)) * 4, s, g, w.rows, w.eid, w.ep, w.wpart, w.ypart,
                      w.head);
     BT_COUNT_LAUNCH();
     const cudaError_t e = cudaGetLastError();

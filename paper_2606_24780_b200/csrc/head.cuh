@@ -80,6 +80,11 @@ inline float head_growth(double n) { return (float)(1.0 + 0.5 * 0.56 / (1 << 24)
 bool head_direct_fits(int64_t N);
 int head_direct_strips(int V);
 cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float* rowf, float2* stats, int* err, cudaStream_t s);
+// The same of u (as launch_head_grad, for `cols` columns from v0 on), and dx = (+ dx) g_n u W from those columns, as planes too with the last.
+cudaError_t launch_head_direct_grad(const HeadArgs& h, const HalfMat& x, int v0, int cols, const float* rowf, const RowParams* rows, __half* u, int64_t ldu,
+                                    int64_t u_plane, int* err, cudaStream_t s);
+cudaError_t launch_head_direct_dx(const HeadArgs& h, const HalfMat& u, int v0, const RowParams* rows, bool onto, bool last, float* partials, int* err,
+                                  cudaStream_t s);
 
 // Logit of entry k of a row in units of the softened softmax, -inf where there is none (a weight of zero).  An id
 // behind the vocabulary counts as id 0 and is recorded.

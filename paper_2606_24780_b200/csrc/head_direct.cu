@@ -28,11 +28,20 @@ constexpr int kTileRows = 128, kGroup = 32, kBlock = 64, kMostX = 128;
 constexpr int kThreads = 512;
 constexpr int kRegsIssue = 40, kRegsPairs = 120, kRegsSums = 224;      // of the launch's 4 x 128
 
+// What becomes of the products of x and W (kStats, kGrad), and the product of u and W.
+enum Mode { kStats, kGrad, kDx };
+
 struct Args {
-    int N, V, groups, blocks, Nr;           // groups of 32 rows of W; Nr: rows of x, up to a multiple of 16
+    int N, C, V, groups, blocks, Nr;        // groups of 32 rows of W; Nr: rows of x, up to a multiple of 16
     int x_stages;
     const float* rowf;                      // [N]
-    float2* stats;                          // [N][4 CTAs]
+    float2* stats;                          // kStats: [N][4 CTAs]
+    const RowParams* rows;                  // kGrad
+    int v0;                                 // kGrad: first column of this piece
+    __half* u;                              // kGrad: [2][N][ldu]
+    long long u_plane, ldu;
+    int c_tiles, splits;                    // kDx: of 128 columns of W, and of the vocabulary
+    float* parts;                           // kDx: [splits][N][C]
     float grow;
     int* err;
 };
@@ -74,7 +83,7 @@ __device__ __forceinline__ float across(float (&v)[32], int lane) {
     return v[0];
 }
 
-template <bool PLANES>
+template <bool PLANES, int MODE>
 __global__ void __launch_bounds__(kThreads, 1)
 head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmGroup, const __grid_constant__ CUtensorMap tmX,
                    const Args g) {
@@ -96,10 +105,16 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     auto x_empty_bar = [&](int s) { return bars + 8u * (2 * C::kStages + 6 + kMostXStages + s); };
     const uint32_t tmem_slot = bars + 8u * (2 * C::kStages + 6 + 2 * kMostXStages);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    // the CTA's share of W, taken four groups at a time; the same number for all, where that takes more than once
-    const bool once = 4 * gridDim.x >= g.groups;
-    const int g0 = once ? 4 * blockIdx.x : (int)((int64_t)blockIdx.x * g.groups / gridDim.x);
-    const int g1 = once ? min(g.groups, g0 + 4) : (int)((blockIdx.x + 1LL) * g.groups / gridDim.x);
+    // The CTA's share of W: four groups in every complete round of all CTAs, and an even part of what is left, if there were any.
+    // kDx: one tile of columns, and every splits-th block of rows, from the end of W, which the call before has left in L2.
+    const int ctas = gridDim.x, full = g.groups / (4 * ctas), rest = g.groups - 4 * ctas * full;
+    const int r0 = full == 0 ? 4 * blockIdx.x : 4 * ctas * full + (int)((int64_t)blockIdx.x * rest / ctas);
+    const int r1 = full == 0 ? min(g.groups, r0 + 4) : 4 * ctas * full + (int)((blockIdx.x + 1LL) * rest / ctas);
+    const int c_tile = MODE == kDx ? (int)blockIdx.x % g.c_tiles : 0, split = MODE == kDx ? (int)blockIdx.x / g.c_tiles : 0;
+    const int passes = MODE == kDx ? 1 : full + (r1 > r0 ? 1 : 0), blocks = MODE == kDx ? (g.blocks - split + g.splits - 1) / g.splits : g.blocks;
+    auto first_of = [&](int p) { return MODE == kDx ? 0 : p < full ? 4 * ((int)blockIdx.x + p * ctas) : r0; };
+    auto groups_of = [&](int p) { return MODE == kDx ? min(4, (g.C - c_tile * kTileRows) / kGroup) : p < full ? 4 : r1 - r0; };
+    auto block_of = [&](int b) { return MODE == kDx ? g.blocks - 1 - split - b * g.splits : b; };
 
     if (threadIdx.x == 0) {
         prefetch_tensormap(&tmW);
@@ -139,13 +154,16 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         if ((warp == 0 || warp == 2) && lane == 0) {
             uint32_t it = 0, xs = 0, xp = 0;           // stage of x and how often it has come round
             bool ok = true;
-            for (int first = g0; first < g1 && ok; first += 4)
-                for (int b = 0; b < g.blocks; ++b, ++it) {
+            for (int p = 0; p < passes && ok; ++p)
+                for (int i = 0; i < blocks; ++i, ++it) {
+                    const int b = block_of(i);
                     if (warp == 0) {
-                        const int s = it % C::kStages, n = min(4, g1 - first);
+                        const int s = it % C::kStages, n = groups_of(p), first = first_of(p);
                         if (!mbar_wait(empty_bar(s), ((it / C::kStages) & 1u) ^ 1u, g.err, 41)) { ok = false; break; }
-                        mbar_expect_tx(full_bar(s), 2u * C::kForms * n * C::kBox);
-                        if (n == 4) {
+                        mbar_expect_tx(full_bar(s), MODE == kDx ? C::kW : 2u * C::kForms * n * C::kBox);
+                        if (MODE == kDx) {
+                            tma_load_3d(base + s * C::kW, &tmW, full_bar(s), c_tile * kTileRows, b * kBlock, 0);
+                        } else if (n == 4) {
                             tma_load_3d(base + s * C::kW, &tmW, full_bar(s), b * kBlock, first * kGroup, 0);
                             tma_load_3d(base + s * C::kW + C::kW / 2, &tmW, full_bar(s), b * kBlock + 32, first * kGroup, 0);
                         } else {
@@ -169,8 +187,8 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
             const uint32_t idesc = (1u << 4) | ((uint32_t)(g.Nr >> 3) << 17) | ((uint32_t)(kTileRows >> 4) << 24);
             uint32_t it = 0, xs = 0, xp = 0;
             bool ok = true;
-            for (int first = g0; first < g1 && ok; first += 4)
-                for (int b = 0; b < g.blocks; ++b, ++it) {
+            for (int p = 0; p < passes && ok; ++p)
+                for (int b = 0; b < blocks; ++b, ++it) {
                     const int a = it & 1;
                     if (!mbar_wait_warp(x_full_bar(xs), xp & 1u, g.err, 48) || !mbar_wait_warp(pairs_bar(a), (it >> 1) & 1u, g.err, 42)) { ok = false; break; }
                     tc_fence_after();
@@ -196,12 +214,13 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         const uint32_t t_row = t_pair(a) + ((uint32_t)(quad * 32) << 16);
         uint32_t it = 0;
         bool ok = true;
-        for (int first = g0; first < g1 && ok; first += 4)
-            for (int b = 0; b < g.blocks; ++b, ++it) {
+        for (int p = 0; p < passes && ok; ++p) {
+            const bool mine = quad < groups_of(p);
+            for (int b = 0; b < blocks; ++b, ++it) {
                 if ((int)(it & 1u) != a) continue;
                 const int s = it % C::kStages;
                 if (!mbar_wait_warp(full_bar(s), (it / C::kStages) & 1u, g.err, 43)) { ok = false; break; }
-                if (first + quad >= g1) {   // behind the share: these lanes' products are not looked at
+                if (!mine) {                // behind the share: these lanes' products are not looked at
                     if (!mbar_wait_warp(drained_bar(a), ((it >> 1) & 1u) ^ 1u, g.err, 44)) { ok = false; break; }
                     if (lane == 0) {
                         mbar_arrive(empty_bar(s));
@@ -209,10 +228,17 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                     }
                     continue;
                 }
-                // the 16-byte units of a row of 128 bytes lie swizzled by the row
                 float v[kBlock];
+                if (MODE == kDx) {          // a column of [64][128]
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                    for (int i = 0; i < kBlock; ++i) {
+                        const float* p = reinterpret_cast<const float*>(base_ptr + s * C::kW) + i * kTileRows + row;
+                        v[i] = PLANES ? p[0] + p[kBlock * kTileRows] : p[0];
+                    }
+                }
+                // the 16-byte units of a row of 128 bytes lie swizzled by the row
+#pragma unroll
+                for (int h = 0; MODE != kDx && h < 2; ++h)
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {
                         const uint8_t* p = base_ptr + s * C::kW + (4 * C::kForms * h + quad) * C::kBox + lane * 128 + ((q ^ (lane & 7)) << 4);
@@ -242,27 +268,38 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                 __syncwarp();
                 if (lane == 0) mbar_arrive(pairs_bar(a));
             }
+        }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSums));
         const int quad = warp & 3, row = quad * 32 + lane;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         float *const ref = refs + quad * kMostX, *const sum = refs + (4 + quad) * kMostX;     // over the tiles, in units of the reference
+        float* const row_l = refs;          // kGrad
+        int* const hit = reinterpret_cast<int*>(refs + kMostX);
         uint32_t it = 0;
         bool ok = true;
         for (int n = lane; n < kMostX; n += 32) {
-            if (quad == 0) row_f[n] = n < g.N ? g.rowf[n] * g.grow : 0.f;
-            ref[n] = -INFINITY;
-            sum[n] = 0.f;
+            if (MODE != kDx && quad == 0) row_f[n] = n < g.N ? g.rowf[n] * g.grow : 0.f;
+            if (MODE == kStats) {
+                ref[n] = -INFINITY;
+                sum[n] = 0.f;
+            }
+            if (MODE == kGrad && quad == 0) {
+                const RowParams r = n < g.N ? g.rows[n] : RowParams{INFINITY, 0.f, 0.f, -1};
+                row_l[n] = (r.L - 15.0f) + r.L_rest;           // see kGrad in head_tc.cu
+                hit[n] = r.target < 0 ? -1 : r.target - g.v0;
+            }
         }
         asm volatile("bar.sync 1, 128;" ::: "memory");         // these four warps
-        for (int first = g0; first < g1 && ok; first += 4) {
-            const bool mine = first + quad < g1;
+        for (int p = 0; p < passes && ok; ++p) {
+            const int first = first_of(p);
+            const bool mine = quad < groups_of(p);
             float z[4][32];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
 #pragma unroll
                 for (int j = 0; j < 32; ++j) z[q][j] = 0.f;
-            for (int b = 0; b < g.blocks; ++b, ++it) {
+            for (int b = 0; b < blocks; ++b, ++it) {
                 const int a = it & 1;
                 // the products are there, and the block's scales before them
                 if (!mbar_wait_warp(done_bar(a), (it >> 1) & 1u, g.err, 45) || !mbar_wait_warp(pairs_bar(a), (it >> 1) & 1u, g.err, 46)) { ok = false; break; }
@@ -289,7 +326,8 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
             }
             if (!ok) break;
             if (!mine) continue;
-            const bool there = (first + quad) * kGroup + lane < g.V;
+            const int v_at = (first + quad) * kGroup + lane;
+            const bool there = v_at < g.V;
             // through tensor memory, which takes an index: what follows is one piece of code for all 32 columns at a time (four
             // of them in line are fetched anew for every tile: 16 us of 79 at 100 rows, V 50,257, C 1,024)
 #pragma unroll
@@ -305,6 +343,52 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                 uint32_t zr[32];
                 tmem_ld32(tmem + 384u + lanes + q * 32u, zr);
                 tmem_ld_wait();
+                if (MODE == kDx) {
+                    float* dst = g.parts + ((long long)split * g.N + q * 32) * g.C + c_tile * kTileRows + row;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (q * 32 + j < g.N) dst[(long long)j * g.C] = __uint_as_float(zr[j]) * g.grow;
+                    continue;
+                }
+                if (MODE == kGrad) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        const float4 f = *reinterpret_cast<const float4*>(row_f + q * 32 + j), l = *reinterpret_cast<const float4*>(row_l + q * 32 + j);
+                        const int4 t = *reinterpret_cast<const int4*>(hit + q * 32 + j);
+                        const float fs[4] = {f.x, f.y, f.z, f.w}, ls[4] = {l.x, l.y, l.z, l.w};
+                        const int ts[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float e = ex2_fast(fmaf(__uint_as_float(zr[j + i]) * fs[i], 32768.0f, -ls[i]));
+                            if (ls[i] == INFINITY) e = 0.f;    // whatever the row holds
+                            if (ts[i] == v_at) e -= 32768.0f;
+                            const __half h = __float2half_rn(e), r = __float2half_rn(e - __half2float(h));
+                            zr[j + i] = (uint32_t)__half_as_ushort(h) | (uint32_t)__half_as_ushort(r) << 16;
+                        }
+                    }
+                    // four lanes trade their values of four rows for four columns of a row each: 8 bytes to a store, columns behind
+                    // the piece into the padding of u
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        uint32_t a[4];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t keep = lane & 2 ? zr[j + 2 + i] : zr[j + i], got = __shfl_xor_sync(0xffffffffu, lane & 2 ? zr[j + i] : zr[j + 2 + i], 2);
+                            a[i] = lane & 2 ? got : keep;              // columns 0, 1 (after the next step) ...
+                            a[2 + i] = lane & 2 ? keep : got;          // ... and 2, 3 of the lane's two rows
+                        }
+                        const uint32_t k0 = lane & 1 ? a[1] : a[0], k1 = lane & 1 ? a[3] : a[2];
+                        const uint32_t g0 = __shfl_xor_sync(0xffffffffu, lane & 1 ? a[0] : a[1], 1), g1 = __shfl_xor_sync(0xffffffffu, lane & 1 ? a[2] : a[3], 1);
+                        const uint32_t c0 = lane & 1 ? g0 : k0, c1 = lane & 1 ? k0 : g0, c2 = lane & 1 ? g1 : k1, c3 = lane & 1 ? k1 : g1;
+                        const int n = q * 32 + j + (lane & 3);
+                        __half* dst = g.u + n * g.ldu + (v_at & ~3);
+                        if (n < g.N) {
+                            *reinterpret_cast<uint2*>(dst) = make_uint2(__byte_perm(c0, c1, 0x5410), __byte_perm(c2, c3, 0x5410));
+                            *reinterpret_cast<uint2*>(dst + g.u_plane) = make_uint2(__byte_perm(c0, c1, 0x7632), __byte_perm(c2, c3, 0x7632));
+                        }
+                    }
+                    continue;
+                }
                 const int n = q * 32 + lane;
                 float v[32], most = -INFINITY;
 #pragma unroll
@@ -340,7 +424,7 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
             }
         }
         // a warp without rows of W has the sum zero
-        for (int n = lane; n < g.N; n += 32) g.stats[(long long)n * (4 * gridDim.x) + 4 * blockIdx.x + quad] = make_float2(ref[n], sum[n]);
+        for (int n = lane; MODE == kStats && n < g.N; n += 32) g.stats[(long long)n * (4 * gridDim.x) + 4 * blockIdx.x + quad] = make_float2(ref[n], sum[n]);
     }
 
     tc_fence_before();
@@ -348,19 +432,21 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
-template <bool PLANES>
-cudaError_t launch(const HeadArgs& h, const HalfMat& x, const Args& g, cudaStream_t s) {
+// kGrad and kDx: `rows` of W from row v0 on.
+template <bool PLANES, int MODE>
+cudaError_t launch(const HeadArgs& h, int v0, int rows, const HalfMat& x, int grid, const Args& g, cudaStream_t s) {
     using C = Cfg<PLANES>;
     if (!tensor_map_encoder()) return cudaErrorNotSupported;
     CUtensorMap tmW, tmGroup, tmX;
     const cuuint32_t one[3] = {1, 1, 1};
-    const cuuint64_t w_dims[3] = {(cuuint64_t)h.C, (cuuint64_t)h.V, PLANES ? 2u : 1u}, w_strides[2] = {(cuuint64_t)h.C * 4, (cuuint64_t)h.V * h.C * 4};
-    const cuuint32_t w_box[3] = {32, kTileRows, C::kForms}, group_box[3] = {32, kGroup, 1};
+    const cuuint64_t w_dims[3] = {(cuuint64_t)h.C, (cuuint64_t)rows, PLANES ? 2u : 1u}, w_strides[2] = {(cuuint64_t)h.C * 4, (cuuint64_t)h.V * h.C * 4};
+    const cuuint32_t w_box[3] = {MODE == kDx ? kTileRows : 32u, MODE == kDx ? kBlock : kTileRows, C::kForms}, group_box[3] = {32, kGroup, 1};
+    void* const w = (void*)(h.w + (int64_t)v0 * h.C);
     const cuuint64_t x_dims[3] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows, 2}, x_strides[2] = {(cuuint64_t)x.ld * 2, (cuuint64_t)x.plane * 2};
     const cuuint32_t x_box[3] = {kBlock, (cuuint32_t)g.Nr, 2};
-    if (tensor_map_encoder()(&tmW, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, (void*)h.w, w_dims, w_strides, w_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
-        tensor_map_encoder()(&tmGroup, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, (void*)h.w, w_dims, w_strides, group_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    if (tensor_map_encoder()(&tmW, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, w, w_dims, w_strides, w_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                             MODE == kDx ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
+        tensor_map_encoder()(&tmGroup, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, w, w_dims, w_strides, group_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
         tensor_map_encoder()(&tmX, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, (void*)x.hi, x_dims, x_strides, x_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
@@ -368,12 +454,49 @@ cudaError_t launch(const HeadArgs& h, const HalfMat& x, const Args& g, cudaStrea
     const uint32_t fit = (kSmemMost - C::kFixed) / x_bytes(g.Nr);
     Args a = g;
     a.x_stages = fit < (uint32_t)kMostXStages ? (int)fit : kMostXStages;       // two and more: 128 rows take 32 KB
-    const cudaError_t e = allow_smem<head_direct_kernel<PLANES>>(kSmemMost);
+    const cudaError_t e = allow_smem<head_direct_kernel<PLANES, MODE>>(kSmemMost);
     if (e != cudaSuccess) return e;
-    BT_KERNEL_LAUNCH((head_direct_kernel<PLANES>), head_direct_strips(h.V) / 4, kThreads, (size_t)(C::kFixed + a.x_stages * x_bytes(g.Nr)), s,
+    BT_KERNEL_LAUNCH((head_direct_kernel<PLANES, MODE>), grid, kThreads, (size_t)(C::kFixed + a.x_stages * x_bytes(g.Nr)), s,
                      tmW, tmGroup, tmX, a);
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
+}
+
+// dx of the rows from the splits' sums, 32 columns of four per CTA, an eighth of the splits to a warp.  The sums over earlier pieces
+// of the vocabulary lie where the result will be.
+__global__ void __launch_bounds__(256) head_direct_dx_kernel(const HeadArgs g, const RowParams* __restrict__ rows, int splits, const float* __restrict__ parts,
+                                                             bool onto, bool last) {
+    __shared__ float4 sm[8][32];
+    pdl_wait();
+    pdl_trigger();
+    const int C4 = g.C / 4, lane = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t i = blockIdx.x * 32LL + lane, n4 = g.N * C4;
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i < n4) {
+#pragma unroll 8
+        for (int k = y; k < splits; k += 8) t = add4(t, ld4(parts, k * n4 + i));
+    }
+    sm[y][lane] = t;
+    __syncthreads();
+    if (y > 0 || i >= n4) return;
+    for (int k = 1; k < 8; ++k) t = add4(t, sm[k][lane]);
+    const float rg = rows[i / C4].g;
+    t = rg == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(t.x * rg, t.y * rg, t.z * rg, t.w * rg);      // zero: the row has no part in the loss
+    float* const sums = g.dx ? g.dx : g.dx_hi;
+    if (onto) t = add4(t, ld4(sums, i));
+    if (last) store_raw_split(t, g.dx, g.dx_hi, g.dx_lo, i);
+    else reinterpret_cast<float4*>(sums)[i] = t;
+}
+
+Args args_for(const HeadArgs& h, int rows, int* err) {
+    Args g{};
+    g.N = (int)h.N; g.C = h.C; g.V = rows;
+    g.groups = (rows + kGroup - 1) / kGroup;
+    g.blocks = (h.C + kBlock - 1) / kBlock;
+    g.Nr = ((int)h.N + 15) / 16 * 16;
+    g.err = err;
+    g.grow = head_growth(3 * kBlock / 16);
+    return g;
 }
 
 }  // namespace
@@ -385,14 +508,34 @@ int head_direct_strips(int V) {
 }
 
 cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float* rowf, float2* stats, int* err, cudaStream_t s) {
-    Args g{};
-    g.N = (int)h.N; g.V = h.V;
-    g.groups = (h.V + kGroup - 1) / kGroup;
-    g.blocks = (h.C + kBlock - 1) / kBlock;
-    g.Nr = ((int)h.N + 15) / 16 * 16;
-    g.rowf = rowf; g.stats = stats; g.err = err;
-    g.grow = head_growth(3 * kBlock / 16);
-    return h.w_lo ? launch<true>(h, x, g, s) : launch<false>(h, x, g, s);
+    Args g = args_for(h, h.V, err);
+    g.rowf = rowf; g.stats = stats;
+    const int grid = head_direct_strips(h.V) / 4;
+    return h.w_lo ? launch<true, kStats>(h, 0, h.V, x, grid, g, s) : launch<false, kStats>(h, 0, h.V, x, grid, g, s);
+}
+
+cudaError_t launch_head_direct_grad(const HeadArgs& h, const HalfMat& x, int v0, int cols, const float* rowf, const RowParams* rows, __half* u, int64_t ldu,
+                                    int64_t u_plane, int* err, cudaStream_t s) {
+    Args g = args_for(h, cols, err);
+    g.rowf = rowf; g.rows = rows; g.v0 = v0; g.u = u; g.ldu = ldu; g.u_plane = u_plane;
+    const int grid = head_direct_strips(cols) / 4;
+    return h.w_lo ? launch<true, kGrad>(h, v0, cols, x, grid, g, s) : launch<false, kGrad>(h, v0, cols, x, grid, g, s);
+}
+
+cudaError_t launch_head_direct_dx(const HeadArgs& h, const HalfMat& u, int v0, const RowParams* rows, bool onto, bool last, float* partials, int* err,
+                                  cudaStream_t s) {
+    const int cols = (int)u.cols, sms = sm_count() < 148 ? sm_count() : 148;       // head_partial_bytes() counts on 148
+    Args g = args_for(h, cols, err);
+    g.blocks = (cols + kBlock - 1) / kBlock;
+    g.c_tiles = (h.C + kTileRows - 1) / kTileRows;
+    g.splits = sms / g.c_tiles < g.blocks ? sms / g.c_tiles : g.blocks;
+    g.parts = partials;
+    const int grid = g.c_tiles * g.splits;
+    const cudaError_t e = h.w_lo ? launch<true, kDx>(h, v0, cols, u, grid, g, s) : launch<false, kDx>(h, v0, cols, u, grid, g, s);
+    if (e != cudaSuccess) return e;
+    BT_KERNEL_LAUNCH((head_direct_dx_kernel), (unsigned)((h.N * h.C / 4 + 31) / 32), 256, 0, s, h, rows, g.splits, (const float*)partials, onto, last);
+    BT_COUNT_LAUNCH();
+    return cudaGetLastError();
 }
 
 }  // namespace bt
