@@ -68,6 +68,11 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, u
                  ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr));
+}
+
 // Maxima (MAX) or sums over the warp's lanes of 32 values per lane: lane l gets that of value l.
 template <bool MAX>
 __device__ __forceinline__ float across(float (&v)[32], int lane) {
@@ -338,23 +343,29 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                 if (q * 32 < g.N) tmem_st32(tmem + 384u + lanes + q * 32u, r);
             }
             tmem_st_wait();
+            if (MODE == kDx) {
+                float* dst = g.parts + (long long)split * g.N * g.C + c_tile * kTileRows + row;
 #pragma unroll 1
-            for (int q = 0; q * 32 < g.N; ++q) {
-                uint32_t zr[32];
-                tmem_ld32(tmem + 384u + lanes + q * 32u, zr);
-                tmem_ld_wait();
-                if (MODE == kDx) {
-                    float* dst = g.parts + ((long long)split * g.N + q * 32) * g.C + c_tile * kTileRows + row;
+                for (int n0 = 0; n0 < g.N; n0 += 8, dst += 8 * g.C) {
+                    uint32_t zr[8];
+                    tmem_ld8(tmem + 384u + lanes + n0, zr);
+                    tmem_ld_wait();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (q * 32 + j < g.N) dst[(long long)j * g.C] = __uint_as_float(zr[j]) * g.grow;
-                    continue;
+                    for (int j = 0; j < 8; ++j)
+                        if (n0 + j < g.N) dst[j * g.C] = __uint_as_float(zr[j]) * g.grow;
                 }
-                if (MODE == kGrad) {
+            }
+            if (MODE == kGrad) {
+                __half* dst = g.u + (lane & 3) * g.ldu + (v_at & ~3);
+#pragma unroll 1
+                for (int n0 = 0; n0 < g.N; n0 += 8, dst += 8 * g.ldu) {
+                    uint32_t zr[8];
+                    tmem_ld8(tmem + 384u + lanes + n0, zr);
+                    tmem_ld_wait();
 #pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        const float4 f = *reinterpret_cast<const float4*>(row_f + q * 32 + j), l = *reinterpret_cast<const float4*>(row_l + q * 32 + j);
-                        const int4 t = *reinterpret_cast<const int4*>(hit + q * 32 + j);
+                    for (int j = 0; j < 8; j += 4) {
+                        const float4 f = *reinterpret_cast<const float4*>(row_f + n0 + j), l = *reinterpret_cast<const float4*>(row_l + n0 + j);
+                        const int4 t = *reinterpret_cast<const int4*>(hit + n0 + j);
                         const float fs[4] = {f.x, f.y, f.z, f.w}, ls[4] = {l.x, l.y, l.z, l.w};
                         const int ts[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
@@ -369,7 +380,7 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                     // four lanes trade their values of four rows for four columns of a row each: 8 bytes to a store, columns behind
                     // the piece into the padding of u
 #pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
+                    for (int j = 0; j < 8; j += 4) {
                         uint32_t a[4];
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
@@ -380,15 +391,18 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                         const uint32_t k0 = lane & 1 ? a[1] : a[0], k1 = lane & 1 ? a[3] : a[2];
                         const uint32_t g0 = __shfl_xor_sync(0xffffffffu, lane & 1 ? a[0] : a[1], 1), g1 = __shfl_xor_sync(0xffffffffu, lane & 1 ? a[2] : a[3], 1);
                         const uint32_t c0 = lane & 1 ? g0 : k0, c1 = lane & 1 ? k0 : g0, c2 = lane & 1 ? g1 : k1, c3 = lane & 1 ? k1 : g1;
-                        const int n = q * 32 + j + (lane & 3);
-                        __half* dst = g.u + n * g.ldu + (v_at & ~3);
-                        if (n < g.N) {
-                            *reinterpret_cast<uint2*>(dst) = make_uint2(__byte_perm(c0, c1, 0x5410), __byte_perm(c2, c3, 0x5410));
-                            *reinterpret_cast<uint2*>(dst + g.u_plane) = make_uint2(__byte_perm(c0, c1, 0x7632), __byte_perm(c2, c3, 0x7632));
+                        if (n0 + j + (lane & 3) < g.N) {
+                            *reinterpret_cast<uint2*>(dst + j * g.ldu) = make_uint2(__byte_perm(c0, c1, 0x5410), __byte_perm(c2, c3, 0x5410));
+                            *reinterpret_cast<uint2*>(dst + j * g.ldu + g.u_plane) = make_uint2(__byte_perm(c0, c1, 0x7632), __byte_perm(c2, c3, 0x7632));
                         }
                     }
-                    continue;
                 }
+            }
+#pragma unroll 1
+            for (int q = 0; MODE == kStats && q * 32 < g.N; ++q) {
+                uint32_t zr[32];
+                tmem_ld32(tmem + 384u + lanes + q * 32u, zr);
+                tmem_ld_wait();
                 const int n = q * 32 + lane;
                 float v[32], most = -INFINITY;
 #pragma unroll
