@@ -8,9 +8,9 @@
 // g_n = inv_count w_n tau S_n.  The forward keeps one (maximum, sum) pair per row and strip of the vocabulary, joined
 // by head_finish_kernel, which also forms the few scores that the loss needs by themselves; the backward forms z again.
 //
-// Up to eight rows go through head_rows.cu in plain FP32, where the weights are read once; the forward of up to 128 through
-// head_direct.cu, where they are read once too and go to the tensor cores as pairs of FP16 numbers; more rows, and their
-// gradients, to head_tc.cu, after kernels here have made such pairs of all of x and W.
+// Up to eight rows go through head_rows.cu in plain FP32, where the weights are read once; up to 128 through head_direct.cu, where the
+// products with W (z, dx) read it as it is and make pairs of FP16 numbers on the way to the tensor cores; more rows to head_tc.cu,
+// after kernels here have made such pairs of all of x and W.  dW of more than eight rows is head_tc.cu's.
 #include <climits>
 
 #include "head.cuh"
@@ -50,10 +50,12 @@ struct Scratch {
     float* partials;
 };
 
-// Rows up to which the plain kernels are used: those of one pass over the weights.  V 50,257, C 768, raw: 8 rows 53 us, 9 in two
-// passes 90, 24 on the tensor cores 58.  The backward takes two passes where W is small, the second adding to dW (9 to 16 rows,
-// V 5,000, C 256: 38 to 41 us, on the tensor cores 61; V 23,670, C 320: 82 to 94 and 69).
-bool few_rows(int64_t N, int C, int V, bool back) { return N <= (back && (int64_t)V * C <= (1 << 22) ? 2 : 1) * kFewRows; }
+// Rows up to which the plain kernels are used, on the same inputs as the tensor cores from W as it is.  Forward: 3 rows against 50,257 x
+// 768 35 us and 40, 5 rows 44 and 40, but against 9,000 x 2,048, too few rows of W for a tile to every SM, 27 and 32.  Backward: as
+// long as one launch carries them (8 rows against 50,257 x 768 105 us and 122, against 5,000 x 4,096 in two launches 129 and 103).
+bool few_rows(int64_t N, int C, int V, bool back) {
+    return N <= kFewRows && (back ? N <= head_few_at_once(C) : N <= 4 || V < 148 * 128);
+}
 
 // Columns of one piece of the vocabulary, a multiple of 256: pieces of about the same size, of at most `piece` columns or
 // 512 MB of u.
@@ -83,7 +85,7 @@ enum Forward { kFew, kDirect, kPairs };
 Forward forward_of(int64_t N, int C, int V) { return few_rows(N, C, V, false) ? kFew : head_direct_fits(N) ? kDirect : kPairs; }
 int strips_of(int64_t N, int C, int V) {
     const Forward f = forward_of(N, C, V);
-    return f == kFew ? head_few_strips(N, C, V) : f == kDirect ? head_direct_strips(V) : head_stats_strips(N, C, V).count;
+    return f == kFew ? head_few_strips(N, C, V) : f == kDirect ? head_direct_strips(C, V) : head_stats_strips(N, C, V).count;
 }
 
 size_t fwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K) {
@@ -429,18 +431,17 @@ __global__ void __launch_bounds__(kThreads) head_row_pairs_kernel(const HeadArgs
     }
 }
 
-// Backward: W (where its pairs are made here) and y at one power of two each, since they are summed over their rows, the rows of x
-// each at its own.
+// Backward: W and y at one power of two each, since they are summed over their rows, the rows of x each at its own.
 __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, const RowParams* __restrict__ rows, const Scratch s) {
     __shared__ float smf[kThreads / 32];
     pdl_wait();
     pdl_trigger();
     float m = 0.f, my = 0.f;
-    for (int i = threadIdx.x; s.wpart && i < kParts; i += kThreads) m = fmaxf(m, s.wpart[i]);
+    for (int i = threadIdx.x; i < kParts; i += kThreads) m = fmaxf(m, s.wpart[i]);
     for (int i = threadIdx.x; i < row_ctas(g.N); i += kThreads) my = fmaxf(my, s.ypart[i]);
-    const int kw = s.wpart ? pair_exponent(block_all<kThreads>(m, smf, MaxOp())) : 0, ky = pair_exponent(block_all<kThreads>(my, smf, MaxOp()));
+    const int kw = pair_exponent(block_all<kThreads>(m, smf, MaxOp())), ky = pair_exponent(block_all<kThreads>(my, smf, MaxOp()));
     if (blockIdx.x == 0 && threadIdx.x == 0) *s.scales = Scales{ldexpf(1.0f, -15 - kw), ldexpf(1.0f, -15 - ky)};
-    const int64_t n8 = s.wpart ? (int64_t)g.V * g.C / 8 : 0, step = (int64_t)gridDim.x * kThreads;
+    const int64_t n8 = (int64_t)g.V * g.C / 8, step = (int64_t)gridDim.x * kThreads;
     const float sw = pow2(kw), sy = pow2(ky);
 #pragma unroll 4
     for (int64_t k = blockIdx.x * (int64_t)kThreads + threadIdx.x; k < n8; k += step) {
@@ -469,40 +470,99 @@ __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, 
     }
 }
 
-// A teacher's entries of a row by ascending column, those that are not there behind all columns, and where each strip's begin.
+// The same without W, a row per CTA.
+__global__ void __launch_bounds__(kThreads) head_pairs_of_rows_kernel(const HeadArgs g, const RowParams* __restrict__ rows, const Scratch s) {
+    constexpr int kHeld = 4;                // C4 is at most 1,024
+    __shared__ float smf[kThreads / 32];
+    pdl_wait();
+    pdl_trigger();
+    const int64_t row = blockIdx.x;
+    const int C4 = g.C / 4;
+    float4 t[kHeld];
+    float m = 0.f, my = 0.f;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        t[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (threadIdx.x + kThreads * i < C4) t[i] = ld_value(g.x, g.x_lo, row * C4 + threadIdx.x + kThreads * i);
+        m = max4(m, t[i]);
+    }
+    for (int i = threadIdx.x; i < row_ctas(g.N); i += kThreads) my = fmaxf(my, s.ypart[i]);
+    const int kx = pair_exponent(block_all<kThreads>(m, smf, MaxOp())), ky = pair_exponent(block_all<kThreads>(my, smf, MaxOp()));
+    const float sx = pow2(kx), sy = pow2(ky), gr = rows[row].g;
+    uint2 *const x = reinterpret_cast<uint2*>(s.x16) + row * C4, *const y = reinterpret_cast<uint2*>(s.y16) + row * C4;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        const int c = threadIdx.x + kThreads * i;
+        if (c >= C4) continue;
+        uint2 h, l;
+        pairs4(t[i], sx, h, l);
+        x[c] = h;
+        x[g.N * C4 + c] = l;
+        pairs4(make_float4(t[i].x * gr, t[i].y * gr, t[i].z * gr, t[i].w * gr), sy, h, l);
+        if (gr == 0.f) h = l = make_uint2(0u, 0u);              // whatever the row holds
+        y[c] = h;
+        y[g.N * C4 + c] = l;
+    }
+    if (threadIdx.x > 0) return;
+    s.rowf[row] = ldexpf(kLog2e / g.aim.tau, -kx);
+    if (row == 0) *s.scales = Scales{0.f, ldexpf(1.0f, -15 - ky)};
+}
+
+// A teacher's entries of a row by ascending column, those that are not there behind all columns, and where each strip's begin.  A CTA
+// sorts 512 entries at once, of several rows where they are shorter (3,740 rows of 101 one by one: 30 us).
+constexpr int kSorted = 512;
+__host__ __device__ inline int sorted_size(int K) {
+    int n = 1;
+    while (n < K) n *= 2;
+    return n;
+}
+// Rows of a CTA: no more than leave four CTAs to an SM, whose threads search for the strips' first entries afterwards.
+__host__ __device__ inline int rows_sorted(int64_t N, int K) {
+    int rows = 1;
+    while (2 * rows * sorted_size(K) <= kSorted && N / (2 * rows) >= 592) rows *= 2;
+    return rows;
+}
 __global__ void __launch_bounds__(kThreads) head_sort_kernel(const HeadArgs g, int2* entries, uint16_t* strip_first, HeadStrips strips) {
     __shared__ unsigned long long key[kMaxEntries];
     pdl_wait();
     pdl_trigger();
-    const int64_t row = blockIdx.x;
     const LossAim& a = g.aim;
-    int n = 1;
-    while (n < a.K) n *= 2;
-    for (int k = threadIdx.x; k < n; k += kThreads) {
+    const int n = sorted_size(a.K), rows = rows_sorted(g.N, a.K), all = n * rows;
+    const int64_t row0 = blockIdx.x * (int64_t)rows;
+    for (int i = threadIdx.x; i < all; i += kThreads) {
+        const int k = i & (n - 1);
+        const int64_t row = row0 + i / n;
         int id = -1;
-        if (k < a.K && entry_logit(a, row, k, g.V, g.bad, id) == -INFINITY) id = -1;
-        key[k] = ((unsigned long long)(id < 0 ? INT_MAX : id) << 32) | (unsigned)k;
+        if (k < a.K && row < g.N && entry_logit(a, row, k, g.V, g.bad, id) == -INFINITY) id = -1;
+        key[i] = ((unsigned long long)(id < 0 ? INT_MAX : id) << 32) | (unsigned)k;
     }
     for (int size = 2; size <= n; size *= 2)
         for (int d = size / 2; d > 0; d /= 2) {
             __syncthreads();
-            for (int i = threadIdx.x; i < n / 2; i += kThreads) {
-                const int lo = (i / d) * 2 * d + i % d, hi = lo + d;
+            for (int i = threadIdx.x; i < all / 2; i += kThreads) {
+                const int lo = 2 * i - (i & (d - 1)), hi = lo + d;
                 const unsigned long long x = key[lo], y = key[hi];
-                if ((x > y) == ((lo & size) == 0)) {
+                if ((x > y) == ((lo & (n - 1) & size) == 0)) {
                     key[lo] = y;
                     key[hi] = x;
                 }
             }
         }
     __syncthreads();
-    for (int k = threadIdx.x; k < a.K; k += kThreads) entries[row * a.K + k] = make_int2((int)(key[k] >> 32), (int)(unsigned)key[k]);
-    for (int t = threadIdx.x; t <= strips.count; t += kThreads) {
-        const unsigned long long from = (unsigned long long)t * strips.cols << 32;
+    for (int i = threadIdx.x; i < all; i += kThreads) {
+        const int k = i & (n - 1);
+        const int64_t row = row0 + i / n;
+        if (k < a.K && row < g.N) entries[row * a.K + k] = make_int2((int)(key[i] >> 32), (int)(unsigned)key[i]);
+    }
+    for (int i = threadIdx.x; i < rows * (strips.count + 1); i += kThreads) {
+        const int r = i / (strips.count + 1), t = i - r * (strips.count + 1);
+        const int64_t row = row0 + r;
+        if (row >= g.N) break;
+        const unsigned long long from = (unsigned long long)t * strips.cols << 32, *own = key + r * n;
         int lo = 0, left = a.K;             // the first entry from there on
         while (left > 0) {
             const int h = left / 2;
-            if (key[lo + h] < from) {
+            if (own[lo + h] < from) {
                 lo += h + 1;
                 left -= h + 1;
             } else {
@@ -544,7 +604,8 @@ HalfMat pair_matrix(const __half* p, int64_t rows, int64_t cols) { return HalfMa
 
 cudaError_t backward_in_pieces(const HeadArgs& g, const Scratch& w, int K, cudaStream_t s) {
     const bool direct = head_direct_fits(g.N);
-    BT_KERNEL_LAUNCH((head_pairs_kernel), direct ? ((int)g.N + 7) / 8 : 148 * 8, kThreads, 0, s, g, (const RowParams*)w.rows, w);
+    if (direct) BT_KERNEL_LAUNCH((head_pairs_of_rows_kernel), (unsigned)g.N, kThreads, 0, s, g, (const RowParams*)w.rows, w);
+    else BT_KERNEL_LAUNCH((head_pairs_kernel), 148 * 8, kThreads, 0, s, g, (const RowParams*)w.rows, w);
     BT_COUNT_LAUNCH();
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
@@ -618,7 +679,7 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     } else {
         e = launch_row_pairs(g, g.V, w, s);
         if (K) {
-            BT_KERNEL_LAUNCH((head_sort_kernel), (unsigned)g.N, kThreads, 0, s, g, w.entries, w.strip_first, head_stats_strips(g.N, g.C, g.V));
+            BT_KERNEL_LAUNCH((head_sort_kernel), (unsigned)((g.N + rows_sorted(g.N, K) - 1) / rows_sorted(g.N, K)), kThreads, 0, s, g, w.entries, w.strip_first, head_stats_strips(g.N, g.C, g.V));
             BT_COUNT_LAUNCH();
         }
         if (e == cudaSuccess)

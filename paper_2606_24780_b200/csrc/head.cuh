@@ -50,6 +50,7 @@ cudaError_t launch_head_dw(const HalfMat& u, const HalfMat& y, const float* scal
 // Few rows in plain FP32 (head_rows.cu): statistics [N][head_few_strips(N, C, V)]; gradients with a table [V][kFewRows] and parts
 // of dx [head_few_strips(N, C, V)][kFewRows][C] in scratch.
 constexpr int kFewRows = 8;                 // of x in one pass over the weights
+int head_few_at_once(int C);                // rows that one launch carries; the backward takes no more
 int head_few_strips(int64_t N, int C, int V);
 cudaError_t launch_head_few_stats(const HeadArgs& g, float2* stats, HeadHeader* head, cudaStream_t s);
 cudaError_t launch_head_few_grad(const HeadArgs& g, const RowParams* params, int K, const int* eid, const float* ep, float* aim, float* dx_part,
@@ -76,9 +77,9 @@ __device__ __forceinline__ void to_pairs(float a, float b, uint32_t& hi, uint32_
 // two sums in registers; the products are made longer by 0.56.
 inline float head_growth(double n) { return (float)(1.0 + 0.5 * 0.56 / (1 << 24) * n); }
 
-// Statistics of up to 128 rows straight from W (head_direct.cu): [N][head_direct_strips(V)].
+// Statistics of up to 128 rows straight from W (head_direct.cu): [N][head_direct_strips(C, V)].
 bool head_direct_fits(int64_t N);
-int head_direct_strips(int V);
+int head_direct_strips(int C, int V);
 cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float* rowf, float2* stats, int* err, cudaStream_t s);
 // The same of u (as launch_head_grad, for `cols` columns from v0 on), and dx = (+ dx) g_n u W from those columns, as planes too with the last.
 cudaError_t launch_head_direct_grad(const HeadArgs& h, const HalfMat& x, int v0, int cols, const float* rowf, const RowParams* rows, __half* u, int64_t ldu,

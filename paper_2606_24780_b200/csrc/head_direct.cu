@@ -28,12 +28,17 @@ constexpr int kTileRows = 128, kGroup = 32, kBlock = 64, kMostX = 128;
 constexpr int kThreads = 512;
 constexpr int kRegsIssue = 40, kRegsPairs = 120, kRegsSums = 224;      // of the launch's 4 x 128
 
+// W by boxes of one to four groups (boxes of one group alone, up to sixteen to a stage, take half as long again).
+struct WMaps {
+    CUtensorMap of[4];
+};
+
 // What becomes of the products of x and W (kStats, kGrad), and the product of u and W.
 enum Mode { kStats, kGrad, kDx };
 
 struct Args {
     int N, C, V, groups, blocks, Nr;        // groups of 32 rows of W; Nr: rows of x, up to a multiple of 16
-    int x_stages;
+    int x_stages, per;                      // groups of a CTA that has one pass over them
     const float* rowf;                      // [N]
     float2* stats;                          // kStats: [N][4 CTAs]
     const RowParams* rows;                  // kGrad
@@ -48,7 +53,7 @@ struct Args {
 
 template <bool PLANES>
 struct Cfg {
-    static constexpr uint32_t kForms = PLANES ? 2u : 1u, kBox = kGroup * 32u * 4u;       // a stage: [2 halves of the block][forms][4 groups] boxes
+    static constexpr uint32_t kForms = PLANES ? 2u : 1u, kBox = kGroup * 32u * 4u;       // a stage: [2 halves of the block][forms][groups]
     static constexpr uint32_t kW = 8u * kForms * kBox;
     static constexpr int kStages = PLANES ? 2 : 4;                      // of W; those of x are as many as fit
     static constexpr uint32_t kScales = (2u * kTileRows + kMostX + 8u * kMostX) * 4u;      // scales, rowf, references and sums of four warps
@@ -90,8 +95,7 @@ __device__ __forceinline__ float across(float (&v)[32], int lane) {
 
 template <bool PLANES, int MODE>
 __global__ void __launch_bounds__(kThreads, 1)
-head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmGroup, const __grid_constant__ CUtensorMap tmX,
-                   const Args g) {
+head_direct_kernel(const __grid_constant__ WMaps tmW, const __grid_constant__ CUtensorMap tmX, const Args g) {
     using C = Cfg<PLANES>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -112,9 +116,9 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // The CTA's share of W: four groups in every complete round of all CTAs, and an even part of what is left, if there were any.
     // kDx: one tile of columns, and every splits-th block of rows, from the end of W, which the call before has left in L2.
-    const int ctas = gridDim.x, full = g.groups / (4 * ctas), rest = g.groups - 4 * ctas * full;
-    const int r0 = full == 0 ? 4 * blockIdx.x : 4 * ctas * full + (int)((int64_t)blockIdx.x * rest / ctas);
-    const int r1 = full == 0 ? min(g.groups, r0 + 4) : 4 * ctas * full + (int)((blockIdx.x + 1LL) * rest / ctas);
+    const int ctas = gridDim.x, full = g.per < 4 ? 0 : g.groups / (4 * ctas), rest = g.groups - 4 * ctas * full;
+    const int r0 = full == 0 ? g.per * blockIdx.x : 4 * ctas * full + (int)((int64_t)blockIdx.x * rest / ctas);
+    const int r1 = full == 0 ? min(g.groups, r0 + g.per) : 4 * ctas * full + (int)((blockIdx.x + 1LL) * rest / ctas);
     const int c_tile = MODE == kDx ? (int)blockIdx.x % g.c_tiles : 0, split = MODE == kDx ? (int)blockIdx.x / g.c_tiles : 0;
     const int passes = MODE == kDx ? 1 : full + (r1 > r0 ? 1 : 0), blocks = MODE == kDx ? (g.blocks - split + g.splits - 1) / g.splits : g.blocks;
     auto first_of = [&](int p) { return MODE == kDx ? 0 : p < full ? 4 * ((int)blockIdx.x + p * ctas) : r0; };
@@ -122,8 +126,7 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     auto block_of = [&](int b) { return MODE == kDx ? g.blocks - 1 - split - b * g.splits : b; };
 
     if (threadIdx.x == 0) {
-        prefetch_tensormap(&tmW);
-        prefetch_tensormap(&tmGroup);
+        prefetch_tensormap(&tmW.of[MODE == kDx ? 0 : groups_of(0) - 1]);
         prefetch_tensormap(&tmX);
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(full_bar(s), 1);
@@ -166,16 +169,12 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                         const int s = it % C::kStages, n = groups_of(p), first = first_of(p);
                         if (!mbar_wait(empty_bar(s), ((it / C::kStages) & 1u) ^ 1u, g.err, 41)) { ok = false; break; }
                         mbar_expect_tx(full_bar(s), MODE == kDx ? C::kW : 2u * C::kForms * n * C::kBox);
+                        const CUtensorMap* tm = MODE == kDx ? &tmW.of[0] : &tmW.of[n - 1];
                         if (MODE == kDx) {
-                            tma_load_3d(base + s * C::kW, &tmW, full_bar(s), c_tile * kTileRows, b * kBlock, 0);
-                        } else if (n == 4) {
-                            tma_load_3d(base + s * C::kW, &tmW, full_bar(s), b * kBlock, first * kGroup, 0);
-                            tma_load_3d(base + s * C::kW + C::kW / 2, &tmW, full_bar(s), b * kBlock + 32, first * kGroup, 0);
+                            tma_load_3d(base + s * C::kW, tm, full_bar(s), c_tile * kTileRows, b * kBlock, 0);
                         } else {
-                            for (uint32_t i = 0; i < 2 * C::kForms; ++i)
-                                for (int k = 0; k < n; ++k)
-                                    tma_load_3d(base + s * C::kW + (4u * i + k) * C::kBox, &tmGroup, full_bar(s), b * kBlock + (int)(i / C::kForms) * 32,
-                                                (first + k) * kGroup, (int)(i % C::kForms));
+                            tma_load_3d(base + s * C::kW, tm, full_bar(s), b * kBlock, first * kGroup, 0);
+                            tma_load_3d(base + s * C::kW + C::kW / 2, tm, full_bar(s), b * kBlock + 32, first * kGroup, 0);
                         }
                     } else {
                         if (!mbar_wait(x_empty_bar(xs), (xp & 1u) ^ 1u, g.err, 47)) { ok = false; break; }
@@ -220,7 +219,8 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         uint32_t it = 0;
         bool ok = true;
         for (int p = 0; p < passes && ok; ++p) {
-            const bool mine = quad < groups_of(p);
+            const int groups = groups_of(p);
+            const bool mine = quad < groups;
             for (int b = 0; b < blocks; ++b, ++it) {
                 if ((int)(it & 1u) != a) continue;
                 const int s = it % C::kStages;
@@ -248,7 +248,7 @@ head_direct_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                     for (int q = 0; q < 8; ++q) {
                         const uint8_t* p = base_ptr + s * C::kW + (4 * C::kForms * h + quad) * C::kBox + lane * 128 + ((q ^ (lane & 7)) << 4);
                         float4 w = *reinterpret_cast<const float4*>(p);
-                        if (PLANES) w = add4(w, *reinterpret_cast<const float4*>(p + 4 * C::kBox));
+                        if (PLANES) w = add4(w, *reinterpret_cast<const float4*>(p + groups * C::kBox));
                         v[h * 32 + 4 * q] = w.x; v[h * 32 + 4 * q + 1] = w.y; v[h * 32 + 4 * q + 2] = w.z; v[h * 32 + 4 * q + 3] = w.w;
                     }
                 __syncwarp();
@@ -451,27 +451,28 @@ template <bool PLANES, int MODE>
 cudaError_t launch(const HeadArgs& h, int v0, int rows, const HalfMat& x, int grid, const Args& g, cudaStream_t s) {
     using C = Cfg<PLANES>;
     if (!tensor_map_encoder()) return cudaErrorNotSupported;
-    CUtensorMap tmW, tmGroup, tmX;
+    WMaps tmW;
+    CUtensorMap tmX;
     const cuuint32_t one[3] = {1, 1, 1};
     const cuuint64_t w_dims[3] = {(cuuint64_t)h.C, (cuuint64_t)rows, PLANES ? 2u : 1u}, w_strides[2] = {(cuuint64_t)h.C * 4, (cuuint64_t)h.V * h.C * 4};
-    const cuuint32_t w_box[3] = {MODE == kDx ? kTileRows : 32u, MODE == kDx ? kBlock : kTileRows, C::kForms}, group_box[3] = {32, kGroup, 1};
-    void* const w = (void*)(h.w + (int64_t)v0 * h.C);
-    const cuuint64_t x_dims[3] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows, 2}, x_strides[2] = {(cuuint64_t)x.ld * 2, (cuuint64_t)x.plane * 2};
     const cuuint32_t x_box[3] = {kBlock, (cuuint32_t)g.Nr, 2};
-    if (tensor_map_encoder()(&tmW, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, w, w_dims, w_strides, w_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                             MODE == kDx ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
-        tensor_map_encoder()(&tmGroup, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, w, w_dims, w_strides, group_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
-        tensor_map_encoder()(&tmX, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, (void*)x.hi, x_dims, x_strides, x_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return cudaErrorInvalidValue;
+    const cuuint64_t x_dims[3] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows, 2}, x_strides[2] = {(cuuint64_t)x.ld * 2, (cuuint64_t)x.plane * 2};
+    bool ok = tensor_map_encoder()(&tmX, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, (void*)x.hi, x_dims, x_strides, x_box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    for (int n = 1; ok && n <= (MODE == kDx ? 1 : 4); ++n) {
+        const cuuint32_t w_box[3] = {MODE == kDx ? (cuuint32_t)kTileRows : 32u, MODE == kDx ? (cuuint32_t)kBlock : (cuuint32_t)(n * kGroup), C::kForms};
+        ok = tensor_map_encoder()(&tmW.of[n - 1], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, (void*)(h.w + (int64_t)v0 * h.C), w_dims, w_strides, w_box, one,
+                                  CU_TENSOR_MAP_INTERLEAVE_NONE, MODE == kDx ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    }
+    if (!ok) return cudaErrorInvalidValue;
     const uint32_t fit = (kSmemMost - C::kFixed) / x_bytes(g.Nr);
     Args a = g;
     a.x_stages = fit < (uint32_t)kMostXStages ? (int)fit : kMostXStages;       // two and more: 128 rows take 32 KB
     const cudaError_t e = allow_smem<head_direct_kernel<PLANES, MODE>>(kSmemMost);
     if (e != cudaSuccess) return e;
     BT_KERNEL_LAUNCH((head_direct_kernel<PLANES, MODE>), grid, kThreads, (size_t)(C::kFixed + a.x_stages * x_bytes(g.Nr)), s,
-                     tmW, tmGroup, tmX, a);
+                     tmW, tmX, a);
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }
@@ -502,8 +503,23 @@ __global__ void __launch_bounds__(256) head_direct_dx_kernel(const HeadArgs g, c
     else reinterpret_cast<float4*>(sums)[i] = t;
 }
 
+// Four groups to a CTA, or fewer where that leaves SMs idle and a CTA keeps 64 KB of W: x has to come to every CTA, and the next
+// kernel starts earlier where SMs are free.  9 rows against planes of 3,000 x 2,048 35 us, four groups each 40; against 5,000 x 256
+// 14.5, on 148 SMs 17.0.
+struct Share {
+    int per, ctas;
+};
+Share share_of(int C, int rows) {
+    const int groups = (rows + kGroup - 1) / kGroup, sms = sm_count();
+    Share s{4, 0};
+    while (s.per > 1 && (groups + s.per / 2 - 1) / (s.per / 2) <= sms && s.per / 2 * kGroup * C * 4 >= 64 * 1024) s.per /= 2;
+    s.ctas = (groups + s.per - 1) / s.per < sms ? (groups + s.per - 1) / s.per : sms;
+    return s;
+}
+
 Args args_for(const HeadArgs& h, int rows, int* err) {
     Args g{};
+    g.per = share_of(h.C, rows).per;
     g.N = (int)h.N; g.C = h.C; g.V = rows;
     g.groups = (rows + kGroup - 1) / kGroup;
     g.blocks = (h.C + kBlock - 1) / kBlock;
@@ -516,15 +532,12 @@ Args args_for(const HeadArgs& h, int rows, int* err) {
 }  // namespace
 
 bool head_direct_fits(int64_t N) { return N <= kMostX; }
-int head_direct_strips(int V) {
-    const int tiles = (V + kTileRows - 1) / kTileRows, sms = sm_count();
-    return 4 * (tiles < sms ? tiles : sms);
-}
+int head_direct_strips(int C, int V) { return 4 * share_of(C, V).ctas; }
 
 cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float* rowf, float2* stats, int* err, cudaStream_t s) {
     Args g = args_for(h, h.V, err);
     g.rowf = rowf; g.stats = stats;
-    const int grid = head_direct_strips(h.V) / 4;
+    const int grid = share_of(h.C, h.V).ctas;
     return h.w_lo ? launch<true, kStats>(h, 0, h.V, x, grid, g, s) : launch<false, kStats>(h, 0, h.V, x, grid, g, s);
 }
 
@@ -532,7 +545,7 @@ cudaError_t launch_head_direct_grad(const HeadArgs& h, const HalfMat& x, int v0,
                                     int64_t u_plane, int* err, cudaStream_t s) {
     Args g = args_for(h, cols, err);
     g.rowf = rowf; g.rows = rows; g.v0 = v0; g.u = u; g.ldu = ldu; g.u_plane = u_plane;
-    const int grid = head_direct_strips(cols) / 4;
+    const int grid = share_of(h.C, cols).ctas;
     return h.w_lo ? launch<true, kGrad>(h, v0, cols, x, grid, g, s) : launch<false, kGrad>(h, v0, cols, x, grid, g, s);
 }
 

@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(ROWS, THREADS)) head_few_ker
                     const int c = t + a.G * k;
                     if (c >= C4) continue;
                     float4* out = reinterpret_cast<float4*>(g.dw) + (v0 + r) * C4 + c;
-                    stv(out, a.row0 ? addv(ldv(out), d[k]) : d[k]);
+                    stv(out, d[k]);
                 }
             }
         }
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(ROWS, THREADS)) head_few_ker
 }
 
 // dx of the rows from the CTAs' parts, 32 columns of four per CTA.
-__global__ void __launch_bounds__(256) head_few_dx_kernel(const HeadArgs g, int64_t row0, int parts, const float* __restrict__ dx_part) {
+__global__ void __launch_bounds__(256) head_few_dx_kernel(const HeadArgs g, int parts, const float* __restrict__ dx_part) {
     __shared__ float4 sm[8][32];
     pdl_wait();
     pdl_trigger();
@@ -262,19 +262,19 @@ __global__ void __launch_bounds__(256) head_few_dx_kernel(const HeadArgs g, int6
     __syncthreads();
     if (y == 0 && i < C4) {
         for (int k = 1; k < 8; ++k) t = add4(t, sm[k][lane]);
-        store_raw_split(t, g.dx, g.dx_hi, g.dx_lo, (row0 + n) * C4 + i);
+        store_raw_split(t, g.dx, g.dx_hi, g.dx_lo, (int64_t)n * C4 + i);
     }
 }
 
 // A teacher's entries as a dense table over the vocabulary, zero elsewhere.
-__global__ void __launch_bounds__(256) head_few_aim_kernel(int64_t row0, int rows, int K, const int* __restrict__ eid, const float* __restrict__ ep,
+__global__ void __launch_bounds__(256) head_few_aim_kernel(int rows, int K, const int* __restrict__ eid, const float* __restrict__ ep,
                                                            float* aim) {
     pdl_wait();
     pdl_trigger();
     const int i = blockIdx.x * 256 + threadIdx.x;
     if (i >= rows * K) return;
-    const int id = eid[row0 * K + i];
-    if (id >= 0) aim[(int64_t)id * kFewRows + i / K] = ep[row0 * K + i];
+    const int id = eid[i];
+    if (id >= 0) aim[(int64_t)id * kFewRows + i / K] = ep[i];
 }
 
 struct Shape {
@@ -323,6 +323,7 @@ int grid_of(const Shape& p, int V, int64_t rows) {
 
 }  // namespace
 
+int head_few_at_once(int C) { return rows_at_once(shape_of(C)); }
 int head_few_strips(int64_t N, int C, int V) { return grid_of(shape_of(C), V, N); }
 cudaError_t launch_head_few_stats(const HeadArgs& g, float2* stats, HeadHeader* head, cudaStream_t s) {
     const Shape p = shape_of(g.C);
@@ -341,25 +342,20 @@ cudaError_t launch_head_few_grad(const HeadArgs& g, const RowParams* params, int
                                  cudaStream_t s) {
     const Shape p = shape_of(g.C);
     const int grid = grid_of(p, g.V, g.N);
-    const bool want_dx = g.dx || g.dx_hi;
-    for (int64_t row0 = 0; row0 < g.N; row0 += rows_at_once(p)) {
-        Few a{};
-        a.rows = (int)(g.N - row0 < rows_at_once(p) ? g.N - row0 : rows_at_once(p));
-        a.G = p.G; a.row0 = row0; a.params = params; a.aim = K ? aim : nullptr; a.dx_part = want_dx ? dx_part : nullptr;
-        cudaError_t e;
-        if (K) {
-            e = cudaMemsetAsync(aim, 0, (size_t)g.V * kFewRows * sizeof(float), s);
-            if (e != cudaSuccess) return e;
-            BT_KERNEL_LAUNCH((head_few_aim_kernel), (a.rows * K + 255) / 256, 256, 0, s, row0, a.rows, K, eid, ep, aim);
-            BT_COUNT_LAUNCH();
-        }
-        e = g.w_lo ? launch_rows<true, true>(g, a, p, grid, s) : launch_rows<false, true>(g, a, p, grid, s);
+    Few a{};
+    a.rows = (int)g.N;
+    a.G = p.G; a.params = params; a.aim = K ? aim : nullptr; a.dx_part = g.dx || g.dx_hi ? dx_part : nullptr;
+    cudaError_t e;
+    if (K) {
+        e = cudaMemsetAsync(aim, 0, (size_t)g.V * kFewRows * sizeof(float), s);
         if (e != cudaSuccess) return e;
-        if (want_dx) {
-            BT_KERNEL_LAUNCH((head_few_dx_kernel), dim3((g.C / 4 + 31) / 32, a.rows), 256, 0, s, g, row0, grid, (const float*)dx_part);
-            BT_COUNT_LAUNCH();
-        }
+        BT_KERNEL_LAUNCH((head_few_aim_kernel), (a.rows * K + 255) / 256, 256, 0, s, a.rows, K, eid, ep, aim);
+        BT_COUNT_LAUNCH();
     }
+    e = g.w_lo ? launch_rows<true, true>(g, a, p, grid, s) : launch_rows<false, true>(g, a, p, grid, s);
+    if (e != cudaSuccess || !a.dx_part) return e;
+    BT_KERNEL_LAUNCH((head_few_dx_kernel), dim3((g.C / 4 + 31) / 32, a.rows), 256, 0, s, g, grid, (const float*)dx_part);
+    BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }
 

@@ -290,12 +290,13 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
             const int row0 = w.tm * kTileRows + (int)rank * BM + quad * 32, row = row0 + lane;
             const int col0 = w.tn * BN + part * kCols, cols = g.N - col0;      // cols may be below zero
             int e_at = 0, e_end = 0;
-            int2 entry = make_int2(0, 0);
+            int2 entry = make_int2(0, 0), next = entry;
             if (EPI == kStats && g.K && row < g.M) {
                 const uint16_t* f = g.strip_first + (long long)row * (kParts * g.tiles_n + 1) + kParts * w.tn + part;
                 e_at = f[0];
                 e_end = f[1];
                 if (e_at < e_end) entry = g.entries[(long long)row * g.K + e_at];
+                if (e_at + 1 < e_end) next = g.entries[(long long)row * g.K + e_at + 1];
             }
             RowParams rp{INFINITY, 0.f, 0.f, -1};
             float f = 0.f;
@@ -328,7 +329,15 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
             }
             if (!ok) break;
             if (EPI == kStats) {
-                // scores of the row's entries in this strip, the first of which is here already
+                if (cols > 0) {
+                    const float4* cf = reinterpret_cast<const float4*>(g.colf + col0);     // padded to a multiple of 256 columns
+#pragma unroll
+                    for (int j = 0; j < kCols / 4; ++j) {
+                        const float4 t = cf[j];
+                        v[4 * j] *= t.x * f; v[4 * j + 1] *= t.y * f; v[4 * j + 2] *= t.z * f; v[4 * j + 3] *= t.w * f;
+                    }
+                }
+                // scores of the row's entries in this strip, the first two of which are here already
                 while (__any_sync(0xffffffffu, e_at < e_end)) {
                     const int c = e_at < e_end ? entry.x - col0 : -1;
                     float z = 0.f;
@@ -340,17 +349,13 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
                             if (c == q * 16 + j) z = v[q * 16 + j];
                     }
                     if (e_at < e_end) {
-                        g.zk[(long long)row * g.K + entry.y] = z * (f * g.colf[entry.x]);
-                        if (++e_at < e_end) entry = g.entries[(long long)row * g.K + e_at];
+                        g.zk[(long long)row * g.K + entry.y] = z;
+                        ++e_at;
+                        entry = next;
+                        if (e_at + 1 < e_end) next = g.entries[(long long)row * g.K + e_at + 1];
                     }
                 }
                 if (row < g.M && cols > 0) {
-                    const float4* cf = reinterpret_cast<const float4*>(g.colf + col0);     // padded to a multiple of 256 columns
-#pragma unroll
-                    for (int j = 0; j < kCols / 4; ++j) {
-                        const float4 t = cf[j];
-                        v[4 * j] *= t.x * f; v[4 * j + 1] *= t.y * f; v[4 * j + 2] *= t.z * f; v[4 * j + 3] *= t.w * f;
-                    }
                     if (cols < kCols) {
 #pragma unroll
                         for (int j = 0; j < kCols; ++j)

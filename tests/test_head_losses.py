@@ -287,6 +287,15 @@ def test_distillation(N, C, V, K, tau, whole, planes):
 
 
 @gpu
+@pytest.mark.parametrize("N,C,V,K", [(5, 64, 19000, 0), (8, 256, 18944, 3), (7, 4096, 257, 0), (4, 4096, 300, 2), (8, 2080, 1000, 0), (9, 32, 40, 0), (9, 1024, 3001, 4),
+                                     (40, 96, 18945, 0), (100, 64, 18977, 5), (128, 160, 25000, 0), (127, 544, 9000, 7), (77, 2048, 3009, 0), (33, 4096, 999, 0)])
+@pytest.mark.parametrize("planes", [False, True])
+def test_few_and_some_dozens_of_rows(N, C, V, K, planes):
+    """Either side of where the kernels change, and shares of W of one to four groups of 32 rows."""
+    check(Case(N, C, V, K=K, tau=2.0 if K else 1.0, planes=planes, weights=True, pad=N // 9, seed=N + V))
+
+
+@gpu
 @pytest.mark.parametrize("N", [6, 12, 300])
 @pytest.mark.parametrize("K", [0, 9])
 def test_gradients_in_pieces_of_the_vocabulary(N, K):
