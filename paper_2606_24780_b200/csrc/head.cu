@@ -19,8 +19,15 @@ namespace bt {
 
 namespace {
 
-constexpr int kParts = 592;                 // CTAs that look for the largest of W
-__host__ __device__ constexpr int row_ctas(int64_t N) { return N < 1184 ? (int)N : 1184; }     // and those that look at the rows
+// The backward's look at the rows and at the largest of W, on CTAs of 256 threads; on 64 for rows of a teacher's entries that would not
+// all be under way at once.  All gradients of 6,545 rows of 64 values, V 7,270, with 53 entries 221 us, on 256 threads 268; of 5,320 rows
+// of 192 with targets, V 1,880, 111 on 256 and 126 on 64.
+__host__ __device__ constexpr int row_threads(int64_t N, int K) { return N <= 1184 || K == 0 ? 256 : 64; }
+__host__ __device__ constexpr int w_parts(int64_t N, int K) { return 592 * 256 / row_threads(N, K); }      // CTAs that look for the largest of W
+__host__ __device__ constexpr int row_ctas(int64_t N, int K) {                                              // and those that look at the rows
+    return N < 1184 * 256 / row_threads(N, K) ? (int)N : 1184 * 256 / row_threads(N, K);
+}
+__host__ __device__ inline int entries_of(const HeadArgs& g) { return g.aim.targets ? 0 : g.aim.K; }
 constexpr int kThreads = 256;
 constexpr int kFinishThreads = 256;
 
@@ -44,7 +51,7 @@ struct Scratch {
     float* dx_part;                         // [parts][kFewRows][C]
     // tensor cores
     Scales* scales;
-    float *wpart, *ypart;                   // [kParts], [row_ctas(N)] largest values
+    float *wpart, *ypart;                   // [w_parts(N, K)], [row_ctas(N, K)] largest values
     float* rowf;                            // [N]
     __half *x16, *y16, *w16, *u16;          // pairs: [2][N][C], [2][N][C], [2][V][C], [2][N][ldu]
     float* partials;
@@ -118,8 +125,8 @@ size_t bwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K, int
     }
     const bool direct = head_direct_fits(N);
     tc_layout(s, base, at, N, C, direct ? 0 : V);
-    if (!direct) s.wpart = take<float>(base, at, kParts);
-    s.ypart = take<float>(base, at, row_ctas(N));
+    if (!direct) s.wpart = take<float>(base, at, w_parts(N, K));
+    s.ypart = take<float>(base, at, row_ctas(N, K));
     s.y16 = take<__half>(base, at, 2 * (size_t)N * C);
     s.u16 = take<__half>(base, at, 2 * (size_t)N * piece_columns(N, V, piece));
     s.partials = take<float>(base, at, head_partial_bytes() / sizeof(float));
@@ -272,20 +279,21 @@ __device__ __forceinline__ float max4(float m, float4 v) {
 }
 
 // What the backward needs to know of the rows, one at a time per CTA, and the largest values of W and of y_nc = g_n x_nc.  Entries with the same id are joined into the first of them.
-__global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArgs g, RowParams* rows, int* eid, float* ep,
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) head_rows_kernel(const HeadArgs g, RowParams* rows, int* eid, float* ep,
                                                                    float* wpart, float* ypart, HeadHeader* head) {
     extern __shared__ int ids[];            // [K], then the weights [K] and id_places(K)
-    __shared__ float smf[kFinishThreads / 32];
+    __shared__ float smf[THREADS / 32];
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0 && threadIdx.x == 0) *head = HeadHeader{0, 0u};
-    const int w_ctas = wpart ? kParts : 0;
+    const int w_ctas = wpart ? w_parts(g.N, entries_of(g)) : 0;
     if ((int)blockIdx.x < w_ctas) {         // the largest of W, a part per CTA
-        const int64_t n4 = (int64_t)g.V * (g.C / 4), step = (int64_t)w_ctas * kFinishThreads;
+        const int64_t n4 = (int64_t)g.V * (g.C / 4), step = (int64_t)w_ctas * THREADS;
         float m = 0.f;
 #pragma unroll 8
-        for (int64_t i = blockIdx.x * (int64_t)kFinishThreads + threadIdx.x; i < n4; i += step) m = max4(m, ld4(g.w, i));
-        m = block_all<kFinishThreads>(m, smf, MaxOp());
+        for (int64_t i = blockIdx.x * (int64_t)THREADS + threadIdx.x; i < n4; i += step) m = max4(m, ld4(g.w, i));
+        m = block_all<THREADS>(m, smf, MaxOp());
         if (threadIdx.x == 0) wpart[blockIdx.x] = m;
         return;
     }
@@ -308,11 +316,11 @@ __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArg
             float* p = (float*)(ids + a.K);
             int* table = ids + 2 * a.K;
             const int places = id_places(a.K);
-            for (int k = threadIdx.x; k < places; k += kFinishThreads) table[k] = -1;
+            for (int k = threadIdx.x; k < places; k += THREADS) table[k] = -1;
             bool any, twice = false;
-            const float norm = teacher_norm<kFinishThreads>(a, row, g.V, nullptr, smf, any);
+            const float norm = teacher_norm<THREADS>(a, row, g.V, nullptr, smf, any);
             float sum = 0.f;
-            for (int k = threadIdx.x; k < a.K; k += kFinishThreads) {
+            for (int k = threadIdx.x; k < a.K; k += THREADS) {
                 int id = -1;
                 const float t = any ? entry_logit(a, row, k, g.V, nullptr, id) : -INFINITY;
                 p[k] = any ? expf(t - norm) : 0.f;
@@ -321,10 +329,10 @@ __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArg
                 sum += p[k];
             }
             twice = __syncthreads_or(twice);
-            sum = block_all<kFinishThreads>(sum, smf, SumOp());
+            sum = block_all<THREADS>(sum, smf, SumOp());
             live = live && sum != 0.f;
             r.g *= sum;
-            for (int k = threadIdx.x; k < a.K; k += kFinishThreads) {
+            for (int k = threadIdx.x; k < a.K; k += THREADS) {
                 const int id = ids[k];
                 bool first = live && id >= 0;
                 float w = twice ? 0.f : p[k];
@@ -346,8 +354,8 @@ __global__ void __launch_bounds__(kFinishThreads) head_rows_kernel(const HeadArg
         if (threadIdx.x == 0) rows[row] = r;
         if (ypart && live && r.g != 0.f) {      // the same for all threads
             float m = 0.f;
-            for (int c = threadIdx.x; c < g.C / 4; c += kFinishThreads) m = max4(m, ld4(g.x, row * (g.C / 4) + c));
-            ymax = fmaxf(ymax, fabsf(r.g) * block_all<kFinishThreads>(m, smf, MaxOp()));
+            for (int c = threadIdx.x; c < g.C / 4; c += THREADS) m = max4(m, ld4(g.x, row * (g.C / 4) + c));
+            ymax = fmaxf(ymax, fabsf(r.g) * block_all<THREADS>(m, smf, MaxOp()));
         }
         __syncthreads();                        // the entries in shared memory have been read
     }
@@ -437,8 +445,8 @@ __global__ void __launch_bounds__(kThreads) head_pairs_kernel(const HeadArgs g, 
     pdl_wait();
     pdl_trigger();
     float m = 0.f, my = 0.f;
-    for (int i = threadIdx.x; i < kParts; i += kThreads) m = fmaxf(m, s.wpart[i]);
-    for (int i = threadIdx.x; i < row_ctas(g.N); i += kThreads) my = fmaxf(my, s.ypart[i]);
+    for (int i = threadIdx.x; i < w_parts(g.N, entries_of(g)); i += kThreads) m = fmaxf(m, s.wpart[i]);
+    for (int i = threadIdx.x; i < row_ctas(g.N, entries_of(g)); i += kThreads) my = fmaxf(my, s.ypart[i]);
     const int kw = pair_exponent(block_all<kThreads>(m, smf, MaxOp())), ky = pair_exponent(block_all<kThreads>(my, smf, MaxOp()));
     if (blockIdx.x == 0 && threadIdx.x == 0) *s.scales = Scales{ldexpf(1.0f, -15 - kw), ldexpf(1.0f, -15 - ky)};
     const int64_t n8 = (int64_t)g.V * g.C / 8, step = (int64_t)gridDim.x * kThreads;
@@ -486,7 +494,7 @@ __global__ void __launch_bounds__(kThreads) head_pairs_of_rows_kernel(const Head
         if (threadIdx.x + kThreads * i < C4) t[i] = ld_value(g.x, g.x_lo, row * C4 + threadIdx.x + kThreads * i);
         m = max4(m, t[i]);
     }
-    for (int i = threadIdx.x; i < row_ctas(g.N); i += kThreads) my = fmaxf(my, s.ypart[i]);
+    for (int i = threadIdx.x; i < row_ctas(g.N, entries_of(g)); i += kThreads) my = fmaxf(my, s.ypart[i]);
     const int kx = pair_exponent(block_all<kThreads>(m, smf, MaxOp())), ky = pair_exponent(block_all<kThreads>(my, smf, MaxOp()));
     const float sx = pow2(kx), sy = pow2(ky), gr = rows[row].g;
     uint2 *const x = reinterpret_cast<uint2*>(s.x16) + row * C4, *const y = reinterpret_cast<uint2*>(s.y16) + row * C4;
@@ -665,7 +673,7 @@ cudaError_t launch_row_pairs(const HeadArgs& g, int64_t w_rows, const Scratch& w
 
 cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     Scratch w;
-    const int K = g.aim.targets ? 0 : g.aim.K;
+    const int K = entries_of(g);
     fwd_layout(w, g.scratch, g.N, g.C, g.V, K);
     const Forward f = forward_of(g.N, g.C, g.V);
     const int strips = strips_of(g.N, g.C, g.V);
@@ -701,11 +709,13 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
 
 cudaError_t launch_head_bwd(const HeadArgs& g, cudaStream_t s) {
     Scratch w;
-    const int K = g.aim.targets ? 0 : g.aim.K;
+    const int K = entries_of(g);
     bwd_layout(w, g.scratch, g.N, g.C, g.V, K, g.piece);
     const bool few = few_rows(g.N, g.C, g.V, true);
-    BT_KERNEL_LAUNCH((head_rows_kernel), row_ctas(g.N) + (w.wpart ? kParts : 0), kFinishThreads, (size_t)(2 * K + id_places(K)) * 4, s, g, w.rows, w.eid, w.ep, w.wpart, w.ypart,
-                     w.head);
+    const int ctas = row_ctas(g.N, K) + (w.wpart ? w_parts(g.N, K) : 0);
+    const size_t smem = (size_t)(2 * K + id_places(K)) * 4;
+    if (row_threads(g.N, K) == 64) BT_KERNEL_LAUNCH((head_rows_kernel<64>), ctas, 64, smem, s, g, w.rows, w.eid, w.ep, w.wpart, w.ypart, w.head);
+    else BT_KERNEL_LAUNCH((head_rows_kernel<256>), ctas, 256, smem, s, g, w.rows, w.eid, w.ep, w.wpart, w.ypart, w.head);
     BT_COUNT_LAUNCH();
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
