@@ -6,8 +6,8 @@
 // A CTA, or a cluster of up to eight with a slice of the columns each, walks over a row twice: once for its maximum and sum,
 // once for the gradient, and the second walk reads what the first has left in L2.  Holding the row in registers instead
 // (one read, the next row on its way into shared memory) leaves no room for a second and third CTA per SM, whose loads
-// run while this one reduces: 867 us against 681 at 8,192 x 50,257, where the copies alone take 502 (4.8 TB/s; what is left is the
-// latency of two walks).  The entries touch few columns: every
+// run while this one reduces: 867 us against 681 at 8,192 x 50,257, where the copies alone take 502 (now 665, 5.0 TB/s; what is left is
+// the latency of two walks).  The entries touch few columns: every
 // thread stores its columns of g tau S q, and behind a barrier the threads that own an entry store the columns of the aim
 // once more, from the logits that they have read before.
 #include <cooperative_groups.h>
@@ -246,7 +246,7 @@ cudaError_t launch_softmax_distill(const DistillArgs& g, cudaStream_t s) {
     cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     const int64_t n4 = g.ld / 4;
     // CTAs per row: more while SMs would be idle and a thread keeps a batch, and while the rows that are walked over at the
-    // same time (three CTAs per SM) would leave L2: 131,071 columns 129 us on pairs of CTAs, 149 with two CTAs per SM and longer batches
+    // same time (three CTAs per SM) would leave L2: 131,071 columns 123 us on pairs of CTAs, 149 with two CTAs per SM and longer batches
     int cs = 1;
     while (cs < 8 && ((g.N * cs * 2 <= 2 * sms && n4 > 512 * kBatch / 2 * cs) || 3 * sms / cs * n4 * 16 > ((int64_t)100 << 20))) cs *= 2;
     cudaError_t e;

@@ -1,14 +1,22 @@
-// The head's forward statistics for some dozens of rows of x: W goes through the SMs once, as it is, and becomes FP16 pairs on the way.
+// The head's products with W for some dozens of rows of x: W goes through the SMs as it is, and becomes FP16 pairs on the way.
+//
+//     kStats  z = x W^T, (maximum, sum of exponentials) over a CTA's share of the vocabulary
+//     kGrad   the same z, u = 2^15 (q - [v = target]) as pairs
+//     kDx     dx = u W, a range of the vocabulary each, joined by head_direct_dx_kernel
 //
 // With so few rows the weights' bytes bound the call, and a pass that makes pairs of W (read, written and read again) costs three times
-// as much.  Here a tile of 128 rows of W is the A operand of tcgen05.mma.kind::f16, in tensor memory, lane = row: a thread
-// takes 64 values of its own row out of shared memory, scales them by a power of two of their own, and stores the pairs.  The
-// same lanes hold the products, so the scale comes out again where the thread of the row adds the block to its sums in FP32.
+// as much.  Here a tile of W is the A operand of tcgen05.mma.kind::f16, in tensor memory: 128 rows of W by 64 columns, lane = row, or
+// for dx 128 columns by 64 rows, lane = column.  A thread takes the 64 values of its own lane out of shared memory, scales them by a
+// power of two of their own, and stores the pairs.  The same lanes hold the products, so the scale comes out again where the thread of
+// the lane adds the block to its sums in FP32.
 //
-//     warps 0, 2 (a lane) TMA: W tiles (FP32, raw or planes); the x tile's pairs
-//     warp 1 (one lane)   MMA: z^T += W x^T per 64 of the contraction index (l h' + h l' + h h')
+//     warps 0, 2 (a lane) TMA: W tiles (FP32, raw or planes); the pairs of x or u
+//     warp 1 (one lane)   MMA: += W x^T per 64 of the contraction index (l h' + h l' + h h')
 //     warps 4-7, 8-11     pairs of even and odd blocks
-//     warps 12-15         sums, then (maximum, sum of exponentials) over the warp's 32 rows of W for every row of x
+//     warps 12-15         sums, then the mode's last step
+//
+// W 50,257 x 1,024: statistics of 9 rows take 49 us, of 100 62 (all launches; 4.2 and 3.3 TB/s of W), gradients 156 and 196.  Few rows are bound by the
+// copies; with more, x comes to every SM as often as W and from L2, and a block's chain of copy, pairs, product and sum shows.
 //
 // W's ring has an even number of stages: a stage then always belongs to the same warps.  (Two groups that took turns on one
 // stage could take the fill that the other still waits for to be theirs: a parity tells neighbouring phases apart, not more.)
@@ -67,6 +75,9 @@ __device__ __forceinline__ bool elect_one() {
     uint32_t p;
     asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
     return p != 0;
+}
+__device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* tm, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(tm), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
@@ -151,6 +162,12 @@ head_direct_kernel(const __grid_constant__ WMaps tmW, const __grid_constant__ CU
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(base_ptr + (tmem_slot - base));
+    // the first of W on their way into L2 while the kernel before makes x's pairs (100 rows against 50,257 x 1,024: 73.6 us to 71.8, L2 cold)
+    if (MODE != kDx && threadIdx.x == 0)
+        for (int b = 0; b < min(g.blocks, 2 * C::kStages); ++b) {
+            tma_prefetch_3d(&tmW.of[groups_of(0) - 1], b * kBlock, first_of(0) * kGroup, 0);
+            if (b * kBlock + 32 < g.C) tma_prefetch_3d(&tmW.of[groups_of(0) - 1], b * kBlock + 32, first_of(0) * kGroup, 0);
+        }
     pdl_wait();
     pdl_trigger();
     // tensor memory: products 0-127 and 128-255, pairs (32 columns of h, 32 of l) from 256 and 320, a tile's sums from 384
@@ -333,8 +350,8 @@ head_direct_kernel(const __grid_constant__ WMaps tmW, const __grid_constant__ CU
             if (!mine) continue;
             const int v_at = (first + quad) * kGroup + lane;
             const bool there = v_at < g.V;
-            // through tensor memory, which takes an index: what follows is one piece of code for all 32 columns at a time (four
-            // of them in line are fetched anew for every tile: 16 us of 79 at 100 rows, V 50,257, C 1,024)
+            // through tensor memory, which takes an index: what follows is one small piece of code for a few columns at a time (all of
+            // them in line are fetched anew for every tile: 79 us against 70 for statistics of 100 rows, V 50,257, C 1,024)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 uint32_t r[32];
