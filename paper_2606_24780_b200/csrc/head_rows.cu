@@ -5,8 +5,8 @@
 // sums for dx and the current four rows of W are in registers.  The dot products are folded over a warp, sixteen of
 // them in sixteen shuffles, and over the group through shared memory.  Rows come in by asynchronous copies, sixteen values of
 // four ahead, into places that no other thread reads: what bounds the kernel is the copies' rate (HBM):
-// 31 us for one row against 50,257 x 768 (5.0 TB/s).  The gradients of five rows against 50,257 x 1,024 take 103, reading and
-// writing at 3.9 TB/s: two barriers per four rows of W, and registers for two CTAs to an SM.
+// 31 us for one row against 50,257 x 768 (5.0 TB/s).  The gradients of five rows against 50,257 x 1,024 take 100, reading and
+// writing at 4.1 TB/s: two barriers per four rows of W, and registers for two CTAs to an SM.
 #include "head.cuh"
 
 namespace bt {

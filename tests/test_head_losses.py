@@ -325,6 +325,39 @@ def test_outputs_asked_for_one_by_one(N):
 
 
 @gpu
+@pytest.mark.parametrize("N", [5, 40, 200])
+def test_planes_of_dx_alone_over_several_pieces(N):
+    """The sums over the pieces lie in the hi plane until the last."""
+    c = Case(N, 96, 1500, weights=True, pad=1)
+    lse = c.forward()[1]
+    dx = c.backward(lse, 256)[0]
+    ds = c.backward(lse, 256, dx=False, dw=False, dx_split=True)[2]
+    check_split(ds, dx.cpu().numpy())
+    both = c.backward(lse, 256, dx_split=True)
+    assert torch.equal(both[0], dx) and torch.equal(both[2], ds)
+
+
+@gpu
+@pytest.mark.parametrize("N,C,V", [(4, 96, 700), (40, 96, 19000), (40, 1024, 3001), (200, 64, 700)])
+@pytest.mark.parametrize("planes", [False, True])
+def test_arrays_on_multiples_of_sixteen_bytes(N, C, V, planes):
+    """Every array 16 bytes behind a multiple of 256."""
+    c = Case(N, C, V, planes=planes, weights=True)
+    want = c.forward()
+    grads = c.backward(want[1])[:2]
+    off = lambda t: None if t is None else torch.cat((torch.zeros(4, device=DEV, dtype=t.dtype), t.reshape(-1)))[4:].view(t.shape)  # noqa: E731
+    x, xs, w, ws = (off(t) for t in c.operands())
+    targets, rw, lse = off(c.targets), off(c.rw), off(want[1])
+    out = [torch.full((n + 4,), math.nan, device=DEV)[4:] for n in (N, N, 1)]
+    dx, dw = torch.full((N * C + 4,), math.nan, device=DEV)[4:].view(N, C), torch.full((V * C + 4,), math.nan, device=DEV)[4:].view(V, C)
+    work = torch.empty(max(b.bt_op_head_fwd_scratch_bytes(N, C, V), b.bt_op_head_bwd_scratch_bytes(N, C, V)), dtype=torch.uint8, device=DEV)
+    b.bt_op_head_xent_fwd(x, xs, w, ws, targets, rw, N, C, V, c.inv, *out, work, work.numel())
+    b.bt_op_head_xent_bwd(x, xs, w, ws, targets, rw, lse, N, C, V, c.inv, dx, dw, work, work.numel())
+    b.bt_op_head_check(work)
+    assert all(torch.equal(p, q) for p, q in zip((*out, dx, dw), (*want, *grads)))
+
+
+@gpu
 @pytest.mark.parametrize("N", [4, 40, 150])
 @pytest.mark.parametrize("K", [0, 5])
 def test_two_runs_give_the_same_bits(N, K):
