@@ -419,17 +419,85 @@ __device__ __forceinline__ int row_to_pairs(const float* v, const float* v_lo, i
     return k;
 }
 
+// A teacher's entries of a row by ascending column, those that are not there behind all columns, and where each strip's begin.  A CTA
+// sorts 512 entries at once, of several rows where they are shorter (3,740 rows of 101 one by one: 30 us).
+constexpr int kSorted = 512;
+__host__ __device__ inline int sorted_size(int K) {
+    int n = 1;
+    while (n < K) n *= 2;
+    return n;
+}
+// Rows of a CTA: no more than leave four CTAs to an SM, whose threads search for the strips' first entries afterwards.
+__host__ __device__ inline int rows_sorted(int64_t N, int K) {
+    int rows = 1;
+    while (2 * rows * sorted_size(K) <= kSorted && N / (2 * rows) >= 592) rows *= 2;
+    return rows;
+}
+__device__ __forceinline__ void sort_entries(const HeadArgs& g, int2* entries, uint16_t* strip_first, HeadStrips strips, unsigned long long* key) {
+    const LossAim& a = g.aim;
+    const int n = sorted_size(a.K), rows = rows_sorted(g.N, a.K), all = n * rows;
+    const int64_t row0 = blockIdx.x * (int64_t)rows;
+    for (int i = threadIdx.x; i < all; i += kThreads) {
+        const int k = i & (n - 1);
+        const int64_t row = row0 + i / n;
+        int id = -1;
+        if (k < a.K && row < g.N && entry_logit(a, row, k, g.V, g.bad, id) == -INFINITY) id = -1;
+        key[i] = ((unsigned long long)(id < 0 ? INT_MAX : id) << 32) | (unsigned)k;
+    }
+    for (int size = 2; size <= n; size *= 2)
+        for (int d = size / 2; d > 0; d /= 2) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < all / 2; i += kThreads) {
+                const int lo = 2 * i - (i & (d - 1)), hi = lo + d;
+                const unsigned long long x = key[lo], y = key[hi];
+                if ((x > y) == ((lo & (n - 1) & size) == 0)) {
+                    key[lo] = y;
+                    key[hi] = x;
+                }
+            }
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < all; i += kThreads) {
+        const int k = i & (n - 1);
+        const int64_t row = row0 + i / n;
+        if (k < a.K && row < g.N) entries[row * a.K + k] = make_int2((int)(key[i] >> 32), (int)(unsigned)key[i]);
+    }
+    for (int i = threadIdx.x; i < rows * (strips.count + 1); i += kThreads) {
+        const int r = i / (strips.count + 1), t = i - r * (strips.count + 1);
+        const int64_t row = row0 + r;
+        if (row >= g.N) break;
+        const unsigned long long from = (unsigned long long)t * strips.cols << 32, *own = key + r * n;
+        int lo = 0, left = a.K;             // the first entry from there on
+        while (left > 0) {
+            const int h = left / 2;
+            if (own[lo + h] < from) {
+                lo += h + 1;
+                left -= h + 1;
+            } else {
+                left = h;
+            }
+        }
+        strip_first[row * (strips.count + 1) + t] = (uint16_t)lo;
+    }
+}
+
 // Forward: the rows of W (the first w_rows) and x as pairs, each at its own power of two, which the epilogue takes out of its
-// column or row.  Planes of 16,384 + 2,048 rows of 768 take 39 us, 4.4 TB/s.
-template <int LANES>
-__global__ void __launch_bounds__(kThreads) head_row_pairs_kernel(const HeadArgs g, int64_t w_rows, const Scratch s) {
+// column or row; the first sort_ctas CTAs sort a teacher's entries meanwhile.  Planes of 16,384 + 2,048 rows of 768 take 39 us, 4.4 TB/s.
+template <int LANES, bool SORT>
+__global__ void __launch_bounds__(kThreads) head_row_pairs_kernel(const HeadArgs g, int64_t w_rows, const Scratch s, int sort_ctas,
+                                                                    const HeadStrips strips) {
+    __shared__ unsigned long long key[SORT ? kMaxEntries : 1];
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0 && threadIdx.x == 0) *s.head = HeadHeader{0, 0u};
+    if (SORT && (int)blockIdx.x < sort_ctas) {
+        sort_entries(g, s.entries, s.strip_first, strips, key);
+        return;
+    }
     const int C4 = g.C / 4;
     constexpr int kAtOnce = kThreads / LANES;
     // whole warps stay together: they share a base, and lanes whose row does not exist go along
-    for (int64_t base = blockIdx.x * (int64_t)kAtOnce; base < w_rows + g.N; base += gridDim.x * (int64_t)kAtOnce) {
+    for (int64_t base = (blockIdx.x - sort_ctas) * (int64_t)kAtOnce; base < w_rows + g.N; base += (gridDim.x - sort_ctas) * (int64_t)kAtOnce) {
         const int64_t at = base + threadIdx.x / LANES;
         const bool of_w = at < w_rows, there = at < w_rows + g.N;
         const int64_t row = of_w ? at : at - w_rows;
@@ -516,71 +584,6 @@ __global__ void __launch_bounds__(kThreads) head_pairs_of_rows_kernel(const Head
     if (row == 0) *s.scales = Scales{0.f, ldexpf(1.0f, -15 - ky)};
 }
 
-// A teacher's entries of a row by ascending column, those that are not there behind all columns, and where each strip's begin.  A CTA
-// sorts 512 entries at once, of several rows where they are shorter (3,740 rows of 101 one by one: 30 us).
-constexpr int kSorted = 512;
-__host__ __device__ inline int sorted_size(int K) {
-    int n = 1;
-    while (n < K) n *= 2;
-    return n;
-}
-// Rows of a CTA: no more than leave four CTAs to an SM, whose threads search for the strips' first entries afterwards.
-__host__ __device__ inline int rows_sorted(int64_t N, int K) {
-    int rows = 1;
-    while (2 * rows * sorted_size(K) <= kSorted && N / (2 * rows) >= 592) rows *= 2;
-    return rows;
-}
-__global__ void __launch_bounds__(kThreads) head_sort_kernel(const HeadArgs g, int2* entries, uint16_t* strip_first, HeadStrips strips) {
-    __shared__ unsigned long long key[kMaxEntries];
-    pdl_wait();
-    pdl_trigger();
-    const LossAim& a = g.aim;
-    const int n = sorted_size(a.K), rows = rows_sorted(g.N, a.K), all = n * rows;
-    const int64_t row0 = blockIdx.x * (int64_t)rows;
-    for (int i = threadIdx.x; i < all; i += kThreads) {
-        const int k = i & (n - 1);
-        const int64_t row = row0 + i / n;
-        int id = -1;
-        if (k < a.K && row < g.N && entry_logit(a, row, k, g.V, g.bad, id) == -INFINITY) id = -1;
-        key[i] = ((unsigned long long)(id < 0 ? INT_MAX : id) << 32) | (unsigned)k;
-    }
-    for (int size = 2; size <= n; size *= 2)
-        for (int d = size / 2; d > 0; d /= 2) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < all / 2; i += kThreads) {
-                const int lo = 2 * i - (i & (d - 1)), hi = lo + d;
-                const unsigned long long x = key[lo], y = key[hi];
-                if ((x > y) == ((lo & (n - 1) & size) == 0)) {
-                    key[lo] = y;
-                    key[hi] = x;
-                }
-            }
-        }
-    __syncthreads();
-    for (int i = threadIdx.x; i < all; i += kThreads) {
-        const int k = i & (n - 1);
-        const int64_t row = row0 + i / n;
-        if (k < a.K && row < g.N) entries[row * a.K + k] = make_int2((int)(key[i] >> 32), (int)(unsigned)key[i]);
-    }
-    for (int i = threadIdx.x; i < rows * (strips.count + 1); i += kThreads) {
-        const int r = i / (strips.count + 1), t = i - r * (strips.count + 1);
-        const int64_t row = row0 + r;
-        if (row >= g.N) break;
-        const unsigned long long from = (unsigned long long)t * strips.cols << 32, *own = key + r * n;
-        int lo = 0, left = a.K;             // the first entry from there on
-        while (left > 0) {
-            const int h = left / 2;
-            if (own[lo + h] < from) {
-                lo += h + 1;
-                left -= h + 1;
-            } else {
-                left = h;
-            }
-        }
-        strip_first[row * (strips.count + 1) + t] = (uint16_t)lo;
-    }
-}
-
 // The teacher's part of a piece of u.
 __global__ void __launch_bounds__(256) head_pair_entries_kernel(int64_t N, int K, const int* __restrict__ eid, const float* __restrict__ ep, int v0,
                                                                 int cols, __half* u, int64_t ldu, int64_t plane) {
@@ -658,15 +661,21 @@ size_t head_bwd_scratch_bytes(int64_t N, int C, int V, int K, int piece) {
 
 namespace {
 
-cudaError_t launch_row_pairs(const HeadArgs& g, int64_t w_rows, const Scratch& w, cudaStream_t s) {
-    // as few lanes to a row as hold it: many rows in flight
-    const int lanes = g.C <= 128 ? 4 : g.C <= 256 ? 8 : g.C <= 512 ? 16 : 32, grid = grid_for((w_rows + g.N) * lanes, 148 * 8);
-    if (lanes == 4) BT_KERNEL_LAUNCH((head_row_pairs_kernel<4>), grid, kThreads, 0, s, g, w_rows, w);
-    else if (lanes == 8) BT_KERNEL_LAUNCH((head_row_pairs_kernel<8>), grid, kThreads, 0, s, g, w_rows, w);
-    else if (lanes == 16) BT_KERNEL_LAUNCH((head_row_pairs_kernel<16>), grid, kThreads, 0, s, g, w_rows, w);
-    else BT_KERNEL_LAUNCH((head_row_pairs_kernel<32>), grid, kThreads, 0, s, g, w_rows, w);
+template <int LANES>
+cudaError_t launch_row_pairs_by(const HeadArgs& g, int64_t w_rows, const Scratch& w, int sort_ctas, cudaStream_t s) {
+    const int grid = sort_ctas + grid_for((w_rows + g.N) * LANES, 148 * 8);
+    // the sort's shared memory, where there is none, keeps the next kernel's CTAs off the SM: 3 us
+    if (sort_ctas) BT_KERNEL_LAUNCH((head_row_pairs_kernel<LANES, true>), grid, kThreads, 0, s, g, w_rows, w, sort_ctas, head_stats_strips(g.N, g.C, g.V));
+    else BT_KERNEL_LAUNCH((head_row_pairs_kernel<LANES, false>), grid, kThreads, 0, s, g, w_rows, w, 0, HeadStrips{});
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
+}
+// As few lanes to a row as hold it: many rows in flight.
+cudaError_t launch_row_pairs(const HeadArgs& g, int64_t w_rows, const Scratch& w, int sort_ctas, cudaStream_t s) {
+    return g.C <= 128   ? launch_row_pairs_by<4>(g, w_rows, w, sort_ctas, s)
+           : g.C <= 256 ? launch_row_pairs_by<8>(g, w_rows, w, sort_ctas, s)
+           : g.C <= 512 ? launch_row_pairs_by<16>(g, w_rows, w, sort_ctas, s)
+                        : launch_row_pairs_by<32>(g, w_rows, w, sort_ctas, s);
 }
 
 }  // namespace
@@ -682,14 +691,10 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     if (f == kFew) {
         e = launch_head_few_stats(g, w.stats, w.head, s);
     } else if (f == kDirect) {
-        e = launch_row_pairs(g, 0, w, s);
+        e = launch_row_pairs(g, 0, w, 0, s);
         if (e == cudaSuccess) e = launch_head_direct(g, x, w.rowf, w.stats, &w.head->err, s);
     } else {
-        e = launch_row_pairs(g, g.V, w, s);
-        if (K) {
-            BT_KERNEL_LAUNCH((head_sort_kernel), (unsigned)((g.N + rows_sorted(g.N, K) - 1) / rows_sorted(g.N, K)), kThreads, 0, s, g, w.entries, w.strip_first, head_stats_strips(g.N, g.C, g.V));
-            BT_COUNT_LAUNCH();
-        }
+        e = launch_row_pairs(g, g.V, w, K ? (int)((g.N + rows_sorted(g.N, K) - 1) / rows_sorted(g.N, K)) : 0, s);
         if (e == cudaSuccess)
             e = launch_head_stats(x, pair_matrix(w.w16, g.V, g.C), w.rowf, w.colf, K, w.entries, w.strip_first, w.zk, w.stats, &w.head->err, s);
     }
