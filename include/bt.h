@@ -648,7 +648,7 @@ BT_API bt_status bt_op_dropout_bwd(const float* dy, int64_t n, double p, uint64_
  * largest one lies near FP16's largest.  Values below 2^-18 of the largest lose bits, at an absolute 2^-40 of it.  That is the
  * largest of x's or W's row in the forward, and in the backward that of x's row, of g_n x_n over all rows, and of all of W
  * (of fewer of its values up to 128 rows).
- * Up to eight rows run in plain FP32.  x of rows that count, and W, must be finite; a row whose scores are
+ * Calls of up to four rows, and some of up to eight, run in plain FP32.  x of rows that count, and W, must be finite; a row whose scores are
  * beyond FP32 is not a number in losses and lse.
  * C a multiple of 32, at most 4096; V and N at most 2^24.  N = 0 is nothing to do (loss_mean and dw become 0).
  * scratch: device, 256-byte aligned, of the stated size (K = 0), contents irrelevant on entry; calls that may

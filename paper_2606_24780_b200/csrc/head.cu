@@ -8,7 +8,7 @@
 // g_n = inv_count w_n tau S_n.  The forward keeps one (maximum, sum) pair per row and strip of the vocabulary, joined
 // by head_finish_kernel, which also forms the few scores that the loss needs by themselves; the backward forms z again.
 //
-// Up to eight rows go through head_rows.cu in plain FP32, where the weights are read once; up to 128 through head_direct.cu, where the
+// Up to four rows, or eight (see few_rows), go through head_rows.cu in plain FP32, where the weights are read once; up to 128 through head_direct.cu, where the
 // products with W (z, dx) read it as it is and make pairs of FP16 numbers on the way to the tensor cores; more rows to head_tc.cu,
 // after kernels here have made such pairs of all of x and W.  dW of more than eight rows is head_tc.cu's.
 #include <climits>
