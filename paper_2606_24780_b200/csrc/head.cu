@@ -174,7 +174,8 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_kernel(const HeadA
     for (int k = warp; any && k < g.aim.K; k += kFinishThreads / 32) {
         int id;
         const float lp = entry_logit(g.aim, row, k, g.V, nullptr, id) - norm, p = expf(lp);
-        if (p != 0.f) t += p * (lp + (lse - score(id)));    // NaN is not zero: such a row has no finite loss
+        // NaN is not zero: such a row has no finite loss.  Where the norm is NaN, so is p of an entry that is not there
+        if (id >= 0 && p != 0.f) t += p * (lp + (lse - score(id)));
     }
     loss = block_all<kFinishThreads>(lane == 0 ? t : 0.f, smf, SumOp()) * (g.aim.tau * g.aim.tau);
     if (threadIdx.x == 0) {

@@ -1,0 +1,60 @@
+"""The losses at the language-model head, and distillation on logits, where they could give way: teachers whose numbers are not
+finite beside entries that are not there."""
+import math
+
+import pytest
+import torch
+
+from gpu_util import DEV
+from test_head_losses import Case, logits_case, logits_run
+
+gpu = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------- GPU: teachers that are not finite
+
+def spoil(c, kind, row):
+    """A row whose teacher has no finite normaliser, between entries that are not there (far below zero, and by a logit of -inf)."""
+    c.ids[row, 1], c.ids[row, 3] = -100, -(1 << 31)
+    c.top[row, 0] = 1.0
+    c.top[row, 4] = -math.inf
+    if kind.startswith("lse"):
+        c.top_lse[row] = float(kind[4:])
+    else:
+        c.top[row, 2] = {"nan": math.nan, "inf": math.inf, "overflow": torch.finfo(torch.float32).max}[kind]
+
+
+@gpu
+@pytest.mark.parametrize("N", [4, 40, 150])
+@pytest.mark.parametrize("kind", ["nan", "inf", "overflow", "lse nan", "lse -inf"])
+def test_a_teacher_that_is_not_finite_stays_in_its_row(N, kind):
+    """"overflow": the logit is finite and leaves FP32 when it is divided by the temperature."""
+    make = lambda: Case(N, 64, 900, K=6, tau=0.5, whole=kind.startswith("lse"), weights=True)  # noqa: E731
+    c, plain = make(), make()
+    # a row of weight 1, whose other entries are whole in both
+    row = 3
+    for k in (c, plain):
+        k.ids[row] = torch.arange(6, dtype=torch.int32, device=DEV) * 7
+    spoil(c, kind, row)
+    want, got = plain.forward(), c.forward()
+    keep = [i for i in range(N) if i != row]
+    assert not torch.isfinite(got[0][row]) and not torch.isfinite(got[2][0])
+    assert torch.equal(got[0][keep], want[0][keep]) and torch.equal(got[1], want[1])
+    dx = c.backward(got[1], dw=False)[0]
+    assert not torch.isfinite(dx[row]).any() and torch.equal(dx[keep], plain.backward(want[1], dw=False)[0][keep])
+
+
+@gpu
+@pytest.mark.parametrize("N,V", [(6, 900), (300, 900), (6, 50257)])
+@pytest.mark.parametrize("kind", ["nan", "inf", "overflow", "lse nan", "lse -inf"])
+def test_a_teacher_that_is_not_finite_stays_in_its_row_of_logits(N, V, kind):
+    make = lambda: logits_case(N, V, 6, 0.5, kind.startswith("lse"), pad=0)  # noqa: E731
+    c, plain = make(), make()
+    row = 3
+    for k in (c, plain):
+        k.ids[row] = torch.arange(6, dtype=torch.int32, device=DEV) * 7
+    spoil(c, kind, row)
+    want, got = logits_run(plain), logits_run(c)
+    keep = [i for i in range(N) if i != row]
+    assert not torch.isfinite(got[0][row]) and not torch.isfinite(got[1][0])
+    assert torch.equal(got[0][keep], want[0][keep]) and torch.equal(got[2][keep], want[2][keep])
