@@ -66,6 +66,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const 
     __shared__ Four sm[2][THREADS / 32], all[2][CS];
     __shared__ Entries en;
     extern __shared__ int table[];                                  // [places]
+    if (CS > 1) cg::this_cluster().barrier_arrive();                // waited for before the first store into another CTA's memory
     pdl_wait();
     pdl_trigger();
     const LossAim& a = g.aim;
@@ -120,6 +121,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const 
         m.a = top;
     }
     const float mine = m.a;
+    if (CS > 1) cg::this_cluster().barrier_wait();                  // every CTA of the cluster has started, however short its slice
     m = row_all<THREADS, CS, true>(m, sm[0], all[0]);
     if (mine != m.a && s != 0.f) s *= ex2_fast((mine - m.a) * f);
     const bool any = m.c != 0.f;

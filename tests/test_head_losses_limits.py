@@ -1,12 +1,12 @@
 """The losses at the language-model head, and distillation on logits, where they could give way: teachers whose numbers are not
-finite beside entries that are not there."""
+finite beside entries that are not there; rows of which most CTAs have nothing."""
 import math
 
 import pytest
 import torch
 
 from gpu_util import DEV
-from test_head_losses import Case, logits_case, logits_run
+from test_head_losses import Case, logits_case, logits_run, logits_want
 
 gpu = pytest.mark.gpu
 
@@ -58,3 +58,21 @@ def test_a_teacher_that_is_not_finite_stays_in_its_row_of_logits(N, V, kind):
     keep = [i for i in range(N) if i != row]
     assert not torch.isfinite(got[0][row]) and not torch.isfinite(got[1][0])
     assert torch.equal(got[0][keep], want[0][keep]) and torch.equal(got[2][keep], want[2][keep])
+
+
+# ------------------------------------------------------------------------------- GPU: slices of a row on a cluster
+
+@gpu
+@pytest.mark.parametrize("N,V,ld", [(1, 5, 20000), (30, 3, 20480), (37, 2500, 40004), (74, 1, 8300), (148, 9, 16400), (3, 16390, 17000), (2, 1, 1 << 20)])
+def test_rows_whose_vocabulary_ends_in_the_first_slices(N, V, ld):
+    """CTAs of a cluster that have no column to read are done with their part of the row long before the others: clusters of
+    two, four and eight, several times over."""
+    c = logits_case(N, V, 5, 1.5, False, pad=N // 6, seed=ld, ld=ld)
+    c.z[:, V:] = math.nan
+    losses, mean, d = logits_want(c)
+    top = max(1.0, float(c.z[:, :V].abs().max()) / 1.5)           # as test_distillation_on_logits
+    for _ in range(5):
+        got = logits_run(c)
+        assert float((got[0] - losses).abs().max()) < 2e-6 * 1.5 ** 2 * top * 2
+        assert abs(float(got[1][0]) - float(mean)) < 4e-6 * 1.5 ** 2 * top
+        assert float((got[2] - d).norm()) < 2e-6 * top * c.inv * 1.5 * 2 * float(c.weight().norm()) and not got[2][:, V:].any()
