@@ -42,7 +42,7 @@ struct Scratch {
     float* colf;                            // forward, tensor cores: [V] up to a multiple of 256
     int2* entries;                          // [N][K]
     uint16_t* strip_first;                  // [N][strips + 1]
-    float* zk;                              // [N][K]
+    float* zk;                              // [N] scores of the targets, or [N][K] of a teacher's entries
     RowParams* rows;                        // backward: [N]
     int* eid;                               // [N][K] columns of the aim, each once; below zero: none
     float* ep;                              // [N][K] its weights there
@@ -101,12 +101,12 @@ size_t fwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K) {
     s = Scratch{};
     s.head = (HeadHeader*)base;
     s.stats = take<float2>(base, at, (size_t)N * strips_of(N, C, V));
+    s.zk = take<float>(base, at, (size_t)N * (K ? K : 1));
     if (f == kFew) return at;
     tc_layout(s, base, at, N, C, f == kDirect ? 0 : V);
     if (f == kDirect) return at;
     s.colf = take<float>(base, at, (V + 255) / 256 * 256);
     s.entries = take<int2>(base, at, (size_t)N * K);
-    s.zk = take<float>(base, at, (size_t)N * K);
     if (K) s.strip_first = take<uint16_t>(base, at, (size_t)N * (head_stats_strips(N, C, V).count + 1));
     return at;
 }
@@ -185,9 +185,19 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_kernel(const HeadA
     if (g.loss_mean) mean_by_last<kFinishThreads>(g.aim, g.losses, g.N, &head->rows_done, gridDim.x, g.loss_mean, smd);
 }
 
-// log sum exp of a row from its strips, by one warp or all (WARPS) of a CTA.
+// The sum of a row's exponentials: 2^m s.
+struct RowSum {
+    float m, s;
+};
+__device__ __forceinline__ float lse_of(RowSum r) { return (r.m + log2f(r.s)) * kLn2; }
+// How far log sum exp lies above a score z (in units of log 2) that is part of the sum.  m is such a score too, and s the sum beside it:
+// where z is the largest, m - z is an exact zero and s a number from 1 on.  The straight path's m may lie below the largest score, by 20 at
+// most; the sum is then formed beside z.
+__device__ __forceinline__ float above_score(RowSum r, float z) { return (z > r.m ? log2f(r.s * ex2_fast(r.m - z)) : r.m - z + log2f(r.s)) * kLn2; }
+
+// A row's sum from its strips, by one warp or all (WARPS) of a CTA.
 template <int WARPS>
-__device__ __forceinline__ float row_lse(const float2* st, int strips, float* sm) {
+__device__ __forceinline__ RowSum row_sum(const float2* st, int strips, float* sm) {
     float m = -INFINITY, s = 0.f;
 #pragma unroll 4
     for (int i = WARPS == 1 ? threadIdx.x & 31 : threadIdx.x; i < strips; i += 32 * WARPS) {
@@ -199,14 +209,14 @@ __device__ __forceinline__ float row_lse(const float2* st, int strips, float* sm
         }
     }
     const float top = WARPS == 1 ? warp_max(m) : block_all<32 * WARPS>(m, sm, MaxOp()), t = s != 0.f ? s * ex2_fast(m - top) : 0.f;
-    return (top + log2f(WARPS == 1 ? warp_sum(t) : block_all<32 * WARPS>(t, sm, SumOp()))) * kLn2;
+    return RowSum{top, WARPS == 1 ? warp_sum(t) : block_all<32 * WARPS>(t, sm, SumOp())};
 }
 
 // The loss against targets, a row per warp, or per CTA where there are few rows of many strips (100 rows of 592: 5 us less; 8,192
 // rows take 88 us so, most of it barriers, and 36 with a warp each).
 template <int WARPS>
 __global__ void __launch_bounds__(kFinishThreads) head_finish_target_kernel(const HeadArgs g, const float2* __restrict__ stats, int strips,
-                                                                            HeadHeader* head) {
+                                                                            const float* __restrict__ zk, HeadHeader* head) {
     __shared__ double smd[kFinishThreads / 32];
     __shared__ float smf[kFinishThreads / 32];
     pdl_wait();
@@ -219,18 +229,11 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_target_kernel(cons
             if (g.bad && lane == 0) atomicCAS(g.bad, 0, (int)row + 1);
             t = 0;
         }
-        const float lse = row_lse<WARPS>(stats + row * strips, strips, smf);
-        float z = 0.f;
-        const int C4 = g.C / 4;
-        if (t >= 0) {
-#pragma unroll 4
-            for (int c = lane; c < C4; c += 32 * WARPS)
-                z = dot4(ld_value(g.x, g.x_lo, row * C4 + c), ld_value(g.w, g.w_lo, (int64_t)t * C4 + c), z);
-            z = WARPS == 1 ? warp_sum(z) : block_all<32 * WARPS>(z, smf, SumOp());
-        }
+        const RowSum r = row_sum<WARPS>(stats + row * strips, strips, smf);
         if (lane == 0) {
-            if (g.lse) g.lse[row] = lse;
-            g.losses[row] = t >= 0 ? lse - z : 0.f;
+            if (g.lse) g.lse[row] = lse_of(r);
+            const float loss = t >= 0 ? above_score(r, zk[row]) : 0.f;
+            g.losses[row] = loss < 0.f ? 0.f : loss;           // exponentials rounded: 2^-21 below zero at most
         }
     }
     if (g.loss_mean) mean_by_last<kFinishThreads>(g.aim, g.losses, g.N, &head->rows_done, gridDim.x, g.loss_mean, smd);
@@ -246,7 +249,7 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_entries_kernel(con
     const int lane = threadIdx.x & 31;
     if (row < g.N) {
         const LossAim& a = g.aim;
-        const float lse = row_lse<1>(stats + row * strips, strips, nullptr);
+        const RowSum r = row_sum<1>(stats + row * strips, strips, nullptr);
         float top = -INFINITY, sum = 0.f, loss = 0.f;
         int id;
         bool any = false;
@@ -262,12 +265,12 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_entries_kernel(con
             const float norm = a.lse ? a.lse[row] : top + logf(warp_sum(sum));
             for (int k = lane; k < a.K; k += 32) {
                 const float lp = entry_logit(a, row, k, g.V, nullptr, id) - norm, p = expf(lp);
-                if (p != 0.f) loss += p * (lp + (lse - zk[row * a.K + k] * kLn2));
+                if (p != 0.f) loss += p * (lp + above_score(r, zk[row * a.K + k]));
             }
         }
         loss = warp_sum(loss) * (a.tau * a.tau);
         if (lane == 0) {
-            if (g.lse) g.lse[row] = lse;
+            if (g.lse) g.lse[row] = lse_of(r);
             g.losses[row] = loss;
         }
     }
@@ -688,23 +691,25 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     const Forward f = forward_of(g.N, g.C, g.V);
     const int strips = strips_of(g.N, g.C, g.V);
     const HalfMat x = pair_matrix(w.x16, g.N, g.C);
+    const HeadScores scores{g.aim.targets, K, w.entries, w.strip_first, w.zk};
     cudaError_t e = cudaSuccess;
     if (f == kFew) {
-        e = launch_head_few_stats(g, w.stats, w.head, s);
+        e = launch_head_few_stats(g, w.stats, w.zk, w.head, s);
     } else if (f == kDirect) {
         e = launch_row_pairs(g, 0, w, 0, s);
-        if (e == cudaSuccess) e = launch_head_direct(g, x, w.rowf, w.stats, &w.head->err, s);
+        if (e == cudaSuccess) e = launch_head_direct(g, x, w.rowf, scores, w.stats, &w.head->err, s);
     } else {
         e = launch_row_pairs(g, g.V, w, K ? (int)((g.N + rows_sorted(g.N, K) - 1) / rows_sorted(g.N, K)) : 0, s);
         if (e == cudaSuccess)
-            e = launch_head_stats(x, pair_matrix(w.w16, g.V, g.C), w.rowf, w.colf, K, w.entries, w.strip_first, w.zk, w.stats, &w.head->err, s);
+            e = launch_head_stats(x, pair_matrix(w.w16, g.V, g.C), w.rowf, w.colf, scores, w.stats, &w.head->err, s);
     }
     if (e != cudaSuccess) return e;
     const unsigned ctas = (unsigned)((g.N + kFinishThreads / 32 - 1) / (kFinishThreads / 32));
     if (!K && g.N <= 148 * 8 && strips > 256)
-        BT_KERNEL_LAUNCH((head_finish_target_kernel<kFinishThreads / 32>), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
+        BT_KERNEL_LAUNCH((head_finish_target_kernel<kFinishThreads / 32>), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, (const float*)w.zk,
+                         w.head);
     else if (!K)
-        BT_KERNEL_LAUNCH((head_finish_target_kernel<1>), ctas, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
+        BT_KERNEL_LAUNCH((head_finish_target_kernel<1>), ctas, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, (const float*)w.zk, w.head);
     else if (f == kPairs)
         BT_KERNEL_LAUNCH((head_finish_entries_kernel), ctas, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, (const float*)w.zk, w.head);
     else

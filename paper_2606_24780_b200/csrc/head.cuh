@@ -34,11 +34,20 @@ struct HeadStrips {
 };
 HeadStrips head_stats_strips(int64_t N, int C, int V);
 size_t head_partial_bytes();
+// The scores that the losses need by themselves, in units of log 2: read off the sums that the statistics are made of.  A score formed
+// anew, in another order or another precision, is off by what it is rounded by: with a loss of 1e-8 and a score of 30 that
+// is all of the loss, in either direction.
+struct HeadScores {
+    const int* targets;                     // [N], zk [N]; null: a teacher's K entries,
+    int K;                                  // zk [N][K], of which
+    const int2* entries;                    // [N][K] holds (column, place in zk) by ascending column and
+    const uint16_t* strip_first;            // [N][strips + 1] the first of each strip
+    float* zk;
+};
 // stats [N][strips] = (maximum, sum) of z in units of log 2 over strips of columns, by rowf [N] and colf [V] from
-// accumulators there; zk [N][K] = z of the entries, of which `entries` [N][K] holds (column, place in zk) by ascending column
-// and strip_first [N][strips + 1] the first of each strip.
-cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, const float* colf, int K, const int2* entries,
-                              const uint16_t* strip_first, float* zk, float2* stats, int* err, cudaStream_t s);
+// accumulators there.
+cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, const float* colf, const HeadScores& scores, float2* stats,
+                              int* err, cudaStream_t s);
 // u = 2^15 (q - [v = target]) as pairs for the columns v0 .. v0 + w.rows - 1, zero in rows without part in the loss.
 cudaError_t launch_head_grad(const HalfMat& x, const HalfMat& w, int v0, const float* rowf, const RowParams* rows, __half* u, int64_t ldu,
                              int64_t u_plane, int* err, cudaStream_t s);
@@ -52,7 +61,7 @@ cudaError_t launch_head_dw(const HalfMat& u, const HalfMat& y, const float* scal
 constexpr int kFewRows = 8;                 // of x in one pass over the weights
 int head_few_at_once(int C);                // rows that one launch carries; the backward takes no more
 int head_few_strips(int64_t N, int C, int V);
-cudaError_t launch_head_few_stats(const HeadArgs& g, float2* stats, HeadHeader* head, cudaStream_t s);
+cudaError_t launch_head_few_stats(const HeadArgs& g, float2* stats, float* zk, HeadHeader* head, cudaStream_t s);
 cudaError_t launch_head_few_grad(const HeadArgs& g, const RowParams* params, int K, const int* eid, const float* ep, float* aim, float* dx_part,
                                  cudaStream_t s);
 
@@ -80,7 +89,7 @@ inline float head_growth(double n) { return (float)(1.0 + 0.5 * 0.56 / (1 << 24)
 // Statistics of up to 128 rows straight from W (head_direct.cu): [N][head_direct_strips(C, V)].
 bool head_direct_fits(int64_t N);
 int head_direct_strips(int C, int V);
-cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float* rowf, float2* stats, int* err, cudaStream_t s);
+cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float* rowf, const HeadScores& scores, float2* stats, int* err, cudaStream_t s);
 // The same of u (as launch_head_grad, for `cols` columns from v0 on), and dx = (+ dx) g_n u W from those columns, as planes too with the last.
 cudaError_t launch_head_direct_grad(const HeadArgs& h, const HalfMat& x, int v0, int cols, const float* rowf, const RowParams* rows, __half* u, int64_t ldu,
                                     int64_t u_plane, int* err, cudaStream_t s);

@@ -49,6 +49,7 @@ struct Args {
     int x_stages, per;                      // groups of a CTA that has one pass over them
     const float* rowf;                      // [N]
     float2* stats;                          // kStats: [N][4 CTAs]
+    HeadScores scores;                      // kStats
     const RowParams* rows;                  // kGrad
     int v0;                                 // kGrad: first column of this piece
     __half* u;                              // kGrad: [2][N][ldu]
@@ -64,7 +65,7 @@ struct Cfg {
     static constexpr uint32_t kForms = PLANES ? 2u : 1u, kBox = kGroup * 32u * 4u;       // a stage: [2 halves of the block][forms][groups]
     static constexpr uint32_t kW = 8u * kForms * kBox;
     static constexpr int kStages = PLANES ? 2 : 4;                      // of W; those of x are as many as fit
-    static constexpr uint32_t kScales = (2u * kTileRows + kMostX + 8u * kMostX) * 4u;      // scales, rowf, references and sums of four warps
+    static constexpr uint32_t kScales = (2u * kTileRows + kMostX + 12u * kMostX) * 4u;     // scales, rowf, references, sums and marks of four warps
     static constexpr uint32_t kFixed = 1024 + kStages * kW + kScales + 256;
 };
 constexpr uint32_t kSmemMost = 227u * 1024u;
@@ -87,6 +88,9 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, u
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld1(uint32_t taddr, uint32_t& r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr));
 }
 
 // Maxima (MAX) or sums over the warp's lanes of 32 values per lane: lane l gets that of value l.
@@ -296,6 +300,7 @@ head_direct_kernel(const __grid_constant__ WMaps tmW, const __grid_constant__ CU
         const int quad = warp & 3, row = quad * 32 + lane;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         float *const ref = refs + quad * kMostX, *const sum = refs + (4 + quad) * kMostX;     // over the tiles, in units of the reference
+        int* const mark = reinterpret_cast<int*>(refs + (8 + quad) * kMostX);      // kStats: the target's lane, where it is one of the warp's
         float* const row_l = refs;          // kGrad
         int* const hit = reinterpret_cast<int*>(refs + kMostX);
         uint32_t it = 0;
@@ -316,6 +321,11 @@ head_direct_kernel(const __grid_constant__ WMaps tmW, const __grid_constant__ CU
         for (int p = 0; p < passes && ok; ++p) {
             const int first = first_of(p);
             const bool mine = quad < groups_of(p);
+            for (int n = lane; MODE == kStats && mine && n < kMostX; n += 32) {        // read by the same lane
+                int t = n < g.N && g.scores.targets ? g.scores.targets[n] : -1;
+                if (t >= g.V) t = 0;
+                mark[n] = t < 0 ? -1 : t - (first + quad) * kGroup;
+            }
             float z[4][32];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
@@ -452,6 +462,14 @@ head_direct_kernel(const __grid_constant__ WMaps tmW, const __grid_constant__ CU
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = there ? ex2_fast(v[j]) : 0.f;
                 sum[n] += across<false>(v, lane);
+                // scores of the targets among the warp's rows of W, as the sums have them
+                for (unsigned left = __ballot_sync(0xffffffffu, mark[n] >= 0 && mark[n] < kGroup); left; left &= left - 1) {
+                    const int j = __ffs(left) - 1, at = __shfl_sync(0xffffffffu, mark[n], j);
+                    uint32_t zt;
+                    tmem_ld1(tmem + 384u + lanes + q * 32u + j, zt);
+                    tmem_ld_wait();
+                    if (lane == at) g.scores.zk[q * 32 + j] = __uint_as_float(zt) * row_f[q * 32 + j] * 32768.0f;
+                }
             }
         }
         // a warp without rows of W has the sum zero
@@ -551,9 +569,9 @@ Args args_for(const HeadArgs& h, int rows, int* err) {
 bool head_direct_fits(int64_t N) { return N <= kMostX; }
 int head_direct_strips(int C, int V) { return 4 * share_of(C, V).ctas; }
 
-cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float* rowf, float2* stats, int* err, cudaStream_t s) {
+cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float* rowf, const HeadScores& scores, float2* stats, int* err, cudaStream_t s) {
     Args g = args_for(h, h.V, err);
-    g.rowf = rowf; g.stats = stats;
+    g.rowf = rowf; g.stats = stats; g.scores = scores;
     const int grid = share_of(h.C, h.V).ctas;
     return h.w_lo ? launch<true, kStats>(h, 0, h.V, x, grid, g, s) : launch<false, kStats>(h, 0, h.V, x, grid, g, s);
 }

@@ -61,6 +61,7 @@ struct Few {
     int rows, G;                            // rows of x of this launch; threads of a group, a multiple of 32
     int64_t row0;
     float2* stats;                          // forward: [N][gridDim.x]
+    float* zk;                              // forward: [N] scores of the targets
     const RowParams* params;                // backward
     const float* aim;                       // backward: [V][kFewRows] weights of a teacher's entries (nullable)
     float* dx_part;                         // backward: [gridDim.x][kFewRows][C]
@@ -127,6 +128,11 @@ __global__ void __launch_bounds__(THREADS, few_ctas(ROWS, THREADS)) head_few_ker
     const int my_n = t % NR;                // of the product that this thread sums up over the group (t < R)
     RowParams mine{INFINITY, 0.f, 0.f, -1};
     if (BACK && t < R && my_n < a.rows) mine = a.params[a.row0 + my_n];
+    int target = -1;
+    if (!BACK && g.aim.targets && t < R && my_n < a.rows) {
+        target = g.aim.targets[a.row0 + my_n];
+        if (target >= g.V) target = 0;
+    }
     float m = -INFINITY, s = 0.f;
 
     for (int b = 0; b < batches; ++b) {
@@ -182,9 +188,10 @@ __global__ void __launch_bounds__(THREADS, few_ctas(ROWS, THREADS)) head_few_ker
             const int64_t v = v0 + t / NR;
             if (!BACK) {
                 if (v < v_end) {
-                    const float z2 = z * f, m1 = fmaxf(m, z2);
+                    const float z2 = __fmul_rn(z, f), m1 = fmaxf(m, z2);       // rounded before the differences
                     s = s * ex2_fast(m - m1) + ex2_fast(z2 - m1);
                     m = m1;
+                    if (v == target) a.zk[a.row0 + my_n] = z2;
                 }
             } else {
                 float u = 0.f;
@@ -336,13 +343,13 @@ int grid_of(const Shape& p, int V, int64_t rows) {
 
 int head_few_at_once(int C) { return rows_at_once(shape_of(C)); }
 int head_few_strips(int64_t N, int C, int V) { return grid_of(shape_of(C), V, N); }
-cudaError_t launch_head_few_stats(const HeadArgs& g, float2* stats, HeadHeader* head, cudaStream_t s) {
+cudaError_t launch_head_few_stats(const HeadArgs& g, float2* stats, float* zk, HeadHeader* head, cudaStream_t s) {
     const Shape p = shape_of(g.C);
     const int grid = grid_of(p, g.V, g.N);
     for (int64_t row0 = 0; row0 < g.N; row0 += rows_at_once(p)) {
         Few a{};
         a.rows = (int)(g.N - row0 < rows_at_once(p) ? g.N - row0 : rows_at_once(p));
-        a.G = p.G; a.row0 = row0; a.stats = stats; a.head = head;
+        a.G = p.G; a.row0 = row0; a.stats = stats; a.zk = zk; a.head = head;
         const cudaError_t e = g.w_lo ? launch_rows<true, false>(g, a, p, grid, s) : launch_rows<false, false>(g, a, p, grid, s);
         if (e != cudaSuccess) return e;
     }

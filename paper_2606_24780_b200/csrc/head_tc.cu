@@ -64,10 +64,7 @@ struct Args {
     int* err;
     const float* rowf;                      // [M] factor from accumulator to units of log 2
     const float* colf;                      // kStats: [N] the columns' part of it
-    int K;                                  // kStats: entries per row, with the first of each strip
-    const int2* entries;
-    const uint16_t* strip_first;            // [M][strips + 1]
-    float* zk;
+    HeadScores scores;                      // kStats
     float2* stats;                          // kStats: [M][kParts tiles_n]
     const RowParams* rows;                  // kGrad
     int v0;                                 // kGrad: first column of this piece
@@ -291,12 +288,19 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
             const int col0 = w.tn * BN + part * kCols, cols = g.N - col0;      // cols may be below zero
             int e_at = 0, e_end = 0;
             int2 entry = make_int2(0, 0), next = entry;
-            if (EPI == kStats && g.K && row < g.M) {
-                const uint16_t* f = g.strip_first + (long long)row * (kParts * g.tiles_n + 1) + kParts * w.tn + part;
-                e_at = f[0];
-                e_end = f[1];
-                if (e_at < e_end) entry = g.entries[(long long)row * g.K + e_at];
-                if (e_at + 1 < e_end) next = g.entries[(long long)row * g.K + e_at + 1];
+            if (EPI == kStats && row < g.M) {
+                if (g.scores.targets) {     // one entry at most
+                    int t = g.scores.targets[row];
+                    if (t >= g.N) t = 0;
+                    entry.x = t;
+                    e_end = t >= col0 && t < col0 + kCols ? 1 : 0;
+                } else {
+                    const uint16_t* f = g.scores.strip_first + (long long)row * (kParts * g.tiles_n + 1) + kParts * w.tn + part;
+                    e_at = f[0];
+                    e_end = f[1];
+                    if (e_at < e_end) entry = g.scores.entries[(long long)row * g.scores.K + e_at];
+                    if (e_at + 1 < e_end) next = g.scores.entries[(long long)row * g.scores.K + e_at + 1];
+                }
             }
             RowParams rp{INFINITY, 0.f, 0.f, -1};
             float f = 0.f;
@@ -334,10 +338,14 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
 #pragma unroll
                     for (int j = 0; j < kCols / 4; ++j) {
                         const float4 t = cf[j];
-                        v[4 * j] *= t.x * f; v[4 * j + 1] *= t.y * f; v[4 * j + 2] *= t.z * f; v[4 * j + 3] *= t.w * f;
+                        // rounded here, and not inside the differences below: the maximum is one of these numbers
+                        v[4 * j] = __fmul_rn(v[4 * j], t.x * f);
+                        v[4 * j + 1] = __fmul_rn(v[4 * j + 1], t.y * f);
+                        v[4 * j + 2] = __fmul_rn(v[4 * j + 2], t.z * f);
+                        v[4 * j + 3] = __fmul_rn(v[4 * j + 3], t.w * f);
                     }
                 }
-                // scores of the row's entries in this strip, the first two of which are here already
+                // scores of the row's target or entries in this strip, the first two of which are here already
                 while (__any_sync(0xffffffffu, e_at < e_end)) {
                     const int c = e_at < e_end ? entry.x - col0 : -1;
                     float z = 0.f;
@@ -349,10 +357,10 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
                             if (c == q * 16 + j) z = v[q * 16 + j];
                     }
                     if (e_at < e_end) {
-                        g.zk[(long long)row * g.K + entry.y] = z;
+                        g.scores.zk[g.scores.targets ? row : (long long)row * g.scores.K + entry.y] = z;
                         ++e_at;
                         entry = next;
-                        if (e_at + 1 < e_end) next = g.entries[(long long)row * g.K + e_at + 1];
+                        if (e_at + 1 < e_end) next = g.scores.entries[(long long)row * g.scores.K + e_at + 1];
                     }
                 }
                 if (row < g.M && cols > 0) {
@@ -606,11 +614,11 @@ HeadStrips head_stats_strips(int64_t N, int C, int V) {
 }
 size_t head_partial_bytes() { return (size_t)148 * BM * 256 * sizeof(float); }
 
-cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, const float* colf, int K, const int2* entries,
-                              const uint16_t* strip_first, float* zk, float2* stats, int* err, cudaStream_t s) {
+cudaError_t launch_head_stats(const HalfMat& x, const HalfMat& w, const float* rowf, const float* colf, const HeadScores& scores, float2* stats,
+                              int* err, cudaStream_t s) {
     Args g{};
     g.M = (int)x.rows; g.N = (int)w.rows;
-    g.rowf = rowf; g.colf = colf; g.K = K; g.entries = entries; g.strip_first = strip_first; g.zk = zk; g.stats = stats; g.err = err;
+    g.rowf = rowf; g.colf = colf; g.scores = scores; g.stats = stats; g.err = err;
     return launch_wide<kStats>(g, x, w, x.cols, s);
 }
 

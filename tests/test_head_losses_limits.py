@@ -1,5 +1,5 @@
 """The losses at the language-model head, and distillation on logits, where they could give way: teachers whose numbers are not
-finite beside entries that are not there; rows of which most CTAs have nothing."""
+finite beside entries that are not there; rows of which most CTAs have nothing; rows that are sure of their target."""
 import math
 
 import pytest
@@ -76,3 +76,41 @@ def test_rows_whose_vocabulary_ends_in_the_first_slices(N, V, ld):
         assert float((got[0] - losses).abs().max()) < 2e-6 * 1.5 ** 2 * top * 2
         assert abs(float(got[1][0]) - float(mean)) < 4e-6 * 1.5 ** 2 * top
         assert float((got[2] - d).norm()) < 2e-6 * top * c.inv * 1.5 * 2 * float(c.weight().norm()) and not got[2][:, V:].any()
+
+
+# ------------------------------------------------------------------------------- GPU: rows that are sure of their target
+
+def sure(c, y, top, kind):
+    """Scores of `top` at column y of every row, by operands whose products all have one sign or are one product alone."""
+    if kind == "aligned":
+        c.w[y] = c.x * (top / (c.x.double() ** 2).sum(1, keepdim=True)).float()
+    else:
+        c.x.zero_()
+        c.w[:, 0] = 0
+        c.x[:, 0] = 1.0
+        c.w[y, 0] = top
+    # the products' bound: two operands of 2^-23, the product of their low halves, 72 instructions cut by up to 2^-23 of the running
+    # sum, and what is put back for that (2^-24 for each of them)
+    return (72 * 2.0 ** -23 + 72 * 2.0 ** -24 + 2.0 ** -21) * float((c.x.abs() @ c.w.abs().T).max())
+
+
+@gpu
+@pytest.mark.parametrize("N,C,V", [(1, 768, 50257), (2, 4096, 300), (4, 96, 9001), (6, 768, 20000), (8, 2080, 999), (40, 768, 19000), (100, 64, 5001), (128, 1056, 700),
+                                   (129, 768, 2000), (300, 768, 5003), (1025, 96, 1500)])
+@pytest.mark.parametrize("kind", ["aligned", "alone"])
+@pytest.mark.parametrize("top", [9.0, 30.0, 70.0])
+@pytest.mark.parametrize("planes", [False, True])
+def test_the_loss_of_a_row_that_is_sure_of_its_target(N, C, V, kind, top, planes):
+    """The loss is log sum_v exp(z_v - z_y): score errors e move it by (1 - q_y) times their differences, however large the scores
+    are, and it is not below zero.  The exponentials of a sum, its logarithm and what they are rounded by come to 2^-21."""
+    c = Case(N, C, V, planes=planes, seed=N + C, scale=0.5)
+    y = torch.arange(N, device=DEV) * 7 % V
+    c.targets = y.int()
+    e = sure(c, y, top, kind)
+    losses, lse, mean = c.forward()
+    want = c.want()
+    other = 1.0 - torch.exp(-want[0])
+    assert (losses >= 0).all()
+    assert ((losses.double() - want[0]).abs() <= 2 * e * other + 2.0 ** -21 + 2.0 ** -22 * want[0]).all()
+    assert abs(float(mean[0]) - float(want[2])) <= 2 * e * float(other.max()) + 2.0 ** -20 + 2.0 ** -22 * float(want[2])
+    assert float((lse - want[1]).abs().max()) <= e + 2.0 ** -21 + 2.0 ** -23 * float(want[1].abs().max())
