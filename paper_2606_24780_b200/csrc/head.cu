@@ -6,7 +6,7 @@
 //     both:                     dz_nv = g_n (q_nv - a_nv),   dx = dz W,   dW = dz^T x
 // where a_nv is the row's aim (1 at the target; the sum of p_nk / S_n over the entries with i_nk = v, S_n = sum_k p_nk) and
 // g_n = inv_count w_n tau S_n.  The forward keeps one (maximum, sum) pair per row and strip of the vocabulary, joined
-// by head_finish_kernel, which also forms the few scores that the loss needs by themselves; the backward forms z again.
+// by the finish kernels, and the few scores that the loss needs by themselves; the backward forms z again.
 //
 // Up to four rows, or eight (see few_rows), go through head_rows.cu in plain FP32, where the weights are read once; up to 128 through head_direct.cu, where the
 // products with W (z, dx) read it as it is and make pairs of FP16 numbers on the way to the tensor cores; more rows to head_tc.cu,
@@ -41,8 +41,8 @@ struct Scratch {
     float2* stats;                          // forward: [N][strips]
     float* colf;                            // forward, tensor cores: [V] up to a multiple of 256
     int2* entries;                          // [N][K]
-    uint16_t* strip_first;                  // [N][strips + 1]
-    float* zk;                              // [N] scores of the targets, or [N][K] of a teacher's entries
+    uint32_t* spans;                        // [N][strips]
+    float* zk;                              // [N] scores of the targets, or of a teacher's entries: [N][K], few rows [V][kFewRows]
     RowParams* rows;                        // backward: [N]
     int* eid;                               // [N][K] columns of the aim, each once; below zero: none
     float* ep;                              // [N][K] its weights there
@@ -95,19 +95,23 @@ int strips_of(int64_t N, int C, int V) {
     return f == kFew ? head_few_strips(N, C, V) : f == kDirect ? head_direct_strips(C, V) : head_stats_strips(N, C, V).count;
 }
 
+// Those that a teacher's entries are sorted into.
+HeadStrips entry_strips(int64_t N, int C, int V) {
+    return forward_of(N, C, V) == kDirect ? head_direct_entry_strips(V) : head_stats_strips(N, C, V);
+}
+
 size_t fwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K) {
     size_t at = kHeadHeader;
     const Forward f = forward_of(N, C, V);
     s = Scratch{};
     s.head = (HeadHeader*)base;
     s.stats = take<float2>(base, at, (size_t)N * strips_of(N, C, V));
-    s.zk = take<float>(base, at, (size_t)N * (K ? K : 1));
+    s.zk = take<float>(base, at, K == 0 ? (size_t)N : f == kFew ? (size_t)V * kFewRows : (size_t)N * K);
     if (f == kFew) return at;
     tc_layout(s, base, at, N, C, f == kDirect ? 0 : V);
-    if (f == kDirect) return at;
-    s.colf = take<float>(base, at, (V + 255) / 256 * 256);
+    if (f == kPairs) s.colf = take<float>(base, at, (V + 255) / 256 * 256);
     s.entries = take<int2>(base, at, (size_t)N * K);
-    if (K) s.strip_first = take<uint16_t>(base, at, (size_t)N * (head_stats_strips(N, C, V).count + 1));
+    if (K) s.spans = take<uint32_t>(base, at, (size_t)N * entry_strips(N, C, V).count);
     return at;
 }
 
@@ -136,53 +140,6 @@ size_t bwd_layout(Scratch& s, uint8_t* base, int64_t N, int C, int V, int K, int
 __device__ __forceinline__ float4 ld_value(const float* hi, const float* lo, int64_t i4) {
     const float4 a = ld4(hi, i4);
     return lo ? add4(a, ld4(lo, i4)) : a;
-}
-__device__ __forceinline__ float dot4(float4 a, float4 b, float acc) {
-    return fmaf(a.w, b.w, fmaf(a.z, b.z, fmaf(a.y, b.y, fmaf(a.x, b.x, acc))));
-}
-
-// Up to some dozens of rows against a teacher, one per CTA: joins the partial statistics, forms the scores of the row's entries and the loss.
-__global__ void __launch_bounds__(kFinishThreads) head_finish_kernel(const HeadArgs g, const float2* __restrict__ stats, int strips,
-                                                                     HeadHeader* head) {
-    __shared__ float smf[kFinishThreads / 32];
-    __shared__ double smd[kFinishThreads / 32];
-    pdl_wait();
-    pdl_trigger();
-    const int64_t row = blockIdx.x;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const float2* st = stats + row * strips;
-    float m = -INFINITY, s = 0.f;
-    for (int i = threadIdx.x; i < strips; i += kFinishThreads)
-        if (st[i].y != 0.f) m = fmaxf(m, st[i].x);          // a strip without columns has the sum zero
-    m = block_all<kFinishThreads>(m, smf, MaxOp());
-    for (int i = threadIdx.x; i < strips; i += kFinishThreads)
-        if (st[i].y != 0.f) s += st[i].y * ex2_fast(st[i].x - m);
-    s = block_all<kFinishThreads>(s, smf, SumOp());
-    const float lse = (m + log2f(s)) * kLn2;
-
-    const int C4 = g.C / 4;
-    auto score = [&](int v) {                               // by a warp
-        float z = 0.f;
-        for (int c = lane; c < C4; c += 32)
-            z = dot4(ld_value(g.x, g.x_lo, row * C4 + c), ld_value(g.w, g.w_lo, (int64_t)v * C4 + c), z);
-        return warp_sum(z) * (1.0f / g.aim.tau);
-    };
-    float loss = 0.f;
-    bool any;
-    const float norm = teacher_norm<kFinishThreads>(g.aim, row, g.V, g.bad, smf, any);
-    float t = 0.f;
-    for (int k = warp; any && k < g.aim.K; k += kFinishThreads / 32) {
-        int id;
-        const float lp = entry_logit(g.aim, row, k, g.V, nullptr, id) - norm, p = expf(lp);
-        // NaN is not zero: such a row has no finite loss.  Where the norm is NaN, so is p of an entry that is not there
-        if (id >= 0 && p != 0.f) t += p * (lp + (lse - score(id)));
-    }
-    loss = block_all<kFinishThreads>(lane == 0 ? t : 0.f, smf, SumOp()) * (g.aim.tau * g.aim.tau);
-    if (threadIdx.x == 0) {
-        if (g.lse) g.lse[row] = lse;
-        g.losses[row] = loss;
-    }
-    if (g.loss_mean) mean_by_last<kFinishThreads>(g.aim, g.losses, g.N, &head->rows_done, gridDim.x, g.loss_mean, smd);
 }
 
 // The sum of a row's exponentials: 2^m s.
@@ -239,7 +196,34 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_target_kernel(cons
     if (g.loss_mean) mean_by_last<kFinishThreads>(g.aim, g.losses, g.N, &head->rows_done, gridDim.x, g.loss_mean, smd);
 }
 
-// The same for a teacher whose entries' scores are there already (in units of log 2), a row per warp.
+// Up to some dozens of rows against a teacher, one per CTA.
+template <bool FEW>
+__global__ void __launch_bounds__(kFinishThreads) head_finish_kernel(const HeadArgs g, const float2* __restrict__ stats, int strips,
+                                                                     const float* __restrict__ zk, HeadHeader* head) {
+    __shared__ float smf[kFinishThreads / 32];
+    __shared__ double smd[kFinishThreads / 32];
+    pdl_wait();
+    pdl_trigger();
+    const int64_t row = blockIdx.x;
+    const RowSum r = row_sum<kFinishThreads / 32>(stats + row * strips, strips, smf);
+    bool any;
+    const TeacherNorm norm = teacher_norm<kFinishThreads>(g.aim, row, g.V, g.bad, smf, any);
+    float t = 0.f;
+    for (int k = threadIdx.x; any && k < g.aim.K; k += kFinishThreads) {
+        int id;
+        const float lp = log_weight(entry_logit(g.aim, row, k, g.V, nullptr, id), norm), p = expf(lp);
+        // NaN is not zero: such a row has no finite loss.  Where the norm is NaN, so is p of an entry that is not there
+        if (id >= 0 && p != 0.f) t += p * (lp + above_score(r, zk[FEW ? (int64_t)id * kFewRows + row : row * g.aim.K + k]));
+    }
+    const float loss = block_all<kFinishThreads>(t, smf, SumOp()) * (g.aim.tau * g.aim.tau);
+    if (threadIdx.x == 0) {
+        if (g.lse) g.lse[row] = lse_of(r);
+        g.losses[row] = loss;
+    }
+    if (g.loss_mean) mean_by_last<kFinishThreads>(g.aim, g.losses, g.N, &head->rows_done, gridDim.x, g.loss_mean, smd);
+}
+
+// More rows, one per warp.
 __global__ void __launch_bounds__(kFinishThreads) head_finish_entries_kernel(const HeadArgs g, const float2* __restrict__ stats, int strips,
                                                                              const float* __restrict__ zk, HeadHeader* head) {
     __shared__ double smd[kFinishThreads / 32];
@@ -262,9 +246,9 @@ __global__ void __launch_bounds__(kFinishThreads) head_finish_entries_kernel(con
         if (any) {
             top = warp_max(top);
             for (int k = lane; k < a.K; k += 32) sum += expf(entry_logit(a, row, k, g.V, nullptr, id) - top);
-            const float norm = a.lse ? a.lse[row] : top + logf(warp_sum(sum));
+            const TeacherNorm norm = a.lse ? TeacherNorm{a.lse[row], 0.f} : TeacherNorm{top, logf(warp_sum(sum))};
             for (int k = lane; k < a.K; k += 32) {
-                const float lp = entry_logit(a, row, k, g.V, nullptr, id) - norm, p = expf(lp);
+                const float lp = log_weight(entry_logit(a, row, k, g.V, nullptr, id), norm), p = expf(lp);
                 if (p != 0.f) loss += p * (lp + above_score(r, zk[row * a.K + k]));
             }
         }
@@ -322,12 +306,12 @@ __global__ void __launch_bounds__(THREADS) head_rows_kernel(const HeadArgs g, Ro
             const int places = id_places(a.K);
             for (int k = threadIdx.x; k < places; k += THREADS) table[k] = -1;
             bool any, twice = false;
-            const float norm = teacher_norm<THREADS>(a, row, g.V, nullptr, smf, any);
+            const TeacherNorm norm = teacher_norm<THREADS>(a, row, g.V, nullptr, smf, any);
             float sum = 0.f;
             for (int k = threadIdx.x; k < a.K; k += THREADS) {
                 int id = -1;
                 const float t = any ? entry_logit(a, row, k, g.V, nullptr, id) : -INFINITY;
-                p[k] = any ? expf(t - norm) : 0.f;
+                p[k] = any ? expf(log_weight(t, norm)) : 0.f;
                 ids[k] = p[k] != 0.f ? id : -1;
                 twice |= seen_before(table, places, a.K, ids[k]);
                 sum += p[k];
@@ -437,15 +421,14 @@ __host__ __device__ inline int rows_sorted(int64_t N, int K) {
     while (2 * rows * sorted_size(K) <= kSorted && N / (2 * rows) >= 592) rows *= 2;
     return rows;
 }
-__device__ __forceinline__ void sort_entries(const HeadArgs& g, int2* entries, uint16_t* strip_first, HeadStrips strips, unsigned long long* key) {
+__device__ __forceinline__ void sort_entries(const HeadArgs& g, int2* entries, uint32_t* spans, HeadStrips strips, unsigned long long* key) {
     const LossAim& a = g.aim;
     const int n = sorted_size(a.K), rows = rows_sorted(g.N, a.K), all = n * rows;
     const int64_t row0 = blockIdx.x * (int64_t)rows;
     for (int i = threadIdx.x; i < all; i += kThreads) {
         const int k = i & (n - 1);
         const int64_t row = row0 + i / n;
-        int id = -1;
-        if (k < a.K && row < g.N && entry_logit(a, row, k, g.V, g.bad, id) == -INFINITY) id = -1;
+        const int id = k < a.K && row < g.N ? entry_id(a, row, k, g.V, g.bad) : -1;
         key[i] = ((unsigned long long)(id < 0 ? INT_MAX : id) << 32) | (unsigned)k;
     }
     for (int size = 2; size <= n; size *= 2)
@@ -481,7 +464,9 @@ __device__ __forceinline__ void sort_entries(const HeadArgs& g, int2* entries, u
                 left = h;
             }
         }
-        strip_first[row * (strips.count + 1) + t] = (uint16_t)lo;
+        uint16_t* half = reinterpret_cast<uint16_t*>(spans + row * strips.count);       // where a strip's begin, those of the one before end
+        if (t < strips.count) half[2 * t] = (uint16_t)lo;
+        if (t > 0) half[2 * t - 1] = (uint16_t)lo;
     }
 }
 
@@ -495,7 +480,7 @@ __global__ void __launch_bounds__(kThreads) head_row_pairs_kernel(const HeadArgs
     pdl_trigger();
     if (blockIdx.x == 0 && threadIdx.x == 0) *s.head = HeadHeader{0, 0u};
     if (SORT && (int)blockIdx.x < sort_ctas) {
-        sort_entries(g, s.entries, s.strip_first, strips, key);
+        sort_entries(g, s.entries, s.spans, strips, key);
         return;
     }
     const int C4 = g.C / 4;
@@ -666,20 +651,21 @@ size_t head_bwd_scratch_bytes(int64_t N, int C, int V, int K, int piece) {
 namespace {
 
 template <int LANES>
-cudaError_t launch_row_pairs_by(const HeadArgs& g, int64_t w_rows, const Scratch& w, int sort_ctas, cudaStream_t s) {
+cudaError_t launch_row_pairs_by(const HeadArgs& g, int64_t w_rows, const Scratch& w, cudaStream_t s) {
+    const int K = entries_of(g), sort_ctas = K ? (int)((g.N + rows_sorted(g.N, K) - 1) / rows_sorted(g.N, K)) : 0;
     const int grid = sort_ctas + grid_for((w_rows + g.N) * LANES, 148 * 8);
     // the sort's shared memory, where there is none, keeps the next kernel's CTAs off the SM: 3 us
-    if (sort_ctas) BT_KERNEL_LAUNCH((head_row_pairs_kernel<LANES, true>), grid, kThreads, 0, s, g, w_rows, w, sort_ctas, head_stats_strips(g.N, g.C, g.V));
+    if (sort_ctas) BT_KERNEL_LAUNCH((head_row_pairs_kernel<LANES, true>), grid, kThreads, 0, s, g, w_rows, w, sort_ctas, entry_strips(g.N, g.C, g.V));
     else BT_KERNEL_LAUNCH((head_row_pairs_kernel<LANES, false>), grid, kThreads, 0, s, g, w_rows, w, 0, HeadStrips{});
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }
 // As few lanes to a row as hold it: many rows in flight.
-cudaError_t launch_row_pairs(const HeadArgs& g, int64_t w_rows, const Scratch& w, int sort_ctas, cudaStream_t s) {
-    return g.C <= 128   ? launch_row_pairs_by<4>(g, w_rows, w, sort_ctas, s)
-           : g.C <= 256 ? launch_row_pairs_by<8>(g, w_rows, w, sort_ctas, s)
-           : g.C <= 512 ? launch_row_pairs_by<16>(g, w_rows, w, sort_ctas, s)
-                        : launch_row_pairs_by<32>(g, w_rows, w, sort_ctas, s);
+cudaError_t launch_row_pairs(const HeadArgs& g, int64_t w_rows, const Scratch& w, cudaStream_t s) {
+    return g.C <= 128   ? launch_row_pairs_by<4>(g, w_rows, w, s)
+           : g.C <= 256 ? launch_row_pairs_by<8>(g, w_rows, w, s)
+           : g.C <= 512 ? launch_row_pairs_by<16>(g, w_rows, w, s)
+                        : launch_row_pairs_by<32>(g, w_rows, w, s);
 }
 
 }  // namespace
@@ -691,15 +677,15 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
     const Forward f = forward_of(g.N, g.C, g.V);
     const int strips = strips_of(g.N, g.C, g.V);
     const HalfMat x = pair_matrix(w.x16, g.N, g.C);
-    const HeadScores scores{g.aim.targets, K, w.entries, w.strip_first, w.zk};
+    const HeadScores scores{g.aim.targets, K, w.entries, w.spans, w.zk};
     cudaError_t e = cudaSuccess;
     if (f == kFew) {
         e = launch_head_few_stats(g, w.stats, w.zk, w.head, s);
     } else if (f == kDirect) {
-        e = launch_row_pairs(g, 0, w, 0, s);
+        e = launch_row_pairs(g, 0, w, s);
         if (e == cudaSuccess) e = launch_head_direct(g, x, w.rowf, scores, w.stats, &w.head->err, s);
     } else {
-        e = launch_row_pairs(g, g.V, w, K ? (int)((g.N + rows_sorted(g.N, K) - 1) / rows_sorted(g.N, K)) : 0, s);
+        e = launch_row_pairs(g, g.V, w, s);
         if (e == cudaSuccess)
             e = launch_head_stats(x, pair_matrix(w.w16, g.V, g.C), w.rowf, w.colf, scores, w.stats, &w.head->err, s);
     }
@@ -712,8 +698,10 @@ cudaError_t launch_head_fwd(const HeadArgs& g, cudaStream_t s) {
         BT_KERNEL_LAUNCH((head_finish_target_kernel<1>), ctas, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, (const float*)w.zk, w.head);
     else if (f == kPairs)
         BT_KERNEL_LAUNCH((head_finish_entries_kernel), ctas, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, (const float*)w.zk, w.head);
+    else if (f == kFew)
+        BT_KERNEL_LAUNCH((head_finish_kernel<true>), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, (const float*)w.zk, w.head);
     else
-        BT_KERNEL_LAUNCH((head_finish_kernel), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, w.head);
+        BT_KERNEL_LAUNCH((head_finish_kernel<false>), (unsigned)g.N, kFinishThreads, 0, s, g, (const float2*)w.stats, strips, (const float*)w.zk, w.head);
     BT_COUNT_LAUNCH();
     return cudaGetLastError();
 }

@@ -40,8 +40,8 @@ size_t head_partial_bytes();
 struct HeadScores {
     const int* targets;                     // [N], zk [N]; null: a teacher's K entries,
     int K;                                  // zk [N][K], of which
-    const int2* entries;                    // [N][K] holds (column, place in zk) by ascending column and
-    const uint16_t* strip_first;            // [N][strips + 1] the first of each strip
+    const int2* entries;                    // [N][K] holds (column, place in zk) by ascending column, and
+    const uint32_t* spans;                  // [N][strips] those of each strip: from the lower half to the upper one
     float* zk;
 };
 // stats [N][strips] = (maximum, sum) of z in units of log 2 over strips of columns, by rowf [N] and colf [V] from
@@ -56,7 +56,8 @@ cudaError_t launch_head_dx(const HalfMat& u, const HalfMat& w, const RowParams* 
                            int* err, cudaStream_t s);
 cudaError_t launch_head_dw(const HalfMat& u, const HalfMat& y, const float* scale, float* dw, float* partials, int* err, cudaStream_t s);
 
-// Few rows in plain FP32 (head_rows.cu): statistics [N][head_few_strips(N, C, V)]; gradients with a table [V][kFewRows] and parts
+// Few rows in plain FP32 (head_rows.cu): statistics [N][head_few_strips(N, C, V)], with zk [N] the targets' scores, or [V][kFewRows] all scores
+// where there is a teacher; gradients with a table [V][kFewRows] and parts
 // of dx [head_few_strips(N, C, V)][kFewRows][C] in scratch.
 constexpr int kFewRows = 8;                 // of x in one pass over the weights
 int head_few_at_once(int C);                // rows that one launch carries; the backward takes no more
@@ -86,9 +87,11 @@ __device__ __forceinline__ void to_pairs(float a, float b, uint32_t& hi, uint32_
 // two sums in registers; the products are made longer by 0.56.
 inline float head_growth(double n) { return (float)(1.0 + 0.5 * 0.56 / (1 << 24) * n); }
 
-// Statistics of up to 128 rows straight from W (head_direct.cu): [N][head_direct_strips(C, V)].
+// Statistics of up to 128 rows straight from W (head_direct.cu): [N][head_direct_strips(C, V)].  A teacher's entries are sorted into
+// strips of their own, 32 columns each.
 bool head_direct_fits(int64_t N);
 int head_direct_strips(int C, int V);
+inline HeadStrips head_direct_entry_strips(int V) { return HeadStrips{32, (V + 31) / 32}; }
 cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float* rowf, const HeadScores& scores, float2* stats, int* err, cudaStream_t s);
 // The same of u (as launch_head_grad, for `cols` columns from v0 on), and dx = (+ dx) g_n u W from those columns, as planes too with the last.
 cudaError_t launch_head_direct_grad(const HeadArgs& h, const HalfMat& x, int v0, int cols, const float* rowf, const RowParams* rows, __half* u, int64_t ldu,
@@ -96,16 +99,17 @@ cudaError_t launch_head_direct_grad(const HeadArgs& h, const HalfMat& x, int v0,
 cudaError_t launch_head_direct_dx(const HeadArgs& h, const HalfMat& u, int v0, const RowParams* rows, bool onto, bool last, float* partials, int* err,
                                   cudaStream_t s);
 
-// Logit of entry k of a row in units of the softened softmax, -inf where there is none (a weight of zero).  An id
-// behind the vocabulary counts as id 0 and is recorded.
+// Column of entry k of a row, below zero where there is none.  An id behind the vocabulary counts as id 0 and is recorded.
+__device__ __forceinline__ int entry_id(const LossAim& a, int64_t row, int k, int V, int* bad) {
+    const int id = a.ids[row * a.K + k];
+    if (id < V) return id;
+    if (bad) atomicCAS(bad, 0, (int)row + 1);
+    return 0;
+}
+// Its logit in units of the softened softmax, -inf where there is none (a weight of zero).
 __device__ __forceinline__ float entry_logit(const LossAim& a, int64_t row, int k, int V, int* bad, int& id) {
-    id = a.ids[row * a.K + k];
-    if (id < 0) return -INFINITY;
-    if (id >= V) {
-        if (bad) atomicCAS(bad, 0, (int)row + 1);
-        id = 0;
-    }
-    return a.logits[row * a.K + k] * (1.0f / a.tau);
+    id = entry_id(a, row, k, V, bad);
+    return id < 0 ? -INFINITY : a.logits[row * a.K + k] * (1.0f / a.tau);
 }
 
 // Whether a row has an id twice.  Up to 32 entries, one to a lane of the first warp, are matched there; more go through a table of at least
@@ -156,9 +160,15 @@ struct MaxOp {
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
 
-// The logarithm of a teacher's normaliser for one row; `any`: the row has an entry.  All threads of the block call it.
+// The logarithm of a teacher's normaliser for one row, in two parts: a weight's logarithm is (t - top) - rest, where their sum would be
+// rounded by 2^-24 of the largest logit.
+struct TeacherNorm {
+    float top, rest;
+};
+__device__ __forceinline__ float log_weight(float t, TeacherNorm n) { return (t - n.top) - n.rest; }
+// `any`: the row has an entry.  All threads of the block call it.
 template <int THREADS>
-__device__ __forceinline__ float teacher_norm(const LossAim& a, int64_t row, int V, int* bad, float* sm, bool& any) {
+__device__ __forceinline__ TeacherNorm teacher_norm(const LossAim& a, int64_t row, int V, int* bad, float* sm, bool& any) {
     float m = -INFINITY;
     int id, have = 0;
     for (int k = threadIdx.x; k < a.K; k += THREADS) {
@@ -167,12 +177,12 @@ __device__ __forceinline__ float teacher_norm(const LossAim& a, int64_t row, int
         m = fmaxf(m, t);
     }
     any = __syncthreads_or(have) != 0;
-    if (!any) return 0.f;
-    if (a.lse) return a.lse[row];
+    if (!any) return TeacherNorm{0.f, 0.f};
+    if (a.lse) return TeacherNorm{a.lse[row], 0.f};
     m = block_all<THREADS>(m, sm, MaxOp());
     float s = 0.f;
     for (int k = threadIdx.x; k < a.K; k += THREADS) s += expf(entry_logit(a, row, k, V, nullptr, id) - m);
-    return m + logf(block_all<THREADS>(s, sm, SumOp()));
+    return TeacherNorm{m, logf(block_all<THREADS>(s, sm, SumOp()))};
 }
 
 // The mean loss, by the block that finishes last: inv_count * sum_n w_n losses_n in a fixed order, in 64 bits.  Rows

@@ -1,6 +1,6 @@
 // The head's products with W for some dozens of rows of x: W goes through the SMs as it is, and becomes FP16 pairs on the way.
 //
-//     kStats  z = x W^T, (maximum, sum of exponentials) over a CTA's share of the vocabulary
+//     kStats  z = x W^T, (maximum, sum of exponentials) over a CTA's share of the vocabulary; kStatsTop the same with a teacher's entries
 //     kGrad   the same z, u = 2^15 (q - [v = target]) as pairs
 //     kDx     dx = u W, a range of the vocabulary each, joined by head_direct_dx_kernel
 //
@@ -41,15 +41,15 @@ struct WMaps {
     CUtensorMap of[4];
 };
 
-// What becomes of the products of x and W (kStats, kGrad), and the product of u and W.
-enum Mode { kStats, kGrad, kDx };
+// What becomes of the products of x and W (kStats with targets, kStatsTop with a teacher's entries, kGrad), and the product of u and W.
+enum Mode { kStats, kStatsTop, kGrad, kDx };
 
 struct Args {
     int N, C, V, groups, blocks, Nr;        // groups of 32 rows of W; Nr: rows of x, up to a multiple of 16
     int x_stages, per;                      // groups of a CTA that has one pass over them
     const float* rowf;                      // [N]
-    float2* stats;                          // kStats: [N][4 CTAs]
-    HeadScores scores;                      // kStats
+    float2* stats;                          // kStats, kStatsTop: [N][4 CTAs]
+    HeadScores scores;                      // kStats, kStatsTop
     const RowParams* rows;                  // kGrad
     int v0;                                 // kGrad: first column of this piece
     __half* u;                              // kGrad: [2][N][ldu]
@@ -65,7 +65,7 @@ struct Cfg {
     static constexpr uint32_t kForms = PLANES ? 2u : 1u, kBox = kGroup * 32u * 4u;       // a stage: [2 halves of the block][forms][groups]
     static constexpr uint32_t kW = 8u * kForms * kBox;
     static constexpr int kStages = PLANES ? 2 : 4;                      // of W; those of x are as many as fit
-    static constexpr uint32_t kScales = (2u * kTileRows + kMostX + 12u * kMostX) * 4u;     // scales, rowf, references, sums and marks of four warps
+    static constexpr uint32_t kScales = (2u * kTileRows + kMostX + 24u * kMostX) * 4u;     // scales, rowf; references, sums, spans and entries of four warps
     static constexpr uint32_t kFixed = 1024 + kStages * kW + kScales + 256;
 };
 constexpr uint32_t kSmemMost = 227u * 1024u;
@@ -93,6 +93,13 @@ __device__ __forceinline__ void tmem_ld1(uint32_t taddr, uint32_t& r) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr));
 }
 
+__device__ __forceinline__ void copy4(uint32_t* dst, const uint32_t* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy8(int2* dst, const int2* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+
 // Maxima (MAX) or sums over the warp's lanes of 32 values per lane: lane l gets that of value l.
 template <bool MAX>
 __device__ __forceinline__ float across(float (&v)[32], int lane) {
@@ -112,6 +119,7 @@ template <bool PLANES, int MODE>
 __global__ void __launch_bounds__(kThreads, 1)
 head_direct_kernel(const __grid_constant__ WMaps tmW, const __grid_constant__ CUtensorMap tmX, const Args g) {
     using C = Cfg<PLANES>;
+    constexpr bool kSums = MODE == kStats || MODE == kStatsTop;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -300,14 +308,13 @@ head_direct_kernel(const __grid_constant__ WMaps tmW, const __grid_constant__ CU
         const int quad = warp & 3, row = quad * 32 + lane;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         float *const ref = refs + quad * kMostX, *const sum = refs + (4 + quad) * kMostX;     // over the tiles, in units of the reference
-        int* const mark = reinterpret_cast<int*>(refs + (8 + quad) * kMostX);      // kStats: the target's lane, where it is one of the warp's
         float* const row_l = refs;          // kGrad
         int* const hit = reinterpret_cast<int*>(refs + kMostX);
         uint32_t it = 0;
         bool ok = true;
         for (int n = lane; n < kMostX; n += 32) {
             if (MODE != kDx && quad == 0) row_f[n] = n < g.N ? g.rowf[n] * g.grow : 0.f;
-            if (MODE == kStats) {
+            if (kSums) {
                 ref[n] = -INFINITY;
                 sum[n] = 0.f;
             }
@@ -317,14 +324,34 @@ head_direct_kernel(const __grid_constant__ WMaps tmW, const __grid_constant__ CU
                 hit[n] = r.target < 0 ? -1 : r.target - g.v0;
             }
         }
+        int target[4] = {-1, -1, -1, -1};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (MODE == kStats && q * 32 + lane < g.N) target[q] = g.scores.targets[q * 32 + lane];
+            if (target[q] >= g.V) target[q] = 0;
+        }
+        // kStatsTop: a row's entries among the warp's rows of W, of this pass and the next, and the first of them; each lane copies
+        // what it reads
+        uint32_t* const span = reinterpret_cast<uint32_t*>(refs + 8 * kMostX) + quad * 2 * kMostX;
+        int2* const entry = reinterpret_cast<int2*>(refs + 16 * kMostX) + quad * kMostX;
+        auto fetch_spans = [&](int p) {
+            for (int n = lane; n < g.N; n += 32) {
+                if (quad < groups_of(p)) copy4(span + (p & 1) * kMostX + n, g.scores.spans + (long long)n * g.groups + first_of(p) + quad);
+                else span[(p & 1) * kMostX + n] = 0u;
+            }
+        };
+        if (MODE == kStatsTop) fetch_spans(0);
         asm volatile("bar.sync 1, 128;" ::: "memory");         // these four warps
         for (int p = 0; p < passes && ok; ++p) {
             const int first = first_of(p);
             const bool mine = quad < groups_of(p);
-            for (int n = lane; MODE == kStats && mine && n < kMostX; n += 32) {        // read by the same lane
-                int t = n < g.N && g.scores.targets ? g.scores.targets[n] : -1;
-                if (t >= g.V) t = 0;
-                mark[n] = t < 0 ? -1 : t - (first + quad) * kGroup;
+            if (MODE == kStatsTop) {        // the pass's spans are here; its first entries and the next pass's spans on their way
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                for (int n = lane; n < g.N; n += 32) {
+                    const uint32_t m = span[(p & 1) * kMostX + n];
+                    if ((m & 0xffffu) < m >> 16) copy8(entry + n, g.scores.entries + (long long)n * g.scores.K + (m & 0xffffu));
+                }
+                if (p + 1 < passes) fetch_spans(p + 1);
             }
             float z[4][32];
 #pragma unroll
@@ -426,7 +453,7 @@ head_direct_kernel(const __grid_constant__ WMaps tmW, const __grid_constant__ CU
                 }
             }
 #pragma unroll 1
-            for (int q = 0; MODE == kStats && q * 32 < g.N; ++q) {
+            for (int q = 0; kSums && q * 32 < g.N; ++q) {
                 uint32_t zr[32];
                 tmem_ld32(tmem + 384u + lanes + q * 32u, zr);
                 tmem_ld_wait();
@@ -462,18 +489,46 @@ head_direct_kernel(const __grid_constant__ WMaps tmW, const __grid_constant__ CU
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = there ? ex2_fast(v[j]) : 0.f;
                 sum[n] += across<false>(v, lane);
-                // scores of the targets among the warp's rows of W, as the sums have them
-                for (unsigned left = __ballot_sync(0xffffffffu, mark[n] >= 0 && mark[n] < kGroup); left; left &= left - 1) {
-                    const int j = __ffs(left) - 1, at = __shfl_sync(0xffffffffu, mark[n], j);
-                    uint32_t zt;
-                    tmem_ld1(tmem + 384u + lanes + q * 32u + j, zt);
-                    tmem_ld_wait();
-                    if (lane == at) g.scores.zk[q * 32 + j] = __uint_as_float(zt) * row_f[q * 32 + j] * 32768.0f;
+            }
+            // the scores that the losses need, as the sums have them: few of a warp's groups of W have any
+            auto score = [&](int n, int at, long long to) {
+                uint32_t r;
+                tmem_ld1(tmem + 384u + lanes + n, r);
+                tmem_ld_wait();
+                if (lane == at) g.scores.zk[to] = __uint_as_float(r) * row_f[n] * 32768.0f;
+            };
+            if (MODE == kStats) {
+                const int v_first = (first + quad) * kGroup;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    for (unsigned left = __ballot_sync(0xffffffffu, target[q] >= v_first && target[q] < v_first + kGroup); left; left &= left - 1) {
+                        const int j = __ffs(left) - 1;
+                        score(q * 32 + j, __shfl_sync(0xffffffffu, target[q], j) - v_first, q * 32 + j);
+                    }
+            }
+            if (MODE == kStatsTop) {
+                asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 1
+                for (int q = 0; q * 32 < g.N; ++q) {        // a lane's row of x has its entries in turn, the next on its way meanwhile
+                    const int n = q * 32 + lane;
+                    const uint32_t m = n < g.N ? span[(p & 1) * kMostX + n] : 0u;
+                    int e = m & 0xffffu;
+                    const int e_end = m >> 16;
+                    int2 now = e < e_end ? entry[n] : make_int2(0, 0);
+                    for (unsigned left; (left = __ballot_sync(0xffffffffu, e < e_end)) != 0; ++e) {
+                        const int2 next = e + 1 < e_end ? g.scores.entries[(long long)n * g.scores.K + e + 1] : make_int2(0, 0);
+                        for (; left; left &= left - 1) {
+                            const int j = __ffs(left) - 1, col = __shfl_sync(0xffffffffu, now.x, j), place = __shfl_sync(0xffffffffu, now.y, j);
+                            score(q * 32 + j, col & (kGroup - 1), (long long)(q * 32 + j) * g.scores.K + place);
+                        }
+                        now = next;
+                    }
                 }
             }
         }
+        if (MODE == kStatsTop) asm volatile("cp.async.wait_all;" ::: "memory");       // where a wait ran out
         // a warp without rows of W has the sum zero
-        for (int n = lane; MODE == kStats && n < g.N; n += 32) g.stats[(long long)n * (4 * gridDim.x) + 4 * blockIdx.x + quad] = make_float2(ref[n], sum[n]);
+        for (int n = lane; kSums && n < g.N; n += 32) g.stats[(long long)n * (4 * gridDim.x) + 4 * blockIdx.x + quad] = make_float2(ref[n], sum[n]);
     }
 
     tc_fence_before();
@@ -573,7 +628,8 @@ cudaError_t launch_head_direct(const HeadArgs& h, const HalfMat& x, const float*
     Args g = args_for(h, h.V, err);
     g.rowf = rowf; g.stats = stats; g.scores = scores;
     const int grid = share_of(h.C, h.V).ctas;
-    return h.w_lo ? launch<true, kStats>(h, 0, h.V, x, grid, g, s) : launch<false, kStats>(h, 0, h.V, x, grid, g, s);
+    if (scores.targets) return h.w_lo ? launch<true, kStats>(h, 0, h.V, x, grid, g, s) : launch<false, kStats>(h, 0, h.V, x, grid, g, s);
+    return h.w_lo ? launch<true, kStatsTop>(h, 0, h.V, x, grid, g, s) : launch<false, kStatsTop>(h, 0, h.V, x, grid, g, s);
 }
 
 cudaError_t launch_head_direct_grad(const HeadArgs& h, const HalfMat& x, int v0, int cols, const float* rowf, const RowParams* rows, __half* u, int64_t ldu,

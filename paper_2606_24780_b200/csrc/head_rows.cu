@@ -61,7 +61,7 @@ struct Few {
     int rows, G;                            // rows of x of this launch; threads of a group, a multiple of 32
     int64_t row0;
     float2* stats;                          // forward: [N][gridDim.x]
-    float* zk;                              // forward: [N] scores of the targets
+    float* zk;                              // forward: [N] scores of the targets, or [V][kFewRows] all of them for a teacher
     const RowParams* params;                // backward
     const float* aim;                       // backward: [V][kFewRows] weights of a teacher's entries (nullable)
     float* dx_part;                         // backward: [gridDim.x][kFewRows][C]
@@ -192,6 +192,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(ROWS, THREADS)) head_few_ker
                     s = s * ex2_fast(m - m1) + ex2_fast(z2 - m1);
                     m = m1;
                     if (v == target) a.zk[a.row0 + my_n] = z2;
+                    if (!g.aim.targets && my_n < a.rows) a.zk[v * kFewRows + a.row0 + my_n] = z2;
                 }
             } else {
                 float u = 0.f;

@@ -295,9 +295,9 @@ __device__ __forceinline__ void run(const CUtensorMap* tmA, const CUtensorMap* t
                     entry.x = t;
                     e_end = t >= col0 && t < col0 + kCols ? 1 : 0;
                 } else {
-                    const uint16_t* f = g.scores.strip_first + (long long)row * (kParts * g.tiles_n + 1) + kParts * w.tn + part;
-                    e_at = f[0];
-                    e_end = f[1];
+                    const uint32_t span = g.scores.spans[(long long)row * (kParts * g.tiles_n) + kParts * w.tn + part];
+                    e_at = span & 0xffffu;
+                    e_end = span >> 16;
                     if (e_at < e_end) entry = g.scores.entries[(long long)row * g.scores.K + e_at];
                     if (e_at + 1 < e_end) next = g.scores.entries[(long long)row * g.scores.K + e_at + 1];
                 }

@@ -114,3 +114,32 @@ def test_the_loss_of_a_row_that_is_sure_of_its_target(N, C, V, kind, top, planes
     assert ((losses.double() - want[0]).abs() <= 2 * e * other + 2.0 ** -21 + 2.0 ** -22 * want[0]).all()
     assert abs(float(mean[0]) - float(want[2])) <= 2 * e * float(other.max()) + 2.0 ** -20 + 2.0 ** -22 * float(want[2])
     assert float((lse - want[1]).abs().max()) <= e + 2.0 ** -21 + 2.0 ** -23 * float(want[1].abs().max())
+
+
+@gpu
+@pytest.mark.parametrize("N,C,V,K", [(1, 768, 50257, 5), (4, 96, 9001, 40), (7, 2080, 999, 3), (9, 64, 40, 33), (40, 768, 19000, 8), (100, 64, 5001, 300), (128, 1056, 700, 64),
+                                     (77, 96, 40001, 1), (129, 768, 2000, 33), (1025, 96, 1500, 6)])
+@pytest.mark.parametrize("top", [9.0, 30.0, 70.0])
+@pytest.mark.parametrize("tau,whole", [(1.0, False), (2.0, True)])
+@pytest.mark.parametrize("planes", [False, True])
+def test_the_loss_of_a_student_as_sure_as_its_teacher(N, C, V, K, top, tau, whole, planes):
+    """An entry's part is p (l + d): l = log p is the logit's distance from the largest one, or from lse, d the distance of log sum exp from
+    the score.  Score errors e move d by 2 e (1 - q); it is rounded by 2^-21 and 2^-22 of itself.  l is off by two roundings of what it is
+    formed from, and by the exponentials in its sum; p by the same and 2^-22; the sum over the entries by 2^-20 of its parts."""
+    c = Case(N, C, V, K=K, tau=tau, planes=planes, seed=N + C, scale=0.5)
+    y = torch.arange(N, device=DEV) * 7 % V
+    e = sure(c, y, top, "aligned") / tau
+    c.ids[:, 0] = y.int()
+    c.top = c.top.clamp(-9.0, 9.0)
+    c.top[:, 0] = top
+    if whole:
+        c.top_lse = (torch.logsumexp(c.top.double() / tau, 1) + 0.01).float()
+    losses, lse, _ = c.forward()
+    want = c.want()
+    t = c.top.double() / tau
+    log_p = t - (c.top_lse.double() if whole else torch.logsumexp(t, 1))[:, None]
+    d = want[1][:, None] - (c.x.double() @ c.w.double().T / tau).gather(1, c.ids.long())
+    off = 2.0 ** -22 + 2.0 ** -23 * ((0.0 if whole else t.max(1, keepdim=True)[0] - t) + log_p.abs())
+    part = 2 * e * (1.0 - torch.exp(-d)) + 2.0 ** -21 + 2.0 ** -22 * d + off + (off + 2.0 ** -20) * (log_p + d).abs()
+    assert ((losses.double() - want[0]).abs() <= tau ** 2 * (torch.exp(log_p) * part).sum(1)).all()
+    assert float((lse - want[1]).abs().max()) <= e + 2.0 ** -21 + 2.0 ** -23 * float(want[1].abs().max())
