@@ -647,7 +647,10 @@ BT_API bt_status bt_op_dropout_bwd(const float* dy, int64_t n, double p, uint64_
  * The products run on the tensor cores on pairs of FP16 numbers: 22 bits of each value, scaled by powers of two so that the
  * largest one lies near FP16's largest.  Values below 2^-18 of the largest lose bits, at an absolute 2^-40 of it.  That is the
  * largest of x's or W's row in the forward, and in the backward that of x's row, of g_n x_n over all rows, and of all of W
- * (of fewer of its values up to 128 rows).
+ * (of fewer of its values up to 128 rows).  The backward holds q_nv - [v = y_n] in the same way, its largest being 1: q is
+ * off by up to 2^-40, so that its relative error is 2^-22 down to q = 2^-18, 2^-10 at 2^-30, and a q below 2^-41 counts as none.
+ * A row of dw whose word is that improbable in every row of x has the digits that this leaves, and what
+ * scales gradients by their own size (an optimiser's second moment) sees it; it is 2^-40 g_n x_n from the exact one.
  * Calls of up to four rows, and some of up to eight, run in plain FP32.  x of rows that count, and W, must be finite; a row whose scores are
  * beyond FP32 is not a number in losses and lse.
  * C a multiple of 32, at most 4096; V and N at most 2^24.  N = 0 is nothing to do (loss_mean and dw become 0).

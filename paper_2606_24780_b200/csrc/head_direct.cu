@@ -1,7 +1,7 @@
 // The head's products with W for some dozens of rows of x: W goes through the SMs as it is, and becomes FP16 pairs on the way.
 //
 //     kStats  z = x W^T, (maximum, sum of exponentials) over a CTA's share of the vocabulary; kStatsTop the same with a teacher's entries
-//     kGrad   the same z, u = 2^15 (q - [v = target]) as pairs
+//     kGrad   the same z, u = 2^15 (q - [v = target]) as pairs (q to an absolute 2^-40, see head_tc.cu)
 //     kDx     dx = u W, a range of the vocabulary each, joined by head_direct_dx_kernel
 //
 // With so few rows the weights' bytes bound the call, and a pass that makes pairs of W (read, written and read again) costs three times

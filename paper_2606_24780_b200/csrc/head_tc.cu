@@ -8,7 +8,9 @@
 //
 // Three products share one kernel; NT z = x W^T, NN dx = u W, TN dW = u^T y, with three epilogues:
 //     kStats  (maximum, sum of exponentials) of a strip, half a tile's columns, of a row
-//     kGrad   u = 2^15 (q - [v = target]) as pairs, the operand of the two others
+//     kGrad   u = 2^15 (q - [v = target]) as pairs, the operand of the two others.  One power of two for all of u: dx sums over its
+//             columns and dW over its rows, and 2^15 brings its largest, 1, to the top of FP16.  q is then held to an absolute
+//             2^-40; a power of two per column, which dW could take, needs the whole column before its first pair
 //     kOut    FP32, scaled by a power of two and by the row's own factor, over or onto what is there
 //
 // Warp 0 copies tiles (TMA), warp 1 issues MMAs, warps 4 to 11 take accumulators out of tensor memory.  Tiles are 256 rows on a

@@ -1,5 +1,6 @@
 """The losses at the language-model head, and distillation on logits, where they could give way: teachers whose numbers are not
-finite beside entries that are not there; rows of which most CTAs have nothing; rows that are sure of their target."""
+finite beside entries that are not there; rows of which most CTAs have nothing; rows that are sure of their target; words
+that are improbable everywhere."""
 import math
 
 import pytest
@@ -143,3 +144,33 @@ def test_the_loss_of_a_student_as_sure_as_its_teacher(N, C, V, K, top, tau, whol
     part = 2 * e * (1.0 - torch.exp(-d)) + 2.0 ** -21 + 2.0 ** -22 * d + off + (off + 2.0 ** -20) * (log_p + d).abs()
     assert ((losses.double() - want[0]).abs() <= tau ** 2 * (torch.exp(log_p) * part).sum(1)).all()
     assert float((lse - want[1]).abs().max()) <= e + 2.0 ** -21 + 2.0 ** -23 * float(want[1].abs().max())
+
+
+# ------------------------------------------------------------------------------- GPU: improbable words
+
+@gpu
+@pytest.mark.parametrize("N", [4, 8, 40, 128, 150, 600])
+@pytest.mark.parametrize("K", [0, 3])
+@pytest.mark.parametrize("planes", [False, True])
+def test_gradients_of_improbable_words_row_by_row(N, K, planes):
+    """Words that every row gives a probability of some 2^-20, 2^-30 and 2^-42.  q is held to 2^-40 from nine rows on, and to its own
+    size in plain FP32.  A score error e moves q by e q; weights, sums of up to 72 products cut by 2^-23 each and roundings
+    come to 2^-16 of the sum of the parts; g_n x_n is held to 2^-40 of the largest."""
+    C, V = 768, 900
+    c = Case(N, C, V, K=K, planes=planes, seed=N + K, scale=0.25)
+    c.x[:, 0] = 4.0
+    bits = torch.zeros(V, device=DEV)
+    bits[100:200], bits[200:300], bits[300:400] = 10.0, 20.0, 32.0            # beside the 2^-10 of one word of 900
+    c.w[:, 0] = -bits * math.log(2.0) / 4.0
+    (c.ids if K else c.targets).remainder_(100)                               # aims elsewhere
+    lse = c.forward()[1]
+    want = c.want(lse)[4]
+    _, dw, _ = c.backward(lse, dx=False)
+    q = torch.exp(c.x.double() @ c.w.double().T - lse.double()[:, None])
+    e = (72 * 2.0 ** -23 + 72 * 2.0 ** -24 + 2.0 ** -21) * float((c.x.abs() @ c.w.abs().T).max())
+    size = c.x.double().norm(dim=1) * c.inv
+    held = 0.0 if N <= 8 else 2.0 ** -40
+    bound = (size[:, None] * (held + (e + 2.0 ** -16) * q + 2.0 ** -40 * math.sqrt(C) * q)).sum(0)
+    part = slice(100, 400)                                                    # no aims: sums of parts of one sign in q
+    assert ((dw.double() - want).norm(dim=1)[part] <= bound[part]).all()
+    assert float(q[:, 100:200].max()) < 2.0 ** -17 and float(q[:, 300:400].max()) < 2.0 ** -39
