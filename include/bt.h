@@ -642,8 +642,8 @@ BT_API bt_status bt_op_dropout_bwd(const float* dy, int64_t n, double p, uint64_
  * The backward takes the forward's inputs and lse and overwrites (each nullable, but not all)
  *     dx [N, C] and / or dx_split [2][N][C]:  dx_n = g_n (sum_v q_nv W_v - W_{y_n}),   dw [V, C]:  dw_v = sum_n g_n (q_nv - [v = y_n]) x_n
  * with q_nv = exp(z_nv - lse_n) and g_n = inv_count w_n, in a fixed order (no atomics on floats: two runs give the
- * same bits).  piece: columns of the vocabulary worked on at a time, 0 for the library's choice; it sets the size of the
- * scratch and not the results' accuracy.
+ * same bits).  piece: columns of the vocabulary worked on at a time, rounded up to a multiple of 256; 0 for the library's choice (at most
+ * 2^27 / N, rounded up alike).  It sets the size of the scratch, of which a piece takes 4 N bytes per column, and not the results' accuracy.
  * The products run on the tensor cores on pairs of FP16 numbers: 22 bits of each value, scaled by powers of two so that the
  * largest one lies near FP16's largest.  Values below 2^-18 of the largest lose bits, at an absolute 2^-40 of it.  That is the
  * largest of x's or W's row in the forward, and in the backward that of x's row, of g_n x_n over all rows, and of all of W

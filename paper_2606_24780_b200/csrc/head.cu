@@ -64,8 +64,8 @@ bool few_rows(int64_t N, int C, int V, bool back) {
     return N <= kFewRows && (back ? N <= head_few_at_once(C) : N <= 4 || V < 148 * 128);
 }
 
-// Columns of one piece of the vocabulary, a multiple of 256: pieces of about the same size, of at most `piece` columns or
-// 512 MB of u.
+// Columns of one piece of the vocabulary, a multiple of 256: pieces of about the same size, of at most `piece` columns (or as many
+// as u has in 512 MB) rounded up to the next 256.  u takes 4 N bytes per column, so 1,024 N at least: 1 GB from 2^20 rows on.
 int piece_columns(int64_t N, int V, int piece) {
     int64_t most = piece > 0 ? piece : ((int64_t)1 << 27) / N;
     most = most < 256 ? 256 : (most + 255) / 256 * 256;

@@ -6,10 +6,28 @@ import math
 import pytest
 import torch
 
+from paper_2606_24780_b200 import binding as b
+
 from gpu_util import DEV
-from test_head_losses import Case, logits_case, logits_run, logits_want
+from test_head_losses import Case, lib, logits_case, logits_run, logits_want  # noqa: F401
 
 gpu = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------- CPU: scratch
+
+def test_a_piece_of_the_vocabulary_is_a_multiple_of_256_columns(lib):
+    """Sizes of the scratch for pieces asked for, and for the library's own."""
+    C, V = 32, 50000
+    for N in (9, 300, 1 << 20, 1 << 24):
+        size = lambda piece: b.bt_op_head_bwd_scratch_bytes(N, C, V, 0, piece)  # noqa: E731
+        rest = size(256) - 1024 * N
+        assert size(1) == size(255) == size(256) and size(257) == size(512)
+        for piece in (256, 512, 1000, 50000, 1 << 30):
+            pieces = -(-V // min(-(-piece // 256) * 256, 1 << 30))
+            assert size(piece) == rest + 4 * N * (-(-(-(-V // pieces)) // 256) * 256)
+        own = -(-max(256, (1 << 27) // N) // 256) * 256
+        assert size(0) == size(own) and size(0) - rest <= max(4 * N * 256, (1 << 29) + 4 * N * 256)
 
 
 # ------------------------------------------------------------------------------- GPU: teachers that are not finite
