@@ -651,6 +651,10 @@ BT_API bt_status bt_op_dropout_bwd(const float* dy, int64_t n, double p, uint64_
  * off by up to 2^-40, so that its relative error is 2^-22 down to q = 2^-18, 2^-10 at 2^-30, and a q below 2^-41 counts as none.
  * A row of dw whose word is that improbable in every row of x has the digits that this leaves, and what
  * scales gradients by their own size (an optimiser's second moment) sees it; it is 2^-40 g_n x_n from the exact one.
+ * The tensor cores cut their running sums toward zero; what random operands lose by that on the mean is put back.  Scores whose products
+ * have one sign stay short by up to 2^-18 of themselves (2^-21 up to 128 rows), those of one product alone are too large by up to 2^-19
+ * (2^-22).  lse is off by as much as the scores that make it up; a loss, formed beside the target's own score, by their difference times
+ * 1 - q, and is not below zero.
  * Calls of up to four rows, and some of up to eight, run in plain FP32.  x of rows that count, and W, must be finite; a row whose scores are
  * beyond FP32 is not a number in losses and lse.
  * C a multiple of 32, at most 4096; V and N at most 2^24.  N = 0 is nothing to do (loss_mean and dw become 0).

@@ -84,7 +84,9 @@ __device__ __forceinline__ void to_pairs(float a, float b, uint32_t& hi, uint32_
 // The tensor core cuts its running sum to FP32 with every instruction, always toward zero.  A sum that grows to its final size
 // over n instructions comes out short by some n / 2 times 2^-24 of it times the mean of the cut: measured, 0.54 for
 // random operands, 0.6 for aligned ones, 1.2 where all products are positive.  n is 3 per 16 of the contraction index between
-// two sums in registers; the products are made longer by 0.56.
+// two sums in registers; the products are made longer by 0.56.  That is right on the mean of random operands, and not for others: sums
+// of products of one sign stay short by 1.0e-6 to 2.0e-6 of themselves after 72 instructions (3e-7 after 12), and a score of one product
+// alone, of which nothing is cut, comes out 1.2e-6 (2e-7) too large.  lse has that error; a loss is formed beside the score itself.
 inline float head_growth(double n) { return (float)(1.0 + 0.5 * 0.56 / (1 << 24) * n); }
 
 // Statistics of up to 128 rows straight from W (head_direct.cu): [N][head_direct_strips(C, V)].  A teacher's entries are sorted into

@@ -192,3 +192,61 @@ def test_gradients_of_improbable_words_row_by_row(N, K, planes):
     part = slice(100, 400)                                                    # no aims: sums of parts of one sign in q
     assert ((dw.double() - want).norm(dim=1)[part] <= bound[part]).all()
     assert float(q[:, 100:200].max()) < 2.0 ** -17 and float(q[:, 300:400].max()) < 2.0 ** -39
+
+
+# ------------------------------------------------------------------------------- GPU: what the tensor core cuts
+
+CUT = 0.28 * 2.0 ** -24         # what is put back per instruction
+
+
+def instructions(N):
+    """Between two sums in registers, C a multiple of 384: three for 16 of the contraction index, of 64 or of 384."""
+    return 12 if N <= 128 else 72
+
+
+@gpu
+@pytest.mark.parametrize("N", [128, 2000])
+@pytest.mark.parametrize("planes", [False, True])
+def test_what_is_put_back_for_cut_sums_is_their_mean(N, planes):
+    """Random operands, for which it is measured: within a quarter of it on the mean over all rows, and the 2^-23 by which constants
+    (log2 e, ln 2, their product with what is put back) are rounded; without it, or with twice as much, the test fails.  lse is the
+    largest score, of some 50, and little more; single scores are off by the products' bound."""
+    c = Case(N, 1152, 3000, planes=planes, seed=N, scale=16.0)
+    lse, want = c.forward()[1], c.want()[1]
+    off = (lse.double() - want) / want
+    assert abs(float(off.mean())) < CUT * instructions(N) / 4 + 2.0 ** -23
+    bound = (instructions(N) * 2.0 ** -23 + CUT * instructions(N) + 2.0 ** -21) * float((c.x.abs() @ c.w.abs().T).max())
+    assert float((lse - want).abs().max()) < bound
+
+
+@gpu
+@pytest.mark.parametrize("N", [128, 2000])
+@pytest.mark.parametrize("planes", [False, True])
+def test_scores_of_one_product_get_what_is_put_back_and_no_more(N, planes):
+    """One number in every row of x and of W, both FP16 ones: nothing is cut, and lse is too large by what is put back; constants are
+    rounded by 2^-23, and a score, a sum and a product by 2^-24 each."""
+    c = Case(N, 1152, 1500, planes=planes, seed=N)
+    c.x.zero_()
+    c.w.zero_()
+    c.x[:, 700] = 1.5
+    c.w[::3, 700] = 20.0
+    lse, want = c.forward()[1], c.want()[1]
+    off = (lse.double() - want) / 30.0                            # the sum's logarithm, 6.2, has no part in it
+    own = 5 * 2.0 ** -24 * 36.2 / 30.0
+    assert (off > CUT * instructions(N) - own).all() and (off < CUT * instructions(N) + own).all()
+
+
+@gpu
+@pytest.mark.parametrize("N", [128, 2000])
+@pytest.mark.parametrize("C", [384, 1152, 3456])
+def test_sums_of_products_of_one_sign(N, C):
+    """A sum that grows evenly over n instructions, cut by up to 2^-23 of what it is at each: by 2^-24 n at most over all, less what is put
+    back.  Both bounds with the operands' 2^-22 and lse's own 2^-22."""
+    c = Case(N, C, 900, seed=C)
+    c.x, c.w = c.x.abs() + 0.5, c.w.abs() * 0.1
+    c.w[::3] = c.w[::3].sign().abs() + 0.5 * c.w[::3]
+    c.w *= 40.0 / float((c.x @ c.w.T).max())
+    lse, want = c.forward()[1], c.want()[1]
+    off = (lse.double() - want) / want
+    n = instructions(N)
+    assert (off > -(2.0 ** -24 - CUT) * n - 2.0 ** -21).all() and (off < CUT * n + 2.0 ** -21).all()
