@@ -706,7 +706,8 @@ BT_API bt_status bt_op_head_distill_bwd(const float* x, const float* x_split, co
 /* The same loss on the student's logits [N, ld], of which the first V columns count (ld a multiple of 4, at least V):
  * losses, loss_mean (nullable) and the gradient inv_count w_n d losses_n / d logits_nv, raw (dlogits [N, ld]) and / or as
  * planes (dlogits_split [2][N][ld]), both optional; columns from V on become 0.  The gradient may be written over the
- * logits, dlogits or the hi plane of dlogits_split being the same array.  N at most 2^24, V and ld at most 2^30. */
+ * logits, dlogits or the hi plane of dlogits_split being the same array; no other output may lie over an input, nor dlogits over
+ * its own planes.  N at most 2^24, V and ld at most 2^30. */
 BT_API bt_status bt_op_softmax_distill(const float* logits, const bt_distill* teacher, const float* row_w, int64_t N,
                                        int32_t V, int32_t ld, float inv_count, float* losses, float* loss_mean,
                                        float* dlogits, float* dlogits_split, int32_t* d_bad, void* stream);

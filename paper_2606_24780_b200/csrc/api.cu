@@ -1842,6 +1842,8 @@ extern "C" bt_status bt_op_softmax_distill(const float* logits, const bt_distill
     for (const float* out : {(const float*)losses, (const float*)loss_mean, (const float*)dlogits, (const float*)dlogits_split})
         if (out && (out == g.aim.row_w || out == g.aim.logits || out == g.aim.lse))
             return fail(BT_ERR_INVALID_ARG, "softmax_distill: an output over an input");
+    if (losses == logits || loss_mean == logits) return fail(BT_ERR_INVALID_ARG, "softmax_distill: losses over the logits");
+    if (dlogits && (dlogits == dlogits_split || dlogits == lo)) return fail(BT_ERR_INVALID_ARG, "softmax_distill: dlogits over its own planes");
     g.z = logits;
     g.N = N; g.V = V; g.ld = ld;
     g.losses = losses; g.loss_mean = loss_mean; g.bad = d_bad;

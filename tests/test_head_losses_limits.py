@@ -9,7 +9,7 @@ import torch
 from paper_2606_24780_b200 import binding as b
 
 from gpu_util import DEV
-from test_head_losses import Case, lib, logits_case, logits_run, logits_want  # noqa: F401
+from test_head_losses import Case, lib, logits_case, logits_run, logits_want, refused  # noqa: F401
 
 gpu = pytest.mark.gpu
 
@@ -28,6 +28,17 @@ def test_a_piece_of_the_vocabulary_is_a_multiple_of_256_columns(lib):
             assert size(piece) == rest + 4 * N * (-(-(-(-V // pieces)) // 256) * 256)
         own = -(-max(256, (1 << 27) // N) // 256) * 256
         assert size(0) == size(own) and size(0) - rest <= max(4 * N * 256, (1 << 29) + 4 * N * 256)
+
+
+def test_losses_over_the_logits_and_dlogits_over_its_planes_are_refused(lib):
+    P, N, ld = 0x10000, 4, 100
+    z, lo = 5 * P, 4 * N * ld
+
+    def call(losses=2 * P, mean=None, dz=None, planes=None):
+        b.bt_op_softmax_distill(z, b.bt_distill(4, 1.0, P, P, None), None, N, ld, ld, 1.0, losses, mean, dz, planes, None, 0)
+
+    for bad in (dict(losses=z), dict(mean=z), dict(dz=6 * P, planes=6 * P), dict(dz=6 * P + lo, planes=6 * P), dict(dz=z, planes=z)):
+        refused(lambda: call(**bad))
 
 
 # ------------------------------------------------------------------------------- GPU: teachers that are not finite
