@@ -4,10 +4,10 @@
 //     loss = tau^2 sum_k p_k (log p_k - log q_{i_k}),   dz_v = g tau (S q_v - sum_{k: i_k = v} p_k),   S = sum_k p_k
 //
 // A CTA, or a cluster of up to eight with a slice of the columns each, walks over a row twice: once for its maximum and sum,
-// once for the gradient, and the second walk reads what the first has left in L2.  Holding the row in registers instead
-// (one read, the next row on its way into shared memory) leaves no room for a second and third CTA per SM, whose loads
-// run while this one reduces: 867 us against 681 at 8,192 x 50,257, where the copies alone take 502 (now 665, 5.0 TB/s; what is left is
-// the latency of two walks).  The entries touch few columns: every
+// once for the gradient, and the second walk reads what the first has left in L2, three quarters of it (1,184 rows: 300 MB read for 238).
+// Holding the row in registers instead (one read, the next row on its way into shared memory) leaves no room for a second and third
+// CTA per SM, whose loads run while this one reduces: 867 us against 681 at 8,192 x 50,257 when it was tried, where the copies
+// alone take 502 (681 to 702 by the run, 4.7 TB/s; what is left is the latency of two walks).  The entries touch few columns: every
 // thread stores its columns of g tau S q, and behind a barrier the threads that own an entry store the columns of the aim
 // once more, from the logits that they have read before.
 #include <cooperative_groups.h>

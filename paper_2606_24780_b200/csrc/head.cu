@@ -169,8 +169,8 @@ __device__ __forceinline__ RowSum row_sum(const float2* st, int strips, float* s
     return RowSum{top, WARPS == 1 ? warp_sum(t) : block_all<32 * WARPS>(t, sm, SumOp())};
 }
 
-// The loss against targets, a row per warp, or per CTA where there are few rows of many strips (100 rows of 592: 5 us less; 8,192
-// rows take 88 us so, most of it barriers, and 36 with a warp each).
+// The loss against targets, a row per warp, or per CTA where there are few rows of many strips (100 rows of 592: 7.4 us, by a
+// warp each 9.4; 8,192 rows of 394 37 us so, most of it barriers, and 19 by a warp each).
 template <int WARPS>
 __global__ void __launch_bounds__(kFinishThreads) head_finish_target_kernel(const HeadArgs g, const float2* __restrict__ stats, int strips,
                                                                             const float* __restrict__ zk, HeadHeader* head) {

@@ -15,7 +15,7 @@
 //     warps 4-7, 8-11     pairs of even and odd blocks
 //     warps 12-15         sums, then the mode's last step
 //
-// W 50,257 x 1,024: statistics of 9 rows take 49 us, of 100 62 (all launches; 4.2 and 3.3 TB/s of W), gradients 156 and 196.  Few rows are bound by the
+// W 50,257 x 1,024: statistics of 9 rows take 56 us, of 100 68 (all launches, L2 cold; 3.7 and 3.0 TB/s of W), gradients 155 and 188.  Few rows are bound by the
 // copies; with more, x comes to every SM as often as W and from L2, and a block's chain of copy, pairs, product and sum shows.
 //
 // W's ring has an even number of stages: a stage then always belongs to the same warps.  (Two groups that took turns on one
