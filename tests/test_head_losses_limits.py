@@ -9,7 +9,7 @@ import torch
 from paper_2606_24780_b200 import binding as b
 
 from gpu_util import DEV
-from test_head_losses import Case, lib, logits_case, logits_run, logits_want, refused  # noqa: F401
+from test_head_losses import TOL, Case, lib, logits_case, logits_run, logits_want, refused  # noqa: F401
 
 gpu = pytest.mark.gpu
 
@@ -261,3 +261,25 @@ def test_sums_of_products_of_one_sign(N, C):
     off = (lse.double() - want) / want
     n = instructions(N)
     assert (off > -(2.0 ** -24 - CUT) * n - 2.0 ** -21).all() and (off < CUT * n + 2.0 ** -21).all()
+
+
+@gpu
+@pytest.mark.parametrize("N,C,V,K", [(3, 256, 30000, 20), (100, 256, 50257, 64), (128, 128, 90000, 200), (300, 128, 20000, 50)])
+def test_teachers_in_turn_on_one_scratch(N, C, V, K):
+    """Calls right behind one another, each with entries, spans and scores in the places of the last one's: every value of every call."""
+    cases = [Case(N, C, V, K=K, tau=2.0, seed=s) for s in (1, 2)]
+    for c in cases:
+        c.x, c.w = cases[0].x, cases[0].w
+    plain = [c.forward() for c in cases]
+    want = cases[1].want()
+    assert float((plain[1][0] - want[0]).abs().max()) < TOL * 4 * max(1.0, float(want[1].abs().max()))
+    need = b.bt_op_head_fwd_scratch_bytes(N, C, V, K)
+    work = torch.empty(need, dtype=torch.uint8, device=DEV)
+    outs = [[torch.full((n,), math.nan, device=DEV) for n in (N, N, 1)] for _ in range(12)]
+    aims = [c.aim() for c in cases]
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        b.bt_op_head_distill_fwd(cases[0].x, None, cases[0].w, None, aims[i % 2], None, N, C, V, cases[0].inv, *out, work, need)
+    b.bt_op_head_check(work)
+    for i, out in enumerate(outs):
+        assert all(torch.equal(p, q) for p, q in zip(out, plain[i % 2]))
